@@ -202,6 +202,106 @@ size_t corr_full_volume_bytes(int B, int H, int W, int L);
  */
 size_t corr_workspace_bytes(corr_mode mode, int B, int H, int W, int D, int L, int r);
 
+/*
+ * ---- Rows -------------------------------------------------------------------------------------------
+ * What a flow network does with the lookup's output between two lookups, row by row (a row is one pixel's
+ * channels; CORR_OUT_NHWC writes the lookup's taps as such rows): products with weights, and the norms, gates
+ * and residuals around a block of them.  The paper leaves these to the network; the operations are defined here.
+ *
+ * Matrices are device arrays of `corr_dtype` with contiguous rows; a `_stride` is the number of elements from one
+ * row to the next (at least the row's length).  Vectors (biases, scales, weights of norms, and their gradients)
+ * are fp32 whatever the matrices are.  Sums, statistics and everything between load and store are fp32; a result is rounded
+ * once, to nearest even, when it is stored.  Calls only enqueue kernels on `stream`, allocate nothing and keep
+ * nothing; the caller's `workspace` (16-byte aligned, contents ignored, scratch on return) must not be shared by
+ * calls that overlap, graph replays among them.  Every result has the same bits on every call.  Outputs may not
+ * overlap inputs unless stated.  Zero rows are accepted (sums over rows are then zero); other sizes are positive.
+ */
+typedef enum { CORR_TYPE_F32 = 0, CORR_TYPE_BF16 = 1, CORR_TYPE_F16 = 2 } corr_dtype;
+typedef enum {
+    CORR_ACT_NONE = 0,
+    CORR_ACT_RELU = 1,
+    CORR_ACT_GELU = 2,        /* z/2 (1 + erf(z / sqrt 2)) */
+    CORR_ACT_GELU_TANH = 3,   /* z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) */
+    CORR_ACT_SILU = 4,        /* z / (1 + e^-z) */
+    CORR_ACT_SIGMOID = 5      /* 1 / (1 + e^-z) */
+} corr_activation;
+typedef enum {
+    CORR_NORM_NONE = 0,
+    CORR_NORM_RMS = 1,        /* v / sqrt(mean v^2 + eps) */
+    CORR_NORM_LAYER = 2       /* (v - mean v) / sqrt(mean (v - mean v)^2 + eps) */
+} corr_norm;
+
+/*
+ * z = x w^T + bias,  y = act(z) + residual.
+ *   x        : [M, K] rows, x_stride;  w : [N, K], dense.  16-bit matrices start on a 4-byte border.
+ *   bias     : fp32 [N] or NULL.
+ *   residual : [M, N] rows, residual_stride, or NULL; may be y itself (same pointer and stride).
+ *   preact   : NULL, or [M, N] dense: receives z, which corr_linear_backward reads.
+ *   y        : [M, N] rows, y_stride.
+ * fp32 products carry fp32's precision (each operand as three bf16 parts, six partial products).
+ * Limits: M <= 2^30, N, K and strides <= 2^21, M*N and M*K <= 2^36; beyond: CORR_ERR_UNSUPPORTED.
+ */
+size_t corr_linear_workspace_bytes(corr_dtype type, int64_t M, int64_t N, int64_t K, int64_t x_stride);
+corr_status corr_linear(corr_dtype type, corr_activation act, const void* x, int64_t x_stride, const void* w, const float* bias,
+                        const void* residual, int64_t residual_stride, void* preact, void* y, int64_t y_stride,
+                        int64_t M, int64_t N, int64_t K, void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * With dz = d_y act'(preact):  d_x = dz w,  d_w = dz^T x,  d_bias = sum over rows of dz.  The residual's gradient is d_y itself.
+ *   preact : [M, N] dense, as corr_linear left it; not read (may be NULL) for CORR_ACT_NONE.  relu's slope at 0 is 0.
+ *   d_y    : [M, N] rows, d_y_stride.
+ *   d_x    : [M, K] dense or NULL;  d_w : [N, K] dense or NULL;  d_bias : fp32 [N] or NULL.
+ * For 16-bit types and an activation, dz is rounded to the type once before the two products (the matrix cores'
+ * operand); d_bias adds the unrounded values.
+ */
+size_t corr_linear_backward_workspace_bytes(corr_dtype type, corr_activation act, int64_t M, int64_t N, int64_t K,
+                                            int64_t x_stride, int64_t d_y_stride);
+corr_status corr_linear_backward(corr_dtype type, corr_activation act, const void* x, int64_t x_stride, const void* w,
+                                 const void* preact, const void* d_y, int64_t d_y_stride, void* d_x, void* d_w, float* d_bias,
+                                 int64_t M, int64_t N, int64_t K, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The end of one residual block and the beginning of the next:
+ *   p = post(y) * post_weight + post_bias           the norm after the block whose output is y
+ *   t = h_scale * h + scale * gate_act(gate) * p    gate, scale of the channels, residual
+ *   h_out = t,  n_out = pre(t) * pre_weight + pre_bias     the norm before the next block
+ * n_out is made from t before t is rounded.  Vectors that are NULL are ones (weights, scale) and zeros (biases).
+ *   y    : NULL: no block; then t = h, gate, scale and h_out are NULL, post is CORR_NORM_NONE and h_scale 1.
+ *   gate : NULL: no gate.
+ *   h_out: [rows, cols] dense, of stream_type, or NULL; may be h (if h_stride == cols).
+ *   n_out: [rows, cols] dense, of type; NULL exactly if pre is CORR_NORM_NONE.
+ * stream_type equals type, or is CORR_TYPE_F32 beside a 16-bit type.  A norm of CORR_NORM_NONE has no vectors.
+ * eps > 0 serves both norms.  Limits: cols <= 16384 and strides <= 2^30, rows <= 2^30; beyond: CORR_ERR_UNSUPPORTED.
+ */
+typedef struct {
+    corr_dtype stream_type;              /* h, h_out, d_h_out, d_h */
+    corr_dtype type;                     /* y, gate, n_out, d_n_out, d_y, d_gate */
+    int64_t rows, cols;
+    const void* h; int64_t h_stride;
+    const void* y; int64_t y_stride;
+    const void* gate; int64_t gate_stride;
+    corr_activation gate_act;
+    const float* scale;
+    float h_scale;
+    corr_norm post;
+    const float* post_weight; const float* post_bias;
+    corr_norm pre;
+    const float* pre_weight; const float* pre_bias;
+    float eps;
+} corr_residual_norm_args;
+corr_status corr_residual_norm(const corr_residual_norm_args* args, void* h_out, void* n_out, void* stream);
+/*
+ * Gradients at the forward call's own arguments (its inputs are read again; it saves nothing).
+ *   d_h_out, d_n_out : [rows, cols] dense, or NULL for zero (d_n_out is NULL where pre is CORR_NORM_NONE; not both).
+ *   d_h, d_y, d_gate : [rows, cols] dense, or NULL if not wanted.
+ *   d_scale ... d_pre_bias : fp32 [cols], or NULL if not wanted; only beside the vector of the same name.
+ * No output may overlap an input.
+ */
+size_t corr_residual_norm_backward_workspace_bytes(int64_t rows, int64_t cols);
+corr_status corr_residual_norm_backward(const corr_residual_norm_args* args, const void* d_h_out, const void* d_n_out,
+                                        void* d_h, void* d_y, void* d_gate, float* d_scale, float* d_post_weight,
+                                        float* d_post_bias, float* d_pre_weight, float* d_pre_bias,
+                                        void* workspace, size_t workspace_bytes, void* stream);
+
 const char* corr_status_string(corr_status s);
 
 #ifdef __cplusplus

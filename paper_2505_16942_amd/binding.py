@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -22,6 +23,9 @@ CORR_MODE_BLOCK, CORR_MODE_ONDEMAND, CORR_MODE_FULLVOLUME = 0, 1, 2
 CORR_PREC_BF16X3, CORR_PREC_BF16 = 0, 1
 CORR_OUT_NCHW, CORR_OUT_NHWC = 0, 1
 CORR_REP_SPLIT, CORR_REP_F32, CORR_REP_BF16 = 1, 2, 4
+CORR_TYPE_F32, CORR_TYPE_BF16, CORR_TYPE_F16 = 0, 1, 2
+CORR_ACT_NONE, CORR_ACT_RELU, CORR_ACT_GELU, CORR_ACT_GELU_TANH, CORR_ACT_SILU, CORR_ACT_SIGMOID = 0, 1, 2, 3, 4, 5
+CORR_NORM_NONE, CORR_NORM_RMS, CORR_NORM_LAYER = 0, 1, 2
 
 # the method's boundary (include/corr.h)
 EXPORTS = [
@@ -29,6 +33,8 @@ EXPORTS = [
     "corr_sample", "corr_sample_mode", "corr_sample_layout", "corr_sample_static",
     "corr_full_volume_bytes", "corr_workspace_bytes", "corr_status_string",
     "corr_backward_workspace_bytes", "corr_sample_backward",
+    "corr_linear_workspace_bytes", "corr_linear", "corr_linear_backward_workspace_bytes", "corr_linear_backward",
+    "corr_residual_norm", "corr_residual_norm_backward_workspace_bytes", "corr_residual_norm_backward",
 ]
 # measurement and test hooks (include/corr_bench.h)
 BENCH_EXPORTS = [
@@ -56,6 +62,15 @@ class BlockStats(ctypes.Structure):
 class Profile(ctypes.Structure):
     _fields_ = [("lookups", ctypes.c_int64), ("dropped", ctypes.c_int64),
                 ("binning_ms", ctypes.c_double), ("block_ms", ctypes.c_double)]
+
+
+class ResidualNormArgs(ctypes.Structure):
+    _fields_ = [("stream_type", ctypes.c_int), ("type", ctypes.c_int), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("h", ctypes.c_void_p), ("h_stride", ctypes.c_int64), ("y", ctypes.c_void_p), ("y_stride", ctypes.c_int64),
+                ("gate", ctypes.c_void_p), ("gate_stride", ctypes.c_int64), ("gate_act", ctypes.c_int),
+                ("scale", ctypes.c_void_p), ("h_scale", ctypes.c_float),
+                ("post", ctypes.c_int), ("post_weight", ctypes.c_void_p), ("post_bias", ctypes.c_void_p),
+                ("pre", ctypes.c_int), ("pre_weight", ctypes.c_void_p), ("pre_bias", ctypes.c_void_p), ("eps", ctypes.c_float)]
 
 
 _lib = None
@@ -90,6 +105,22 @@ def load_library():
     lib.corr_backward_workspace_bytes.restype = sz
     lib.corr_sample_backward.argtypes = [vp, vp, vp, ci, ci, ci, ci, ci, ci, vp, vp, vp, sz, vp]
     lib.corr_sample_backward.restype = ci
+    i64 = ctypes.c_int64
+    lib.corr_linear_workspace_bytes.argtypes = [ci, i64, i64, i64, i64]
+    lib.corr_linear_workspace_bytes.restype = sz
+    lib.corr_linear.argtypes = [ci, ci, vp, i64, vp, vp, vp, i64, vp, vp, i64, i64, i64, i64, vp, sz, vp]
+    lib.corr_linear.restype = ci
+    lib.corr_linear_backward_workspace_bytes.argtypes = [ci, ci, i64, i64, i64, i64, i64]
+    lib.corr_linear_backward_workspace_bytes.restype = sz
+    lib.corr_linear_backward.argtypes = [ci, ci, vp, i64, vp, vp, vp, i64, vp, vp, vp, i64, i64, i64, vp, sz, vp]
+    lib.corr_linear_backward.restype = ci
+    norm_args = ctypes.POINTER(ResidualNormArgs)
+    lib.corr_residual_norm.argtypes = [norm_args, vp, vp, vp]
+    lib.corr_residual_norm.restype = ci
+    lib.corr_residual_norm_backward_workspace_bytes.argtypes = [i64, i64]
+    lib.corr_residual_norm_backward_workspace_bytes.restype = sz
+    lib.corr_residual_norm_backward.argtypes = [norm_args] + [vp] * 11 + [sz, vp]
+    lib.corr_residual_norm_backward.restype = ci
     lib.corr_full_volume_bytes.argtypes = [ci, ci, ci, ci]
     lib.corr_full_volume_bytes.restype = sz
     lib.corr_workspace_bytes.argtypes = [ci, ci, ci, ci, ci, ci, ci]
@@ -301,6 +332,275 @@ def corr_sample_backward(pyramid: Pyramid, coords: torch.Tensor, d_out: torch.Te
     if st != CORR_OK:
         raise CorrError(st, "corr_sample_backward")
     return outs[0], outs[1]
+
+
+# ---- rows: products with weights, norms around a block ------------------------------------------------------------
+
+_TYPES = {torch.float32: CORR_TYPE_F32, torch.bfloat16: CORR_TYPE_BF16, torch.float16: CORR_TYPE_F16}
+
+
+def _on_device(t, name: str, device=None) -> None:
+    """Kernels go to the current device's current stream: a tensor elsewhere is refused."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        raise TypeError("%s must be a tensor on the GPU" % name)
+    if device is None:
+        if t.device.index != torch.cuda.current_device():
+            raise ValueError("%s is on %s, which is not the current device" % (name, t.device))
+    elif t.device != device:
+        raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
+
+
+def _rows(t: torch.Tensor, name: str):
+    """(rows, length, stride) of a tensor [..., length] whose rows are contiguous and evenly spaced."""
+    if t.dim() == 0:
+        raise ValueError("%s must have at least one dimension" % name)
+    cols = t.shape[-1]
+    if t.is_contiguous():
+        return t.numel() // max(cols, 1), cols, cols
+    if cols > 1 and t.stride(-1) != 1:
+        raise ValueError("%s must have contiguous rows" % name)
+    rows, stride = 1, 0
+    for size, step in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if size == 1:
+            continue
+        if rows == 1:
+            stride = step
+        elif step != rows * stride:
+            raise ValueError("%s must have evenly spaced rows" % name)
+        rows *= size
+    return rows, cols, stride if rows > 1 else cols
+
+
+def _pointer(t) -> int:
+    """An empty tensor has no address, and NULL means absent: any other address does, nothing is read there."""
+    return t.data_ptr() or 256
+
+
+def _matrix(t, name: str, dtype, device, rows: int, cols: int):
+    """(pointer, stride) of an optional matrix of known size and type."""
+    if t is None:
+        return None, 0
+    _on_device(t, name, device)
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s" % (name, dtype))
+    r, c, stride = _rows(t, name)
+    if r != rows or c != cols:
+        raise ValueError("%s must have %d rows of %d" % (name, rows, cols))
+    return _pointer(t), stride
+
+
+def _dense(t, name: str, dtype, device, shape):
+    """Pointer of an optional contiguous tensor of known size and type."""
+    if t is None:
+        return None
+    _on_device(t, name, device)
+    if t.dtype != dtype or not t.is_contiguous():
+        raise TypeError("%s must be contiguous and %s" % (name, dtype))
+    if t.shape != shape:
+        raise ValueError("%s must be %s" % (name, list(shape)))
+    return _pointer(t)
+
+
+def _workspace(workspace, need: int, device):
+    """(tensor that holds it, pointer, bytes); allocated on the current stream if None."""
+    if workspace is None:
+        if not need:
+            return None, None, 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        return workspace, workspace.data_ptr(), need
+    _on_device(workspace, "workspace", device)
+    size = workspace.numel() * workspace.element_size()
+    if not workspace.is_contiguous() or size < need:
+        raise ValueError("workspace must be a contiguous device buffer of at least %d bytes" % need)
+    return workspace, workspace.data_ptr(), size
+
+
+def _type_of(t, name: str) -> int:
+    code = _TYPES.get(t.dtype)
+    if code is None:
+        raise TypeError("%s must be float32, bfloat16 or float16" % name)
+    return code
+
+
+def corr_linear_workspace_bytes(dtype: torch.dtype, M: int, N: int, K: int, x_stride: int | None = None) -> int:
+    return int(load_library().corr_linear_workspace_bytes(_TYPES[dtype], M, N, K, K if x_stride is None else x_stride))
+
+
+def corr_linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, act: int = CORR_ACT_NONE,
+                residual: torch.Tensor | None = None, out: torch.Tensor | None = None, preact: torch.Tensor | None = None,
+                workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """act(x w^T + bias) + residual.  x: [..., K] with contiguous, evenly spaced rows (corr_sample's CORR_OUT_NHWC output is
+    one); w: [N, K]; both float32, bfloat16 or float16.  bias: float32 [N].  residual, out: [..., N] of x's type; out may be
+    residual.  preact: a contiguous [..., N] that receives the sum before the activation (corr_linear_backward reads it)."""
+    lib = load_library()
+    _on_device(x, "x")
+    code, dtype, device = _type_of(x, "x"), x.dtype, x.device
+    M, K, xs = _rows(x, "x")
+    if not isinstance(w, torch.Tensor) or w.dim() != 2 or w.shape[1] != K:
+        raise ValueError("w must be [N, %d]" % K)
+    N = w.shape[0]
+    shape = x.shape[:-1] + (N,)
+    pw = _dense(w, "w", dtype, device, w.shape)
+    pb = _dense(bias, "bias", torch.float32, device, (N,))
+    pr, rs = _matrix(residual, "residual", dtype, device, M, N)
+    pz = _dense(preact, "preact", dtype, device, shape)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=device)
+        po, os_ = _pointer(out), N
+    else:
+        if out.shape != shape:
+            raise ValueError("out must be %s" % list(shape))
+        po, os_ = _matrix(out, "out", dtype, device, M, N)
+    held, ws, size = _workspace(workspace, lib.corr_linear_workspace_bytes(code, M, N, K, xs), device)
+    st = lib.corr_linear(code, act, _pointer(x), xs, pw, pb, pr, rs, pz, po, os_, M, N, K, ws, size, _stream())
+    if st != CORR_OK:
+        raise CorrError(st, "corr_linear")
+    return out
+
+
+def corr_linear_backward_workspace_bytes(dtype: torch.dtype, act: int, M: int, N: int, K: int, x_stride: int | None = None,
+                                         d_out_stride: int | None = None) -> int:
+    return int(load_library().corr_linear_backward_workspace_bytes(_TYPES[dtype], act, M, N, K, K if x_stride is None else x_stride,
+                                                                   N if d_out_stride is None else d_out_stride))
+
+
+def corr_linear_backward(x: torch.Tensor, w: torch.Tensor, d_out: torch.Tensor, preact: torch.Tensor | None = None,
+                         act: int = CORR_ACT_NONE, want_x: bool = True, want_w: bool = True, want_bias: bool = True,
+                         d_x: torch.Tensor | None = None, d_w: torch.Tensor | None = None, d_bias: torch.Tensor | None = None,
+                         workspace: torch.Tensor | None = None):
+    """(d_x, d_w, d_bias) of corr_linear, None where not wanted: x's type for the first two, float32 for the bias.  d_out: the
+    gradient of its result, which is the residual's too; preact: what corr_linear stored (needed for an activation)."""
+    lib = load_library()
+    _on_device(x, "x")
+    code, dtype, device = _type_of(x, "x"), x.dtype, x.device
+    M, K, xs = _rows(x, "x")
+    if not isinstance(w, torch.Tensor) or w.dim() != 2 or w.shape[1] != K:
+        raise ValueError("w must be [N, %d]" % K)
+    N = w.shape[0]
+    pw = _dense(w, "w", dtype, device, w.shape)
+    if d_out is None:
+        raise TypeError("d_out must be a tensor on the GPU")
+    pg, gs = _matrix(d_out, "d_out", dtype, device, M, N)
+    if act != CORR_ACT_NONE and preact is None:
+        raise ValueError("the gradient of an activation needs preact")
+    pz = _dense(preact, "preact", dtype, device, x.shape[:-1] + (N,)) if act != CORR_ACT_NONE else None
+
+    def output(t, wanted, name, kind, shape):
+        if not wanted:
+            return None, None
+        if t is None:
+            t = torch.empty(shape, dtype=kind, device=device)
+        return t, _dense(t, name, kind, device, shape)
+    d_x, px = output(d_x, want_x, "d_x", dtype, x.shape)
+    d_w, pdw = output(d_w, want_w, "d_w", dtype, w.shape)
+    d_bias, pdb = output(d_bias, want_bias, "d_bias", torch.float32, (N,))
+    held, ws, size = _workspace(workspace, lib.corr_linear_backward_workspace_bytes(code, act, M, N, K, xs, gs), device)
+    st = lib.corr_linear_backward(code, act, _pointer(x), xs, pw, pz, pg, gs, px, pdw, pdb, M, N, K, ws, size, _stream())
+    if st != CORR_OK:
+        raise CorrError(st, "corr_linear_backward")
+    return d_x, d_w, d_bias
+
+
+def _norm_args(h, y, gate, gate_act, scale, h_scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps, dtype):
+    _on_device(h, "h")
+    device = h.device
+    rows, cols, hs = _rows(h, "h")
+    if y is not None:
+        if not isinstance(y, torch.Tensor):
+            raise TypeError("y must be a tensor on the GPU")
+        dtype = y.dtype
+    elif dtype is None:
+        dtype = h.dtype
+    if dtype not in _TYPES:
+        raise TypeError("rows must be float32, bfloat16 or float16")
+    py, ys = _matrix(y, "y", dtype, device, rows, cols)
+    pg, gs = _matrix(gate, "gate", dtype, device, rows, cols)
+    one = (cols,)
+    ps, pw1, pb1, pw2, pb2 = (None if v is None else _dense(v, name, torch.float32, device, one) for v, name in
+                              ((scale, "scale"), (post_weight, "post_weight"), (post_bias, "post_bias"), (pre_weight, "pre_weight"),
+                               (pre_bias, "pre_bias")))
+    return ResidualNormArgs(_type_of(h, "h"), _TYPES[dtype], rows, cols, _pointer(h), hs, py, ys, pg, gs, gate_act, ps, h_scale,
+                            post, pw1, pb1, pre, pw2, pb2, eps), dtype
+
+
+def corr_residual_norm(h: torch.Tensor, y: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+                       gate_act: int = CORR_ACT_SIGMOID, scale: torch.Tensor | None = None, h_scale: float = 1.0,
+                       post: int = CORR_NORM_NONE, post_weight: torch.Tensor | None = None, post_bias: torch.Tensor | None = None,
+                       pre: int = CORR_NORM_RMS, pre_weight: torch.Tensor | None = None, pre_bias: torch.Tensor | None = None,
+                       eps: float = 1e-5, h_out: torch.Tensor | None = None, n_out: torch.Tensor | None = None,
+                       dtype: torch.dtype | None = None):
+    """The end of one residual block and the beginning of the next (include/corr.h):
+        t = h_scale h + scale gate_act(gate) (post(y) post_weight + post_bias),   n = pre(t) pre_weight + pre_bias.
+    Returns (t, n): t of h's type (h itself without y), n of y's (of `dtype`, or h's, without y), None for CORR_NORM_NONE.
+    h, y, gate: [..., C] with contiguous, evenly spaced rows; vectors: float32 [C].  h_out may be h."""
+    a, dtype = _norm_args(h, y, gate, gate_act, scale, h_scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps, dtype)
+    device = h.device
+    ph = pn = None
+    if y is None:
+        if h_out is not None:
+            raise ValueError("without y there is no h_out: it is h")
+    else:
+        if h_out is None:
+            h_out = torch.empty(h.shape, dtype=h.dtype, device=device)
+        ph = _dense(h_out, "h_out", h.dtype, device, h.shape)
+    if pre != CORR_NORM_NONE:
+        if n_out is None:
+            n_out = torch.empty(h.shape, dtype=dtype, device=device)
+        pn = _dense(n_out, "n_out", dtype, device, h.shape)
+    elif n_out is not None:
+        raise ValueError("without a norm there is no n_out")
+    st = load_library().corr_residual_norm(ctypes.byref(a), ph, pn, _stream())
+    if st != CORR_OK:
+        raise CorrError(st, "corr_residual_norm")
+    return (h if y is None else h_out), n_out
+
+
+class ResidualNormGrads(NamedTuple):
+    """Gradients of corr_residual_norm's arguments; None for what was absent."""
+    d_h: torch.Tensor
+    d_y: torch.Tensor | None
+    d_gate: torch.Tensor | None
+    d_scale: torch.Tensor | None
+    d_post_weight: torch.Tensor | None
+    d_post_bias: torch.Tensor | None
+    d_pre_weight: torch.Tensor | None
+    d_pre_bias: torch.Tensor | None
+
+
+def corr_residual_norm_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return int(load_library().corr_residual_norm_backward_workspace_bytes(rows, cols))
+
+
+def corr_residual_norm_backward(h: torch.Tensor, y: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+                                gate_act: int = CORR_ACT_SIGMOID, scale: torch.Tensor | None = None, h_scale: float = 1.0,
+                                post: int = CORR_NORM_NONE, post_weight: torch.Tensor | None = None,
+                                post_bias: torch.Tensor | None = None, pre: int = CORR_NORM_RMS,
+                                pre_weight: torch.Tensor | None = None, pre_bias: torch.Tensor | None = None, eps: float = 1e-5,
+                                d_h_out: torch.Tensor | None = None, d_n_out: torch.Tensor | None = None,
+                                workspace: torch.Tensor | None = None) -> ResidualNormGrads:
+    """Gradients at corr_residual_norm's own arguments (its inputs, not its outputs).  d_h_out, d_n_out: the gradients of its two
+    results, contiguous; one of them may be None (zero).  Matrices have the type of what they are the gradient of, vectors float32."""
+    lib = load_library()
+    if y is None and d_n_out is not None and isinstance(d_n_out, torch.Tensor):
+        dtype = d_n_out.dtype
+    else:
+        dtype = None
+    a, dtype = _norm_args(h, y, gate, gate_act, scale, h_scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps, dtype)
+    device = h.device
+    pdh = _dense(d_h_out, "d_h_out", h.dtype, device, h.shape)
+    pdn = _dense(d_n_out, "d_n_out", dtype, device, h.shape)
+    if pdh is None and pdn is None:
+        raise ValueError("d_h_out or d_n_out is needed")
+    new = lambda like, kind: None if like is None else torch.empty(like.shape, dtype=kind, device=device)  # noqa: E731
+    g = ResidualNormGrads(new(h, h.dtype), new(y, dtype), new(gate, dtype), *(
+        new(v, torch.float32) for v in (scale, post_weight, post_bias, pre_weight, pre_bias)))
+    ptr = [None if t is None else _pointer(t) for t in g]
+    need = int(lib.corr_residual_norm_backward_workspace_bytes(a.rows, a.cols)) if any(ptr[3:]) else 0
+    held, ws, size = _workspace(workspace, need, device)
+    st = lib.corr_residual_norm_backward(ctypes.byref(a), pdh, pdn, *ptr, ws, size, _stream())
+    if st != CORR_OK:
+        raise CorrError(st, "corr_residual_norm_backward")
+    return g
 
 
 def corr_last_block_stats(pyramid: Pyramid, r: int = 4) -> dict:

@@ -1,0 +1,739 @@
+// Products of rows with weights: y = act(x w^T + bias) + residual, and the two products of its gradient.
+#include <type_traits>
+#include "rows_internal.h"
+
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) unsigned char lds_byte;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+__device__ __forceinline__ f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+template <class T> struct Frag;
+template <> struct Frag<__bf16> { typedef bf16x8 type; };
+template <> struct Frag<_Float16> { typedef f16x8 type; };
+
+// 16 bytes per lane from a buffer straight into LDS at lds + lane * 16.  A lane whose offset lies beyond the resource's size
+// writes zeros.
+__device__ __forceinline__ void dma16(i32x4 rsrc, unsigned lds, unsigned voff) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :: "s"(lds), "v"(voff), "s"(rsrc) : "memory");
+}
+// Everything this wave has asked for has arrived, then everything every wave has: the next tile can be read, and the
+// reads of the last one are over.
+__device__ __forceinline__ void arrive_all() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// The part of an operand that one workgroup reads: `at` moves with the k loop, `left` bytes of the matrix lie from there on
+// (offsets inside one step stay below 2^31: the callers limit row strides).
+struct Window {
+    const unsigned char* at;
+    int64_t left, step;
+    __device__ __forceinline__ unsigned size() const { return (unsigned)(left < 0 ? 0 : left > 0x7ffffff0 ? 0x7ffffff0 : left); }
+    __device__ __forceinline__ i32x4 rsrc() const {
+        const uint64_t p = (uint64_t)at;
+        return i32x4{__builtin_amdgcn_readfirstlane((int)p), __builtin_amdgcn_readfirstlane((int)(p >> 32) & 0xffff),
+                     __builtin_amdgcn_readfirstlane((int)size()), 0x00020000};
+    }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer() const {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(at), 0, __builtin_amdgcn_readfirstlane((int)size()), 0x00020000);
+    }
+    __device__ __forceinline__ void next() { at += step; left -= step; }
+};
+// rows r0 .. of a [rows][ld] matrix with k contiguous, from k0 on; or of a [K][ld] matrix with the rows contiguous
+template <bool ROWS, int ES, int BK>
+__device__ __forceinline__ Window window(const void* p, int64_t ld, int rows, int K, int r0, int k0) {
+    Window w;
+    w.at = (const unsigned char*)p + ((ROWS ? (int64_t)k0 * ld + r0 : (int64_t)r0 * ld + k0)) * ES;
+    w.left = ROWS ? ((int64_t)(K - 1 - k0) * ld + (rows - r0)) * ES : ((int64_t)(rows - 1 - r0) * ld + (K - k0)) * ES;
+    w.left = (w.left + 3) & ~(int64_t)3;                 // whole words: odd lengths come in rows that are padded
+    w.step = (ROWS ? (int64_t)BK * ld : BK) * ES;
+    return w;
+}
+
+// Which tile workgroup w of T takes.  Workgroup w runs on XCD w % 8: each XCD gets a run of consecutive tiles, and the tiles are
+// numbered in panels of eight columns, so that the 32 tiles an XCD works on at a time share operands in its L2.
+__device__ __forceinline__ void tile_of(int w, int tm, int tn, int& m, int& n) {
+    const int T = tm * tn, q = T >> 3, r = T & 7, x = w & 7;
+    const int t = x * q + min(x, r) + (w >> 3);
+    const int per = 8 * tm, panel = t / per, in = t - panel * per, wide = min(8, tn - 8 * panel);
+    m = in / wide;
+    n = 8 * panel + in - m * wide;
+}
+
+// One 16 x 16 block of C held as f32x4: rows of the instruction's first operand are n, so a lane has four consecutive n of one m.
+template <class T>
+__device__ __forceinline__ void store4(T* p, f32x4 v, int n_left, bool whole) {
+    if (whole) {
+        const float a[4] = {v[0], v[1], v[2], v[3]};
+        row_store<T, 4>(p, a);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (e < n_left) p[e] = (T)v[e];
+    }
+}
+template <class T>
+__device__ __forceinline__ void finish4(const ProductArgs& g, f32x4 v, int m, int n, bool whole) {
+    const int n_left = g.N - n;
+    if (m >= g.M || n_left <= 0) return;
+    if (g.bias) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) if (e < n_left) v[e] += g.bias[n + e];
+    }
+    if (g.pre) store4<T>((T*)g.pre + (int64_t)m * g.N + n, v, n_left, whole);
+    if (g.act != CORR_ACT_NONE) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = row_act(g.act, v[e]);
+    }
+    if (g.res) {
+        const T* r = (const T*)g.res + (int64_t)m * g.ld_res + n;
+        if (whole) {
+            float a[4];
+            row_load<T, 4>(r, a);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += a[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) if (e < n_left) v[e] += (float)r[e];
+        }
+    }
+    store4<T>((T*)g.y + (int64_t)m * g.ldy + n, v, n_left, whole);
+}
+// Four elements at once are loaded and stored where every row starts on their border and n_left is a multiple of four.
+template <class T>
+__device__ __forceinline__ bool rows_whole(const ProductArgs& g) {
+    const uintptr_t mask = 4 * sizeof(T) - 1;
+    return (g.N & 3) == 0 && (g.ldy & 3) == 0 && ((uintptr_t)g.y & mask) == 0 && ((uintptr_t)g.pre & mask) == 0 &&
+           (!g.res || ((g.ld_res & 3) == 0 && ((uintptr_t)g.res & mask) == 0));
+}
+template <class T>
+__device__ __forceinline__ void finish_tile4(const ProductArgs& g, f32x4 v, int m, int n, bool whole, int split, int splits) {
+    if (splits > 1) {
+        if (m < g.M && n < g.N) store4<float>(g.part + ((int64_t)split * g.M + m) * g.N + n, v, g.N - n, (g.N & 3) == 0);
+    } else finish4<T>(g, v, m, n, whole);
+}
+
+// ------------------------------------------------------------------------------------------------ 16-bit operands
+// A workgroup makes BM x BN elements in steps of 64 k.  Tiles lie in LDS as they are stored, in two halves that take turns: while
+// one is multiplied, the next step's 16-byte pieces land in the other.
+//   k contiguous:    rows of 128 bytes, piece p of row r at p ^ (r & 7)
+//   rows contiguous: 64 k-rows of 2 R bytes, 32-byte block c of row k at c ^ turn(k); read by the transposing LDS load
+// so that neither the rows of a fragment nor the k of a transposed one meet in a bank.
+template <int R> __device__ __forceinline__ int turn(int k) {
+    return R >= 128 ? (k & 3) | ((k >> 3) & 1) << 2 : (k & 3) ^ ((k >> 3) & 1);
+}
+template <bool ROWS, int R, int WAVES>
+struct Loader16 {
+    static constexpr int PIECES = R * 128 / (1024 * WAVES);
+    unsigned voff[PIECES];
+    __device__ __forceinline__ void plan(int wave, int lane, int64_t ld) {
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) {
+            const int p = (q * WAVES + wave) * 1024 + lane * 16;
+            if constexpr (ROWS) {
+                const int k = p / (2 * R), piece = (p % (2 * R)) >> 4;
+                voff[q] = (unsigned)(k * ld * 2) + ((((piece >> 1) ^ turn<R>(k)) << 1) | (piece & 1)) * 16;
+            } else {
+                const int row = p >> 7, piece = (p >> 4) & 7;
+                voff[q] = (unsigned)(row * ld * 2) + (piece ^ (row & 7)) * 16;
+            }
+        }
+    }
+    __device__ __forceinline__ void issue(const Window& w, unsigned lds, int wave) const {
+        const i32x4 rsrc = w.rsrc();
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) dma16(rsrc, lds + (q * WAVES + wave) * 1024, voff[q]);
+    }
+};
+// F fragments of 16 rows from row `base` on: lane (lr, lg) holds k = 8 lg .. + 7 of a row of 32 k.
+template <class T, bool ROWS, int R, int F>
+struct Reader16 {
+    unsigned off[ROWS ? F : 2];
+    __device__ __forceinline__ void plan(int base, int lr, int lg) {
+        if constexpr (ROWS) {
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
+                const int k = 8 * lg + (lr >> 2);
+                off[i] = k * (2 * R) + (((base >> 4) + i) ^ turn<R>(k)) * 32 + (lr & 3) * 8;
+            }
+        } else {
+            off[0] = (base + lr) * 128 + ((lg ^ (lr & 7)) << 4);
+            off[1] = off[0] ^ 64;
+        }
+    }
+    __device__ __forceinline__ typename Frag<T>::type get(lds_byte* tile, int i, int ks) const {
+        if constexpr (ROWS) {
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + off[i] + ks * 32 * 2 * R));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + off[i] + (ks * 32 + 4) * 2 * R));
+            return __builtin_bit_cast(typename Frag<T>::type, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            return *(__attribute__((address_space(3))) typename Frag<T>::type*)(tile + off[ks] + i * 2048);
+        }
+    }
+};
+// Elements from k = left on are taken out: what lies behind a row's end belongs to the next row.
+template <class V>
+__device__ __forceinline__ V keep_first(V v, int left) {
+    u32x4 u = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+    for (int d = 0; d < 4; ++d) u[d] &= left >= 2 * d + 2 ? 0xffffffffu : left == 2 * d + 1 ? 0xffffu : 0u;
+    return __builtin_bit_cast(V, u);
+}
+
+template <class T, bool AR, bool BR, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN, 2) void product16_kernel(ProductArgs g, int tm, int tn, int splits, int steps_per) {
+    constexpr int WAVES = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
+    constexpr int A_BYTES = BM * 128, HALF = (BM + BN) * 128;
+    __shared__ __align__(1024) unsigned char smem[2 * HALF];
+    lds_byte* const lds = (lds_byte*)smem;
+    const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)lds);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lg = lane >> 4;
+    int mt, nt;
+    tile_of(blockIdx.x, tm, tn, mt, nt);
+    const int m0 = mt * BM, n0 = nt * BN, split = blockIdx.y;
+    const int k0 = split * steps_per * 64, k_left = min(g.K - k0, steps_per * 64);
+    const int whole = k_left >> 6, tail = k_left & 63, steps = whole + (tail != 0);
+    Window wa = window<AR, 2, 64>(g.a, g.lda, g.M, g.K, m0, k0), wb = window<BR, 2, 64>(g.b, g.ldb, g.N, g.K, n0, k0);
+    Loader16<AR, BM, WAVES> la;
+    Loader16<BR, BN, WAVES> lb;
+    la.plan(wave, lane, g.lda);
+    lb.plan(wave, lane, g.ldb);
+    const int wm = (wave % WM) * TM, wn = (wave / WM) * TN;
+    Reader16<T, AR, BM, FM> ra;
+    Reader16<T, BR, BN, FN> rb;
+    ra.plan(wm, lr, lg);
+    rb.plan(wn, lr, lg);
+    f32x4 acc[FN][FM] = {};
+    auto ask = [&](int half) {
+        la.issue(wa, lds_at + half * HALF, wave);
+        lb.issue(wb, lds_at + half * HALF + A_BYTES, wave);
+        wa.next(); wb.next();
+    };
+    auto multiply = [&](int half, auto last) {
+        lds_byte* const ta = lds + half * HALF;
+        lds_byte* const tb = ta + A_BYTES;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            typename Frag<T>::type fa[FM], fb[FN];
+#pragma unroll
+            for (int j = 0; j < FM; ++j) fa[j] = ra.get(ta, j, ks);
+#pragma unroll
+            for (int i = 0; i < FN; ++i) fb[i] = rb.get(tb, i, ks);
+            if constexpr (decltype(last)::value) {
+                const int left = tail - ks * 32 - lg * 8;
+#pragma unroll
+                for (int j = 0; j < FM; ++j) if (!AR) fa[j] = keep_first(fa[j], left);
+#pragma unroll
+                for (int i = 0; i < FN; ++i) if (!BR) fb[i] = keep_first(fb[i], left);
+            }
+#pragma unroll
+            for (int i = 0; i < FN; ++i)
+#pragma unroll
+                for (int j = 0; j < FM; ++j) acc[i][j] = mma(fb[i], fa[j], acc[i][j]);
+        }
+    };
+    ask(0);
+    for (int t = 0; t < whole; ++t) {
+        arrive_all();
+        if (t + 1 < steps) ask((t + 1) & 1);
+        multiply(t & 1, std::false_type{});
+    }
+    if (tail) {
+        arrive_all();
+        multiply(whole & 1, std::true_type{});
+    }
+    const bool full = rows_whole<T>(g);
+#pragma unroll
+    for (int j = 0; j < FM; ++j)
+#pragma unroll
+        for (int i = 0; i < FN; ++i)
+            finish_tile4<T>(g, acc[i][j], m0 + wm + 16 * j + lr, n0 + wn + 16 * i + 4 * lg, full, split, splits);
+}
+
+// ------------------------------------------------------------------------------------------------ fp32 operands
+// An fp32 value is the sum of three bf16 values; the six of the nine partial products that reach 2^-24 are accumulated in
+// fp32.  Steps of 32 k: the thread that loads four elements splits them and writes them to three planes in LDS, the next step's on
+// their way into registers meanwhile.
+//   k contiguous:    rows of 64 bytes, piece p of row r at p ^ (r / 2 & 3)
+//   rows contiguous: as for 16 bits, 32 k-rows
+template <bool ROWS, int R, int NT>
+struct Loader32 {
+    static constexpr int PIECES = R * 8 / NT;
+    unsigned voff[PIECES], dst[PIECES];
+    f32x4 x[PIECES];
+    int k[PIECES];
+    __device__ __forceinline__ void plan(int tid, int64_t ld) {
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) {
+            const int p = q * NT + tid;
+            if constexpr (ROWS) {
+                const int kr = p / (R / 4), c = p % (R / 4);
+                k[q] = kr;
+                voff[q] = (unsigned)(kr * ld * 4) + c * 16;
+                dst[q] = kr * 2 * R + (((c >> 2) ^ turn<R>(kr)) << 5) + (c & 3) * 8;
+            } else {
+                const int row = p >> 3, c = p & 7;
+                k[q] = c * 4;
+                voff[q] = (unsigned)(row * ld * 4) + c * 16;
+                dst[q] = row * 64 + (((c >> 1) ^ (row >> 1 & 3)) << 4) + (c & 1) * 8;
+            }
+        }
+    }
+    __device__ __forceinline__ void ask(const Window& w) {
+        const __amdgpu_buffer_rsrc_t r = w.buffer();
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q)
+            x[q] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)voff[q], 0, 0));
+    }
+    __device__ __forceinline__ void cut(int left) {      // the last step of rows with k contiguous
+        if constexpr (!ROWS) {
+#pragma unroll
+            for (int q = 0; q < PIECES; ++q)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) if (k[q] + e >= left) x[q][e] = 0.f;
+        }
+    }
+    __device__ __forceinline__ void split(unsigned char* plane0) const {
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) {
+            f32x2 lo = {x[q][0], x[q][1]}, hi = {x[q][2], x[q][3]};
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+                const bf16x2 cl = __builtin_convertvector(lo, bf16x2), ch = __builtin_convertvector(hi, bf16x2);
+                *reinterpret_cast<u32x2*>(plane0 + p * (R * 64) + dst[q]) = u32x2{__builtin_bit_cast(unsigned, cl), __builtin_bit_cast(unsigned, ch)};
+                if (p < 2) {
+                    lo -= __builtin_convertvector(cl, f32x2);
+                    hi -= __builtin_convertvector(ch, f32x2);
+                }
+            }
+        }
+    }
+};
+template <bool ROWS, int R, int F>
+struct Reader32 {
+    unsigned off[ROWS ? F : 1];
+    __device__ __forceinline__ void plan(int base, int lr, int lg) {
+        if constexpr (ROWS) {
+#pragma unroll
+            for (int i = 0; i < F; ++i) {
+                const int k = 8 * lg + (lr >> 2);
+                off[i] = k * (2 * R) + (((base >> 4) + i) ^ turn<R>(k)) * 32 + (lr & 3) * 8;
+            }
+        } else off[0] = (base + lr) * 64 + ((lg ^ (lr >> 1 & 3)) << 4);
+    }
+    __device__ __forceinline__ bf16x8 get(lds_byte* plane, int i) const {
+        if constexpr (ROWS) {
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(plane + off[i]));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(plane + off[i] + 4 * 2 * R));
+            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else return *(__attribute__((address_space(3))) bf16x8*)(plane + off[0] + i * 1024);
+    }
+};
+
+template <bool AR, bool BR, int BM, int BN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN, 2) void product32_kernel(ProductArgs g, int tm, int tn, int splits, int steps_per) {
+    constexpr int NT = 64 * WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
+    constexpr int PA = BM * 64, PB = BN * 64;
+    __shared__ __align__(1024) unsigned char smem[3 * (PA + PB)];
+    lds_byte* const lds = (lds_byte*)smem;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lg = lane >> 4;
+    int mt, nt;
+    tile_of(blockIdx.x, tm, tn, mt, nt);
+    const int m0 = mt * BM, n0 = nt * BN, split = blockIdx.y;
+    const int k0 = split * steps_per * 32, k_left = min(g.K - k0, steps_per * 32), steps = (k_left + 31) >> 5;
+    Window wa = window<AR, 4, 32>(g.a, g.lda, g.M, g.K, m0, k0), wb = window<BR, 4, 32>(g.b, g.ldb, g.N, g.K, n0, k0);
+    Loader32<AR, BM, NT> la;
+    Loader32<BR, BN, NT> lb;
+    la.plan(tid, g.lda);
+    lb.plan(tid, g.ldb);
+    const int wm = (wave % WM) * TM, wn = (wave / WM) * TN;
+    Reader32<AR, BM, FM> ra;
+    Reader32<BR, BN, FN> rb;
+    ra.plan(wm, lr, lg);
+    rb.plan(wn, lr, lg);
+    f32x4 acc[FN][FM] = {};
+    la.ask(wa); lb.ask(wb);
+    for (int t = 0; t < steps; ++t) {
+        if (t + 1 == steps && (k_left & 31)) { la.cut(k_left & 31); lb.cut(k_left & 31); }
+        __syncthreads();                                 // the last step's fragments have been read
+        la.split(smem); lb.split(smem + 3 * PA);
+        if (t + 1 < steps) {
+            wa.next(); wb.next();
+            la.ask(wa); lb.ask(wb);
+        }
+        __syncthreads();
+        bf16x8 fa[3][FM], fb[3][FN];
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+#pragma unroll
+            for (int i = 0; i < FN; ++i) fb[p][i] = rb.get(lds + 3 * PA + p * PB, i);
+#pragma unroll
+            for (int j = 0; j < FM; ++j) fa[p][j] = ra.get(lds + p * PA, j);
+        }
+        // small products first
+        constexpr int QA[6] = {2, 0, 1, 1, 0, 0}, QB[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+        for (int q = 0; q < 6; ++q)
+#pragma unroll
+            for (int i = 0; i < FN; ++i)
+#pragma unroll
+                for (int j = 0; j < FM; ++j) acc[i][j] = mma(fb[QB[q]][i], fa[QA[q]][j], acc[i][j]);
+    }
+    // An infinity, a NaN or a value beyond bf16's range has no three parts (its remainder is infinity - infinity): what is
+    // not finite here is taken from fp32 instructions instead, one k of a row per lane.
+    float none = 0.f;                                    // NaN if any sum is not finite
+#pragma unroll
+    for (int i = 0; i < FN; ++i)
+#pragma unroll
+        for (int j = 0; j < FM; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) none = fmaf(acc[i][j][e], 0.f, none);
+    if (__any(none != 0.f)) {
+        const float* const A = (const float*)g.a;
+        const float* const B = (const float*)g.b;
+        for (int i = 0; i < FN; ++i)
+            for (int j = 0; j < FM; ++j) {
+                f32x4 plain = {};
+                const int64_t m = min(m0 + wm + 16 * j + lr, g.M - 1), n = min(n0 + wn + 16 * i + lr, g.N - 1);
+                for (int k = 0; k < k_left; k += 4) {
+                    float xa = 0.f, xb = 0.f;
+                    if (k + lg < k_left) {
+                        const int64_t kk = k0 + k + lg;
+                        xa = A[AR ? kk * g.lda + m : m * g.lda + kk];
+                        xb = B[BR ? kk * g.ldb + n : n * g.ldb + kk];
+                    }
+                    plain = __builtin_amdgcn_mfma_f32_16x16x4f32(xb, xa, plain, 0, 0, 0);
+                }
+#pragma unroll
+                for (int ii = 0; ii < FN; ++ii)
+#pragma unroll
+                    for (int jj = 0; jj < FM; ++jj)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (ii == i && jj == j && !(fabsf(acc[ii][jj][e]) < INFINITY)) acc[ii][jj][e] = plain[e];
+            }
+    }
+    const bool full = rows_whole<float>(g);
+#pragma unroll
+    for (int j = 0; j < FM; ++j)
+#pragma unroll
+        for (int i = 0; i < FN; ++i)
+            finish_tile4<float>(g, acc[i][j], m0 + wm + 16 * j + lr, n0 + wn + 16 * i + 4 * lg, full, split, splits);
+}
+
+// ------------------------------------------------------------------------------------------------ few rows
+// Up to 16 MT rows: every weight is read once, straight into the matrix instruction's fragments.  A workgroup makes 16 columns
+// of C; its waves take turns along k and add up in LDS.  WIDE: rows on 4-byte borders, loaded 16 bytes a lane.
+template <class T, bool WIDE>
+__device__ __forceinline__ typename Frag<T>::type few_load(const T* p, int left) {       // 8 elements, zeros from `left` on
+    typedef typename Frag<T>::type V;
+    if (WIDE && left >= 8) {
+        struct __attribute__((packed, aligned(4))) U { u32x4 v; };
+        return __builtin_bit_cast(V, reinterpret_cast<const U*>(p)->v);
+    }
+    V v = {};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) if (e < left) v[e] = p[e];
+    return v;
+}
+template <class T, bool WIDE, int WAVES, int MT>
+__global__ __launch_bounds__(64 * WAVES) void few_rows16_kernel(ProductArgs g) {
+    __shared__ f32x4 sums[WAVES][MT][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, lg = lane >> 4;
+    const int n0 = blockIdx.x * 16, n = n0 + lr;
+    const T* const W = (const T*)g.b + (int64_t)min(n, g.N - 1) * g.ldb;
+    const T* X[MT];
+#pragma unroll
+    for (int j = 0; j < MT; ++j) X[j] = (const T*)g.a + (int64_t)min(16 * j + lr, g.M - 1) * g.lda;
+    f32x4 acc[MT] = {};
+    constexpr int U = MT == 1 ? 4 : 2;                   // 32 k each
+    int k = wave * 32 * U + lg * 8;
+    for (; k - lg * 8 + 32 * U <= g.K; k += WAVES * 32 * U) {
+        typename Frag<T>::type w[U], x[U][MT];
+#pragma unroll
+        for (int u = 0; u < U; ++u) w[u] = few_load<T, WIDE>(W + k + 32 * u, 8);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < MT; ++j) x[u][j] = few_load<T, WIDE>(X[j] + k + 32 * u, 8);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < MT; ++j) acc[j] = mma(w[u], x[u][j], acc[j]);
+    }
+    for (int u = 0; u < U; ++u, k += 32) {               // the one wave whose turn the last, shorter stretch is
+        if (k - lg * 8 >= g.K) break;
+        const typename Frag<T>::type w = few_load<T, WIDE>(W + k, g.K - k);
+#pragma unroll
+        for (int j = 0; j < MT; ++j) acc[j] = mma(w, few_load<T, WIDE>(X[j] + k, g.K - k), acc[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < MT; ++j) sums[wave][j][lane] = acc[j];
+    __syncthreads();
+    const bool full = rows_whole<T>(g);
+    for (int j = wave; j < MT; j += WAVES) {
+        f32x4 v = sums[0][j][lane];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v += sums[w][j][lane];
+        finish4<T>(g, v, 16 * j + lr, n0 + 4 * lg, full);
+    }
+}
+// fp32: v_mfma_f32_16x16x4_f32, whose four k are the same element of four lanes' 16 bytes.
+__device__ __forceinline__ f32x4 few_load32(const float* p, int left) {
+    if (left >= 4) {
+        struct __attribute__((packed, aligned(4))) U { f32x4 v; };
+        return reinterpret_cast<const U*>(p)->v;
+    }
+    f32x4 v = {};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) if (e < left) v[e] = p[e];
+    return v;
+}
+template <int WAVES, int MT>
+__global__ __launch_bounds__(64 * WAVES) void few_rows32_kernel(ProductArgs g) {
+    __shared__ f32x4 sums[WAVES][MT][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, lg = lane >> 4;
+    const int n0 = blockIdx.x * 16, n = n0 + lr;
+    const float* const W = (const float*)g.b + (int64_t)min(n, g.N - 1) * g.ldb;
+    const float* X[MT];
+#pragma unroll
+    for (int j = 0; j < MT; ++j) X[j] = (const float*)g.a + (int64_t)min(16 * j + lr, g.M - 1) * g.lda;
+    f32x4 acc[MT] = {};
+    constexpr int U = MT == 1 ? 4 : 2;                   // 16 k each
+    int k = wave * 16 * U + lg * 4;
+    for (; k - lg * 4 + 16 * U <= g.K; k += WAVES * 16 * U) {
+        f32x4 w[U], x[U][MT];
+#pragma unroll
+        for (int u = 0; u < U; ++u) w[u] = few_load32(W + k + 16 * u, 4);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < MT; ++j) x[u][j] = few_load32(X[j] + k + 16 * u, 4);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int j = 0; j < MT; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[u][e], x[u][j][e], acc[j], 0, 0, 0);
+    }
+    for (int u = 0; u < U; ++u, k += 16) {
+        if (k - lg * 4 >= g.K) break;
+        const f32x4 w = few_load32(W + k, g.K - k);
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+            const f32x4 x = few_load32(X[j] + k, g.K - k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[e], x[e], acc[j], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < MT; ++j) sums[wave][j][lane] = acc[j];
+    __syncthreads();
+    const bool full = rows_whole<float>(g);
+    for (int j = wave; j < MT; j += WAVES) {
+        f32x4 v = sums[0][j][lane];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v += sums[w][j][lane];
+        finish4<float>(g, v, 16 * j + lr, n0 + 4 * lg, full);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ splits, packing, slopes
+// The splits' sums in their order, then the epilogue.
+template <class T>
+__global__ __launch_bounds__(256) void join_kernel(ProductArgs g, int splits) {
+    const int quads = (g.N + 3) >> 2;
+    const int64_t total = (int64_t)g.M * quads, plane = (int64_t)g.M * g.N;
+    const bool full = rows_whole<T>(g);
+    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (int64_t)gridDim.x * 256) {
+        const int64_t m = q / quads;
+        const int n = (int)(q - m * quads) * 4;
+        const float* p = g.part + m * g.N + n;
+        f32x4 v = {};
+        for (int s = 0; s < splits; ++s, p += plane) {
+            if ((g.N & 3) == 0) v += *reinterpret_cast<const f32x4*>(p);
+            else
+#pragma unroll
+                for (int e = 0; e < 4; ++e) if (n + e < g.N) v[e] += p[e];
+        }
+        finish4<T>(g, v, (int)m, n, full);
+    }
+}
+
+__global__ __launch_bounds__(256) void pack16_kernel(const uint16_t* __restrict__ src, int64_t ld_src, uint16_t* __restrict__ dst,
+                                                     int64_t ld_dst, int64_t rows, int64_t cols) {
+    const int64_t total = rows * ld_dst;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / ld_dst, c = i - r * ld_dst;
+        dst[i] = c < cols ? src[r * ld_src + c] : (uint16_t)0;
+    }
+}
+
+// A thread has V columns and every RT-th row of its workgroup's share; the sums over rows meet in LDS.
+constexpr int SLOPE_THREADS = 256;
+template <class T, int V>
+__global__ __launch_bounds__(SLOPE_THREADS) void slope_kernel(int act, const T* __restrict__ dy, int64_t ld_dy, const T* __restrict__ z,
+                                                             T* __restrict__ dz, int64_t ld_dz, float* __restrict__ part, int64_t M, int N,
+                                                             int ct, int64_t rows_per) {
+    __shared__ float sums[SLOPE_THREADS][V];
+    const int tid = threadIdx.x, c = tid % ct, rt = SLOPE_THREADS / ct, r0 = tid / ct;
+    const int n = (blockIdx.x * ct + c) * V;
+    const int64_t lo = (int64_t)blockIdx.y * rows_per, hi = min(M, lo + rows_per);
+    float sum[V] = {};
+    if (n < N) {
+        for (int64_t m = lo + r0; m < hi; m += rt) {
+            float v[V], s[V];
+            row_load<T, V>(dy + m * ld_dy + n, v);
+            if (act != CORR_ACT_NONE) {
+                row_load<T, V>(z + m * N + n, s);
+#pragma unroll
+                for (int e = 0; e < V; ++e) v[e] *= row_act_slope(act, s[e]);
+            }
+            if (dz) row_store<T, V>(dz + m * ld_dz + n, v);
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[e] += v[e];
+        }
+    }
+    if (!part) return;
+#pragma unroll
+    for (int e = 0; e < V; ++e) sums[tid][e] = sum[e];
+    __syncthreads();
+    if (r0 == 0 && n < N) {
+        for (int r = 1; r < rt; ++r)
+#pragma unroll
+            for (int e = 0; e < V; ++e) sum[e] += sums[r * ct + c][e];
+#pragma unroll
+        for (int e = 0; e < V; ++e) part[(int64_t)blockIdx.y * N + n + e] = sum[e];
+    }
+}
+
+enum Tile { TILE_FEW = 0, TILE_64, TILE_128, TILE_256 };
+inline int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+template <class T, bool AR, bool BR, int BM, int BN, int WM, int WN>
+void run16(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
+    const int tm = cdiv(g.M, BM), tn = cdiv(g.N, BN);
+    hipLaunchKernelGGL((product16_kernel<T, AR, BR, BM, BN, WM, WN>), dim3(tm * tn, p.splits), dim3(64 * WM * WN), 0, s, g, tm, tn, p.splits, p.steps);
+}
+template <class T, bool AR, bool BR>
+void run16(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
+    if (p.tile == TILE_256) run16<T, AR, BR, 256, 256, 2, 4>(g, p, s);
+    else if (p.tile == TILE_128) run16<T, AR, BR, 128, 128, 2, 2>(g, p, s);
+    else run16<T, AR, BR, 64, 64, 2, 2>(g, p, s);
+}
+template <class T>
+void few16(const ProductArgs& g, hipStream_t s) {
+    const bool wide = product_direct(g.type, g.a, g.lda, 0) && product_direct(g.type, g.b, g.ldb, 0);
+    const dim3 grid(cdiv(g.N, 16));
+#define FEW16(W, WAVES, MT) hipLaunchKernelGGL((few_rows16_kernel<T, W, WAVES, MT>), grid, dim3(64 * WAVES), 0, s, g)
+    const bool narrow = g.N <= 4096;
+    if (g.M <= 16) { if (wide) { if (narrow) FEW16(true, 8, 1); else FEW16(true, 4, 1); } else FEW16(false, 8, 1); }
+    else { if (wide) { if (narrow) FEW16(true, 8, 2); else FEW16(true, 4, 2); } else FEW16(false, 8, 2); }
+#undef FEW16
+}
+template <class T>
+void product16(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
+    if (p.tile == TILE_FEW) few16<T>(g, s);
+    else if (!g.a_rows && !g.b_rows) run16<T, false, false>(g, p, s);
+    else if (!g.a_rows) run16<T, false, true>(g, p, s);
+    else run16<T, true, true>(g, p, s);
+    if (p.splits > 1)
+        hipLaunchKernelGGL(join_kernel<T>, dim3(min(2048, cdiv((int64_t)g.M * ((g.N + 3) / 4), 256))), dim3(256), 0, s, g, p.splits);
+}
+template <bool AR, bool BR>
+void run32(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
+    if (p.tile == TILE_64) {
+        const int tm = cdiv(g.M, 64), tn = cdiv(g.N, 64);
+        hipLaunchKernelGGL((product32_kernel<AR, BR, 64, 64, 2, 2>), dim3(tm * tn, p.splits), dim3(256), 0, s, g, tm, tn, p.splits, p.steps);
+    } else {
+        const int tm = cdiv(g.M, 128), tn = cdiv(g.N, 128);
+        hipLaunchKernelGGL((product32_kernel<AR, BR, 128, 128, 2, 2>), dim3(tm * tn, p.splits), dim3(256), 0, s, g, tm, tn, p.splits, p.steps);
+    }
+}
+void product32(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
+    if (p.tile == TILE_FEW) {
+        const dim3 grid(cdiv(g.N, 16));
+        if (g.M <= 16) hipLaunchKernelGGL((few_rows32_kernel<8, 1>), grid, dim3(512), 0, s, g);
+        else hipLaunchKernelGGL((few_rows32_kernel<8, 2>), grid, dim3(512), 0, s, g);
+    } else if (!g.a_rows && !g.b_rows) run32<false, false>(g, p, s);
+    else if (!g.a_rows) run32<false, true>(g, p, s);
+    else run32<true, true>(g, p, s);
+    if (p.splits > 1)
+        hipLaunchKernelGGL(join_kernel<float>, dim3(min(2048, cdiv((int64_t)g.M * ((g.N + 3) / 4), 256))), dim3(256), 0, s, g, p.splits);
+}
+
+}  // namespace
+
+ProductPlan product_plan(corr_dtype type, int a_rows, int b_rows, int M, int N, int K) {
+    const bool wide = type == CORR_TYPE_F32;
+    const int bk = wide ? 32 : 64, all = cdiv(K, bk);
+    ProductPlan p = {TILE_64, 1, all};
+    if (M <= 32 && !a_rows && !b_rows) { p.tile = TILE_FEW; return p; }
+    int side = 64;
+    int64_t tiles = (int64_t)cdiv(M, 64) * cdiv(N, 64);
+    const int64_t t128 = (int64_t)cdiv(M, 128) * cdiv(N, 128), t256 = (int64_t)cdiv(M, 256) * cdiv(N, 256);
+    if (!wide && t256 >= 256) { p.tile = TILE_256; side = 256; tiles = t256; }
+    else if (t128 * all >= 256 * 8) { p.tile = TILE_128; side = 128; tiles = t128; }
+    (void)side;
+    // workgroups for two or three on every compute unit, and at least eight steps for each
+    const int64_t want = p.tile == TILE_256 ? 256 : p.tile == TILE_128 ? 512 : 1024;
+    if (tiles < want / 2) {
+        int splits = (int)min((int64_t)(all / 8 > 0 ? all / 8 : 1), want / tiles);
+        if (splits > 1) {
+            p.steps = cdiv(all, splits);
+            p.splits = cdiv(all, p.steps);
+        }
+    }
+    return p;
+}
+
+hipError_t launch_product(const ProductArgs& g, hipStream_t s) {
+    const ProductPlan p = product_plan(g.type, g.a_rows, g.b_rows, g.M, g.N, g.K);
+    if (g.type == CORR_TYPE_F32) product32(g, p, s);
+    else if (g.type == CORR_TYPE_BF16) product16<__bf16>(g, p, s);
+    else product16<_Float16>(g, p, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_pack16(const void* src, int64_t ld_src, void* dst, int64_t ld_dst, int64_t rows, int64_t cols, hipStream_t s) {
+    const int64_t blocks = (rows * ld_dst + 255) / 256;
+    hipLaunchKernelGGL(pack16_kernel, dim3((unsigned)min(blocks, (int64_t)1 << 20)), dim3(256), 0, s, (const uint16_t*)src, ld_src, (uint16_t*)dst, ld_dst, rows, cols);
+    return hipGetLastError();
+}
+
+int slope_parts(int64_t M, int N) { (void)N; return (int)min((int64_t)512, max((int64_t)1, (M + 31) / 32)); }
+
+namespace {
+template <class T, int V>
+void slope(int act, const void* dy, int64_t ld_dy, const void* z, void* dz, int64_t ld_dz, float* part, int64_t M, int N, hipStream_t s) {
+    int ct = 1;
+    while (ct < SLOPE_THREADS && ct * V < N) ct *= 2;
+    const int parts = slope_parts(M, N);
+    const int64_t per = (M + parts - 1) / parts;
+    hipLaunchKernelGGL((slope_kernel<T, V>), dim3(cdiv(N, ct * V), parts), dim3(SLOPE_THREADS), 0, s, act, (const T*)dy, ld_dy, (const T*)z,
+                       (T*)dz, ld_dz, part, M, N, ct, per);
+}
+template <class T>
+void slope_of(int act, const void* dy, int64_t ld_dy, const void* z, void* dz, int64_t ld_dz, float* part, int64_t M, int N, hipStream_t s) {
+    constexpr int V = 16 / sizeof(T);
+    const bool wide = N % V == 0 && ld_dy % V == 0 && ld_dz % V == 0 && (((uintptr_t)dy | (uintptr_t)z | (uintptr_t)dz) & 15) == 0;
+    if (wide) slope<T, V>(act, dy, ld_dy, z, dz, ld_dz, part, M, N, s);
+    else slope<T, 1>(act, dy, ld_dy, z, dz, ld_dz, part, M, N, s);
+}
+}  // namespace
+
+hipError_t launch_slope(corr_dtype t, int act, const void* dy, int64_t ld_dy, const void* z, void* dz, int64_t ld_dz, float* part,
+                        int64_t M, int N, hipStream_t s) {
+    if (t == CORR_TYPE_F32) slope_of<float>(act, dy, ld_dy, z, dz, ld_dz, part, M, N, s);
+    else if (t == CORR_TYPE_BF16) slope_of<__bf16>(act, dy, ld_dy, z, dz, ld_dz, part, M, N, s);
+    else slope_of<_Float16>(act, dy, ld_dy, z, dz, ld_dz, part, M, N, s);
+    return hipGetLastError();
+}

@@ -1,0 +1,49 @@
+// Launchers of the row operators (linear.hip, residual_norm.hip), called by rows_api.hip after its checks.
+#pragma once
+#include "rows.h"
+
+// C[m][n] = sum over k < K of A(m, k) B(n, k).  An operand is stored with its k contiguous ([m][k], `lda` elements from row to
+// row) or with its rows contiguous ([k][m]); which of the two is part of the kernel chosen.
+struct ProductArgs {
+    corr_dtype type;
+    const void* a; const void* b;
+    int64_t lda, ldb;
+    int a_rows, b_rows;        // 1: rows contiguous ([k][m] / [k][n])
+    int M, N, K;
+    // epilogue: z = C + bias (to `pre`, if there), y = act(z) + res
+    const float* bias;
+    const void* res; int64_t ld_res;
+    void* pre;                 // [M][N]
+    void* y; int64_t ldy;
+    int act;
+    float* part;               // [splits][M][N] fp32, where the plan says more than one split
+};
+struct ProductPlan { int tile, splits, steps; };   // steps of the k loop per split
+ProductPlan product_plan(corr_dtype type, int a_rows, int b_rows, int M, int N, int K);
+static inline size_t product_part_bytes(const ProductPlan& p, int M, int N) {
+    return p.splits > 1 ? (size_t)p.splits * M * N * 4 : 0;
+}
+hipError_t launch_product(const ProductArgs& p, hipStream_t s);
+// whether the 16-byte pieces of a matrix can be loaded where they lie: rows of `cols` elements, `ld` apart, on 4-byte borders
+static inline bool product_direct(corr_dtype t, const void* p, int64_t ld, int64_t cols) {
+    return t == CORR_TYPE_F32 || (((uintptr_t)p & 3) == 0 && (ld & 1) == 0 && (cols & 1) == 0);
+}
+// dst[r][0 .. ld_dst) = src[r][0 .. cols), zeros behind (16-bit elements)
+hipError_t launch_pack16(const void* src, int64_t ld_src, void* dst, int64_t ld_dst, int64_t rows, int64_t cols, hipStream_t s);
+// dz = dy * act'(z) as `type` (dz may be null), and the column sums of the unrounded dz by parts (part may be null)
+int slope_parts(int64_t M, int N);
+hipError_t launch_slope(corr_dtype t, int act, const void* dy, int64_t ld_dy, const void* z, void* dz, int64_t ld_dz, float* part,
+                        int64_t M, int N, hipStream_t s);
+
+// ---- norms around a block (residual_norm.hip)
+struct NormArgs {
+    corr_residual_norm_args a;
+    void* h_out; void* n_out;
+    const void* d_h_out; const void* d_n_out;      // gradient: either may be null (zero)
+    void* d_h; void* d_y; void* d_gate;            // each may be null
+    float* part;                                   // [parts][5][cols]: scale, post weight, post bias, pre weight, pre bias
+    int parts;
+};
+int norm_backward_parts(int64_t rows, int64_t cols);
+hipError_t launch_residual_norm(const NormArgs& n, hipStream_t s);
+hipError_t launch_residual_norm_backward(const NormArgs& n, hipStream_t s);
