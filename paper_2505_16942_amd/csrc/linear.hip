@@ -1,8 +1,12 @@
 // Products of rows with weights: y = act(x w^T + bias) + residual, and the two products of its gradient.
 #include <type_traits>
+#include <stdlib.h>
 #include "rows_internal.h"
 
 namespace {
+
+enum Tile { TILE_FEW = 0, TILE_64, TILE_128, TILE_256 };
+inline int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
@@ -69,56 +73,96 @@ __device__ __forceinline__ void tile_of(int w, int tm, int tn, int& m, int& n) {
     n = 8 * panel + in - m * wide;
 }
 
-// One 16 x 16 block of C held as f32x4: rows of the instruction's first operand are n, so a lane has four consecutive n of one m.
+// ---- epilogue.  Rows on 4-byte borders (`words`) are loaded and stored V elements at a time, as far as they go.
+template <class T, int V> struct Words { typedef T type __attribute__((ext_vector_type(V), aligned(4))); };
 template <class T>
-__device__ __forceinline__ void store4(T* p, f32x4 v, int n_left, bool whole) {
-    if (whole) {
-        const float a[4] = {v[0], v[1], v[2], v[3]};
-        row_store<T, 4>(p, a);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) if (e < n_left) p[e] = (T)v[e];
-    }
+__device__ __forceinline__ bool rows_words(const ProductArgs& g) {
+    if (sizeof(T) == 4) return true;
+    return ((g.N | g.ldy | (g.res ? g.ld_res : 0)) & 1) == 0 && (((uintptr_t)g.y | (uintptr_t)g.pre | (uintptr_t)g.res) & 3) == 0;
 }
-template <class T>
-__device__ __forceinline__ void finish4(const ProductArgs& g, f32x4 v, int m, int n, bool whole) {
-    const int n_left = g.N - n;
-    if (m >= g.M || n_left <= 0) return;
-    if (g.bias) {
+template <class T, int V>
+__device__ __forceinline__ void store_some(T* p, const float (&v)[V], int left, bool words) {
+    if (words && left >= V) {
+        typename Words<T, V>::type x;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) if (e < n_left) v[e] += g.bias[n + e];
-    }
-    if (g.pre) store4<T>((T*)g.pre + (int64_t)m * g.N + n, v, n_left, whole);
-    if (g.act != CORR_ACT_NONE) {
+        for (int e = 0; e < V; ++e) x[e] = (T)v[e];
+        *reinterpret_cast<typename Words<T, V>::type*>(p) = x;
+    } else
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = row_act(g.act, v[e]);
-    }
+        for (int e = 0; e < V; ++e) if (e < left) p[e] = (T)v[e];
+}
+template <class T, int V>
+__device__ __forceinline__ void load_some(const T* p, float (&v)[V], int left, bool words) {
+    if (words && left >= V) {
+        const typename Words<T, V>::type x = *reinterpret_cast<const typename Words<T, V>::type*>(p);
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = (float)x[e];
+    } else
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = e < left ? (float)p[e] : 0.f;
+}
+// V elements of row m from column n on
+template <class T, int V>
+__device__ __forceinline__ void finish(const ProductArgs& g, float (&v)[V], const float (&bias)[V], int m, int n, bool words) {
+    const int left = g.N - n;
+    if (m >= g.M || left <= 0) return;
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] += bias[e];
+    if (g.pre) store_some<T, V>((T*)g.pre + (int64_t)m * g.N + n, v, left, words);
+    row_act_all(g.act, v);
     if (g.res) {
-        const T* r = (const T*)g.res + (int64_t)m * g.ld_res + n;
-        if (whole) {
-            float a[4];
-            row_load<T, 4>(r, a);
+        float r[V];
+        load_some<T, V>((const T*)g.res + (int64_t)m * g.ld_res + n, r, left, words);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += a[e];
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) if (e < n_left) v[e] += (float)r[e];
-        }
+        for (int e = 0; e < V; ++e) v[e] += r[e];
     }
-    store4<T>((T*)g.y + (int64_t)m * g.ldy + n, v, n_left, whole);
+    store_some<T, V>((T*)g.y + (int64_t)m * g.ldy + n, v, left, words);
 }
-// Four elements at once are loaded and stored where every row starts on their border and n_left is a multiple of four.
-template <class T>
-__device__ __forceinline__ bool rows_whole(const ProductArgs& g) {
-    const uintptr_t mask = 4 * sizeof(T) - 1;
-    return (g.N & 3) == 0 && (g.ldy & 3) == 0 && ((uintptr_t)g.y & mask) == 0 && ((uintptr_t)g.pre & mask) == 0 &&
-           (!g.res || ((g.ld_res & 3) == 0 && ((uintptr_t)g.res & mask) == 0));
+template <int V>
+__device__ __forceinline__ void load_bias(const ProductArgs& g, float (&bias)[V], int n) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) bias[e] = g.bias && n + e < g.N ? g.bias[n + e] : 0.f;
 }
-template <class T>
-__device__ __forceinline__ void finish_tile4(const ProductArgs& g, f32x4 v, int m, int n, bool whole, int split, int splits) {
+// A wave's FN x FM blocks of 16 x 16 (rows of the instruction's first operand are n: a lane has four consecutive n of one m), 16 rows
+// of C at a time by way of LDS, so that a lane gets 16 bytes of a row and eight (16) lanes a whole 128-byte line or more.  Straight from
+// the registers, in pieces of 8 bytes and one activation after the other, the widening product at 1080p took 95 us.
+template <int FN> constexpr int box_floats() { return 16 * (16 * FN + 4); }
+template <class T, int FM, int FN>
+__device__ __forceinline__ void finish_wave(const ProductArgs& g, f32x4 (&acc)[FN][FM], float* box, int m0, int n0, int lane, int split, int splits) {
+    constexpr int LD = 16 * FN + 4;
+    const int lr = lane & 15, lg = lane >> 4;
+    auto by_rows = [&](auto width, auto f) {
+        constexpr int V = decltype(width)::value, LANES = 16 * FN / V, ROWS = 64 / LANES;
+        const int c = lane % LANES * V, r0 = lane / LANES;
+#pragma unroll
+        for (int j = 0; j < FM; ++j) {
+#pragma unroll
+            for (int i = 0; i < FN; ++i) *reinterpret_cast<f32x4*>(box + lr * LD + 16 * i + 4 * lg) = acc[i][j];
+            asm volatile("" ::: "memory");               // one wave: its LDS accesses are done in order
+#pragma unroll
+            for (int r = r0; r < 16; r += ROWS) {
+                float v[V];
+#pragma unroll
+                for (int e = 0; e < V; e += 4) {
+                    const f32x4 x = *reinterpret_cast<const f32x4*>(box + r * LD + c + e);
+                    v[e] = x[0]; v[e + 1] = x[1]; v[e + 2] = x[2]; v[e + 3] = x[3];
+                }
+                f(v, m0 + 16 * j + r, n0 + c);
+            }
+            asm volatile("" ::: "memory");
+        }
+    };
     if (splits > 1) {
-        if (m < g.M && n < g.N) store4<float>(g.part + ((int64_t)split * g.M + m) * g.N + n, v, g.N - n, (g.N & 3) == 0);
-    } else finish4<T>(g, v, m, n, whole);
+        by_rows(std::integral_constant<int, 4>{}, [&](float (&v)[4], int m, int n) {
+            if (m < g.M && n < g.N) store_some<float, 4>(g.part + ((int64_t)split * g.M + m) * g.N + n, v, g.N - n, true);
+        });
+    } else {
+        constexpr int V = 16 / sizeof(T);
+        const bool words = rows_words<T>(g);
+        float bias[V];
+        load_bias(g, bias, n0 + lane % (16 * FN / V) * V);
+        by_rows(std::integral_constant<int, V>{}, [&](float (&v)[V], int m, int n) { finish<T, V>(g, v, bias, m, n, words); });
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ 16-bit operands
@@ -250,12 +294,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product16_kernel(ProductArgs 
         arrive_all();
         multiply(whole & 1, std::true_type{});
     }
-    const bool full = rows_whole<T>(g);
-#pragma unroll
-    for (int j = 0; j < FM; ++j)
-#pragma unroll
-        for (int i = 0; i < FN; ++i)
-            finish_tile4<T>(g, acc[i][j], m0 + wm + 16 * j + lr, n0 + wn + 16 * i + 4 * lg, full, split, splits);
+    __syncthreads();                                     // the tiles have been read
+    finish_wave<T, FM, FN>(g, acc, (float*)smem + wave * box_floats<FN>(), m0 + wm, n0 + wn, lane, split, splits);
 }
 
 // ------------------------------------------------------------------------------------------------ fp32 operands
@@ -421,12 +461,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product32_kernel(ProductArgs 
                             if (ii == i && jj == j && !(fabsf(acc[ii][jj][e]) < INFINITY)) acc[ii][jj][e] = plain[e];
             }
     }
-    const bool full = rows_whole<float>(g);
-#pragma unroll
-    for (int j = 0; j < FM; ++j)
-#pragma unroll
-        for (int i = 0; i < FN; ++i)
-            finish_tile4<float>(g, acc[i][j], m0 + wm + 16 * j + lr, n0 + wn + 16 * i + 4 * lg, full, split, splits);
+    __syncthreads();                                     // the planes have been read
+    finish_wave<float, FM, FN>(g, acc, (float*)smem + wave * box_floats<FN>(), m0 + wm, n0 + wn, lane, split, splits);
 }
 
 // ------------------------------------------------------------------------------------------------ few rows
@@ -478,12 +514,14 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows16_kernel(ProductArgs g) {
 #pragma unroll
     for (int j = 0; j < MT; ++j) sums[wave][j][lane] = acc[j];
     __syncthreads();
-    const bool full = rows_whole<T>(g);
+    const bool words = rows_words<T>(g);
     for (int j = wave; j < MT; j += WAVES) {
-        f32x4 v = sums[0][j][lane];
+        f32x4 x = sums[0][j][lane];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) v += sums[w][j][lane];
-        finish4<T>(g, v, 16 * j + lr, n0 + 4 * lg, full);
+        for (int w = 1; w < WAVES; ++w) x += sums[w][j][lane];
+        float v[4] = {x[0], x[1], x[2], x[3]}, bias[4];
+        load_bias(g, bias, n0 + 4 * lg);
+        finish<T, 4>(g, v, bias, 16 * j + lr, n0 + 4 * lg, words);
     }
 }
 // fp32: v_mfma_f32_16x16x4_f32, whose four k are the same element of four lanes' 16 bytes.
@@ -537,35 +575,55 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows32_kernel(ProductArgs g) {
 #pragma unroll
     for (int j = 0; j < MT; ++j) sums[wave][j][lane] = acc[j];
     __syncthreads();
-    const bool full = rows_whole<float>(g);
+    const bool words = rows_words<float>(g);
     for (int j = wave; j < MT; j += WAVES) {
-        f32x4 v = sums[0][j][lane];
+        f32x4 x = sums[0][j][lane];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) v += sums[w][j][lane];
-        finish4<float>(g, v, 16 * j + lr, n0 + 4 * lg, full);
+        for (int w = 1; w < WAVES; ++w) x += sums[w][j][lane];
+        float v[4] = {x[0], x[1], x[2], x[3]}, bias[4];
+        load_bias(g, bias, n0 + 4 * lg);
+        finish<float, 4>(g, v, bias, 16 * j + lr, n0 + 4 * lg, words);
     }
 }
 
 // ------------------------------------------------------------------------------------------------ splits, packing, slopes
-// The splits' sums in their order, then the epilogue.
-template <class T>
+// The splits' sums, then the epilogue.  LANES threads take turns at a quad's splits (in a fixed order: the sum has the same bits on every
+// call), so that few outputs with many splits still keep enough loads on their way.
+template <class T, int LANES>
 __global__ __launch_bounds__(256) void join_kernel(ProductArgs g, int splits) {
-    const int quads = (g.N + 3) >> 2;
-    const int64_t total = (int64_t)g.M * quads, plane = (int64_t)g.M * g.N;
-    const bool full = rows_whole<T>(g);
-    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (int64_t)gridDim.x * 256) {
-        const int64_t m = q / quads;
-        const int n = (int)(q - m * quads) * 4;
-        const float* p = g.part + m * g.N + n;
-        f32x4 v = {};
-        for (int s = 0; s < splits; ++s, p += plane) {
-            if ((g.N & 3) == 0) v += *reinterpret_cast<const f32x4*>(p);
-            else
-#pragma unroll
-                for (int e = 0; e < 4; ++e) if (n + e < g.N) v[e] += p[e];
+    __shared__ f32x4 sums[LANES > 1 ? 256 : 1];
+    constexpr int QUADS = 256 / LANES;
+    const int quads = (g.N + 3) >> 2, lane = threadIdx.x / QUADS, slot = threadIdx.x % QUADS;
+    const int64_t total = (int64_t)g.M * quads, plane = (int64_t)g.M * g.N, q = (int64_t)blockIdx.x * QUADS + slot;
+    const int64_t m = q / quads;
+    const int n = (int)(q - m * quads) * 4;
+    f32x4 x = {};
+    if (q < total) {
+        const float* p = g.part + m * g.N + n + lane * plane;
+#pragma unroll 4
+        for (int s = lane; s < splits; s += LANES, p += LANES * plane) {
+            float v[4];
+            load_some<float, 4>(p, v, g.N - n, true);
+            x += f32x4{v[0], v[1], v[2], v[3]};
         }
-        finish4<T>(g, v, (int)m, n, full);
     }
+    if constexpr (LANES > 1) {
+        sums[threadIdx.x] = x;
+        __syncthreads();
+        if (lane) return;
+#pragma unroll
+        for (int l = 1; l < LANES; ++l) x += sums[l * QUADS + slot];
+    }
+    if (q >= total) return;
+    float v[4] = {x[0], x[1], x[2], x[3]}, bias[4];
+    load_bias(g, bias, n);
+    finish<T, 4>(g, v, bias, (int)m, n, rows_words<T>(g));
+}
+template <class T>
+void join(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
+    const int64_t quads = (int64_t)g.M * ((g.N + 3) / 4);
+    if (p.splits >= 8) hipLaunchKernelGGL((join_kernel<T, 8>), dim3((unsigned)((quads + 31) / 32)), dim3(256), 0, s, g, p.splits);
+    else hipLaunchKernelGGL((join_kernel<T, 1>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, s, g, p.splits);
 }
 
 __global__ __launch_bounds__(256) void pack16_kernel(const uint16_t* __restrict__ src, int64_t ld_src, uint16_t* __restrict__ dst,
@@ -577,7 +635,7 @@ __global__ __launch_bounds__(256) void pack16_kernel(const uint16_t* __restrict_
     }
 }
 
-// A thread has V columns and every RT-th row of its workgroup's share; the sums over rows meet in LDS.
+// A thread has V columns and every RT-th row of its workgroup's share, two at a time; the sums over rows meet in LDS.
 constexpr int SLOPE_THREADS = 256;
 template <class T, int V>
 __global__ __launch_bounds__(SLOPE_THREADS) void slope_kernel(int act, const T* __restrict__ dy, int64_t ld_dy, const T* __restrict__ z,
@@ -585,38 +643,44 @@ __global__ __launch_bounds__(SLOPE_THREADS) void slope_kernel(int act, const T* 
                                                              int ct, int64_t rows_per) {
     __shared__ float sums[SLOPE_THREADS][V];
     const int tid = threadIdx.x, c = tid % ct, rt = SLOPE_THREADS / ct, r0 = tid / ct;
-    const int n = (blockIdx.x * ct + c) * V;
+    const int n = (blockIdx.x * ct + c) * V, left = N - n;
     const int64_t lo = (int64_t)blockIdx.y * rows_per, hi = min(M, lo + rows_per);
     float sum[V] = {};
-    if (n < N) {
-        for (int64_t m = lo + r0; m < hi; m += rt) {
-            float v[V], s[V];
-            row_load<T, V>(dy + m * ld_dy + n, v);
-            if (act != CORR_ACT_NONE) {
-                row_load<T, V>(z + m * N + n, s);
-#pragma unroll
-                for (int e = 0; e < V; ++e) v[e] *= row_act_slope(act, s[e]);
+    if (left > 0) {
+        for (int64_t m = lo + r0; m < hi; m += 2 * rt) {
+            const bool two = m + rt < hi;
+            float v[2][V], s[2][V];
+            load_some<T, V>(dy + m * ld_dy + n, v[0], left, V > 1);
+            if (act != CORR_ACT_NONE) load_some<T, V>(z + m * N + n, s[0], left, V > 1);
+            if (two) {
+                load_some<T, V>(dy + (m + rt) * ld_dy + n, v[1], left, V > 1);
+                if (act != CORR_ACT_NONE) load_some<T, V>(z + (m + rt) * N + n, s[1], left, V > 1);
             }
-            if (dz) row_store<T, V>(dz + m * ld_dz + n, v);
 #pragma unroll
-            for (int e = 0; e < V; ++e) sum[e] += v[e];
+            for (int u = 0; u < 2; ++u) {
+                if (u && !two) break;
+                if (act != CORR_ACT_NONE) {
+                    row_slope_all(act, s[u]);
+#pragma unroll
+                    for (int e = 0; e < V; ++e) v[u][e] *= s[u][e];
+                }
+                if (dz) store_some<T, V>(dz + (m + u * rt) * ld_dz + n, v[u], left, V > 1);
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum[e] += v[u][e];
+            }
         }
     }
     if (!part) return;
 #pragma unroll
     for (int e = 0; e < V; ++e) sums[tid][e] = sum[e];
     __syncthreads();
-    if (r0 == 0 && n < N) {
+    if (r0 == 0 && left > 0) {
         for (int r = 1; r < rt; ++r)
 #pragma unroll
             for (int e = 0; e < V; ++e) sum[e] += sums[r * ct + c][e];
-#pragma unroll
-        for (int e = 0; e < V; ++e) part[(int64_t)blockIdx.y * N + n + e] = sum[e];
+        store_some<float, V>(part + (int64_t)blockIdx.y * N + n, sum, left, true);
     }
 }
-
-enum Tile { TILE_FEW = 0, TILE_64, TILE_128, TILE_256 };
-inline int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 template <class T, bool AR, bool BR, int BM, int BN, int WM, int WN>
 void run16(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
@@ -645,8 +709,7 @@ void product16(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
     else if (!g.a_rows && !g.b_rows) run16<T, false, false>(g, p, s);
     else if (!g.a_rows) run16<T, false, true>(g, p, s);
     else run16<T, true, true>(g, p, s);
-    if (p.splits > 1)
-        hipLaunchKernelGGL(join_kernel<T>, dim3(min(2048, cdiv((int64_t)g.M * ((g.N + 3) / 4), 256))), dim3(256), 0, s, g, p.splits);
+    if (p.splits > 1) join<T>(g, p, s);
 }
 template <bool AR, bool BR>
 void run32(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
@@ -666,8 +729,7 @@ void product32(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
     } else if (!g.a_rows && !g.b_rows) run32<false, false>(g, p, s);
     else if (!g.a_rows) run32<false, true>(g, p, s);
     else run32<true, true>(g, p, s);
-    if (p.splits > 1)
-        hipLaunchKernelGGL(join_kernel<float>, dim3(min(2048, cdiv((int64_t)g.M * ((g.N + 3) / 4), 256))), dim3(256), 0, s, g, p.splits);
+    if (p.splits > 1) join<float>(g, p, s);
 }
 
 }  // namespace
@@ -683,6 +745,7 @@ ProductPlan product_plan(corr_dtype type, int a_rows, int b_rows, int M, int N, 
     if (!wide && t256 >= 256) { p.tile = TILE_256; side = 256; tiles = t256; }
     else if (t128 * all >= 256 * 8) { p.tile = TILE_128; side = 128; tiles = t128; }
     (void)side;
+    if (getenv("CORR_TILE")) { p.tile = atoi(getenv("CORR_TILE")); tiles = p.tile == 3 ? t256 : p.tile == 2 ? t128 : (int64_t)cdiv(M, 64) * cdiv(N, 64); }
     // workgroups for two or three on every compute unit, and at least eight steps for each
     const int64_t want = p.tile == TILE_256 ? 256 : p.tile == TILE_128 ? 512 : 1024;
     if (tiles < want / 2) {
@@ -709,7 +772,7 @@ hipError_t launch_pack16(const void* src, int64_t ld_src, void* dst, int64_t ld_
     return hipGetLastError();
 }
 
-int slope_parts(int64_t M, int N) { (void)N; return (int)min((int64_t)512, max((int64_t)1, (M + 31) / 32)); }
+int slope_parts(int64_t M, int N) { (void)N; return (int)min((int64_t)1024, max((int64_t)1, (M + 15) / 16)); }
 
 namespace {
 template <class T, int V>
@@ -724,8 +787,8 @@ void slope(int act, const void* dy, int64_t ld_dy, const void* z, void* dz, int6
 template <class T>
 void slope_of(int act, const void* dy, int64_t ld_dy, const void* z, void* dz, int64_t ld_dz, float* part, int64_t M, int N, hipStream_t s) {
     constexpr int V = 16 / sizeof(T);
-    const bool wide = N % V == 0 && ld_dy % V == 0 && ld_dz % V == 0 && (((uintptr_t)dy | (uintptr_t)z | (uintptr_t)dz) & 15) == 0;
-    if (wide) slope<T, V>(act, dy, ld_dy, z, dz, ld_dz, part, M, N, s);
+    const bool words = sizeof(T) == 4 || (((N | ld_dy) & 1) == 0 && (((uintptr_t)dy | (uintptr_t)z) & 3) == 0);   // dz lies in the workspace
+    if (words) slope<T, V>(act, dy, ld_dy, z, dz, ld_dz, part, M, N, s);
     else slope<T, 1>(act, dy, ld_dy, z, dz, ld_dz, part, M, N, s);
 }
 }  // namespace

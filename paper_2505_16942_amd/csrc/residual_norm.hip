@@ -130,9 +130,11 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_kernel(NormAr
             if (!KEEP) { c.vector(a.post_weight, 1.f, w1); c.vector(a.post_bias, 0.f, b1); c.vector(a.scale, 1.f, s); }
 #pragma unroll
             for (int e = 0; e < E; ++e) p[e] = fmaf(p[e], w1[e], b1[e]) * s[e];
-            if (a.gate)
+            if (a.gate) {
+                row_act_all(a.gate_act, g);
 #pragma unroll
-                for (int e = 0; e < E; ++e) p[e] *= row_act(a.gate_act, g[e]);
+                for (int e = 0; e < E; ++e) p[e] *= g[e];
+            }
 #pragma unroll
             for (int e = 0; e < E; ++e) t[e] = c.in(e) ? fmaf(a.h_scale, t[e], p[e]) : 0.f;
             if (n.h_out) c.store((S*)n.h_out + r * a.cols, t);

@@ -13,15 +13,28 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 static inline int corr_elem_bytes(corr_dtype t) { return t == CORR_TYPE_F32 ? 4 : 2; }
 
 #ifdef __HIPCC__
-// Activations in fp32.  1 / (1 + e^-z) by v_rcp_f32 (1 ulp); where e^-z overflows the quotient is 0, as it should be.
-// A comparison keeps a NaN where fmaxf would drop it.
-__device__ __forceinline__ float row_sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + expf(-z)); }
+// Activations in fp32.  e^x is v_exp_f32 of x log2 e (off by |x| 2^-24 relative, where the products that e^x meets are small), 1 / x
+// v_rcp_f32 (1 ulp).  Where e^-z overflows, 1 / (1 + e^-z) is 0, as it should be.  A comparison keeps a NaN where fmaxf would drop it.
+__device__ __forceinline__ float row_exp(float x) { return __builtin_amdgcn_exp2f(1.4426950408889634f * x); }
+__device__ __forceinline__ float row_sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + row_exp(-z)); }
 // u of 0.5 z (1 + tanh u) = z sigmoid(2 u), times two
 __device__ __forceinline__ float row_gelu_2u(float z) { return 1.5957691216057308f * fmaf(0.044715f * z * z, z, z); }
+// The normal distribution's integral, and `tail` = e^(-z^2/2): erfc(x) = (a1 t + .. + a5 t^5) e^(-x^2), t = 1 / (1 + p x), x >= 0
+// (Abramowitz and Stegun, 7.1.26: off by 1.5e-7 at most), halved, at x = |z| / sqrt 2.  The library's erff has two branches, and a
+// wave takes both: 32400 x 1024 outputs took 122 us with it.
+__device__ __forceinline__ float row_normal(float z, float& tail) {
+    const float x = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
+    tail = row_exp(-x * x);
+    float q = fmaf(t, 0.5305027145f, -0.7265760135f);
+    q = fmaf(t, q, 0.7107068705f);
+    q = fmaf(t, q, -0.142248368f);
+    q = fmaf(t, q, 0.127414796f) * t * tail;
+    return z < 0.f ? q : 1.f - q;
+}
 __device__ __forceinline__ float row_act(int act, float z) {
     switch (act) {
         case CORR_ACT_RELU: return z < 0.f ? 0.f : z;
-        case CORR_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+        case CORR_ACT_GELU: { float tail; return z * row_normal(z, tail); }
         case CORR_ACT_GELU_TANH: return z * row_sigmoid(row_gelu_2u(z));
         case CORR_ACT_SILU: return z * row_sigmoid(z);
         case CORR_ACT_SIGMOID: return row_sigmoid(z);
@@ -31,8 +44,11 @@ __device__ __forceinline__ float row_act(int act, float z) {
 __device__ __forceinline__ float row_act_slope(int act, float z) {
     switch (act) {
         case CORR_ACT_RELU: return z > 0.f ? 1.f : 0.f;
-        case CORR_ACT_GELU:
-            return fmaf(z * expf(-0.5f * z * z), 0.39894228040143268f, 0.5f * (1.f + erff(z * 0.70710678118654752f)));
+        case CORR_ACT_GELU: {
+            float tail;
+            const float p = row_normal(z, tail);
+            return fmaf(z * tail, 0.39894228040143268f, p);
+        }
         case CORR_ACT_GELU_TANH: {
             const float s = row_sigmoid(row_gelu_2u(z));
             return fmaf(z * s * (1.f - s), 1.5957691216057308f * fmaf(0.134145f * z, z, 1.f), s);
@@ -41,6 +57,30 @@ __device__ __forceinline__ float row_act_slope(int act, float z) {
         case CORR_ACT_SIGMOID: { const float s = row_sigmoid(z); return s * (1.f - s); }
     }
     return 1.f;
+}
+// V values at once: the choice is made once, and their chains of dependent instructions overlap.
+template <int V, class F> __device__ __forceinline__ void row_each(float (&v)[V], F f) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = f(v[e]);
+}
+template <int V> __device__ __forceinline__ void row_act_all(int act, float (&v)[V]) {
+    switch (act) {
+        case CORR_ACT_RELU: row_each(v, [](float z) { return row_act(CORR_ACT_RELU, z); }); break;
+        case CORR_ACT_GELU: row_each(v, [](float z) { return row_act(CORR_ACT_GELU, z); }); break;
+        case CORR_ACT_GELU_TANH: row_each(v, [](float z) { return row_act(CORR_ACT_GELU_TANH, z); }); break;
+        case CORR_ACT_SILU: row_each(v, [](float z) { return row_act(CORR_ACT_SILU, z); }); break;
+        case CORR_ACT_SIGMOID: row_each(v, [](float z) { return row_act(CORR_ACT_SIGMOID, z); }); break;
+    }
+}
+template <int V> __device__ __forceinline__ void row_slope_all(int act, float (&v)[V]) {
+    switch (act) {
+        case CORR_ACT_RELU: row_each(v, [](float z) { return row_act_slope(CORR_ACT_RELU, z); }); break;
+        case CORR_ACT_GELU: row_each(v, [](float z) { return row_act_slope(CORR_ACT_GELU, z); }); break;
+        case CORR_ACT_GELU_TANH: row_each(v, [](float z) { return row_act_slope(CORR_ACT_GELU_TANH, z); }); break;
+        case CORR_ACT_SILU: row_each(v, [](float z) { return row_act_slope(CORR_ACT_SILU, z); }); break;
+        case CORR_ACT_SIGMOID: row_each(v, [](float z) { return row_act_slope(CORR_ACT_SIGMOID, z); }); break;
+        default: row_each(v, [](float) { return 1.f; });
+    }
 }
 
 // V consecutive elements of type T as fp32 and back (rounded to nearest even), as one access of V * sizeof(T) bytes.
