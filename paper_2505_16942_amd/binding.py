@@ -7,6 +7,7 @@ CPU fallback: if the library is missing or no GPU is visible, calls raise.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import NamedTuple
 
@@ -339,28 +340,38 @@ def corr_sample_backward(pyramid: Pyramid, coords: torch.Tensor, d_out: torch.Te
 _TYPES = {torch.float32: CORR_TYPE_F32, torch.bfloat16: CORR_TYPE_BF16, torch.float16: CORR_TYPE_F16}
 
 
-def _on_device(t, name: str, device=None) -> None:
-    """Kernels go to the current device's current stream: a tensor elsewhere is refused."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+def _device_index():
+    raw = getattr(torch._C, "_cuda_getDevice", None)     # see _stream_handle
+    return raw if raw is not None else torch.cuda.current_device
+
+
+_current_device = _device_index()
+
+
+def _on_device(t, name: str, device: int | None = None) -> int:
+    """Kernels go to the current device's current stream: a tensor elsewhere is refused.  Returns the device's index."""
+    if not isinstance(t, torch.Tensor):
         raise TypeError("%s must be a tensor on the GPU" % name)
-    if device is None:
-        if t.device.index != torch.cuda.current_device():
-            raise ValueError("%s is on %s, which is not the current device" % (name, t.device))
-    elif t.device != device:
-        raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
+    index = t.get_device()
+    if index < 0:
+        raise TypeError("%s must be a tensor on the GPU" % name)
+    if index != (_current_device() if device is None else device):
+        raise ValueError("%s is on %s, which is not %s" % (name, t.device, "the current device" if device is None else "cuda:%d" % device))
+    return index
 
 
 def _rows(t: torch.Tensor, name: str):
     """(rows, length, stride) of a tensor [..., length] whose rows are contiguous and evenly spaced."""
-    if t.dim() == 0:
+    shape = t.shape
+    if not shape:
         raise ValueError("%s must have at least one dimension" % name)
-    cols = t.shape[-1]
+    cols = shape[-1]
     if t.is_contiguous():
-        return t.numel() // max(cols, 1), cols, cols
+        return (shape[0] if len(shape) == 2 else t.numel() // max(cols, 1)), cols, cols
     if cols > 1 and t.stride(-1) != 1:
         raise ValueError("%s must have contiguous rows" % name)
     rows, stride = 1, 0
-    for size, step in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+    for size, step in zip(reversed(shape[:-1]), reversed(t.stride()[:-1])):
         if size == 1:
             continue
         if rows == 1:
@@ -376,37 +387,40 @@ def _pointer(t) -> int:
     return t.data_ptr() or 256
 
 
-def _matrix(t, name: str, dtype, device, rows: int, cols: int):
-    """(pointer, stride) of an optional matrix of known size and type."""
-    if t is None:
-        return None, 0
+def _matrix(t, name: str, dtype, device: int, rows: int, cols: int):
+    """(pointer, stride) of a matrix of known size and type."""
     _on_device(t, name, device)
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError("%s must be %s" % (name, dtype))
     r, c, stride = _rows(t, name)
     if r != rows or c != cols:
         raise ValueError("%s must have %d rows of %d" % (name, rows, cols))
-    return _pointer(t), stride
+    return t.data_ptr() or 256, stride
 
 
-def _dense(t, name: str, dtype, device, shape):
-    """Pointer of an optional contiguous tensor of known size and type."""
-    if t is None:
-        return None
+def _dense(t, name: str, dtype, device: int, shape) -> int:
+    """Pointer of a contiguous tensor of known size and type."""
     _on_device(t, name, device)
-    if t.dtype != dtype or not t.is_contiguous():
+    if t.dtype is not dtype or not t.is_contiguous():
         raise TypeError("%s must be contiguous and %s" % (name, dtype))
     if t.shape != shape:
         raise ValueError("%s must be %s" % (name, list(shape)))
-    return _pointer(t)
+    return t.data_ptr() or 256
 
 
-def _workspace(workspace, need: int, device):
+def _new(like: torch.Tensor, shape, dtype):
+    """A plain tensor on like's device, whatever like's class."""
+    if type(like) is torch.Tensor:
+        return like.new_empty(shape, dtype=dtype)
+    return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _workspace(workspace, need: int, like: torch.Tensor, device: int):
     """(tensor that holds it, pointer, bytes); allocated on the current stream if None."""
     if workspace is None:
         if not need:
             return None, None, 0
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        workspace = _new(like, need, torch.uint8)
         return workspace, workspace.data_ptr(), need
     _on_device(workspace, "workspace", device)
     size = workspace.numel() * workspace.element_size()
@@ -415,11 +429,33 @@ def _workspace(workspace, need: int, device):
     return workspace, workspace.data_ptr(), size
 
 
+# the sizes are functions of their arguments alone
+@functools.lru_cache(maxsize=1024)
+def _linear_need(*sizes) -> int:
+    return int(load_library().corr_linear_workspace_bytes(*sizes))
+
+
+@functools.lru_cache(maxsize=1024)
+def _linear_backward_need(*sizes) -> int:
+    return int(load_library().corr_linear_backward_workspace_bytes(*sizes))
+
+
+@functools.lru_cache(maxsize=1024)
+def _norm_backward_need(*sizes) -> int:
+    return int(load_library().corr_residual_norm_backward_workspace_bytes(*sizes))
+
+
 def _type_of(t, name: str) -> int:
     code = _TYPES.get(t.dtype)
     if code is None:
         raise TypeError("%s must be float32, bfloat16 or float16" % name)
     return code
+
+
+def _weights(w, K: int) -> int:
+    if not isinstance(w, torch.Tensor) or w.dim() != 2 or w.shape[1] != K:
+        raise ValueError("w must be [N, %d]" % K)
+    return w.shape[0]
 
 
 def corr_linear_workspace_bytes(dtype: torch.dtype, M: int, N: int, K: int, x_stride: int | None = None) -> int:
@@ -432,27 +468,26 @@ def corr_linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = No
     """act(x w^T + bias) + residual.  x: [..., K] with contiguous, evenly spaced rows (corr_sample's CORR_OUT_NHWC output is
     one); w: [N, K]; both float32, bfloat16 or float16.  bias: float32 [N].  residual, out: [..., N] of x's type; out may be
     residual.  preact: a contiguous [..., N] that receives the sum before the activation (corr_linear_backward reads it)."""
-    lib = load_library()
-    _on_device(x, "x")
-    code, dtype, device = _type_of(x, "x"), x.dtype, x.device
+    lib = _lib or load_library()
+    device = _on_device(x, "x")
+    dtype = x.dtype
+    code = _type_of(x, "x")
     M, K, xs = _rows(x, "x")
-    if not isinstance(w, torch.Tensor) or w.dim() != 2 or w.shape[1] != K:
-        raise ValueError("w must be [N, %d]" % K)
-    N = w.shape[0]
-    shape = x.shape[:-1] + (N,)
+    N = _weights(w, K)
     pw = _dense(w, "w", dtype, device, w.shape)
-    pb = _dense(bias, "bias", torch.float32, device, (N,))
-    pr, rs = _matrix(residual, "residual", dtype, device, M, N)
-    pz = _dense(preact, "preact", dtype, device, shape)
+    shape = x.shape[:-1] + (N,)
+    pb = None if bias is None else _dense(bias, "bias", torch.float32, device, (N,))
+    pr, rs = (None, 0) if residual is None else _matrix(residual, "residual", dtype, device, M, N)
+    pz = None if preact is None else _dense(preact, "preact", dtype, device, shape)
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=device)
-        po, os_ = _pointer(out), N
+        out = _new(x, shape, dtype)
+        po, ys = _pointer(out), N
+    elif out.shape != shape:
+        raise ValueError("out must be %s" % list(shape))
     else:
-        if out.shape != shape:
-            raise ValueError("out must be %s" % list(shape))
-        po, os_ = _matrix(out, "out", dtype, device, M, N)
-    held, ws, size = _workspace(workspace, lib.corr_linear_workspace_bytes(code, M, N, K, xs), device)
-    st = lib.corr_linear(code, act, _pointer(x), xs, pw, pb, pr, rs, pz, po, os_, M, N, K, ws, size, _stream())
+        po, ys = _matrix(out, "out", dtype, device, M, N)
+    held, ws, size = _workspace(workspace, _linear_need(code, M, N, K, xs), x, device)
+    st = lib.corr_linear(code, act, _pointer(x), xs, pw, pb, pr, rs, pz, po, ys, M, N, K, ws, size, _stream())
     if st != CORR_OK:
         raise CorrError(st, "corr_linear")
     return out
@@ -470,40 +505,39 @@ def corr_linear_backward(x: torch.Tensor, w: torch.Tensor, d_out: torch.Tensor, 
                          workspace: torch.Tensor | None = None):
     """(d_x, d_w, d_bias) of corr_linear, None where not wanted: x's type for the first two, float32 for the bias.  d_out: the
     gradient of its result, which is the residual's too; preact: what corr_linear stored (needed for an activation)."""
-    lib = load_library()
-    _on_device(x, "x")
-    code, dtype, device = _type_of(x, "x"), x.dtype, x.device
+    lib = _lib or load_library()
+    device = _on_device(x, "x")
+    dtype = x.dtype
+    code = _type_of(x, "x")
     M, K, xs = _rows(x, "x")
-    if not isinstance(w, torch.Tensor) or w.dim() != 2 or w.shape[1] != K:
-        raise ValueError("w must be [N, %d]" % K)
-    N = w.shape[0]
+    N = _weights(w, K)
     pw = _dense(w, "w", dtype, device, w.shape)
-    if d_out is None:
-        raise TypeError("d_out must be a tensor on the GPU")
     pg, gs = _matrix(d_out, "d_out", dtype, device, M, N)
-    if act != CORR_ACT_NONE and preact is None:
-        raise ValueError("the gradient of an activation needs preact")
-    pz = _dense(preact, "preact", dtype, device, x.shape[:-1] + (N,)) if act != CORR_ACT_NONE else None
-
-    def output(t, wanted, name, kind, shape):
-        if not wanted:
-            return None, None
-        if t is None:
-            t = torch.empty(shape, dtype=kind, device=device)
-        return t, _dense(t, name, kind, device, shape)
-    d_x, px = output(d_x, want_x, "d_x", dtype, x.shape)
-    d_w, pdw = output(d_w, want_w, "d_w", dtype, w.shape)
-    d_bias, pdb = output(d_bias, want_bias, "d_bias", torch.float32, (N,))
-    held, ws, size = _workspace(workspace, lib.corr_linear_backward_workspace_bytes(code, act, M, N, K, xs, gs), device)
+    pz = None
+    if act != CORR_ACT_NONE:
+        if preact is None:
+            raise ValueError("the gradient of an activation needs preact")
+        pz = _dense(preact, "preact", dtype, device, x.shape[:-1] + (N,))
+    px = pdw = pdb = None
+    if want_x:
+        d_x = _new(x, x.shape, dtype) if d_x is None else d_x
+        px = _dense(d_x, "d_x", dtype, device, x.shape)
+    if want_w:
+        d_w = _new(x, w.shape, dtype) if d_w is None else d_w
+        pdw = _dense(d_w, "d_w", dtype, device, w.shape)
+    if want_bias:
+        d_bias = _new(x, (N,), torch.float32) if d_bias is None else d_bias
+        pdb = _dense(d_bias, "d_bias", torch.float32, device, (N,))
+    held, ws, size = _workspace(workspace, _linear_backward_need(code, act, M, N, K, xs, gs), x, device)
     st = lib.corr_linear_backward(code, act, _pointer(x), xs, pw, pz, pg, gs, px, pdw, pdb, M, N, K, ws, size, _stream())
     if st != CORR_OK:
         raise CorrError(st, "corr_linear_backward")
-    return d_x, d_w, d_bias
+    return d_x if want_x else None, d_w if want_w else None, d_bias if want_bias else None
 
 
 def _norm_args(h, y, gate, gate_act, scale, h_scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps, dtype):
-    _on_device(h, "h")
-    device = h.device
+    """(arguments, type of the rows beside the stream, device)"""
+    device = _on_device(h, "h")
     rows, cols, hs = _rows(h, "h")
     if y is not None:
         if not isinstance(y, torch.Tensor):
@@ -513,14 +547,17 @@ def _norm_args(h, y, gate, gate_act, scale, h_scale, post, post_weight, post_bia
         dtype = h.dtype
     if dtype not in _TYPES:
         raise TypeError("rows must be float32, bfloat16 or float16")
-    py, ys = _matrix(y, "y", dtype, device, rows, cols)
-    pg, gs = _matrix(gate, "gate", dtype, device, rows, cols)
+    py, ys = (None, 0) if y is None else _matrix(y, "y", dtype, device, rows, cols)
+    pg, gs = (None, 0) if gate is None else _matrix(gate, "gate", dtype, device, rows, cols)
     one = (cols,)
-    ps, pw1, pb1, pw2, pb2 = (None if v is None else _dense(v, name, torch.float32, device, one) for v, name in
-                              ((scale, "scale"), (post_weight, "post_weight"), (post_bias, "post_bias"), (pre_weight, "pre_weight"),
-                               (pre_bias, "pre_bias")))
-    return ResidualNormArgs(_type_of(h, "h"), _TYPES[dtype], rows, cols, _pointer(h), hs, py, ys, pg, gs, gate_act, ps, h_scale,
-                            post, pw1, pb1, pre, pw2, pb2, eps), dtype
+    f32 = torch.float32
+    return ResidualNormArgs(
+        _type_of(h, "h"), _TYPES[dtype], rows, cols, _pointer(h), hs, py, ys, pg, gs, gate_act,
+        None if scale is None else _dense(scale, "scale", f32, device, one), h_scale,
+        post, None if post_weight is None else _dense(post_weight, "post_weight", f32, device, one),
+        None if post_bias is None else _dense(post_bias, "post_bias", f32, device, one),
+        pre, None if pre_weight is None else _dense(pre_weight, "pre_weight", f32, device, one),
+        None if pre_bias is None else _dense(pre_bias, "pre_bias", f32, device, one), eps), dtype, device
 
 
 def corr_residual_norm(h: torch.Tensor, y: torch.Tensor | None = None, gate: torch.Tensor | None = None,
@@ -533,23 +570,26 @@ def corr_residual_norm(h: torch.Tensor, y: torch.Tensor | None = None, gate: tor
         t = h_scale h + scale gate_act(gate) (post(y) post_weight + post_bias),   n = pre(t) pre_weight + pre_bias.
     Returns (t, n): t of h's type (h itself without y), n of y's (of `dtype`, or h's, without y), None for CORR_NORM_NONE.
     h, y, gate: [..., C] with contiguous, evenly spaced rows; vectors: float32 [C].  h_out may be h."""
-    a, dtype = _norm_args(h, y, gate, gate_act, scale, h_scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps, dtype)
-    device = h.device
+    lib = _lib or load_library()
+    a, dtype, device = _norm_args(h, y, gate, gate_act, scale, h_scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps, dtype)
     ph = pn = None
     if y is None:
         if h_out is not None:
             raise ValueError("without y there is no h_out: it is h")
+    elif h_out is None:
+        h_out = _new(h, h.shape, h.dtype)
+        ph = _pointer(h_out)
     else:
-        if h_out is None:
-            h_out = torch.empty(h.shape, dtype=h.dtype, device=device)
         ph = _dense(h_out, "h_out", h.dtype, device, h.shape)
     if pre != CORR_NORM_NONE:
         if n_out is None:
-            n_out = torch.empty(h.shape, dtype=dtype, device=device)
-        pn = _dense(n_out, "n_out", dtype, device, h.shape)
+            n_out = _new(h, h.shape, dtype)
+            pn = _pointer(n_out)
+        else:
+            pn = _dense(n_out, "n_out", dtype, device, h.shape)
     elif n_out is not None:
         raise ValueError("without a norm there is no n_out")
-    st = load_library().corr_residual_norm(ctypes.byref(a), ph, pn, _stream())
+    st = lib.corr_residual_norm(ctypes.byref(a), ph, pn, _stream())
     if st != CORR_OK:
         raise CorrError(st, "corr_residual_norm")
     return (h if y is None else h_out), n_out
@@ -580,24 +620,20 @@ def corr_residual_norm_backward(h: torch.Tensor, y: torch.Tensor | None = None, 
                                 workspace: torch.Tensor | None = None) -> ResidualNormGrads:
     """Gradients at corr_residual_norm's own arguments (its inputs, not its outputs).  d_h_out, d_n_out: the gradients of its two
     results, contiguous; one of them may be None (zero).  Matrices have the type of what they are the gradient of, vectors float32."""
-    lib = load_library()
-    if y is None and d_n_out is not None and isinstance(d_n_out, torch.Tensor):
-        dtype = d_n_out.dtype
-    else:
-        dtype = None
-    a, dtype = _norm_args(h, y, gate, gate_act, scale, h_scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps, dtype)
-    device = h.device
-    pdh = _dense(d_h_out, "d_h_out", h.dtype, device, h.shape)
-    pdn = _dense(d_n_out, "d_n_out", dtype, device, h.shape)
-    if pdh is None and pdn is None:
+    lib = _lib or load_library()
+    dtype = d_n_out.dtype if y is None and isinstance(d_n_out, torch.Tensor) else None
+    a, dtype, device = _norm_args(h, y, gate, gate_act, scale, h_scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps, dtype)
+    if d_h_out is None and d_n_out is None:
         raise ValueError("d_h_out or d_n_out is needed")
-    new = lambda like, kind: None if like is None else torch.empty(like.shape, dtype=kind, device=device)  # noqa: E731
-    g = ResidualNormGrads(new(h, h.dtype), new(y, dtype), new(gate, dtype), *(
-        new(v, torch.float32) for v in (scale, post_weight, post_bias, pre_weight, pre_bias)))
-    ptr = [None if t is None else _pointer(t) for t in g]
-    need = int(lib.corr_residual_norm_backward_workspace_bytes(a.rows, a.cols)) if any(ptr[3:]) else 0
-    held, ws, size = _workspace(workspace, need, device)
-    st = lib.corr_residual_norm_backward(ctypes.byref(a), pdh, pdn, *ptr, ws, size, _stream())
+    pdh = None if d_h_out is None else _dense(d_h_out, "d_h_out", h.dtype, device, h.shape)
+    pdn = None if d_n_out is None else _dense(d_n_out, "d_n_out", dtype, device, h.shape)
+    vectors = [v is not None for v in (scale, post_weight, post_bias, pre_weight, pre_bias)]
+    one = _new(h, (sum(vectors), a.cols), torch.float32).unbind() if any(vectors) else ()
+    each = iter(one)
+    g = ResidualNormGrads(_new(h, h.shape, h.dtype), None if y is None else _new(h, h.shape, dtype),
+                          None if gate is None else _new(h, h.shape, dtype), *[next(each) if there else None for there in vectors])
+    held, ws, size = _workspace(workspace, _norm_backward_need(a.rows, a.cols) if one else 0, h, device)
+    st = lib.corr_residual_norm_backward(ctypes.byref(a), pdh, pdn, *[None if t is None else _pointer(t) for t in g], ws, size, _stream())
     if st != CORR_OK:
         raise CorrError(st, "corr_residual_norm_backward")
     return g

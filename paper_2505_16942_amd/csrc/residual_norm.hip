@@ -1,15 +1,38 @@
 // Norms before and after a block, with the block's gate, its scale and the residual, and their gradient:
 //   p = norm1(y) w1 + b1,   t = alpha h + s act(g) p   (h_out),   n = norm2(t) w2 + b2.
-// A row's elements stay in the registers of G threads from its only load to its only store; sums over a row go through the
-// lanes of a wave and, for rows that need more than a wave, LDS.  Means and squares in fp32; the layer norm subtracts the mean
-// before it squares.  The gradient makes the forward pass's row again from the forward pass's inputs (as many bytes as
-// reading saved ones) and keeps the sums over rows of its columns in registers from row to row.
+// A row's elements stay in the registers of G threads from its only load to its only store; the next row's are on their way
+// meanwhile.  Sums over a row go through the lanes of a wave and, for rows that need more than a wave, LDS.  Means and squares in
+// fp32; the layer norm subtracts the mean before it squares.  The gradient makes the forward pass's row again from the
+// forward pass's inputs (as many bytes as reading saved ones) and keeps the sums over rows of its columns in registers from row to row.
 #include "rows_internal.h"
 
 namespace {
 
 enum { V_SCALE, V_W1, V_B1, V_W2, V_B2, VECTORS };
 
+template <int CTRL> __device__ __forceinline__ float dpp(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, false));
+}
+// Sum over aligned groups of W lanes, in every lane: neighbours, pairs, quads and eights by lane permutations inside the add,
+// 16 and 32 lanes by exchanging rows of the wave with itself.
+template <int W> __device__ __forceinline__ float lane_sum(float x) {
+    if constexpr (W >= 2) x += dpp<0xB1>(x);             // quad_perm 1 0 3 2
+    if constexpr (W >= 4) x += dpp<0x4E>(x);             // quad_perm 2 3 0 1
+    if constexpr (W >= 8) x += dpp<0x141>(x);            // row_half_mirror
+    if constexpr (W >= 16) x += dpp<0x140>(x);           // row_mirror
+    // (the casts matter: __builtin_bit_cast of a vector's element takes its first)
+    if constexpr (W >= 32) {
+        const unsigned u = __builtin_bit_cast(unsigned, x);
+        const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+        x = __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+    }
+    if constexpr (W >= 64) {
+        const unsigned u = __builtin_bit_cast(unsigned, x);
+        const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+        x = __builtin_bit_cast(float, (unsigned)r[0]) + __builtin_bit_cast(float, (unsigned)r[1]);
+    }
+    return x;
+}
 // Sums over the G threads of a row.  Waves of one row add up in LDS (two buffers in turn: a wave may be one sum ahead of
 // another, never two).
 template <int G>
@@ -17,38 +40,53 @@ struct RowSum {
     float2* lds;
     int turn;
     __device__ __forceinline__ float2 operator()(float x, float y) {
-        constexpr int WIDTH = G < 64 ? G : 64;
-#pragma unroll
-        for (int d = WIDTH / 2; d > 0; d >>= 1) {
-            x += __shfl_xor(x, d);
-            y += __shfl_xor(y, d);
-        }
+        x = lane_sum<(G < 64 ? G : 64)>(x);
+        y = lane_sum<(G < 64 ? G : 64)>(y);
         if constexpr (G > 64) {
             constexpr int WAVES = G / 64;
             float2* const b = lds + (turn ^= 1) * WAVES;
             if ((threadIdx.x & 63) == 0) b[threadIdx.x >> 6] = make_float2(x, y);
             __syncthreads();
-            x = y = 0.f;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) { x += b[w].x; y += b[w].y; }
+            const float2 v = b[threadIdx.x % WAVES];
+            x = lane_sum<WAVES>(v.x);
+            y = lane_sum<WAVES>(v.y);
         }
         return make_float2(x, y);
     }
+    __device__ __forceinline__ float operator()(float x) {
+        if constexpr (G > 64) return (*this)(x, 0.f).x;
+        else return lane_sum<G>(x);
+    }
 };
 
-// E elements of a row per thread, in pieces of V: element e of thread j is column ((e / V) * G + j) * V + e % V.
+// E elements of a row per thread, in pieces of V: element e of thread j is column ((e / V) * G + j) * V + e % V.  A piece is
+// inside the row or outside it as a whole.
+template <class T, int E, int V> struct Raw { typename RowVec<T, V>::type v[E / V]; };
 template <int G, int E, int V>
 struct Cols {
     int j, C;
     __device__ __forceinline__ int at(int piece) const { return (piece * G + j) * V; }
-    template <class T> __device__ __forceinline__ void load(const T* row, float (&v)[E]) const {
+    __device__ __forceinline__ bool in(int e) const { return at(e / V) < C; }
+    template <class T> __device__ __forceinline__ void ask(const T* row, Raw<T, E, V>& r) const {
 #pragma unroll
         for (int q = 0; q < E / V; ++q) {
-            float x[V] = {};
-            if (at(q) < C) row_load<T, V>(row + at(q), x);
-#pragma unroll
-            for (int e = 0; e < V; ++e) v[q * V + e] = x[e];
+            r.v[q] = {};
+            if (at(q) < C) r.v[q] = *reinterpret_cast<const typename RowVec<T, V>::type*>(row + at(q));
         }
+    }
+    template <class T> __device__ __forceinline__ void open(const Raw<T, E, V>& r, float (&v)[E]) const {
+#pragma unroll
+        for (int q = 0; q < E / V; ++q)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                if constexpr (V == 1) v[q] = (float)r.v[q];
+                else v[q * V + e] = (float)r.v[q][e];
+            }
+    }
+    template <class T> __device__ __forceinline__ void load(const T* row, float (&v)[E]) const {
+        Raw<T, E, V> r;
+        ask(row, r);
+        open(r, v);
     }
     template <class T> __device__ __forceinline__ void store(T* row, const float (&v)[E]) const {
 #pragma unroll
@@ -66,7 +104,6 @@ struct Cols {
 #pragma unroll
             for (int e = 0; e < E; ++e) v[e] = none;
     }
-    __device__ __forceinline__ bool in(int e) const { return at(e / V) < C; }
 };
 
 // v becomes the normalised row; returns 1 / its spread (1 for CORR_NORM_NONE).  Elements past the row's end stay zero.
@@ -77,14 +114,14 @@ __device__ __forceinline__ float normalise(int kind, float (&v)[E], const Cols<G
         float m = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) m += v[e];
-        const float mean = sum(m, 0.f).x * inv;
+        const float mean = sum(m) * inv;
 #pragma unroll
         for (int e = 0; e < E; ++e) v[e] = c.in(e) ? v[e] - mean : 0.f;
     }
     float q = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) q = fmaf(v[e], v[e], q);
-    const float rho = 1.f / sqrtf(sum(q, 0.f).x * inv + eps);
+    const float rho = 1.f / sqrtf(sum(q) * inv + eps);
 #pragma unroll
     for (int e = 0; e < E; ++e) v[e] *= rho;
     return rho;
@@ -96,17 +133,26 @@ __device__ __forceinline__ void normalise_back(int kind, float (&q)[E], const fl
     if (kind == CORR_NORM_NONE) return;
     float a = 0.f, b = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) { a = fmaf(q[e], hat[e], a); b += q[e]; }
-    const float2 s = sum(a, b);
-    const float along = s.x * inv, mean = kind == CORR_NORM_LAYER ? s.y * inv : 0.f;
+    for (int e = 0; e < E; ++e) a = fmaf(q[e], hat[e], a);
+    if (kind == CORR_NORM_LAYER) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) q[e] = c.in(e) ? rho * (q[e] - mean - hat[e] * along) : 0.f;
+        for (int e = 0; e < E; ++e) b += q[e];
+        const float2 s = sum(a, b);
+        a = s.x * inv;
+        b = s.y * inv;
+#pragma unroll
+        for (int e = 0; e < E; ++e) q[e] = c.in(e) ? rho * (q[e] - b - hat[e] * a) : 0.f;
+    } else {
+        a = sum(a) * inv;
+#pragma unroll
+        for (int e = 0; e < E; ++e) q[e] = rho * (q[e] - hat[e] * a);
+    }
 }
 
 template <class S, class T, int G, int E, int V>
 __global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_kernel(NormArgs n) {
     constexpr int THREADS = G < 256 ? 256 : G, GROUPS = THREADS / G;
-    constexpr bool KEEP = E <= 8;                        // vectors stay in registers from row to row
+    constexpr bool KEEP = G < 1024, AHEAD = E <= 8 && (G < 1024 || V > 1);      // vectors stay in registers from row to row
     __shared__ float2 lds[G > 64 ? 2 * (G / 64) : 1];
     const corr_residual_norm_args& a = n.a;
     const Cols<G, E, V> c = {(int)threadIdx.x % G, (int)a.cols};
@@ -118,14 +164,25 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_kernel(NormAr
         c.vector(a.post_weight, 1.f, w1); c.vector(a.post_bias, 0.f, b1);
         c.vector(a.pre_weight, 1.f, w2); c.vector(a.pre_bias, 0.f, b2);
     }
-    for (int64_t r = (int64_t)blockIdx.x * GROUPS + threadIdx.x / G; r < a.rows; r += (int64_t)gridDim.x * GROUPS) {
-        float t[E];
-        c.load((const S*)a.h + r * a.h_stride, t);
+    Raw<S, E, V> rh;
+    Raw<T, E, V> ry, rg;
+    auto ask = [&](int64_t r) {
+        if (r >= a.rows) return;
+        c.ask((const S*)a.h + r * a.h_stride, rh);
+        if (a.y) c.ask((const T*)a.y + r * a.y_stride, ry);
+        if (a.gate) c.ask((const T*)a.gate + r * a.gate_stride, rg);
+    };
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
+    int64_t r = (int64_t)blockIdx.x * GROUPS + threadIdx.x / G;
+    if (AHEAD) ask(r);
+    for (; r < a.rows; r += step) {
+        if (!AHEAD) ask(r);
+        float t[E], p[E], g[E];
+        c.open(rh, t);
+        if (a.y) c.open(ry, p);
+        if (a.gate) c.open(rg, g);
+        if (AHEAD) ask(r + step);
         if (a.y) {
-            float p[E];
-            c.load((const T*)a.y + r * a.y_stride, p);
-            float g[E];
-            if (a.gate) c.load((const T*)a.gate + r * a.gate_stride, g);
             normalise(a.post, p, c, inv, a.eps, sum);
             if (!KEEP) { c.vector(a.post_weight, 1.f, w1); c.vector(a.post_bias, 0.f, b1); c.vector(a.scale, 1.f, s); }
 #pragma unroll
@@ -149,11 +206,12 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_kernel(NormAr
     }
 }
 
-// Rows past 8192 columns leave no registers for the columns' sums: they are added up in the workgroup's own part, in memory.
-template <class S, class T, int G, int E, int V>
+// FULL: sums for all five vectors; else for the two weights alone (no scale, no biases), which leaves registers.  Rows past 8192
+// columns leave none for the columns' sums: they are added up in the workgroup's own part, in memory.
+template <class S, class T, bool FULL, int G, int E, int V>
 __global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_backward_kernel(NormArgs n) {
     constexpr int THREADS = G < 256 ? 256 : G, GROUPS = THREADS / G;
-    constexpr bool KEEP = E <= 4, IN_MEMORY = E > 8 && G >= 1024;
+    constexpr bool IN_MEMORY = E > 8 && G >= 1024, KEEP = E <= 8 && (G <= 256 || !FULL), AHEAD = G < 1024 || (!FULL && E <= 8);
     __shared__ float2 lds[G > 64 ? 2 * (G / 64) : 1];
     __shared__ float join[GROUPS > 1 ? (GROUPS - 1) * G * E : 1];
     const corr_residual_norm_args& a = n.a;
@@ -162,11 +220,12 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_backward_kern
     const float inv = 1.f / (float)a.cols;
     RowSum<G> sum = {lds, 0};
     float s[E], w1[E], b1[E], w2[E];
-    if (KEEP) {
-        c.vector(a.scale, 1.f, s);
-        c.vector(a.post_weight, 1.f, w1); c.vector(a.post_bias, 0.f, b1);
-        c.vector(a.pre_weight, 1.f, w2);
-    }
+    auto block_vectors = [&] {
+        c.vector(a.post_weight, 1.f, w1);
+        if (FULL) { c.vector(a.scale, 1.f, s); c.vector(a.post_bias, 0.f, b1); }
+    };
+    if (KEEP) { block_vectors(); c.vector(a.pre_weight, 1.f, w2); }
+    auto branch = [&](int e, float hat) { return FULL ? fmaf(hat, w1[e], b1[e]) : hat * w1[e]; };
     float* const part = n.part ? n.part + (int64_t)blockIdx.x * VECTORS * a.cols : nullptr;
     float acc[IN_MEMORY ? 1 : VECTORS][E] = {};
     bool first = true;
@@ -184,76 +243,89 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_backward_kern
             for (int e = 0; e < E; ++e) acc[v][e] += value(e);
         }
     };
-    for (int64_t r = (int64_t)blockIdx.x * GROUPS + group; r < a.rows; r += (int64_t)gridDim.x * GROUPS) {
-        float t[E], p[E], g[E], D[E];
-        c.load((const S*)a.h + r * a.h_stride, t);
+    Raw<S, E, V> rh, rdh;
+    Raw<T, E, V> ry, rg, rdn;
+    auto ask = [&](int64_t r) {
+        if (r >= a.rows) return;
+        c.ask((const S*)a.h + r * a.h_stride, rh);
+        if (a.y) c.ask((const T*)a.y + r * a.y_stride, ry);
+        if (a.gate) c.ask((const T*)a.gate + r * a.gate_stride, rg);
+        if (n.d_n_out) c.ask((const T*)n.d_n_out + r * a.cols, rdn);
+        if (n.d_h_out) c.ask((const S*)n.d_h_out + r * a.cols, rdh);
+    };
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
+    int64_t r = (int64_t)blockIdx.x * GROUPS + group;
+    if (AHEAD) ask(r);
+    for (; r < a.rows; r += step) {
+        if (!AHEAD) ask(r);
+        float t[E], p[E], g[E], D[E], x[E];              // g becomes act'(g), x act(g); t the normalised row, then act(g)
+        c.open(rh, t);
+        if (a.y) c.open(ry, p);
+        if (a.gate) c.open(rg, g);
+        if (n.d_n_out) c.open(rdn, D);
+        Raw<S, E, V> now = rdh;
+        if (AHEAD) ask(r + step);
         float rho1 = 1.f;
-        if (a.y) {
-            c.load((const T*)a.y + r * a.y_stride, p);
-            if (a.gate) c.load((const T*)a.gate + r * a.gate_stride, g);
+        if (a.gate) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = g[e];
+            row_act_all(a.gate_act, x);
+            row_slope_all(a.gate_act, g);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = 1.f;
         }
-        if (n.d_n_out) c.load((const T*)n.d_n_out + r * a.cols, D);
         if (a.y) {
             rho1 = normalise(a.post, p, c, inv, a.eps, sum);
-            if (!KEEP) { c.vector(a.post_weight, 1.f, w1); c.vector(a.post_bias, 0.f, b1); c.vector(a.scale, 1.f, s); }
+            if (!KEEP) block_vectors();
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const float u = fmaf(p[e], w1[e], b1[e]) * s[e] * (a.gate ? row_act(a.gate_act, g[e]) : 1.f);
+                const float u = branch(e, p[e]) * (FULL ? s[e] * x[e] : x[e]);
                 t[e] = c.in(e) ? fmaf(a.h_scale, t[e], u) : 0.f;
             }
         }
         if (n.d_n_out) {
             const float rho2 = normalise(a.pre, t, c, inv, a.eps, sum);
             if (a.pre_weight) add(V_W2, [&](int e) { return D[e] * t[e]; });
-            if (a.pre_bias) add(V_B2, [&](int e) { return D[e]; });
+            if (FULL && a.pre_bias) add(V_B2, [&](int e) { return D[e]; });
             if (!KEEP) c.vector(a.pre_weight, 1.f, w2);
 #pragma unroll
             for (int e = 0; e < E; ++e) D[e] *= w2[e];
             normalise_back(a.pre, D, t, rho2, c, inv, sum);
             if (n.d_h_out) {
-                float x[E];
-                c.load((const S*)n.d_h_out + r * a.cols, x);
+                c.open(now, t);
 #pragma unroll
-                for (int e = 0; e < E; ++e) D[e] += x[e];
+                for (int e = 0; e < E; ++e) D[e] += t[e];
             }
         } else {
-            c.load((const S*)n.d_h_out + r * a.cols, D);
+            c.open(now, D);
             if (IN_MEMORY && first) {                    // nothing reaches these: zeros
                 add(V_W2, [](int) { return 0.f; });
                 add(V_B2, [](int) { return 0.f; });
             }
         }
-        const float alpha = a.y ? a.h_scale : 1.f;
         if (n.d_h) {
-            float x[E];
+            const float alpha = a.y ? a.h_scale : 1.f;
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[e] = alpha * D[e];
-            c.store((S*)n.d_h + r * a.cols, x);
+            for (int e = 0; e < E; ++e) t[e] = alpha * D[e];
+            c.store((S*)n.d_h + r * a.cols, t);
         }
         if (a.y) {
-            // from here on t holds act(g), D the gradient of s act(g) p
-            if (a.gate) {
-#pragma unroll
-                for (int e = 0; e < E; ++e) t[e] = row_act(a.gate_act, g[e]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e) t[e] = 1.f;
-            }
-            if (a.scale) {
-                add(V_SCALE, [&](int e) { return D[e] * t[e] * fmaf(p[e], w1[e], b1[e]); });
+            // D becomes the gradient of act(g) p, then of p, then of the normalised y
+            if (FULL && a.scale) {
+                add(V_SCALE, [&](int e) { return D[e] * x[e] * branch(e, p[e]); });
 #pragma unroll
                 for (int e = 0; e < E; ++e) D[e] *= s[e];
             }
             if (n.d_gate) {
-                float x[E];
 #pragma unroll
-                for (int e = 0; e < E; ++e) x[e] = D[e] * fmaf(p[e], w1[e], b1[e]) * row_act_slope(a.gate_act, g[e]);
-                c.store((T*)n.d_gate + r * a.cols, x);
+                for (int e = 0; e < E; ++e) t[e] = D[e] * branch(e, p[e]) * g[e];
+                c.store((T*)n.d_gate + r * a.cols, t);
             }
 #pragma unroll
-            for (int e = 0; e < E; ++e) D[e] *= t[e];
+            for (int e = 0; e < E; ++e) D[e] *= x[e];
             if (a.post_weight) add(V_W1, [&](int e) { return D[e] * p[e]; });
-            if (a.post_bias) add(V_B1, [&](int e) { return D[e]; });
+            if (FULL && a.post_bias) add(V_B1, [&](int e) { return D[e]; });
 #pragma unroll
             for (int e = 0; e < E; ++e) D[e] *= w1[e];
             normalise_back(a.post, D, p, rho1, c, inv, sum);
@@ -265,6 +337,7 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_backward_kern
     if constexpr (!IN_MEMORY) {
 #pragma unroll
         for (int v = 0; v < VECTORS; ++v) {
+            if (!FULL && v != V_W1 && v != V_W2) continue;
             if constexpr (GROUPS > 1) {
                 __syncthreads();
                 if (group) {
@@ -282,37 +355,38 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_backward_kern
     }
 }
 
-// Rows of up to `cols` columns in pieces of V.
-template <class S, class T, bool BACK, int G, int E, int V>
+template <class S, class T, bool BACK, bool FULL, int G, int E, int V>
 void run(const NormArgs& n, hipStream_t s) {
     constexpr int THREADS = G < 256 ? 256 : G, GROUPS = THREADS / G;
-    const int64_t need = (n.a.rows + GROUPS - 1) / GROUPS;
-    if (BACK) hipLaunchKernelGGL((residual_norm_backward_kernel<S, T, G, E, V>), dim3(n.parts), dim3(THREADS), 0, s, n);
+    if constexpr (BACK) hipLaunchKernelGGL((residual_norm_backward_kernel<S, T, FULL, G, E, V>), dim3(n.parts), dim3(THREADS), 0, s, n);
     else {
-        const int64_t most = 2048 * 256 / THREADS;
+        const int64_t need = (n.a.rows + GROUPS - 1) / GROUPS, most = 2048 * 256 / THREADS;
         hipLaunchKernelGGL((residual_norm_kernel<S, T, G, E, V>), dim3((unsigned)(need < most ? need : most)), dim3(THREADS), 0, s, n);
     }
 }
-template <class S, class T, bool BACK>
+template <class S, class T, bool BACK, bool FULL>
 void run(const NormArgs& n, bool wide, hipStream_t s) {
     const int64_t C = n.a.cols;
     if (wide) {
-        if (C <= 64) run<S, T, BACK, 16, 4, 4>(n, s);
-        else if (C <= 256) run<S, T, BACK, 64, 4, 4>(n, s);
-        else if (C <= 512) run<S, T, BACK, 64, 8, 8>(n, s);
-        else if (C <= 1024) run<S, T, BACK, 256, 4, 4>(n, s);
-        else if (C <= 2048) run<S, T, BACK, 256, 8, 8>(n, s);
-        else if (C <= 4096) run<S, T, BACK, 512, 8, 8>(n, s);
-        else if (C <= 8192) run<S, T, BACK, 1024, 8, 8>(n, s);
-        else run<S, T, BACK, 1024, 16, 8>(n, s);
+        if (C <= 64) run<S, T, BACK, FULL, 8, 8, 8>(n, s);
+        else if (C <= 256) run<S, T, BACK, FULL, 32, 8, 8>(n, s);
+        else if (C <= 512) run<S, T, BACK, FULL, 64, 8, 8>(n, s);
+        else if (C <= 2048) run<S, T, BACK, FULL, 256, 8, 8>(n, s);
+        else if (C <= 4096) run<S, T, BACK, FULL, 512, 8, 8>(n, s);
+        else if (C <= 8192) {
+            if constexpr (BACK && FULL) run<S, T, BACK, FULL, 512, 16, 8>(n, s);
+            else run<S, T, BACK, FULL, 1024, 8, 8>(n, s);
+        } else run<S, T, BACK, FULL, 1024, 16, 8>(n, s);
     } else {
-        if (C <= 256) run<S, T, BACK, 64, 4, 1>(n, s);
-        else if (C <= 1024) run<S, T, BACK, 256, 4, 1>(n, s);
-        else if (C <= 8192) run<S, T, BACK, 1024, 8, 1>(n, s);
-        else run<S, T, BACK, 1024, 16, 1>(n, s);
+        if (C <= 256) run<S, T, BACK, FULL, 32, 8, 1>(n, s);
+        else if (C <= 2048) run<S, T, BACK, FULL, 256, 8, 1>(n, s);
+        else if (C <= 8192) {
+            if constexpr (BACK && FULL) run<S, T, BACK, FULL, 512, 16, 1>(n, s);
+            else run<S, T, BACK, FULL, 1024, 8, 1>(n, s);
+        } else run<S, T, BACK, FULL, 1024, 16, 1>(n, s);
     }
 }
-template <bool BACK>
+template <bool BACK, bool FULL>
 hipError_t launch(const NormArgs& n, hipStream_t s) {
     const corr_residual_norm_args& a = n.a;
     // eight elements at once: rows of whole pieces that start on the border of every access (16 bytes, the widest)
@@ -321,20 +395,22 @@ hipError_t launch(const NormArgs& n, hipStream_t s) {
                           (uintptr_t)n.d_h_out | (uintptr_t)n.d_n_out | (uintptr_t)n.d_h | (uintptr_t)n.d_y | (uintptr_t)n.d_gate;
     const bool wide = (all & 15) == 0 && ((a.cols | a.h_stride | a.y_stride | a.gate_stride) & 7) == 0;
     if (a.stream_type == CORR_TYPE_F32) {
-        if (a.type == CORR_TYPE_F32) run<float, float, BACK>(n, wide, s);
-        else if (a.type == CORR_TYPE_BF16) run<float, __bf16, BACK>(n, wide, s);
-        else run<float, _Float16, BACK>(n, wide, s);
-    } else if (a.type == CORR_TYPE_BF16) run<__bf16, __bf16, BACK>(n, wide, s);
-    else run<_Float16, _Float16, BACK>(n, wide, s);
+        if (a.type == CORR_TYPE_F32) run<float, float, BACK, FULL>(n, wide, s);
+        else if (a.type == CORR_TYPE_BF16) run<float, __bf16, BACK, FULL>(n, wide, s);
+        else run<float, _Float16, BACK, FULL>(n, wide, s);
+    } else if (a.type == CORR_TYPE_BF16) run<__bf16, __bf16, BACK, FULL>(n, wide, s);
+    else run<_Float16, _Float16, BACK, FULL>(n, wide, s);
     return hipGetLastError();
 }
 
 }  // namespace
 
 int norm_backward_parts(int64_t rows, int64_t cols) {
-    const int64_t per = cols <= 64 ? 16 : cols <= 512 ? 4 : 1;      // rows a workgroup has at a time (a lower bound)
-    const int64_t most = cols <= 1024 ? 1024 : 512, need = (rows + per - 1) / per;
+    const int64_t per = cols <= 64 ? 32 : cols <= 256 ? 8 : cols <= 512 ? 4 : 1;      // the most rows a workgroup has at a time
+    const int64_t most = cols <= 512 ? 768 : 512, need = (rows + per - 1) / per;
     return (int)(need < most ? need : most);
 }
-hipError_t launch_residual_norm(const NormArgs& n, hipStream_t s) { return launch<false>(n, s); }
-hipError_t launch_residual_norm_backward(const NormArgs& n, hipStream_t s) { return launch<true>(n, s); }
+hipError_t launch_residual_norm(const NormArgs& n, hipStream_t s) { return launch<false, true>(n, s); }
+hipError_t launch_residual_norm_backward(const NormArgs& n, hipStream_t s) {
+    return n.a.scale || n.a.post_bias || n.a.pre_bias ? launch<true, true>(n, s) : launch<true, false>(n, s);
+}

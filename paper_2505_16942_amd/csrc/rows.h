@@ -25,7 +25,7 @@ __device__ __forceinline__ float row_gelu_2u(float z) { return 1.595769121605730
 __device__ __forceinline__ float row_normal(float z, float& tail) {
     const float x = fabsf(z) * 0.70710678118654752f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
     tail = row_exp(-x * x);
-    float q = fmaf(t, 0.5305027145f, -0.7265760135f);
+    float q = fmaf(t, 0.5307027145f, -0.7265760135f);
     q = fmaf(t, q, 0.7107068705f);
     q = fmaf(t, q, -0.142248368f);
     q = fmaf(t, q, 0.127414796f) * t * tail;
