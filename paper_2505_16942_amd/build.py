@@ -15,7 +15,9 @@ OBJ_DIR = os.path.join(PKG, "_build")
 # compilations first)
 SOURCES = [("block.hip", "block_r%d_c%d.o" % (r, nc), ["-DCORR_BLOCK_R=%d" % r, "-DCORR_BLOCK_NC=%d" % nc])
            for nc in (8, 5, 4, 6, 3) for r in (4, 3, 2, 1)]
-SOURCES += [(f + ".hip", f + ".o", []) for f in ("linear", "residual_norm", "rows", "rows_api")]
+# residual_norm.hip once per pair of types
+SOURCES += [("residual_norm.hip", "residual_norm_%d.o" % k, ["-DCORR_NORM_PAIR=%d" % k]) for k in range(5)]
+SOURCES += [(f + ".hip", f + ".o", []) for f in ("linear", "rows", "rows_api")]
 SOURCES += [("corr_api.hip", "corr_api.o", []), ("features.hip", "features.o", []), ("binning.hip", "binning.o", []),
             ("ondemand.hip", "ondemand.o", []), ("fullvol.hip", "fullvol.o", []), ("backward.hip", "backward.o", [])]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -59,42 +59,49 @@ struct RowSum {
     }
 };
 
-// E elements of a row per thread, in pieces of V: element e of thread j is column ((e / V) * G + j) * V + e % V.  A piece is
-// inside the row or outside it as a whole.
-template <class T, int E, int V> struct Raw { typename RowVec<T, V>::type v[E / V]; };
-template <int G, int E, int V>
+// E elements of a row per thread, in pieces of V = 8: element e of thread j is column ((e / V) * G + j) * V + e % V.  RAGGED: rows
+// that start on their elements' borders alone and may end inside a piece; else a piece is whole, on 16-byte borders.
+constexpr int V = 8;
+template <class T, bool RAGGED> struct Piece { typedef typename RowVec<T, V>::value value; typedef value type __attribute__((aligned(RAGGED ? sizeof(T) : 16))); };
+template <class T, int E> struct Raw { typename RowVec<T, V>::value v[E / V]; };
+template <int G, int E, bool RAGGED>
 struct Cols {
     int j, C;
     __device__ __forceinline__ int at(int piece) const { return (piece * G + j) * V; }
-    __device__ __forceinline__ bool in(int e) const { return at(e / V) < C; }
-    template <class T> __device__ __forceinline__ void ask(const T* row, Raw<T, E, V>& r) const {
+    __device__ __forceinline__ bool in(int e) const { return at(e / V) + (RAGGED ? e % V : 0) < C; }
+    __device__ __forceinline__ bool whole(int piece) const { return at(piece) + (RAGGED ? V - 1 : 0) < C; }
+    template <class T> __device__ __forceinline__ void ask(const T* row, Raw<T, E>& r) const {
 #pragma unroll
         for (int q = 0; q < E / V; ++q) {
             r.v[q] = {};
-            if (at(q) < C) r.v[q] = *reinterpret_cast<const typename RowVec<T, V>::type*>(row + at(q));
+            if (whole(q)) r.v[q] = *reinterpret_cast<const typename Piece<T, RAGGED>::type*>(row + at(q));
+            else if (RAGGED) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) if (at(q) + e < C) r.v[q][e] = row[at(q) + e];
+            }
         }
     }
-    template <class T> __device__ __forceinline__ void open(const Raw<T, E, V>& r, float (&v)[E]) const {
+    template <class T> __device__ __forceinline__ void open(const Raw<T, E>& r, float (&v)[E]) const {
 #pragma unroll
-        for (int q = 0; q < E / V; ++q)
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                if constexpr (V == 1) v[q] = (float)r.v[q];
-                else v[q * V + e] = (float)r.v[q][e];
-            }
+        for (int e = 0; e < E; ++e) v[e] = (float)r.v[e / V][e % V];
     }
     template <class T> __device__ __forceinline__ void load(const T* row, float (&v)[E]) const {
-        Raw<T, E, V> r;
+        Raw<T, E> r;
         ask(row, r);
         open(r, v);
     }
     template <class T> __device__ __forceinline__ void store(T* row, const float (&v)[E]) const {
 #pragma unroll
         for (int q = 0; q < E / V; ++q) {
-            float x[V];
+            if (whole(q)) {
+                typename Piece<T, RAGGED>::value x;
 #pragma unroll
-            for (int e = 0; e < V; ++e) x[e] = v[q * V + e];
-            if (at(q) < C) row_store<T, V>(row + at(q), x);
+                for (int e = 0; e < V; ++e) x[e] = (T)v[q * V + e];
+                *reinterpret_cast<typename Piece<T, RAGGED>::type*>(row + at(q)) = x;
+            } else if (RAGGED) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) if (at(q) + e < C) row[at(q) + e] = (T)v[q * V + e];
+            }
         }
     }
     // a vector of parameters; `none` where there is none
@@ -105,10 +112,11 @@ struct Cols {
             for (int e = 0; e < E; ++e) v[e] = none;
     }
 };
+constexpr int threads_of(int G) { return G < 128 ? 256 : G; }
 
 // v becomes the normalised row; returns 1 / its spread (1 for CORR_NORM_NONE).  Elements past the row's end stay zero.
-template <int G, int E, int V>
-__device__ __forceinline__ float normalise(int kind, float (&v)[E], const Cols<G, E, V>& c, float inv, float eps, RowSum<G>& sum) {
+template <int G, int E, bool RAGGED>
+__device__ __forceinline__ float normalise(int kind, float (&v)[E], const Cols<G, E, RAGGED>& c, float inv, float eps, RowSum<G>& sum) {
     if (kind == CORR_NORM_NONE) return 1.f;
     if (kind == CORR_NORM_LAYER) {
         float m = 0.f;
@@ -127,8 +135,8 @@ __device__ __forceinline__ float normalise(int kind, float (&v)[E], const Cols<G
     return rho;
 }
 // q, the gradient of the normalised row `hat`, becomes the gradient of the row.
-template <int G, int E, int V>
-__device__ __forceinline__ void normalise_back(int kind, float (&q)[E], const float (&hat)[E], float rho, const Cols<G, E, V>& c, float inv,
+template <int G, int E, bool RAGGED>
+__device__ __forceinline__ void normalise_back(int kind, float (&q)[E], const float (&hat)[E], float rho, const Cols<G, E, RAGGED>& c, float inv,
                                                RowSum<G>& sum) {
     if (kind == CORR_NORM_NONE) return;
     float a = 0.f, b = 0.f;
@@ -149,13 +157,13 @@ __device__ __forceinline__ void normalise_back(int kind, float (&q)[E], const fl
     }
 }
 
-template <class S, class T, int G, int E, int V>
-__global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_kernel(NormArgs n) {
-    constexpr int THREADS = G < 256 ? 256 : G, GROUPS = THREADS / G;
-    constexpr bool KEEP = G < 1024, AHEAD = E <= 8 && (G < 1024 || V > 1);      // vectors stay in registers from row to row
+template <class S, class T, bool RAGGED, int G, int E>
+__global__ __launch_bounds__(threads_of(G)) void residual_norm_kernel(NormArgs n) {
+    constexpr int GROUPS = threads_of(G) / G;
+    constexpr bool KEEP = G < 1024, AHEAD = E <= V;      // vectors stay in registers from row to row; the next row is asked for early
     __shared__ float2 lds[G > 64 ? 2 * (G / 64) : 1];
     const corr_residual_norm_args& a = n.a;
-    const Cols<G, E, V> c = {(int)threadIdx.x % G, (int)a.cols};
+    const Cols<G, E, RAGGED> c = {(int)threadIdx.x % G, (int)a.cols};
     const float inv = 1.f / (float)a.cols;
     RowSum<G> sum = {lds, 0};
     float s[E], w1[E], b1[E], w2[E], b2[E];
@@ -164,8 +172,8 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_kernel(NormAr
         c.vector(a.post_weight, 1.f, w1); c.vector(a.post_bias, 0.f, b1);
         c.vector(a.pre_weight, 1.f, w2); c.vector(a.pre_bias, 0.f, b2);
     }
-    Raw<S, E, V> rh;
-    Raw<T, E, V> ry, rg;
+    Raw<S, E> rh;
+    Raw<T, E> ry, rg;
     auto ask = [&](int64_t r) {
         if (r >= a.rows) return;
         c.ask((const S*)a.h + r * a.h_stride, rh);
@@ -184,9 +192,15 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_kernel(NormAr
         if (AHEAD) ask(r + step);
         if (a.y) {
             normalise(a.post, p, c, inv, a.eps, sum);
-            if (!KEEP) { c.vector(a.post_weight, 1.f, w1); c.vector(a.post_bias, 0.f, b1); c.vector(a.scale, 1.f, s); }
+            if (!KEEP) c.vector(a.post_weight, 1.f, w1);
 #pragma unroll
-            for (int e = 0; e < E; ++e) p[e] = fmaf(p[e], w1[e], b1[e]) * s[e];
+            for (int e = 0; e < E; ++e) p[e] *= w1[e];
+            if (!KEEP) c.vector(a.post_bias, 0.f, w1);
+#pragma unroll
+            for (int e = 0; e < E; ++e) p[e] += KEEP ? b1[e] : w1[e];
+            if (!KEEP) c.vector(a.scale, 1.f, w1);
+#pragma unroll
+            for (int e = 0; e < E; ++e) p[e] *= KEEP ? s[e] : w1[e];
             if (a.gate) {
                 row_act_all(a.gate_act, g);
 #pragma unroll
@@ -198,34 +212,53 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_kernel(NormAr
         }
         if (a.pre != CORR_NORM_NONE) {
             normalise(a.pre, t, c, inv, a.eps, sum);
-            if (!KEEP) { c.vector(a.pre_weight, 1.f, w2); c.vector(a.pre_bias, 0.f, b2); }
+            if (!KEEP) c.vector(a.pre_weight, 1.f, w2);
 #pragma unroll
-            for (int e = 0; e < E; ++e) t[e] = fmaf(t[e], w2[e], b2[e]);
+            for (int e = 0; e < E; ++e) t[e] *= w2[e];
+            if (!KEEP) c.vector(a.pre_bias, 0.f, w2);
+#pragma unroll
+            for (int e = 0; e < E; ++e) t[e] += KEEP ? b2[e] : w2[e];
             c.store((T*)n.n_out + r * a.cols, t);
         }
     }
 }
 
-// FULL: sums for all five vectors; else for the two weights alone (no scale, no biases), which leaves registers.  Rows past 8192
-// columns leave none for the columns' sums: they are added up in the workgroup's own part, in memory.
-template <class S, class T, bool FULL, int G, int E, int V>
-__global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_backward_kernel(NormArgs n) {
-    constexpr int THREADS = G < 256 ? 256 : G, GROUPS = THREADS / G;
-    constexpr bool IN_MEMORY = E > 8 && G >= 1024, KEEP = E <= 8 && (G <= 256 || !FULL), AHEAD = G < 1024 || (!FULL && E <= 8);
+// FULL: sums for all five vectors; else for the two weights alone (no scale, no biases), which leaves registers.  Rows of a
+// thousand threads (more than 4096 columns) leave few: the normalised y waits in LDS, and vectors and the gate are read again.
+// Past 8192 columns there are none for the columns' sums: they are added up in the workgroup's own part, in memory.
+template <class S, class T, bool RAGGED, bool FULL, int G, int E>
+__global__ __launch_bounds__(threads_of(G)) void residual_norm_backward_kernel(NormArgs n) {
+    constexpr int GROUPS = threads_of(G) / G;
+    constexpr bool TIGHT = G >= 1024, IN_MEMORY = TIGHT && E > V, AHEAD = !TIGHT, KEEP = !TIGHT && (G <= 256 || !FULL);
     __shared__ float2 lds[G > 64 ? 2 * (G / 64) : 1];
-    __shared__ float join[GROUPS > 1 ? (GROUPS - 1) * G * E : 1];
+    __shared__ float join[GROUPS > 1 ? (GROUPS - 1) * G * E : TIGHT ? G * E : 1];      // also where the normalised y waits
     const corr_residual_norm_args& a = n.a;
-    const Cols<G, E, V> c = {(int)threadIdx.x % G, (int)a.cols};
+    const Cols<G, E, RAGGED> c = {(int)threadIdx.x % G, (int)a.cols};
     const int group = threadIdx.x / G;
     const float inv = 1.f / (float)a.cols;
     RowSum<G> sum = {lds, 0};
     float s[E], w1[E], b1[E], w2[E];
-    auto block_vectors = [&] {
-        c.vector(a.post_weight, 1.f, w1);
+    if (KEEP) {
+        c.vector(a.post_weight, 1.f, w1); c.vector(a.pre_weight, 1.f, w2);
         if (FULL) { c.vector(a.scale, 1.f, s); c.vector(a.post_bias, 0.f, b1); }
+    }
+    // the branch p = hat w1 + b1 of normalised y in place of it
+    auto branch = [&](float (&v)[E]) {
+        if (!KEEP) c.vector(a.post_weight, 1.f, w1);
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] *= w1[e];
+        if (FULL && a.post_bias) {
+            if (!KEEP) c.vector(a.post_bias, 0.f, b1);
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] += b1[e];
+        }
     };
-    if (KEEP) { block_vectors(); c.vector(a.pre_weight, 1.f, w2); }
-    auto branch = [&](int e, float hat) { return FULL ? fmaf(hat, w1[e], b1[e]) : hat * w1[e]; };
+    auto scaled = [&](float (&v)[E]) {
+        if (!FULL || !a.scale) return;
+        if (!KEEP) c.vector(a.scale, 1.f, s);
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] *= s[e];
+    };
     float* const part = n.part ? n.part + (int64_t)blockIdx.x * VECTORS * a.cols : nullptr;
     float acc[IN_MEMORY ? 1 : VECTORS][E] = {};
     bool first = true;
@@ -243,8 +276,8 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_backward_kern
             for (int e = 0; e < E; ++e) acc[v][e] += value(e);
         }
     };
-    Raw<S, E, V> rh, rdh;
-    Raw<T, E, V> ry, rg, rdn;
+    Raw<S, E> rh, rdh;
+    Raw<T, E> ry, rg, rdn;
     auto ask = [&](int64_t r) {
         if (r >= a.rows) return;
         c.ask((const S*)a.h + r * a.h_stride, rh);
@@ -257,35 +290,47 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_backward_kern
     int64_t r = (int64_t)blockIdx.x * GROUPS + group;
     if (AHEAD) ask(r);
     for (; r < a.rows; r += step) {
-        if (!AHEAD) ask(r);
-        float t[E], p[E], g[E], D[E], x[E];              // g becomes act'(g), x act(g); t the normalised row, then act(g)
-        c.open(rh, t);
-        if (a.y) c.open(ry, p);
-        if (a.gate) c.open(rg, g);
-        if (n.d_n_out) c.open(rdn, D);
-        Raw<S, E, V> now = rdh;
-        if (AHEAD) ask(r + step);
+        float t[E], p[E], g[E], D[E], x[E];              // p: normalised y; x: act(g); g: act'(g); t: the normalised row, and scratch
+        Raw<S, E> now_dh = rdh;
+        Raw<T, E> now_dn = rdn;
         float rho1 = 1.f;
+        if (AHEAD) {
+            c.open(rh, t);
+            if (a.y) c.open(ry, p);
+            if (a.gate) c.open(rg, g);
+            ask(r + step);
+        } else {
+            if (a.y) c.load((const T*)a.y + r * a.y_stride, p);
+            if (a.gate) c.load((const T*)a.gate + r * a.gate_stride, g);
+        }
         if (a.gate) {
 #pragma unroll
             for (int e = 0; e < E; ++e) x[e] = g[e];
             row_act_all(a.gate_act, x);
-            row_slope_all(a.gate_act, g);
-        } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e) x[e] = 1.f;
+            if (!TIGHT) row_slope_all(a.gate_act, g);
         }
         if (a.y) {
             rho1 = normalise(a.post, p, c, inv, a.eps, sum);
-            if (!KEEP) block_vectors();
+            float u[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const float u = branch(e, p[e]) * (FULL ? s[e] * x[e] : x[e]);
-                t[e] = c.in(e) ? fmaf(a.h_scale, t[e], u) : 0.f;
+                u[e] = p[e];
+                if (TIGHT) join[e * G + c.j] = p[e];
             }
-        }
+            branch(u);
+            if (a.gate) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) u[e] *= x[e];
+            }
+            scaled(u);
+            if (!AHEAD) c.load((const S*)a.h + r * a.h_stride, t);
+#pragma unroll
+            for (int e = 0; e < E; ++e) t[e] = c.in(e) ? fmaf(a.h_scale, t[e], u[e]) : 0.f;
+        } else if (!AHEAD) c.load((const S*)a.h + r * a.h_stride, t);
         if (n.d_n_out) {
             const float rho2 = normalise(a.pre, t, c, inv, a.eps, sum);
+            if (AHEAD) c.open(now_dn, D);
+            else c.load((const T*)n.d_n_out + r * a.cols, D);
             if (a.pre_weight) add(V_W2, [&](int e) { return D[e] * t[e]; });
             if (FULL && a.pre_bias) add(V_B2, [&](int e) { return D[e]; });
             if (!KEEP) c.vector(a.pre_weight, 1.f, w2);
@@ -293,12 +338,14 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_backward_kern
             for (int e = 0; e < E; ++e) D[e] *= w2[e];
             normalise_back(a.pre, D, t, rho2, c, inv, sum);
             if (n.d_h_out) {
-                c.open(now, t);
+                if (AHEAD) c.open(now_dh, t);
+                else c.load((const S*)n.d_h_out + r * a.cols, t);
 #pragma unroll
                 for (int e = 0; e < E; ++e) D[e] += t[e];
             }
         } else {
-            c.open(now, D);
+            if (AHEAD) c.open(now_dh, D);
+            else c.load((const S*)n.d_h_out + r * a.cols, D);
             if (IN_MEMORY && first) {                    // nothing reaches these: zeros
                 add(V_W2, [](int) { return 0.f; });
                 add(V_B2, [](int) { return 0.f; });
@@ -311,23 +358,47 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_backward_kern
             c.store((S*)n.d_h + r * a.cols, t);
         }
         if (a.y) {
+            if (TIGHT) {
+                if (a.gate) {
+                    c.load((const T*)a.gate + r * a.gate_stride, g);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) x[e] = g[e];
+                    row_act_all(a.gate_act, x);
+                    row_slope_all(a.gate_act, g);
+                }
+#pragma unroll
+                for (int e = 0; e < E; ++e) p[e] = join[e * G + c.j];
+            }
             // D becomes the gradient of act(g) p, then of p, then of the normalised y
-            if (FULL && a.scale) {
-                add(V_SCALE, [&](int e) { return D[e] * x[e] * branch(e, p[e]); });
+            if ((FULL && a.scale) || n.d_gate) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) D[e] *= s[e];
+                for (int e = 0; e < E; ++e) t[e] = p[e];
+                branch(t);
+#pragma unroll
+                for (int e = 0; e < E; ++e) t[e] *= D[e];
+                if (FULL && a.scale) {
+                    if (a.gate) add(V_SCALE, [&](int e) { return t[e] * x[e]; });
+                    else add(V_SCALE, [&](int e) { return t[e]; });
+                }
+                if (n.d_gate) {
+                    scaled(t);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) t[e] *= g[e];
+                    c.store((T*)n.d_gate + r * a.cols, t);
+                }
             }
-            if (n.d_gate) {
+            scaled(D);
+            if (a.gate) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) t[e] = D[e] * branch(e, p[e]) * g[e];
-                c.store((T*)n.d_gate + r * a.cols, t);
+                for (int e = 0; e < E; ++e) D[e] *= x[e];
             }
-#pragma unroll
-            for (int e = 0; e < E; ++e) D[e] *= x[e];
             if (a.post_weight) add(V_W1, [&](int e) { return D[e] * p[e]; });
             if (FULL && a.post_bias) add(V_B1, [&](int e) { return D[e]; });
+            if (a.post_weight) {
+                if (!KEEP) c.vector(a.post_weight, 1.f, w1);
 #pragma unroll
-            for (int e = 0; e < E; ++e) D[e] *= w1[e];
+                for (int e = 0; e < E; ++e) D[e] *= w1[e];
+            }
             normalise_back(a.post, D, p, rho1, c, inv, sum);
             if (n.d_y) c.store((T*)n.d_y + r * a.cols, D);
         }
@@ -355,62 +426,68 @@ __global__ __launch_bounds__(G < 256 ? 256 : G) void residual_norm_backward_kern
     }
 }
 
-template <class S, class T, bool BACK, bool FULL, int G, int E, int V>
+template <class S, class T, bool BACK, bool FULL, bool RAGGED, int G, int E>
 void run(const NormArgs& n, hipStream_t s) {
-    constexpr int THREADS = G < 256 ? 256 : G, GROUPS = THREADS / G;
-    if constexpr (BACK) hipLaunchKernelGGL((residual_norm_backward_kernel<S, T, FULL, G, E, V>), dim3(n.parts), dim3(THREADS), 0, s, n);
+    constexpr int THREADS = threads_of(G), GROUPS = THREADS / G;
+    if constexpr (BACK) hipLaunchKernelGGL((residual_norm_backward_kernel<S, T, RAGGED, FULL, G, E>), dim3(n.parts), dim3(THREADS), 0, s, n);
     else {
         const int64_t need = (n.a.rows + GROUPS - 1) / GROUPS, most = 2048 * 256 / THREADS;
-        hipLaunchKernelGGL((residual_norm_kernel<S, T, G, E, V>), dim3((unsigned)(need < most ? need : most)), dim3(THREADS), 0, s, n);
+        hipLaunchKernelGGL((residual_norm_kernel<S, T, RAGGED, G, E>), dim3((unsigned)(need < most ? need : most)), dim3(THREADS), 0, s, n);
     }
+}
+template <class S, class T, bool BACK, bool FULL, bool RAGGED>
+void by_cols(const NormArgs& n, hipStream_t s) {
+    const int64_t C = n.a.cols;
+    if (C <= 64) run<S, T, BACK, FULL, RAGGED, 8, 8>(n, s);
+    else if (C <= 128) run<S, T, BACK, FULL, RAGGED, 16, 8>(n, s);
+    else if (C <= 256) run<S, T, BACK, FULL, RAGGED, 32, 8>(n, s);
+    else if (C <= 512) run<S, T, BACK, FULL, RAGGED, 64, 8>(n, s);
+    else if (C <= 1024) run<S, T, BACK, FULL, RAGGED, 128, 8>(n, s);
+    else if (C <= 2048) run<S, T, BACK, FULL, RAGGED, 256, 8>(n, s);
+    else if (C <= 4096) run<S, T, BACK, FULL, RAGGED, 512, 8>(n, s);
+    else if (C <= 8192) run<S, T, BACK, FULL, RAGGED, 1024, 8>(n, s);
+    else run<S, T, BACK, FULL, RAGGED, 1024, 16>(n, s);
 }
 template <class S, class T, bool BACK, bool FULL>
-void run(const NormArgs& n, bool wide, hipStream_t s) {
-    const int64_t C = n.a.cols;
-    if (wide) {
-        if (C <= 64) run<S, T, BACK, FULL, 8, 8, 8>(n, s);
-        else if (C <= 256) run<S, T, BACK, FULL, 32, 8, 8>(n, s);
-        else if (C <= 512) run<S, T, BACK, FULL, 64, 8, 8>(n, s);
-        else if (C <= 2048) run<S, T, BACK, FULL, 256, 8, 8>(n, s);
-        else if (C <= 4096) run<S, T, BACK, FULL, 512, 8, 8>(n, s);
-        else if (C <= 8192) {
-            if constexpr (BACK && FULL) run<S, T, BACK, FULL, 512, 16, 8>(n, s);
-            else run<S, T, BACK, FULL, 1024, 8, 8>(n, s);
-        } else run<S, T, BACK, FULL, 1024, 16, 8>(n, s);
-    } else {
-        if (C <= 256) run<S, T, BACK, FULL, 32, 8, 1>(n, s);
-        else if (C <= 2048) run<S, T, BACK, FULL, 256, 8, 1>(n, s);
-        else if (C <= 8192) {
-            if constexpr (BACK && FULL) run<S, T, BACK, FULL, 512, 16, 1>(n, s);
-            else run<S, T, BACK, FULL, 1024, 8, 1>(n, s);
-        } else run<S, T, BACK, FULL, 1024, 16, 1>(n, s);
-    }
-}
-template <bool BACK, bool FULL>
-hipError_t launch(const NormArgs& n, hipStream_t s) {
+hipError_t by_border(const NormArgs& n, hipStream_t s) {
     const corr_residual_norm_args& a = n.a;
-    // eight elements at once: rows of whole pieces that start on the border of every access (16 bytes, the widest)
     const uintptr_t all = (uintptr_t)a.h | (uintptr_t)a.y | (uintptr_t)a.gate | (uintptr_t)a.scale | (uintptr_t)a.post_weight |
                           (uintptr_t)a.post_bias | (uintptr_t)a.pre_weight | (uintptr_t)a.pre_bias | (uintptr_t)n.h_out | (uintptr_t)n.n_out |
                           (uintptr_t)n.d_h_out | (uintptr_t)n.d_n_out | (uintptr_t)n.d_h | (uintptr_t)n.d_y | (uintptr_t)n.d_gate;
-    const bool wide = (all & 15) == 0 && ((a.cols | a.h_stride | a.y_stride | a.gate_stride) & 7) == 0;
-    if (a.stream_type == CORR_TYPE_F32) {
-        if (a.type == CORR_TYPE_F32) run<float, float, BACK, FULL>(n, wide, s);
-        else if (a.type == CORR_TYPE_BF16) run<float, __bf16, BACK, FULL>(n, wide, s);
-        else run<float, _Float16, BACK, FULL>(n, wide, s);
-    } else if (a.type == CORR_TYPE_BF16) run<__bf16, __bf16, BACK, FULL>(n, wide, s);
-    else run<_Float16, _Float16, BACK, FULL>(n, wide, s);
+    if ((all & 15) == 0 && ((a.cols | a.h_stride | a.y_stride | a.gate_stride) & (V - 1)) == 0) by_cols<S, T, BACK, FULL, false>(n, s);
+    else by_cols<S, T, BACK, FULL, true>(n, s);
     return hipGetLastError();
+}
+template <class S, class T>
+hipError_t forward(const NormArgs& n, hipStream_t s) { return by_border<S, T, false, true>(n, s); }
+template <class S, class T>
+hipError_t backward(const NormArgs& n, hipStream_t s) {
+    return n.a.scale || n.a.post_bias || n.a.pre_bias ? by_border<S, T, true, true>(n, s) : by_border<S, T, true, false>(n, s);
 }
 
 }  // namespace
 
-int norm_backward_parts(int64_t rows, int64_t cols) {
-    const int64_t per = cols <= 64 ? 32 : cols <= 256 ? 8 : cols <= 512 ? 4 : 1;      // the most rows a workgroup has at a time
-    const int64_t most = cols <= 512 ? 768 : 512, need = (rows + per - 1) / per;
-    return (int)(need < most ? need : most);
-}
-hipError_t launch_residual_norm(const NormArgs& n, hipStream_t s) { return launch<false, true>(n, s); }
-hipError_t launch_residual_norm_backward(const NormArgs& n, hipStream_t s) {
-    return n.a.scale || n.a.post_bias || n.a.pre_bias ? launch<true, true>(n, s) : launch<true, false>(n, s);
-}
+// This file is compiled once for each pair of types (CORR_NORM_PAIR, in NORM_PAIRS' order).
+#if CORR_NORM_PAIR == 0
+#define S float
+#define T float
+#define NAME(f) f##_f32_f32
+#elif CORR_NORM_PAIR == 1
+#define S float
+#define T __bf16
+#define NAME(f) f##_f32_bf16
+#elif CORR_NORM_PAIR == 2
+#define S float
+#define T _Float16
+#define NAME(f) f##_f32_f16
+#elif CORR_NORM_PAIR == 3
+#define S __bf16
+#define T __bf16
+#define NAME(f) f##_bf16_bf16
+#else
+#define S _Float16
+#define T _Float16
+#define NAME(f) f##_f16_f16
+#endif
+hipError_t NAME(launch_residual_norm)(const NormArgs& n, hipStream_t s) { return forward<S, T>(n, s); }
+hipError_t NAME(launch_residual_norm_backward)(const NormArgs& n, hipStream_t s) { return backward<S, T>(n, s); }

@@ -97,7 +97,28 @@ corr_residual_norm_args plain(const corr_residual_norm_args& a) {
     return b;
 }
 
+hipError_t launch_norm(const NormArgs& n, hipStream_t s) {
+#define PAIR(S, T, name) if (n.a.stream_type == CORR_TYPE_##S && n.a.type == CORR_TYPE_##T) return launch_residual_norm_##name(n, s);
+    NORM_PAIRS(PAIR)
+#undef PAIR
+    return hipErrorInvalidValue;
+}
+hipError_t launch_norm_backward(const NormArgs& n, hipStream_t s) {
+#define PAIR(S, T, name) if (n.a.stream_type == CORR_TYPE_##S && n.a.type == CORR_TYPE_##T) return launch_residual_norm_backward_##name(n, s);
+    NORM_PAIRS(PAIR)
+#undef PAIR
+    return hipErrorInvalidValue;
+}
+
 }  // namespace
+
+// Workgroups of the gradient's kernel, each with a part of the column sums: two or three for every compute unit, and none without a row
+// (residual_norm.hip: `per` is the most rows that a workgroup has at a time).
+int norm_backward_parts(int64_t rows, int64_t cols) {
+    const int64_t per = cols <= 64 ? 32 : cols <= 128 ? 16 : cols <= 256 ? 8 : cols <= 512 ? 4 : 1;
+    const int64_t most = cols <= 512 ? 768 : cols <= 1024 ? 1536 : 512, need = (rows + per - 1) / per;
+    return (int)(need < most ? need : most);
+}
 
 extern "C" {
 
@@ -221,7 +242,7 @@ corr_status corr_residual_norm(const corr_residual_norm_args* a, void* h_out, vo
     NormArgs n = {};
     n.a = plain(*a);
     n.h_out = h_out; n.n_out = n_out;
-    return launch_residual_norm(n, static_cast<hipStream_t>(stream)) == hipSuccess ? CORR_OK : CORR_ERR_HIP;
+    return launch_norm(n, static_cast<hipStream_t>(stream)) == hipSuccess ? CORR_OK : CORR_ERR_HIP;
 }
 
 size_t corr_residual_norm_backward_workspace_bytes(int64_t rows, int64_t cols) {
@@ -261,7 +282,7 @@ corr_status corr_residual_norm_backward(const corr_residual_norm_args* a, const 
     n.d_h = d_h; n.d_y = d_y; n.d_gate = d_gate;
     n.part = wanted ? static_cast<float*>(workspace) : nullptr;
     n.parts = norm_backward_parts(R, C);
-    hipError_t e = launch_residual_norm_backward(n, s);
+    hipError_t e = launch_norm_backward(n, s);
     // vectors of a norm that d_n_out does not reach have no sums of their own
     if (e == hipSuccess && wanted) e = launch_column_sums(n.part, n.parts, 5, (int)C, sums, s);
     return e == hipSuccess ? CORR_OK : CORR_ERR_HIP;

@@ -45,5 +45,10 @@ struct NormArgs {
     int parts;
 };
 int norm_backward_parts(int64_t rows, int64_t cols);
-hipError_t launch_residual_norm(const NormArgs& n, hipStream_t s);
-hipError_t launch_residual_norm_backward(const NormArgs& n, hipStream_t s);
+// one instantiation of residual_norm.hip per pair of stream and row types
+#define NORM_PAIRS(X) X(F32, F32, f32_f32) X(F32, BF16, f32_bf16) X(F32, F16, f32_f16) X(BF16, BF16, bf16_bf16) X(F16, F16, f16_f16)
+#define CORR_DECLARE_NORM(S, T, name)                                          \
+    hipError_t launch_residual_norm_##name(const NormArgs& n, hipStream_t s);  \
+    hipError_t launch_residual_norm_backward_##name(const NormArgs& n, hipStream_t s);
+NORM_PAIRS(CORR_DECLARE_NORM)
+#undef CORR_DECLARE_NORM
