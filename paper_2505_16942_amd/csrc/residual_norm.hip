@@ -59,8 +59,9 @@ struct RowSum {
     }
 };
 
-// E elements of a row per thread, in pieces of V = 8: element e of thread j is column ((e / V) * G + j) * V + e % V.  RAGGED: rows
-// that start on their elements' borders alone and may end inside a piece; else a piece is whole, on 16-byte borders.
+// E elements of a row per thread, in pieces of V = 8: piece q of thread j begins at column (q * G + j) * V.  RAGGED: rows that start
+// on their elements' borders alone and may end inside a piece; then the last piece is the row's last eight columns, some of which
+// another thread has too: both compute and store the same, and sums over the row count them once (in()).
 constexpr int V = 8;
 template <class T, bool RAGGED> struct Piece { typedef typename RowVec<T, V>::value value; typedef value type __attribute__((aligned(RAGGED ? sizeof(T) : 16))); };
 template <class T, int E> struct Raw { typename RowVec<T, V>::value v[E / V]; };
@@ -68,17 +69,21 @@ template <int G, int E, bool RAGGED>
 struct Cols {
     int j, C;
     __device__ __forceinline__ int at(int piece) const { return (piece * G + j) * V; }
-    __device__ __forceinline__ bool in(int e) const { return at(e / V) + (RAGGED ? e % V : 0) < C; }
-    __device__ __forceinline__ bool whole(int piece) const { return at(piece) + (RAGGED ? V - 1 : 0) < C; }
+    __device__ __forceinline__ bool has(int piece) const { return at(piece) < C; }
+    __device__ __forceinline__ int start(int piece) const { return RAGGED ? min(at(piece), C - V) : at(piece); }
+    __device__ __forceinline__ bool in(int e) const {
+        const int q = e / V;
+        return has(q) && (!RAGGED || (C < V ? e % V < C : start(q) + e % V >= at(q)));
+    }
     template <class T> __device__ __forceinline__ void ask(const T* row, Raw<T, E>& r) const {
 #pragma unroll
         for (int q = 0; q < E / V; ++q) {
             r.v[q] = {};
-            if (whole(q)) r.v[q] = *reinterpret_cast<const typename Piece<T, RAGGED>::type*>(row + at(q));
-            else if (RAGGED) {
+            if (!has(q)) continue;
+            if (!RAGGED || C >= V) r.v[q] = *reinterpret_cast<const typename Piece<T, RAGGED>::type*>(row + start(q));
+            else
 #pragma unroll
-                for (int e = 0; e < V; ++e) if (at(q) + e < C) r.v[q][e] = row[at(q) + e];
-            }
+                for (int e = 0; e < V; ++e) if (e < C) r.v[q][e] = row[e];
         }
     }
     template <class T> __device__ __forceinline__ void open(const Raw<T, E>& r, float (&v)[E]) const {
@@ -90,18 +95,21 @@ struct Cols {
         ask(row, r);
         open(r, v);
     }
-    template <class T> __device__ __forceinline__ void store(T* row, const float (&v)[E]) const {
+    // OWN: of columns that two threads have, only the one's that counts them (sums that are read again)
+    template <bool OWN = false, class T> __device__ __forceinline__ void store(T* row, const float (&v)[E]) const {
 #pragma unroll
         for (int q = 0; q < E / V; ++q) {
-            if (whole(q)) {
-                typename Piece<T, RAGGED>::value x;
+            if (!has(q)) continue;
+            typename Piece<T, RAGGED>::value x;
 #pragma unroll
-                for (int e = 0; e < V; ++e) x[e] = (T)v[q * V + e];
-                *reinterpret_cast<typename Piece<T, RAGGED>::type*>(row + at(q)) = x;
-            } else if (RAGGED) {
+            for (int e = 0; e < V; ++e) x[e] = (T)v[q * V + e];
+            if (OWN && RAGGED && start(q) < at(q)) {
 #pragma unroll
-                for (int e = 0; e < V; ++e) if (at(q) + e < C) row[at(q) + e] = (T)v[q * V + e];
-            }
+                for (int e = 0; e < V; ++e) if (in(q * V + e)) row[max(start(q), 0) + e] = x[e];
+            } else if (!RAGGED || C >= V) *reinterpret_cast<typename Piece<T, RAGGED>::type*>(row + start(q)) = x;
+            else
+#pragma unroll
+                for (int e = 0; e < V; ++e) if (e < C) row[e] = x[e];
         }
     }
     // a vector of parameters; `none` where there is none
@@ -114,21 +122,21 @@ struct Cols {
 };
 constexpr int threads_of(int G) { return G < 128 ? 256 : G; }
 
-// v becomes the normalised row; returns 1 / its spread (1 for CORR_NORM_NONE).  Elements past the row's end stay zero.
+// v becomes the normalised row; returns 1 / its spread (1 for CORR_NORM_NONE).
 template <int G, int E, bool RAGGED>
 __device__ __forceinline__ float normalise(int kind, float (&v)[E], const Cols<G, E, RAGGED>& c, float inv, float eps, RowSum<G>& sum) {
     if (kind == CORR_NORM_NONE) return 1.f;
     if (kind == CORR_NORM_LAYER) {
         float m = 0.f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) m += v[e];
+        for (int e = 0; e < E; ++e) m += c.in(e) ? v[e] : 0.f;
         const float mean = sum(m) * inv;
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = c.in(e) ? v[e] - mean : 0.f;
+        for (int e = 0; e < E; ++e) v[e] -= mean;
     }
     float q = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) q = fmaf(v[e], v[e], q);
+    for (int e = 0; e < E; ++e) q = c.in(e) ? fmaf(v[e], v[e], q) : q;
     const float rho = 1.f / sqrtf(sum(q) * inv + eps);
 #pragma unroll
     for (int e = 0; e < E; ++e) v[e] *= rho;
@@ -141,15 +149,15 @@ __device__ __forceinline__ void normalise_back(int kind, float (&q)[E], const fl
     if (kind == CORR_NORM_NONE) return;
     float a = 0.f, b = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) a = fmaf(q[e], hat[e], a);
+    for (int e = 0; e < E; ++e) a = c.in(e) ? fmaf(q[e], hat[e], a) : a;
     if (kind == CORR_NORM_LAYER) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) b += q[e];
+        for (int e = 0; e < E; ++e) b += c.in(e) ? q[e] : 0.f;
         const float2 s = sum(a, b);
         a = s.x * inv;
         b = s.y * inv;
 #pragma unroll
-        for (int e = 0; e < E; ++e) q[e] = c.in(e) ? rho * (q[e] - b - hat[e] * a) : 0.f;
+        for (int e = 0; e < E; ++e) q[e] = rho * (q[e] - b - hat[e] * a);
     } else {
         a = sum(a) * inv;
 #pragma unroll
@@ -184,12 +192,16 @@ __global__ __launch_bounds__(threads_of(G)) void residual_norm_kernel(NormArgs n
     int64_t r = (int64_t)blockIdx.x * GROUPS + threadIdx.x / G;
     if (AHEAD) ask(r);
     for (; r < a.rows; r += step) {
-        if (!AHEAD) ask(r);
         float t[E], p[E], g[E];
-        c.open(rh, t);
-        if (a.y) c.open(ry, p);
-        if (a.gate) c.open(rg, g);
-        if (AHEAD) ask(r + step);
+        if (AHEAD) {
+            c.open(rh, t);
+            if (a.y) c.open(ry, p);
+            if (a.gate) c.open(rg, g);
+            ask(r + step);
+        } else {
+            if (a.y) c.load((const T*)a.y + r * a.y_stride, p);
+            if (a.gate) c.load((const T*)a.gate + r * a.gate_stride, g);
+        }
         if (a.y) {
             normalise(a.post, p, c, inv, a.eps, sum);
             if (!KEEP) c.vector(a.post_weight, 1.f, w1);
@@ -206,10 +218,13 @@ __global__ __launch_bounds__(threads_of(G)) void residual_norm_kernel(NormArgs n
 #pragma unroll
                 for (int e = 0; e < E; ++e) p[e] *= g[e];
             }
+            if (!AHEAD) c.load((const S*)a.h + r * a.h_stride, t);
 #pragma unroll
-            for (int e = 0; e < E; ++e) t[e] = c.in(e) ? fmaf(a.h_scale, t[e], p[e]) : 0.f;
+            for (int e = 0; e < E; ++e) t[e] = fmaf(a.h_scale, t[e], p[e]);
+            // in place, a wave may not write what another still has to read of this row
+            if (RAGGED && G > 64 && n.h_out == a.h) __syncthreads();
             if (n.h_out) c.store((S*)n.h_out + r * a.cols, t);
-        }
+        } else if (!AHEAD) c.load((const S*)a.h + r * a.h_stride, t);
         if (a.pre != CORR_NORM_NONE) {
             normalise(a.pre, t, c, inv, a.eps, sum);
             if (!KEEP) c.vector(a.pre_weight, 1.f, w2);
@@ -270,7 +285,7 @@ __global__ __launch_bounds__(threads_of(G)) void residual_norm_backward_kernel(N
             if (!first) c.load(row, x);
 #pragma unroll
             for (int e = 0; e < E; ++e) x[e] += value(e);
-            c.store(row, x);
+            c.template store<true>(row, x);
         } else {
 #pragma unroll
             for (int e = 0; e < E; ++e) acc[v][e] += value(e);
@@ -325,7 +340,7 @@ __global__ __launch_bounds__(threads_of(G)) void residual_norm_backward_kernel(N
             scaled(u);
             if (!AHEAD) c.load((const S*)a.h + r * a.h_stride, t);
 #pragma unroll
-            for (int e = 0; e < E; ++e) t[e] = c.in(e) ? fmaf(a.h_scale, t[e], u[e]) : 0.f;
+            for (int e = 0; e < E; ++e) t[e] = fmaf(a.h_scale, t[e], u[e]);
         } else if (!AHEAD) c.load((const S*)a.h + r * a.h_stride, t);
         if (n.d_n_out) {
             const float rho2 = normalise(a.pre, t, c, inv, a.eps, sum);

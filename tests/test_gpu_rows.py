@@ -340,6 +340,34 @@ def test_norm_strides_in_place_and_guards(C, ld):
             ref.check(name, g, *want)
 
 
+@pytest.mark.parametrize("C", [8193, 8705, 9001])
+def test_norm_sums_in_memory_of_ragged_rows(C):
+    """More rows than workgroups, rows that end in a piece whose other columns belong to the next wave's neighbour or to another piece."""
+    b, rows = _b(), 1100
+    new, h, kw, r = _case(F32, F32, rows, C, FORMS[2], C)
+    dh, dn = new(rows, C), new(rows, C)
+    got = b.corr_residual_norm_backward(h, d_h_out=dh, d_n_out=dn, **kw)
+    for i, want in enumerate(r.backward(dh, dn)):
+        if i >= 3:
+            ref.check("%s C=%d" % (got._fields[i], C), got[i], *want)
+            rel = float((got[i].double().cpu() - want[0]).norm() / want[0].norm())
+            assert rel < 1e-5, (got._fields[i], rel)     # one of 1100 rows counted twice is 1e-3
+
+
+@pytest.mark.parametrize("C", [129, 516, 1027, 2049, 4100, 8191, 8705])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_norm_in_place_ragged(C, dtype):
+    """In place with rows that several waves share and that end inside a piece: as out of place, bit for bit."""
+    b, rows = _b(), 900
+    new = _gen(C)
+    h, y, w = new(rows, C, dtype=dtype), new(rows, C, dtype=dtype), new(C, mean=1.0)
+    t, n = b.corr_residual_norm(h, y=y, pre_weight=w)
+    acc = h.clone()
+    _, n2 = b.corr_residual_norm(acc, y=y, pre_weight=w, h_out=acc)
+    assert torch.equal(acc, t) and torch.equal(n, n2)
+    assert torch.equal(t, (h.float() + y.float()).to(dtype))
+
+
 def test_norm_edges():
     """Rows of zeros (eps alone), of one value (no spread), very large and very small ones; a NaN stays in its row; no rows."""
     b = _b()
