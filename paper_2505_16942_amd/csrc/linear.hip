@@ -63,11 +63,14 @@ __device__ __forceinline__ Window window(const void* p, int64_t ld, int rows, in
     return w;
 }
 
-// Which tile workgroup w of T takes.  Workgroup w runs on XCD w % 8: each XCD gets a run of consecutive tiles, and the tiles are
-// numbered in panels of eight columns, so that the 32 tiles an XCD works on at a time share operands in its L2.
-__device__ __forceinline__ void tile_of(int w, int tm, int tn, int& m, int& n) {
-    const int T = tm * tn, q = T >> 3, r = T & 7, x = w & 7;
-    const int t = x * q + min(x, r) + (w >> 3);
+// Which tile and split workgroup w takes.  Workgroup w runs on XCD w % 8: each XCD gets a run of consecutive pieces of work; a split's tiles
+// follow each other, and tiles are numbered in panels of eight columns, so that the 32 pieces an XCD works on at a time share
+// operands in its L2.
+__device__ __forceinline__ void tile_of(int w, int tm, int tn, int splits, int& m, int& n, int& split) {
+    const int T = tm * tn, all = T * splits, q = all >> 3, r = all & 7, x = w & 7;
+    int t = x * q + min(x, r) + (w >> 3);
+    split = t / T;
+    t -= split * T;
     const int per = 8 * tm, panel = t / per, in = t - panel * per, wide = min(8, tn - 8 * panel);
     m = in / wide;
     n = 8 * panel + in - m * wide;
@@ -80,13 +83,15 @@ __device__ __forceinline__ bool rows_words(const ProductArgs& g) {
     if (sizeof(T) == 4) return true;
     return ((g.N | g.ldy | (g.res ? g.ld_res : 0)) & 1) == 0 && (((uintptr_t)g.y | (uintptr_t)g.pre | (uintptr_t)g.res) & 3) == 0;
 }
+// `past`: past the caches
 template <class T, int V>
-__device__ __forceinline__ void store_some(T* p, const float (&v)[V], int left, bool words) {
+__device__ __forceinline__ void store_some(T* p, const float (&v)[V], int left, bool words, bool past = false) {
     if (words && left >= V) {
         typename Words<T, V>::type x;
 #pragma unroll
         for (int e = 0; e < V; ++e) x[e] = (T)v[e];
-        *reinterpret_cast<typename Words<T, V>::type*>(p) = x;
+        if (past) __builtin_nontemporal_store(x, reinterpret_cast<typename Words<T, V>::type*>(p));
+        else *reinterpret_cast<typename Words<T, V>::type*>(p) = x;
     } else
 #pragma unroll
         for (int e = 0; e < V; ++e) if (e < left) p[e] = (T)v[e];
@@ -108,7 +113,7 @@ __device__ __forceinline__ void finish(const ProductArgs& g, float (&v)[V], cons
     if (m >= g.M || left <= 0) return;
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] += bias[e];
-    if (g.pre) store_some<T, V>((T*)g.pre + (int64_t)m * g.N + n, v, left, words);
+    if (g.pre) store_some<T, V>((T*)g.pre + (int64_t)m * g.N + n, v, left, words, g.past);
     row_act_all(g.act, v);
     if (g.res) {
         float r[V];
@@ -116,7 +121,7 @@ __device__ __forceinline__ void finish(const ProductArgs& g, float (&v)[V], cons
 #pragma unroll
         for (int e = 0; e < V; ++e) v[e] += r[e];
     }
-    store_some<T, V>((T*)g.y + (int64_t)m * g.ldy + n, v, left, words);
+    store_some<T, V>((T*)g.y + (int64_t)m * g.ldy + n, v, left, words, g.past);
 }
 template <int V>
 __device__ __forceinline__ void load_bias(const ProductArgs& g, float (&bias)[V], int n) {
@@ -240,9 +245,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product16_kernel(ProductArgs 
     lds_byte* const lds = (lds_byte*)smem;
     const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)lds);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lg = lane >> 4;
-    int mt, nt;
-    tile_of(blockIdx.x, tm, tn, mt, nt);
-    const int m0 = mt * BM, n0 = nt * BN, split = blockIdx.y;
+    int mt, nt, split;
+    tile_of(blockIdx.x, tm, tn, splits, mt, nt, split);
+    const int m0 = mt * BM, n0 = nt * BN;
     const int k0 = split * steps_per * 64, k_left = min(g.K - k0, steps_per * 64);
     const int whole = k_left >> 6, tail = k_left & 63, steps = whole + (tail != 0);
     Window wa = window<AR, 2, 64>(g.a, g.lda, g.M, g.K, m0, k0), wb = window<BR, 2, 64>(g.b, g.ldb, g.N, g.K, n0, k0);
@@ -385,9 +390,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product32_kernel(ProductArgs 
     __shared__ __align__(1024) unsigned char smem[3 * (PA + PB)];
     lds_byte* const lds = (lds_byte*)smem;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lg = lane >> 4;
-    int mt, nt;
-    tile_of(blockIdx.x, tm, tn, mt, nt);
-    const int m0 = mt * BM, n0 = nt * BN, split = blockIdx.y;
+    int mt, nt, split;
+    tile_of(blockIdx.x, tm, tn, splits, mt, nt, split);
+    const int m0 = mt * BM, n0 = nt * BN;
     const int k0 = split * steps_per * 32, k_left = min(g.K - k0, steps_per * 32), steps = (k_left + 31) >> 5;
     Window wa = window<AR, 4, 32>(g.a, g.lda, g.M, g.K, m0, k0), wb = window<BR, 4, 32>(g.b, g.ldb, g.N, g.K, n0, k0);
     Loader32<AR, BM, NT> la;
@@ -685,7 +690,7 @@ __global__ __launch_bounds__(SLOPE_THREADS) void slope_kernel(int act, const T* 
 template <class T, bool AR, bool BR, int BM, int BN, int WM, int WN>
 void run16(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
     const int tm = cdiv(g.M, BM), tn = cdiv(g.N, BN);
-    hipLaunchKernelGGL((product16_kernel<T, AR, BR, BM, BN, WM, WN>), dim3(tm * tn, p.splits), dim3(64 * WM * WN), 0, s, g, tm, tn, p.splits, p.steps);
+    hipLaunchKernelGGL((product16_kernel<T, AR, BR, BM, BN, WM, WN>), dim3(tm * tn * p.splits), dim3(64 * WM * WN), 0, s, g, tm, tn, p.splits, p.steps);
 }
 template <class T, bool AR, bool BR>
 void run16(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
@@ -715,10 +720,10 @@ template <bool AR, bool BR>
 void run32(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
     if (p.tile == TILE_64) {
         const int tm = cdiv(g.M, 64), tn = cdiv(g.N, 64);
-        hipLaunchKernelGGL((product32_kernel<AR, BR, 64, 64, 2, 2>), dim3(tm * tn, p.splits), dim3(256), 0, s, g, tm, tn, p.splits, p.steps);
+        hipLaunchKernelGGL((product32_kernel<AR, BR, 64, 64, 2, 2>), dim3(tm * tn * p.splits), dim3(256), 0, s, g, tm, tn, p.splits, p.steps);
     } else {
         const int tm = cdiv(g.M, 128), tn = cdiv(g.N, 128);
-        hipLaunchKernelGGL((product32_kernel<AR, BR, 128, 128, 2, 2>), dim3(tm * tn, p.splits), dim3(256), 0, s, g, tm, tn, p.splits, p.steps);
+        hipLaunchKernelGGL((product32_kernel<AR, BR, 128, 128, 2, 2>), dim3(tm * tn * p.splits), dim3(256), 0, s, g, tm, tn, p.splits, p.steps);
     }
 }
 void product32(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
@@ -739,12 +744,13 @@ ProductPlan product_plan(corr_dtype type, int a_rows, int b_rows, int M, int N, 
     const int bk = wide ? 32 : 64, all = cdiv(K, bk);
     ProductPlan p = {TILE_64, 1, all};
     if (M <= 32 && !a_rows && !b_rows) { p.tile = TILE_FEW; return p; }
-    int side = 64;
     int64_t tiles = (int64_t)cdiv(M, 64) * cdiv(N, 64);
     const int64_t t128 = (int64_t)cdiv(M, 128) * cdiv(N, 128), t256 = (int64_t)cdiv(M, 256) * cdiv(N, 256);
-    if (!wide && t256 >= 256) { p.tile = TILE_256; side = 256; tiles = t256; }
-    else if (t128 * all >= 256 * 8) { p.tile = TILE_128; side = 128; tiles = t128; }
-    (void)side;
+    // Tiles of 256 read operands half as often, but one workgroup fills a compute unit: for products that give every unit one, and
+    // that do not make them multiply much more (129600 x 256 -> 324: 58 us in tiles of 128, 70 in 256; x 324 -> 256: 53 and 48).
+    // Tiles of 64 where 128 leaves units idle: 2852 x 1024 -> 256: 12.7 us, 14.8 in 128; 32400 x 256 -> 256: 12.6 and 11.9.
+    if (!wide && t256 >= 256 && t256 * 4 <= t128 * 1.25) { p.tile = TILE_256; tiles = t256; }
+    else if (t128 * all >= 256 * 4) { p.tile = TILE_128; tiles = t128; }
     if (getenv("CORR_TILE")) { p.tile = atoi(getenv("CORR_TILE")); tiles = p.tile == 3 ? t256 : p.tile == 2 ? t128 : (int64_t)cdiv(M, 64) * cdiv(N, 64); }
     // workgroups for two or three on every compute unit, and at least eight steps for each
     const int64_t want = p.tile == TILE_256 ? 256 : p.tile == TILE_128 ? 512 : 1024;
@@ -758,8 +764,13 @@ ProductPlan product_plan(corr_dtype type, int a_rows, int b_rows, int M, int N, 
     return p;
 }
 
-hipError_t launch_product(const ProductArgs& g, hipStream_t s) {
+hipError_t launch_product(const ProductArgs& args, hipStream_t s) {
+    ProductArgs g = args;
     const ProductPlan p = product_plan(g.type, g.a_rows, g.b_rows, g.M, g.N, g.K);
+    // A result larger than half of the memory-side cache goes past the caches, so that the operands stay in them (259200 x 1024 -> 128
+    // bf16: 137 -> 119 us); whole lines only (rows of 648 bytes: 43 -> 46 us).
+    const int64_t row = g.ldy * corr_elem_bytes(g.type);
+    g.past = (int64_t)g.M * row >= (128 << 20) && row % 64 == 0 && ((uintptr_t)g.y & 63) == 0;
     if (g.type == CORR_TYPE_F32) product32(g, p, s);
     else if (g.type == CORR_TYPE_BF16) product16<__bf16>(g, p, s);
     else product16<_Float16>(g, p, s);

@@ -2,11 +2,12 @@
 #include "rows.h"
 
 namespace {
-// 64 columns a workgroup, 16 shares of the parts each: the loads of a share are independent, its sum is in order.
-constexpr int SHARES = 16;
-__global__ __launch_bounds__(64 * SHARES) void column_sums_kernel(const float* __restrict__ part, int parts, int C, ColumnSums o) {
-    __shared__ float sums[SHARES][64];
-    const int lane = threadIdx.x & 63, share = threadIdx.x >> 6, c = blockIdx.x * 64 + lane, v = blockIdx.y;
+// 16 columns a workgroup, 64 shares of the parts each: a share's loads are independent and its sum is in order, as is the sum of the shares.
+// With 64 columns and 16 shares, 1024 parts of 1024 columns took 11 us.
+constexpr int SHARES = 64, COLS = 16;
+__global__ __launch_bounds__(COLS * SHARES) void column_sums_kernel(const float* __restrict__ part, int parts, int C, ColumnSums o) {
+    __shared__ float sums[SHARES][COLS];
+    const int col = threadIdx.x % COLS, share = threadIdx.x / COLS, c = blockIdx.x * COLS + col, v = blockIdx.y;
     float* const out = o.out[v];
     if (!out) return;
     const int64_t stride = (int64_t)gridDim.y * C;
@@ -16,10 +17,11 @@ __global__ __launch_bounds__(64 * SHARES) void column_sums_kernel(const float* _
 #pragma unroll 8
         for (int i = share; i < parts; i += SHARES) sum += p[i * stride];
     }
-    sums[share][lane] = sum;
+    sums[share][col] = sum;
     __syncthreads();
     if (share == 0 && c < C) {
-        for (int s = 1; s < SHARES; ++s) sum += sums[s][lane];
+#pragma unroll 8
+        for (int s = 1; s < SHARES; ++s) sum += sums[s][col];
         out[c] = sum;
     }
 }
@@ -38,6 +40,6 @@ hipError_t launch_zero(void* p, size_t bytes, hipStream_t s) {
 }
 
 hipError_t launch_column_sums(const float* part, int parts, int vectors, int C, const ColumnSums& o, hipStream_t s) {
-    hipLaunchKernelGGL(column_sums_kernel, dim3((C + 63) / 64, vectors), dim3(64 * SHARES), 0, s, part, parts, C, o);
+    hipLaunchKernelGGL(column_sums_kernel, dim3((C + COLS - 1) / COLS, vectors), dim3(COLS * SHARES), 0, s, part, parts, C, o);
     return hipGetLastError();
 }

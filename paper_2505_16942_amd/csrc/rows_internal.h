@@ -16,6 +16,7 @@ struct ProductArgs {
     void* pre;                 // [M][N]
     void* y; int64_t ldy;
     int act;
+    bool past;                 // set by launch_product: y and pre are stored past the caches
     float* part;               // [splits][M][N] fp32, where the plan says more than one split
 };
 struct ProductPlan { int tile, splits, steps; };   // steps of the k loop per split
