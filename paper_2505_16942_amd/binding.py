@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 from typing import NamedTuple
 
 import torch
@@ -65,13 +66,14 @@ class Profile(ctypes.Structure):
                 ("binning_ms", ctypes.c_double), ("block_ms", ctypes.c_double)]
 
 
-class ResidualNormArgs(ctypes.Structure):
-    _fields_ = [("stream_type", ctypes.c_int), ("type", ctypes.c_int), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
-                ("h", ctypes.c_void_p), ("h_stride", ctypes.c_int64), ("y", ctypes.c_void_p), ("y_stride", ctypes.c_int64),
-                ("gate", ctypes.c_void_p), ("gate_stride", ctypes.c_int64), ("gate_act", ctypes.c_int),
-                ("scale", ctypes.c_void_p), ("h_scale", ctypes.c_float),
-                ("post", ctypes.c_int), ("post_weight", ctypes.c_void_p), ("post_bias", ctypes.c_void_p),
-                ("pre", ctypes.c_int), ("pre_weight", ctypes.c_void_p), ("pre_bias", ctypes.c_void_p), ("eps", ctypes.c_float)]
+# corr_residual_norm_args as C lays it out: stream_type, type, rows, cols, h, h_stride, y, y_stride, gate, gate_stride, gate_act, scale,
+# h_scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps.  struct's native layout is C's; packing takes a third of what a
+# ctypes structure takes.
+_NORM_ARGS = struct.Struct("@iiqqPqPqPqiPfiPPiPPf0P")
+
+
+def residual_norm_args(*fields) -> bytes:
+    return _NORM_ARGS.pack(*[0 if f is None else f for f in fields])
 
 
 _lib = None
@@ -115,7 +117,7 @@ def load_library():
     lib.corr_linear_backward_workspace_bytes.restype = sz
     lib.corr_linear_backward.argtypes = [ci, ci, vp, i64, vp, vp, vp, i64, vp, vp, vp, i64, i64, i64, vp, sz, vp]
     lib.corr_linear_backward.restype = ci
-    norm_args = ctypes.POINTER(ResidualNormArgs)
+    norm_args = ctypes.c_char_p                          # bytes of corr_residual_norm_args
     lib.corr_residual_norm.argtypes = [norm_args, vp, vp, vp]
     lib.corr_residual_norm.restype = ci
     lib.corr_residual_norm_backward_workspace_bytes.argtypes = [i64, i64]
@@ -536,7 +538,7 @@ def corr_linear_backward(x: torch.Tensor, w: torch.Tensor, d_out: torch.Tensor, 
 
 
 def _norm_args(h, y, gate, gate_act, scale, h_scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps, dtype):
-    """(arguments, type of the rows beside the stream, device)"""
+    """(arguments, rows, length, type of the rows beside the stream, device)"""
     device = _on_device(h, "h")
     rows, cols, hs = _rows(h, "h")
     if y is not None:
@@ -551,13 +553,13 @@ def _norm_args(h, y, gate, gate_act, scale, h_scale, post, post_weight, post_bia
     pg, gs = (None, 0) if gate is None else _matrix(gate, "gate", dtype, device, rows, cols)
     one = (cols,)
     f32 = torch.float32
-    return ResidualNormArgs(
+    return residual_norm_args(
         _type_of(h, "h"), _TYPES[dtype], rows, cols, _pointer(h), hs, py, ys, pg, gs, gate_act,
         None if scale is None else _dense(scale, "scale", f32, device, one), h_scale,
         post, None if post_weight is None else _dense(post_weight, "post_weight", f32, device, one),
         None if post_bias is None else _dense(post_bias, "post_bias", f32, device, one),
         pre, None if pre_weight is None else _dense(pre_weight, "pre_weight", f32, device, one),
-        None if pre_bias is None else _dense(pre_bias, "pre_bias", f32, device, one), eps), dtype, device
+        None if pre_bias is None else _dense(pre_bias, "pre_bias", f32, device, one), eps), rows, cols, dtype, device
 
 
 def corr_residual_norm(h: torch.Tensor, y: torch.Tensor | None = None, gate: torch.Tensor | None = None,
@@ -571,7 +573,7 @@ def corr_residual_norm(h: torch.Tensor, y: torch.Tensor | None = None, gate: tor
     Returns (t, n): t of h's type (h itself without y), n of y's (of `dtype`, or h's, without y), None for CORR_NORM_NONE.
     h, y, gate: [..., C] with contiguous, evenly spaced rows; vectors: float32 [C].  h_out may be h."""
     lib = _lib or load_library()
-    a, dtype, device = _norm_args(h, y, gate, gate_act, scale, h_scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps, dtype)
+    a, rows, cols, dtype, device = _norm_args(h, y, gate, gate_act, scale, h_scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps, dtype)
     ph = pn = None
     if y is None:
         if h_out is not None:
@@ -589,7 +591,7 @@ def corr_residual_norm(h: torch.Tensor, y: torch.Tensor | None = None, gate: tor
             pn = _dense(n_out, "n_out", dtype, device, h.shape)
     elif n_out is not None:
         raise ValueError("without a norm there is no n_out")
-    st = lib.corr_residual_norm(ctypes.byref(a), ph, pn, _stream())
+    st = lib.corr_residual_norm(a, ph, pn, _stream())
     if st != CORR_OK:
         raise CorrError(st, "corr_residual_norm")
     return (h if y is None else h_out), n_out
@@ -622,18 +624,18 @@ def corr_residual_norm_backward(h: torch.Tensor, y: torch.Tensor | None = None, 
     results, contiguous; one of them may be None (zero).  Matrices have the type of what they are the gradient of, vectors float32."""
     lib = _lib or load_library()
     dtype = d_n_out.dtype if y is None and isinstance(d_n_out, torch.Tensor) else None
-    a, dtype, device = _norm_args(h, y, gate, gate_act, scale, h_scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps, dtype)
+    a, rows, cols, dtype, device = _norm_args(h, y, gate, gate_act, scale, h_scale, post, post_weight, post_bias, pre, pre_weight, pre_bias, eps, dtype)
     if d_h_out is None and d_n_out is None:
         raise ValueError("d_h_out or d_n_out is needed")
     pdh = None if d_h_out is None else _dense(d_h_out, "d_h_out", h.dtype, device, h.shape)
     pdn = None if d_n_out is None else _dense(d_n_out, "d_n_out", dtype, device, h.shape)
     vectors = [v is not None for v in (scale, post_weight, post_bias, pre_weight, pre_bias)]
-    one = _new(h, (sum(vectors), a.cols), torch.float32).unbind() if any(vectors) else ()
+    one = _new(h, (sum(vectors), cols), torch.float32).unbind() if any(vectors) else ()
     each = iter(one)
     g = ResidualNormGrads(_new(h, h.shape, h.dtype), None if y is None else _new(h, h.shape, dtype),
                           None if gate is None else _new(h, h.shape, dtype), *[next(each) if there else None for there in vectors])
-    held, ws, size = _workspace(workspace, _norm_backward_need(a.rows, a.cols) if one else 0, h, device)
-    st = lib.corr_residual_norm_backward(ctypes.byref(a), pdh, pdn, *[None if t is None else _pointer(t) for t in g], ws, size, _stream())
+    held, ws, size = _workspace(workspace, _norm_backward_need(rows, cols) if one else 0, h, device)
+    st = lib.corr_residual_norm_backward(a, pdh, pdn, *[None if t is None else _pointer(t) for t in g], ws, size, _stream())
     if st != CORR_OK:
         raise CorrError(st, "corr_residual_norm_backward")
     return g

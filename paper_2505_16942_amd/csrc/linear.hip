@@ -1,11 +1,10 @@
 // Products of rows with weights: y = act(x w^T + bias) + residual, and the two products of its gradient.
 #include <type_traits>
-#include <stdlib.h>
 #include "rows_internal.h"
 
 namespace {
 
-enum Tile { TILE_FEW = 0, TILE_64, TILE_128, TILE_256 };
+enum Tile { TILE_FEW = 0, TILE_64, TILE_128, TILE_256, TILE_ROWS };
 inline int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -41,7 +40,11 @@ __device__ __forceinline__ void arrive_all() {
 struct Window {
     const unsigned char* at;
     int64_t left, step;
-    __device__ __forceinline__ unsigned size() const { return (unsigned)(left < 0 ? 0 : left > 0x7ffffff0 ? 0x7ffffff0 : left); }
+    __device__ __forceinline__ unsigned size() const {     // by halves: whole 64-bit comparisons would go to the vector unit
+        const int hi = (int)(left >> 32);
+        const unsigned lo = (unsigned)left;
+        return hi < 0 ? 0 : hi > 0 || lo > 0x7ffffff0u ? 0x7ffffff0u : lo;
+    }
     __device__ __forceinline__ i32x4 rsrc() const {
         const uint64_t p = (uint64_t)at;
         return i32x4{__builtin_amdgcn_readfirstlane((int)p), __builtin_amdgcn_readfirstlane((int)(p >> 32) & 0xffff),
@@ -179,9 +182,11 @@ __device__ __forceinline__ void finish_wave(const ProductArgs& g, f32x4 (&acc)[F
 template <int R> __device__ __forceinline__ int turn(int k) {
     return R >= 128 ? (k & 3) | ((k >> 3) & 1) << 2 : (k & 3) ^ ((k >> 3) & 1);
 }
-template <bool ROWS, int R, int WAVES>
+// piece p of row r of BK elements: where it lies
+template <int BK> __device__ __forceinline__ int place(int r, int p) { return BK == 64 ? p ^ (r & 7) : p ^ (r >> 1 & 3); }
+template <bool ROWS, int R, int WAVES, int BK>
 struct Loader16 {
-    static constexpr int PIECES = R * 128 / (1024 * WAVES);
+    static constexpr int PIECES = R * BK * 2 / (1024 * WAVES);
     unsigned voff[PIECES];
     __device__ __forceinline__ void plan(int wave, int lane, int64_t ld) {
 #pragma unroll
@@ -191,8 +196,8 @@ struct Loader16 {
                 const int k = p / (2 * R), piece = (p % (2 * R)) >> 4;
                 voff[q] = (unsigned)(k * ld * 2) + ((((piece >> 1) ^ turn<R>(k)) << 1) | (piece & 1)) * 16;
             } else {
-                const int row = p >> 7, piece = (p >> 4) & 7;
-                voff[q] = (unsigned)(row * ld * 2) + (piece ^ (row & 7)) * 16;
+                const int row = p / (2 * BK), piece = (p >> 4) % (BK / 8);
+                voff[q] = (unsigned)(row * ld * 2) + place<BK>(row, piece) * 16;
             }
         }
     }
@@ -203,7 +208,7 @@ struct Loader16 {
     }
 };
 // F fragments of 16 rows from row `base` on: lane (lr, lg) holds k = 8 lg .. + 7 of a row of 32 k.
-template <class T, bool ROWS, int R, int F>
+template <class T, bool ROWS, int R, int F, int BK>
 struct Reader16 {
     unsigned off[ROWS ? F : 2];
     __device__ __forceinline__ void plan(int base, int lr, int lg) {
@@ -214,7 +219,7 @@ struct Reader16 {
                 off[i] = k * (2 * R) + (((base >> 4) + i) ^ turn<R>(k)) * 32 + (lr & 3) * 8;
             }
         } else {
-            off[0] = (base + lr) * 128 + ((lg ^ (lr & 7)) << 4);
+            off[0] = (base + lr) * (2 * BK) + place<BK>(lr, lg) * 16;
             off[1] = off[0] ^ 64;
         }
     }
@@ -224,7 +229,7 @@ struct Reader16 {
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + off[i] + (ks * 32 + 4) * 2 * R));
             return __builtin_bit_cast(typename Frag<T>::type, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
-            return *(__attribute__((address_space(3))) typename Frag<T>::type*)(tile + off[ks] + i * 2048);
+            return *(__attribute__((address_space(3))) typename Frag<T>::type*)(tile + off[ks] + i * 32 * BK);
         }
     }
 };
@@ -237,10 +242,10 @@ __device__ __forceinline__ V keep_first(V v, int left) {
     return __builtin_bit_cast(V, u);
 }
 
-template <class T, bool AR, bool BR, int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN, 2) void product16_kernel(ProductArgs g, int tm, int tn, int splits, int steps_per) {
+template <class T, bool AR, bool BR, int BM, int BN, int WM, int WN, int BK>
+__global__ __launch_bounds__(64 * WM * WN, BK == 32 ? 4 : 2) void product16_kernel(ProductArgs g, int tm, int tn, int splits, int steps_per) {
     constexpr int WAVES = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
-    constexpr int A_BYTES = BM * 128, HALF = (BM + BN) * 128;
+    constexpr int A_BYTES = BM * BK * 2, HALF = (BM + BN) * BK * 2;
     __shared__ __align__(1024) unsigned char smem[2 * HALF];
     lds_byte* const lds = (lds_byte*)smem;
     const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)lds);
@@ -249,15 +254,15 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product16_kernel(ProductArgs 
     tile_of(blockIdx.x, tm, tn, splits, mt, nt, split);
     const int m0 = mt * BM, n0 = nt * BN;
     const int k0 = split * steps_per * 64, k_left = min(g.K - k0, steps_per * 64);
-    const int whole = k_left >> 6, tail = k_left & 63, steps = whole + (tail != 0);
-    Window wa = window<AR, 2, 64>(g.a, g.lda, g.M, g.K, m0, k0), wb = window<BR, 2, 64>(g.b, g.ldb, g.N, g.K, n0, k0);
-    Loader16<AR, BM, WAVES> la;
-    Loader16<BR, BN, WAVES> lb;
+    const int whole = k_left / BK, tail = k_left % BK, steps = whole + (tail != 0);
+    Window wa = window<AR, 2, BK>(g.a, g.lda, g.M, g.K, m0, k0), wb = window<BR, 2, BK>(g.b, g.ldb, g.N, g.K, n0, k0);
+    Loader16<AR, BM, WAVES, BK> la;
+    Loader16<BR, BN, WAVES, BK> lb;
     la.plan(wave, lane, g.lda);
     lb.plan(wave, lane, g.ldb);
     const int wm = (wave % WM) * TM, wn = (wave / WM) * TN;
-    Reader16<T, AR, BM, FM> ra;
-    Reader16<T, BR, BN, FN> rb;
+    Reader16<T, AR, BM, FM, BK> ra;
+    Reader16<T, BR, BN, FN, BK> rb;
     ra.plan(wm, lr, lg);
     rb.plan(wn, lr, lg);
     f32x4 acc[FN][FM] = {};
@@ -270,7 +275,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product16_kernel(ProductArgs 
         lds_byte* const ta = lds + half * HALF;
         lds_byte* const tb = ta + A_BYTES;
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
+        for (int ks = 0; ks < BK / 32; ++ks) {
             typename Frag<T>::type fa[FM], fb[FN];
 #pragma unroll
             for (int j = 0; j < FM; ++j) fa[j] = ra.get(ta, j, ks);
@@ -406,11 +411,11 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product32_kernel(ProductArgs 
     rb.plan(wn, lr, lg);
     f32x4 acc[FN][FM] = {};
     la.ask(wa); lb.ask(wb);
-    for (int t = 0; t < steps; ++t) {
-        if (t + 1 == steps && (k_left & 31)) { la.cut(k_left & 31); lb.cut(k_left & 31); }
+    auto step = [&](auto last) {
+        if constexpr (decltype(last)::value) { la.cut(k_left - 32 * (steps - 1)); lb.cut(k_left - 32 * (steps - 1)); }
         __syncthreads();                                 // the last step's fragments have been read
         la.split(smem); lb.split(smem + 3 * PA);
-        if (t + 1 < steps) {
+        if constexpr (!decltype(last)::value) {
             wa.next(); wb.next();
             la.ask(wa); lb.ask(wb);
         }
@@ -431,7 +436,9 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product32_kernel(ProductArgs 
             for (int i = 0; i < FN; ++i)
 #pragma unroll
                 for (int j = 0; j < FM; ++j) acc[i][j] = mma(fb[QB[q]][i], fa[QA[q]][j], acc[i][j]);
-    }
+    };
+    for (int t = 0; t + 1 < steps; ++t) step(std::false_type{});
+    step(std::true_type{});                              // the only one that can be short
     // An infinity, a NaN or a value beyond bf16's range has no three parts (its remainder is infinity - infinity): what is
     // not finite here is taken from fp32 instructions instead, one k of a row per lane.
     float none = 0.f;                                    // NaN if any sum is not finite
@@ -631,13 +638,21 @@ void join(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
     else hipLaunchKernelGGL((join_kernel<T, 1>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, s, g, p.splits);
 }
 
+// Rows to 16-byte borders, zeros behind their ends: eight elements a thread (ld_dst is a multiple of eight).
 __global__ __launch_bounds__(256) void pack16_kernel(const uint16_t* __restrict__ src, int64_t ld_src, uint16_t* __restrict__ dst,
-                                                     int64_t ld_dst, int64_t rows, int64_t cols) {
-    const int64_t total = rows * ld_dst;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / ld_dst, c = i - r * ld_dst;
-        dst[i] = c < cols ? src[r * ld_src + c] : (uint16_t)0;
+                                                     int pieces, int64_t total, int cols) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= total) return;
+    const int64_t r = total < (1LL << 31) ? (int64_t)((unsigned)i / (unsigned)pieces) : i / pieces;
+    const int c = (int)(i - r * pieces) * 8;
+    const uint16_t* const p = src + r * ld_src + c;
+    u32x4 v;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+        const unsigned lo = c + 2 * d < cols ? p[2 * d] : 0, hi = c + 2 * d + 1 < cols ? p[2 * d + 1] : 0;
+        v[d] = lo | hi << 16;
     }
+    *reinterpret_cast<u32x4*>(dst + i * 8) = v;
 }
 
 // A thread has V columns and every RT-th row of its workgroup's share, two at a time; the sums over rows meet in LDS.
@@ -687,16 +702,17 @@ __global__ __launch_bounds__(SLOPE_THREADS) void slope_kernel(int act, const T* 
     }
 }
 
-template <class T, bool AR, bool BR, int BM, int BN, int WM, int WN>
+template <class T, bool AR, bool BR, int BM, int BN, int WM, int WN, int BK>
 void run16(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
     const int tm = cdiv(g.M, BM), tn = cdiv(g.N, BN);
-    hipLaunchKernelGGL((product16_kernel<T, AR, BR, BM, BN, WM, WN>), dim3(tm * tn * p.splits), dim3(64 * WM * WN), 0, s, g, tm, tn, p.splits, p.steps);
+    hipLaunchKernelGGL((product16_kernel<T, AR, BR, BM, BN, WM, WN, BK>), dim3(tm * tn * p.splits), dim3(64 * WM * WN), 0, s, g, tm, tn, p.splits, p.steps);
 }
 template <class T, bool AR, bool BR>
 void run16(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
-    if (p.tile == TILE_256) run16<T, AR, BR, 256, 256, 2, 4>(g, p, s);
-    else if (p.tile == TILE_128) run16<T, AR, BR, 128, 128, 2, 2>(g, p, s);
-    else run16<T, AR, BR, 64, 64, 2, 2>(g, p, s);
+    if (p.tile == TILE_256) run16<T, AR, BR, 256, 256, 2, 4, 64>(g, p, s);
+    else if (p.tile == TILE_128) run16<T, AR, BR, 128, 128, 2, 2, 64>(g, p, s);
+    else if (p.tile == TILE_ROWS) run16<T, AR, BR, 128, 256, 2, 4, 32>(g, p, s);
+    else run16<T, AR, BR, 64, 64, 2, 2, 64>(g, p, s);
 }
 template <class T>
 void few16(const ProductArgs& g, hipStream_t s) {
@@ -746,14 +762,17 @@ ProductPlan product_plan(corr_dtype type, int a_rows, int b_rows, int M, int N, 
     if (M <= 32 && !a_rows && !b_rows) { p.tile = TILE_FEW; return p; }
     int64_t tiles = (int64_t)cdiv(M, 64) * cdiv(N, 64);
     const int64_t t128 = (int64_t)cdiv(M, 128) * cdiv(N, 128), t256 = (int64_t)cdiv(M, 256) * cdiv(N, 256);
+    const int64_t trows = (int64_t)cdiv(M, 128) * cdiv(N, 256);
+    // Tiles of 128 x 256 in steps of 32 k, 16 waves a compute unit, where there is little to multiply for every element that is stored:
+    // 259200 x 128 -> 256: 44 us, 53 in tiles of 256; 32400 x 256 -> 1024 with gelu and preact: 48.5 and 54.  At k = 384: 95 and 88.
     // Tiles of 256 read operands half as often, but one workgroup fills a compute unit: for products that give every unit one, and
-    // that do not make them multiply much more (129600 x 256 -> 324: 58 us in tiles of 128, 70 in 256; x 324 -> 256: 53 and 48).
+    // that do not make them multiply much more (129600 x 320 -> 324: 58 us in tiles of 128, 70 in 256; x 324 -> 256: 53 and 48).
     // Tiles of 64 where 128 leaves units idle: 2852 x 1024 -> 256: 12.7 us, 14.8 in 128; 32400 x 256 -> 256: 12.6 and 11.9.
-    if (!wide && t256 >= 256 && t256 * 4 <= t128 * 1.25) { p.tile = TILE_256; tiles = t256; }
+    if (!wide && K <= 256 && N > 128 && trows >= 512) { p.tile = TILE_ROWS; tiles = trows; }
+    else if (!wide && t256 >= 256 && t256 * 4 <= t128 * 1.25) { p.tile = TILE_256; tiles = t256; }
     else if (t128 * all >= 256 * 4) { p.tile = TILE_128; tiles = t128; }
-    if (getenv("CORR_TILE")) { p.tile = atoi(getenv("CORR_TILE")); tiles = p.tile == 3 ? t256 : p.tile == 2 ? t128 : (int64_t)cdiv(M, 64) * cdiv(N, 64); }
     // workgroups for two or three on every compute unit, and at least eight steps for each
-    const int64_t want = p.tile == TILE_256 ? 256 : p.tile == TILE_128 ? 512 : 1024;
+    const int64_t want = p.tile == TILE_256 ? 256 : p.tile == TILE_128 || p.tile == TILE_ROWS ? 512 : 1024;
     if (tiles < want / 2) {
         int splits = (int)min((int64_t)(all / 8 > 0 ? all / 8 : 1), want / tiles);
         if (splits > 1) {
@@ -778,8 +797,9 @@ hipError_t launch_product(const ProductArgs& args, hipStream_t s) {
 }
 
 hipError_t launch_pack16(const void* src, int64_t ld_src, void* dst, int64_t ld_dst, int64_t rows, int64_t cols, hipStream_t s) {
-    const int64_t blocks = (rows * ld_dst + 255) / 256;
-    hipLaunchKernelGGL(pack16_kernel, dim3((unsigned)min(blocks, (int64_t)1 << 20)), dim3(256), 0, s, (const uint16_t*)src, ld_src, (uint16_t*)dst, ld_dst, rows, cols);
+    const int64_t total = rows * (ld_dst / 8);
+    hipLaunchKernelGGL(pack16_kernel, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, s, (const uint16_t*)src, ld_src, (uint16_t*)dst,
+                       (int)(ld_dst / 8), total, (int)cols);
     return hipGetLastError();
 }
 

@@ -1,6 +1,5 @@
 """The row operators' refusals and host arithmetic: no device work.  Refused calls return before anything is enqueued, so made-up
 addresses do."""
-import ctypes
 import os
 
 import pytest
@@ -50,7 +49,7 @@ def test_no_rows_need_nothing():
     assert _linear(b, M=0, x=None, w=None, y=None, ws=None, size=0) == 0
     assert b.corr_linear_workspace_bytes(torch.bfloat16, 0, 48, 64) == 0
     a = _norm(rows=0, h=None)
-    assert b.load_library().corr_residual_norm(ctypes.byref(a), H_OUT, N_OUT, None) == 0
+    assert b.load_library().corr_residual_norm(a, H_OUT, N_OUT, None) == 0
 
 
 def _backward(b, **kw):
@@ -78,7 +77,7 @@ def _norm(**kw):
     a = dict(stream_type=0, type=1, rows=10, cols=64, h=H, h_stride=64, y=Y, y_stride=64, gate=GATE, gate_stride=64, gate_act=5, scale=S1,
              h_scale=1.0, post=2, post_weight=P1, post_bias=P2, pre=1, pre_weight=P3, pre_bias=P4, eps=1e-5)
     a.update(kw)
-    return b.ResidualNormArgs(*a.values())
+    return b.residual_norm_args(*a.values())
 
 
 NO_BLOCK = dict(y=None, y_stride=0, gate=None, gate_stride=0, scale=None, post=0, post_weight=None, post_bias=None)
@@ -99,7 +98,7 @@ NO_BLOCK = dict(y=None, y_stride=0, gate=None, gate_stride=0, scale=None, post=0
 def test_norm_refusals(kw, outs, status):
     b = _b()
     a, o = _norm(**kw), dict({"h_out": H_OUT, "n_out": N_OUT}, **outs)
-    assert b.load_library().corr_residual_norm(ctypes.byref(a), o["h_out"], o["n_out"], None) == status
+    assert b.load_library().corr_residual_norm(a, o["h_out"], o["n_out"], None) == status
 
 
 def test_norm_refuses_no_arguments():
@@ -120,7 +119,7 @@ def test_norm_backward_refusals(kw, outs, status):
     o = dict(dh=DH, dn=DN, d1=D1, d2=D2, d3=D3, d4=D4, d5=D5, d6=D6, d7=D7, d8=D8, ws=WS, size=1 << 30)
     o.update(outs)
     a = _norm(**kw)
-    assert b.load_library().corr_residual_norm_backward(ctypes.byref(a), *o.values(), None) == status
+    assert b.load_library().corr_residual_norm_backward(a, *o.values(), None) == status
 
 
 def test_workspace_sizes():
