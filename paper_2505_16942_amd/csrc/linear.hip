@@ -767,18 +767,20 @@ ProductPlan product_plan(corr_dtype type, int a_rows, int b_rows, int M, int N, 
     // 259200 x 128 -> 256: 44 us, 53 in tiles of 256; 32400 x 256 -> 1024 with gelu and preact: 48.5 and 54.  At k = 384: 95 and 88.
     // Tiles of 256 read operands half as often, but one workgroup fills a compute unit: for products that give every unit one, and
     // that do not make them multiply much more (129600 x 320 -> 324: 58 us in tiles of 128, 70 in 256; x 324 -> 256: 53 and 48).
-    // Tiles of 64 where 128 leaves units idle: 2852 x 1024 -> 256: 12.7 us, 14.8 in 128; 32400 x 256 -> 256: 12.6 and 11.9.
+    // Tiles of 128 if they, or their splits, give 320 workgroups (5704 x 4096 -> 1024 fp16: 58 us, 77 in tiles of 64), else tiles of 64: 2048 x 1024 -> 256 fp32: 24 us in 128, 17 in 64;
+    // 2852 x 1024 -> 256 fp16: 14.8 and 12.7; 32400 x 256 -> 256: 11.9 and 12.6.
+    // Splits have eight steps or more; joining them costs about 4 us, as much as 16 steps of 16-bit tiles of 64 (2852 x 1024 -> 256: 7.5 us
+    // whole, 11.4 in two) or six of fp32.
+    const int most = all >= 32 || wide ? max(1, all / 8) : 1;
     if (!wide && K <= 256 && N > 128 && trows >= 512) { p.tile = TILE_ROWS; tiles = trows; }
     else if (!wide && t256 >= 256 && t256 * 4 <= t128 * 1.25) { p.tile = TILE_256; tiles = t256; }
-    else if (t128 * all >= 256 * 4) { p.tile = TILE_128; tiles = t128; }
-    // workgroups for two or three on every compute unit, and at least eight steps for each
-    const int64_t want = p.tile == TILE_256 ? 256 : p.tile == TILE_128 || p.tile == TILE_ROWS ? 512 : 1024;
+    else if (t128 * max((int64_t)1, min((int64_t)most, 512 / t128)) >= 320) { p.tile = TILE_128; tiles = t128; }
+    // workgroups for two (tiles of 64: four) on every compute unit
+    const int64_t want = p.tile == TILE_256 ? 256 : p.tile == TILE_64 ? 1024 : 512;
     if (tiles < want / 2) {
-        int splits = (int)min((int64_t)(all / 8 > 0 ? all / 8 : 1), want / tiles);
-        if (splits > 1) {
-            p.steps = cdiv(all, splits);
-            p.splits = cdiv(all, p.steps);
-        }
+        const int splits = (int)min((int64_t)most, want / tiles);
+        p.steps = cdiv(all, splits);
+        p.splits = cdiv(all, p.steps);
     }
     return p;
 }
