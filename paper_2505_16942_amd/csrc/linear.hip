@@ -759,7 +759,11 @@ ProductPlan product_plan(corr_dtype type, int a_rows, int b_rows, int M, int N, 
     const bool wide = type == CORR_TYPE_F32;
     const int bk = wide ? 32 : 64, all = cdiv(K, bk);
     ProductPlan p = {TILE_64, 1, all};
-    if (M <= 32 && !a_rows && !b_rows) { p.tile = TILE_FEW; return p; }
+    // Few rows: weights straight into the fragments, no joins.  A workgroup walks along all of k, so that a long k goes to tiles and splits
+    // instead (16 x 16384 -> 1024 bf16: 30 us, 11 in tiles; x 1024 -> 1024: 4.4 and 7.1), unless there are columns for every compute unit and
+    // the weights' bytes are what counts (1 x 16384 -> 16384 bf16: 110 and 143; 8 x 4096 -> 16384 fp32: 52 and 81).
+    const bool few = wide ? K <= 2048 || N >= 4096 : K <= 2048 || (M <= 8 && K <= 4096) || (M <= 16 && (int64_t)N * K >= 1 << 27);
+    if (M <= 32 && few && !a_rows && !b_rows) { p.tile = TILE_FEW; return p; }
     int64_t tiles = (int64_t)cdiv(M, 64) * cdiv(N, 64);
     const int64_t t128 = (int64_t)cdiv(M, 128) * cdiv(N, 128), t256 = (int64_t)cdiv(M, 256) * cdiv(N, 256);
     const int64_t trows = (int64_t)cdiv(M, 128) * cdiv(N, 256);

@@ -33,7 +33,8 @@ def _gen(seed):
 
 # (M, N, K): one element; few rows with whole, short and odd rows; one tile and its neighbours; a long k over few tiles; odd everything
 SIZES = [(1, 1, 1), (1, 16, 32), (1, 300, 1000), (3, 5, 7), (16, 256, 324), (17, 33, 65), (32, 130, 512), (33, 64, 64), (64, 64, 324),
-         (65, 126, 243), (129, 127, 81), (130, 1000, 36), (300, 8, 1024), (257, 257, 1100), (700, 256, 130), (40, 24, 4099)]
+         (65, 126, 243), (129, 127, 81), (130, 1000, 36), (300, 8, 1024), (257, 257, 1100), (700, 256, 130), (40, 24, 4099),
+         (100, 20, 3), (77, 1, 5), (2000, 1, 1), (1, 40, 9001), (32, 33, 2051), (20, 4100, 2100)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
@@ -105,6 +106,25 @@ def test_linear_large_tiles(dtype):
     x3, w3, dy3 = new(66000, 254, dtype=dtype), new(40, 254, dtype=dtype), new(66000, 40, dtype=dtype)
     for g, (v, e), what in zip(b.corr_linear_backward(x3, w3, dy3), ref.linear_backward(x3, w3, dy3, None, "none"), ("d_x", "d_w", "d_b")):
         ref.check("long " + what, g, v, e)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_linear_short_sums_and_large_results(dtype):
+    """Tiles for short sums (K up to 256, more than 128 columns, many rows), and results that go past the caches: rows here and there."""
+    b, new = _b(), _gen(5)
+    x, w, bias = new(66000, 70, dtype=dtype), new(131, 70, sigma=0.1, dtype=dtype), new(131)
+    z = torch.empty(66000, 131, dtype=dtype, device="cuda")
+    y = b.corr_linear(x, w, bias=bias, act=b.CORR_ACT_SILU, preact=z)
+    some = torch.cat([torch.arange(130), torch.arange(32700, 32900), torch.arange(65870, 66000)]).cuda()
+    wy, wz, ey, ez = ref.linear(x[some], w, bias, "silu", None)
+    ref.check("y", y[some], wy, ey)
+    ref.check("z", z[some], wz, ez)
+    M = (130 << 20) // 256 // x.element_size()
+    x, w, res = new(M, 264, dtype=dtype), new(256, 264, sigma=0.1, dtype=dtype), new(M, 256, dtype=dtype)
+    y = b.corr_linear(x, w, act=b.CORR_ACT_RELU, residual=res)
+    some = torch.cat([torch.arange(260), torch.arange(M // 2, M // 2 + 100), torch.arange(M - 300, M)]).cuda()
+    wy, _, ey, _ = ref.linear(x[some], w, None, "relu", res[some])
+    ref.check("large", y[some], wy, ey)
 
 
 @pytest.mark.parametrize("dtype", TYPES)

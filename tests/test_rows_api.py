@@ -127,7 +127,7 @@ def test_workspace_sizes():
     column sums.  Zero for sizes that are refused."""
     b = _b()
     assert b.corr_linear_workspace_bytes(torch.bfloat16, 129600, 256, 324) == 0
-    assert b.corr_linear_workspace_bytes(torch.bfloat16, 16, 256, 4097) == 0          # few rows are read as they are
+    assert b.corr_linear_workspace_bytes(torch.bfloat16, 16, 256, 2047) == 0          # few rows are read as they are
     split = b.corr_linear_workspace_bytes(torch.bfloat16, 64, 64, 1 << 16)
     assert split > 0 and split % (64 * 64 * 4) == 0
     odd = b.corr_linear_workspace_bytes(torch.float16, 4096, 256, 243)
