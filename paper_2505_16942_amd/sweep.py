@@ -140,10 +140,53 @@ def _backward_point(width: int, D: int, calls: int = 5):
     return H, W, res[0], res[1], res[2]
 
 
+def _timed_ms(fn, n: int = 5) -> float:
+    import torch
+    fn(); fn()
+    torch.cuda.synchronize()
+    e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    e0.record()
+    for _ in range(n):
+        fn()
+    e1.record()
+    torch.cuda.synchronize()
+    return e0.elapsed_time(e1) / n
+
+
+def _rows_point(H: int, W: int, dtype, C: int = 256, taps: int = 324):
+    """ms of an update block's calls on an H x W map, in their order, and of their gradients."""
+    import torch
+    from . import binding as cb
+    dev = torch.device("cuda:0")
+    g = torch.Generator(device=dev)
+    g.manual_seed(H)
+
+    def new(*shape, sigma=1.0, kind=dtype):
+        return (torch.randn(shape, device=dev, generator=g) * sigma).to(kind)
+    f32 = torch.float32
+    x, h, y = new(H * W, taps), new(H * W, C), new(H * W, C)
+    w0, w1, w2 = new(C, taps, sigma=taps ** -0.5), new(4 * C, C, sigma=C ** -0.5), new(C, 4 * C, sigma=(4 * C) ** -0.5)
+    b0, b1, b2, s, n1, n2, c2 = (new(k, sigma=0.1, kind=f32) for k in (C, 4 * C, C, C, C, C, C))
+    z0, z1, u = torch.empty_like(h), new(H * W, 4 * C), new(H * W, 4 * C)
+    end = dict(y=y, scale=s, pre=cb.CORR_NORM_LAYER, pre_weight=n2, pre_bias=c2)
+    calls = [lambda: cb.corr_linear(x, w0, bias=b0, act=cb.CORR_ACT_RELU, preact=z0),
+             lambda: cb.corr_residual_norm(h, pre_weight=n1),
+             lambda: cb.corr_linear(y, w1, bias=b1, act=cb.CORR_ACT_GELU, preact=z1),
+             lambda: cb.corr_linear(u, w2, bias=b2),
+             lambda: cb.corr_residual_norm(h, **end),
+             lambda: cb.corr_residual_norm_backward(h, d_h_out=y, d_n_out=y, **end),
+             lambda: cb.corr_linear_backward(u, w2, y),
+             lambda: cb.corr_linear_backward(y, w1, u, preact=z1, act=cb.CORR_ACT_GELU),
+             lambda: cb.corr_residual_norm_backward(h, pre_weight=n1, d_h_out=y, d_n_out=y),
+             lambda: cb.corr_linear_backward(x, w0, y, preact=z0, act=cb.CORR_ACT_RELU)]
+    return [_timed_ms(c) for c in calls]
+
+
 def main(argv=None) -> int:
     ap = argparse.ArgumentParser()
     ap.add_argument("--quick", action="store_true", help="fewer and smaller points")
     ap.add_argument("--backward", action="store_true", help="the gradient's table instead of the lookup's")
+    ap.add_argument("--block", action="store_true", help="the table of the calls that follow a lookup in an update block")
     args = ap.parse_args(argv)
     import torch
     from . import binding as cb
@@ -159,6 +202,15 @@ def main(argv=None) -> int:
         for var, val, (w, d) in pts:
             H, W, fwd, items, queries = _backward_point(w, d)
             print("| %s | %d | %dx%d | %.3f | %.3f | %.3f |" % (var, val, H, W, fwd, items, queries), flush=True)
+        return 0
+    if args.block:
+        print("| map HxW | type | projection ms | norm ms | widening ms | narrowing ms | residual and norm ms | gradients in turn, last first ms |")
+        print("|---|---|---|---|---|---|---|---|")
+        for H, W in ((46, 62), (135, 240)) if args.quick else ((46, 62), (135, 240), (270, 480), (540, 960)):
+            for dtype, name in ((torch.float32, "fp32"), (torch.bfloat16, "bf16")):
+                t = _rows_point(H, W, dtype)
+                print("| %dx%d | %s | %s | %s |" % (H, W, name, " | ".join("%.3f" % v for v in t[:5]), " ".join("%.3f" % v for v in t[5:])), flush=True)
+                torch.cuda.empty_cache()
         return 0
     base_w, base_it, base_d = 512, 32, 256
     if args.quick:
