@@ -239,7 +239,7 @@ typedef enum {
  *   preact   : NULL, or [M, N] dense: receives z, which corr_linear_backward reads.
  *   y        : [M, N] rows, y_stride.
  * fp32 products carry fp32's precision (each operand as three bf16 parts, six partial products).
- * Limits: M <= 2^30, N, K and strides <= 2^21, M*N and M*K <= 2^36; beyond: CORR_ERR_UNSUPPORTED.
+ * Limits: M <= 2^30, N, K and strides <= 2^21, M*N, M*K and N*K <= 2^36; beyond: CORR_ERR_UNSUPPORTED.
  */
 size_t corr_linear_workspace_bytes(corr_dtype type, int64_t M, int64_t N, int64_t K, int64_t x_stride);
 corr_status corr_linear(corr_dtype type, corr_activation act, const void* x, int64_t x_stride, const void* w, const float* bias,

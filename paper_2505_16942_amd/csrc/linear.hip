@@ -79,30 +79,25 @@ __device__ __forceinline__ void tile_of(int w, int tm, int tn, int splits, int& 
     n = 8 * panel + in - m * wide;
 }
 
-// ---- epilogue.  Rows on 4-byte borders (`words`) are loaded and stored V elements at a time, as far as they go.
-template <class T, int V> struct Words { typedef T type __attribute__((ext_vector_type(V), aligned(4))); };
-template <class T>
-__device__ __forceinline__ bool rows_words(const ProductArgs& g) {
-    if (sizeof(T) == 4) return true;
-    return ((g.N | g.ldy | (g.res ? g.ld_res : 0)) & 1) == 0 && (((uintptr_t)g.y | (uintptr_t)g.pre | (uintptr_t)g.res) & 3) == 0;
-}
+// ---- epilogue.  V elements of a row at a time, as far as they go, wherever the row begins (vector accesses need no border).
+template <class T, int V> struct Some { typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T)))); };
 // `past`: past the caches
 template <class T, int V>
-__device__ __forceinline__ void store_some(T* p, const float (&v)[V], int left, bool words, bool past = false) {
-    if (words && left >= V) {
-        typename Words<T, V>::type x;
+__device__ __forceinline__ void store_some(T* p, const float (&v)[V], int left, bool past = false) {
+    if (left >= V) {
+        typename Some<T, V>::type x;
 #pragma unroll
         for (int e = 0; e < V; ++e) x[e] = (T)v[e];
-        if (past) __builtin_nontemporal_store(x, reinterpret_cast<typename Words<T, V>::type*>(p));
-        else *reinterpret_cast<typename Words<T, V>::type*>(p) = x;
+        if (past) __builtin_nontemporal_store(x, reinterpret_cast<typename Some<T, V>::type*>(p));
+        else *reinterpret_cast<typename Some<T, V>::type*>(p) = x;
     } else
 #pragma unroll
         for (int e = 0; e < V; ++e) if (e < left) p[e] = (T)v[e];
 }
 template <class T, int V>
-__device__ __forceinline__ void load_some(const T* p, float (&v)[V], int left, bool words) {
-    if (words && left >= V) {
-        const typename Words<T, V>::type x = *reinterpret_cast<const typename Words<T, V>::type*>(p);
+__device__ __forceinline__ void load_some(const T* p, float (&v)[V], int left) {
+    if (left >= V) {
+        const typename Some<T, V>::type x = *reinterpret_cast<const typename Some<T, V>::type*>(p);
 #pragma unroll
         for (int e = 0; e < V; ++e) v[e] = (float)x[e];
     } else
@@ -111,20 +106,20 @@ __device__ __forceinline__ void load_some(const T* p, float (&v)[V], int left, b
 }
 // V elements of row m from column n on
 template <class T, int V>
-__device__ __forceinline__ void finish(const ProductArgs& g, float (&v)[V], const float (&bias)[V], int m, int n, bool words) {
+__device__ __forceinline__ void finish(const ProductArgs& g, float (&v)[V], const float (&bias)[V], int m, int n) {
     const int left = g.N - n;
     if (m >= g.M || left <= 0) return;
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] += bias[e];
-    if (g.pre) store_some<T, V>((T*)g.pre + (int64_t)m * g.N + n, v, left, words, g.past);
+    if (g.pre) store_some<T, V>((T*)g.pre + (int64_t)m * g.N + n, v, left, g.past);
     row_act_all(g.act, v);
     if (g.res) {
         float r[V];
-        load_some<T, V>((const T*)g.res + (int64_t)m * g.ld_res + n, r, left, words);
+        load_some<T, V>((const T*)g.res + (int64_t)m * g.ld_res + n, r, left);
 #pragma unroll
         for (int e = 0; e < V; ++e) v[e] += r[e];
     }
-    store_some<T, V>((T*)g.y + (int64_t)m * g.ldy + n, v, left, words, g.past);
+    store_some<T, V>((T*)g.y + (int64_t)m * g.ldy + n, v, left, g.past);
 }
 template <int V>
 __device__ __forceinline__ void load_bias(const ProductArgs& g, float (&bias)[V], int n) {
@@ -162,14 +157,13 @@ __device__ __forceinline__ void finish_wave(const ProductArgs& g, f32x4 (&acc)[F
     };
     if (splits > 1) {
         by_rows(std::integral_constant<int, 4>{}, [&](float (&v)[4], int m, int n) {
-            if (m < g.M && n < g.N) store_some<float, 4>(g.part + ((int64_t)split * g.M + m) * g.N + n, v, g.N - n, true);
+            if (m < g.M && n < g.N) store_some<float, 4>(g.part + ((int64_t)split * g.M + m) * g.N + n, v, g.N - n);
         });
     } else {
         constexpr int V = 16 / sizeof(T);
-        const bool words = rows_words<T>(g);
         float bias[V];
         load_bias(g, bias, n0 + lane % (16 * FN / V) * V);
-        by_rows(std::integral_constant<int, V>{}, [&](float (&v)[V], int m, int n) { finish<T, V>(g, v, bias, m, n, words); });
+        by_rows(std::integral_constant<int, V>{}, [&](float (&v)[V], int m, int n) { finish<T, V>(g, v, bias, m, n); });
     }
 }
 
@@ -441,13 +435,14 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product32_kernel(ProductArgs 
     step(std::true_type{});                              // the only one that can be short
     // An infinity, a NaN or a value beyond bf16's range has no three parts (its remainder is infinity - infinity): what is
     // not finite here is taken from fp32 instructions instead, one k of a row per lane.
-    float none = 0.f;                                    // NaN if any sum is not finite
+    float none = 0.f;                                    // NaN if any sum is not finite (past the borders anything may lie)
 #pragma unroll
     for (int i = 0; i < FN; ++i)
 #pragma unroll
         for (int j = 0; j < FM; ++j)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) none = fmaf(acc[i][j][e], 0.f, none);
+            for (int e = 0; e < 4; ++e)
+                none = fmaf(m0 + wm + 16 * j + lr < g.M && n0 + wn + 16 * i + 4 * lg + e < g.N ? acc[i][j][e] : 0.f, 0.f, none);
     if (__any(none != 0.f)) {
         const float* const A = (const float*)g.a;
         const float* const B = (const float*)g.b;
@@ -479,20 +474,16 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product32_kernel(ProductArgs 
 
 // ------------------------------------------------------------------------------------------------ few rows
 // Up to 16 MT rows: every weight is read once, straight into the matrix instruction's fragments.  A workgroup makes 16 columns
-// of C; its waves take turns along k and add up in LDS.  WIDE: rows on 4-byte borders, loaded 16 bytes a lane.
-template <class T, bool WIDE>
+// of C; its waves take turns along k and add up in LDS.
+template <class T>
 __device__ __forceinline__ typename Frag<T>::type few_load(const T* p, int left) {       // 8 elements, zeros from `left` on
-    typedef typename Frag<T>::type V;
-    if (WIDE && left >= 8) {
-        struct __attribute__((packed, aligned(4))) U { u32x4 v; };
-        return __builtin_bit_cast(V, reinterpret_cast<const U*>(p)->v);
-    }
-    V v = {};
+    if (left >= 8) return *reinterpret_cast<const typename Some<T, 8>::type*>(p);
+    typename Frag<T>::type v = {};
 #pragma unroll
     for (int e = 0; e < 8; ++e) if (e < left) v[e] = p[e];
     return v;
 }
-template <class T, bool WIDE, int WAVES, int MT>
+template <class T, int WAVES, int MT>
 __global__ __launch_bounds__(64 * WAVES) void few_rows16_kernel(ProductArgs g) {
     __shared__ f32x4 sums[WAVES][MT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, lg = lane >> 4;
@@ -507,11 +498,11 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows16_kernel(ProductArgs g) {
     for (; k - lg * 8 + 32 * U <= g.K; k += WAVES * 32 * U) {
         typename Frag<T>::type w[U], x[U][MT];
 #pragma unroll
-        for (int u = 0; u < U; ++u) w[u] = few_load<T, WIDE>(W + k + 32 * u, 8);
+        for (int u = 0; u < U; ++u) w[u] = few_load<T>(W + k + 32 * u, 8);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int j = 0; j < MT; ++j) x[u][j] = few_load<T, WIDE>(X[j] + k + 32 * u, 8);
+            for (int j = 0; j < MT; ++j) x[u][j] = few_load<T>(X[j] + k + 32 * u, 8);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -519,29 +510,25 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows16_kernel(ProductArgs g) {
     }
     for (int u = 0; u < U; ++u, k += 32) {               // the one wave whose turn the last, shorter stretch is
         if (k - lg * 8 >= g.K) break;
-        const typename Frag<T>::type w = few_load<T, WIDE>(W + k, g.K - k);
+        const typename Frag<T>::type w = few_load<T>(W + k, g.K - k);
 #pragma unroll
-        for (int j = 0; j < MT; ++j) acc[j] = mma(w, few_load<T, WIDE>(X[j] + k, g.K - k), acc[j]);
+        for (int j = 0; j < MT; ++j) acc[j] = mma(w, few_load<T>(X[j] + k, g.K - k), acc[j]);
     }
 #pragma unroll
     for (int j = 0; j < MT; ++j) sums[wave][j][lane] = acc[j];
     __syncthreads();
-    const bool words = rows_words<T>(g);
     for (int j = wave; j < MT; j += WAVES) {
         f32x4 x = sums[0][j][lane];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) x += sums[w][j][lane];
         float v[4] = {x[0], x[1], x[2], x[3]}, bias[4];
         load_bias(g, bias, n0 + 4 * lg);
-        finish<T, 4>(g, v, bias, 16 * j + lr, n0 + 4 * lg, words);
+        finish<T, 4>(g, v, bias, 16 * j + lr, n0 + 4 * lg);
     }
 }
 // fp32: v_mfma_f32_16x16x4_f32, whose four k are the same element of four lanes' 16 bytes.
 __device__ __forceinline__ f32x4 few_load32(const float* p, int left) {
-    if (left >= 4) {
-        struct __attribute__((packed, aligned(4))) U { f32x4 v; };
-        return reinterpret_cast<const U*>(p)->v;
-    }
+    if (left >= 4) return *reinterpret_cast<const Some<float, 4>::type*>(p);
     f32x4 v = {};
 #pragma unroll
     for (int e = 0; e < 4; ++e) if (e < left) v[e] = p[e];
@@ -587,14 +574,13 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows32_kernel(ProductArgs g) {
 #pragma unroll
     for (int j = 0; j < MT; ++j) sums[wave][j][lane] = acc[j];
     __syncthreads();
-    const bool words = rows_words<float>(g);
     for (int j = wave; j < MT; j += WAVES) {
         f32x4 x = sums[0][j][lane];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) x += sums[w][j][lane];
         float v[4] = {x[0], x[1], x[2], x[3]}, bias[4];
         load_bias(g, bias, n0 + 4 * lg);
-        finish<float, 4>(g, v, bias, 16 * j + lr, n0 + 4 * lg, words);
+        finish<float, 4>(g, v, bias, 16 * j + lr, n0 + 4 * lg);
     }
 }
 
@@ -615,7 +601,7 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs g, int splits) {
 #pragma unroll 4
         for (int s = lane; s < splits; s += LANES, p += LANES * plane) {
             float v[4];
-            load_some<float, 4>(p, v, g.N - n, true);
+            load_some<float, 4>(p, v, g.N - n);
             x += f32x4{v[0], v[1], v[2], v[3]};
         }
     }
@@ -629,7 +615,7 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs g, int splits) {
     if (q >= total) return;
     float v[4] = {x[0], x[1], x[2], x[3]}, bias[4];
     load_bias(g, bias, n);
-    finish<T, 4>(g, v, bias, (int)m, n, rows_words<T>(g));
+    finish<T, 4>(g, v, bias, (int)m, n);
 }
 template <class T>
 void join(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
@@ -638,21 +624,26 @@ void join(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
     else hipLaunchKernelGGL((join_kernel<T, 1>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, s, g, p.splits);
 }
 
-// Rows to 16-byte borders, zeros behind their ends: eight elements a thread (ld_dst is a multiple of eight).
-__global__ __launch_bounds__(256) void pack16_kernel(const uint16_t* __restrict__ src, int64_t ld_src, uint16_t* __restrict__ dst,
-                                                     int pieces, int64_t total, int cols) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= total) return;
-    const int64_t r = total < (1LL << 31) ? (int64_t)((unsigned)i / (unsigned)pieces) : i / pieces;
-    const int c = (int)(i - r * pieces) * 8;
-    const uint16_t* const p = src + r * ld_src + c;
-    u32x4 v;
+// Rows to 16-byte borders, zeros behind their ends, of two matrices in one launch: eight elements a thread.
+__global__ __launch_bounds__(256) void pack16_kernel(Pack16 one, Pack16 two) {
+    const int64_t ones = one.rows * (one.ld_dst / 8), all = ones + two.rows * (two.ld_dst / 8);
+    for (int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x; k < all; k += (int64_t)gridDim.x * 256) {
+        const Pack16& p = k < ones ? one : two;
+        const int64_t i = k < ones ? k : k - ones;
+        const int pieces = (int)(p.ld_dst / 8);
+        const int64_t r = all < (1LL << 31) ? (int64_t)((unsigned)i / (unsigned)pieces) : i / pieces;
+        const int c = (int)(i - r * pieces) * 8;
+        const uint16_t* const src = (const uint16_t*)p.src + r * p.ld_src + c;
+        u32x4 x;
+        if (c + 8 <= p.cols) x = __builtin_bit_cast(u32x4, *reinterpret_cast<const Some<short, 8>::type*>(src));
+        else
 #pragma unroll
-    for (int d = 0; d < 4; ++d) {
-        const unsigned lo = c + 2 * d < cols ? p[2 * d] : 0, hi = c + 2 * d + 1 < cols ? p[2 * d + 1] : 0;
-        v[d] = lo | hi << 16;
+            for (int d = 0; d < 4; ++d) {
+                const unsigned lo = c + 2 * d < p.cols ? src[2 * d] : 0, hi = c + 2 * d + 1 < p.cols ? src[2 * d + 1] : 0;
+                x[d] = lo | hi << 16;
+            }
+        *reinterpret_cast<u32x4*>((uint16_t*)p.dst + i * 8) = x;
     }
-    *reinterpret_cast<u32x4*>(dst + i * 8) = v;
 }
 
 // A thread has V columns and every RT-th row of its workgroup's share, two at a time; the sums over rows meet in LDS.
@@ -670,11 +661,11 @@ __global__ __launch_bounds__(SLOPE_THREADS) void slope_kernel(int act, const T* 
         for (int64_t m = lo + r0; m < hi; m += 2 * rt) {
             const bool two = m + rt < hi;
             float v[2][V], s[2][V];
-            load_some<T, V>(dy + m * ld_dy + n, v[0], left, V > 1);
-            if (act != CORR_ACT_NONE) load_some<T, V>(z + m * N + n, s[0], left, V > 1);
+            load_some<T, V>(dy + m * ld_dy + n, v[0], left);
+            if (act != CORR_ACT_NONE) load_some<T, V>(z + m * N + n, s[0], left);
             if (two) {
-                load_some<T, V>(dy + (m + rt) * ld_dy + n, v[1], left, V > 1);
-                if (act != CORR_ACT_NONE) load_some<T, V>(z + (m + rt) * N + n, s[1], left, V > 1);
+                load_some<T, V>(dy + (m + rt) * ld_dy + n, v[1], left);
+                if (act != CORR_ACT_NONE) load_some<T, V>(z + (m + rt) * N + n, s[1], left);
             }
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
@@ -684,7 +675,7 @@ __global__ __launch_bounds__(SLOPE_THREADS) void slope_kernel(int act, const T* 
 #pragma unroll
                     for (int e = 0; e < V; ++e) v[u][e] *= s[u][e];
                 }
-                if (dz) store_some<T, V>(dz + (m + u * rt) * ld_dz + n, v[u], left, V > 1);
+                if (dz) store_some<T, V>(dz + (m + u * rt) * ld_dz + n, v[u], left);
 #pragma unroll
                 for (int e = 0; e < V; ++e) sum[e] += v[u][e];
             }
@@ -698,7 +689,7 @@ __global__ __launch_bounds__(SLOPE_THREADS) void slope_kernel(int act, const T* 
         for (int r = 1; r < rt; ++r)
 #pragma unroll
             for (int e = 0; e < V; ++e) sum[e] += sums[r * ct + c][e];
-        store_some<float, V>(part + (int64_t)blockIdx.y * N + n, sum, left, true);
+        store_some<float, V>(part + (int64_t)blockIdx.y * N + n, sum, left);
     }
 }
 
@@ -716,12 +707,11 @@ void run16(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
 }
 template <class T>
 void few16(const ProductArgs& g, hipStream_t s) {
-    const bool wide = product_direct(g.type, g.a, g.lda, 0) && product_direct(g.type, g.b, g.ldb, 0);
     const dim3 grid(cdiv(g.N, 16));
-#define FEW16(W, WAVES, MT) hipLaunchKernelGGL((few_rows16_kernel<T, W, WAVES, MT>), grid, dim3(64 * WAVES), 0, s, g)
+#define FEW16(WAVES, MT) hipLaunchKernelGGL((few_rows16_kernel<T, WAVES, MT>), grid, dim3(64 * WAVES), 0, s, g)
     const bool narrow = g.N <= 4096;
-    if (g.M <= 16) { if (wide) { if (narrow) FEW16(true, 8, 1); else FEW16(true, 4, 1); } else FEW16(false, 8, 1); }
-    else { if (wide) { if (narrow) FEW16(true, 8, 2); else FEW16(true, 4, 2); } else FEW16(false, 8, 2); }
+    if (g.M <= 16) { if (narrow) FEW16(8, 1); else FEW16(4, 1); }
+    else { if (narrow) FEW16(8, 2); else FEW16(4, 2); }
 #undef FEW16
 }
 template <class T>
@@ -802,14 +792,15 @@ hipError_t launch_product(const ProductArgs& args, hipStream_t s) {
     return hipGetLastError();
 }
 
-hipError_t launch_pack16(const void* src, int64_t ld_src, void* dst, int64_t ld_dst, int64_t rows, int64_t cols, hipStream_t s) {
-    const int64_t total = rows * (ld_dst / 8);
-    hipLaunchKernelGGL(pack16_kernel, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, s, (const uint16_t*)src, ld_src, (uint16_t*)dst,
-                       (int)(ld_dst / 8), total, (int)cols);
+hipError_t launch_pack16(const Pack16& one, const Pack16& two, hipStream_t s) {
+    const int64_t total = one.rows * (one.ld_dst / 8) + two.rows * (two.ld_dst / 8);
+    if (!total) return hipSuccess;
+    const int64_t blocks = (total + 255) / 256;
+    hipLaunchKernelGGL(pack16_kernel, dim3((unsigned)(blocks < 1 << 20 ? blocks : 1 << 20)), dim3(256), 0, s, one, two);
     return hipGetLastError();
 }
 
-int slope_parts(int64_t M, int N) { (void)N; return (int)min((int64_t)1024, max((int64_t)1, (M + 15) / 16)); }
+int slope_parts(int64_t M, int N) { (void)N; return (int)min((int64_t)1024, max((int64_t)1, (M + 31) / 32)); }
 
 namespace {
 template <class T, int V>
@@ -821,19 +812,12 @@ void slope(int act, const void* dy, int64_t ld_dy, const void* z, void* dz, int6
     hipLaunchKernelGGL((slope_kernel<T, V>), dim3(cdiv(N, ct * V), parts), dim3(SLOPE_THREADS), 0, s, act, (const T*)dy, ld_dy, (const T*)z,
                        (T*)dz, ld_dz, part, M, N, ct, per);
 }
-template <class T>
-void slope_of(int act, const void* dy, int64_t ld_dy, const void* z, void* dz, int64_t ld_dz, float* part, int64_t M, int N, hipStream_t s) {
-    constexpr int V = 16 / sizeof(T);
-    const bool words = sizeof(T) == 4 || (((N | ld_dy) & 1) == 0 && (((uintptr_t)dy | (uintptr_t)z) & 3) == 0);   // dz lies in the workspace
-    if (words) slope<T, V>(act, dy, ld_dy, z, dz, ld_dz, part, M, N, s);
-    else slope<T, 1>(act, dy, ld_dy, z, dz, ld_dz, part, M, N, s);
-}
 }  // namespace
 
 hipError_t launch_slope(corr_dtype t, int act, const void* dy, int64_t ld_dy, const void* z, void* dz, int64_t ld_dz, float* part,
                         int64_t M, int N, hipStream_t s) {
-    if (t == CORR_TYPE_F32) slope_of<float>(act, dy, ld_dy, z, dz, ld_dz, part, M, N, s);
-    else if (t == CORR_TYPE_BF16) slope_of<__bf16>(act, dy, ld_dy, z, dz, ld_dz, part, M, N, s);
-    else slope_of<_Float16>(act, dy, ld_dy, z, dz, ld_dz, part, M, N, s);
+    if (t == CORR_TYPE_F32) slope<float, 4>(act, dy, ld_dy, z, dz, ld_dz, part, M, N, s);
+    else if (t == CORR_TYPE_BF16) slope<__bf16, 8>(act, dy, ld_dy, z, dz, ld_dz, part, M, N, s);
+    else slope<_Float16, 8>(act, dy, ld_dy, z, dz, ld_dz, part, M, N, s);
     return hipGetLastError();
 }

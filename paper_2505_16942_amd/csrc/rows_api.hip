@@ -33,7 +33,7 @@ struct Carver {                           // pieces of the workspace on 256-byte
 
 corr_status check_linear(corr_dtype type, corr_activation act, int64_t M, int64_t N, int64_t K) {
     if (!known(type) || !known(act) || M < 0 || N <= 0 || K <= 0) return CORR_ERR_INVALID_ARG;
-    if (M > MAX_ROWS || N > MAX_COLS || K > MAX_COLS || M * N > MAX_ELEMENTS || M * K > MAX_ELEMENTS) return CORR_ERR_UNSUPPORTED;
+    if (M > MAX_ROWS || N > MAX_COLS || K > MAX_COLS || M * N > MAX_ELEMENTS || M * K > MAX_ELEMENTS || N * K > MAX_ELEMENTS) return CORR_ERR_UNSUPPORTED;
     return CORR_OK;
 }
 // rows of an odd number of 16-bit elements (or an odd number apart) are copied to rows that start on 16-byte borders
@@ -153,8 +153,9 @@ corr_status corr_linear(corr_dtype type, corr_activation act, const void* x, int
     p.a = x; p.lda = x_stride;
     p.b = w; p.ldb = K;
     p.M = (int)M; p.N = (int)N; p.K = (int)K;
-    if (l.pack_x) { e = launch_pack16(x, x_stride, ws + l.x, up8(K), M, K, s); p.a = ws + l.x; p.lda = up8(K); }
-    if (l.pack_w && e == hipSuccess) { e = launch_pack16(w, K, ws + l.w, up8(K), N, K, s); p.b = ws + l.w; p.ldb = up8(K); }
+    e = launch_pack16({x, x_stride, ws + l.x, up8(K), l.pack_x ? M : 0, K}, {w, K, ws + l.w, up8(K), l.pack_w ? N : 0, K}, s);
+    if (l.pack_x) { p.a = ws + l.x; p.lda = up8(K); }
+    if (l.pack_w) { p.b = ws + l.w; p.ldb = up8(K); }
     p.bias = bias; p.res = residual; p.ld_res = residual_stride; p.pre = preact; p.y = y; p.ldy = y_stride;
     p.part = reinterpret_cast<float*>(ws + l.part);
     if (e == hipSuccess) e = launch_product(p, s);
@@ -203,23 +204,25 @@ corr_status corr_linear_backward(corr_dtype type, corr_activation act, const voi
             e = launch_column_sums(sums, l.parts, 1, (int)N, o, s);
         }
     }
+    if (e == hipSuccess)
+        e = launch_pack16({x, x_stride, ws + l.x, up8(K), l.pack_x && d_w ? M : 0, K}, {w, K, ws + l.w, up8(K), l.pack_w && d_x ? N : 0, K}, s);
     ProductArgs p = {};
     p.type = type; p.act = CORR_ACT_NONE;
     p.a = dz; p.lda = ld_dz;
     p.part = reinterpret_cast<float*>(ws + l.part);
     if (d_x && e == hipSuccess) {
         p.b = w; p.ldb = K; p.b_rows = 1;
-        if (l.pack_w) { e = launch_pack16(w, K, ws + l.w, up8(K), N, K, s); p.b = ws + l.w; p.ldb = up8(K); }
+        if (l.pack_w) { p.b = ws + l.w; p.ldb = up8(K); }
         p.M = (int)M; p.N = (int)K; p.K = (int)N;
         p.y = d_x; p.ldy = K;
-        if (e == hipSuccess) e = launch_product(p, s);
+        e = launch_product(p, s);
     }
     if (d_w && e == hipSuccess) {
         p.b = x; p.ldb = x_stride; p.a_rows = p.b_rows = 1;
-        if (l.pack_x) { e = launch_pack16(x, x_stride, ws + l.x, up8(K), M, K, s); p.b = ws + l.x; p.ldb = up8(K); }
+        if (l.pack_x) { p.b = ws + l.x; p.ldb = up8(K); }
         p.M = (int)N; p.N = (int)K; p.K = (int)M;
         p.y = d_w; p.ldy = K;
-        if (e == hipSuccess) e = launch_product(p, s);
+        e = launch_product(p, s);
     }
     return e == hipSuccess ? CORR_OK : CORR_ERR_HIP;
 }

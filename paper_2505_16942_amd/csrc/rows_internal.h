@@ -25,12 +25,9 @@ static inline size_t product_part_bytes(const ProductPlan& p, int M, int N) {
     return p.splits > 1 ? (size_t)p.splits * M * N * 4 : 0;
 }
 hipError_t launch_product(const ProductArgs& p, hipStream_t s);
-// whether the 16-byte pieces of a matrix can be loaded where they lie: rows of `cols` elements, `ld` apart, on 4-byte borders
-static inline bool product_direct(corr_dtype t, const void* p, int64_t ld, int64_t cols) {
-    return t == CORR_TYPE_F32 || (((uintptr_t)p & 3) == 0 && (ld & 1) == 0 && (cols & 1) == 0);
-}
-// dst[r][0 .. ld_dst) = src[r][0 .. cols), zeros behind (16-bit elements)
-hipError_t launch_pack16(const void* src, int64_t ld_src, void* dst, int64_t ld_dst, int64_t rows, int64_t cols, hipStream_t s);
+// dst[r][0 .. ld_dst) = src[r][0 .. cols), zeros behind (16-bit elements, ld_dst a multiple of eight); no rows: nothing to do
+struct Pack16 { const void* src; int64_t ld_src; void* dst; int64_t ld_dst, rows, cols; };
+hipError_t launch_pack16(const Pack16& one, const Pack16& two, hipStream_t s);
 // dz = dy * act'(z) as `type` (dz may be null), and the column sums of the unrounded dz by parts (part may be null)
 int slope_parts(int64_t M, int N);
 hipError_t launch_slope(corr_dtype t, int act, const void* dy, int64_t ld_dy, const void* z, void* dz, int64_t ld_dz, float* part,

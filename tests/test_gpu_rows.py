@@ -200,6 +200,18 @@ def test_linear_not_finite(dtype, M, K):
     assert torch.isfinite(d_w).all(1).cpu().tolist() == [n != 5 for n in range(N)]
 
 
+def test_linear_odd_columns_beside_nan_in_the_workspace():
+    """The gradient's own dz has rows with room behind them: what an earlier call left there reaches no result."""
+    b, new = _b(), _gen(41)
+    for dtype in TYPES:
+        M, N, K = 300, 37, 70
+        x, w, dy, z = new(M, K, dtype=dtype), new(N, K, sigma=0.1, dtype=dtype), new(M, N, dtype=dtype), new(M, N, dtype=dtype)
+        ws = torch.full((b.corr_linear_backward_workspace_bytes(dtype, b.CORR_ACT_SILU, M, N, K),), 0xff, dtype=torch.uint8, device="cuda")
+        got = b.corr_linear_backward(x, w, dy, preact=z, act=b.CORR_ACT_SILU, workspace=ws)
+        for g, (v, e), what in zip(got, ref.linear_backward(x, w, dy, z, "silu"), ("d_x", "d_w", "d_b")):
+            ref.check("%s %s" % (what, dtype), g, v, e)
+
+
 def test_linear_huge_fp32():
     """Values past the largest bf16 and products that only just fit."""
     b, new = _b(), _gen(9)

@@ -30,7 +30,7 @@ def _linear(b, **kw):
     (dict(type=3), -1), (dict(type=-1), -1), (dict(act=6), -1), (dict(act=-1), -1), (dict(x=None), -1), (dict(w=None), -1), (dict(y=None), -1),
     (dict(M=-1), -1), (dict(N=0), -1), (dict(K=0), -1), (dict(N=-4), -1), (dict(xs=63), -1), (dict(ys=47), -1), (dict(res=RES, rs=47), -1),
     (dict(M=(1 << 30) + 1), -2), (dict(N=MAX + 1, ys=MAX + 1), -2), (dict(K=MAX + 1, xs=MAX + 1), -2), (dict(xs=MAX + 1), -2),
-    (dict(ys=MAX + 1), -2), (dict(res=RES, rs=MAX + 1), -2), (dict(M=1 << 30, N=128, ys=128), -2), (dict(M=1 << 30, K=128, xs=128), -2),
+    (dict(ys=MAX + 1), -2), (dict(res=RES, rs=MAX + 1), -2), (dict(M=1 << 30, N=128, ys=128), -2), (dict(M=1 << 30, K=128, xs=128), -2), (dict(N=1 << 19, ys=1 << 19, K=1 << 18, xs=1 << 18), -2),
     (dict(x=X + 2), -1), (dict(w=W + 2), -1), (dict(y=Y + 1), -1), (dict(bias=BIAS + 2), -1), (dict(pre=PRE + 1), -1), (dict(type=0, y=Y + 2), -1),
     (dict(res=RES + 1, rs=48), -1),
     # results that lie in what is read, or in each other; a residual that is nearly the result
