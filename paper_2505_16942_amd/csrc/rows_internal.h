@@ -42,7 +42,7 @@ struct NormArgs {
     float* part;                                   // [parts][5][cols]: scale, post weight, post bias, pre weight, pre bias
     int parts;
 };
-int norm_backward_parts(int64_t rows, int64_t cols);
+int norm_backward_parts(int64_t rows, int64_t cols, bool full);
 // one instantiation of residual_norm.hip per pair of stream and row types
 #define NORM_PAIRS(X) X(F32, F32, f32_f32) X(F32, BF16, f32_bf16) X(F32, F16, f32_f16) X(BF16, BF16, bf16_bf16) X(F16, F16, f16_f16)
 #define CORR_DECLARE_NORM(S, T, name)                                          \
