@@ -11,7 +11,6 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) unsigned char lds_byte;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
@@ -168,11 +167,14 @@ __device__ __forceinline__ void finish_wave(const ProductArgs& g, f32x4 (&acc)[F
 }
 
 // ------------------------------------------------------------------------------------------------ 16-bit operands
-// A workgroup makes BM x BN elements in steps of 64 k.  Tiles lie in LDS as they are stored, in two halves that take turns: while
+// A workgroup makes BM x BN elements in steps of BK k.  Tiles lie in LDS as they are stored, in two halves that take turns: while
 // one is multiplied, the next step's 16-byte pieces land in the other.
-//   k contiguous:    rows of 128 bytes, piece p of row r at p ^ (r & 7)
-//   rows contiguous: 64 k-rows of 2 R bytes, 32-byte block c of row k at c ^ turn(k); read by the transposing LDS load
-// so that neither the rows of a fragment nor the k of a transposed one meet in a bank.
+//   k contiguous:    rows of 2 BK bytes, piece p of row r at p ^ (r & 7) (BK = 32: p ^ (r / 2 & 3))
+//   rows contiguous: BK k-rows of 2 R bytes, 32-byte block c of row k at c ^ turn(k); read by the transposing LDS load
+// so that neither the rows of a fragment nor the k of a transposed one meet in a bank (LDS conflict cycles: 1 in 900).
+// 8192^3 bf16 with residual: 0.88 ms, 1.26 PFLOP/s, bound by the matrix cores under the card's power limit.  Short sums are bound by
+// bytes and by the turns of a tile (load, multiply, store): 32400 x 256 -> 1024, gelu, preact: 48 us, 149 MB.  A third stage in LDS and
+// orders of k that differ from tile to tile made no difference.
 template <int R> __device__ __forceinline__ int turn(int k) {
     return R >= 128 ? (k & 3) | ((k >> 3) & 1) << 2 : (k & 3) ^ ((k >> 3) & 1);
 }
@@ -308,6 +310,9 @@ __global__ __launch_bounds__(64 * WM * WN, BK == 32 ? 4 : 2) void product16_kern
 // their way into registers meanwhile.
 //   k contiguous:    rows of 64 bytes, piece p of row r at p ^ (r / 2 & 3)
 //   rows contiguous: as for 16 bits, 32 k-rows
+// 4096^3: 0.61 ms = 225 TFLOP/s, 1.35 PFLOP/s of bf16 products; 518400 x 324 -> 256: 600 to 690 us.  There matrix instructions fill 43 % of the
+// cycles, splitting 28 %, at a clock that power holds at 1.8 GHz; without loads it takes 531 us, without stores 611, with one product
+// of six 472.  Two workgroups a compute unit; a third spills (838 us), and so does a second set of loads on their way.
 template <bool ROWS, int R, int NT>
 struct Loader32 {
     static constexpr int PIECES = R * 8 / NT;
@@ -474,7 +479,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product32_kernel(ProductArgs 
 
 // ------------------------------------------------------------------------------------------------ few rows
 // Up to 16 MT rows: every weight is read once, straight into the matrix instruction's fragments.  A workgroup makes 16 columns
-// of C; its waves take turns along k and add up in LDS.
+// of C; its waves take turns along k and add up in LDS.  Bound by the weights' bytes: 1 x 4096 -> 16384 bf16: 22 us, 6.1 TB/s (weights that
+// lie in the memory-side cache; 28 from memory).
 template <class T>
 __device__ __forceinline__ typename Frag<T>::type few_load(const T* p, int left) {       // 8 elements, zeros from `left` on
     if (left >= 8) return *reinterpret_cast<const typename Some<T, 8>::type*>(p);
@@ -646,7 +652,9 @@ __global__ __launch_bounds__(256) void pack16_kernel(Pack16 one, Pack16 two) {
     }
 }
 
-// A thread has V columns and every RT-th row of its workgroup's share, two at a time; the sums over rows meet in LDS.
+// dz = dy act'(z) and its column sums in one pass.  A thread has V columns and every RT-th row of its workgroup's share, two at a time; the sums
+// over rows meet in LDS.  Bound by bytes: 32400 x 1024 fp32: 74 us, 5.4 TB/s; 129600 x 256 bf16: 42 us, 4.7 TB/s.  dz is rounded to the
+// operands' type because the matrix cores take it so; the sums add what was not rounded.
 constexpr int SLOPE_THREADS = 256;
 template <class T, int V>
 __global__ __launch_bounds__(SLOPE_THREADS) void slope_kernel(int act, const T* __restrict__ dy, int64_t ld_dy, const T* __restrict__ z,
@@ -761,8 +769,8 @@ ProductPlan product_plan(corr_dtype type, int a_rows, int b_rows, int M, int N, 
     // 259200 x 128 -> 256: 44 us, 53 in tiles of 256; 32400 x 256 -> 1024 with gelu and preact: 48.5 and 54.  At k = 384: 95 and 88.
     // Tiles of 256 read operands half as often, but one workgroup fills a compute unit: for products that give every unit one, and
     // that do not make them multiply much more (129600 x 320 -> 324: 58 us in tiles of 128, 70 in 256; x 324 -> 256: 53 and 48).
-    // Tiles of 128 if they, or their splits, give 320 workgroups (5704 x 4096 -> 1024 fp16: 58 us, 77 in tiles of 64), else tiles of 64: 2048 x 1024 -> 256 fp32: 24 us in 128, 17 in 64;
-    // 2852 x 1024 -> 256 fp16: 14.8 and 12.7; 32400 x 256 -> 256: 11.9 and 12.6.
+    // Tiles of 128 if they, or their splits, give 320 workgroups (5704 x 4096 -> 1024 fp16: 58 us, 77 in tiles of 64), else tiles of 64
+    // (2048 x 1024 -> 256 fp32: 18 us, 24 in tiles of 128; 2852 x 1024 -> 256 fp16: 12.7 and 14.8).
     // Splits have eight steps or more; joining them costs about 4 us, as much as 16 steps of 16-bit tiles of 64 (2852 x 1024 -> 256: 7.5 us
     // whole, 11.4 in two) or six of fp32.
     const int most = all >= 32 || wide ? max(1, all / 8) : 1;
@@ -800,14 +808,14 @@ hipError_t launch_pack16(const Pack16& one, const Pack16& two, hipStream_t s) {
     return hipGetLastError();
 }
 
-int slope_parts(int64_t M, int N) { (void)N; return (int)min((int64_t)1024, max((int64_t)1, (M + 31) / 32)); }
+int slope_parts(int64_t M) { return (int)min((int64_t)1024, max((int64_t)1, (M + 31) / 32)); }
 
 namespace {
 template <class T, int V>
 void slope(int act, const void* dy, int64_t ld_dy, const void* z, void* dz, int64_t ld_dz, float* part, int64_t M, int N, hipStream_t s) {
     int ct = 1;
     while (ct < SLOPE_THREADS && ct * V < N) ct *= 2;
-    const int parts = slope_parts(M, N);
+    const int parts = slope_parts(M);
     const int64_t per = (M + parts - 1) / parts;
     hipLaunchKernelGGL((slope_kernel<T, V>), dim3(cdiv(N, ct * V), parts), dim3(SLOPE_THREADS), 0, s, act, (const T*)dy, ld_dy, (const T*)z,
                        (T*)dz, ld_dz, part, M, N, ct, per);

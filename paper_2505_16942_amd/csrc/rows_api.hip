@@ -67,7 +67,7 @@ BackwardLayout backward_layout(corr_dtype t, corr_activation act, int64_t M, int
     const size_t px = product_part_bytes(product_plan(t, 0, 1, (int)M, (int)K, (int)N), (int)M, (int)K);
     const size_t pw = product_part_bytes(product_plan(t, 1, 1, (int)N, (int)K, (int)M), (int)N, (int)K);
     l.part = c.take(px > pw ? px : pw);
-    l.parts = slope_parts(M, (int)N);
+    l.parts = slope_parts(M);
     l.sums = c.take((size_t)l.parts * N * 4);
     l.total = c.used;
     return l;

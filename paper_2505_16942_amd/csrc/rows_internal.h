@@ -29,7 +29,7 @@ hipError_t launch_product(const ProductArgs& p, hipStream_t s);
 struct Pack16 { const void* src; int64_t ld_src; void* dst; int64_t ld_dst, rows, cols; };
 hipError_t launch_pack16(const Pack16& one, const Pack16& two, hipStream_t s);
 // dz = dy * act'(z) as `type` (dz may be null), and the column sums of the unrounded dz by parts (part may be null)
-int slope_parts(int64_t M, int N);
+int slope_parts(int64_t M);
 hipError_t launch_slope(corr_dtype t, int act, const void* dy, int64_t ld_dy, const void* z, void* dz, int64_t ld_dz, float* part,
                         int64_t M, int N, hipStream_t s);
 

@@ -319,9 +319,12 @@ def test_norm_forms(form, S, T):
                 continue
             q = None
         got = b.corr_residual_norm_backward(h, d_h_out=p, d_n_out=q, **kw)
-        for name, g, want in zip(got._fields, got, r.backward(p, q)):
+        for i, (name, g, want) in enumerate(zip(got._fields, got, r.backward(p, q))):
             if g is not None:
                 ref.check("%s %s" % (name, form), g, *want)
+                # sums over 5003 rows of terms that are some EPS off, in random directions: far below the bounds' sums of magnitudes
+                if i >= 3 and float(want[0].norm()):
+                    assert float((g.double().cpu() - want[0]).norm() / want[0].norm()) < 1e-5, name
 
 
 def test_norm_alone_and_wide_rows_without_their_gradient():
@@ -443,6 +446,35 @@ def test_norm_streams_and_graphs():
         torch.cuda.synchronize()
         want = b.corr_residual_norm(h, **kw) + tuple(b.corr_residual_norm_backward(h, d_h_out=dh, d_n_out=dn, **kw))
         assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
+def test_offsets_past_32_bits():
+    """More than 2^31 elements and 2^32 bytes: the first and the last rows, forward and gradients (whose other rows' d_out is zero)."""
+    b = _b()
+    M, K, N = (1 << 31) // 324 + 4001, 324, 16
+    x = torch.zeros(M, K, dtype=BF16, device="cuda")
+    some = torch.cat([torch.arange(40), torch.arange(M - 300, M)]).cuda()
+    new = _gen(2)
+    x[some] = new(340, K, dtype=BF16)
+    w = new(N, K, sigma=0.1, dtype=BF16)
+    y = b.corr_linear(x, w)
+    wy, _, ey, _ = ref.linear(x[some], w, None, "none", None)
+    ref.check("y", y[some], wy, ey)
+    assert (y[40:50] == 0).all()
+    dy = torch.zeros(M, N, dtype=BF16, device="cuda")
+    dy[some] = new(340, N, dtype=BF16)
+    d_x, d_w, d_b = b.corr_linear_backward(x, w, dy)
+    for g, (v, e), what in zip((d_x[some], d_w, d_b), ref.linear_backward(x[some], w, dy[some], None, "none"), ("d_x", "d_w", "d_b")):
+        ref.check(what, g, v, e)
+    assert (d_x[100] == 0).all()
+    del y, d_x, dy
+    n = b.corr_residual_norm(x, pre=b.CORR_NORM_RMS)[1]
+    r = ref.Norm(x[some], None, None, "none", None, 1.0, "none", None, None, "rms", None, None, 1e-5, BF16)
+    ref.check("n", n[some], *r.forward()[0])
+    g = b.corr_residual_norm_backward(x, pre=b.CORR_NORM_RMS, d_n_out=n)
+    ref.check("d_h", g.d_h[some], *r.backward(None, n[some])[0])
+    del x, n, g
+    torch.cuda.empty_cache()
 
 
 # ------------------------------------------------------------------------------------------------------------ together
