@@ -10,13 +10,18 @@ bool known(corr_activation a) { return a >= CORR_ACT_NONE && a <= CORR_ACT_SIGMO
 bool known(corr_norm n) { return n >= CORR_NORM_NONE && n <= CORR_NORM_LAYER; }
 bool on(const void* p, int border) { return ((uintptr_t)p & (uintptr_t)(border - 1)) == 0; }
 
-// The bytes [at, end) of a matrix, to compare with another's.
-struct Range { uintptr_t at, end; };
+// The bytes [at, end) of a matrix, in rows of `row` bytes `stride` apart, to compare with another's.
+struct Range { uintptr_t at, end, row, stride; };
 Range range(const void* p, int64_t rows, int64_t cols, int64_t stride, int es) {
-    if (!p || rows <= 0) return {0, 0};
-    return {(uintptr_t)p, (uintptr_t)p + (uintptr_t)((rows - 1) * stride + cols) * es};
+    if (!p || rows <= 0) return {0, 0, 0, 0};
+    return {(uintptr_t)p, (uintptr_t)p + (uintptr_t)((rows - 1) * stride + cols) * es, (uintptr_t)cols * es, (uintptr_t)stride * es};
 }
-bool overlap(Range a, Range b) { return a.at < b.end && b.at < a.end; }
+bool overlap(const Range& a, const Range& b) {
+    if (a.at >= b.end || b.at >= a.end) return false;
+    if (a.stride != b.stride || !a.stride) return true;
+    const uintptr_t off = b.at >= a.at ? (b.at - a.at) % a.stride : (a.stride - (a.at - b.at) % a.stride) % a.stride;
+    return off < a.row || off + b.row > a.stride;        // else columns beside each other in one buffer
+}
 template <int NO, int NI>
 bool any_overlap(const Range (&out)[NO], const Range (&in)[NI]) {
     for (int i = 0; i < NO; ++i) {

@@ -154,6 +154,22 @@ def test_linear_strides_and_guards(dtype, M, K, ldx, ldy, ldr):
         ref.check(what + " plain", g, v, e)
 
 
+def test_columns_of_one_buffer():
+    """x, the residual and the results side by side in the rows of one buffer; columns that do meet are refused."""
+    b, new = _b(), _gen(55)
+    buf = new(50, 160, dtype=F16)
+    w = new(32, 64, sigma=0.1, dtype=F16)
+    x, res, out = buf[:, :64], buf[:, 64:96], buf[:, 96:128]
+    keep = buf.clone()
+    b.corr_linear(x, w, act=b.CORR_ACT_RELU, residual=res, out=out)
+    wy, _, ey, _ = ref.linear(keep[:, :64], w, None, "relu", keep[:, 64:96])
+    ref.check("out", out, wy, ey)
+    assert torch.equal(buf[:, :96], keep[:, :96]) and torch.equal(buf[:, 128:], keep[:, 128:])
+    for bad in (buf[:, 63:95], buf[:, 32:64], buf[:, 80:112]):
+        with pytest.raises(b.CorrError):
+            b.corr_linear(x, w, residual=res, out=bad)
+
+
 def test_linear_shapes():
     """Leading dimensions, one row without any, no rows, evenly spaced views."""
     b, new = _b(), _gen(3)
