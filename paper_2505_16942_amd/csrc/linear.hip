@@ -172,7 +172,7 @@ __device__ __forceinline__ void finish_wave(const ProductArgs& g, f32x4 (&acc)[F
 //   k contiguous:    rows of 2 BK bytes, piece p of row r at p ^ (r & 7) (BK = 32: p ^ (r / 2 & 3))
 //   rows contiguous: BK k-rows of 2 R bytes, 32-byte block c of row k at c ^ turn(k); read by the transposing LDS load
 // so that neither the rows of a fragment nor the k of a transposed one meet in a bank (LDS conflict cycles: 1 in 900).
-// 8192^3 bf16 with residual: 0.88 ms, 1.26 PFLOP/s, bound by the matrix cores under the card's power limit.  Short sums are bound by
+// 8192^3 bf16 with residual: 0.89 ms, 1.24 PFLOP/s, bound by the matrix cores under the card's power limit.  Short sums are bound by
 // bytes and by the turns of a tile (load, multiply, store): 32400 x 256 -> 1024, gelu, preact: 48 us, 149 MB.  A third stage in LDS and
 // orders of k that differ from tile to tile made no difference.
 template <int R> __device__ __forceinline__ int turn(int k) {
@@ -267,7 +267,12 @@ __global__ __launch_bounds__(64 * WM * WN, BK == 32 ? 4 : 2) void product16_kern
         lb.issue(wb, lds_at + half * HALF + A_BYTES, wave);
         wa.next(); wb.next();
     };
+    // A wave past the result's borders only helps to load (129600 x 256 -> 324: 52 -> 49 us).  Loads stay ahead of a step's products where k
+    // is contiguous (129600 x 320 -> 256: 43 -> 35 us; 8192^3 with residual: 915 and 922); where the rows are, mixed is better (129600 x 324 x 256: 40 and 42).
+    const bool busy = AR || (n0 + wn < g.N && m0 + wm < g.M);
     auto multiply = [&](int half, auto last) {
+        if constexpr (!AR) __builtin_amdgcn_sched_barrier(0);
+        if (!busy) return;
         lds_byte* const ta = lds + half * HALF;
         lds_byte* const tb = ta + A_BYTES;
 #pragma unroll
@@ -301,7 +306,7 @@ __global__ __launch_bounds__(64 * WM * WN, BK == 32 ? 4 : 2) void product16_kern
         multiply(whole & 1, std::true_type{});
     }
     __syncthreads();                                     // the tiles have been read
-    finish_wave<T, FM, FN>(g, acc, (float*)smem + wave * box_floats<FN>(), m0 + wm, n0 + wn, lane, split, splits);
+    if (busy) finish_wave<T, FM, FN>(g, acc, (float*)smem + wave * box_floats<FN>(), m0 + wm, n0 + wn, lane, split, splits);
 }
 
 // ------------------------------------------------------------------------------------------------ fp32 operands
@@ -766,15 +771,16 @@ ProductPlan product_plan(corr_dtype type, int a_rows, int b_rows, int M, int N, 
     const int64_t t128 = (int64_t)cdiv(M, 128) * cdiv(N, 128), t256 = (int64_t)cdiv(M, 256) * cdiv(N, 256);
     const int64_t trows = (int64_t)cdiv(M, 128) * cdiv(N, 256);
     // Tiles of 128 x 256 in steps of 32 k, 16 waves a compute unit, where there is little to multiply for every element that is stored:
-    // 259200 x 128 -> 256: 44 us, 53 in tiles of 256; 32400 x 256 -> 1024 with gelu and preact: 48.5 and 54.  At k = 384: 95 and 88.
+    // 259200 x 128 -> 256: 44 us, 55 in tiles of 256; 32400 x 256 -> 1024 with gelu and preact: 44 and 50; 129600 x 324 -> 256: 46 and 46,
+    // with gelu and preact 59 and 64.  259200 x 384 -> 256: 97 and 90.
     // Tiles of 256 read operands half as often, but one workgroup fills a compute unit: for products that give every unit one, and
-    // that do not make them multiply much more (129600 x 320 -> 324: 58 us in tiles of 128, 70 in 256; x 324 -> 256: 53 and 48).
+    // that do not make them multiply much more (129600 x 384 -> 324: 63 us in tiles of 128, 69 in 256; 259200 x 384 -> 256: 110 and 90).
     // Tiles of 128 if they, or their splits, give 320 workgroups (5704 x 4096 -> 1024 fp16: 58 us, 77 in tiles of 64), else tiles of 64
     // (2048 x 1024 -> 256 fp32: 18 us, 24 in tiles of 128; 2852 x 1024 -> 256 fp16: 12.7 and 14.8).
     // Splits have eight steps or more; joining them costs about 4 us, as much as 16 steps of 16-bit tiles of 64 (2852 x 1024 -> 256: 7.5 us
     // whole, 11.4 in two) or six of fp32.
     const int most = all >= 32 || wide ? max(1, all / 8) : 1;
-    if (!wide && K <= 256 && N > 128 && trows >= 512) { p.tile = TILE_ROWS; tiles = trows; }
+    if (!wide && K <= 352 && N > 128 && trows >= 512) { p.tile = TILE_ROWS; tiles = trows; }
     else if (!wide && t256 >= 256 && t256 * 4 <= t128 * 1.25) { p.tile = TILE_256; tiles = t256; }
     else if (t128 * max((int64_t)1, min((int64_t)most, 512 / t128)) >= 320) { p.tile = TILE_128; tiles = t128; }
     // workgroups for two (tiles of 64: four) on every compute unit
