@@ -214,7 +214,8 @@ size_t corr_workspace_bytes(corr_mode mode, int B, int H, int W, int D, int L, i
  * once, to nearest even, when it is stored.  Calls only enqueue kernels on `stream`, allocate nothing and keep
  * nothing; the caller's `workspace` (16-byte aligned, contents ignored, scratch on return) must not be shared by
  * calls that overlap, graph replays among them.  Every result has the same bits on every call.  Outputs may not
- * overlap inputs unless stated.  Zero rows are accepted (sums over rows are then zero); other sizes are positive.
+ * overlap inputs or each other unless stated; columns beside each other in one buffer, rows equally far apart, do
+ * not.  Zero rows are accepted (sums over rows are then zero); other sizes are positive.
  */
 typedef enum { CORR_TYPE_F32 = 0, CORR_TYPE_BF16 = 1, CORR_TYPE_F16 = 2 } corr_dtype;
 typedef enum {
