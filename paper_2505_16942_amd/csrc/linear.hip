@@ -771,8 +771,9 @@ ProductPlan product_plan(corr_dtype type, int a_rows, int b_rows, int M, int N, 
     const int64_t t128 = (int64_t)cdiv(M, 128) * cdiv(N, 128), t256 = (int64_t)cdiv(M, 256) * cdiv(N, 256);
     const int64_t trows = (int64_t)cdiv(M, 128) * cdiv(N, 256);
     // Tiles of 128 x 256 in steps of 32 k, 16 waves a compute unit, where there is little to multiply for every element that is stored:
-    // 259200 x 128 -> 256: 44 us, 55 in tiles of 256; 32400 x 256 -> 1024 with gelu and preact: 44 and 50; 129600 x 324 -> 256: 46 and 46,
-    // with gelu and preact 59 and 64.  259200 x 384 -> 256: 97 and 90.
+    // 259200 x 128 -> 256: 44 us, 55 in tiles of 256; 32400 x 256 -> 1024 with gelu and preact: 44 and 50; 129600 x 324 -> 256: 45 and 46,
+    // with gelu and preact 57 and 62.  Past the memory-side cache (256 MB; a preact is not counted) steps of whole pieces of 64 bytes only, and
+    // a shorter k: 518400 x 324 -> 256: 240 us, 200 to 218 in tiles of 256; x 240: 183 and 160; x 352: 202 and 189; x 256: 135 and 141.
     // Tiles of 256 read operands half as often, but one workgroup fills a compute unit: for products that give every unit one, and
     // that do not make them multiply much more (129600 x 384 -> 324: 63 us in tiles of 128, 69 in 256; 259200 x 384 -> 256: 110 and 90).
     // Tiles of 128 if they, or their splits, give 320 workgroups (5704 x 4096 -> 1024 fp16: 58 us, 77 in tiles of 64), else tiles of 64
@@ -780,8 +781,9 @@ ProductPlan product_plan(corr_dtype type, int a_rows, int b_rows, int M, int N, 
     // Splits have eight steps or more; joining them costs about 4 us, as much as 16 steps of 16-bit tiles of 64 (2852 x 1024 -> 256: 7.5 us
     // whole, 11.4 in two) or six of fp32.
     const int most = all >= 32 || wide ? max(1, all / 8) : 1;
-    if (!wide && K <= 352 && N > 128 && trows >= 512) { p.tile = TILE_ROWS; tiles = trows; }
-    else if (!wide && t256 >= 256 && t256 * 4 <= t128 * 1.25) { p.tile = TILE_256; tiles = t256; }
+    const bool large = !wide && t256 >= 256 && t256 * 4 <= t128 * 1.25, cached = (int64_t)M * (K + N) * 2 <= 192 << 20;
+    if (!wide && K <= (cached ? 352 : 256) && N > 128 && trows >= 512 && (cached || K % 32 == 0 || !large)) { p.tile = TILE_ROWS; tiles = trows; }
+    else if (large) { p.tile = TILE_256; tiles = t256; }
     else if (t128 * max((int64_t)1, min((int64_t)most, 512 / t128)) >= 320) { p.tile = TILE_128; tiles = t128; }
     // workgroups for two (tiles of 64: four) on every compute unit
     const int64_t want = p.tile == TILE_256 ? 256 : p.tile == TILE_64 ? 1024 : 512;
