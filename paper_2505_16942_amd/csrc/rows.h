@@ -17,6 +17,11 @@ static inline int corr_elem_bytes(corr_dtype t) { return t == CORR_TYPE_F32 ? 4 
 // v_rcp_f32 (1 ulp).  Where e^-z overflows, 1 / (1 + e^-z) is 0, as it should be.  A comparison keeps a NaN where fmaxf would drop it.
 __device__ __forceinline__ float row_exp(float x) { return __builtin_amdgcn_exp2f(1.4426950408889634f * x); }
 __device__ __forceinline__ float row_sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + row_exp(-z)); }
+// e^-z / (1 + e^-z)^2 is even: from |z| no digits cancel (1 - sigmoid(z) has none left at z = 17, where the slope is 4e-8).
+__device__ __forceinline__ float row_sigmoid_slope(float z) {
+    const float e = row_exp(-fabsf(z)), r = __builtin_amdgcn_rcpf(1.f + e);
+    return e * r * r;
+}
 // u of 0.5 z (1 + tanh u) = z sigmoid(2 u), times two
 __device__ __forceinline__ float row_gelu_2u(float z) { return 1.5957691216057308f * fmaf(0.044715f * z * z, z, z); }
 // The normal distribution's integral, and `tail` = e^(-z^2/2): erfc(x) = (a1 t + .. + a5 t^5) e^(-x^2), t = 1 / (1 + p x), x >= 0
@@ -54,7 +59,7 @@ __device__ __forceinline__ float row_act_slope(int act, float z) {
             return fmaf(z * s * (1.f - s), 1.5957691216057308f * fmaf(0.134145f * z, z, 1.f), s);
         }
         case CORR_ACT_SILU: { const float s = row_sigmoid(z); return s * fmaf(z, 1.f - s, 1.f); }
-        case CORR_ACT_SIGMOID: { const float s = row_sigmoid(z); return s * (1.f - s); }
+        case CORR_ACT_SIGMOID: return row_sigmoid_slope(z);
     }
     return 1.f;
 }
