@@ -5,8 +5,13 @@ EPS = 2^-24, one rounding; v_exp_f32 and v_rcp_f32 are off by one unit in the la
     e^-|z|            its argument is a product with a rounded constant: 2 |z| EPS, and 2 EPS
     sigmoid, silu     (2 |z| + 8) EPS: the exponential, 1 + e, the reciprocal, the product
     sigmoid's slope   (2 |z| + 16) EPS: e / (1 + e)^2, even in z
+    gelu              the normal integral's tail: z^2 and two products with a rounded constant in the exponent, 1.5 z^2 EPS; a polynomial
+                      of eight steps, a reciprocal and its denominator, three products: 32 EPS.  Of 1 - tail no more.
+    gelu's slope      the same of the tail q and of |z| density, which have opposite signs below zero: relative to their sum
 The product that carries the value adds 28 EPS (rows_reference.py's bound for a sum of one term).
 """
+import math
+
 import pytest
 
 import rows_reference as ref
@@ -63,3 +68,17 @@ def test_silu(dtype):
     z = _values(dtype, 80.0)
     d = z.double().cpu()
     _check("silu", _forward("silu", z), d * torch.sigmoid(d), 2 * d.abs() + 8, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gelu_and_its_slope_keep_their_tails(dtype):
+    z = _values(dtype, 12.0)
+    d = z.double().cpu()
+    tail = 0.5 * torch.erfc(d.abs() / math.sqrt(2.0))
+    density = torch.exp(-0.5 * d * d) / math.sqrt(2 * math.pi)
+    phi = torch.where(d < 0, tail, 1 - tail)
+    per = 1.5 * d * d + 32
+    _check("gelu", _forward("gelu", z), d * phi, per, dtype)
+    want = phi + d * density
+    apart = (phi + d.abs() * density) / want.abs().clamp_min(1e-30)
+    _check("slope", _slope("gelu", z), want, (per + 28) * apart, dtype)
