@@ -61,8 +61,9 @@ __device__ __forceinline__ float row_act_slope(int act, float z) {
             return fmaf(z * tail, 0.39894228040143268f, p);
         }
         case CORR_ACT_GELU_TANH: {
-            const float s = row_sigmoid(row_gelu_2u(z));
-            return fmaf(z * s * (1.f - s), 1.5957691216057308f * fmaf(0.134145f * z, z, 1.f), s);
+            // where z^2 overflows s (1 - s) is zero, and has to stay it: a finite factor (a NaN is in s too)
+            const float s = row_sigmoid(row_gelu_2u(z)), d2u = fminf(1.5957691216057308f * fmaf(0.134145f * z, z, 1.f), 3e38f);
+            return fmaf(z * (s * (1.f - s)), d2u, s);
         }
         case CORR_ACT_SILU: { const float s = row_sigmoid(z); return s * fmaf(z, 1.f - s, 1.f); }
         case CORR_ACT_SIGMOID: return row_sigmoid_slope(z);

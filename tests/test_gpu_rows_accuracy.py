@@ -82,3 +82,17 @@ def test_gelu_and_its_slope_keep_their_tails(dtype):
     want = phi + d * density
     apart = (phi + d.abs() * density) / want.abs().clamp_min(1e-30)
     _check("slope", _slope("gelu", z), want, (per + 28) * apart, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("name", ref.ACTS[2:])
+def test_huge_sums(name, dtype):
+    """Far from zero an activation is its argument or zero (the sigmoid one or zero), its slope one or zero (the sigmoid's zero),
+    also where squares and cubes on the way overflow."""
+    big = [6e4] if dtype == F16 else [1e5, 1e15, 1e19, 1e20, 1e25, 3e38]
+    z = torch.tensor(big + [-v for v in big]).to(dtype).reshape(-1, 1).cuda()
+    up = (z > 0).double().cpu()
+    want, slope = (up, 0 * up) if name == "sigmoid" else (z.double().cpu() * up, up)
+    zero = torch.zeros_like(up)
+    _check(name, _forward(name, z), want, zero, dtype)
+    _check("slope of " + name, _slope(name, z), slope, zero, dtype)
