@@ -25,7 +25,7 @@ depend on that.
 Usage (GPU machine, repository root):  python -m paper_2505_16942_amd.sweep [--quick]
 Prints a markdown table.  With --backward it prints a second kind of table instead: one call of the lookup's
 gradient (corr_sample_backward) over the same widths and feature dimensionalities, in both of its forms, beside one
-lookup.
+lookup; with --block the calls of an update block that follows a lookup, and their gradients.
 """
 from __future__ import annotations
 
@@ -153,33 +153,39 @@ def _timed_ms(fn, n: int = 5) -> float:
     return e0.elapsed_time(e1) / n
 
 
-def _rows_point(H: int, W: int, dtype, C: int = 256, taps: int = 324):
-    """ms of an update block's calls on an H x W map, in their order, and of their gradients."""
+def _rows_calls(H: int, W: int, dtype, device, C: int = 256, taps: int = 324):
+    """An update block's calls on an H x W map, in their order, and their gradients', as (function, arguments, named arguments).
+    Every matrix is one of its own, as in a network: a matrix in two places would be read from memory once."""
     import torch
     from . import binding as cb
-    dev = torch.device("cuda:0")
-    g = torch.Generator(device=dev)
+    g = torch.Generator(device=device)
     g.manual_seed(H)
 
     def new(*shape, sigma=1.0, kind=dtype):
-        return (torch.randn(shape, device=dev, generator=g) * sigma).to(kind)
-    f32 = torch.float32
-    x, h, y = new(H * W, taps), new(H * W, C), new(H * W, C)
+        return (torch.randn(shape, device=device, generator=g) * sigma).to(kind)
+    f32, P = torch.float32, H * W
+    x, h, n, u, y = new(P, taps), new(P, C), new(P, C), new(P, 4 * C), new(P, C)
     w0, w1, w2 = new(C, taps, sigma=taps ** -0.5), new(4 * C, C, sigma=C ** -0.5), new(C, 4 * C, sigma=(4 * C) ** -0.5)
     b0, b1, b2, s, n1, n2, c2 = (new(k, sigma=0.1, kind=f32) for k in (C, 4 * C, C, C, C, C, C))
-    z0, z1, u = torch.empty_like(h), new(H * W, 4 * C), new(H * W, 4 * C)
+    z0, z1 = torch.empty_like(h), new(P, 4 * C)
+    dt, dn2, dy, du, dn, dh, d0 = new(P, C), new(P, C), new(P, C), new(P, 4 * C), new(P, C), new(P, C), new(P, C)
     end = dict(y=y, scale=s, pre=cb.CORR_NORM_LAYER, pre_weight=n2, pre_bias=c2)
-    calls = [lambda: cb.corr_linear(x, w0, bias=b0, act=cb.CORR_ACT_RELU, preact=z0),
-             lambda: cb.corr_residual_norm(h, pre_weight=n1),
-             lambda: cb.corr_linear(y, w1, bias=b1, act=cb.CORR_ACT_GELU, preact=z1),
-             lambda: cb.corr_linear(u, w2, bias=b2),
-             lambda: cb.corr_residual_norm(h, **end),
-             lambda: cb.corr_residual_norm_backward(h, d_h_out=y, d_n_out=y, **end),
-             lambda: cb.corr_linear_backward(u, w2, y),
-             lambda: cb.corr_linear_backward(y, w1, u, preact=z1, act=cb.CORR_ACT_GELU),
-             lambda: cb.corr_residual_norm_backward(h, pre_weight=n1, d_h_out=y, d_n_out=y),
-             lambda: cb.corr_linear_backward(x, w0, y, preact=z0, act=cb.CORR_ACT_RELU)]
-    return [_timed_ms(c) for c in calls]
+    return [(cb.corr_linear, (x, w0), dict(bias=b0, act=cb.CORR_ACT_RELU, preact=z0)),
+            (cb.corr_residual_norm, (h,), dict(pre_weight=n1)),
+            (cb.corr_linear, (n, w1), dict(bias=b1, act=cb.CORR_ACT_GELU, preact=z1)),
+            (cb.corr_linear, (u, w2), dict(bias=b2)),
+            (cb.corr_residual_norm, (h,), end),
+            (cb.corr_residual_norm_backward, (h,), dict(d_h_out=dt, d_n_out=dn2, **end)),
+            (cb.corr_linear_backward, (u, w2, dy), {}),
+            (cb.corr_linear_backward, (n, w1, du), dict(preact=z1, act=cb.CORR_ACT_GELU)),
+            (cb.corr_residual_norm_backward, (h,), dict(pre_weight=n1, d_h_out=dh, d_n_out=dn)),
+            (cb.corr_linear_backward, (x, w0, d0), dict(preact=z0, act=cb.CORR_ACT_RELU))]
+
+
+def _rows_point(H: int, W: int, dtype):
+    """ms of each of _rows_calls"""
+    import torch
+    return [_timed_ms(lambda: f(*a, **k)) for f, a, k in _rows_calls(H, W, dtype, torch.device("cuda:0"))]
 
 
 def main(argv=None) -> int:
