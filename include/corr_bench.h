@@ -111,6 +111,15 @@ corr_status corr_debug_cell_coords(const corr_pyramid* pyr, int cell_id, int* b,
  *   rep = CORR_REP_F32 : the fp32 copy;  CORR_REP_SPLIT : hi + lo;  CORR_REP_BF16 : the hi parts.
  */
 corr_status corr_debug_read_level(const corr_pyramid* pyr, unsigned rep, int level, float* dst, void* stream);
+/*
+ * Test hook (host only, no GPU work): the tile of the result that a workgroup of corr_linear (product 0: y) or corr_linear_backward
+ * (1: d_x, 2: d_w) makes at these sizes, and into how many parts its sum is split.  Few rows, whose weights go straight into the matrix
+ * instructions' fragments, have tile_rows = 0 (tile_cols = 16).  CORR_ERR_INVALID_ARG for sizes that the calls refuse.
+ */
+#define CORR_PRODUCT_Y 0
+#define CORR_PRODUCT_DX 1
+#define CORR_PRODUCT_DW 2
+corr_status corr_debug_linear_tile(corr_dtype type, int product, int64_t M, int64_t N, int64_t K, int* tile_rows, int* tile_cols, int* splits);
 
 #ifdef __cplusplus
 }

@@ -42,6 +42,7 @@ EXPORTS = [
 BENCH_EXPORTS = [
     "corr_last_block_stats", "corr_profile_enable", "corr_profile_read", "corr_bin_geometry", "corr_copy_f32",
     "corr_debug_read_plan", "corr_debug_cell_coords", "corr_debug_read_level", "corr_debug_item_map",
+    "corr_debug_linear_tile",
     "corr_debug_set_level_split",
     "corr_debug_set_backward_form",
 ]
@@ -145,6 +146,8 @@ def load_library():
     lib.corr_debug_cell_coords.restype = ci
     lib.corr_debug_item_map.argtypes = [ci, ctypes.POINTER(ctypes.c_int32), ctypes.c_size_t, ctypes.POINTER(ci)]
     lib.corr_debug_item_map.restype = ci
+    lib.corr_debug_linear_tile.argtypes = [ci, ci, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64] + [ctypes.POINTER(ci)] * 3
+    lib.corr_debug_linear_tile.restype = ci
     lib.corr_debug_set_level_split.argtypes = [ci]
     lib.corr_debug_set_level_split.restype = ci
     lib.corr_debug_set_backward_form.argtypes = [ci]
@@ -722,6 +725,15 @@ def corr_debug_item_map(max_items: int):
     if st != CORR_OK:
         raise CorrError(st, "corr_debug_item_map")
     return grid.value, m
+
+
+def corr_debug_linear_tile(dtype: torch.dtype, product: int, M: int, N: int, K: int):
+    """(rows, columns, splits) of the tiles in which corr_linear (product 0: y) or corr_linear_backward (1: d_x, 2: d_w) makes its result."""
+    vals = [ctypes.c_int() for _ in range(3)]
+    st = load_library().corr_debug_linear_tile(_TYPES[dtype], product, M, N, K, *[ctypes.byref(v) for v in vals])
+    if st != CORR_OK:
+        raise CorrError(st, "corr_debug_linear_tile")
+    return tuple(v.value for v in vals)
 
 
 def corr_debug_cell_coords(pyramid: Pyramid, cell_id: int):

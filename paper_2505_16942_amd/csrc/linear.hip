@@ -795,6 +795,11 @@ ProductPlan product_plan(corr_dtype type, int a_rows, int b_rows, int M, int N, 
     return p;
 }
 
+void product_tile(const ProductPlan& p, int& rows, int& cols) {
+    rows = p.tile == TILE_256 ? 256 : p.tile == TILE_64 ? 64 : p.tile == TILE_FEW ? 0 : 128;
+    cols = p.tile == TILE_256 || p.tile == TILE_ROWS ? 256 : p.tile == TILE_128 ? 128 : p.tile == TILE_64 ? 64 : 16;
+}
+
 hipError_t launch_product(const ProductArgs& args, hipStream_t s) {
     ProductArgs g = args;
     const ProductPlan p = product_plan(g.type, g.a_rows, g.b_rows, g.M, g.N, g.K);

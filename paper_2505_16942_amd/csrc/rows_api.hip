@@ -1,5 +1,6 @@
 // Host side of the row operators declared in include/corr.h: argument checks, the workspace's layout and the order of kernels.
 #include "rows_internal.h"
+#include "corr_bench.h"
 
 namespace {
 
@@ -231,6 +232,20 @@ corr_status corr_linear_backward(corr_dtype type, corr_activation act, const voi
         e = launch_product(p, s);
     }
     return e == hipSuccess ? CORR_OK : CORR_ERR_HIP;
+}
+
+corr_status corr_debug_linear_tile(corr_dtype type, int product, int64_t M, int64_t N, int64_t K, int* tile_rows, int* tile_cols, int* splits) {
+    if (!tile_rows || !tile_cols || !splits || M <= 0 || check_linear(type, CORR_ACT_NONE, M, N, K) != CORR_OK) return CORR_ERR_INVALID_ARG;
+    ProductPlan p;
+    switch (product) {
+        case CORR_PRODUCT_Y: p = product_plan(type, 0, 0, (int)M, (int)N, (int)K); break;
+        case CORR_PRODUCT_DX: p = product_plan(type, 0, 1, (int)M, (int)K, (int)N); break;
+        case CORR_PRODUCT_DW: p = product_plan(type, 1, 1, (int)N, (int)K, (int)M); break;
+        default: return CORR_ERR_INVALID_ARG;
+    }
+    product_tile(p, *tile_rows, *tile_cols);
+    *splits = p.splits;
+    return CORR_OK;
 }
 
 corr_status corr_residual_norm(const corr_residual_norm_args* a, void* h_out, void* n_out, void* stream) {
