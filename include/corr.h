@@ -251,8 +251,9 @@ corr_status corr_linear(corr_dtype type, corr_activation act, const void* x, int
  *   preact : [M, N] dense, as corr_linear left it; not read (may be NULL) for CORR_ACT_NONE.  relu's slope at 0 is 0.
  *   d_y    : [M, N] rows, d_y_stride.
  *   d_x    : [M, K] dense or NULL;  d_w : [N, K] dense or NULL;  d_bias : fp32 [N] or NULL.
- * For 16-bit types and an activation, dz is rounded to the type once before the two products (the matrix cores'
- * operand); d_bias adds the unrounded values.
+ * dz as the products' operand: fp32 whole; bf16 rounded once, beside the results' own rounding (together sqrt 2 times its
+ * error); fp16 in two parts of 22 bits together, so that d_x and d_w are rounded once and small gradients keep their digits (with relu or
+ * none dz is d_y or zero, one part, exact).  d_bias adds the unrounded values.
  */
 size_t corr_linear_backward_workspace_bytes(corr_dtype type, corr_activation act, int64_t M, int64_t N, int64_t K,
                                             int64_t x_stride, int64_t d_y_stride);

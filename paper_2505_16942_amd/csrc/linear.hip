@@ -238,7 +238,10 @@ __device__ __forceinline__ V keep_first(V v, int left) {
     return __builtin_bit_cast(V, u);
 }
 
-template <class T, bool AR, bool BR, int BM, int BN, int WM, int WN, int BK>
+// TWO: the first operand is in two parts (rows_internal.h), multiplied one after the other, the low one first: twice the matrix work and twice the
+// loads (fp16 gradients with silu beside relu: 14570 x 243 -> 126: 51 and 41 us; 32400 x 256 -> 1024: 153 and 104; 4096^3: 503 and 265).  A sum of the low part's products that is not finite says that an element of the second operand is not (fp16's values cannot
+// overflow it): then the high part alone gives what the whole would.
+template <class T, bool AR, bool BR, int BM, int BN, int WM, int WN, int BK, bool TWO>
 __global__ __launch_bounds__(64 * WM * WN, BK == 32 ? 4 : 2) void product16_kernel(ProductArgs g, int tm, int tn, int splits, int steps_per) {
     constexpr int WAVES = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
     constexpr int A_BYTES = BM * BK * 2, HALF = (BM + BN) * BK * 2;
@@ -251,7 +254,7 @@ __global__ __launch_bounds__(64 * WM * WN, BK == 32 ? 4 : 2) void product16_kern
     const int m0 = mt * BM, n0 = nt * BN;
     const int k0 = split * steps_per * 64, k_left = min(g.K - k0, steps_per * 64);
     const int whole = k_left / BK, tail = k_left % BK, steps = whole + (tail != 0);
-    Window wa = window<AR, 2, BK>(g.a, g.lda, g.M, g.K, m0, k0), wb = window<BR, 2, BK>(g.b, g.ldb, g.N, g.K, n0, k0);
+    Window wa = window<AR, 2, BK>(TWO ? g.a_lo : g.a, g.lda, g.M, g.K, m0, k0), wb = window<BR, 2, BK>(g.b, g.ldb, g.N, g.K, n0, k0);
     Loader16<AR, BM, WAVES, BK> la;
     Loader16<BR, BN, WAVES, BK> lb;
     la.plan(wave, lane, g.lda);
@@ -295,15 +298,39 @@ __global__ __launch_bounds__(64 * WM * WN, BK == 32 ? 4 : 2) void product16_kern
                 for (int j = 0; j < FM; ++j) acc[i][j] = mma(fb[i], fa[j], acc[i][j]);
         }
     };
-    ask(0);
-    for (int t = 0; t < whole; ++t) {
-        arrive_all();
-        if (t + 1 < steps) ask((t + 1) & 1);
-        multiply(t & 1, std::false_type{});
+    auto pass = [&] {
+        ask(0);
+        for (int t = 0; t < whole; ++t) {
+            arrive_all();
+            if (t + 1 < steps) ask((t + 1) & 1);
+            multiply(t & 1, std::false_type{});
+        }
+        if (tail) {
+            arrive_all();
+            multiply(whole & 1, std::true_type{});
+        }
+    };
+    auto scale = [&](float by) {
+#pragma unroll
+        for (int i = 0; i < FN; ++i)
+#pragma unroll
+            for (int j = 0; j < FM; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = fabsf(acc[i][j][e]) < INFINITY ? acc[i][j][e] * by : 0.f;
+    };
+    if constexpr (TWO) {
+        pass();
+        scale(1.f / LOW_PART);
+        wa = window<AR, 2, BK>(g.a, g.lda, g.M, g.K, m0, k0);
+        wb = window<BR, 2, BK>(g.b, g.ldb, g.N, g.K, n0, k0);
+        arrive_all();                                    // the tiles have been read
     }
-    if (tail) {
-        arrive_all();
-        multiply(whole & 1, std::true_type{});
+    pass();
+    if constexpr (TWO) {
+#pragma unroll
+        for (int i = 0; i < FN; ++i)
+#pragma unroll
+            for (int j = 0; j < FM; ++j) acc[i][j] *= 1.f / HIGH_PART;
     }
     __syncthreads();                                     // the tiles have been read
     if (busy) finish_wave<T, FM, FN>(g, acc, (float*)smem + wave * box_floats<FN>(), m0 + wm, n0 + wn, lane, split, splits);
@@ -659,12 +686,15 @@ __global__ __launch_bounds__(256) void pack16_kernel(Pack16 one, Pack16 two) {
 
 // dz = dy act'(z) and its column sums in one pass.  A thread has V columns and every RT-th row of its workgroup's share, two at a time; the sums
 // over rows meet in LDS.  Bound by bytes: 32400 x 1024 fp32: 74 us, 5.4 TB/s; 129600 x 256 bf16: 42 us, 4.7 TB/s.  dz is rounded to the
-// operands' type because the matrix cores take it so; the sums add what was not rounded.
+// operands' type because the matrix cores take it so; the sums add what was not rounded.  bf16: once; the rounding is as large as that of the
+// results, whose error grows to sqrt 2 times theirs alone.  fp16 holds dz in two parts where an activation shapes it (`dz_lo`):
+// with one, a small d_y times a small slope would lose its digits below 6e-5 and vanish below 3e-8, and one above 1 / slope times fp16's
+// largest overflow (over half of the results were not the nearest fp16 values, and errors of 70 steps; now 1 in 1000).
 constexpr int SLOPE_THREADS = 256;
 template <class T, int V>
 __global__ __launch_bounds__(SLOPE_THREADS) void slope_kernel(int act, const T* __restrict__ dy, int64_t ld_dy, const T* __restrict__ z,
-                                                             T* __restrict__ dz, int64_t ld_dz, float* __restrict__ part, int64_t M, int N,
-                                                             int ct, int64_t rows_per) {
+                                                             T* __restrict__ dz, T* __restrict__ dz_lo, int64_t ld_dz, float* __restrict__ part,
+                                                             int64_t M, int N, int ct, int64_t rows_per) {
     __shared__ float sums[SLOPE_THREADS][V];
     const int tid = threadIdx.x, c = tid % ct, rt = SLOPE_THREADS / ct, r0 = tid / ct;
     const int n = (blockIdx.x * ct + c) * V, left = N - n;
@@ -688,9 +718,19 @@ __global__ __launch_bounds__(SLOPE_THREADS) void slope_kernel(int act, const T* 
 #pragma unroll
                     for (int e = 0; e < V; ++e) v[u][e] *= s[u][e];
                 }
-                if (dz) store_some<T, V>(dz + (m + u * rt) * ld_dz + n, v[u], left);
 #pragma unroll
                 for (int e = 0; e < V; ++e) sum[e] += v[u][e];
+                if (dz_lo) {
+                    float lo[V];
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float x = HIGH_PART * v[u][e], d = x - (float)(T)x;
+                        lo[e] = d == d ? LOW_PART * d : 0.f;         // an infinity or NaN is in the high part
+                        v[u][e] = x;
+                    }
+                    store_some<T, V>(dz_lo + (m + u * rt) * ld_dz + n, lo, left);
+                }
+                if (dz) store_some<T, V>(dz + (m + u * rt) * ld_dz + n, v[u], left);
             }
         }
     }
@@ -709,7 +749,13 @@ __global__ __launch_bounds__(SLOPE_THREADS) void slope_kernel(int act, const T* 
 template <class T, bool AR, bool BR, int BM, int BN, int WM, int WN, int BK>
 void run16(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
     const int tm = cdiv(g.M, BM), tn = cdiv(g.N, BN);
-    hipLaunchKernelGGL((product16_kernel<T, AR, BR, BM, BN, WM, WN, BK>), dim3(tm * tn * p.splits), dim3(64 * WM * WN), 0, s, g, tm, tn, p.splits, p.steps);
+    if constexpr (std::is_same<T, _Float16>::value && BR) {
+        if (g.a_lo) {
+            hipLaunchKernelGGL((product16_kernel<T, AR, BR, BM, BN, WM, WN, BK, true>), dim3(tm * tn * p.splits), dim3(64 * WM * WN), 0, s, g, tm, tn, p.splits, p.steps);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((product16_kernel<T, AR, BR, BM, BN, WM, WN, BK, false>), dim3(tm * tn * p.splits), dim3(64 * WM * WN), 0, s, g, tm, tn, p.splits, p.steps);
 }
 template <class T, bool AR, bool BR>
 void run16(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
@@ -825,20 +871,20 @@ int slope_parts(int64_t M) { return (int)min((int64_t)1024, max((int64_t)1, (M +
 
 namespace {
 template <class T, int V>
-void slope(int act, const void* dy, int64_t ld_dy, const void* z, void* dz, int64_t ld_dz, float* part, int64_t M, int N, hipStream_t s) {
+void slope(int act, const void* dy, int64_t ld_dy, const void* z, void* dz, void* dz_lo, int64_t ld_dz, float* part, int64_t M, int N, hipStream_t s) {
     int ct = 1;
     while (ct < SLOPE_THREADS && ct * V < N) ct *= 2;
     const int parts = slope_parts(M);
     const int64_t per = (M + parts - 1) / parts;
     hipLaunchKernelGGL((slope_kernel<T, V>), dim3(cdiv(N, ct * V), parts), dim3(SLOPE_THREADS), 0, s, act, (const T*)dy, ld_dy, (const T*)z,
-                       (T*)dz, ld_dz, part, M, N, ct, per);
+                       (T*)dz, (T*)dz_lo, ld_dz, part, M, N, ct, per);
 }
 }  // namespace
 
-hipError_t launch_slope(corr_dtype t, int act, const void* dy, int64_t ld_dy, const void* z, void* dz, int64_t ld_dz, float* part,
-                        int64_t M, int N, hipStream_t s) {
-    if (t == CORR_TYPE_F32) slope<float, 4>(act, dy, ld_dy, z, dz, ld_dz, part, M, N, s);
-    else if (t == CORR_TYPE_BF16) slope<__bf16, 8>(act, dy, ld_dy, z, dz, ld_dz, part, M, N, s);
-    else slope<_Float16, 8>(act, dy, ld_dy, z, dz, ld_dz, part, M, N, s);
+hipError_t launch_slope(corr_dtype t, int act, const void* dy, int64_t ld_dy, const void* z, void* dz, void* dz_lo, int64_t ld_dz,
+                        float* part, int64_t M, int N, hipStream_t s) {
+    if (t == CORR_TYPE_F32) slope<float, 4>(act, dy, ld_dy, z, dz, dz_lo, ld_dz, part, M, N, s);
+    else if (t == CORR_TYPE_BF16) slope<__bf16, 8>(act, dy, ld_dy, z, dz, dz_lo, ld_dz, part, M, N, s);
+    else slope<_Float16, 8>(act, dy, ld_dy, z, dz, dz_lo, ld_dz, part, M, N, s);
     return hipGetLastError();
 }

@@ -60,16 +60,18 @@ LinearLayout linear_layout(corr_dtype t, int64_t M, int64_t N, int64_t K, int64_
     return l;
 }
 
-struct BackwardLayout { size_t x, w, dz, part, sums, total; bool pack_x, pack_w, own_dz; int parts; };
+struct BackwardLayout { size_t x, w, dz, dz_lo, part, sums, total; bool pack_x, pack_w, own_dz, two; int parts; };
 BackwardLayout backward_layout(corr_dtype t, corr_activation act, int64_t M, int64_t N, int64_t K, int64_t x_stride, int64_t dy_stride) {
     BackwardLayout l = {};
     Carver c;
     l.pack_x = packed(t, K, x_stride);
     l.pack_w = packed(t, K, K);
     l.own_dz = act != CORR_ACT_NONE || packed(t, N, dy_stride);
+    l.two = t == CORR_TYPE_F16 && act != CORR_ACT_NONE && act != CORR_ACT_RELU;     // d_y itself, or zero, needs no second part
     l.x = c.take(l.pack_x ? (size_t)M * up8(K) * 2 : 0);
     l.w = c.take(l.pack_w ? (size_t)N * up8(K) * 2 : 0);
     l.dz = c.take(l.own_dz ? (size_t)M * up8(N) * corr_elem_bytes(t) : 0);
+    l.dz_lo = c.take(l.two ? (size_t)M * up8(N) * 2 : 0);
     const size_t px = product_part_bytes(product_plan(t, 0, 1, (int)M, (int)K, (int)N), (int)M, (int)K);
     const size_t pw = product_part_bytes(product_plan(t, 1, 1, (int)N, (int)K, (int)M), (int)N, (int)K);
     l.part = c.take(px > pw ? px : pw);
@@ -205,7 +207,8 @@ corr_status corr_linear_backward(corr_dtype type, corr_activation act, const voi
     float* const sums = d_bias ? reinterpret_cast<float*>(ws + l.sums) : nullptr;
     if (l.own_dz && (d_x || d_w)) { dz = ws + l.dz; ld_dz = up8(N); }
     if (dz != d_y || sums) {
-        e = launch_slope(type, act, d_y, d_y_stride, preact, dz == d_y ? nullptr : ws + l.dz, up8(N), sums, M, (int)N, s);
+        e = launch_slope(type, act, d_y, d_y_stride, preact, dz == d_y ? nullptr : ws + l.dz, dz == d_y || !l.two ? nullptr : ws + l.dz_lo, up8(N),
+                         sums, M, (int)N, s);
         if (sums && e == hipSuccess) {
             const ColumnSums o = {{d_bias, nullptr, nullptr, nullptr, nullptr}};
             e = launch_column_sums(sums, l.parts, 1, (int)N, o, s);
@@ -216,6 +219,7 @@ corr_status corr_linear_backward(corr_dtype type, corr_activation act, const voi
     ProductArgs p = {};
     p.type = type; p.act = CORR_ACT_NONE;
     p.a = dz; p.lda = ld_dz;
+    if (l.two) p.a_lo = ws + l.dz_lo;
     p.part = reinterpret_cast<float*>(ws + l.part);
     if (d_x && e == hipSuccess) {
         p.b = w; p.ldb = K; p.b_rows = 1;

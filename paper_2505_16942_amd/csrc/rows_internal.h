@@ -2,11 +2,16 @@
 #pragma once
 #include "rows.h"
 
+// A first operand in two fp16 parts (`a_lo` is there): HIGH_PART x = a + a_lo / LOW_PART, so that fp16 holds x, an fp32 value, to 22 bits: no |x| up
+// to 1.13 times fp16's largest overflows, and what is below its normal values keeps its digits in the low part.
+constexpr float HIGH_PART = 0.5f, LOW_PART = 2048.f;
+
 // C[m][n] = sum over k < K of A(m, k) B(n, k).  An operand is stored with its k contiguous ([m][k], `lda` elements from row to
 // row) or with its rows contiguous ([k][m]); which of the two is part of the kernel chosen.
 struct ProductArgs {
     corr_dtype type;
     const void* a; const void* b;
+    const void* a_lo;          // laid out as a; null but for fp16 whose second operand has its rows contiguous
     int64_t lda, ldb;
     int a_rows, b_rows;        // 1: rows contiguous ([k][m] / [k][n])
     int M, N, K;
@@ -29,10 +34,10 @@ hipError_t launch_product(const ProductArgs& p, hipStream_t s);
 // dst[r][0 .. ld_dst) = src[r][0 .. cols), zeros behind (16-bit elements, ld_dst a multiple of eight); no rows: nothing to do
 struct Pack16 { const void* src; int64_t ld_src; void* dst; int64_t ld_dst, rows, cols; };
 hipError_t launch_pack16(const Pack16& one, const Pack16& two, hipStream_t s);
-// dz = dy * act'(z) as `type` (dz may be null), and the column sums of the unrounded dz by parts (part may be null)
+// dz = dy * act'(z) as `type` (dz may be null; in two parts if dz_lo is there), and the column sums of the unrounded dz by parts (part may be null)
 int slope_parts(int64_t M);
-hipError_t launch_slope(corr_dtype t, int act, const void* dy, int64_t ld_dy, const void* z, void* dz, int64_t ld_dz, float* part,
-                        int64_t M, int N, hipStream_t s);
+hipError_t launch_slope(corr_dtype t, int act, const void* dy, int64_t ld_dy, const void* z, void* dz, void* dz_lo, int64_t ld_dz,
+                        float* part, int64_t M, int N, hipStream_t s);
 
 // ---- norms around a block (residual_norm.hip)
 struct NormArgs {

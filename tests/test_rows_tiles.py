@@ -50,6 +50,15 @@ def test_refusals():
             b.corr_debug_linear_tile(*bad)
 
 
+def test_workspace_of_the_half_gradient():
+    """fp16 with an activation that shapes dz holds it in two parts."""
+    b = _binding()
+    size = lambda act: b.corr_linear_backward_workspace_bytes(F16, act, 4096, 256, 64)  # noqa: E731
+    assert size(b.CORR_ACT_RELU) - size(b.CORR_ACT_NONE) == 2 * 4096 * 256
+    for act in (b.CORR_ACT_GELU, b.CORR_ACT_GELU_TANH, b.CORR_ACT_SILU, b.CORR_ACT_SIGMOID):
+        assert size(act) - size(b.CORR_ACT_NONE) == 4 * 4096 * 256
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("tile,split,dtype,product,R,C,S", CASES)
 def test_tile(tile, split, dtype, product, R, C, S):
