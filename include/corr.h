@@ -239,7 +239,8 @@ typedef enum {
  *   residual : [M, N] rows, residual_stride, or NULL; may be y itself (same pointer and stride).
  *   preact   : NULL, or [M, N] dense: receives z, which corr_linear_backward reads.
  *   y        : [M, N] rows, y_stride.
- * fp32 products carry fp32's precision (each operand as three bf16 parts, six partial products).
+ * fp32 products carry fp32's precision (each operand as three bf16 parts, six partial products; elements below 2^-112 may
+ * lose digits).
  * Limits: M <= 2^30, N, K and strides <= 2^21, M*N, M*K and N*K <= 2^36; beyond: CORR_ERR_UNSUPPORTED.
  */
 size_t corr_linear_workspace_bytes(corr_dtype type, int64_t M, int64_t N, int64_t K, int64_t x_stride);
@@ -249,7 +250,7 @@ corr_status corr_linear(corr_dtype type, corr_activation act, const void* x, int
 /*
  * With dz = d_y act'(preact):  d_x = dz w,  d_w = dz^T x,  d_bias = sum over rows of dz.  The residual's gradient is d_y itself.
  *   preact : [M, N] dense, as corr_linear left it; not read (may be NULL) for CORR_ACT_NONE.  relu's slope at 0 is 0.
- *   d_y    : [M, N] rows, d_y_stride.
+ *   d_y    : [M, N] rows, d_y_stride.  x, w and d_y of 16 bits start on a 4-byte border.
  *   d_x    : [M, K] dense or NULL;  d_w : [N, K] dense or NULL;  d_bias : fp32 [N] or NULL.
  * dz as the products' operand: fp32 whole; bf16 rounded once, beside the results' own rounding (together sqrt 2 times its
  * error); fp16 in two parts of 22 bits together, so that d_x and d_w are rounded once and small gradients keep their digits (with relu or
@@ -272,7 +273,8 @@ corr_status corr_linear_backward(corr_dtype type, corr_activation act, const voi
  *   h_out: [rows, cols] dense, of stream_type, or NULL; may be h (if h_stride == cols).
  *   n_out: [rows, cols] dense, of type; NULL exactly if pre is CORR_NORM_NONE.
  * stream_type equals type, or is CORR_TYPE_F32 beside a 16-bit type.  A norm of CORR_NORM_NONE has no vectors.
- * eps > 0 serves both norms.  Limits: cols <= 16384 and strides <= 2^30, rows <= 2^30; beyond: CORR_ERR_UNSUPPORTED.
+ * eps > 0 serves both norms.  A row's squares are added in fp32: where their sum passes 3.4e38 (values of 1e18 and more) the normalised
+ * row is zero.  Limits: cols <= 16384 and strides <= 2^30, rows <= 2^30; beyond: CORR_ERR_UNSUPPORTED.
  */
 typedef struct {
     corr_dtype stream_type;              /* h, h_out, d_h_out, d_h */

@@ -471,7 +471,7 @@ def corr_linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = No
                 residual: torch.Tensor | None = None, out: torch.Tensor | None = None, preact: torch.Tensor | None = None,
                 workspace: torch.Tensor | None = None) -> torch.Tensor:
     """act(x w^T + bias) + residual.  x: [..., K] with contiguous, evenly spaced rows (corr_sample's CORR_OUT_NHWC output is
-    one); w: [N, K]; both float32, bfloat16 or float16.  bias: float32 [N].  residual, out: [..., N] of x's type; out may be
+    one); w: [N, K]; both float32, bfloat16 or float16 (16-bit ones start on a 4-byte border).  bias: float32 [N].  residual, out: [..., N] of x's type; out may be
     residual.  preact: a contiguous [..., N] that receives the sum before the activation (corr_linear_backward reads it)."""
     lib = _lib or load_library()
     device = _on_device(x, "x")
@@ -509,7 +509,8 @@ def corr_linear_backward(x: torch.Tensor, w: torch.Tensor, d_out: torch.Tensor, 
                          d_x: torch.Tensor | None = None, d_w: torch.Tensor | None = None, d_bias: torch.Tensor | None = None,
                          workspace: torch.Tensor | None = None):
     """(d_x, d_w, d_bias) of corr_linear, None where not wanted: x's type for the first two, float32 for the bias.  d_out: the
-    gradient of its result, which is the residual's too; preact: what corr_linear stored (needed for an activation)."""
+    gradient of its result, which is the residual's too, on a 4-byte border as x and w; preact: what corr_linear stored (needed for an
+    activation)."""
     lib = _lib or load_library()
     device = _on_device(x, "x")
     dtype = x.dtype

@@ -172,8 +172,8 @@ __device__ __forceinline__ void finish_wave(const ProductArgs& g, f32x4 (&acc)[F
 //   k contiguous:    rows of 2 BK bytes, piece p of row r at p ^ (r & 7) (BK = 32: p ^ (r / 2 & 3))
 //   rows contiguous: BK k-rows of 2 R bytes, 32-byte block c of row k at c ^ turn(k); read by the transposing LDS load
 // so that neither the rows of a fragment nor the k of a transposed one meet in a bank (LDS conflict cycles: 1 in 900).
-// 8192^3 bf16 with residual: 0.89 ms, 1.24 PFLOP/s, bound by the matrix cores under the card's power limit.  Short sums are bound by
-// bytes and by the turns of a tile (load, multiply, store): 32400 x 256 -> 1024, gelu, preact: 48 us, 149 MB.  A third stage in LDS and
+// 8192^3 bf16 with residual: 0.89 to 1.0 ms, 1.1 to 1.24 PFLOP/s, bound by the matrix cores under the card's power limit.  Short sums are
+// bound by bytes and by the turns of a tile (load, multiply, store): 32400 x 256 -> 1024, gelu, preact: 50 us, 149 MB.  A third stage in LDS and
 // orders of k that differ from tile to tile made no difference.
 template <int R> __device__ __forceinline__ int turn(int k) {
     return R >= 128 ? (k & 3) | ((k >> 3) & 1) << 2 : (k & 3) ^ ((k >> 3) & 1);
@@ -239,8 +239,9 @@ __device__ __forceinline__ V keep_first(V v, int left) {
 }
 
 // TWO: the first operand is in two parts (rows_internal.h), multiplied one after the other, the low one first: twice the matrix work and twice the
-// loads (fp16 gradients with silu beside relu: 14570 x 243 -> 126: 51 and 41 us; 32400 x 256 -> 1024: 153 and 104; 4096^3: 503 and 265).  A sum of the low part's products that is not finite says that an element of the second operand is not (fp16's values cannot
-// overflow it): then the high part alone gives what the whole would.
+// loads (fp16 gradients with silu, and with relu: 14570 x 243 -> 126: 51 and 41 us; 32400 x 256 -> 1024: 153 and 104; 4096^3: 503 and
+// 265).  A sum of the low part's products that is not finite says that an element of the second operand is not (fp16's values
+// cannot overflow it): then the high part alone gives what the whole would.
 template <class T, bool AR, bool BR, int BM, int BN, int WM, int WN, int BK, bool TWO>
 __global__ __launch_bounds__(64 * WM * WN, BK == 32 ? 4 : 2) void product16_kernel(ProductArgs g, int tm, int tn, int splits, int steps_per) {
     constexpr int WAVES = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
@@ -342,9 +343,10 @@ __global__ __launch_bounds__(64 * WM * WN, BK == 32 ? 4 : 2) void product16_kern
 // their way into registers meanwhile.
 //   k contiguous:    rows of 64 bytes, piece p of row r at p ^ (r / 2 & 3)
 //   rows contiguous: as for 16 bits, 32 k-rows
-// 4096^3: 0.61 ms = 225 TFLOP/s, 1.35 PFLOP/s of bf16 products; 518400 x 324 -> 256: 600 to 690 us.  There matrix instructions fill 43 % of the
-// cycles, splitting 28 %, at a clock that power holds at 1.8 GHz; without loads it takes 531 us, without stores 611, with one product
-// of six 472.  Two workgroups a compute unit; a third spills (838 us), and so does a second set of loads on their way.
+// 4096^3: 0.61 ms = 225 TFLOP/s, 1.35 PFLOP/s of bf16 products: the library's rate.  Short sums add their stores to that, one after the other:
+// 518400 x 1024 -> 256 is 1290 us of products and 109 of stores, 1399 in all; x 324 -> 256: 438 and 109, 600 to 710 us (as the clock falls under
+// sustained work: 1.8 GHz, matrix instructions in 43 % of the cycles, splitting in 28 %).  Without loads that took 531 us, with one
+// product of six 472.  Two workgroups a compute unit; a third spills (838 us), and so does a second set of loads on their way.
 template <bool ROWS, int R, int NT>
 struct Loader32 {
     static constexpr int PIECES = R * 8 / NT;
@@ -688,8 +690,8 @@ __global__ __launch_bounds__(256) void pack16_kernel(Pack16 one, Pack16 two) {
 // over rows meet in LDS.  Bound by bytes: 32400 x 1024 fp32: 74 us, 5.4 TB/s; 129600 x 256 bf16: 42 us, 4.7 TB/s.  dz is rounded to the
 // operands' type because the matrix cores take it so; the sums add what was not rounded.  bf16: once; the rounding is as large as that of the
 // results, whose error grows to sqrt 2 times theirs alone.  fp16 holds dz in two parts where an activation shapes it (`dz_lo`):
-// with one, a small d_y times a small slope would lose its digits below 6e-5 and vanish below 3e-8, and one above 1 / slope times fp16's
-// largest overflow (over half of the results were not the nearest fp16 values, and errors of 70 steps; now 1 in 1000).
+// with one, a small d_y times a small slope would lose its digits below 6e-5 and vanish below 3e-8, fp16's largest times gelu's 1.13 would
+// overflow, and half of the results would not be the nearest fp16 values (with two: 1 in 1000).
 constexpr int SLOPE_THREADS = 256;
 template <class T, int V>
 __global__ __launch_bounds__(SLOPE_THREADS) void slope_kernel(int act, const T* __restrict__ dy, int64_t ld_dy, const T* __restrict__ z,
@@ -720,7 +722,7 @@ __global__ __launch_bounds__(SLOPE_THREADS) void slope_kernel(int act, const T* 
                 }
 #pragma unroll
                 for (int e = 0; e < V; ++e) sum[e] += v[u][e];
-                if (dz_lo) {
+                if constexpr (std::is_same<T, _Float16>::value) if (dz_lo) {
                     float lo[V];
 #pragma unroll
                     for (int e = 0; e < V; ++e) {

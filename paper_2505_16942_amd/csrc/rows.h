@@ -26,9 +26,9 @@ __device__ __forceinline__ float row_sigmoid_slope(float z) {
 __device__ __forceinline__ float row_gelu_2u(float z) { return 1.5957691216057308f * fmaf(0.044715f * z * z, z, z); }
 // The normal distribution's integral up to z, and `tail` = e^(-z^2/2).  The integral from |z| on is tail t P(t), t = 1 / (1 + 0.35 |z|): P, of
 // degree eight, has the least relative error over t (3e-8, fitted on Chebyshev points), so that gelu keeps its digits where it dies away:
-// off by (1.5 z^2 + 32) 2^-24 at most, relative, most of it from the exponent.  A polynomial that is good to 1.5e-7 absolute
-// lets go of them there (Abramowitz and Stegun 7.1.26: 5e-5 off at z = -3, 1.6e-3 at -5); the
-// library's erff has two branches, and a wave takes both: 32400 x 1024 outputs took 122 us with it.
+// off by (1.5 z^2 + 32) 2^-24 at most, relative, most of it from the exponent.  A polynomial that is good to 1.5e-7
+// absolute (Abramowitz and Stegun 7.1.26) is 5e-5 off at z = -3, 1.6e-3 at -5.  The library's erff has two branches, and a wave takes
+// both: 32400 x 1024 outputs took 122 us with it.
 __device__ __forceinline__ float row_normal(float z, float& tail) {
     const float t = __builtin_amdgcn_rcpf(fmaf(0.35f, fabsf(z), 1.f));
     tail = __builtin_amdgcn_exp2f(-0.72134752044448170f * (z * z));
