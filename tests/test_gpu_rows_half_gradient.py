@@ -89,3 +89,29 @@ def test_not_finite(N, K):
         assert torch.equal(torch.isnan(got), torch.isnan(want))
         assert torch.equal(got.isinf() * got.sign().nan_to_num(), want.isinf() * want.sign().nan_to_num())
     assert torch.isfinite(d_x[11, 9]) and abs(float(d_x[11, 9]) - 0.5 * float(dz[11, 6])) <= 32
+
+
+def test_captured_and_on_another_stream():
+    """Both parts lie in the call's own workspace: replays between eager calls on changing inputs, and a call on another stream, give its bits."""
+    b = _b()
+    x, w, dy, z, act = _case(700, 126, 243, 0.05, "silu", 8)
+    call = lambda **kw: b.corr_linear_backward(x, w, dy, preact=z, act=act, **kw)  # noqa: E731
+    want = call()
+    ws = torch.full((b.corr_linear_backward_workspace_bytes(F16, act, 700, 126, 243),), 0xff, dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = call(workspace=ws)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = call()
+    for k in range(4):
+        _, _, dy_k, z_k, _ = _case(700, 126, 243, 0.05, "silu", 20 + k)
+        dy.copy_(dy_k)
+        z.copy_(z_k)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(held, call())), k
