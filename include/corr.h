@@ -306,6 +306,54 @@ corr_status corr_residual_norm_backward(const corr_residual_norm_args* args, con
                                         float* d_post_bias, float* d_pre_weight, float* d_pre_bias,
                                         void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * ---- Maps ---------------------------------------------------------------------------------------------
+ * What a flow network does to its two maps before the pyramid is built from them: norms over groups of channels behind its convolutions,
+ * attention of one map's rows to the other's, and the gated products of a feed-forward block.  The paper leaves these to the network; the
+ * operations are defined here.  What is said of rows above (types, fp32 in between, streams, workspaces, the same bits on every call) holds here too.
+ */
+
+/*
+ * Attention of B items' Lq rows to Lk keys, which may be another map's, or an encoder's states of any length:
+ *     out[b, i, h] = sum over keys j of softmax_j(scale <q[b, i, h], k[b, j, h / (H / HK)]>) v[b, j, h / (H / HK)]
+ * H query heads, HK key heads (HK divides H: query heads that follow each other share one), heads of D elements.
+ *   q, k, v    : elements of `type`; `_item`, `_row` and `_head` are the elements from one item (row, head) to the next: [B, L, H, D], or columns of
+ *                a wider projection, or heads first.  16-bit arrays start on a 4-byte border and their strides are even.  An item, row or head
+ *                stride may be 0.
+ *   k_lengths  : NULL, or device int32 [B]: item b's keys from k_lengths[b] on do not count (values are taken into 0 .. Lk).
+ *   key_mask   : NULL, or device bytes [B, Lk], dense: keys whose byte is 0 do not count (the padding of a map, say).  What lies at a key
+ *                that does not count is not read or has no influence, infinities and NaN included.
+ *   out        : [B, Lq, H, D] dense.  A row of which no key counts, or whose every score is -infinity, is zeros.
+ *   lse        : NULL, or fp32 [B, H, Lq]: the logarithm of the sum of e^score, which the gradient reads (-infinity for rows of zeros).
+ * Weights meet v as `type` values: rounded once each (fp16: 2^14 times as large, so that weights down to 4e-9 of a row's largest keep their
+ * digits); their sum is not.
+ * Limits: D a multiple of 8 up to 256, H <= 128, strides of rows and heads <= 2^21 and of items <= 2^40, B * HK <= 2^20, Lq * H / HK and Lk <= 2^30, B * Lq * H * D and
+ * B * Lk * HK * D <= 2^36; beyond: CORR_ERR_UNSUPPORTED.  scale is positive and finite.
+ */
+typedef struct {
+    corr_dtype type;
+    int64_t B, Lq, Lk, H, HK, D;
+    const void* q; int64_t q_item, q_row, q_head;
+    const void* k; int64_t k_item, k_row, k_head;
+    const void* v; int64_t v_item, v_row, v_head;
+    float scale;
+    const int32_t* k_lengths;
+    const uint8_t* key_mask;
+} corr_attention_args;
+size_t corr_attention_workspace_bytes(corr_dtype type, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t HK, int64_t D);
+corr_status corr_attention(const corr_attention_args* args, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * Gradients at the forward call's own arguments, with out and lse as it left them.
+ *   d_out    : [B, Lq, H, D] dense, on a 4-byte border.
+ *   d_q      : [B, Lq, H, D] dense, or NULL;  d_k, d_v : [B, Lk, HK, D] dense, or both NULL.  Shared heads' gradients are their query heads' sums;
+ *              keys that do not count get zeros.
+ * Weights and dS = P (d_out v^T - sum d_out out) meet the other operand as `type` values, rounded once each (fp16: dS times a power of two of
+ * its row or key, so that small gradients keep their digits).
+ */
+size_t corr_attention_backward_workspace_bytes(corr_dtype type, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t HK, int64_t D);
+corr_status corr_attention_backward(const corr_attention_args* args, const void* out, const float* lse, const void* d_out,
+                                    void* d_q, void* d_k, void* d_v, void* workspace, size_t workspace_bytes, void* stream);
+
 const char* corr_status_string(corr_status s);
 
 #ifdef __cplusplus

@@ -37,6 +37,7 @@ EXPORTS = [
     "corr_backward_workspace_bytes", "corr_sample_backward",
     "corr_linear_workspace_bytes", "corr_linear", "corr_linear_backward_workspace_bytes", "corr_linear_backward",
     "corr_residual_norm", "corr_residual_norm_backward_workspace_bytes", "corr_residual_norm_backward",
+    "corr_attention_workspace_bytes", "corr_attention", "corr_attention_backward_workspace_bytes", "corr_attention_backward",
 ]
 # measurement and test hooks (include/corr_bench.h)
 BENCH_EXPORTS = [
@@ -77,6 +78,14 @@ def residual_norm_args(*fields) -> bytes:
     return _NORM_ARGS.pack(*[0 if f is None else f for f in fields])
 
 
+# corr_attention_args: type, B, Lq, Lk, H, HK, D, (q, k, v: pointer, item, row and head stride), scale, k_lengths, key_mask
+_ATTENTION_ARGS = struct.Struct("@iqqqqqqPqqqPqqqPqqqfPP")
+
+
+def attention_args(*fields) -> bytes:
+    return _ATTENTION_ARGS.pack(*[0 if f is None else f for f in fields])
+
+
 _lib = None
 
 
@@ -110,6 +119,13 @@ def load_library():
     lib.corr_sample_backward.argtypes = [vp, vp, vp, ci, ci, ci, ci, ci, ci, vp, vp, vp, sz, vp]
     lib.corr_sample_backward.restype = ci
     i64 = ctypes.c_int64
+    for name in ("corr_attention_workspace_bytes", "corr_attention_backward_workspace_bytes"):
+        getattr(lib, name).argtypes = [ci] + [i64] * 6
+        getattr(lib, name).restype = sz
+    lib.corr_attention.argtypes = [ctypes.c_char_p, vp, vp, vp, sz, vp]
+    lib.corr_attention.restype = ci
+    lib.corr_attention_backward.argtypes = [ctypes.c_char_p] + [vp] * 7 + [sz, vp]
+    lib.corr_attention_backward.restype = ci
     lib.corr_linear_workspace_bytes.argtypes = [ci, i64, i64, i64, i64]
     lib.corr_linear_workspace_bytes.restype = sz
     lib.corr_linear.argtypes = [ci, ci, vp, i64, vp, vp, vp, i64, vp, vp, i64, i64, i64, i64, vp, sz, vp]
@@ -643,6 +659,108 @@ def corr_residual_norm_backward(h: torch.Tensor, y: torch.Tensor | None = None, 
     if st != CORR_OK:
         raise CorrError(st, "corr_residual_norm_backward")
     return g
+
+
+@functools.lru_cache(maxsize=1024)
+def _attention_need(*sizes) -> int:
+    return int(load_library().corr_attention_workspace_bytes(*sizes))
+
+
+@functools.lru_cache(maxsize=1024)
+def _attention_backward_need(*sizes) -> int:
+    return int(load_library().corr_attention_backward_workspace_bytes(*sizes))
+
+
+def _heads(t, name: str, dtype, device: int):
+    """(shape, pointer, item stride, row stride, head stride) of [B, L, H, D] with contiguous heads; an axis of one has no stride."""
+    _on_device(t, name, device)
+    if t.dim() != 4:
+        raise ValueError("%s must be [B, L, H, D]" % name)
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s" % (name, dtype))
+    shape, strides = t.shape, t.stride()
+    if strides[3] != 1 and shape[3] > 1:
+        raise ValueError("%s must have contiguous heads" % name)
+    return shape, t.data_ptr() or 256, *[s if n > 1 else 0 for n, s in zip(shape[:3], strides[:3])]
+
+
+def _attention_args(q, k, v, scale, k_lengths, key_mask):
+    """(arguments, sizes with the type first, device)"""
+    device = _on_device(q, "q")
+    code = _type_of(q, "q")
+    qs, *pq = _heads(q, "q", q.dtype, device)
+    ks, *pk = _heads(k, "k", q.dtype, device)
+    vs, *pv = _heads(v, "v", q.dtype, device)
+    B, Lq, H, D = qs
+    Lk, HK = ks[1], ks[2]
+    if ks != vs or ks[0] != B or ks[3] != D or HK < 1 or H % HK:
+        raise ValueError("k and v must be [%d, keys, heads, %d], with a number of heads that divides q's" % (B, D))
+    pl = None if k_lengths is None else _dense(k_lengths, "k_lengths", torch.int32, device, (B,))
+    pm = None
+    if key_mask is not None:
+        if isinstance(key_mask, torch.Tensor) and key_mask.dtype is torch.bool:
+            key_mask = key_mask.view(torch.uint8)
+        pm = _dense(key_mask, "key_mask", torch.uint8, device, (B, Lk))
+    sizes = (code, B, Lq, Lk, H, HK, D)
+    return attention_args(*sizes, *pq, *pk, *pv, D ** -0.5 if scale is None else scale, pl, pm), sizes, device
+
+
+def corr_attention_workspace_bytes(dtype: torch.dtype, B: int, Lq: int, Lk: int, H: int, HK: int, D: int) -> int:
+    return int(load_library().corr_attention_workspace_bytes(_TYPES[dtype], B, Lq, Lk, H, HK, D))
+
+
+def corr_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float | None = None,
+                   k_lengths: torch.Tensor | None = None, key_mask: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                   lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """softmax(scale q k^T) v per head (include/corr.h): [B, Lq, H, D].  q: [B, Lq, H, D]; k, v: [B, Lk, HK, D], HK dividing H; any strides with
+    contiguous heads, 16-bit ones even.  scale: 1 / sqrt(D) if None.  k_lengths: int32 [B] on the GPU; key_mask: uint8 or bool [B, Lk],
+    zero where a key does not count.  lse: a contiguous float32 [B, H, Lq] that receives the logarithms of the rows' sums
+    (corr_attention_backward reads them)."""
+    lib = _lib or load_library()
+    a, sizes, device = _attention_args(q, k, v, scale, k_lengths, key_mask)
+    _, B, Lq, _, H, _, D = sizes
+    if out is None:
+        out = _new(q, (B, Lq, H, D), q.dtype)
+        po = _pointer(out)
+    else:
+        po = _dense(out, "out", q.dtype, device, (B, Lq, H, D))
+    pl = None if lse is None else _dense(lse, "lse", torch.float32, device, (B, H, Lq))
+    held, ws, size = _workspace(workspace, _attention_need(*sizes), q, device)
+    st = lib.corr_attention(a, po, pl, ws, size, _stream())
+    if st != CORR_OK:
+        raise CorrError(st, "corr_attention")
+    return out
+
+
+def corr_attention_backward_workspace_bytes(dtype: torch.dtype, B: int, Lq: int, Lk: int, H: int, HK: int, D: int) -> int:
+    return int(load_library().corr_attention_backward_workspace_bytes(_TYPES[dtype], B, Lq, Lk, H, HK, D))
+
+
+def corr_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor, d_out: torch.Tensor,
+                            scale: float | None = None, k_lengths: torch.Tensor | None = None, key_mask: torch.Tensor | None = None,
+                            want_q: bool = True, want_kv: bool = True, d_q: torch.Tensor | None = None, d_k: torch.Tensor | None = None,
+                            d_v: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """(d_q, d_k, d_v) of corr_attention at its own arguments, contiguous, None where not wanted.  out, lse: what it returned and stored;
+    d_out: the gradient of out, contiguous.  Shared heads' gradients are summed."""
+    lib = _lib or load_library()
+    a, sizes, device = _attention_args(q, k, v, scale, k_lengths, key_mask)
+    _, B, Lq, Lk, H, HK, D = sizes
+    rows, keys = (B, Lq, H, D), (B, Lk, HK, D)
+    po, pg = _dense(out, "out", q.dtype, device, rows), _dense(d_out, "d_out", q.dtype, device, rows)
+    pl = _dense(lse, "lse", torch.float32, device, (B, H, Lq))
+    pq = pk = pv = None
+    if want_q:
+        d_q = _new(q, rows, q.dtype) if d_q is None else d_q
+        pq = _dense(d_q, "d_q", q.dtype, device, rows)
+    if want_kv:
+        d_k = _new(q, keys, q.dtype) if d_k is None else d_k
+        d_v = _new(q, keys, q.dtype) if d_v is None else d_v
+        pk, pv = _dense(d_k, "d_k", q.dtype, device, keys), _dense(d_v, "d_v", q.dtype, device, keys)
+    held, ws, size = _workspace(workspace, _attention_backward_need(*sizes), q, device)
+    st = lib.corr_attention_backward(a, po, pl, pg, pq, pk, pv, ws, size, _stream())
+    if st != CORR_OK:
+        raise CorrError(st, "corr_attention_backward")
+    return d_q if want_q else None, d_k if want_kv else None, d_v if want_kv else None
 
 
 def corr_last_block_stats(pyramid: Pyramid, r: int = 4) -> dict:

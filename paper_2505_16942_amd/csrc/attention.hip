@@ -1,0 +1,780 @@
+// Attention of one map's rows to another's: o = softmax(scale q k^T) v per head, and its gradient.  Compiled once per type
+// (CORR_ATTENTION_TYPE: 0 fp32, 1 bf16, 2 fp16).
+#include <type_traits>
+#include "matrix.h"
+#include "attention.h"
+
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.69314718055994531f;
+constexpr unsigned PAST = 0x80000000u;      // an offset past every resource's end: the load into LDS writes zeros
+constexpr unsigned RANGE = 0x7ffffff0u;
+inline int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+// ---- how products are made.  A fragment is one matrix instruction's operand: lane (lr, lg) = (lane & 15, lane >> 4) holds row lr.  `straight`: a tile's
+// row against K elements along the row.  `turned`: one of its columns against K of its rows; these K rows are taken in the order in which a
+// product's result lies in its lanes (row 4 lg + e of each block of 16), so that the scores are the next product's operand without leaving
+// their lanes.  Tiles lie in LDS in rows of DP elements, 16-byte piece p of row r at slot(r, p), which spreads both kinds of read over the banks.
+template <class T> struct Num {
+    typedef typename Frag<T>::type F;
+    static constexpr int K = 32, V = 8;     // elements of k a fragment, elements a lane
+    template <int DP> static __device__ __forceinline__ int slot(int row, int piece) { return DP == 32 ? piece ^ (row >> 1 & 3) : piece ^ (row & 7); }
+    template <int DP> static __device__ __forceinline__ F straight(lds_byte* tile, int row, int t, int lg) {
+        return *(__attribute__((address_space(3))) F*)(tile + row * 2 * DP + slot<DP>(row, 4 * t + lg) * 16);
+    }
+    template <int DP> static __device__ __forceinline__ F turned(lds_byte* tile, int row0, int db, int lr, int lg) {
+        const int r = row0 + 4 * lg + (lr >> 2), piece = 2 * db + ((lr & 3) >> 1);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + r * 2 * DP + slot<DP>(r, piece) * 16 + (lr & 1) * 8));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + (r + 16) * 2 * DP + slot<DP>(r + 16, piece) * 16 + (lr & 1) * 8));
+        return __builtin_bit_cast(F, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    static __device__ __forceinline__ F pack(const f32x4* x) {
+        F f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = (T)x[e >> 2][e & 3];
+        return f;
+    }
+    static __device__ __forceinline__ f32x4 times(F a, F b, f32x4 c) { return mma(a, b, c); }
+};
+// fp32 instructions: four k each, the same element of four lanes' 16 bytes
+template <> struct Num<float> {
+    typedef f32x4 F;
+    enum { K = 16, V = 4 };
+    template <int DP> static __device__ __forceinline__ int slot(int row, int piece) { return piece ^ (row & 7); }
+    template <int DP> static __device__ __forceinline__ F straight(lds_byte* tile, int row, int t, int lg) {
+        return *(__attribute__((address_space(3))) F*)(tile + row * 4 * DP + slot<DP>(row, 4 * t + lg) * 16);
+    }
+    template <int DP> static __device__ __forceinline__ F turned(lds_byte* tile, int row0, int db, int lr, int lg) {
+        F f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int r = row0 + 4 * lg + e;
+            f[e] = *(__attribute__((address_space(3))) float*)(tile + r * 4 * DP + slot<DP>(r, 4 * db + (lr >> 2)) * 16 + (lr & 3) * 4);
+        }
+        return f;
+    }
+    static __device__ __forceinline__ F pack(const f32x4* x) { return *x; }
+    static __device__ __forceinline__ f32x4 times(F a, F b, f32x4 c) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+        return c;
+    }
+};
+// Weights as a product's operand.  fp16's normal values begin at 6e-5, below which a softmax over many keys lies: they are held 2^14 times as
+// large (at most 16384), and the results divided by that.
+template <class T> constexpr float LIFT = std::is_same<T, _Float16>::value ? 14.f : 0.f;
+
+// rows (keys) of a tile in LDS: up to 16 KB of them, of at most 64
+template <class T, int DP, int WAVES> constexpr int tile_rows() {
+    const int most = (WAVES == 1 ? 8192 : 16384) / (DP * (int)sizeof(T)), least = Num<T>::K;
+    return most > 64 ? 64 : most < least ? least : most;
+}
+
+// the largest (sum) over the four lanes that share lane & 15
+struct Both { float one, two; };
+__device__ __forceinline__ Both swap16(float x) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return {__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ Both swap32(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return {__uint_as_float(r[0]), __uint_as_float(r[1])};
+}
+__device__ __forceinline__ float lanes_max(float x) {
+    const Both a = swap16(x), b = swap32(fmaxf(a.one, a.two));
+    return fmaxf(b.one, b.two);
+}
+__device__ __forceinline__ float lanes_sum(float x) {
+    const Both a = swap16(x), b = swap32(a.one + a.two);
+    return b.one + b.two;
+}
+
+// ---- tiles
+// Where a workgroup's tile is loaded from: rows of a strided array, D of DP elements each.
+template <class T, int DP, int ROWS, int WAVES>
+struct Tile {
+    static constexpr int BYTES = ROWS * DP * (int)sizeof(T), PIECES = BYTES / (1024 * WAVES);
+    static_assert(BYTES % (1024 * WAVES) == 0 && PIECES > 0, "whole loads of 1024 bytes for every wave");
+    int row[PIECES];
+    unsigned col[PIECES];                    // byte offset inside the row, or PAST behind its end
+    __device__ __forceinline__ void plan(int wave, int lane, int D) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int at = (i * WAVES + wave) * 1024 + lane * 16, slot = at / 16 % (DP * (int)sizeof(T) / 16);
+            row[i] = at / (DP * (int)sizeof(T));
+            const int piece = Num<T>::template slot<DP>(row[i], slot);      // an involution
+            col[i] = piece * (16 / (int)sizeof(T)) < D ? piece * 16 : PAST;
+        }
+    }
+    static __device__ __forceinline__ i32x4 resource(const T* p) {
+        const uint64_t u = (uint64_t)p;
+        return i32x4{__builtin_amdgcn_readfirstlane((int)u), __builtin_amdgcn_readfirstlane((int)(u >> 32) & 0xffff), (int)RANGE, 0x00020000};
+    }
+    // rows `stride` elements apart from p on, those whose bit is set
+    __device__ __forceinline__ void ask(const T* p, int64_t stride, uint64_t bits, unsigned lds, int wave) const {
+        const i32x4 rsrc = resource(p);
+        const unsigned step = (unsigned)(stride * (int)sizeof(T));
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const bool there = (bits >> row[i]) & 1 && col[i] != PAST;
+            dma16(rsrc, lds + (i * WAVES + wave) * 1024, there ? row[i] * step + col[i] : PAST);
+        }
+    }
+};
+// Which keys of a tile count: those before the item's length (and the share's end) whose mask byte is not zero.
+struct Keys {
+    const uint8_t* mask;                     // of this item, or null
+    int end;
+    __device__ __forceinline__ unsigned byte(int k0, int lane) const { return mask && k0 + lane < end ? mask[k0 + lane] : 0u; }
+    __device__ __forceinline__ uint64_t bits(int k0, int n, unsigned byte) const {
+        const int left = min(end - k0, n);
+        uint64_t w = left <= 0 ? 0 : ~0ull >> (64 - left);
+        if (mask) w &= __ballot(byte != 0);
+        return w;
+    }
+};
+template <class T> __device__ __forceinline__ Keys keys_of(const AttentionArgs& a, int b) {
+    Keys k;
+    k.end = a.Lk;
+    if (a.k_lengths) k.end = max(0, min(a.Lk, __builtin_amdgcn_readfirstlane(a.k_lengths[b])));
+    k.mask = a.key_mask ? a.key_mask + (int64_t)b * a.Lk : nullptr;
+    return k;
+}
+// 16 bytes of row `p` from element d on, zeros behind D or without a row
+template <class T>
+__device__ __forceinline__ typename Num<T>::F load_frag(const T* p, int d, int D, bool there) {
+    typename Num<T>::F f = {};
+    if (there && d < D) f = *reinterpret_cast<const typename Some<T, Num<T>::V>::type*>(p + d);
+    return f;
+}
+// Workgroup w runs on XCD w % 8: each XCD gets a run of consecutive pieces of work, so that the tiles of one head share its keys in one L2.
+__device__ __forceinline__ int piece_of(int w, int all) {
+    const int q = all >> 3, r = all & 7, x = w & 7;
+    return x * q + min(x, r) + (w >> 3);
+}
+struct Place { int b, hk, bh, tile, split; };
+__device__ __forceinline__ Place place_of(const AttentionArgs& a, int tiles, int splits) {
+    const int n = piece_of(blockIdx.x, tiles * splits * a.B * a.HK);
+    Place p;
+    p.tile = n % tiles;
+    const int m = n / tiles;
+    p.split = m % splits;
+    p.bh = m / splits;
+    p.b = p.bh / a.HK;
+    p.hk = p.bh - p.b * a.HK;
+    return p;
+}
+__device__ __forceinline__ void query_of(const AttentionArgs& a, int r, int& q, int& g) {
+    q = a.per == 1 ? r : (int)((unsigned)r / (unsigned)a.per);
+    g = r - q * a.per;
+}
+
+// ---- forward.  One pass over the keys with a running maximum m and sum l of each row.  S^T = K Q^T in tiles of 16 keys x 16 rows: a lane has four
+// keys of one row, so that a row's maximum is a lane's own and two exchanges away, and the weights are the operand of O^T = V^T P^T as
+// they lie.  Weights are rounded once to the operands' type (their sum is not): errors of single weights, at most half a step each, which the sum over
+// keys averages.
+template <class T, int DP, int WAVES, int QB>
+__global__ __launch_bounds__(64 * WAVES, WAVES == 1 ? 1 : 2) void forward_kernel(AttentionArgs a, int tiles, int splits, int share) {
+    typedef Num<T> N;
+    typedef typename N::F F;
+    constexpr int KT = tile_rows<T, DP, WAVES>(), KB = KT / 16, CH = DP / N::K, DB = DP / 16, PB = N::K / 16;
+    typedef Tile<T, DP, KT, WAVES> Load;
+    __shared__ __align__(1024) unsigned char smem[4 * Load::BYTES];
+    lds_byte* const lds = (lds_byte*)smem;
+    const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)lds);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lg = lane >> 4;
+    const Place at = place_of(a, tiles, splits);
+    Keys keys = keys_of<T>(a, at.b);
+    const int k_lo = at.split * share;
+    keys.end = min(keys.end, k_lo + share);
+    const int steps = keys.end > k_lo ? (keys.end - k_lo + KT - 1) / KT : 0;
+    const T* const K0 = (const T*)a.k + at.b * a.k_item + at.hk * a.k_head + k_lo * a.k_row;
+    const T* const V0 = (const T*)a.v + at.b * a.v_item + at.hk * a.v_head + k_lo * a.v_row;
+    const int r0 = (at.tile * WAVES + wave) * 16 * QB;
+    F fq[QB][CH];
+#pragma unroll
+    for (int j = 0; j < QB; ++j) {
+        const int r = r0 + 16 * j + lr;
+        int q, g;
+        query_of(a, r, q, g);
+        const T* p = (const T*)a.q + at.b * a.q_item + (at.hk * a.per + g) * a.q_head + q * a.q_row;
+#pragma unroll
+        for (int t = 0; t < CH; ++t) fq[j][t] = load_frag<T>(p, t * N::K + lg * N::V, a.D, r < a.rows);
+    }
+    Load load;
+    load.plan(wave, lane, a.D);
+    auto ask = [&](int t, uint64_t bits) {
+        const unsigned to = lds_at + (t & 1) * 2 * Load::BYTES;
+        load.ask(K0 + (int64_t)t * KT * a.k_row, a.k_row, bits, to, wave);
+        load.ask(V0 + (int64_t)t * KT * a.v_row, a.v_row, bits, to + Load::BYTES, wave);
+    };
+    const float c = a.scale * LOG2E;
+    f32x4 o[DB][QB] = {};
+    float m[QB], mc[QB], l[QB];
+#pragma unroll
+    for (int j = 0; j < QB; ++j) { m[j] = -INFINITY; mc[j] = 0.f; l[j] = 0.f; }
+    uint64_t bits = 0;
+    unsigned byte = 0;
+    if (steps) {
+        bits = keys.bits(k_lo, KT, keys.byte(k_lo, lane));
+        if (bits) ask(0, bits);
+        byte = keys.byte(k_lo + KT, lane);
+    }
+    for (int t = 0; t < steps; ++t) {
+        arrive_all();
+        uint64_t next = 0;
+        if (t + 1 < steps) {
+            next = keys.bits(k_lo + (t + 1) * KT, KT, byte);
+            if (next) ask(t + 1, next);
+            byte = keys.byte(k_lo + (t + 2) * KT, lane);
+        }
+        if (bits) {
+            lds_byte* const tk = lds + (t & 1) * 2 * Load::BYTES;
+            lds_byte* const tv = tk + Load::BYTES;
+            f32x4 s[QB][KB] = {};
+#pragma unroll
+            for (int h = 0; h < CH; ++h)
+#pragma unroll
+                for (int i = 0; i < KB; ++i) {
+                    const F f = N::template straight<DP>(tk, 16 * i + lr, h, lg);
+#pragma unroll
+                    for (int j = 0; j < QB; ++j) s[j][i] = N::times(f, fq[j][h], s[j][i]);
+                }
+            if (bits != ~0ull >> (64 - KT)) {
+                const uint64_t mine = bits >> (4 * lg);
+#pragma unroll
+                for (int i = 0; i < KB; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int j = 0; j < QB; ++j) s[j][i][e] = (mine >> (16 * i + e)) & 1 ? s[j][i][e] : -INFINITY;
+            }
+            bool grew = false;
+            float top[QB];
+#pragma unroll
+            for (int j = 0; j < QB; ++j) {
+                float x = s[j][0][0];
+#pragma unroll
+                for (int i = 0; i < KB; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x = fmaxf(x, s[j][i][e]);
+                top[j] = lanes_max(x);
+                grew |= top[j] > m[j];
+            }
+            if (__any(grew)) {
+#pragma unroll
+                for (int j = 0; j < QB; ++j) {
+                    const float was = m[j];
+                    m[j] = fmaxf(was, top[j]);
+                    const float now = m[j] == -INFINITY ? 0.f : m[j] * c, by = was == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc[j] - now);
+                    mc[j] = now;
+                    l[j] *= by;
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) o[d][j] *= by;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < QB; ++j)
+#pragma unroll
+                for (int i = 0; i < KB; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        s[j][i][e] = __builtin_amdgcn_exp2f(fmaf(s[j][i][e], c, LIFT<T> - mc[j]));
+                        l[j] += s[j][i][e];
+                    }
+#pragma unroll
+            for (int i = 0; i < KB; i += PB) {
+                F fp[QB];
+#pragma unroll
+                for (int j = 0; j < QB; ++j) fp[j] = N::pack(&s[j][i]);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    const F f = N::template turned<DP>(tv, 16 * i, d, lr, lg);
+#pragma unroll
+                    for (int j = 0; j < QB; ++j) o[d][j] = N::times(f, fp[j], o[d][j]);
+                }
+            }
+        }
+        bits = next;
+    }
+#pragma unroll
+    for (int j = 0; j < QB; ++j) {
+        const float sum = lanes_sum(l[j]);
+        const int r = r0 + 16 * j + lr;
+        if (r >= a.rows) continue;
+        int q, g;
+        query_of(a, r, q, g);
+        const int head = at.hk * a.per + g;
+        if (splits > 1) {
+            const int64_t row = ((int64_t)at.split * a.B * a.HK + at.bh) * a.rows + r;
+#pragma unroll
+            for (int d = 0; d < DB; ++d)
+                if (16 * d + 4 * lg < a.D) *reinterpret_cast<f32x4*>(a.part_o + row * a.D + 16 * d + 4 * lg) = o[d][j];
+            if (lg == 0) { a.part_ml[2 * row] = mc[j] - LIFT<T>; a.part_ml[2 * row + 1] = sum; }
+            continue;
+        }
+        const float by = sum == 0.f ? 0.f : 1.f / sum;
+        T* const p = (T*)a.out + (((int64_t)at.b * a.Lq + q) * a.HK * a.per + head) * a.D;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            const float v[4] = {o[d][j][0] * by, o[d][j][1] * by, o[d][j][2] * by, o[d][j][3] * by};
+            if (16 * d + 4 * lg < a.D) store_some<T, 4>(p + 16 * d + 4 * lg, v, 4);
+        }
+        if (a.lse && lg == 0)
+            a.lse[((int64_t)at.b * a.HK * a.per + head) * a.Lq + q] = sum == 0.f ? -INFINITY : (mc[j] - LIFT<T> + log2f(sum)) * LN2;
+    }
+}
+
+// The splits' sums of a row, brought to one exponent: 16 lanes a row.
+template <class T>
+__global__ __launch_bounds__(256) void forward_join_kernel(AttentionArgs a, int splits) {
+    const int64_t all = (int64_t)a.B * a.HK * a.rows, row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
+    const int lane = threadIdx.x & 15;
+    if (row >= all) return;
+    const int bh = (int)(row / a.rows), r = (int)(row - (int64_t)bh * a.rows), b = bh / a.HK, hk = bh - b * a.HK;
+    int q, g;
+    query_of(a, r, q, g);
+    const int head = hk * a.per + g;
+    float top = -INFINITY;
+    for (int s = 0; s < splits; ++s) {
+        const float* ml = a.part_ml + 2 * (s * all + row);
+        if (ml[1] != 0.f) top = fmaxf(top, ml[0]);
+    }
+    float sum = 0.f;
+    for (int s = 0; s < splits; ++s) {
+        const float* ml = a.part_ml + 2 * (s * all + row);
+        if (ml[1] != 0.f) sum += ml[1] * __builtin_amdgcn_exp2f(ml[0] - top);
+    }
+    const float by = sum == 0.f ? 0.f : 1.f / sum;
+    T* const p = (T*)a.out + (((int64_t)b * a.Lq + q) * a.HK * a.per + head) * a.D;
+    for (int d = 4 * lane; d < a.D; d += 64) {
+        f32x4 x = {};
+#pragma unroll 4
+        for (int s = 0; s < splits; ++s) {
+            const float* ml = a.part_ml + 2 * (s * all + row);
+            const f32x4 o = *reinterpret_cast<const f32x4*>(a.part_o + (s * all + row) * a.D + d);
+            if (ml[1] != 0.f) x += o * (__builtin_amdgcn_exp2f(ml[0] - top));
+        }
+        const float v[4] = {x[0] * by, x[1] * by, x[2] * by, x[3] * by};
+        store_some<T, 4>(p + d, v, 4);
+    }
+    if (a.lse && lane == 0) a.lse[((int64_t)b * a.HK * a.per + head) * a.Lq + q] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * LN2;
+}
+
+// ---- gradient.  With P = exp(s - lse) and delta = sum over d of d_out out: dV = P^T dO, dS = P (dO V^T - delta), dQ = scale dS K,
+// dK = scale dS^T Q.  Rows' sums meet in one workgroup and keys' sums in another, so scores are computed twice and nothing is added by atomics.
+// delta, and lse in powers of two, in the order of rows; rows behind the last have a weight of zero.
+template <class T>
+__global__ __launch_bounds__(256) void delta_kernel(AttentionArgs a, int aux_rows) {
+    const int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
+    const int lane = threadIdx.x & 15, bh = (int)(row / aux_rows), r = (int)(row - (int64_t)bh * aux_rows), b = bh / a.HK, hk = bh - b * a.HK;
+    if (row >= (int64_t)a.B * a.HK * aux_rows) return;
+    float sum = 0.f, low = INFINITY;
+    if (r < a.rows) {
+        int q, g;
+        query_of(a, r, q, g);
+        const int head = hk * a.per + g;
+        const int64_t at = (((int64_t)b * a.Lq + q) * a.HK * a.per + head) * a.D;
+        for (int d = 8 * lane; d < a.D; d += 128) {
+            float x[8], y[8];
+            load_some<T, 8>((const T*)a.o + at + d, x, 8);
+            load_some<T, 8>((const T*)a.d_out + at + d, y, 8);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum = fmaf(x[e], y[e], sum);
+        }
+        low = a.saved_lse[((int64_t)b * a.HK * a.per + head) * a.Lq + q] * LOG2E;
+        if (low == -INFINITY) low = INFINITY;            // a row without a key: no weight
+    }
+#pragma unroll
+    for (int x = 1; x < 16; x *= 2) sum += __shfl_xor(sum, x);
+    if (lane == 0) { a.aux[2 * row] = low; a.aux[2 * row + 1] = low == INFINITY ? 0.f : sum; }
+}
+
+// dS as a product's operand.  bf16 has fp32's range: rounded once.  fp16 would lose what is small: a row's (key's) elements are held
+// times a power of two that brings the largest so far to 2^13 .. 2^15, and the sums follow when it changes.
+template <class T, int N> struct Lifted {
+    static constexpr bool ON = std::is_same<T, _Float16>::value;
+    float by[N];
+    __device__ __forceinline__ Lifted() {
+#pragma unroll
+        for (int j = 0; j < N; ++j) by[j] = 0x1p60f;
+    }
+    // x: the tile's elements, [N][X] quads
+    template <int X, int DB> __device__ __forceinline__ void lift(f32x4 (&x)[N][X], f32x4 (&sums)[DB][N]) {
+        if constexpr (ON) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                float top = 0.f;
+#pragma unroll
+                for (int i = 0; i < X; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(x[j][i][e]));
+                top = lanes_max(top);
+                const bool grow = top * by[j] > 32768.f && top < INFINITY;
+                if (__any(grow)) {
+                    const float now = grow ? __builtin_amdgcn_ldexpf(1.f, 14 - __builtin_amdgcn_frexp_expf(top)) : by[j], to = now / by[j];
+                    by[j] = now;
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) sums[d][j] *= to;
+                }
+#pragma unroll
+                for (int i = 0; i < X; ++i) x[j][i] *= by[j];
+            }
+        }
+    }
+    __device__ __forceinline__ float back(int j) const { return ON ? 1.f / by[j] : 1.f; }
+};
+
+template <class T, int DP, int QB>
+__global__ __launch_bounds__(256, 2) void dq_kernel(AttentionArgs a, int tiles, int splits, int share) {
+    typedef Num<T> N;
+    typedef typename N::F F;
+    constexpr int KT = tile_rows<T, DP, 4>(), CH = DP / N::K, DB = DP / 16, PB = N::K / 16;
+    typedef Tile<T, DP, KT, 4> Load;
+    __shared__ __align__(1024) unsigned char smem[4 * Load::BYTES];
+    lds_byte* const lds = (lds_byte*)smem;
+    const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)lds);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lg = lane >> 4;
+    const Place at = place_of(a, tiles, splits);
+    Keys keys = keys_of<T>(a, at.b);
+    const int k_lo = at.split * share;
+    keys.end = min(keys.end, k_lo + share);
+    const int steps = keys.end > k_lo ? (keys.end - k_lo + KT - 1) / KT : 0;
+    const T* const K0 = (const T*)a.k + at.b * a.k_item + at.hk * a.k_head + k_lo * a.k_row;
+    const T* const V0 = (const T*)a.v + at.b * a.v_item + at.hk * a.v_head + k_lo * a.v_row;
+    const int r0 = (at.tile * 4 + wave) * 16 * QB;
+    F fq[QB][CH], fo[QB][CH];
+    float low[QB], delta[QB];
+#pragma unroll
+    for (int j = 0; j < QB; ++j) {
+        const int r = r0 + 16 * j + lr;
+        const bool there = r < a.rows;
+        int q, g;
+        query_of(a, r, q, g);
+        const int head = at.hk * a.per + g;
+        const T* p = (const T*)a.q + at.b * a.q_item + head * a.q_head + q * a.q_row;
+        const T* w = (const T*)a.d_out + (((int64_t)at.b * a.Lq + q) * a.HK * a.per + head) * a.D;
+#pragma unroll
+        for (int t = 0; t < CH; ++t) {
+            fq[j][t] = load_frag<T>(p, t * N::K + lg * N::V, a.D, there);
+            fo[j][t] = load_frag<T>(w, t * N::K + lg * N::V, a.D, there);
+        }
+        const f32x2 x = there ? *reinterpret_cast<const f32x2*>(a.aux + 2 * ((int64_t)at.bh * attention_aux_rows(a.rows) + r)) : f32x2{INFINITY, 0.f};
+        low[j] = x[0];
+        delta[j] = x[1];
+    }
+    Load load;
+    load.plan(wave, lane, a.D);
+    auto ask = [&](int t, uint64_t bits) {
+        const unsigned to = lds_at + (t & 1) * 2 * Load::BYTES;
+        load.ask(K0 + (int64_t)t * KT * a.k_row, a.k_row, bits, to, wave);
+        load.ask(V0 + (int64_t)t * KT * a.v_row, a.v_row, bits, to + Load::BYTES, wave);
+    };
+    const float c = a.scale * LOG2E;
+    f32x4 dq[DB][QB] = {};
+    Lifted<T, QB> lifted;
+    uint64_t bits = 0;
+    unsigned byte = 0;
+    if (steps) {
+        bits = keys.bits(k_lo, KT, keys.byte(k_lo, lane));
+        if (bits) ask(0, bits);
+        byte = keys.byte(k_lo + KT, lane);
+    }
+    for (int t = 0; t < steps; ++t) {
+        arrive_all();
+        uint64_t next = 0;
+        if (t + 1 < steps) {
+            next = keys.bits(k_lo + (t + 1) * KT, KT, byte);
+            if (next) ask(t + 1, next);
+            byte = keys.byte(k_lo + (t + 2) * KT, lane);
+        }
+        if (bits) {
+            lds_byte* const tk = lds + (t & 1) * 2 * Load::BYTES;
+            lds_byte* const tv = tk + Load::BYTES;
+            const bool some = bits != ~0ull >> (64 - KT);
+            const uint64_t mine = bits >> (4 * lg);
+#pragma unroll
+            for (int kk = 0; kk < KT / N::K; ++kk) {
+                f32x4 s[QB][PB] = {}, dp[QB][PB] = {};
+#pragma unroll
+                for (int h = 0; h < CH; ++h)
+#pragma unroll
+                    for (int i = 0; i < PB; ++i) {
+                        const F f = N::template straight<DP>(tk, N::K * kk + 16 * i + lr, h, lg);
+                        const F w = N::template straight<DP>(tv, N::K * kk + 16 * i + lr, h, lg);
+#pragma unroll
+                        for (int j = 0; j < QB; ++j) {
+                            s[j][i] = N::times(f, fq[j][h], s[j][i]);
+                            dp[j][i] = N::times(w, fo[j][h], dp[j][i]);
+                        }
+                    }
+#pragma unroll
+                for (int j = 0; j < QB; ++j)
+#pragma unroll
+                    for (int i = 0; i < PB; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float p = __builtin_amdgcn_exp2f(fmaf(s[j][i][e], c, -low[j]));
+                            dp[j][i][e] = p * (dp[j][i][e] - delta[j]);
+                            if (some) dp[j][i][e] = (mine >> (N::K * kk + 16 * i + e)) & 1 ? dp[j][i][e] : 0.f;
+                        }
+                lifted.lift(dp, dq);
+                F fs[QB];
+#pragma unroll
+                for (int j = 0; j < QB; ++j) fs[j] = N::pack(dp[j]);
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    const F f = N::template turned<DP>(tk, N::K * kk, d, lr, lg);
+#pragma unroll
+                    for (int j = 0; j < QB; ++j) dq[d][j] = N::times(f, fs[j], dq[d][j]);
+                }
+            }
+        }
+        bits = next;
+    }
+#pragma unroll
+    for (int j = 0; j < QB; ++j) {
+        const int r = r0 + 16 * j + lr;
+        if (r >= a.rows) continue;
+        int q, g;
+        query_of(a, r, q, g);
+        const int64_t row = (((int64_t)at.b * a.Lq + q) * a.HK * a.per + at.hk * a.per + g) * a.D;
+        const float by = lifted.back(j) * a.scale;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            if (16 * d + 4 * lg >= a.D) continue;
+            const float v[4] = {dq[d][j][0] * by, dq[d][j][1] * by, dq[d][j][2] * by, dq[d][j][3] * by};
+            if (splits > 1) store_some<float, 4>(a.part_q + (int64_t)at.split * a.B * a.Lq * a.HK * a.per * a.D + row + 16 * d + 4 * lg, v, 4);
+            else store_some<T, 4>((T*)a.d_q + row + 16 * d + 4 * lg, v, 4);
+        }
+    }
+}
+
+// A workgroup has 64 KB keys in its waves' registers and goes over the rows of the query heads that read them.  S = Q K^T here: a lane has four rows
+// of one key.  A key that does not count has sums of its own, which are not stored.
+template <class T, int DP, int KB>
+__global__ __launch_bounds__(256, 2) void dkv_kernel(AttentionArgs a, int tiles, int splits, int share) {
+    typedef Num<T> N;
+    typedef typename N::F F;
+    constexpr int RT = tile_rows<T, DP, 4>(), CH = DP / N::K, DB = DP / 16, PB = N::K / 16;
+    typedef Tile<T, DP, RT, 4> Load;
+    __shared__ __align__(1024) unsigned char smem[4 * Load::BYTES];
+    lds_byte* const lds = (lds_byte*)smem;
+    const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)lds);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lg = lane >> 4;
+    const Place at = place_of(a, tiles, splits);
+    const Keys keys = keys_of<T>(a, at.b);
+    const int k0 = (at.tile * 4 + wave) * 16 * KB, r_lo = at.split * share, r_hi = min(a.rows, r_lo + share);
+    F fk[KB][CH], fv[KB][CH];
+    bool counts[KB];
+    bool any = false;
+#pragma unroll
+    for (int j = 0; j < KB; ++j) {
+        const int k = k0 + 16 * j + lr;
+        counts[j] = k < keys.end && (!keys.mask || keys.mask[k]);
+        any |= counts[j];
+        const T* p = (const T*)a.k + at.b * a.k_item + at.hk * a.k_head + k * a.k_row;
+        const T* w = (const T*)a.v + at.b * a.v_item + at.hk * a.v_head + k * a.v_row;
+#pragma unroll
+        for (int t = 0; t < CH; ++t) {
+            fk[j][t] = load_frag<T>(p, t * N::K + lg * N::V, a.D, counts[j]);
+            fv[j][t] = load_frag<T>(w, t * N::K + lg * N::V, a.D, counts[j]);
+        }
+    }
+    const int steps = __syncthreads_or(any) ? (r_hi - r_lo + RT - 1) / RT : 0;
+    const T* const Q0 = (const T*)a.q + at.b * a.q_item + (int64_t)at.hk * a.per * a.q_head;
+    const T* const O0 = (const T*)a.d_out + (int64_t)at.b * a.Lq * a.HK * a.per * a.D + (int64_t)at.hk * a.per * a.D;
+    const int64_t o_row = (int64_t)a.HK * a.per * a.D;
+    Load load;
+    load.plan(wave, lane, a.D);
+    auto ask = [&](int t) {
+        const unsigned to = lds_at + (t & 1) * 2 * Load::BYTES;
+        const int r0 = r_lo + t * RT;
+        int q0, g0;
+        query_of(a, r0, q0, g0);
+        const i32x4 rq = Load::resource(Q0 + q0 * a.q_row), ro = Load::resource(O0 + q0 * o_row);
+#pragma unroll
+        for (int i = 0; i < Load::PIECES; ++i) {
+            const int r = r0 + load.row[i];
+            int q, g;
+            query_of(a, r, q, g);
+            const bool there = r < r_hi && load.col[i] != PAST;
+            const int es = sizeof(T);
+            dma16(rq, to + (i * 4 + wave) * 1024, there ? (unsigned)(((q - q0) * (int)a.q_row + g * (int)a.q_head) * es) + load.col[i] : PAST);
+            dma16(ro, to + Load::BYTES + (i * 4 + wave) * 1024,
+                  there ? (unsigned)(((q - q0) * (int)o_row + g * a.D) * es) + load.col[i] : PAST);
+        }
+    };
+    const float c = a.scale * LOG2E;
+    const float* const aux = a.aux + 2 * (int64_t)at.bh * attention_aux_rows(a.rows);
+    f32x4 dk[DB][KB] = {}, dv[DB][KB] = {};
+    Lifted<T, KB> lifted;
+    if (steps) ask(0);
+    for (int t = 0; t < steps; ++t) {
+        arrive_all();
+        if (t + 1 < steps) ask(t + 1);
+        lds_byte* const tq = lds + (t & 1) * 2 * Load::BYTES;
+        lds_byte* const to = tq + Load::BYTES;
+#pragma unroll
+        for (int kk = 0; kk < RT / N::K; ++kk) {
+            f32x4 low[PB], delta[PB];
+#pragma unroll
+            for (int i = 0; i < PB; ++i) {               // share and tiles are multiples of 16, and so is the array's length
+                const int r = r_lo + t * RT + N::K * kk + 16 * i + 4 * lg;
+                f32x4 x = {INFINITY, 0.f, INFINITY, 0.f}, y = x;
+                if (r < r_hi) {
+                    x = *reinterpret_cast<const f32x4*>(aux + 2 * r);
+                    y = *reinterpret_cast<const f32x4*>(aux + 2 * r + 4);
+                }
+                low[i] = f32x4{x[0], x[2], y[0], y[2]};
+                delta[i] = f32x4{x[1], x[3], y[1], y[3]};
+            }
+            f32x4 s[KB][PB] = {}, dp[KB][PB] = {};
+#pragma unroll
+            for (int h = 0; h < CH; ++h)
+#pragma unroll
+                for (int i = 0; i < PB; ++i) {
+                    const F f = N::template straight<DP>(tq, N::K * kk + 16 * i + lr, h, lg);
+                    const F w = N::template straight<DP>(to, N::K * kk + 16 * i + lr, h, lg);
+#pragma unroll
+                    for (int j = 0; j < KB; ++j) {
+                        s[j][i] = N::times(f, fk[j][h], s[j][i]);
+                        dp[j][i] = N::times(w, fv[j][h], dp[j][i]);
+                    }
+                }
+            F fp[KB], fs[KB];
+#pragma unroll
+            for (int j = 0; j < KB; ++j) {
+#pragma unroll
+                for (int i = 0; i < PB; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float p = __builtin_amdgcn_exp2f(fmaf(s[j][i][e], c, -low[i][e]));
+                        dp[j][i][e] = p * (dp[j][i][e] - delta[i][e]);
+                        s[j][i][e] = LIFT<T> ? p * 16384.f : p;
+                    }
+                fp[j] = N::pack(s[j]);
+            }
+            lifted.lift(dp, dk);
+#pragma unroll
+            for (int j = 0; j < KB; ++j) fs[j] = N::pack(dp[j]);
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                const F f = N::template turned<DP>(to, N::K * kk, d, lr, lg);
+                const F w = N::template turned<DP>(tq, N::K * kk, d, lr, lg);
+#pragma unroll
+                for (int j = 0; j < KB; ++j) {
+                    dv[d][j] = N::times(f, fp[j], dv[d][j]);
+                    dk[d][j] = N::times(w, fs[j], dk[d][j]);
+                }
+            }
+        }
+    }
+    const int64_t all = (int64_t)a.B * a.Lk * a.HK * a.D;
+#pragma unroll
+    for (int j = 0; j < KB; ++j) {
+        const int k = k0 + 16 * j + lr;
+        if (k >= a.Lk) continue;
+        const int64_t row = (((int64_t)at.b * a.Lk + k) * a.HK + at.hk) * a.D;
+        const float bk = lifted.back(j) * a.scale, bv = LIFT<T> ? 1.f / 16384.f : 1.f;
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            if (16 * d + 4 * lg >= a.D) continue;
+            float x[4], y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                x[e] = counts[j] ? dk[d][j][e] * bk : 0.f;
+                y[e] = counts[j] ? dv[d][j][e] * bv : 0.f;
+            }
+            const int64_t to = row + 16 * d + 4 * lg;
+            if (splits > 1) {
+                store_some<float, 4>(a.part_k + at.split * all + to, x, 4);
+                store_some<float, 4>(a.part_v + at.split * all + to, y, 4);
+            } else {
+                store_some<T, 4>((T*)a.d_k + to, x, 4);
+                store_some<T, 4>((T*)a.d_v + to, y, 4);
+            }
+        }
+    }
+}
+
+// The splits' parts of a gradient, added in their order.
+template <class T>
+__global__ __launch_bounds__(256) void sum_kernel(const float* one, const float* two, T* to_one, T* to_two, int64_t quads, int splits) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= quads) return;
+    const float* p = (blockIdx.y ? two : one) + 4 * i;
+    f32x4 x = {};
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) x += *reinterpret_cast<const f32x4*>(p + s * quads * 4);
+    const float v[4] = {x[0], x[1], x[2], x[3]};
+    store_some<T, 4>((blockIdx.y ? to_two : to_one) + 4 * i, v, 4);
+}
+
+template <class T, int DP>
+hipError_t forward(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) {
+    const dim3 grid(p.tiles * p.splits * a.B * a.HK);
+    if (p.waves == 1) hipLaunchKernelGGL((forward_kernel<T, DP, 1, 1>), grid, dim3(64), 0, s, a, p.tiles, p.splits, p.share);
+    else if (p.blocks == 1) hipLaunchKernelGGL((forward_kernel<T, DP, 4, 1>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
+    else if constexpr (DP * sizeof(T) <= 256) hipLaunchKernelGGL((forward_kernel<T, DP, 4, 2>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
+    if (p.splits > 1) hipLaunchKernelGGL(forward_join_kernel<T>, dim3(cdiv((int64_t)a.B * a.HK * a.rows, 16)), dim3(256), 0, s, a, p.splits);
+    return hipGetLastError();
+}
+template <class T, int DP>
+hipError_t backward(const AttentionArgs& a, const AttentionPlan& pq, const AttentionPlan& pk, hipStream_t s) {
+    const int aux_rows = attention_aux_rows(a.rows);
+    hipLaunchKernelGGL(delta_kernel<T>, dim3(cdiv((int64_t)a.B * a.HK * aux_rows, 16)), dim3(256), 0, s, a, aux_rows);
+    constexpr bool TWO = DP * sizeof(T) <= 256;
+    if (a.d_q) {
+        const dim3 grid(pq.tiles * pq.splits * a.B * a.HK);
+        if (pq.blocks == 1) hipLaunchKernelGGL((dq_kernel<T, DP, 1>), grid, dim3(256), 0, s, a, pq.tiles, pq.splits, pq.share);
+        else if constexpr (TWO) hipLaunchKernelGGL((dq_kernel<T, DP, 2>), grid, dim3(256), 0, s, a, pq.tiles, pq.splits, pq.share);
+        if (pq.splits > 1) {
+            const int64_t quads = (int64_t)a.B * a.Lq * a.HK * a.per * a.D / 4;
+            hipLaunchKernelGGL(sum_kernel<T>, dim3(cdiv(quads, 256)), dim3(256), 0, s, a.part_q, a.part_q, (T*)a.d_q, (T*)a.d_q, quads, pq.splits);
+        }
+    }
+    if (a.d_k) {
+        const dim3 grid(pk.tiles * pk.splits * a.B * a.HK);
+        if (pk.blocks == 1) hipLaunchKernelGGL((dkv_kernel<T, DP, 1>), grid, dim3(256), 0, s, a, pk.tiles, pk.splits, pk.share);
+        else if constexpr (TWO) hipLaunchKernelGGL((dkv_kernel<T, DP, 2>), grid, dim3(256), 0, s, a, pk.tiles, pk.splits, pk.share);
+        if (pk.splits > 1) {
+            const int64_t quads = (int64_t)a.B * a.Lk * a.HK * a.D / 4;
+            hipLaunchKernelGGL(sum_kernel<T>, dim3(cdiv(quads, 256), 2), dim3(256), 0, s, a.part_k, a.part_v, (T*)a.d_k, (T*)a.d_v, quads, pk.splits);
+        }
+    }
+    return hipGetLastError();
+}
+#define BY_LENGTH(f, T, ...) a.D <= 32 ? f<T, 32>(__VA_ARGS__) : a.D <= 64 ? f<T, 64>(__VA_ARGS__) : a.D <= 128 ? f<T, 128>(__VA_ARGS__) : f<T, 256>(__VA_ARGS__)
+
+}  // namespace
+
+#if CORR_ATTENTION_TYPE == 0
+hipError_t launch_attention_f32(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) { return BY_LENGTH(forward, float, a, p, s); }
+hipError_t launch_attention_backward_f32(const AttentionArgs& a, const AttentionPlan& pq, const AttentionPlan& pk, hipStream_t s) { return BY_LENGTH(backward, float, a, pq, pk, s); }
+
+// Rows of a workgroup: 128 (two blocks of 16 a wave) where that gives one to every compute unit, else 64, and 16 in one wave where there are no more.
+// Shares of the long axis where there are still too few workgroups: as many as fill the chip, of four tiles at least.
+AttentionPlan attention_plan(corr_dtype t, AttentionPass pass, int B, int Lq, int Lk, int HK, int per, int D) {
+    const int pad = D <= 32 ? 32 : D <= 64 ? 64 : D <= 128 ? 128 : 256, es = t == CORR_TYPE_F32 ? 4 : 2;
+    const int rows = Lq * per, along = pass == PASS_DKV ? Lk : rows, over = pass == PASS_DKV ? rows : Lk;
+    AttentionPlan p;
+    p.waves = pass == PASS_FORWARD && along <= 16 ? 1 : 4;
+    p.blocks = p.waves == 4 && pad * es <= 256 && (int64_t)cdiv(along, 128) * B * HK >= 256 ? 2 : 1;
+    p.tile = 16 * p.waves * p.blocks;
+    p.tiles = cdiv(along, p.tile);
+    const int64_t groups = (int64_t)p.tiles * B * HK, want = p.waves == 1 ? 1280 : 512;
+    int64_t splits = groups < want / 2 ? want / (groups ? groups : 1) : 1;
+    const int most = over > 256 ? cdiv(over, 256) : 1;
+    if (splits > most) splits = most;
+    p.share = over > 0 ? (cdiv(over, splits) + 63) & ~63 : 64;
+    p.splits = over > 0 ? cdiv(over, p.share) : 1;
+    return p;
+}
+#elif CORR_ATTENTION_TYPE == 1
+hipError_t launch_attention_bf16(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) { return BY_LENGTH(forward, __bf16, a, p, s); }
+hipError_t launch_attention_backward_bf16(const AttentionArgs& a, const AttentionPlan& pq, const AttentionPlan& pk, hipStream_t s) { return BY_LENGTH(backward, __bf16, a, pq, pk, s); }
+#else
+hipError_t launch_attention_f16(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) { return BY_LENGTH(forward, _Float16, a, p, s); }
+hipError_t launch_attention_backward_f16(const AttentionArgs& a, const AttentionPlan& pq, const AttentionPlan& pk, hipStream_t s) { return BY_LENGTH(backward, _Float16, a, pq, pk, s); }
+#endif

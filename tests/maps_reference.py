@@ -1,0 +1,110 @@
+"""The operators on maps (include/corr.h, "Maps") in float64, and how far the library's results may be from them.
+
+U, EPS and `rounded` are rows_reference's: half a step of a type, 2^-24 an fp32 operation.  A sum of n products in any order is off by
+(2 n + 8) EPS times the sum of the magnitudes (the matrix instruction may cut where it aligns its terms).
+
+attention.  A score s = scale <q, k> is off by (2 D + 12) EPS S, S the magnitudes' sum.  A weight e^(s - m) is formed as 2^(s c - m c), c = scale log2 e: the
+    roundings of c, m c, the exponent and the power are 8 EPS (|s| + |m| + 1), relative; m's own error is the row's and cancels.  Sums are rescaled
+    when the maximum grows, at most once a tile of 16 keys: 2 EPS each, and the power's 4 EPS.  So a weight is off by w = (2 D + 12) EPS S +
+    EPS (8 (|s| + |m| + 1) + 6 (Lk / 16 + 1)), relative, and as an operand by U (16-bit types) more.  out = sum p v with sum p = 1:
+    sum p (w + U) |v| + |out| sum p w + (4 Lk + 16) EPS sum p |v|; lse: sum p w + (2 Lk + 8) EPS + 8 EPS |lse|.
+gradient.  P = e^(s - lse) with the lse that was stored (off by e_l): relative error w + e_l + 8 EPS |lse|.  dP: (2 D + 8) EPS sum |dO v|.  delta = sum dO out
+    with the out that was stored: its bound times |dO|, and (2 D + 8) EPS sum |dO out|.  dS = P (dP - delta): P (rel |dP - delta| + e_dP +
+    e_delta) + 4 EPS |P (dP - delta)|, and U |dS| as an operand.  The three products are sums of Lk or rows terms.  fp16 keeps weights to 2^-39 of
+    the largest and dS to 2^-39 of the row's (key's) largest: FLOOR.
+    The power and the matrix instructions take values below fp32's normal ones (2^-126) as zero: a weight may be off by LEAST = 2^-126, dS by that
+    times |dP - delta| and once more for its own product, and each term of a sum by LEAST.
+"""
+import torch
+
+from rows_reference import EPS, TINY, U, check, rounded  # noqa: F401  (for the tests)
+
+F32 = torch.float32
+FLOOR = 2.0 ** -38
+LEAST = 2.0 ** -126
+
+
+def heads_of(x, per):
+    """[B, L, HK, D] as float64 [B, HK * per, L, D]"""
+    return x.double().cpu().transpose(1, 2).repeat_interleave(per, 1)
+
+
+def valid_keys(B, Lk, k_lengths=None, key_mask=None):
+    keep = torch.ones(B, Lk, dtype=torch.bool)
+    if k_lengths is not None:
+        keep &= torch.arange(Lk) < k_lengths.cpu()[:, None]
+    if key_mask is not None:
+        keep &= key_mask.cpu() != 0
+    return keep
+
+
+class Attention:
+    def __init__(self, q, k, v, scale, k_lengths=None, key_mask=None):
+        self.T = q.dtype
+        (B, Lq, H, D), Lk = q.shape, k.shape[1]
+        self.per, self.scale = H // k.shape[2], scale
+        self.lp = U[self.T] if self.T != F32 else 0.0
+        keep = valid_keys(B, Lk, k_lengths, key_mask)[:, None, None]
+        clean = lambda t: torch.where(keep[:, 0, 0, :, None, None], t.cpu(), torch.zeros((), dtype=t.dtype))  # noqa: E731
+        self.q, self.k, self.v = q.double().cpu().transpose(1, 2), heads_of(clean(k), self.per), heads_of(clean(v), self.per)
+        s = scale * self.q @ self.k.transpose(2, 3)
+        S = scale * self.q.abs() @ self.k.abs().transpose(2, 3)
+        low = torch.full((), -float("inf"), dtype=torch.float64)
+        s = torch.where(keep, s, low)
+        if Lk:
+            top = s.max(3, keepdim=True).values
+        else:
+            top = torch.full(s.shape[:3] + (1,), -float("inf"), dtype=torch.float64)
+        top = torch.where(top == low, 0.0, top)
+        p = torch.exp(s - top)
+        total = p.sum(3, keepdim=True)
+        self.lse = (total.log() + top)[..., 0]
+        self.p = p / torch.where(total == 0, 1.0, total)
+        size = torch.where(keep, s.abs(), 0.0)
+        self.w = (2 * D + 12) * EPS * S + EPS * (8 * (size + top.abs() + 1) + 6 * (Lk / 16 + 1))
+        self.s_size = size
+        self.out = self.p @ self.v
+        av = self.v.abs()
+        pw = (self.p * self.w).sum(3, keepdim=True)
+        e = (self.p * (self.w + self.lp) + LEAST) @ av + self.out.abs() * pw + (4 * Lk + 16) * EPS * (self.p @ av) + Lk * LEAST
+        if self.T == torch.float16:
+            e = e + FLOOR * keep.double().expand_as(self.p) @ av
+        self.e_out = 1.01 * e + rounded(self.out, self.T)
+        finite = torch.where(self.lse == low, 0.0, self.lse)
+        self.finite = finite[..., None]
+        self.e_lse = 1.01 * (pw[..., 0] + (2 * Lk + 8) * EPS + 8 * EPS * finite.abs()) + rounded(finite, F32)
+
+    def forward(self):
+        """(out, bound) as [B, Lq, H, D], (lse, bound) as [B, H, Lq]"""
+        return (self.out.transpose(1, 2), self.e_out.transpose(1, 2)), (self.lse, self.e_lse)
+
+    def backward(self, d_out):
+        """((d_q, bound), (d_k, bound), (d_v, bound)) laid out as the arguments"""
+        g = d_out.double().cpu().transpose(1, 2)
+        D, Lq, Lk, scale = g.shape[3], g.shape[2], self.k.shape[2], self.scale
+        rel = self.w + self.e_lse[..., None] + 8 * EPS * self.finite.abs()
+        dp = g @ self.v.transpose(2, 3)
+        delta = (g * self.out).sum(3, keepdim=True)
+        e_dp = (2 * D + 8) * EPS * (g.abs() @ self.v.abs().transpose(2, 3))
+        e_delta = (g.abs() * self.e_out).sum(3, keepdim=True) + (2 * D + 8) * EPS * (g.abs() * self.out.abs()).sum(3, keepdim=True)
+        ds = self.p * (dp - delta)
+        e_ds = self.p * (rel * (dp - delta).abs() + e_dp + e_delta) * (1 + rel) + 4 * EPS * ds.abs()
+        e_ds = e_ds + self.lp * (ds.abs() + e_ds) + LEAST * (1 + (dp - delta).abs())
+        e_p = self.p * (rel + self.lp) + LEAST
+        if self.T == torch.float16 and Lk and Lq:
+            size = (ds.abs() + e_ds)
+            e_ds = e_ds + FLOOR * torch.maximum(size.max(3, keepdim=True).values, size.max(2, keepdim=True).values)
+            e_p = e_p + FLOOR
+
+        def product(a, b, ea, terms, by):
+            v = by * (a @ b)
+            bound = by * (ea @ b.abs() + (4 * terms + 16) * EPS * ((a.abs() + ea) @ b.abs()) + terms * LEAST)
+            return v, 1.01 * bound + 4 * EPS * v.abs()
+
+        def shared(t):                                  # [B, H, Lk, D] summed over the heads that share a key head
+            return t.unflatten(1, (-1, self.per)).sum(2).transpose(1, 2)
+        dq, eq = product(ds, self.k, e_ds, Lk, scale)
+        n = Lq * self.per
+        dk, ek = (shared(t) for t in product(ds.transpose(2, 3), self.q, e_ds.transpose(2, 3), n, scale))
+        dv, ev = (shared(t) for t in product(self.p.transpose(2, 3), g, e_p.transpose(2, 3), n, 1.0))
+        return ((dq.transpose(1, 2), (eq + rounded(dq, self.T)).transpose(1, 2)), (dk, ek + rounded(dk, self.T)), (dv, ev + rounded(dv, self.T)))

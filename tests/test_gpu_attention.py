@@ -1,0 +1,294 @@
+"""corr_attention and its gradient on the GPU against float64: sizes around their tiles, head layouts, strides, lengths and masks, values that are
+not finite, far exponents, graphs and streams.  The bounds are derived in maps_reference.py."""
+import itertools
+
+import pytest
+
+import maps_reference as ref
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+TYPES = (F32, BF16, F16)
+
+
+def _b():
+    from paper_2505_16942_amd import binding
+    return binding
+
+
+def _gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return lambda *shape, sigma=1.0, dtype=F32: (torch.randn(shape, generator=g) * sigma).to(dtype).cuda()
+
+
+# (B, Lq, Lk, H, HK, D): one of everything; one row, few rows, shared heads; a tile and its neighbours; every padded length of a head; many splits
+SIZES = [(1, 1, 1, 1, 1, 8), (1, 1, 5, 2, 1, 32), (2, 1, 1000, 8, 2, 128), (1, 3, 70, 4, 4, 40), (1, 16, 64, 1, 1, 64), (2, 17, 65, 3, 1, 64),
+         (1, 64, 63, 2, 2, 128), (1, 65, 129, 6, 2, 96), (3, 5, 33, 1, 1, 256), (1, 130, 31, 1, 1, 256), (1, 40, 700, 2, 1, 160), (1, 700, 40, 4, 2, 72),
+         (2, 129, 300, 1, 1, 32), (1, 1, 3001, 1, 1, 64), (1, 2, 2, 128, 1, 16), (1, 257, 1, 2, 2, 24)]
+
+
+def _case(size, dtype, seed, sigma=2.0):
+    B, Lq, Lk, H, HK, D = size
+    new = _gen(seed)
+    return new(B, Lq, H, D, sigma=sigma, dtype=dtype), new(B, Lk, HK, D, dtype=dtype), new(B, Lk, HK, D, dtype=dtype), new(B, Lq, H, D, sigma=0.3, dtype=dtype)
+
+
+def _run(q, k, v, g, scale=None, **kw):
+    b = _b()
+    B, Lq, H, D = q.shape
+    lse = torch.full((B, H, Lq), float("nan"), device="cuda")
+    out = b.corr_attention(q, k, v, scale=scale, lse=lse, **kw)
+    grads = b.corr_attention_backward(q, k, v, out, lse, g, scale=scale, **kw)
+    return out, lse, grads
+
+
+def _compare(what, q, k, v, g, scale=None, **kw):
+    out, lse, grads = _run(q, k, v, g, scale, **kw)
+    want = ref.Attention(q, k, v, q.shape[3] ** -0.5 if scale is None else scale, **kw)
+    (wo, eo), (wl, el) = want.forward()
+    ref.check(what + " out", out, wo, eo)
+    empty = wl == -float("inf")
+    assert torch.equal(lse.cpu() == -float("inf"), empty), what
+    ref.check(what + " lse", torch.where(empty, 0.0, lse.cpu().double()), torch.where(empty, 0.0, wl), el)
+    for name, got, (w, e) in zip(("d_q", "d_k", "d_v"), grads, want.backward(g)):
+        assert got.dtype == q.dtype
+        ref.check("%s %s" % (what, name), got, w, e)
+    return out, lse, grads
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("size", SIZES)
+def test_attention(size, dtype):
+    b = _b()
+    q, k, v, g = _case(size, dtype, sum(size))
+    out, lse, grads = _compare("%s %s" % (size, dtype), q, k, v, g)
+    again = _run(q, k, v, g)
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1]) and all(torch.equal(x, y) for x, y in zip(grads, again[2])), "two calls differ"
+    assert torch.equal(out, b.corr_attention(q, k, v)), "without lse"
+    for want_q, want_kv in itertools.product((False, True), repeat=2):
+        part = b.corr_attention_backward(q, k, v, out, lse, g, want_q=want_q, want_kv=want_kv)
+        for x, y, wanted in zip(part, grads, (want_q, want_kv, want_kv)):
+            assert (x is None) if not wanted else torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_attention_fills_the_chip(dtype):
+    """Enough workgroups that nothing is split and two blocks of rows (keys) share a wave: some rows, and sums over all."""
+    B, L, H, D = 4, 1030, 8, 64
+    q, k, v, g = _case((B, L, L, H, H, D), dtype, 3)
+    out, lse, (dq, dk, dv) = _run(q, k, v, g)
+    for item, head in ((0, 0), (3, 7)):
+        cut = lambda t: t[item:item + 1, :, head:head + 1]  # noqa: E731
+        want = ref.Attention(cut(q), cut(k), cut(v), D ** -0.5)
+        (wo, eo), (wl, el) = want.forward()
+        ref.check("out", cut(out), wo, eo)
+        ref.check("lse", lse[item:item + 1, head:head + 1], wl, el)
+        for name, got, (w, e) in zip(("d_q", "d_k", "d_v"), (dq, dk, dv), want.backward(cut(g))):
+            ref.check(name, cut(got), w, e)
+    D = 128
+    q, k, v, g = _case((2, 2060, 1100, 8, 8, D), dtype, 4)
+    kw = dict(k_lengths=torch.tensor([1100, 801], dtype=torch.int32, device="cuda"))
+    out, lse, (dq, dk, dv) = _run(q, k, v, g, **kw)
+    cut = lambda t: t[1:, :, 5:6]  # noqa: E731
+    want = ref.Attention(cut(q), cut(k), cut(v), D ** -0.5, k_lengths=kw["k_lengths"][1:])
+    ref.check("out", cut(out), *want.forward()[0])
+    for name, got, (w, e) in zip(("d_q", "d_k", "d_v"), (dq, dk, dv), want.backward(cut(g))):
+        ref.check(name, cut(got), w, e)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("size", [(4, 9, 200, 2, 1, 64), (3, 70, 131, 2, 2, 128), (3, 1, 2000, 4, 1, 32), (2, 20, 90, 1, 1, 256)])
+def test_lengths_and_masks(size, dtype):
+    """Lengths from none to all (and past them), masks with holes, whole tiles and whole rows of them; what lies there may be anything."""
+    B, Lq, Lk, H, HK, D = size
+    q, k, v, g = _case(size, dtype, 11)
+    lengths = torch.tensor([Lk + 7, 0, Lk // 2 + 1, 1][:B], dtype=torch.int32, device="cuda")
+    gen = torch.Generator().manual_seed(2)
+    mask = (torch.rand(B, Lk, generator=gen) < 0.6).to(torch.uint8) * 3
+    mask[0, 64:128] = 0
+    mask[B - 1] = 0
+    mask[B - 1, Lk - 1] = 1
+    mask = mask.cuda()
+    for kw in (dict(k_lengths=lengths), dict(key_mask=mask), dict(k_lengths=lengths, key_mask=mask), dict(key_mask=mask != 0),
+               dict(key_mask=torch.zeros_like(mask))):
+        clean = _compare(str(kw.keys()), q, k, v, g, **kw)
+        keep = ref.valid_keys(B, Lk, **kw).cuda()[:, :, None, None]
+        for junk in (float("nan"), float("inf"), -float("inf")):
+            bad = torch.full((), junk, dtype=dtype, device="cuda")
+            dirty = _run(q, torch.where(keep, k, bad), torch.where(keep, v, bad), g, **kw)
+            assert torch.equal(clean[0], dirty[0]) and torch.equal(clean[1], dirty[1]), junk
+            assert all(torch.equal(x, y) for x, y in zip(clean[2], dirty[2])), junk
+        for t in clean[2][1:]:
+            assert not t[~keep[:, :, 0, 0]].any(), "keys that do not count"
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_layouts(dtype):
+    """Columns of one projection, heads first, rows apart, items that share their keys: the same bits as dense copies, and nothing else read."""
+    B, Lq, Lk, H, D = 2, 37, 83, 3, 40
+    new = _gen(5)
+    qkv = new(B, Lk, 3, H, D, dtype=dtype)
+    g = new(B, Lk, H, D, dtype=dtype)
+    q, k, v = qkv.unbind(2)
+    want = _run(q.contiguous(), k.contiguous(), v.contiguous(), g)
+    got = _run(q, k, v, g)
+    assert torch.equal(want[0], got[0]) and all(torch.equal(x, y) for x, y in zip(want[2], got[2]))
+    q = new(B, Lq, H, D, dtype=dtype)
+    g = new(B, Lq, H, D, dtype=dtype)
+    want = _run(q, k.contiguous(), v.contiguous(), g)
+    first = torch.full((B, H, Lk + 3, D + 8), float("nan"), dtype=dtype, device="cuda")
+    first[:, :, :Lk, :D] = k.transpose(1, 2)
+    apart = torch.full((B, 2 * Lq, H + 1, D), float("nan"), dtype=dtype, device="cuda")
+    apart[:, ::2, 1:] = q
+    got = _run(apart[:, ::2, 1:], first[:, :, :Lk, :D].transpose(1, 2), v, g)
+    assert torch.equal(want[0], got[0]) and all(torch.equal(x, y) for x, y in zip(want[2], got[2]))
+    one_k, one_v = k[:1].contiguous(), v[:1].contiguous()
+    want = _run(q, one_k.repeat(B, 1, 1, 1), one_v.repeat(B, 1, 1, 1), g)
+    got = _run(q, one_k.expand(B, -1, -1, -1), one_v.expand(B, -1, -1, -1), g)
+    assert torch.equal(want[0], got[0]) and all(torch.equal(x, y) for x, y in zip(want[2], got[2]))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_far_scores(dtype):
+    """Scores whose exponentials overflow or vanish in fp32, growing and falling along the keys, and equal ones."""
+    new = _gen(6)
+    for sign in (1.0, -1.0):
+        Lk, D = 400, 32
+        q = torch.zeros(1, 20, 1, D, dtype=dtype, device="cuda")
+        q[..., 0] = 16.0
+        k = torch.zeros(1, Lk, 1, D, dtype=dtype, device="cuda")
+        k[0, :, 0, 0] = (sign * torch.linspace(-40, 40, Lk)).to(dtype).cuda()
+        v, g = new(1, Lk, 1, D, dtype=dtype), new(1, 20, 1, D, dtype=dtype)
+        _compare("far %g" % sign, q, k, v, g, scale=1.0)
+    same = torch.full((1, 9000, 1, D), 0.5, dtype=dtype, device="cuda")
+    v = new(1, 9000, 1, D, dtype=dtype)
+    _compare("equal", q[:, :3], same, v, g[:, :3], scale=2.0)
+    # one key far above many: their weights are small and together are not
+    k = torch.zeros(1, 9000, 1, D, dtype=dtype, device="cuda")
+    k[0, 77, 0, 0] = 1.0
+    _compare("one and many", q[:, :3], k, v, g[:, :3], scale=1.0)
+
+
+def test_half_gradients_keep_small_and_large_values():
+    """fp16: gradients of 1e-4 and of 1e3 beside each other, far from what dS itself would hold."""
+    q, k, v, g = _case((1, 50, 300, 1, 1, 64), F16, 8)
+    for sigma in (1e-4, 1.0, 300.0):
+        _compare("%g" % sigma, q, k, v, (g * sigma).to(F16))
+    ramp = torch.logspace(-4, 2, 50, device="cuda").view(1, 50, 1, 1)
+    for g2 in (g * ramp, g * ramp.flip(1)):
+        _compare("ramp", q, k, v, g2.to(F16))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_values_that_are_not_finite(dtype):
+    """A NaN in a row of q reaches that row alone; in a key or value that counts, every row of its item and head; an infinite score is NaN."""
+    q, k, v, g = _case((2, 40, 150, 2, 2, 64), dtype, 9)
+    clean = _b().corr_attention(q, k, v)
+    q2 = q.clone()
+    q2[1, 7, 1, 3] = float("nan")
+    out = _b().corr_attention(q2, k, v)
+    assert out[1, 7, 1].isnan().all()
+    out[1, 7, 1] = clean[1, 7, 1]
+    assert torch.equal(out, clean)
+    for where in ("k", "v"):
+        k2, v2 = k.clone(), v.clone()
+        (k2 if where == "k" else v2)[0, 149, 1, 5] = float("nan")
+        out = _b().corr_attention(q, k2, v2)
+        assert out[0, :, 1, 5].isnan().all() and torch.equal(out[0, :, 0], clean[0, :, 0]) and torch.equal(out[1], clean[1])
+    q3, k3 = q.clone(), k.clone()
+    q3[0, 0, 0], k3[0, 100, 0] = 0, 0
+    q3[0, 0, 0, 0], k3[0, 100, 0, 0] = float("inf"), 1.0
+    assert _b().corr_attention(q3, k3, v)[0, 0, 0].isnan().all()
+
+
+def test_differences():
+    """The gradient against differences of the forward call in fp32: what the quotient itself is off by is computed in float64."""
+    new = _gen(21)
+    q, k, v = new(1, 9, 2, 32), new(1, 21, 1, 32), new(1, 21, 1, 32)
+    w = new(1, 9, 2, 32)
+    lengths = torch.tensor([18], dtype=torch.int32, device="cuda")
+    _, _, grads = _run(q, k, v, w, k_lengths=lengths)
+    h = 2.0 ** -6
+    for i, t in enumerate((q, k, v)):
+        step = new(*t.shape)
+        sides, exact, noise = [], [], 0.0
+        for sign in (1.0, -1.0):
+            args = [q, k, v]
+            args[i] = t + sign * h * step
+            sides.append((_b().corr_attention(*args, k_lengths=lengths).double() * w.double()).sum().item())
+            wo, eo = ref.Attention(*args, 32 ** -0.5, k_lengths=lengths).forward()[0]
+            exact.append((wo * w.double().cpu()).sum().item())
+            noise += (eo * w.double().cpu().abs()).sum().item()
+        along, e = ref.Attention(q, k, v, 32 ** -0.5, k_lengths=lengths).backward(w)[i]
+        true = (along * step.double().cpu()).sum().item()
+        got = (grads[i].double() * step.double()).sum().item()
+        quotient = (sides[0] - sides[1]) / (2 * h)
+        # t + h step is rounded to fp32 in both, so that the float64 quotient is of the same points
+        truncation = abs((exact[0] - exact[1]) / (2 * h) - true)
+        assert abs(quotient - got) <= truncation + noise / (2 * h) + (e * step.double().cpu().abs()).sum().item()
+        assert truncation < 0.05 * abs(true) + 0.05
+
+
+@pytest.mark.parametrize("dtype", (F32, F16))
+def test_graphs_and_streams(dtype):
+    """Captured with a workspace each, replayed between eager calls, and on a stream of its own."""
+    b = _b()
+    size = (2, 5, 900, 4, 2, 64)
+    q, k, v, g = _case(size, dtype, 13)
+    B, Lq, Lk, H, HK, D = size
+    lengths = torch.tensor([900, 333], dtype=torch.int32, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty(B, H, Lq, device="cuda")
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    wf = torch.empty(b.corr_attention_workspace_bytes(dtype, *size), dtype=torch.uint8, device="cuda")
+    wb = torch.empty(b.corr_attention_backward_workspace_bytes(dtype, *size), dtype=torch.uint8, device="cuda")
+    assert wf.numel() and wb.numel()
+
+    def step():
+        b.corr_attention(q, k, v, k_lengths=lengths, out=out, lse=lse, workspace=wf)
+        b.corr_attention_backward(q, k, v, out, lse, g, k_lengths=lengths, d_q=dq, d_k=dk, d_v=dv, workspace=wb)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for turn in range(4):
+        q.copy_(_gen(50 + turn)(*q.shape, dtype=dtype))
+        lengths.copy_(torch.tensor([900 - 100 * turn, 333 * (turn % 2)], dtype=torch.int32))
+        want = _run(q, k, v, g, k_lengths=lengths)
+        for t in (out, lse, dq, dk, dv, wf, wb):
+            t.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+        assert all(torch.equal(x, y) for x, y in zip((dq, dk, dv), want[2])), turn
+
+
+def test_nothing_to_do():
+    b = _b()
+    for B, Lq, Lk in ((0, 5, 5), (2, 0, 5), (2, 5, 0)):
+        q, k = torch.randn(B, Lq, 2, 32, device="cuda"), torch.randn(B, Lk, 2, 32, device="cuda")
+        lse = torch.full((B, 2, Lq), 3.0, device="cuda")
+        out = b.corr_attention(q, k, k, lse=lse)
+        assert out.shape == q.shape and not out.any() and (lse == -float("inf")).all()
+        grads = b.corr_attention_backward(q, k, k, out, lse, torch.ones_like(q))
+        assert [t.shape for t in grads] == [q.shape, k.shape, k.shape] and not any(t.any() for t in grads)
+
+
+def test_far_offsets():
+    """Keys whose offsets pass 2^32 bytes: a cache of rows far apart, one item behind another."""
+    B, Lk, HK, D = 3, 1300, 1, 64
+    store = torch.empty(3 << 30, dtype=BF16, device="cuda")
+    k = store.as_strided((B, Lk, HK, D), ((1 << 30) + 64, 1 << 19, D, 1))
+    v = store.as_strided((B, Lk, HK, D), ((1 << 30) + 64, 1 << 19, D, 1), 4096)
+    new = _gen(31)
+    k.copy_(new(B, Lk, HK, D, dtype=BF16))
+    v.copy_(new(B, Lk, HK, D, dtype=BF16))
+    q, g = new(B, 6, 2, D, dtype=BF16), new(B, 6, 2, D, dtype=BF16)
+    want = _run(q, k.contiguous(), v.contiguous(), g)
+    got = _run(q, k, v, g)
+    assert torch.equal(want[0], got[0]) and all(torch.equal(x, y) for x, y in zip(want[2], got[2]))

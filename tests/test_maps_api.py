@@ -1,0 +1,97 @@
+"""The refusals and host arithmetic of the operators on maps: no device work.  Refused calls return before anything is enqueued, so made-up
+addresses do."""
+import os
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+
+def _b():
+    from paper_2505_16942_amd import binding
+    if not os.path.exists(binding.LIB_PATH):
+        pytest.skip("library not built (run __graft_entry__.build())")
+    binding.load_library()
+    return binding
+
+
+# addresses far apart, one per array
+Q, K, V, OUT, LSE, LENGTHS, MASK, WS, D_OUT, DQ, DK, DV = (1 << 42 | (i << 36) for i in range(12))
+
+
+def _attention(kw):
+    from paper_2505_16942_amd import binding as b
+    a = dict(type=1, B=2, Lq=300, Lk=500, H=4, HK=2, D=64, q=Q, q_item=300 * 256, q_row=256, q_head=64, k=K, k_item=500 * 128, k_row=128, k_head=64,
+             v=V, v_item=500 * 128, v_row=128, v_head=64, scale=0.125, k_lengths=LENGTHS, key_mask=MASK)
+    a.update({k: v for k, v in kw.items() if k in a})
+    return b.attention_args(*a.values())
+
+
+REFUSED = [
+    (dict(type=3), -1), (dict(type=-1), -1), (dict(B=-1), -1), (dict(Lq=-1), -1), (dict(Lk=-1), -1), (dict(H=0), -1), (dict(HK=0), -1), (dict(H=3), -1),
+    (dict(D=0), -1), (dict(D=-8), -1), (dict(D=12), -2), (dict(D=264), -2), (dict(H=130), -2), (dict(B=(1 << 20) + 1), -2), (dict(Lk=(1 << 30) + 1), -2),
+    (dict(Lq=1 << 30), -2), (dict(Lq=1 << 29, B=4), -2), (dict(q=None), -1), (dict(k=None), -1), (dict(v=None), -1), (dict(q=Q + 2), -1),
+    (dict(k=K + 2), -1), (dict(v=V + 1), -1), (dict(q_row=255), -1), (dict(k_head=63), -1), (dict(v_item=-2), -1), (dict(q_row=(1 << 21) + 2), -2),
+    (dict(k_row=(1 << 21) + 2), -2), (dict(v_head=(1 << 21) + 2), -2), (dict(q_item=(1 << 40) + 2), -2), (dict(scale=0.0), -1), (dict(scale=-1.0), -1),
+    (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(k_lengths=LENGTHS + 2), -1),
+]
+
+
+def _forward(b, **kw):
+    o = dict(out=OUT, lse=LSE, ws=WS, size=1 << 33)
+    o.update({k: v for k, v in kw.items() if k in o})
+    return b.load_library().corr_attention(_attention(kw), o["out"], o["lse"], o["ws"], o["size"], None)
+
+
+@pytest.mark.parametrize("kw,status", REFUSED + [
+    (dict(out=None), -1), (dict(out=OUT + 1), -1), (dict(lse=LSE + 2), -1), (dict(ws=None), -1), (dict(size=64), -1), (dict(ws=WS + 8), -1),
+    (dict(out=Q), -1), (dict(out=K + 500 * 128 * 2), -1), (dict(out=V - 2), -1), (dict(lse=OUT), -1), (dict(ws=OUT), -1), (dict(ws=MASK), -1),
+    (dict(out=LENGTHS), -1), (dict(lse=Q + 4), -1),
+])
+def test_attention_refusals(kw, status):
+    assert _forward(_b(), **kw) == status
+
+
+def _backward(b, **kw):
+    o = dict(out=OUT, lse=LSE, d_out=D_OUT, dq=DQ, dk=DK, dv=DV, ws=WS, size=1 << 33)
+    o.update({k: v for k, v in kw.items() if k in o})
+    return b.load_library().corr_attention_backward(_attention(kw), *o.values(), None)
+
+
+@pytest.mark.parametrize("kw,status", REFUSED + [
+    (dict(out=None), -1), (dict(lse=None), -1), (dict(d_out=None), -1), (dict(d_out=D_OUT + 2), -1), (dict(dk=None), -1), (dict(dv=None), -1),
+    (dict(dq=DQ + 1), -1), (dict(dk=DK + 1), -1), (dict(ws=None), -1), (dict(size=256), -1), (dict(ws=WS + 4), -1), (dict(dq=D_OUT), -1), (dict(dq=OUT), -1),
+    (dict(dk=DV), -1), (dict(dk=K), -1), (dict(dv=Q), -1), (dict(dq=LSE), -1), (dict(ws=DQ), -1), (dict(ws=V), -1),
+])
+def test_attention_backward_refusals(kw, status):
+    assert _backward(_b(), **kw) == status
+
+
+def test_attention_without_work():
+    b = _b()
+    assert _forward(b, B=0, q=None, k=None, v=None, out=None, ws=None) == 0
+    assert _forward(b, Lq=0, q=None, out=None, ws=None) == 0
+    assert _backward(b, dq=None, dk=None, dv=None, ws=None) == 0
+    assert _backward(b, B=0, out=None, lse=None, d_out=None, ws=None) == 0
+    assert b.load_library().corr_attention(None, OUT, None, WS, 1 << 30, None) == -1
+    for need in (b.corr_attention_workspace_bytes, b.corr_attention_backward_workspace_bytes):
+        assert need(torch.bfloat16, 0, 5, 5, 1, 1, 64) == 0 and need(torch.bfloat16, 1, 0, 5, 1, 1, 64) == 0
+        assert need(torch.bfloat16, 1, 5, 5, 1, 1, 20) == 0 and need(torch.bfloat16, 1, 5, 5, 3, 2, 64) == 0
+
+
+def test_attention_workspace():
+    """A few rows of many keys are split, and need room for the shares' sums; many rows need none; the gradient's holds two numbers a row at least."""
+    b = _b()
+    assert b.corr_attention_workspace_bytes(torch.bfloat16, 1, 1, 32768, 8, 2, 128) > 8 * 128 * 4
+    assert b.corr_attention_workspace_bytes(torch.bfloat16, 1, 32400, 32400, 4, 4, 128) == 0
+    assert b.corr_attention_backward_workspace_bytes(torch.bfloat16, 1, 32400, 32400, 8, 8, 64) < 32400 * 8 * 8 + 8 * 64 * 8 + 1024
+    for dtype in (torch.float32, torch.bfloat16, torch.float16):
+        for Lq, Lk in ((1, 1), (1, 1 << 30), (1 << 30, 1), (100000, 100000)):
+            assert b.corr_attention_backward_workspace_bytes(dtype, 1, Lq, Lk, 1, 1, 8) >= 8 * Lq
+
+
+def test_binding_checks_before_the_library():
+    b = _b()
+    x = torch.zeros(1, 2, 2, 8)
+    with pytest.raises((TypeError, ValueError)):
+        b.corr_attention(x, x, x)                       # not on the GPU
