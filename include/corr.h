@@ -314,6 +314,29 @@ corr_status corr_residual_norm_backward(const corr_residual_norm_args* args, con
  */
 
 /*
+ * y = act((x - mean) / sqrt(var + eps) * weight + bias): mean and var (the mean square about it) over all P rows of an item and the C / G
+ * neighbouring channels of a group.  G = C normalises every channel by itself, G = 1 the whole item.
+ *   x            : [B * P, C] rows, x_stride; item b's are rows b P to b P + P - 1.
+ *   weight, bias : fp32 [C], or NULL (ones, zeros).
+ *   stats        : NULL, or fp32 [B, G, 2]: mean and 1 / sqrt(var + eps), which the gradient reads.
+ *   y            : [B * P, C] dense; may be x (if x_stride == C).
+ * Limits: C <= 16384, B <= 65535, B * C <= 2^23, B * P <= 2^30, strides <= 2^21; beyond: CORR_ERR_UNSUPPORTED.  eps > 0.  Without pixels (P = 0) stats are zeros.
+ */
+size_t corr_group_norm_workspace_bytes(corr_dtype type, int64_t B, int64_t P, int64_t C, int64_t G);
+corr_status corr_group_norm(corr_dtype type, corr_activation act, const void* x, int64_t x_stride, const float* weight, const float* bias,
+                            float eps, float* stats, void* y, int64_t B, int64_t P, int64_t C, int64_t G,
+                            void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * Gradients at the forward call's own x, weight, bias and activation, with stats as it left them.
+ *   d_y : [B * P, C] rows, d_y_stride.   d_x : [B * P, C] dense or NULL;  d_weight, d_bias : fp32 [C] or NULL.
+ */
+size_t corr_group_norm_backward_workspace_bytes(corr_dtype type, int64_t B, int64_t P, int64_t C, int64_t G);
+corr_status corr_group_norm_backward(corr_dtype type, corr_activation act, const void* x, int64_t x_stride, const float* stats,
+                                     const float* weight, const float* bias, const void* d_y, int64_t d_y_stride,
+                                     void* d_x, float* d_weight, float* d_bias, int64_t B, int64_t P, int64_t C, int64_t G,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Attention of B items' Lq rows to Lk keys, which may be another map's, or an encoder's states of any length:
  *     out[b, i, h] = sum over keys j of softmax_j(scale <q[b, i, h], k[b, j, h / (H / HK)]>) v[b, j, h / (H / HK)]
  * H query heads, HK key heads (HK divides H: query heads that follow each other share one), heads of D elements.

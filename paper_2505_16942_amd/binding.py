@@ -37,6 +37,7 @@ EXPORTS = [
     "corr_backward_workspace_bytes", "corr_sample_backward",
     "corr_linear_workspace_bytes", "corr_linear", "corr_linear_backward_workspace_bytes", "corr_linear_backward",
     "corr_residual_norm", "corr_residual_norm_backward_workspace_bytes", "corr_residual_norm_backward",
+    "corr_group_norm_workspace_bytes", "corr_group_norm", "corr_group_norm_backward_workspace_bytes", "corr_group_norm_backward",
     "corr_attention_workspace_bytes", "corr_attention", "corr_attention_backward_workspace_bytes", "corr_attention_backward",
 ]
 # measurement and test hooks (include/corr_bench.h)
@@ -119,6 +120,14 @@ def load_library():
     lib.corr_sample_backward.argtypes = [vp, vp, vp, ci, ci, ci, ci, ci, ci, vp, vp, vp, sz, vp]
     lib.corr_sample_backward.restype = ci
     i64 = ctypes.c_int64
+    f32 = ctypes.c_float
+    for name in ("corr_group_norm_workspace_bytes", "corr_group_norm_backward_workspace_bytes"):
+        getattr(lib, name).argtypes = [ci] + [i64] * 4
+        getattr(lib, name).restype = sz
+    lib.corr_group_norm.argtypes = [ci, ci, vp, i64, vp, vp, f32, vp, vp, i64, i64, i64, i64, vp, sz, vp]
+    lib.corr_group_norm.restype = ci
+    lib.corr_group_norm_backward.argtypes = [ci, ci, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, i64, i64, i64, i64, vp, sz, vp]
+    lib.corr_group_norm_backward.restype = ci
     for name in ("corr_attention_workspace_bytes", "corr_attention_backward_workspace_bytes"):
         getattr(lib, name).argtypes = [ci] + [i64] * 6
         getattr(lib, name).restype = sz
@@ -659,6 +668,92 @@ def corr_residual_norm_backward(h: torch.Tensor, y: torch.Tensor | None = None, 
     if st != CORR_OK:
         raise CorrError(st, "corr_residual_norm_backward")
     return g
+
+
+@functools.lru_cache(maxsize=1024)
+def _group_norm_need(*sizes) -> int:
+    return int(load_library().corr_group_norm_workspace_bytes(*sizes))
+
+
+@functools.lru_cache(maxsize=1024)
+def _group_norm_backward_need(*sizes) -> int:
+    return int(load_library().corr_group_norm_backward_workspace_bytes(*sizes))
+
+
+def _items(x, groups: int):
+    """(device, type code, B, P, C, stride) of a channels-last map whose first axis are the items."""
+    device = _on_device(x, "x")
+    code = _type_of(x, "x")
+    if x.dim() < 2:
+        raise ValueError("x must be [B, ..., C]")
+    rows, C, stride = _rows(x, "x")
+    B = x.shape[0]
+    P = 1
+    for n in x.shape[1:-1]:
+        P *= n
+    if C < 1 or groups < 1 or C % groups:
+        raise ValueError("the number of groups must divide the channels (%d)" % C)
+    return device, code, B, P, C, stride
+
+
+def corr_group_norm_workspace_bytes(dtype: torch.dtype, B: int, P: int, C: int, G: int) -> int:
+    return int(load_library().corr_group_norm_workspace_bytes(_TYPES[dtype], B, P, C, G))
+
+
+def corr_group_norm(x: torch.Tensor, groups: int, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+                    act: int = CORR_ACT_NONE, eps: float = 1e-5, out: torch.Tensor | None = None, stats: torch.Tensor | None = None,
+                    workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """act(norm of x over each item's pixels and a group's channels, times weight, plus bias).  x: [B, ..., C] with contiguous, evenly spaced rows
+    (channels last); weight, bias: float32 [C].  out: contiguous, may be x.  stats: a contiguous float32 [B, groups, 2] that receives mean
+    and 1 / sqrt(var + eps) (corr_group_norm_backward reads it)."""
+    lib = _lib or load_library()
+    device, code, B, P, C, xs = _items(x, groups)
+    pw = None if weight is None else _dense(weight, "weight", torch.float32, device, (C,))
+    pb = None if bias is None else _dense(bias, "bias", torch.float32, device, (C,))
+    ps = None if stats is None else _dense(stats, "stats", torch.float32, device, (B, groups, 2))
+    if out is None:
+        out = _new(x, x.shape, x.dtype)
+        po = _pointer(out)
+    else:
+        po = _dense(out, "out", x.dtype, device, x.shape)
+    held, ws, size = _workspace(workspace, _group_norm_need(code, B, P, C, groups), x, device)
+    st = lib.corr_group_norm(code, act, _pointer(x), xs, pw, pb, eps, ps, po, B, P, C, groups, ws, size, _stream())
+    if st != CORR_OK:
+        raise CorrError(st, "corr_group_norm")
+    return out
+
+
+def corr_group_norm_backward_workspace_bytes(dtype: torch.dtype, B: int, P: int, C: int, G: int) -> int:
+    return int(load_library().corr_group_norm_backward_workspace_bytes(_TYPES[dtype], B, P, C, G))
+
+
+def corr_group_norm_backward(x: torch.Tensor, groups: int, stats: torch.Tensor, d_out: torch.Tensor, weight: torch.Tensor | None = None,
+                             bias: torch.Tensor | None = None, act: int = CORR_ACT_NONE, want_x: bool = True, want_weight: bool = True,
+                             want_bias: bool = True, d_x: torch.Tensor | None = None, d_weight: torch.Tensor | None = None,
+                             d_bias: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """(d_x, d_weight, d_bias) of corr_group_norm at its own x, weight, bias and activation, None where not wanted: x's type for the first,
+    float32 for the others (also where weight or bias are None: ones and zeros).  stats: what corr_group_norm stored; d_out: rows of x's type."""
+    lib = _lib or load_library()
+    device, code, B, P, C, xs = _items(x, groups)
+    pw = None if weight is None else _dense(weight, "weight", torch.float32, device, (C,))
+    pb = None if bias is None else _dense(bias, "bias", torch.float32, device, (C,))
+    ps = _dense(stats, "stats", torch.float32, device, (B, groups, 2))
+    pg, gs = _matrix(d_out, "d_out", x.dtype, device, B * P, C)
+    px = pdw = pdb = None
+    if want_x:
+        d_x = _new(x, x.shape, x.dtype) if d_x is None else d_x
+        px = _dense(d_x, "d_x", x.dtype, device, x.shape)
+    if want_weight:
+        d_weight = _new(x, (C,), torch.float32) if d_weight is None else d_weight
+        pdw = _dense(d_weight, "d_weight", torch.float32, device, (C,))
+    if want_bias:
+        d_bias = _new(x, (C,), torch.float32) if d_bias is None else d_bias
+        pdb = _dense(d_bias, "d_bias", torch.float32, device, (C,))
+    held, ws, size = _workspace(workspace, _group_norm_backward_need(code, B, P, C, groups), x, device)
+    st = lib.corr_group_norm_backward(code, act, _pointer(x), xs, ps, pw, pb, pg, gs, px, pdw, pdb, B, P, C, groups, ws, size, _stream())
+    if st != CORR_OK:
+        raise CorrError(st, "corr_group_norm_backward")
+    return d_x if want_x else None, d_weight if want_weight else None, d_bias if want_bias else None
 
 
 @functools.lru_cache(maxsize=1024)

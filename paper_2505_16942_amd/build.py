@@ -19,7 +19,7 @@ SOURCES = [("block.hip", "block_r%d_c%d.o" % (r, nc), ["-DCORR_BLOCK_R=%d" % r, 
 SOURCES += [("residual_norm.hip", "residual_norm_%d.o" % k, ["-DCORR_NORM_PAIR=%d" % k]) for k in range(5)]
 # attention.hip once per type
 SOURCES += [("attention.hip", "attention_%d.o" % k, ["-DCORR_ATTENTION_TYPE=%d" % k]) for k in range(3)]
-SOURCES += [(f + ".hip", f + ".o", []) for f in ("linear", "rows", "rows_api", "maps_api")]
+SOURCES += [(f + ".hip", f + ".o", []) for f in ("linear", "rows", "rows_api", "group_norm", "maps_api")]
 SOURCES += [("corr_api.hip", "corr_api.o", []), ("features.hip", "features.o", []), ("binning.hip", "binning.o", []),
             ("ondemand.hip", "ondemand.o", []), ("fullvol.hip", "fullvol.o", []), ("backward.hip", "backward.o", [])]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

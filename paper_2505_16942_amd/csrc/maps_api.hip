@@ -2,6 +2,7 @@
 #include <math.h>
 #include "attention.h"
 #include "checks.h"
+#include "group_norm.h"
 
 namespace {
 
@@ -77,9 +78,99 @@ GradientLayout gradient_layout(corr_dtype t, int64_t B, int64_t Lq, int64_t Lk, 
     return l;
 }
 
+// ---- group norm
+corr_status check_group_norm(corr_dtype type, corr_activation act, int64_t B, int64_t P, int64_t C, int64_t G) {
+    if (!known(type) || !known(act) || B < 0 || P < 0 || C <= 0 || G <= 0 || C % G) return CORR_ERR_INVALID_ARG;
+    if (C > 16384 || B > 65535 || B * C > 1 << 23 || P > MAX_LENGTH || B * P > MAX_LENGTH) return CORR_ERR_UNSUPPORTED;
+    return CORR_OK;
+}
+struct GroupNormLayout { GroupNormArgs args; size_t part, sums, stats, total; };
+GroupNormLayout group_norm_layout(corr_dtype type, int64_t B, int64_t P, int64_t C, int64_t G, bool gradient) {
+    GroupNormLayout l = {};
+    Carver c;
+    l.args.type = type;
+    l.args.B = (int)B; l.args.P = P; l.args.C = (int)C; l.args.G = (int)G;
+    group_norm_plan(l.args, gradient);
+    l.part = c.take((size_t)B * l.args.parts * C * 8);
+    if (gradient) l.sums = c.take((size_t)B * C * 8);
+    else l.stats = c.take((size_t)B * G * 8);            // where the caller keeps none
+    l.total = c.used;
+    return l;
+}
+
 }  // namespace
 
 extern "C" {
+
+size_t corr_group_norm_workspace_bytes(corr_dtype type, int64_t B, int64_t P, int64_t C, int64_t G) {
+    if (check_group_norm(type, CORR_ACT_NONE, B, P, C, G) != CORR_OK || !B || !P) return 0;
+    return group_norm_layout(type, B, P, C, G, false).total;
+}
+
+corr_status corr_group_norm(corr_dtype type, corr_activation act, const void* x, int64_t x_stride, const float* weight, const float* bias,
+                            float eps, float* stats, void* y, int64_t B, int64_t P, int64_t C, int64_t G,
+                            void* workspace, size_t workspace_bytes, void* stream) {
+    corr_status st = check_group_norm(type, act, B, P, C, G);
+    if (st != CORR_OK) return st;
+    if (!(eps > 0.f) || !on(stats, 4) || !on(weight, 4) || !on(bias, 4)) return CORR_ERR_INVALID_ARG;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (!B || !P) return launch_zero(stats, (size_t)B * G * 8, s) == hipSuccess ? CORR_OK : CORR_ERR_HIP;
+    const int es = corr_elem_bytes(type);
+    if (!x || !y || x_stride < C || !on(x, es) || !on(y, es)) return CORR_ERR_INVALID_ARG;
+    if (x_stride > MAX_STRIDE) return CORR_ERR_UNSUPPORTED;
+    const GroupNormLayout l = group_norm_layout(type, B, P, C, G, false);
+    if (!workspace || workspace_bytes < l.total || !on(workspace, 16)) return CORR_ERR_INVALID_ARG;
+    const bool in_place = y == x && x_stride == C;
+    const Range outs[] = {range(y, B * P, C, C, es), range(stats, 1, B * G * 2, 0, 4), range(workspace, 1, (int64_t)l.total, 0, 1)};
+    const Range in[] = {range(in_place ? nullptr : x, B * P, C, x_stride, es), range(weight, 1, C, 0, 4), range(bias, 1, C, 0, 4)};
+    if (any_overlap(outs, in)) return CORR_ERR_INVALID_ARG;
+    GroupNormArgs a = l.args;
+    char* const ws = static_cast<char*>(workspace);
+    a.act = act; a.eps = eps;
+    a.x = x; a.x_stride = x_stride; a.weight = weight; a.bias = bias; a.y = y;
+    a.stats = stats ? stats : reinterpret_cast<float*>(ws + l.stats);
+    a.part = reinterpret_cast<float*>(ws + l.part);
+    return launch_group_norm(a, s) == hipSuccess ? CORR_OK : CORR_ERR_HIP;
+}
+
+size_t corr_group_norm_backward_workspace_bytes(corr_dtype type, int64_t B, int64_t P, int64_t C, int64_t G) {
+    if (check_group_norm(type, CORR_ACT_NONE, B, P, C, G) != CORR_OK || !B || !P) return 0;
+    return group_norm_layout(type, B, P, C, G, true).total;
+}
+
+corr_status corr_group_norm_backward(corr_dtype type, corr_activation act, const void* x, int64_t x_stride, const float* stats,
+                                     const float* weight, const float* bias, const void* d_y, int64_t d_y_stride,
+                                     void* d_x, float* d_weight, float* d_bias, int64_t B, int64_t P, int64_t C, int64_t G,
+                                     void* workspace, size_t workspace_bytes, void* stream) {
+    corr_status st = check_group_norm(type, act, B, P, C, G);
+    if (st != CORR_OK) return st;
+    const int es = corr_elem_bytes(type);
+    if (!on(d_x, es) || !on(d_weight, 4) || !on(d_bias, 4)) return CORR_ERR_INVALID_ARG;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (!B || !P) {
+        hipError_t e = launch_zero(d_weight, (size_t)C * 4, s);
+        if (e == hipSuccess) e = launch_zero(d_bias, (size_t)C * 4, s);
+        return e == hipSuccess ? CORR_OK : CORR_ERR_HIP;
+    }
+    if (!x || !stats || !d_y || x_stride < C || d_y_stride < C || !on(x, es) || !on(d_y, es) || !on(stats, 4) || !on(weight, 4) || !on(bias, 4))
+        return CORR_ERR_INVALID_ARG;
+    if (x_stride > MAX_STRIDE || d_y_stride > MAX_STRIDE) return CORR_ERR_UNSUPPORTED;
+    const GroupNormLayout l = group_norm_layout(type, B, P, C, G, true);
+    if (!workspace || workspace_bytes < l.total || !on(workspace, 16)) return CORR_ERR_INVALID_ARG;
+    const Range outs[] = {range(d_x, B * P, C, C, es), range(d_weight, 1, C, 0, 4), range(d_bias, 1, C, 0, 4),
+                          range(workspace, 1, (int64_t)l.total, 0, 1)};
+    const Range in[] = {range(x, B * P, C, x_stride, es), range(d_y, B * P, C, d_y_stride, es), range(stats, 1, B * G * 2, 0, 4),
+                        range(weight, 1, C, 0, 4), range(bias, 1, C, 0, 4)};
+    if (any_overlap(outs, in)) return CORR_ERR_INVALID_ARG;
+    GroupNormArgs a = l.args;
+    char* const ws = static_cast<char*>(workspace);
+    a.act = act;
+    a.x = x; a.x_stride = x_stride; a.weight = weight; a.bias = bias; a.stats = const_cast<float*>(stats);
+    a.d_y = d_y; a.d_y_stride = d_y_stride; a.d_x = d_x; a.d_weight = d_weight; a.d_bias = d_bias;
+    a.part = reinterpret_cast<float*>(ws + l.part);
+    a.sums = reinterpret_cast<float*>(ws + l.sums);
+    return launch_group_norm_backward(a, s) == hipSuccess ? CORR_OK : CORR_ERR_HIP;
+}
 
 size_t corr_attention_workspace_bytes(corr_dtype type, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t HK, int64_t D) {
     if (check_sizes(type, B, Lq, Lk, H, HK, D) != CORR_OK || !B || !Lq) return 0;

@@ -108,3 +108,74 @@ class Attention:
         dk, ek = (shared(t) for t in product(ds.transpose(2, 3), self.q, e_ds.transpose(2, 3), n, scale))
         dv, ev = (shared(t) for t in product(self.p.transpose(2, 3), g, e_p.transpose(2, 3), n, 1.0))
         return ((dq.transpose(1, 2), (eq + rounded(dq, self.T)).transpose(1, 2)), (dk, ek + rounded(dk, self.T)), (dv, ev + rounded(dv, self.T)))
+
+
+class GroupNorm:
+    """Means and squares are merged along a chain: at most 16 chunks of a thread, 8 steps over threads, and P C / G / 2048 + 9 of a group's parts, of three
+    operations each: OPS of them, relative to the largest magnitude for the mean; the squares are of differences whose own error is that of the
+    mean.  Sums over rows go through at most P / 8 + 64 additions.  relu's slope may fall on either side where |z| is within its error."""
+
+    def __init__(self, x, G, w, b, name, eps):
+        self.T, self.name, self.G, self.wide = x.dtype, name, G, x.shape[2]
+        x = x.double().cpu()
+        B, P, C = x.shape
+        one, zero = torch.ones(C, dtype=torch.float64), torch.zeros(C, dtype=torch.float64)
+        by = lambda v: v.view(G, C // G)  # noqa: E731
+        self.w, self.b = by(one if w is None else w.double().cpu()), by(zero if b is None else b.double().cpu())
+        x = x.view(B, P, G, C // G)
+        self.n = P * (C // G)
+        mean = x.mean((1, 3), keepdim=True)
+        var = ((x - mean) ** 2).mean((1, 3), keepdim=True)
+        rho = 1 / torch.sqrt(var + eps)
+        ops = 3 * (33 + self.n / 2048)
+        most = x.abs().amax((1, 3), keepdim=True)
+        e_mean = ops * EPS * most
+        e_var = ops * EPS * (var + 2 * most * var.sqrt() + ops * EPS * most ** 2)
+        e_rho = rho * (0.5 * e_var / (var + eps) + 4 * EPS)
+        self.hat, self.rho, self.P = (x - mean) * rho, rho, P
+        self.e_hat = (x - mean).abs() * e_rho + (rho + e_rho) * (e_mean + EPS * (x.abs() + mean.abs()))
+        self.e_rho = e_rho
+        self.z = self.hat * self.w + self.b
+        self.e_z = self.w.abs() * self.e_hat + 4 * EPS * ((self.hat * self.w).abs() + self.b.abs())
+        self.stats = torch.cat([mean, rho], 3).view(B, G, 2)
+        self.e_stats = 1.01 * torch.cat([e_mean, e_rho], 3).view(B, G, 2) + EPS * self.stats.abs()
+
+    def _flat(self, v):
+        return v.reshape(v.shape[0], v.shape[1], self.wide)
+
+    def forward(self):
+        from rows_reference import act
+        y = act(self.name, self.z)
+        e = 1.13 * self.e_z + (16 * EPS * (self.z.abs() + 1) if self.name != "none" else 0)
+        return (self._flat(y), self._flat(1.01 * e + rounded(y, self.T))), (self.stats, self.e_stats)
+
+    def backward(self, d_y):
+        from rows_reference import slope
+        g = d_y.double().cpu().view(self.z.shape)
+        e_slope = torch.zeros_like(g)
+        if self.name == "relu":
+            e_slope = (self.z.abs() <= self.e_z).double()
+        elif self.name != "none":
+            e_slope = 16 * EPS * (2 + self.z.abs()) + 1.2 * self.e_z
+        dz = g * slope(self.name, self.z)
+        e_dz = g.abs() * (e_slope + EPS)
+        chain = (self.P / 8 + 64) * EPS
+
+        def total(v, e, dims):
+            return v.sum(dims, keepdim=True), e.sum(dims, keepdim=True) + chain * (v.abs() + e).sum(dims, keepdim=True)
+        h, e_h = dz * self.hat, e_dz * (self.hat.abs() + self.e_hat) + dz.abs() * self.e_hat
+        q, e_q = dz * self.w, (e_dz + EPS * dz.abs()) * self.w.abs()
+        qh, e_qh = h * self.w, (e_h + 2 * EPS * h.abs()) * self.w.abs()
+        s1, e1 = total(q, e_q, (1, 3))
+        s2, e2 = total(qh, e_qh, (1, 3))
+        n = self.n
+        inner = q - s1 / n - self.hat * s2 / n
+        size = q.abs() + s1.abs() / n + (self.hat * s2).abs() / n
+        e_inner = e_q + (e1 + self.hat.abs() * e2 + self.e_hat * (s2.abs() + e2)) / n + 8 * EPS * size
+        dx = self.rho * inner
+        e_dx = self.rho * e_inner + (inner.abs() + e_inner) * self.e_rho + 2 * EPS * dx.abs()
+        out = [(self._flat(dx), self._flat(1.01 * e_dx + rounded(dx, self.T)))]
+        for v, e in ((h, e_h), (dz, e_dz)):
+            s, es = total(v, e, (0, 1))
+            out.append((s.reshape(-1), (1.01 * es + rounded(s, F32)).reshape(-1)))
+        return out

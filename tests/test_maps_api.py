@@ -95,3 +95,47 @@ def test_binding_checks_before_the_library():
     x = torch.zeros(1, 2, 2, 8)
     with pytest.raises((TypeError, ValueError)):
         b.corr_attention(x, x, x)                       # not on the GPU
+
+
+X, Y, STATS, W, BIAS, DY, DX, DW, DB = (1 << 43 | (i << 36) for i in range(9))
+
+
+def _norm(b, **kw):
+    a = dict(type=1, act=1, x=X, xs=64, w=W, bias=BIAS, eps=1e-5, stats=STATS, y=Y, B=2, P=100, C=64, G=8, ws=WS, size=1 << 30)
+    a.update(kw)
+    return b.load_library().corr_group_norm(*a.values(), None)
+
+
+NORM_REFUSED = [
+    (dict(type=3), -1), (dict(act=6), -1), (dict(act=-1), -1), (dict(B=-1), -1), (dict(P=-1), -1), (dict(C=0), -1), (dict(G=0), -1), (dict(G=7), -1),
+    (dict(G=128), -1), (dict(C=16392, xs=16392), -2), (dict(B=65536), -2), (dict(B=60000, C=256, xs=256), -2), (dict(P=1 << 30), -2),
+    (dict(x=None), -1), (dict(xs=63), -1), (dict(xs=(1 << 21) + 1), -2), (dict(x=X + 1), -1), (dict(w=W + 2), -1), (dict(bias=BIAS + 1), -1),
+    (dict(ws=None), -1), (dict(size=100), -1), (dict(ws=WS + 8), -1),
+]
+
+
+@pytest.mark.parametrize("kw,status", NORM_REFUSED + [
+    (dict(eps=0.0), -1), (dict(eps=-1.0), -1), (dict(eps=float("nan")), -1), (dict(y=None), -1), (dict(y=Y + 1), -1), (dict(stats=STATS + 2), -1),
+    (dict(y=X + 2), -1), (dict(y=X, xs=66), -1), (dict(y=W), -1), (dict(stats=Y), -1), (dict(ws=X), -1), (dict(ws=Y), -1), (dict(stats=X), -1),
+])
+def test_group_norm_refusals(kw, status):
+    assert _norm(_b(), **kw) == status
+
+
+@pytest.mark.parametrize("kw,status", NORM_REFUSED + [
+    (dict(stats=None), -1), (dict(dy=None), -1), (dict(dys=63), -1), (dict(dys=(1 << 21) + 1), -2), (dict(dx=DX + 1), -1), (dict(dw=DW + 2), -1),
+    (dict(db=DB + 1), -1), (dict(dx=X), -1), (dict(dx=DY), -1), (dict(dw=DX), -1), (dict(db=DW), -1), (dict(dw=STATS), -1), (dict(ws=DY), -1), (dict(db=W), -1),
+])
+def test_group_norm_backward_refusals(kw, status):
+    b = _b()
+    a = dict(type=1, act=1, x=X, xs=64, stats=STATS, w=W, bias=BIAS, dy=DY, dys=64, dx=DX, dw=DW, db=DB, B=2, P=100, C=64, G=8, ws=WS, size=1 << 30)
+    a.update(kw)
+    assert b.load_library().corr_group_norm_backward(*a.values(), None) == status
+
+
+def test_group_norm_workspace():
+    b = _b()
+    for need in (b.corr_group_norm_workspace_bytes, b.corr_group_norm_backward_workspace_bytes):
+        assert need(torch.float32, 0, 5, 8, 2) == 0 and need(torch.float32, 1, 0, 8, 2) == 0 and need(torch.float32, 1, 5, 8, 3) == 0
+        for B, P, C, G in ((1, 1, 1, 1), (2, 518400, 256, 32), (65535, 3, 64, 2), (1, 1 << 30, 8, 8), (512, 16, 16384, 16384)):
+            assert B * C * 8 <= need(torch.bfloat16, B, P, C, G) < (1 << 26) + 32 * B * C
