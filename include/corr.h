@@ -377,6 +377,29 @@ size_t corr_attention_backward_workspace_bytes(corr_dtype type, int64_t B, int64
 corr_status corr_attention_backward(const corr_attention_args* args, const void* out, const float* lse, const void* d_out,
                                     void* d_q, void* d_k, void* d_v, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * The gated products of a feed-forward block, both in one kernel (corr_linear is the product back, with its residual):
+ *     z = x w^T + bias,   y = act(first N columns of z) * (last N columns of z)
+ *   x : [M, K] rows, x_stride;  w : [2 N, K], dense, the gate's N rows first;  bias : fp32 [2 N] or NULL.  16-bit matrices start on a 4-byte border.
+ *   preact : NULL, or [M, 2 N] dense: receives z, which corr_gated_linear_backward reads.
+ *   y      : [M, N] rows, y_stride; made from z before z is rounded.
+ * Precision and limits as for corr_linear with 2 N columns.
+ */
+size_t corr_gated_linear_workspace_bytes(corr_dtype type, int64_t M, int64_t N, int64_t K, int64_t x_stride);
+corr_status corr_gated_linear(corr_dtype type, corr_activation act, const void* x, int64_t x_stride, const void* w, const float* bias,
+                              void* preact, void* y, int64_t y_stride, int64_t M, int64_t N, int64_t K,
+                              void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * With z = (gate, up) from preact: dz = (d_y up act'(gate), d_y act(gate)),  d_x = dz w,  d_w = dz^T x,  d_bias = sum over rows of dz.
+ *   preact : [M, 2 N] dense, as corr_gated_linear left it;  d_y : [M, N] rows, d_y_stride.  x and w of 16 bits start on a 4-byte border.
+ *   d_x    : [M, K] dense or NULL;  d_w : [2 N, K] dense or NULL;  d_bias : fp32 [2 N] or NULL.
+ * dz is rounded as corr_linear_backward's (bf16 once, fp16 in two parts, fp32 whole); fp16's holds values up to 1.3e5, beyond which it is infinite.
+ */
+size_t corr_gated_linear_backward_workspace_bytes(corr_dtype type, int64_t M, int64_t N, int64_t K, int64_t x_stride);
+corr_status corr_gated_linear_backward(corr_dtype type, corr_activation act, const void* x, int64_t x_stride, const void* w,
+                                       const void* preact, const void* d_y, int64_t d_y_stride, void* d_x, void* d_w, float* d_bias,
+                                       int64_t M, int64_t N, int64_t K, void* workspace, size_t workspace_bytes, void* stream);
+
 const char* corr_status_string(corr_status s);
 
 #ifdef __cplusplus

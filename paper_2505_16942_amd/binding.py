@@ -38,6 +38,7 @@ EXPORTS = [
     "corr_linear_workspace_bytes", "corr_linear", "corr_linear_backward_workspace_bytes", "corr_linear_backward",
     "corr_residual_norm", "corr_residual_norm_backward_workspace_bytes", "corr_residual_norm_backward",
     "corr_group_norm_workspace_bytes", "corr_group_norm", "corr_group_norm_backward_workspace_bytes", "corr_group_norm_backward",
+    "corr_gated_linear_workspace_bytes", "corr_gated_linear", "corr_gated_linear_backward_workspace_bytes", "corr_gated_linear_backward",
     "corr_attention_workspace_bytes", "corr_attention", "corr_attention_backward_workspace_bytes", "corr_attention_backward",
 ]
 # measurement and test hooks (include/corr_bench.h)
@@ -120,6 +121,13 @@ def load_library():
     lib.corr_sample_backward.argtypes = [vp, vp, vp, ci, ci, ci, ci, ci, ci, vp, vp, vp, sz, vp]
     lib.corr_sample_backward.restype = ci
     i64 = ctypes.c_int64
+    for name in ("corr_gated_linear_workspace_bytes", "corr_gated_linear_backward_workspace_bytes"):
+        getattr(lib, name).argtypes = [ci] + [i64] * 4
+        getattr(lib, name).restype = sz
+    lib.corr_gated_linear.argtypes = [ci, ci, vp, i64, vp, vp, vp, vp, i64, i64, i64, i64, vp, sz, vp]
+    lib.corr_gated_linear.restype = ci
+    lib.corr_gated_linear_backward.argtypes = [ci, ci, vp, i64, vp, vp, vp, i64, vp, vp, vp, i64, i64, i64, vp, sz, vp]
+    lib.corr_gated_linear_backward.restype = ci
     f32 = ctypes.c_float
     for name in ("corr_group_norm_workspace_bytes", "corr_group_norm_backward_workspace_bytes"):
         getattr(lib, name).argtypes = [ci] + [i64] * 4
@@ -563,6 +571,92 @@ def corr_linear_backward(x: torch.Tensor, w: torch.Tensor, d_out: torch.Tensor, 
     st = lib.corr_linear_backward(code, act, _pointer(x), xs, pw, pz, pg, gs, px, pdw, pdb, M, N, K, ws, size, _stream())
     if st != CORR_OK:
         raise CorrError(st, "corr_linear_backward")
+    return d_x if want_x else None, d_w if want_w else None, d_bias if want_bias else None
+
+
+@functools.lru_cache(maxsize=1024)
+def _gated_need(*sizes) -> int:
+    return int(load_library().corr_gated_linear_workspace_bytes(*sizes))
+
+
+@functools.lru_cache(maxsize=1024)
+def _gated_backward_need(*sizes) -> int:
+    return int(load_library().corr_gated_linear_backward_workspace_bytes(*sizes))
+
+
+def _gated_weights(w, K: int) -> int:
+    N2 = _weights(w, K)
+    if N2 % 2:
+        raise ValueError("w must have an even number of rows: the gate's, then as many others")
+    return N2 // 2
+
+
+def corr_gated_linear_workspace_bytes(dtype: torch.dtype, M: int, N: int, K: int, x_stride: int | None = None) -> int:
+    return int(load_library().corr_gated_linear_workspace_bytes(_TYPES[dtype], M, N, K, K if x_stride is None else x_stride))
+
+
+def corr_gated_linear(x: torch.Tensor, w: torch.Tensor, bias: torch.Tensor | None = None, act: int = CORR_ACT_SILU,
+                      out: torch.Tensor | None = None, preact: torch.Tensor | None = None,
+                      workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """act(x wg^T + bg) * (x wu^T + bu).  x: [..., K] with contiguous, evenly spaced rows; w: [2 N, K], the gate's rows first, both float32, bfloat16
+    or float16 (16-bit ones start on a 4-byte border); bias: float32 [2 N]; out: [..., N].  preact: a contiguous [..., 2 N] that receives
+    both sums (corr_gated_linear_backward reads it)."""
+    lib = _lib or load_library()
+    device = _on_device(x, "x")
+    dtype = x.dtype
+    code = _type_of(x, "x")
+    M, K, xs = _rows(x, "x")
+    N = _gated_weights(w, K)
+    pw = _dense(w, "w", dtype, device, w.shape)
+    shape = x.shape[:-1] + (N,)
+    pb = None if bias is None else _dense(bias, "bias", torch.float32, device, (2 * N,))
+    pz = None if preact is None else _dense(preact, "preact", dtype, device, x.shape[:-1] + (2 * N,))
+    if out is None:
+        out = _new(x, shape, dtype)
+        po, ys = _pointer(out), N
+    elif out.shape != shape:
+        raise ValueError("out must be %s" % list(shape))
+    else:
+        po, ys = _matrix(out, "out", dtype, device, M, N)
+    held, ws, size = _workspace(workspace, _gated_need(code, M, N, K, xs), x, device)
+    st = lib.corr_gated_linear(code, act, _pointer(x), xs, pw, pb, pz, po, ys, M, N, K, ws, size, _stream())
+    if st != CORR_OK:
+        raise CorrError(st, "corr_gated_linear")
+    return out
+
+
+def corr_gated_linear_backward_workspace_bytes(dtype: torch.dtype, M: int, N: int, K: int, x_stride: int | None = None) -> int:
+    return int(load_library().corr_gated_linear_backward_workspace_bytes(_TYPES[dtype], M, N, K, K if x_stride is None else x_stride))
+
+
+def corr_gated_linear_backward(x: torch.Tensor, w: torch.Tensor, d_out: torch.Tensor, preact: torch.Tensor, act: int = CORR_ACT_SILU,
+                               want_x: bool = True, want_w: bool = True, want_bias: bool = True, d_x: torch.Tensor | None = None,
+                               d_w: torch.Tensor | None = None, d_bias: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """(d_x, d_w, d_bias) of corr_gated_linear, None where not wanted: x's type for the first two, float32 [2 N] for the bias.  d_out: the gradient
+    of its result; preact: what corr_gated_linear stored."""
+    lib = _lib or load_library()
+    device = _on_device(x, "x")
+    dtype = x.dtype
+    code = _type_of(x, "x")
+    M, K, xs = _rows(x, "x")
+    N = _gated_weights(w, K)
+    pw = _dense(w, "w", dtype, device, w.shape)
+    pg, gs = _matrix(d_out, "d_out", dtype, device, M, N)
+    pz = _dense(preact, "preact", dtype, device, x.shape[:-1] + (2 * N,))
+    px = pdw = pdb = None
+    if want_x:
+        d_x = _new(x, x.shape, dtype) if d_x is None else d_x
+        px = _dense(d_x, "d_x", dtype, device, x.shape)
+    if want_w:
+        d_w = _new(x, w.shape, dtype) if d_w is None else d_w
+        pdw = _dense(d_w, "d_w", dtype, device, w.shape)
+    if want_bias:
+        d_bias = _new(x, (2 * N,), torch.float32) if d_bias is None else d_bias
+        pdb = _dense(d_bias, "d_bias", torch.float32, device, (2 * N,))
+    held, ws, size = _workspace(workspace, _gated_backward_need(code, M, N, K, xs), x, device)
+    st = lib.corr_gated_linear_backward(code, act, _pointer(x), xs, pw, pz, pg, gs, px, pdw, pdb, M, N, K, ws, size, _stream())
+    if st != CORR_OK:
+        raise CorrError(st, "corr_gated_linear_backward")
     return d_x if want_x else None, d_w if want_w else None, d_bias if want_bias else None
 
 

@@ -75,6 +75,31 @@ __device__ __forceinline__ void load_bias(const ProductArgs& g, float (&bias)[V]
 #pragma unroll
     for (int e = 0; e < V; ++e) bias[e] = g.bias && n + e < g.N ? g.bias[n + e] : 0.f;
 }
+// Gated: V elements of both halves.  g.N columns of y; bias and pre have 2 N, the gate's first.
+template <class T, int V>
+__device__ __forceinline__ void finish_gated(const ProductArgs& g, float (&gate)[V], float (&up)[V], const float (&bias)[2][V], int m, int n) {
+    const int left = g.N - n;
+    if (m >= g.M || left <= 0) return;
+#pragma unroll
+    for (int e = 0; e < V; ++e) { gate[e] += bias[0][e]; up[e] += bias[1][e]; }
+    if (g.pre) {
+        T* const z = (T*)g.pre + (int64_t)m * 2 * g.N + n;
+        store_some<T, V>(z, gate, left, g.past);
+        store_some<T, V>(z + g.N, up, left, g.past);
+    }
+    row_act_all(g.act, gate);
+#pragma unroll
+    for (int e = 0; e < V; ++e) gate[e] *= up[e];
+    store_some<T, V>((T*)g.y + (int64_t)m * g.ldy + n, gate, left, g.past);
+}
+template <int V>
+__device__ __forceinline__ void load_gated_bias(const ProductArgs& g, float (&bias)[2][V], int n) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        bias[0][e] = g.bias && n + e < g.N ? g.bias[n + e] : 0.f;
+        bias[1][e] = g.bias && n + e < g.N ? g.bias[g.N + n + e] : 0.f;
+    }
+}
 // A wave's FN x FM blocks of 16 x 16 (rows of the instruction's first operand are n: a lane has four consecutive n of one m), 16 rows
 // of C at a time by way of LDS, so that a lane gets 16 bytes of a row and eight (16) lanes a whole 128-byte line or more.  Straight from
 // the registers, in pieces of 8 bytes and one activation after the other, the widening product at 1080p took 95 us.
@@ -116,6 +141,54 @@ __device__ __forceinline__ void finish_wave(const ProductArgs& g, f32x4 (&acc)[F
     }
 }
 
+// Gated: even blocks of columns are the gate's, odd ones the other half's of the same columns of y, from column n0 on.
+template <class T, int FM, int FN>
+__device__ __forceinline__ void finish_gated_wave(const ProductArgs& g, f32x4 (&acc)[FN][FM], float* box, int m0, int n0, int lane, int split, int splits) {
+    constexpr int LD = 16 * FN + 4;
+    const int lr = lane & 15, lg = lane >> 4;
+    auto by_rows = [&](auto width, auto f) {
+        constexpr int V = decltype(width)::value, LANES = 8 * FN / V, ROWS = 64 / LANES;
+        const int c = lane % LANES * V, r0 = lane / LANES, at = c / 16 * 32 + c % 16;
+#pragma unroll
+        for (int j = 0; j < FM; ++j) {
+#pragma unroll
+            for (int i = 0; i < FN; ++i) *reinterpret_cast<f32x4*>(box + lr * LD + 16 * i + 4 * lg) = acc[i][j];
+            asm volatile("" ::: "memory");               // one wave: its LDS accesses are done in order
+#pragma unroll
+            for (int r = r0; r < 16; r += ROWS) {
+                float v[2][V];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < V; e += 4) {
+                        const f32x4 x = *reinterpret_cast<const f32x4*>(box + r * LD + at + 16 * h + e);
+                        v[h][e] = x[0]; v[h][e + 1] = x[1]; v[h][e + 2] = x[2]; v[h][e + 3] = x[3];
+                    }
+                f(v, m0 + 16 * j + r, n0 + c);
+            }
+            asm volatile("" ::: "memory");
+        }
+    };
+    if (splits > 1) {
+        by_rows(std::integral_constant<int, 4>{}, [&](float (&v)[2][4], int m, int n) {
+            if (m >= g.M || n >= g.N) return;
+            float* const p = g.part + ((int64_t)split * g.M + m) * 2 * g.N + n;
+            store_some<float, 4>(p, v[0], g.N - n);
+            store_some<float, 4>(p + g.N, v[1], g.N - n);
+        });
+    } else {
+        constexpr int V = 16 / sizeof(T);
+        float bias[2][V];
+        load_gated_bias(g, bias, n0 + lane % (8 * FN / V) * V);
+        by_rows(std::integral_constant<int, V>{}, [&](float (&v)[2][V], int m, int n) { finish_gated<T, V>(g, v[0], v[1], bias, m, n); });
+    }
+}
+
+// Gated: row r of a tile of weights is row in_half(r) of the gate's weights or (second_half(r)) of the other half's, in turns of 16, so that a
+// lane's blocks 2 i and 2 i + 1 belong to the same columns of y.
+__device__ __forceinline__ int in_half(int r) { return (r >> 5) * 16 + (r & 15); }
+__device__ __forceinline__ int second_half(int r) { return r >> 4 & 1; }
+
 // ------------------------------------------------------------------------------------------------ 16-bit operands
 // A workgroup makes BM x BN elements in steps of BK k.  Tiles lie in LDS as they are stored, in two halves that take turns: while
 // one is multiplied, the next step's 16-byte pieces land in the other.
@@ -130,7 +203,7 @@ template <int R> __device__ __forceinline__ int turn(int k) {
 }
 // piece p of row r of BK elements: where it lies
 template <int BK> __device__ __forceinline__ int place(int r, int p) { return BK == 64 ? p ^ (r & 7) : p ^ (r >> 1 & 3); }
-template <bool ROWS, int R, int WAVES, int BK>
+template <bool ROWS, int R, int WAVES, int BK, bool GATED = false>
 struct Loader16 {
     static constexpr int PIECES = R * BK * 2 / (1024 * WAVES);
     unsigned voff[PIECES];
@@ -143,7 +216,7 @@ struct Loader16 {
                 voff[q] = (unsigned)(k * ld * 2) + ((((piece >> 1) ^ turn<R>(k)) << 1) | (piece & 1)) * 16;
             } else {
                 const int row = p / (2 * BK), piece = (p >> 4) % (BK / 8);
-                voff[q] = (unsigned)(row * ld * 2) + place<BK>(row, piece) * 16;
+                voff[q] = (unsigned)((GATED ? in_half(row) : row) * ld * 2) + place<BK>(row, piece) * 16;
             }
         }
     }
@@ -151,6 +224,13 @@ struct Loader16 {
         const i32x4 rsrc = w.rsrc();
 #pragma unroll
         for (int q = 0; q < PIECES; ++q) dma16(rsrc, lds + (q * WAVES + wave) * 1024, voff[q]);
+    }
+    // a load's 1024 bytes are rows of one half
+    __device__ __forceinline__ void issue(const Window& gate, const Window& up, unsigned lds, int wave) const {
+        const i32x4 one = gate.rsrc(), two = up.rsrc();
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q)
+            dma16(second_half((q * WAVES + wave) * (512 / BK)) ? two : one, lds + (q * WAVES + wave) * 1024, voff[q]);
     }
 };
 // F fragments of 16 rows from row `base` on: lane (lr, lg) holds k = 8 lg .. + 7 of a row of 32 k.
@@ -192,7 +272,8 @@ __device__ __forceinline__ V keep_first(V v, int left) {
 // loads (fp16 gradients with silu, and with relu: 14570 x 243 -> 126: 51 and 41 us; 32400 x 256 -> 1024: 153 and 104; 4096^3: 503 and
 // 265).  A sum of the low part's products that is not finite says that an element of the second operand is not (fp16's values
 // cannot overflow it): then the high part alone gives what the whole would.
-template <class T, bool AR, bool BR, int BM, int BN, int WM, int WN, int BK, bool TWO>
+// GATED: the second operand's rows come in turns from its two halves of g.N (BN / 2 columns of y a tile).
+template <class T, bool AR, bool BR, int BM, int BN, int WM, int WN, int BK, bool TWO, bool GATED = false>
 __global__ __launch_bounds__(64 * WM * WN, BK == 32 ? 4 : 2) void product16_kernel(ProductArgs g, int tm, int tn, int splits, int steps_per) {
     constexpr int WAVES = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
     constexpr int A_BYTES = BM * BK * 2, HALF = (BM + BN) * BK * 2;
@@ -202,12 +283,14 @@ __global__ __launch_bounds__(64 * WM * WN, BK == 32 ? 4 : 2) void product16_kern
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lg = lane >> 4;
     int mt, nt, split;
     tile_of(blockIdx.x, tm, tn, splits, mt, nt, split);
-    const int m0 = mt * BM, n0 = nt * BN;
+    const int m0 = mt * BM, n0 = nt * (GATED ? BN / 2 : BN);
     const int k0 = split * steps_per * 64, k_left = min(g.K - k0, steps_per * 64);
     const int whole = k_left / BK, tail = k_left % BK, steps = whole + (tail != 0);
     Window wa = window<AR, 2, BK>(TWO ? g.a_lo : g.a, g.lda, g.M, g.K, m0, k0), wb = window<BR, 2, BK>(g.b, g.ldb, g.N, g.K, n0, k0);
+    Window wu = wb;
+    if constexpr (GATED) wu.at += (int64_t)g.N * g.ldb * 2;
     Loader16<AR, BM, WAVES, BK> la;
-    Loader16<BR, BN, WAVES, BK> lb;
+    Loader16<BR, BN, WAVES, BK, GATED> lb;
     la.plan(wave, lane, g.lda);
     lb.plan(wave, lane, g.ldb);
     const int wm = (wave % WM) * TM, wn = (wave / WM) * TN;
@@ -218,12 +301,13 @@ __global__ __launch_bounds__(64 * WM * WN, BK == 32 ? 4 : 2) void product16_kern
     f32x4 acc[FN][FM] = {};
     auto ask = [&](int half) {
         la.issue(wa, lds_at + half * HALF, wave);
-        lb.issue(wb, lds_at + half * HALF + A_BYTES, wave);
+        if constexpr (GATED) { lb.issue(wb, wu, lds_at + half * HALF + A_BYTES, wave); wu.next(); }
+        else lb.issue(wb, lds_at + half * HALF + A_BYTES, wave);
         wa.next(); wb.next();
     };
     // A wave past the result's borders only helps to load (129600 x 256 -> 324: 52 -> 49 us).  Loads stay ahead of a step's products where k
     // is contiguous (129600 x 320 -> 256: 43 -> 35 us; 8192^3 with residual: 915 and 922); where the rows are, mixed is better (129600 x 324 x 256: 40 and 42).
-    const bool busy = AR || (n0 + wn < g.N && m0 + wm < g.M);
+    const bool busy = AR || (n0 + (GATED ? wn / 2 : wn) < g.N && m0 + wm < g.M);
     auto multiply = [&](int half, auto last) {
         if constexpr (!AR) __builtin_amdgcn_sched_barrier(0);
         if (!busy) return;
@@ -284,7 +368,9 @@ __global__ __launch_bounds__(64 * WM * WN, BK == 32 ? 4 : 2) void product16_kern
             for (int j = 0; j < FM; ++j) acc[i][j] *= 1.f / HIGH_PART;
     }
     __syncthreads();                                     // the tiles have been read
-    if (busy) finish_wave<T, FM, FN>(g, acc, (float*)smem + wave * box_floats<FN>(), m0 + wm, n0 + wn, lane, split, splits);
+    if constexpr (GATED) {
+        if (busy) finish_gated_wave<T, FM, FN>(g, acc, (float*)smem + wave * box_floats<FN>(), m0 + wm, n0 + wn / 2, lane, split, splits);
+    } else if (busy) finish_wave<T, FM, FN>(g, acc, (float*)smem + wave * box_floats<FN>(), m0 + wm, n0 + wn, lane, split, splits);
 }
 
 // ------------------------------------------------------------------------------------------------ fp32 operands
@@ -297,7 +383,7 @@ __global__ __launch_bounds__(64 * WM * WN, BK == 32 ? 4 : 2) void product16_kern
 // 518400 x 1024 -> 256 is 1290 us of products and 109 of stores, 1399 in all; x 324 -> 256: 438 and 109, 600 to 710 us (as the clock falls under
 // sustained work: 1.8 GHz, matrix instructions in 43 % of the cycles, splitting in 28 %).  Without loads that took 531 us, with one
 // product of six 472.  Two workgroups a compute unit; a third spills (838 us), and so does a second set of loads on their way.
-template <bool ROWS, int R, int NT>
+template <bool ROWS, int R, int NT, bool GATED = false>
 struct Loader32 {
     static constexpr int PIECES = R * 8 / NT;
     unsigned voff[PIECES], dst[PIECES];
@@ -315,7 +401,7 @@ struct Loader32 {
             } else {
                 const int row = p >> 3, c = p & 7;
                 k[q] = c * 4;
-                voff[q] = (unsigned)(row * ld * 4) + c * 16;
+                voff[q] = (unsigned)((GATED ? in_half(row) : row) * ld * 4) + c * 16;
                 dst[q] = row * 64 + (((c >> 1) ^ (row >> 1 & 3)) << 4) + (c & 1) * 8;
             }
         }
@@ -325,6 +411,14 @@ struct Loader32 {
 #pragma unroll
         for (int q = 0; q < PIECES; ++q)
             x[q] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)voff[q], 0, 0));
+    }
+    // a wave's 64 pieces are eight rows of one half
+    __device__ __forceinline__ void ask(const Window& gate, const Window& up, int wave) {
+#pragma unroll
+        for (int q = 0; q < PIECES; ++q) {
+            const __amdgpu_buffer_rsrc_t r = second_half((q * NT / 64 + wave) * 8) ? up.buffer() : gate.buffer();
+            x[q] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)voff[q], 0, 0));
+        }
     }
     __device__ __forceinline__ void cut(int left) {      // the last step of rows with k contiguous
         if constexpr (!ROWS) {
@@ -371,7 +465,7 @@ struct Reader32 {
     }
 };
 
-template <bool AR, bool BR, int BM, int BN, int WM, int WN>
+template <bool AR, bool BR, int BM, int BN, int WM, int WN, bool GATED = false>
 __global__ __launch_bounds__(64 * WM * WN, 2) void product32_kernel(ProductArgs g, int tm, int tn, int splits, int steps_per) {
     constexpr int NT = 64 * WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
     constexpr int PA = BM * 64, PB = BN * 64;
@@ -380,11 +474,13 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product32_kernel(ProductArgs 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lg = lane >> 4;
     int mt, nt, split;
     tile_of(blockIdx.x, tm, tn, splits, mt, nt, split);
-    const int m0 = mt * BM, n0 = nt * BN;
+    const int m0 = mt * BM, n0 = nt * (GATED ? BN / 2 : BN);
     const int k0 = split * steps_per * 32, k_left = min(g.K - k0, steps_per * 32), steps = (k_left + 31) >> 5;
     Window wa = window<AR, 4, 32>(g.a, g.lda, g.M, g.K, m0, k0), wb = window<BR, 4, 32>(g.b, g.ldb, g.N, g.K, n0, k0);
+    Window wu = wb;
+    if constexpr (GATED) wu.at += (int64_t)g.N * g.ldb * 4;
     Loader32<AR, BM, NT> la;
-    Loader32<BR, BN, NT> lb;
+    Loader32<BR, BN, NT, GATED> lb;
     la.plan(tid, g.lda);
     lb.plan(tid, g.ldb);
     const int wm = (wave % WM) * TM, wn = (wave / WM) * TN;
@@ -393,14 +489,20 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product32_kernel(ProductArgs 
     ra.plan(wm, lr, lg);
     rb.plan(wn, lr, lg);
     f32x4 acc[FN][FM] = {};
-    la.ask(wa); lb.ask(wb);
+    auto ask = [&] {
+        la.ask(wa);
+        if constexpr (GATED) lb.ask(wb, wu, wave);
+        else lb.ask(wb);
+    };
+    ask();
     auto step = [&](auto last) {
         if constexpr (decltype(last)::value) { la.cut(k_left - 32 * (steps - 1)); lb.cut(k_left - 32 * (steps - 1)); }
         __syncthreads();                                 // the last step's fragments have been read
         la.split(smem); lb.split(smem + 3 * PA);
         if constexpr (!decltype(last)::value) {
             wa.next(); wb.next();
-            la.ask(wa); lb.ask(wb);
+            if constexpr (GATED) wu.next();
+            ask();
         }
         __syncthreads();
         bf16x8 fa[3][FM], fb[3][FN];
@@ -425,20 +527,21 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product32_kernel(ProductArgs 
     // An infinity, a NaN or a value beyond bf16's range has no three parts (its remainder is infinity - infinity): what is
     // not finite here is taken from fp32 instructions instead, one k of a row per lane.
     float none = 0.f;                                    // NaN if any sum is not finite (past the borders anything may lie)
+    auto column = [&](int i) { return n0 + (GATED ? in_half(wn + 16 * i) : wn + 16 * i); };
 #pragma unroll
     for (int i = 0; i < FN; ++i)
 #pragma unroll
         for (int j = 0; j < FM; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                none = fmaf(m0 + wm + 16 * j + lr < g.M && n0 + wn + 16 * i + 4 * lg + e < g.N ? acc[i][j][e] : 0.f, 0.f, none);
+                none = fmaf(m0 + wm + 16 * j + lr < g.M && column(i) + 4 * lg + e < g.N ? acc[i][j][e] : 0.f, 0.f, none);
     if (__any(none != 0.f)) {
         const float* const A = (const float*)g.a;
         const float* const B = (const float*)g.b;
         for (int i = 0; i < FN; ++i)
             for (int j = 0; j < FM; ++j) {
                 f32x4 plain = {};
-                const int64_t m = min(m0 + wm + 16 * j + lr, g.M - 1), n = min(n0 + wn + 16 * i + lr, g.N - 1);
+                const int64_t m = min(m0 + wm + 16 * j + lr, g.M - 1), n = min(column(i) + lr, g.N - 1) + (GATED && (i & 1) ? g.N : 0);
                 for (int k = 0; k < k_left; k += 4) {
                     float xa = 0.f, xb = 0.f;
                     if (k + lg < k_left) {
@@ -458,7 +561,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void product32_kernel(ProductArgs 
             }
     }
     __syncthreads();                                     // the planes have been read
-    finish_wave<float, FM, FN>(g, acc, (float*)smem + wave * box_floats<FN>(), m0 + wm, n0 + wn, lane, split, splits);
+    if constexpr (GATED) finish_gated_wave<float, FM, FN>(g, acc, (float*)smem + wave * box_floats<FN>(), m0 + wm, n0 + wn / 2, lane, split, splits);
+    else finish_wave<float, FM, FN>(g, acc, (float*)smem + wave * box_floats<FN>(), m0 + wm, n0 + wn, lane, split, splits);
 }
 
 // ------------------------------------------------------------------------------------------------ few rows
@@ -473,22 +577,51 @@ __device__ __forceinline__ typename Frag<T>::type few_load(const T* p, int left)
     for (int e = 0; e < 8; ++e) if (e < left) v[e] = p[e];
     return v;
 }
-template <class T, int WAVES, int MT>
+// The waves' sums in their order, and the epilogue.
+template <class T, int WAVES, int MT, bool GATED>
+__device__ __forceinline__ void few_finish(const ProductArgs& g, f32x4 (&sums)[WAVES][GATED ? 2 * MT : MT][64], int wave, int lane, int n0) {
+    const int lr = lane & 15, lg = lane >> 4;
+    for (int j = wave; j < MT; j += WAVES) {
+        f32x4 x = sums[0][j][lane];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) x += sums[w][j][lane];
+        float v[4] = {x[0], x[1], x[2], x[3]};
+        if constexpr (GATED) {
+            x = sums[0][MT + j][lane];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) x += sums[w][MT + j][lane];
+            float up[4] = {x[0], x[1], x[2], x[3]}, bias[2][4];
+            load_gated_bias(g, bias, n0 + 4 * lg);
+            finish_gated<T, 4>(g, v, up, bias, 16 * j + lr, n0 + 4 * lg);
+        } else {
+            float bias[4];
+            load_bias(g, bias, n0 + 4 * lg);
+            finish<T, 4>(g, v, bias, 16 * j + lr, n0 + 4 * lg);
+        }
+    }
+}
+// GATED: 16 columns of both halves, as MT more sums.
+template <class T, int WAVES, int MT, bool GATED = false>
 __global__ __launch_bounds__(64 * WAVES) void few_rows16_kernel(ProductArgs g) {
-    __shared__ f32x4 sums[WAVES][MT][64];
+    constexpr int H = GATED ? 2 : 1;
+    __shared__ f32x4 sums[WAVES][H * MT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, lg = lane >> 4;
     const int n0 = blockIdx.x * 16, n = n0 + lr;
-    const T* const W = (const T*)g.b + (int64_t)min(n, g.N - 1) * g.ldb;
+    const T* W[H];
+#pragma unroll
+    for (int h = 0; h < H; ++h) W[h] = (const T*)g.b + ((int64_t)min(n, g.N - 1) + (int64_t)h * g.N) * g.ldb;
     const T* X[MT];
 #pragma unroll
     for (int j = 0; j < MT; ++j) X[j] = (const T*)g.a + (int64_t)min(16 * j + lr, g.M - 1) * g.lda;
-    f32x4 acc[MT] = {};
-    constexpr int U = MT == 1 ? 4 : 2;                   // 32 k each
+    f32x4 acc[H * MT] = {};
+    constexpr int U = H * MT == 1 ? 4 : 2;               // 32 k each
     int k = wave * 32 * U + lg * 8;
     for (; k - lg * 8 + 32 * U <= g.K; k += WAVES * 32 * U) {
-        typename Frag<T>::type w[U], x[U][MT];
+        typename Frag<T>::type w[U][H], x[U][MT];
 #pragma unroll
-        for (int u = 0; u < U; ++u) w[u] = few_load<T>(W + k + 32 * u, 8);
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < H; ++h) w[u][h] = few_load<T>(W[h] + k + 32 * u, 8);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -496,25 +629,23 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows16_kernel(ProductArgs g) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int j = 0; j < MT; ++j) acc[j] = mma(w[u], x[u][j], acc[j]);
+            for (int h = 0; h < H; ++h)
+#pragma unroll
+                for (int j = 0; j < MT; ++j) acc[h * MT + j] = mma(w[u][h], x[u][j], acc[h * MT + j]);
     }
     for (int u = 0; u < U; ++u, k += 32) {               // the one wave whose turn the last, shorter stretch is
         if (k - lg * 8 >= g.K) break;
-        const typename Frag<T>::type w = few_load<T>(W + k, g.K - k);
 #pragma unroll
-        for (int j = 0; j < MT; ++j) acc[j] = mma(w, few_load<T>(X[j] + k, g.K - k), acc[j]);
+        for (int h = 0; h < H; ++h) {
+            const typename Frag<T>::type w = few_load<T>(W[h] + k, g.K - k);
+#pragma unroll
+            for (int j = 0; j < MT; ++j) acc[h * MT + j] = mma(w, few_load<T>(X[j] + k, g.K - k), acc[h * MT + j]);
+        }
     }
 #pragma unroll
-    for (int j = 0; j < MT; ++j) sums[wave][j][lane] = acc[j];
+    for (int j = 0; j < H * MT; ++j) sums[wave][j][lane] = acc[j];
     __syncthreads();
-    for (int j = wave; j < MT; j += WAVES) {
-        f32x4 x = sums[0][j][lane];
-#pragma unroll
-        for (int w = 1; w < WAVES; ++w) x += sums[w][j][lane];
-        float v[4] = {x[0], x[1], x[2], x[3]}, bias[4];
-        load_bias(g, bias, n0 + 4 * lg);
-        finish<T, 4>(g, v, bias, 16 * j + lr, n0 + 4 * lg);
-    }
+    few_finish<T, WAVES, MT, GATED>(g, sums, wave, lane, n0);
 }
 // fp32: v_mfma_f32_16x16x4_f32, whose four k are the same element of four lanes' 16 bytes.
 __device__ __forceinline__ f32x4 few_load32(const float* p, int left) {
@@ -524,22 +655,27 @@ __device__ __forceinline__ f32x4 few_load32(const float* p, int left) {
     for (int e = 0; e < 4; ++e) if (e < left) v[e] = p[e];
     return v;
 }
-template <int WAVES, int MT>
+template <int WAVES, int MT, bool GATED = false>
 __global__ __launch_bounds__(64 * WAVES) void few_rows32_kernel(ProductArgs g) {
-    __shared__ f32x4 sums[WAVES][MT][64];
+    constexpr int H = GATED ? 2 : 1;
+    __shared__ f32x4 sums[WAVES][H * MT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lr = lane & 15, lg = lane >> 4;
     const int n0 = blockIdx.x * 16, n = n0 + lr;
-    const float* const W = (const float*)g.b + (int64_t)min(n, g.N - 1) * g.ldb;
+    const float* W[H];
+#pragma unroll
+    for (int h = 0; h < H; ++h) W[h] = (const float*)g.b + ((int64_t)min(n, g.N - 1) + (int64_t)h * g.N) * g.ldb;
     const float* X[MT];
 #pragma unroll
     for (int j = 0; j < MT; ++j) X[j] = (const float*)g.a + (int64_t)min(16 * j + lr, g.M - 1) * g.lda;
-    f32x4 acc[MT] = {};
-    constexpr int U = MT == 1 ? 4 : 2;                   // 16 k each
+    f32x4 acc[H * MT] = {};
+    constexpr int U = H * MT == 1 ? 4 : 2;               // 16 k each
     int k = wave * 16 * U + lg * 4;
     for (; k - lg * 4 + 16 * U <= g.K; k += WAVES * 16 * U) {
-        f32x4 w[U], x[U][MT];
+        f32x4 w[U][H], x[U][MT];
 #pragma unroll
-        for (int u = 0; u < U; ++u) w[u] = few_load32(W + k + 16 * u, 4);
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int h = 0; h < H; ++h) w[u][h] = few_load32(W[h] + k + 16 * u, 4);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -549,29 +685,28 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows32_kernel(ProductArgs g) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
 #pragma unroll
-                for (int j = 0; j < MT; ++j) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[u][e], x[u][j][e], acc[j], 0, 0, 0);
+                for (int h = 0; h < H; ++h)
+#pragma unroll
+                    for (int j = 0; j < MT; ++j)
+                        acc[h * MT + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[u][h][e], x[u][j][e], acc[h * MT + j], 0, 0, 0);
     }
     for (int u = 0; u < U; ++u, k += 16) {
         if (k - lg * 4 >= g.K) break;
-        const f32x4 w = few_load32(W + k, g.K - k);
 #pragma unroll
-        for (int j = 0; j < MT; ++j) {
-            const f32x4 x = few_load32(X[j] + k, g.K - k);
+        for (int h = 0; h < H; ++h) {
+            const f32x4 w = few_load32(W[h] + k, g.K - k);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[e], x[e], acc[j], 0, 0, 0);
+            for (int j = 0; j < MT; ++j) {
+                const f32x4 x = few_load32(X[j] + k, g.K - k);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[h * MT + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[e], x[e], acc[h * MT + j], 0, 0, 0);
+            }
         }
     }
 #pragma unroll
-    for (int j = 0; j < MT; ++j) sums[wave][j][lane] = acc[j];
+    for (int j = 0; j < H * MT; ++j) sums[wave][j][lane] = acc[j];
     __syncthreads();
-    for (int j = wave; j < MT; j += WAVES) {
-        f32x4 x = sums[0][j][lane];
-#pragma unroll
-        for (int w = 1; w < WAVES; ++w) x += sums[w][j][lane];
-        float v[4] = {x[0], x[1], x[2], x[3]}, bias[4];
-        load_bias(g, bias, n0 + 4 * lg);
-        finish<float, 4>(g, v, bias, 16 * j + lr, n0 + 4 * lg);
-    }
+    few_finish<float, WAVES, MT, GATED>(g, sums, wave, lane, n0);
 }
 
 // ------------------------------------------------------------------------------------------------ splits, packing, slopes
@@ -607,8 +742,32 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs g, int splits) {
     load_bias(g, bias, n);
     finish<T, 4>(g, v, bias, (int)m, n);
 }
+// Gated: the two halves' sums.
+template <class T>
+__global__ __launch_bounds__(256) void join_gated_kernel(ProductArgs g, int splits) {
+    const int quads = (g.N + 3) >> 2;
+    const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x, m = q / quads, plane = (int64_t)g.M * 2 * g.N;
+    if (m >= g.M) return;
+    const int n = (int)(q - m * quads) * 4;
+    const float* p = g.part + m * 2 * g.N + n;
+    float sum[2][4] = {}, bias[2][4];
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s, p += plane) {
+        float v[4], w[4];
+        load_some<float, 4>(p, v, g.N - n);
+        load_some<float, 4>(p + g.N, w, g.N - n);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { sum[0][e] += v[e]; sum[1][e] += w[e]; }
+    }
+    load_gated_bias(g, bias, n);
+    finish_gated<T, 4>(g, sum[0], sum[1], bias, (int)m, n);
+}
 template <class T>
 void join(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
+    if (g.gated) {
+        hipLaunchKernelGGL((join_gated_kernel<T>), dim3((unsigned)(((int64_t)g.M * ((g.N + 3) / 4) + 255) / 256)), dim3(256), 0, s, g, p.splits);
+        return;
+    }
     const int64_t quads = (int64_t)g.M * ((g.N + 3) / 4);
     if (p.splits >= 8) hipLaunchKernelGGL((join_kernel<T, 8>), dim3((unsigned)((quads + 31) / 32)), dim3(256), 0, s, g, p.splits);
     else hipLaunchKernelGGL((join_kernel<T, 1>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, s, g, p.splits);
@@ -698,8 +857,78 @@ __global__ __launch_bounds__(SLOPE_THREADS) void slope_kernel(int act, const T* 
     }
 }
 
+// Gated: dz of both halves, [M][2 N]: d_y up act'(gate) and d_y act(gate), rounded (fp16: in two parts) as above, and their column sums.  fp16's parts
+// hold values up to 1.3e5.
+template <class T, int V>
+__global__ __launch_bounds__(SLOPE_THREADS) void slope_gated_kernel(int act, const T* __restrict__ dy, int64_t ld_dy, const T* __restrict__ z,
+                                                                   T* __restrict__ dz, T* __restrict__ dz_lo, int64_t ld_dz, float* __restrict__ part,
+                                                                   int64_t M, int N, int ct, int64_t rows_per) {
+    __shared__ float sums[2][SLOPE_THREADS][V];
+    const int tid = threadIdx.x, c = tid % ct, rt = SLOPE_THREADS / ct, r0 = tid / ct;
+    const int n = (blockIdx.x * ct + c) * V, left = N - n;
+    const int64_t lo = (int64_t)blockIdx.y * rows_per, hi = min(M, lo + rows_per);
+    float sum[2][V] = {};
+    if (left > 0)
+        for (int64_t m = lo + r0; m < hi; m += rt) {
+            float d[2][V], gate[V], up[V];
+            load_some<T, V>(dy + m * ld_dy + n, d[0], left);
+            load_some<T, V>(z + m * 2 * N + n, gate, left);
+            load_some<T, V>(z + m * 2 * N + N + n, up, left);
+            float slope[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) slope[e] = gate[e];
+            row_act_all(act, gate);
+            row_slope_all(act, slope);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                d[1][e] = d[0][e] * gate[e];
+                d[0][e] *= up[e] * slope[e];
+                sum[0][e] += d[0][e];
+                sum[1][e] += d[1][e];
+            }
+            if (!dz) continue;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t to = m * ld_dz + h * N + n;
+                if constexpr (std::is_same<T, _Float16>::value) {
+                    float lo_part[V];
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const float x = HIGH_PART * d[h][e], r = x - (float)(T)x;
+                        lo_part[e] = r == r ? LOW_PART * r : 0.f;        // an infinity or NaN is in the high part
+                        d[h][e] = x;
+                    }
+                    store_some<T, V>(dz_lo + to, lo_part, left);
+                }
+                store_some<T, V>(dz + to, d[h], left);
+            }
+        }
+    if (!part) return;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < V; ++e) sums[h][tid][e] = sum[h][e];
+    __syncthreads();
+    if (r0 == 0 && left > 0) {
+        for (int r = 1; r < rt; ++r)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < V; ++e) sum[h][e] += sums[h][r * ct + c][e];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) store_some<float, V>(part + (int64_t)blockIdx.y * 2 * N + h * N + n, sum[h], left);
+    }
+}
+
 template <class T, bool AR, bool BR, int BM, int BN, int WM, int WN, int BK>
 void run16(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
+    if constexpr (!AR && !BR) {
+        if (g.gated) {
+            const int tm = cdiv(g.M, BM), tn = cdiv(g.N, BN / 2);
+            hipLaunchKernelGGL((product16_kernel<T, AR, BR, BM, BN, WM, WN, BK, false, true>), dim3(tm * tn * p.splits), dim3(64 * WM * WN), 0, s, g, tm, tn, p.splits, p.steps);
+            return;
+        }
+    }
     const int tm = cdiv(g.M, BM), tn = cdiv(g.N, BN);
     if constexpr (std::is_same<T, _Float16>::value && BR) {
         if (g.a_lo) {
@@ -719,6 +948,11 @@ void run16(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
 template <class T>
 void few16(const ProductArgs& g, hipStream_t s) {
     const dim3 grid(cdiv(g.N, 16));
+    if (g.gated) {
+        if (g.M <= 16) hipLaunchKernelGGL((few_rows16_kernel<T, 8, 1, true>), grid, dim3(512), 0, s, g);
+        else hipLaunchKernelGGL((few_rows16_kernel<T, 8, 2, true>), grid, dim3(512), 0, s, g);
+        return;
+    }
 #define FEW16(WAVES, MT) hipLaunchKernelGGL((few_rows16_kernel<T, WAVES, MT>), grid, dim3(64 * WAVES), 0, s, g)
     const bool narrow = g.N <= 4096;
     if (g.M <= 16) { if (narrow) FEW16(8, 1); else FEW16(4, 1); }
@@ -735,6 +969,14 @@ void product16(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
 }
 template <bool AR, bool BR>
 void run32(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
+    if constexpr (!AR && !BR) {
+        if (g.gated) {
+            const int edge = p.tile == TILE_64 ? 64 : 128, tm = cdiv(g.M, edge), tn = cdiv(g.N, edge / 2);
+            if (edge == 64) hipLaunchKernelGGL((product32_kernel<AR, BR, 64, 64, 2, 2, true>), dim3(tm * tn * p.splits), dim3(256), 0, s, g, tm, tn, p.splits, p.steps);
+            else hipLaunchKernelGGL((product32_kernel<AR, BR, 128, 128, 2, 2, true>), dim3(tm * tn * p.splits), dim3(256), 0, s, g, tm, tn, p.splits, p.steps);
+            return;
+        }
+    }
     if (p.tile == TILE_64) {
         const int tm = cdiv(g.M, 64), tn = cdiv(g.N, 64);
         hipLaunchKernelGGL((product32_kernel<AR, BR, 64, 64, 2, 2>), dim3(tm * tn * p.splits), dim3(256), 0, s, g, tm, tn, p.splits, p.steps);
@@ -746,7 +988,9 @@ void run32(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
 void product32(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
     if (p.tile == TILE_FEW) {
         const dim3 grid(cdiv(g.N, 16));
-        if (g.M <= 16) hipLaunchKernelGGL((few_rows32_kernel<8, 1>), grid, dim3(512), 0, s, g);
+        if (g.gated && g.M <= 16) hipLaunchKernelGGL((few_rows32_kernel<8, 1, true>), grid, dim3(512), 0, s, g);
+        else if (g.gated) hipLaunchKernelGGL((few_rows32_kernel<8, 2, true>), grid, dim3(512), 0, s, g);
+        else if (g.M <= 16) hipLaunchKernelGGL((few_rows32_kernel<8, 1>), grid, dim3(512), 0, s, g);
         else hipLaunchKernelGGL((few_rows32_kernel<8, 2>), grid, dim3(512), 0, s, g);
     } else if (!g.a_rows && !g.b_rows) run32<false, false>(g, p, s);
     else if (!g.a_rows) run32<false, true>(g, p, s);
@@ -800,7 +1044,7 @@ void product_tile(const ProductPlan& p, int& rows, int& cols) {
 
 hipError_t launch_product(const ProductArgs& args, hipStream_t s) {
     ProductArgs g = args;
-    const ProductPlan p = product_plan(g.type, g.a_rows, g.b_rows, g.M, g.N, g.K);
+    const ProductPlan p = product_plan(g.type, g.a_rows, g.b_rows, g.M, g.gated ? 2 * g.N : g.N, g.K);
     // A result larger than half of the memory-side cache goes past the caches, so that the operands stay in them (259200 x 1024 -> 128
     // bf16: 137 -> 119 us); whole lines only (rows of 648 bytes: 43 -> 46 us).
     const int64_t row = g.ldy * corr_elem_bytes(g.type);
@@ -838,5 +1082,24 @@ hipError_t launch_slope(corr_dtype t, int act, const void* dy, int64_t ld_dy, co
     if (t == CORR_TYPE_F32) slope<float, 4>(act, dy, ld_dy, z, dz, dz_lo, ld_dz, part, M, N, s);
     else if (t == CORR_TYPE_BF16) slope<__bf16, 8>(act, dy, ld_dy, z, dz, dz_lo, ld_dz, part, M, N, s);
     else slope<_Float16, 8>(act, dy, ld_dy, z, dz, dz_lo, ld_dz, part, M, N, s);
+    return hipGetLastError();
+}
+
+namespace {
+template <class T, int V>
+void slope_gated(int act, const void* dy, int64_t ld_dy, const void* z, void* dz, void* dz_lo, int64_t ld_dz, float* part, int64_t M, int N, hipStream_t s) {
+    int ct = 1;
+    while (ct < SLOPE_THREADS && ct * V < N) ct *= 2;
+    const int parts = slope_parts(M);
+    hipLaunchKernelGGL((slope_gated_kernel<T, V>), dim3(cdiv(N, ct * V), parts), dim3(SLOPE_THREADS), 0, s, act, (const T*)dy, ld_dy, (const T*)z,
+                       (T*)dz, (T*)dz_lo, ld_dz, part, M, N, ct, (M + parts - 1) / parts);
+}
+}  // namespace
+
+hipError_t launch_slope_gated(corr_dtype t, int act, const void* dy, int64_t ld_dy, const void* z, void* dz, void* dz_lo, int64_t ld_dz,
+                              float* part, int64_t M, int N, hipStream_t s) {
+    if (t == CORR_TYPE_F32) slope_gated<float, 4>(act, dy, ld_dy, z, dz, dz_lo, ld_dz, part, M, N, s);
+    else if (t == CORR_TYPE_BF16) slope_gated<__bf16, 8>(act, dy, ld_dy, z, dz, dz_lo, ld_dz, part, M, N, s);
+    else slope_gated<_Float16, 8>(act, dy, ld_dy, z, dz, dz_lo, ld_dz, part, M, N, s);
     return hipGetLastError();
 }

@@ -51,6 +51,40 @@ BackwardLayout backward_layout(corr_dtype t, corr_activation act, int64_t M, int
     return l;
 }
 
+// d_x = dz w and d_w = dz^T x, each if wanted.
+hipError_t gradient_products(corr_dtype type, const BackwardLayout& l, const void* dz, int64_t ld_dz, const void* x, int64_t x_stride, const void* w,
+                             void* d_x, void* d_w, int64_t M, int64_t N, int64_t K, char* ws, hipStream_t s) {
+    hipError_t e = launch_pack16({x, x_stride, ws + l.x, up8(K), l.pack_x && d_w ? M : 0, K}, {w, K, ws + l.w, up8(K), l.pack_w && d_x ? N : 0, K}, s);
+    ProductArgs p = {};
+    p.type = type; p.act = CORR_ACT_NONE;
+    p.a = dz; p.lda = ld_dz;
+    if (l.two) p.a_lo = ws + l.dz_lo;
+    p.part = reinterpret_cast<float*>(ws + l.part);
+    if (d_x && e == hipSuccess) {
+        p.b = w; p.ldb = K; p.b_rows = 1;
+        if (l.pack_w) { p.b = ws + l.w; p.ldb = up8(K); }
+        p.M = (int)M; p.N = (int)K; p.K = (int)N;
+        p.y = d_x; p.ldy = K;
+        e = launch_product(p, s);
+    }
+    if (d_w && e == hipSuccess) {
+        p.b = x; p.ldb = x_stride; p.a_rows = p.b_rows = 1;
+        if (l.pack_x) { p.b = ws + l.x; p.ldb = up8(K); }
+        p.M = (int)N; p.N = (int)K; p.K = (int)M;
+        p.y = d_w; p.ldy = K;
+        e = launch_product(p, s);
+    }
+    return e;
+}
+
+corr_status check_gated(corr_dtype type, corr_activation act, int64_t M, int64_t N, int64_t K) {
+    return N > MAX_COLS ? CORR_ERR_UNSUPPORTED : check_linear(type, act, M, 2 * N, K);
+}
+// dz is always a matrix of its own, and for fp16 in two parts.
+BackwardLayout gated_backward_layout(corr_dtype t, int64_t M, int64_t N, int64_t K, int64_t x_stride) {
+    return backward_layout(t, CORR_ACT_SILU, M, 2 * N, K, x_stride, 2 * N);
+}
+
 corr_status check_norm(const corr_residual_norm_args* a) {
     if (!a || !known(a->stream_type) || !known(a->type) || !known(a->gate_act) || !known(a->post) || !known(a->pre)) return CORR_ERR_INVALID_ARG;
     if (a->stream_type != a->type && a->stream_type != CORR_TYPE_F32) return CORR_ERR_INVALID_ARG;
@@ -184,27 +218,85 @@ corr_status corr_linear_backward(corr_dtype type, corr_activation act, const voi
             e = launch_column_sums(sums, l.parts, 1, (int)N, o, s);
         }
     }
-    if (e == hipSuccess)
-        e = launch_pack16({x, x_stride, ws + l.x, up8(K), l.pack_x && d_w ? M : 0, K}, {w, K, ws + l.w, up8(K), l.pack_w && d_x ? N : 0, K}, s);
+    if (e == hipSuccess) e = gradient_products(type, l, dz, ld_dz, x, x_stride, w, d_x, d_w, M, N, K, ws, s);
+    return e == hipSuccess ? CORR_OK : CORR_ERR_HIP;
+}
+
+size_t corr_gated_linear_workspace_bytes(corr_dtype type, int64_t M, int64_t N, int64_t K, int64_t x_stride) {
+    if (check_gated(type, CORR_ACT_NONE, M, N, K) != CORR_OK || M == 0) return 0;
+    return linear_layout(type, M, 2 * N, K, x_stride).total;
+}
+
+corr_status corr_gated_linear(corr_dtype type, corr_activation act, const void* x, int64_t x_stride, const void* w, const float* bias,
+                              void* preact, void* y, int64_t y_stride, int64_t M, int64_t N, int64_t K,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+    corr_status st = check_gated(type, act, M, N, K);
+    if (st != CORR_OK) return st;
+    if (M == 0) return CORR_OK;
+    if (!x || !w || !y || x_stride < K || y_stride < N) return CORR_ERR_INVALID_ARG;
+    if (x_stride > MAX_COLS || y_stride > MAX_COLS) return CORR_ERR_UNSUPPORTED;
+    const int es = corr_elem_bytes(type);
+    if (!on(x, 4) || !on(w, 4) || !on(bias, 4) || !on(preact, es) || !on(y, es)) return CORR_ERR_INVALID_ARG;
+    const LinearLayout l = linear_layout(type, M, 2 * N, K, x_stride);
+    if (l.total && (!workspace || workspace_bytes < l.total || !on(workspace, 16))) return CORR_ERR_INVALID_ARG;
+    const Range out[] = {range(y, M, N, y_stride, es), range(preact, M, 2 * N, 2 * N, es), range(l.total ? workspace : nullptr, 1, (int64_t)l.total, 0, 1)};
+    const Range in[] = {range(x, M, K, x_stride, es), range(w, 2 * N, K, K, es), range(bias, 1, 2 * N, 2 * N, 4)};
+    if (any_overlap(out, in)) return CORR_ERR_INVALID_ARG;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    char* const ws = static_cast<char*>(workspace);
     ProductArgs p = {};
-    p.type = type; p.act = CORR_ACT_NONE;
-    p.a = dz; p.lda = ld_dz;
-    if (l.two) p.a_lo = ws + l.dz_lo;
+    p.type = type; p.act = act; p.gated = 1;
+    p.a = x; p.lda = x_stride;
+    p.b = w; p.ldb = K;
+    p.M = (int)M; p.N = (int)N; p.K = (int)K;
+    hipError_t e = launch_pack16({x, x_stride, ws + l.x, up8(K), l.pack_x ? M : 0, K}, {w, K, ws + l.w, up8(K), l.pack_w ? 2 * N : 0, K}, s);
+    if (l.pack_x) { p.a = ws + l.x; p.lda = up8(K); }
+    if (l.pack_w) { p.b = ws + l.w; p.ldb = up8(K); }
+    p.bias = bias; p.pre = preact; p.y = y; p.ldy = y_stride;
     p.part = reinterpret_cast<float*>(ws + l.part);
-    if (d_x && e == hipSuccess) {
-        p.b = w; p.ldb = K; p.b_rows = 1;
-        if (l.pack_w) { p.b = ws + l.w; p.ldb = up8(K); }
-        p.M = (int)M; p.N = (int)K; p.K = (int)N;
-        p.y = d_x; p.ldy = K;
-        e = launch_product(p, s);
+    if (e == hipSuccess) e = launch_product(p, s);
+    return e == hipSuccess ? CORR_OK : CORR_ERR_HIP;
+}
+
+size_t corr_gated_linear_backward_workspace_bytes(corr_dtype type, int64_t M, int64_t N, int64_t K, int64_t x_stride) {
+    if (check_gated(type, CORR_ACT_NONE, M, N, K) != CORR_OK || M == 0) return 0;
+    return gated_backward_layout(type, M, N, K, x_stride).total;
+}
+
+corr_status corr_gated_linear_backward(corr_dtype type, corr_activation act, const void* x, int64_t x_stride, const void* w,
+                                       const void* preact, const void* d_y, int64_t d_y_stride, void* d_x, void* d_w, float* d_bias,
+                                       int64_t M, int64_t N, int64_t K, void* workspace, size_t workspace_bytes, void* stream) {
+    corr_status st = check_gated(type, act, M, N, K);
+    if (st != CORR_OK) return st;
+    const int es = corr_elem_bytes(type);
+    if (!on(d_x, es) || !on(d_w, es) || !on(d_bias, 4)) return CORR_ERR_INVALID_ARG;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t e = hipSuccess;
+    if (M == 0) {
+        e = launch_zero(d_w, (size_t)2 * N * K * es, s);
+        if (e == hipSuccess) e = launch_zero(d_bias, (size_t)2 * N * 4, s);
+        return e == hipSuccess ? CORR_OK : CORR_ERR_HIP;
     }
-    if (d_w && e == hipSuccess) {
-        p.b = x; p.ldb = x_stride; p.a_rows = p.b_rows = 1;
-        if (l.pack_x) { p.b = ws + l.x; p.ldb = up8(K); }
-        p.M = (int)N; p.N = (int)K; p.K = (int)M;
-        p.y = d_w; p.ldy = K;
-        e = launch_product(p, s);
+    if (!d_y || !preact || (d_w && !x) || (d_x && !w) || (d_w && x_stride < K) || d_y_stride < N) return CORR_ERR_INVALID_ARG;
+    if (x_stride > MAX_COLS || d_y_stride > MAX_COLS) return CORR_ERR_UNSUPPORTED;
+    if (!on(x, 4) || !on(w, 4) || !on(preact, es) || !on(d_y, es)) return CORR_ERR_INVALID_ARG;
+    const BackwardLayout l = gated_backward_layout(type, M, N, K, x_stride);
+    if (!workspace || workspace_bytes < l.total || !on(workspace, 16)) return CORR_ERR_INVALID_ARG;
+    const Range out[] = {range(d_x, M, K, K, es), range(d_w, 2 * N, K, K, es), range(d_bias, 1, 2 * N, 2 * N, 4),
+                         range(workspace, 1, (int64_t)l.total, 0, 1)};
+    const Range in[] = {range(d_w ? x : nullptr, M, K, x_stride, es), range(d_x ? w : nullptr, 2 * N, K, K, es),
+                        range(preact, M, 2 * N, 2 * N, es), range(d_y, M, N, d_y_stride, es)};
+    if (any_overlap(out, in)) return CORR_ERR_INVALID_ARG;
+    if (!d_x && !d_w && !d_bias) return CORR_OK;
+    char* const ws = static_cast<char*>(workspace);
+    float* const sums = d_bias ? reinterpret_cast<float*>(ws + l.sums) : nullptr;
+    e = launch_slope_gated(type, act, d_y, d_y_stride, preact, d_x || d_w ? ws + l.dz : nullptr, l.two ? ws + l.dz_lo : nullptr, up8(2 * N), sums,
+                           M, (int)N, s);
+    if (sums && e == hipSuccess) {
+        const ColumnSums o = {{d_bias, nullptr, nullptr, nullptr, nullptr}};
+        e = launch_column_sums(sums, l.parts, 1, (int)(2 * N), o, s);
     }
+    if (e == hipSuccess) e = gradient_products(type, l, ws + l.dz, up8(2 * N), x, x_stride, w, d_x, d_w, M, 2 * N, K, ws, s);
     return e == hipSuccess ? CORR_OK : CORR_ERR_HIP;
 }
 

@@ -15,6 +15,7 @@ struct ProductArgs {
     int64_t lda, ldb;
     int a_rows, b_rows;        // 1: rows contiguous ([k][m] / [k][n])
     int M, N, K;
+    int gated;                 // 1: b has 2 N rows, y = act(first N) * (second N); bias, pre and part have 2 N columns, no residual
     // epilogue: z = C + bias (to `pre`, if there), y = act(z) + res
     const float* bias;
     const void* res; int64_t ld_res;
@@ -38,6 +39,10 @@ hipError_t launch_pack16(const Pack16& one, const Pack16& two, hipStream_t s);
 int slope_parts(int64_t M);
 hipError_t launch_slope(corr_dtype t, int act, const void* dy, int64_t ld_dy, const void* z, void* dz, void* dz_lo, int64_t ld_dz,
                         float* part, int64_t M, int N, hipStream_t s);
+
+// gated: z is [M][2 N], dz and part have 2 N columns
+hipError_t launch_slope_gated(corr_dtype t, int act, const void* dy, int64_t ld_dy, const void* z, void* dz, void* dz_lo, int64_t ld_dz,
+                              float* part, int64_t M, int N, hipStream_t s);
 
 // ---- norms around a block (residual_norm.hip)
 struct NormArgs {

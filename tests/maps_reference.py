@@ -179,3 +179,47 @@ class GroupNorm:
             s, es = total(v, e, (0, 1))
             out.append((s.reshape(-1), (1.01 * es + rounded(s, F32)).reshape(-1)))
         return out
+
+
+def _gated_ops(dtype, K):
+    return 12 * K + 16 if dtype == F32 else 2 * K + 8
+
+
+def gated(x, w, b, name):
+    """(y, z, bound of y, bound of z) of corr_gated_linear: the sums as rows_reference's linear, the activation off by 16 EPS (|gate| + 1) with a slope of
+    at most 1.13, and their product."""
+    from rows_reference import act
+    dtype, N = x.dtype, w.shape[0] // 2
+    x, w = x.double().cpu(), w.double().cpu()
+    z, S = x @ w.t(), x.abs() @ w.abs().t()
+    if b is not None:
+        z, S = z + b.double().cpu(), S + b.double().cpu().abs()
+    ez = _gated_ops(dtype, x.shape[1]) * EPS * S
+    gate, up = z[:, :N], z[:, N:]
+    a = act(name, gate)
+    ea = 1.13 * ez[:, :N] + (16 * EPS * (gate.abs() + 1) if name != "none" else 0)
+    y = a * up
+    ey = ea * (up.abs() + ez[:, N:]) + a.abs() * ez[:, N:] + 2 * EPS * y.abs()
+    return y, z, 1.01 * ey + rounded(y, dtype), 1.01 * ez + rounded(z, dtype)
+
+
+def gated_backward(x, w, dy, z, name):
+    """((d_x, bound), (d_w, bound), (d_b, bound)).  dz as an operand: bf16 rounded once, fp16 in two parts of 22 bits together with a floor of 2^-36."""
+    from rows_reference import act, slope
+    dtype, (M, K), N = x.dtype, x.shape, w.shape[0] // 2
+    x, w, dy, z = (t.double().cpu() for t in (x, w, dy, z))
+    gate, up = z[:, :N], z[:, N:]
+    far = 16 * EPS * (2 + gate.abs()) if name != "none" else 0
+    dz = torch.cat([dy * up * slope(name, gate), dy * act(name, gate)], 1)
+    e = torch.cat([(dy * up).abs() * far, dy.abs() * far], 1) + 3 * EPS * dz.abs()
+    ep = e + {F32: 0.0, torch.bfloat16: U[torch.bfloat16], torch.float16: 2.0 ** -21}[dtype] * (dz.abs() + e)
+    if dtype == torch.float16:
+        ep = ep + 2.0 ** -35
+    per = 12 if dtype == F32 else 2
+
+    def product(a, b, ea, terms):
+        v = a @ b
+        return v, 1.01 * (ea @ b.abs() + (per * terms + 16) * EPS * ((a.abs() + ea) @ b.abs())) + rounded(v, dtype)
+    db = dz.sum(0)
+    return (product(dz, w, ep, 2 * N), product(dz.t(), x, ep.t(), M),
+            (db, 1.01 * (e.sum(0) + (M + 8) * EPS * dz.abs().sum(0)) + rounded(db, F32)))

@@ -139,3 +139,56 @@ def test_group_norm_workspace():
         assert need(torch.float32, 0, 5, 8, 2) == 0 and need(torch.float32, 1, 0, 8, 2) == 0 and need(torch.float32, 1, 5, 8, 3) == 0
         for B, P, C, G in ((1, 1, 1, 1), (2, 518400, 256, 32), (65535, 3, 64, 2), (1, 1 << 30, 8, 8), (512, 16, 16384, 16384)):
             assert B * C * 8 <= need(torch.bfloat16, B, P, C, G) < (1 << 26) + 32 * B * C
+
+
+Z = 1 << 44
+MAX = 1 << 21
+
+
+def _gated(b, **kw):
+    a = dict(type=1, act=4, x=X, xs=64, w=W, bias=None, z=None, y=Y, ys=48, M=100, N=48, K=64, ws=WS, size=1 << 33)
+    a.update(kw)
+    return b.load_library().corr_gated_linear(*a.values(), None)
+
+
+GATED_REFUSED = [
+    (dict(type=3), -1), (dict(act=6), -1), (dict(M=-1), -1), (dict(N=0), -1), (dict(N=-1), -1), (dict(K=0), -1), (dict(M=(1 << 30) + 1), -2),
+    (dict(N=MAX // 2 + 1), -2), (dict(N=1 << 62), -2), (dict(K=MAX + 1), -2), (dict(M=1 << 30, N=64), -2), (dict(xs=MAX + 1), -2), (dict(xs=63), -1),
+    (dict(x=None), -1), (dict(w=None), -1), (dict(x=X + 2), -1), (dict(w=W + 2), -1),
+]
+
+
+@pytest.mark.parametrize("kw,status", GATED_REFUSED + [
+    (dict(y=None), -1), (dict(ys=47), -1), (dict(ys=MAX + 1), -2), (dict(y=Y + 1), -1), (dict(bias=BIAS + 2), -1), (dict(z=Z + 1), -1), (dict(y=X), -1),
+    (dict(y=W + 64), -1), (dict(z=Y), -1), (dict(z=W), -1), (dict(bias=Y), -1), (dict(K=4096, xs=4096, ws=None), -1), (dict(K=4096, xs=4096, size=16), -1),
+    (dict(K=4096, xs=4096, ws=WS + 8), -1), (dict(K=63, xs=63, size=0), -1),
+])
+def test_gated_linear_refusals(kw, status):
+    assert _gated(_b(), **kw) == status
+
+
+@pytest.mark.parametrize("kw,status", GATED_REFUSED + [
+    (dict(z=None), -1), (dict(z=Z + 1), -1), (dict(dy=None), -1), (dict(dy=DY + 1), -1), (dict(dys=47), -1), (dict(dys=MAX + 1), -2), (dict(dx=DX + 1), -1),
+    (dict(dw=DW + 1), -1), (dict(db=DB + 2), -1), (dict(ws=None), -1), (dict(size=100), -1), (dict(ws=WS + 4), -1), (dict(dx=X), -1), (dict(dw=W), -1),
+    (dict(dx=DY), -1), (dict(dw=DX), -1), (dict(db=DW), -1), (dict(ws=DY), -1), (dict(dx=Z), -1),
+])
+def test_gated_linear_backward_refusals(kw, status):
+    b = _b()
+    a = dict(type=1, act=4, x=X, xs=64, w=W, z=Z, dy=DY, dys=48, dx=DX, dw=DW, db=DB, M=100, N=48, K=64, ws=WS, size=1 << 33)
+    a.update(kw)
+    assert b.load_library().corr_gated_linear_backward(*a.values(), None) == status
+
+
+def test_gated_tiles():
+    """The sizes that the GPU tests use to reach every kind of tile do so."""
+    b = _b()
+    import test_gpu_gated_linear as t
+    kinds = {"few": (0, 16), "64": (64, 64), "64 split": (64, 64), "128": (128, 128), "128 split": (128, 128), "256": (256, 256), "rows": (128, 256)}
+    for dtype in t.TYPES:
+        for kind, (M, N, K) in t.TILES.items():
+            rows, cols, splits = b.corr_debug_linear_tile(dtype, 0, M, 2 * N, K)
+            want = kinds[kind]
+            if dtype == torch.float32 and kind in ("256", "rows"):
+                want = (128, 128)
+            assert (rows, cols) == want, (dtype, kind, rows, cols)
+            assert ("split" in kind) == (splits > 1), (dtype, kind, splits)
