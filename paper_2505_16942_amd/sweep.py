@@ -188,11 +188,42 @@ def _rows_point(H: int, W: int, dtype):
     return [_timed_ms(lambda: f(*a, **k)) for f, a, k in _rows_calls(H, W, dtype, torch.device("cuda:0"))]
 
 
+def _features_calls(H: int, W: int, dtype, device, C: int = 128, heads: int = 1, B: int = 2):
+    """The calls of a block that refines both maps of a pair before the pyramid's build, each attending to the other, and their gradients, as
+    (function, arguments, named arguments).  Every matrix is one of its own, as in _rows_calls."""
+    import torch
+    from . import binding as cb
+    g = torch.Generator(device=device)
+    g.manual_seed(H)
+
+    def new(*shape, sigma=1.0, kind=dtype):
+        return (torch.randn(shape, device=device, generator=g) * sigma).to(kind)
+    f32, P, D = torch.float32, H * W, C // heads
+    x, n, y = new(B, P, C), new(B, P, C), new(B, P, 2 * C)
+    q, k, v, o = (new(B, P, heads, D) for _ in range(4))
+    w, w2, gw, gb, b1 = new(4 * C, C, sigma=C ** -0.5), new(4 * C, C, sigma=C ** -0.5), new(C, kind=f32), new(C, kind=f32), new(4 * C, kind=f32)
+    stats, lse = torch.ones(B, 8, 2, device=device), torch.full((B, heads, P), 8.0, device=device)
+    z = new(B, P, 4 * C)
+    return [(cb.corr_group_norm, (x, 8), dict(weight=gw, bias=gb, act=cb.CORR_ACT_RELU, stats=stats)),
+            (cb.corr_attention, (q, k, v), dict(lse=lse)),
+            (cb.corr_gated_linear, (n, w), dict(bias=b1, preact=z)),
+            (cb.corr_gated_linear_backward, (n, w2, y, new(B, P, 4 * C)), {}),
+            (cb.corr_attention_backward, (q, k, v, o, torch.full_like(lse, 8.0), new(B, P, heads, D)), {}),
+            (cb.corr_group_norm_backward, (x, 8, torch.ones_like(stats), new(B, P, C)), dict(weight=gw, bias=gb, act=cb.CORR_ACT_RELU))]
+
+
+def _features_point(H: int, W: int, dtype):
+    """ms of each of _features_calls"""
+    import torch
+    return [_timed_ms(lambda: f(*a, **k)) for f, a, k in _features_calls(H, W, dtype, torch.device("cuda:0"))]
+
+
 def main(argv=None) -> int:
     ap = argparse.ArgumentParser()
     ap.add_argument("--quick", action="store_true", help="fewer and smaller points")
     ap.add_argument("--backward", action="store_true", help="the gradient's table instead of the lookup's")
     ap.add_argument("--block", action="store_true", help="the table of the calls that follow a lookup in an update block")
+    ap.add_argument("--features", action="store_true", help="the table of the calls that refine two maps before the pyramid's build")
     args = ap.parse_args(argv)
     import torch
     from . import binding as cb
@@ -216,6 +247,15 @@ def main(argv=None) -> int:
             for dtype, name in ((torch.float32, "fp32"), (torch.bfloat16, "bf16")):
                 t = _rows_point(H, W, dtype)
                 print("| %dx%d | %s | %s | %s |" % (H, W, name, " | ".join("%.3f" % v for v in t[:5]), " ".join("%.3f" % v for v in t[5:])), flush=True)
+                torch.cuda.empty_cache()
+        return 0
+    if args.features:
+        print("| map HxW | type | group norm ms | attention ms | gated products ms | gradients in turn, last first ms |")
+        print("|---|---|---|---|---|---|")
+        for H, W in ((46, 62), (90, 160)) if args.quick else ((46, 62), (90, 160), (135, 240)):
+            for dtype, name in ((torch.float32, "fp32"), (torch.bfloat16, "bf16"), (torch.float16, "fp16")):
+                t = _features_point(H, W, dtype)
+                print("| 2x%dx%d | %s | %s | %s |" % (H, W, name, " | ".join("%.3f" % v for v in t[:3]), " ".join("%.3f" % v for v in t[3:])), flush=True)
                 torch.cuda.empty_cache()
         return 0
     base_w, base_it, base_d = 512, 32, 256
