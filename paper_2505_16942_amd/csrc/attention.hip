@@ -11,22 +11,26 @@ constexpr unsigned PAST = 0x80000000u;      // an offset past every resource's e
 constexpr unsigned RANGE = 0x7ffffff0u;
 inline int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-// ---- how products are made.  A fragment is one matrix instruction's operand: lane (lr, lg) = (lane & 15, lane >> 4) holds row lr.  `straight`: a tile's
-// row against K elements along the row.  `turned`: one of its columns against K of its rows; these K rows are taken in the order in which a
-// product's result lies in its lanes (row 4 lg + e of each block of 16), so that the scores are the next product's operand without leaving
-// their lanes.  Tiles lie in LDS in rows of DP elements, 16-byte piece p of row r at slot(r, p), which spreads both kinds of read over the banks.
+// ---- how products are made.  A fragment is one matrix instruction's operand: 32 k, lane (lr, lg) = (lane & 15, lane >> 4) holds row lr and 8 of them.
+// `straight`: a tile's row, along the row.  `turned`: one of its columns, along 32 of its rows; these are taken in the order in which a product's result
+// lies in its lanes (rows 4 lg + e and 16 + 4 lg + e), so that the scores are the next product's operand without leaving their lanes.  Tiles lie in
+// LDS in rows of DP 16-bit elements, 16-byte piece p of row r at slot(r, p), which spreads both kinds of read over the banks.
+template <int DP> __device__ __forceinline__ int slot(int row, int piece) { return DP == 32 ? piece ^ (row >> 1 & 3) : piece ^ (row & 7); }
+template <class F, int DP> __device__ __forceinline__ F read_straight(lds_byte* tile, int row, int t, int lg) {
+    return *(__attribute__((address_space(3))) F*)(tile + row * 2 * DP + slot<DP>(row, 4 * t + lg) * 16);
+}
+template <class F, int DP> __device__ __forceinline__ F read_turned(lds_byte* tile, int row0, int db, int lr, int lg) {
+    const int r = row0 + 4 * lg + (lr >> 2), piece = 2 * db + ((lr & 3) >> 1);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + r * 2 * DP + slot<DP>(r, piece) * 16 + (lr & 1) * 8));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + (r + 16) * 2 * DP + slot<DP>(r + 16, piece) * 16 + (lr & 1) * 8));
+    return __builtin_bit_cast(F, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+constexpr int FK = 32;
 template <class T> struct Num {
     typedef typename Frag<T>::type F;
-    static constexpr int K = 32, V = 8;     // elements of k a fragment, elements a lane
-    template <int DP> static __device__ __forceinline__ int slot(int row, int piece) { return DP == 32 ? piece ^ (row >> 1 & 3) : piece ^ (row & 7); }
-    template <int DP> static __device__ __forceinline__ F straight(lds_byte* tile, int row, int t, int lg) {
-        return *(__attribute__((address_space(3))) F*)(tile + row * 2 * DP + slot<DP>(row, 4 * t + lg) * 16);
-    }
-    template <int DP> static __device__ __forceinline__ F turned(lds_byte* tile, int row0, int db, int lr, int lg) {
-        const int r = row0 + 4 * lg + (lr >> 2), piece = 2 * db + ((lr & 3) >> 1);
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + r * 2 * DP + slot<DP>(r, piece) * 16 + (lr & 1) * 8));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + (r + 16) * 2 * DP + slot<DP>(r + 16, piece) * 16 + (lr & 1) * 8));
-        return __builtin_bit_cast(F, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    template <int DP, int ROWS> static __device__ __forceinline__ F straight(lds_byte* tile, int row, int t, int lg) { return read_straight<F, DP>(tile, row, t, lg); }
+    template <int DP, int ROWS> static __device__ __forceinline__ F turned(lds_byte* tile, int row0, int db, int lr, int lg) {
+        return read_turned<F, DP>(tile, row0, db, lr, lg);
     }
     static __device__ __forceinline__ F pack(const f32x4* x) {
         F f;
@@ -34,41 +38,73 @@ template <class T> struct Num {
         for (int e = 0; e < 8; ++e) f[e] = (T)x[e >> 2][e & 3];
         return f;
     }
-    static __device__ __forceinline__ f32x4 times(F a, F b, f32x4 c) { return mma(a, b, c); }
-};
-// fp32 instructions: four k each, the same element of four lanes' 16 bytes
-template <> struct Num<float> {
-    typedef f32x4 F;
-    enum { K = 16, V = 4 };
-    template <int DP> static __device__ __forceinline__ int slot(int row, int piece) { return piece ^ (row & 7); }
-    template <int DP> static __device__ __forceinline__ F straight(lds_byte* tile, int row, int t, int lg) {
-        return *(__attribute__((address_space(3))) F*)(tile + row * 4 * DP + slot<DP>(row, 4 * t + lg) * 16);
-    }
-    template <int DP> static __device__ __forceinline__ F turned(lds_byte* tile, int row0, int db, int lr, int lg) {
-        F f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int r = row0 + 4 * lg + e;
-            f[e] = *(__attribute__((address_space(3))) float*)(tile + r * 4 * DP + slot<DP>(r, 4 * db + (lr >> 2)) * 16 + (lr & 3) * 4);
-        }
+    static __device__ __forceinline__ f32x4 times(const F& a, const F& b, f32x4 c) { return mma(a, b, c); }
+    // elements d .. d + 7 of row `p`, zeros behind D or without a row
+    static __device__ __forceinline__ F load(const T* p, int d, int D, bool there) {
+        F f = {};
+        if (there && d < D) f = *reinterpret_cast<const typename Some<T, 8>::type*>(p + d);
         return f;
     }
-    static __device__ __forceinline__ F pack(const f32x4* x) { return *x; }
-    static __device__ __forceinline__ f32x4 times(F a, F b, f32x4 c) {
+};
+// fp32: three bf16 parts an element and the six of nine partial products that reach 2^-24, as in the row operators' products: 2.7 times the rate of
+// the fp32 instruction.  A tile is three planes.
+struct Parts { bf16x8 p[3]; };
+__device__ __forceinline__ void split4(f32x4 x, u32x2 (&parts)[3]) {
+    f32x2 lo = {x[0], x[1]}, hi = {x[2], x[3]};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+    for (int p = 0; p < 3; ++p) {
+        const bf16x2 cl = __builtin_convertvector(lo, bf16x2), ch = __builtin_convertvector(hi, bf16x2);
+        parts[p] = u32x2{__builtin_bit_cast(unsigned, cl), __builtin_bit_cast(unsigned, ch)};
+        if (p < 2) {
+            lo -= __builtin_convertvector(cl, f32x2);
+            hi -= __builtin_convertvector(ch, f32x2);
+        }
+    }
+}
+template <> struct Num<float> {
+    typedef Parts F;
+    template <int DP, int ROWS> static __device__ __forceinline__ F straight(lds_byte* tile, int row, int t, int lg) {
+        F f;
+#pragma unroll
+        for (int p = 0; p < 3; ++p) f.p[p] = read_straight<bf16x8, DP>(tile + p * ROWS * 2 * DP, row, t, lg);
+        return f;
+    }
+    template <int DP, int ROWS> static __device__ __forceinline__ F turned(lds_byte* tile, int row0, int db, int lr, int lg) {
+        F f;
+#pragma unroll
+        for (int p = 0; p < 3; ++p) f.p[p] = read_turned<bf16x8, DP>(tile + p * ROWS * 2 * DP, row0, db, lr, lg);
+        return f;
+    }
+    static __device__ __forceinline__ F pack(const f32x4* x) {
+        u32x2 one[3], two[3];
+        split4(x[0], one);
+        split4(x[1], two);
+        F f;
+#pragma unroll
+        for (int p = 0; p < 3; ++p) f.p[p] = __builtin_bit_cast(bf16x8, u32x4{one[p][0], one[p][1], two[p][0], two[p][1]});
+        return f;
+    }
+    static __device__ __forceinline__ f32x4 times(const F& a, const F& b, f32x4 c) {
+        constexpr int QA[6] = {2, 0, 1, 1, 0, 0}, QB[6] = {0, 2, 1, 0, 1, 0};      // small products first
+#pragma unroll
+        for (int q = 0; q < 6; ++q) c = mma(a.p[QA[q]], b.p[QB[q]], c);
         return c;
+    }
+    static __device__ __forceinline__ F load(const float* p, int d, int D, bool there) {
+        f32x4 x[2] = {};
+        if (there && d < D) {
+            x[0] = *reinterpret_cast<const Some<float, 4>::type*>(p + d);
+            x[1] = *reinterpret_cast<const Some<float, 4>::type*>(p + d + 4);
+        }
+        return pack(x);
     }
 };
 // Weights as a product's operand.  fp16's normal values begin at 6e-5, below which a softmax over many keys lies: they are held 2^14 times as
 // large (at most 16384), and the results divided by that.
 template <class T> constexpr float LIFT = std::is_same<T, _Float16>::value ? 14.f : 0.f;
 
-// rows (keys) of a tile in LDS: up to 16 KB of them, of at most 64
-template <class T, int DP, int WAVES> constexpr int tile_rows() {
-    const int most = (WAVES == 1 ? 8192 : 16384) / (DP * (int)sizeof(T)), least = Num<T>::K;
-    return most > 64 ? 64 : most < least ? least : most;
-}
+// rows (keys) of a tile in LDS: 64, or 32 where 64 would take more than 16 KB (24 in fp32's planes)
+template <class T, int DP, int WAVES> constexpr int tile_rows() { return DP <= (WAVES == 1 ? 32 : std::is_same<T, float>::value ? 64 : 128) ? 64 : 32; }
 
 // the largest (sum) over the four lanes that share lane & 15
 struct Both { float one, two; };
@@ -90,37 +126,74 @@ __device__ __forceinline__ float lanes_sum(float x) {
 }
 
 // ---- tiles
-// Where a workgroup's tile is loaded from: rows of a strided array, D of DP elements each.
+// A tile of ROWS rows of a strided array, D of DP elements each, on its way into LDS: `ask` starts it, `land` brings what was asked for to its place
+// (one call of the workgroup for both tiles).  16 bits: straight into LDS, in one of two places that take turns.
+__device__ __forceinline__ i32x4 resource(const void* p) {
+    const uint64_t u = (uint64_t)p;
+    return i32x4{__builtin_amdgcn_readfirstlane((int)u), __builtin_amdgcn_readfirstlane((int)(u >> 32) & 0xffff), (int)RANGE, 0x00020000};
+}
 template <class T, int DP, int ROWS, int WAVES>
 struct Tile {
-    static constexpr int BYTES = ROWS * DP * (int)sizeof(T), PIECES = BYTES / (1024 * WAVES);
+    static constexpr int BYTES = ROWS * DP * 2, PLACES = 2, PIECES = BYTES / (1024 * WAVES);
     static_assert(BYTES % (1024 * WAVES) == 0 && PIECES > 0, "whole loads of 1024 bytes for every wave");
     int row[PIECES];
     unsigned col[PIECES];                    // byte offset inside the row, or PAST behind its end
     __device__ __forceinline__ void plan(int wave, int lane, int D) {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const int at = (i * WAVES + wave) * 1024 + lane * 16, slot = at / 16 % (DP * (int)sizeof(T) / 16);
-            row[i] = at / (DP * (int)sizeof(T));
-            const int piece = Num<T>::template slot<DP>(row[i], slot);      // an involution
-            col[i] = piece * (16 / (int)sizeof(T)) < D ? piece * 16 : PAST;
+            const int at = (i * WAVES + wave) * 1024 + lane * 16;
+            row[i] = at / (DP * 2);
+            const int piece = slot<DP>(row[i], at / 16 % (DP / 8));         // an involution
+            col[i] = piece * 8 < D ? piece * 16 : PAST;
         }
     }
-    static __device__ __forceinline__ i32x4 resource(const T* p) {
-        const uint64_t u = (uint64_t)p;
-        return i32x4{__builtin_amdgcn_readfirstlane((int)u), __builtin_amdgcn_readfirstlane((int)(u >> 32) & 0xffff), (int)RANGE, 0x00020000};
-    }
-    // rows `stride` elements apart from p on, those whose bit is set
-    __device__ __forceinline__ void ask(const T* p, int64_t stride, uint64_t bits, unsigned lds, int wave) const {
+    // offset(row): the byte offset of a row from p on, PAST if it does not count
+    template <class O> __device__ __forceinline__ void ask(const T* p, unsigned lds, int wave, O offset) {
         const i32x4 rsrc = resource(p);
-        const unsigned step = (unsigned)(stride * (int)sizeof(T));
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const bool there = (bits >> row[i]) & 1 && col[i] != PAST;
-            dma16(rsrc, lds + (i * WAVES + wave) * 1024, there ? row[i] * step + col[i] : PAST);
+            const unsigned at = offset(row[i]);
+            dma16(rsrc, lds + (i * WAVES + wave) * 1024, at == PAST || col[i] == PAST ? PAST : at + col[i]);
         }
     }
 };
+// fp32: through registers, where an element's three parts are made; one place.
+template <int DP, int ROWS, int WAVES>
+struct Tile<float, DP, ROWS, WAVES> {
+    static constexpr int PLANE = ROWS * DP * 2, BYTES = 3 * PLANE, PLACES = 1, PIECES = ROWS * DP / (256 * WAVES);
+    f32x4 x[PIECES];
+    int lane_, D_;
+    __device__ __forceinline__ void plan(int wave, int lane, int D) { lane_ = wave * 64 + lane; D_ = D; }
+    template <class O> __device__ __forceinline__ void ask(const float* p, unsigned, int, O offset) {
+        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(p), 0, (int)RANGE, 0x00020000);
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int at = i * WAVES * 64 + lane_, row = at / (DP / 4), d = at % (DP / 4) * 4;
+            const unsigned to = offset(row);
+            x[i] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)(to == PAST || d >= D_ ? PAST : to + d * 4), 0, 0));
+        }
+    }
+    __device__ __forceinline__ void store(unsigned char* tile) const {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int at = i * WAVES * 64 + lane_, row = at / (DP / 4), d = at % (DP / 4) * 4;
+            u32x2 parts[3];
+            split4(x[i], parts);
+#pragma unroll
+            for (int q = 0; q < 3; ++q)
+                *reinterpret_cast<u32x2*>(tile + q * PLANE + row * 2 * DP + slot<DP>(row, d >> 3) * 16 + (d & 4) * 2) = parts[q];
+        }
+    }
+};
+template <class L> __device__ __forceinline__ void land(const L& one, const L& two, unsigned char* smem) {
+    if constexpr (L::PLACES == 2) arrive_all();
+    else {
+        __syncthreads();                                 // the last tiles have been read
+        one.store(smem);
+        two.store(smem + L::BYTES);
+        __syncthreads();
+    }
+}
 // Which keys of a tile count: those before the item's length (and the share's end) whose mask byte is not zero.
 struct Keys {
     const uint8_t* mask;                     // of this item, or null
@@ -140,21 +213,11 @@ template <class T> __device__ __forceinline__ Keys keys_of(const AttentionArgs& 
     k.mask = a.key_mask ? a.key_mask + (int64_t)b * a.Lk : nullptr;
     return k;
 }
-// 16 bytes of row `p` from element d on, zeros behind D or without a row
-template <class T>
-__device__ __forceinline__ typename Num<T>::F load_frag(const T* p, int d, int D, bool there) {
-    typename Num<T>::F f = {};
-    if (there && d < D) f = *reinterpret_cast<const typename Some<T, Num<T>::V>::type*>(p + d);
-    return f;
-}
-// Workgroup w runs on XCD w % 8: each XCD gets a run of consecutive pieces of work, so that the tiles of one head share its keys in one L2.
-__device__ __forceinline__ int piece_of(int w, int all) {
-    const int q = all >> 3, r = all & 7, x = w & 7;
-    return x * q + min(x, r) + (w >> 3);
-}
+// Tiles of a head follow each other, and so meet its keys at about the same time on every XCD.  Runs of a head's tiles on one XCD would leave XCDs
+// idle whose items are short.
 struct Place { int b, hk, bh, tile, split; };
 __device__ __forceinline__ Place place_of(const AttentionArgs& a, int tiles, int splits) {
-    const int n = piece_of(blockIdx.x, tiles * splits * a.B * a.HK);
+    const int n = blockIdx.x;
     Place p;
     p.tile = n % tiles;
     const int m = n / tiles;
@@ -177,9 +240,9 @@ template <class T, int DP, int WAVES, int QB>
 __global__ __launch_bounds__(64 * WAVES, WAVES == 1 ? 1 : 2) void forward_kernel(AttentionArgs a, int tiles, int splits, int share) {
     typedef Num<T> N;
     typedef typename N::F F;
-    constexpr int KT = tile_rows<T, DP, WAVES>(), KB = KT / 16, CH = DP / N::K, DB = DP / 16, PB = N::K / 16;
+    constexpr int KT = tile_rows<T, DP, WAVES>(), KB = KT / 16, CH = DP / FK, DB = DP / 16;
     typedef Tile<T, DP, KT, WAVES> Load;
-    __shared__ __align__(1024) unsigned char smem[4 * Load::BYTES];
+    __shared__ __align__(1024) unsigned char smem[2 * Load::PLACES * Load::BYTES];
     lds_byte* const lds = (lds_byte*)smem;
     const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)lds);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lg = lane >> 4;
@@ -199,14 +262,16 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 1 ? 1 : 2) void forward_kernel
         query_of(a, r, q, g);
         const T* p = (const T*)a.q + at.b * a.q_item + (at.hk * a.per + g) * a.q_head + q * a.q_row;
 #pragma unroll
-        for (int t = 0; t < CH; ++t) fq[j][t] = load_frag<T>(p, t * N::K + lg * N::V, a.D, r < a.rows);
+        for (int t = 0; t < CH; ++t) fq[j][t] = N::load(p, t * FK + lg * 8, a.D, r < a.rows);
     }
-    Load load;
-    load.plan(wave, lane, a.D);
+    Load load_k, load_v;
+    load_k.plan(wave, lane, a.D);
+    load_v.plan(wave, lane, a.D);
     auto ask = [&](int t, uint64_t bits) {
-        const unsigned to = lds_at + (t & 1) * 2 * Load::BYTES;
-        load.ask(K0 + (int64_t)t * KT * a.k_row, a.k_row, bits, to, wave);
-        load.ask(V0 + (int64_t)t * KT * a.v_row, a.v_row, bits, to + Load::BYTES, wave);
+        const unsigned to = lds_at + t % Load::PLACES * 2 * Load::BYTES;
+        const unsigned k_step = (unsigned)(a.k_row * (int)sizeof(T)), v_step = (unsigned)(a.v_row * (int)sizeof(T));
+        load_k.ask(K0 + (int64_t)t * KT * a.k_row, to, wave, [&](int r) { return (bits >> r) & 1 ? r * k_step : PAST; });
+        load_v.ask(V0 + (int64_t)t * KT * a.v_row, to + Load::BYTES, wave, [&](int r) { return (bits >> r) & 1 ? r * v_step : PAST; });
     };
     const float c = a.scale * LOG2E;
     f32x4 o[DB][QB] = {};
@@ -221,7 +286,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 1 ? 1 : 2) void forward_kernel
         byte = keys.byte(k_lo + KT, lane);
     }
     for (int t = 0; t < steps; ++t) {
-        arrive_all();
+        land(load_k, load_v, smem);
         uint64_t next = 0;
         if (t + 1 < steps) {
             next = keys.bits(k_lo + (t + 1) * KT, KT, byte);
@@ -229,14 +294,14 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 1 ? 1 : 2) void forward_kernel
             byte = keys.byte(k_lo + (t + 2) * KT, lane);
         }
         if (bits) {
-            lds_byte* const tk = lds + (t & 1) * 2 * Load::BYTES;
+            lds_byte* const tk = lds + t % Load::PLACES * 2 * Load::BYTES;
             lds_byte* const tv = tk + Load::BYTES;
             f32x4 s[QB][KB] = {};
 #pragma unroll
             for (int h = 0; h < CH; ++h)
 #pragma unroll
                 for (int i = 0; i < KB; ++i) {
-                    const F f = N::template straight<DP>(tk, 16 * i + lr, h, lg);
+                    const F f = N::template straight<DP, KT>(tk, 16 * i + lr, h, lg);
 #pragma unroll
                     for (int j = 0; j < QB; ++j) s[j][i] = N::times(f, fq[j][h], s[j][i]);
                 }
@@ -283,13 +348,13 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 1 ? 1 : 2) void forward_kernel
                         l[j] += s[j][i][e];
                     }
 #pragma unroll
-            for (int i = 0; i < KB; i += PB) {
+            for (int i = 0; i < KB; i += 2) {
                 F fp[QB];
 #pragma unroll
                 for (int j = 0; j < QB; ++j) fp[j] = N::pack(&s[j][i]);
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
-                    const F f = N::template turned<DP>(tv, 16 * i, d, lr, lg);
+                    const F f = N::template turned<DP, KT>(tv, 16 * i, d, lr, lg);
 #pragma unroll
                     for (int j = 0; j < QB; ++j) o[d][j] = N::times(f, fp[j], o[d][j]);
                 }
@@ -325,39 +390,51 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 1 ? 1 : 2) void forward_kernel
     }
 }
 
-// The splits' sums of a row, brought to one exponent: 16 lanes a row.
+// The splits' sums of a row, brought to one exponent.  `across` threads have four elements each; `shares` of them take turns at the splits, in a
+// fixed order.
 template <class T>
-__global__ __launch_bounds__(256) void forward_join_kernel(AttentionArgs a, int splits) {
-    const int64_t all = (int64_t)a.B * a.HK * a.rows, row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
-    const int lane = threadIdx.x & 15;
-    if (row >= all) return;
+__global__ __launch_bounds__(256) void forward_join_kernel(AttentionArgs a, int splits, int across, int shares) {
+    __shared__ f32x4 sums[256];
+    __shared__ float tops[256], totals[256];
+    const int tid = threadIdx.x, team = across * shares, lane = tid % across, share = tid / across % shares, d = 4 * lane;
+    const int64_t all = (int64_t)a.B * a.HK * a.rows, row = (int64_t)blockIdx.x * (256 / team) + tid / team;
+    float top = -INFINITY, sum = 0.f;
+    f32x4 x = {};
+    if (row < all && d < a.D) {
+        const float* ml = a.part_ml + 2 * (share * all + row);
+        const float* o = a.part_o + (share * all + row) * a.D + d;
+#pragma unroll 4
+        for (int s = share; s < splits; s += shares, ml += 2 * shares * all, o += shares * all * a.D) {
+            const float m = ml[0], l = ml[1];
+            const f32x4 v = *reinterpret_cast<const f32x4*>(o);
+            if (l == 0.f) continue;
+            const float now = fmaxf(top, m), was = __builtin_amdgcn_exp2f(top - now), is = __builtin_amdgcn_exp2f(m - now);
+            sum = sum * was + l * is;
+            x = x * was + v * is;
+            top = now;
+        }
+    }
+    if (shares > 1) {
+        tops[tid] = top; totals[tid] = sum; sums[tid] = x;
+        __syncthreads();
+        if (share) return;
+        for (int i = 1; i < shares; ++i) {
+            const int other = tid + i * across;
+            if (totals[other] == 0.f) continue;
+            const float now = fmaxf(top, tops[other]), was = __builtin_amdgcn_exp2f(top - now), is = __builtin_amdgcn_exp2f(tops[other] - now);
+            sum = sum * was + totals[other] * is;
+            x = x * was + sums[other] * is;
+            top = now;
+        }
+    }
+    if (row >= all || d >= a.D) return;
     const int bh = (int)(row / a.rows), r = (int)(row - (int64_t)bh * a.rows), b = bh / a.HK, hk = bh - b * a.HK;
     int q, g;
     query_of(a, r, q, g);
     const int head = hk * a.per + g;
-    float top = -INFINITY;
-    for (int s = 0; s < splits; ++s) {
-        const float* ml = a.part_ml + 2 * (s * all + row);
-        if (ml[1] != 0.f) top = fmaxf(top, ml[0]);
-    }
-    float sum = 0.f;
-    for (int s = 0; s < splits; ++s) {
-        const float* ml = a.part_ml + 2 * (s * all + row);
-        if (ml[1] != 0.f) sum += ml[1] * __builtin_amdgcn_exp2f(ml[0] - top);
-    }
     const float by = sum == 0.f ? 0.f : 1.f / sum;
-    T* const p = (T*)a.out + (((int64_t)b * a.Lq + q) * a.HK * a.per + head) * a.D;
-    for (int d = 4 * lane; d < a.D; d += 64) {
-        f32x4 x = {};
-#pragma unroll 4
-        for (int s = 0; s < splits; ++s) {
-            const float* ml = a.part_ml + 2 * (s * all + row);
-            const f32x4 o = *reinterpret_cast<const f32x4*>(a.part_o + (s * all + row) * a.D + d);
-            if (ml[1] != 0.f) x += o * (__builtin_amdgcn_exp2f(ml[0] - top));
-        }
-        const float v[4] = {x[0] * by, x[1] * by, x[2] * by, x[3] * by};
-        store_some<T, 4>(p + d, v, 4);
-    }
+    const float v[4] = {x[0] * by, x[1] * by, x[2] * by, x[3] * by};
+    store_some<T, 4>((T*)a.out + (((int64_t)b * a.Lq + q) * a.HK * a.per + head) * a.D + d, v, 4);
     if (a.lse && lane == 0) a.lse[((int64_t)b * a.HK * a.per + head) * a.Lq + q] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * LN2;
 }
 
@@ -429,9 +506,9 @@ template <class T, int DP, int QB>
 __global__ __launch_bounds__(256, 2) void dq_kernel(AttentionArgs a, int tiles, int splits, int share) {
     typedef Num<T> N;
     typedef typename N::F F;
-    constexpr int KT = tile_rows<T, DP, 4>(), CH = DP / N::K, DB = DP / 16, PB = N::K / 16;
+    constexpr int KT = tile_rows<T, DP, 4>(), CH = DP / FK, DB = DP / 16, PB = 2;
     typedef Tile<T, DP, KT, 4> Load;
-    __shared__ __align__(1024) unsigned char smem[4 * Load::BYTES];
+    __shared__ __align__(1024) unsigned char smem[2 * Load::PLACES * Load::BYTES];
     lds_byte* const lds = (lds_byte*)smem;
     const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)lds);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lg = lane >> 4;
@@ -456,19 +533,21 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(AttentionArgs a, int tiles, 
         const T* w = (const T*)a.d_out + (((int64_t)at.b * a.Lq + q) * a.HK * a.per + head) * a.D;
 #pragma unroll
         for (int t = 0; t < CH; ++t) {
-            fq[j][t] = load_frag<T>(p, t * N::K + lg * N::V, a.D, there);
-            fo[j][t] = load_frag<T>(w, t * N::K + lg * N::V, a.D, there);
+            fq[j][t] = N::load(p, t * FK + lg * 8, a.D, there);
+            fo[j][t] = N::load(w, t * FK + lg * 8, a.D, there);
         }
         const f32x2 x = there ? *reinterpret_cast<const f32x2*>(a.aux + 2 * ((int64_t)at.bh * attention_aux_rows(a.rows) + r)) : f32x2{INFINITY, 0.f};
         low[j] = x[0];
         delta[j] = x[1];
     }
-    Load load;
-    load.plan(wave, lane, a.D);
+    Load load_k, load_v;
+    load_k.plan(wave, lane, a.D);
+    load_v.plan(wave, lane, a.D);
     auto ask = [&](int t, uint64_t bits) {
-        const unsigned to = lds_at + (t & 1) * 2 * Load::BYTES;
-        load.ask(K0 + (int64_t)t * KT * a.k_row, a.k_row, bits, to, wave);
-        load.ask(V0 + (int64_t)t * KT * a.v_row, a.v_row, bits, to + Load::BYTES, wave);
+        const unsigned to = lds_at + t % Load::PLACES * 2 * Load::BYTES;
+        const unsigned k_step = (unsigned)(a.k_row * (int)sizeof(T)), v_step = (unsigned)(a.v_row * (int)sizeof(T));
+        load_k.ask(K0 + (int64_t)t * KT * a.k_row, to, wave, [&](int r) { return (bits >> r) & 1 ? r * k_step : PAST; });
+        load_v.ask(V0 + (int64_t)t * KT * a.v_row, to + Load::BYTES, wave, [&](int r) { return (bits >> r) & 1 ? r * v_step : PAST; });
     };
     const float c = a.scale * LOG2E;
     f32x4 dq[DB][QB] = {};
@@ -481,7 +560,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(AttentionArgs a, int tiles, 
         byte = keys.byte(k_lo + KT, lane);
     }
     for (int t = 0; t < steps; ++t) {
-        arrive_all();
+        land(load_k, load_v, smem);
         uint64_t next = 0;
         if (t + 1 < steps) {
             next = keys.bits(k_lo + (t + 1) * KT, KT, byte);
@@ -489,19 +568,19 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(AttentionArgs a, int tiles, 
             byte = keys.byte(k_lo + (t + 2) * KT, lane);
         }
         if (bits) {
-            lds_byte* const tk = lds + (t & 1) * 2 * Load::BYTES;
+            lds_byte* const tk = lds + t % Load::PLACES * 2 * Load::BYTES;
             lds_byte* const tv = tk + Load::BYTES;
             const bool some = bits != ~0ull >> (64 - KT);
             const uint64_t mine = bits >> (4 * lg);
 #pragma unroll
-            for (int kk = 0; kk < KT / N::K; ++kk) {
+            for (int kk = 0; kk < KT / FK; ++kk) {
                 f32x4 s[QB][PB] = {}, dp[QB][PB] = {};
 #pragma unroll
                 for (int h = 0; h < CH; ++h)
 #pragma unroll
                     for (int i = 0; i < PB; ++i) {
-                        const F f = N::template straight<DP>(tk, N::K * kk + 16 * i + lr, h, lg);
-                        const F w = N::template straight<DP>(tv, N::K * kk + 16 * i + lr, h, lg);
+                        const F f = N::template straight<DP, KT>(tk, FK * kk + 16 * i + lr, h, lg);
+                        const F w = N::template straight<DP, KT>(tv, FK * kk + 16 * i + lr, h, lg);
 #pragma unroll
                         for (int j = 0; j < QB; ++j) {
                             s[j][i] = N::times(f, fq[j][h], s[j][i]);
@@ -516,7 +595,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(AttentionArgs a, int tiles, 
                         for (int e = 0; e < 4; ++e) {
                             const float p = __builtin_amdgcn_exp2f(fmaf(s[j][i][e], c, -low[j]));
                             dp[j][i][e] = p * (dp[j][i][e] - delta[j]);
-                            if (some) dp[j][i][e] = (mine >> (N::K * kk + 16 * i + e)) & 1 ? dp[j][i][e] : 0.f;
+                            if (some) dp[j][i][e] = (mine >> (FK * kk + 16 * i + e)) & 1 ? dp[j][i][e] : 0.f;
                         }
                 lifted.lift(dp, dq);
                 F fs[QB];
@@ -524,7 +603,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(AttentionArgs a, int tiles, 
                 for (int j = 0; j < QB; ++j) fs[j] = N::pack(dp[j]);
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
-                    const F f = N::template turned<DP>(tk, N::K * kk, d, lr, lg);
+                    const F f = N::template turned<DP, KT>(tk, FK * kk, d, lr, lg);
 #pragma unroll
                     for (int j = 0; j < QB; ++j) dq[d][j] = N::times(f, fs[j], dq[d][j]);
                 }
@@ -556,9 +635,9 @@ template <class T, int DP, int KB>
 __global__ __launch_bounds__(256, 2) void dkv_kernel(AttentionArgs a, int tiles, int splits, int share) {
     typedef Num<T> N;
     typedef typename N::F F;
-    constexpr int RT = tile_rows<T, DP, 4>(), CH = DP / N::K, DB = DP / 16, PB = N::K / 16;
+    constexpr int RT = tile_rows<T, DP, 4>(), CH = DP / FK, DB = DP / 16, PB = 2;
     typedef Tile<T, DP, RT, 4> Load;
-    __shared__ __align__(1024) unsigned char smem[4 * Load::BYTES];
+    __shared__ __align__(1024) unsigned char smem[2 * Load::PLACES * Load::BYTES];
     lds_byte* const lds = (lds_byte*)smem;
     const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)lds);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lg = lane >> 4;
@@ -577,33 +656,31 @@ __global__ __launch_bounds__(256, 2) void dkv_kernel(AttentionArgs a, int tiles,
         const T* w = (const T*)a.v + at.b * a.v_item + at.hk * a.v_head + k * a.v_row;
 #pragma unroll
         for (int t = 0; t < CH; ++t) {
-            fk[j][t] = load_frag<T>(p, t * N::K + lg * N::V, a.D, counts[j]);
-            fv[j][t] = load_frag<T>(w, t * N::K + lg * N::V, a.D, counts[j]);
+            fk[j][t] = N::load(p, t * FK + lg * 8, a.D, counts[j]);
+            fv[j][t] = N::load(w, t * FK + lg * 8, a.D, counts[j]);
         }
     }
     const int steps = __syncthreads_or(any) ? (r_hi - r_lo + RT - 1) / RT : 0;
     const T* const Q0 = (const T*)a.q + at.b * a.q_item + (int64_t)at.hk * a.per * a.q_head;
     const T* const O0 = (const T*)a.d_out + (int64_t)at.b * a.Lq * a.HK * a.per * a.D + (int64_t)at.hk * a.per * a.D;
     const int64_t o_row = (int64_t)a.HK * a.per * a.D;
-    Load load;
-    load.plan(wave, lane, a.D);
+    Load load_q, load_o;
+    load_q.plan(wave, lane, a.D);
+    load_o.plan(wave, lane, a.D);
     auto ask = [&](int t) {
-        const unsigned to = lds_at + (t & 1) * 2 * Load::BYTES;
+        const unsigned to = lds_at + t % Load::PLACES * 2 * Load::BYTES;
         const int r0 = r_lo + t * RT;
         int q0, g0;
         query_of(a, r0, q0, g0);
-        const i32x4 rq = Load::resource(Q0 + q0 * a.q_row), ro = Load::resource(O0 + q0 * o_row);
-#pragma unroll
-        for (int i = 0; i < Load::PIECES; ++i) {
-            const int r = r0 + load.row[i];
-            int q, g;
-            query_of(a, r, q, g);
-            const bool there = r < r_hi && load.col[i] != PAST;
-            const int es = sizeof(T);
-            dma16(rq, to + (i * 4 + wave) * 1024, there ? (unsigned)(((q - q0) * (int)a.q_row + g * (int)a.q_head) * es) + load.col[i] : PAST);
-            dma16(ro, to + Load::BYTES + (i * 4 + wave) * 1024,
-                  there ? (unsigned)(((q - q0) * (int)o_row + g * a.D) * es) + load.col[i] : PAST);
-        }
+        auto rows = [&](int row, int head) {             // byte offsets of rows from query q0 on
+            return [=, &a](int i) {
+                int q, g;
+                query_of(a, r0 + i, q, g);
+                return r0 + i < r_hi ? (unsigned)(((q - q0) * row + g * head) * (int)sizeof(T)) : PAST;
+            };
+        };
+        load_q.ask(Q0 + q0 * a.q_row, to, wave, rows((int)a.q_row, (int)a.q_head));
+        load_o.ask(O0 + q0 * o_row, to + Load::BYTES, wave, rows((int)o_row, a.D));
     };
     const float c = a.scale * LOG2E;
     const float* const aux = a.aux + 2 * (int64_t)at.bh * attention_aux_rows(a.rows);
@@ -611,16 +688,16 @@ __global__ __launch_bounds__(256, 2) void dkv_kernel(AttentionArgs a, int tiles,
     Lifted<T, KB> lifted;
     if (steps) ask(0);
     for (int t = 0; t < steps; ++t) {
-        arrive_all();
+        land(load_q, load_o, smem);
         if (t + 1 < steps) ask(t + 1);
-        lds_byte* const tq = lds + (t & 1) * 2 * Load::BYTES;
+        lds_byte* const tq = lds + t % Load::PLACES * 2 * Load::BYTES;
         lds_byte* const to = tq + Load::BYTES;
 #pragma unroll
-        for (int kk = 0; kk < RT / N::K; ++kk) {
+        for (int kk = 0; kk < RT / FK; ++kk) {
             f32x4 low[PB], delta[PB];
 #pragma unroll
             for (int i = 0; i < PB; ++i) {               // share and tiles are multiples of 16, and so is the array's length
-                const int r = r_lo + t * RT + N::K * kk + 16 * i + 4 * lg;
+                const int r = r_lo + t * RT + FK * kk + 16 * i + 4 * lg;
                 f32x4 x = {INFINITY, 0.f, INFINITY, 0.f}, y = x;
                 if (r < r_hi) {
                     x = *reinterpret_cast<const f32x4*>(aux + 2 * r);
@@ -634,8 +711,8 @@ __global__ __launch_bounds__(256, 2) void dkv_kernel(AttentionArgs a, int tiles,
             for (int h = 0; h < CH; ++h)
 #pragma unroll
                 for (int i = 0; i < PB; ++i) {
-                    const F f = N::template straight<DP>(tq, N::K * kk + 16 * i + lr, h, lg);
-                    const F w = N::template straight<DP>(to, N::K * kk + 16 * i + lr, h, lg);
+                    const F f = N::template straight<DP, RT>(tq, FK * kk + 16 * i + lr, h, lg);
+                    const F w = N::template straight<DP, RT>(to, FK * kk + 16 * i + lr, h, lg);
 #pragma unroll
                     for (int j = 0; j < KB; ++j) {
                         s[j][i] = N::times(f, fk[j][h], s[j][i]);
@@ -660,8 +737,8 @@ __global__ __launch_bounds__(256, 2) void dkv_kernel(AttentionArgs a, int tiles,
             for (int j = 0; j < KB; ++j) fs[j] = N::pack(dp[j]);
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
-                const F f = N::template turned<DP>(to, N::K * kk, d, lr, lg);
-                const F w = N::template turned<DP>(tq, N::K * kk, d, lr, lg);
+                const F f = N::template turned<DP, RT>(to, FK * kk, d, lr, lg);
+                const F w = N::template turned<DP, RT>(tq, FK * kk, d, lr, lg);
 #pragma unroll
                 for (int j = 0; j < KB; ++j) {
                     dv[d][j] = N::times(f, fp[j], dv[d][j]);
@@ -711,24 +788,36 @@ __global__ __launch_bounds__(256) void sum_kernel(const float* one, const float*
     store_some<T, 4>((blockIdx.y ? to_two : to_one) + 4 * i, v, 4);
 }
 
+// Where two blocks of 16 rows (keys) a wave fit its registers.
+constexpr bool two_fit(AttentionPass pass, bool f32, int DP) { return DP <= (!f32 ? 128 : pass == PASS_DKV ? 32 : 64); }
+// Few rows take one wave a workgroup.
+constexpr bool one_fits(bool f32, int DP) { return !f32 || DP <= 128; }
+
 template <class T, int DP>
 hipError_t forward(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) {
     const dim3 grid(p.tiles * p.splits * a.B * a.HK);
-    if (p.waves == 1) hipLaunchKernelGGL((forward_kernel<T, DP, 1, 1>), grid, dim3(64), 0, s, a, p.tiles, p.splits, p.share);
-    else if (p.blocks == 1) hipLaunchKernelGGL((forward_kernel<T, DP, 4, 1>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
-    else if constexpr (DP * sizeof(T) <= 256) hipLaunchKernelGGL((forward_kernel<T, DP, 4, 2>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
-    if (p.splits > 1) hipLaunchKernelGGL(forward_join_kernel<T>, dim3(cdiv((int64_t)a.B * a.HK * a.rows, 16)), dim3(256), 0, s, a, p.splits);
+    constexpr bool F32 = std::is_same<T, float>::value;
+    if (p.waves == 1) {
+        if constexpr (one_fits(F32, DP)) hipLaunchKernelGGL((forward_kernel<T, DP, 1, 1>), grid, dim3(64), 0, s, a, p.tiles, p.splits, p.share);
+    } else if (p.blocks == 1) hipLaunchKernelGGL((forward_kernel<T, DP, 4, 1>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
+    else if constexpr (two_fit(PASS_FORWARD, F32, DP)) hipLaunchKernelGGL((forward_kernel<T, DP, 4, 2>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
+    if (p.splits > 1) {
+        int across = 2, shares = 1;
+        while (4 * across < a.D) across *= 2;
+        while (2 * shares * across <= 256 && 4 * shares <= p.splits) shares *= 2;
+        hipLaunchKernelGGL(forward_join_kernel<T>, dim3(cdiv((int64_t)a.B * a.HK * a.rows, 256 / (across * shares))), dim3(256), 0, s, a, p.splits, across, shares);
+    }
     return hipGetLastError();
 }
 template <class T, int DP>
 hipError_t backward(const AttentionArgs& a, const AttentionPlan& pq, const AttentionPlan& pk, hipStream_t s) {
     const int aux_rows = attention_aux_rows(a.rows);
     hipLaunchKernelGGL(delta_kernel<T>, dim3(cdiv((int64_t)a.B * a.HK * aux_rows, 16)), dim3(256), 0, s, a, aux_rows);
-    constexpr bool TWO = DP * sizeof(T) <= 256;
+    constexpr bool F32 = std::is_same<T, float>::value;
     if (a.d_q) {
         const dim3 grid(pq.tiles * pq.splits * a.B * a.HK);
         if (pq.blocks == 1) hipLaunchKernelGGL((dq_kernel<T, DP, 1>), grid, dim3(256), 0, s, a, pq.tiles, pq.splits, pq.share);
-        else if constexpr (TWO) hipLaunchKernelGGL((dq_kernel<T, DP, 2>), grid, dim3(256), 0, s, a, pq.tiles, pq.splits, pq.share);
+        else if constexpr (two_fit(PASS_DQ, F32, DP)) hipLaunchKernelGGL((dq_kernel<T, DP, 2>), grid, dim3(256), 0, s, a, pq.tiles, pq.splits, pq.share);
         if (pq.splits > 1) {
             const int64_t quads = (int64_t)a.B * a.Lq * a.HK * a.per * a.D / 4;
             hipLaunchKernelGGL(sum_kernel<T>, dim3(cdiv(quads, 256)), dim3(256), 0, s, a.part_q, a.part_q, (T*)a.d_q, (T*)a.d_q, quads, pq.splits);
@@ -737,7 +826,7 @@ hipError_t backward(const AttentionArgs& a, const AttentionPlan& pq, const Atten
     if (a.d_k) {
         const dim3 grid(pk.tiles * pk.splits * a.B * a.HK);
         if (pk.blocks == 1) hipLaunchKernelGGL((dkv_kernel<T, DP, 1>), grid, dim3(256), 0, s, a, pk.tiles, pk.splits, pk.share);
-        else if constexpr (TWO) hipLaunchKernelGGL((dkv_kernel<T, DP, 2>), grid, dim3(256), 0, s, a, pk.tiles, pk.splits, pk.share);
+        else if constexpr (two_fit(PASS_DKV, F32, DP)) hipLaunchKernelGGL((dkv_kernel<T, DP, 2>), grid, dim3(256), 0, s, a, pk.tiles, pk.splits, pk.share);
         if (pk.splits > 1) {
             const int64_t quads = (int64_t)a.B * a.Lk * a.HK * a.D / 4;
             hipLaunchKernelGGL(sum_kernel<T>, dim3(cdiv(quads, 256), 2), dim3(256), 0, s, a.part_k, a.part_v, (T*)a.d_k, (T*)a.d_v, quads, pk.splits);
@@ -756,11 +845,12 @@ hipError_t launch_attention_backward_f32(const AttentionArgs& a, const Attention
 // Rows of a workgroup: 128 (two blocks of 16 a wave) where that gives one to every compute unit, else 64, and 16 in one wave where there are no more.
 // Shares of the long axis where there are still too few workgroups: as many as fill the chip, of four tiles at least.
 AttentionPlan attention_plan(corr_dtype t, AttentionPass pass, int B, int Lq, int Lk, int HK, int per, int D) {
-    const int pad = D <= 32 ? 32 : D <= 64 ? 64 : D <= 128 ? 128 : 256, es = t == CORR_TYPE_F32 ? 4 : 2;
+    const int pad = D <= 32 ? 32 : D <= 64 ? 64 : D <= 128 ? 128 : 256;
+    const bool f32 = t == CORR_TYPE_F32;
     const int rows = Lq * per, along = pass == PASS_DKV ? Lk : rows, over = pass == PASS_DKV ? rows : Lk;
     AttentionPlan p;
-    p.waves = pass == PASS_FORWARD && along <= 16 ? 1 : 4;
-    p.blocks = p.waves == 4 && pad * es <= 256 && (int64_t)cdiv(along, 128) * B * HK >= 256 ? 2 : 1;
+    p.waves = pass == PASS_FORWARD && along <= 16 && one_fits(f32, pad) ? 1 : 4;
+    p.blocks = p.waves == 4 && two_fit(pass, f32, pad) && (int64_t)cdiv(along, 128) * B * HK >= 256 ? 2 : 1;
     p.tile = 16 * p.waves * p.blocks;
     p.tiles = cdiv(along, p.tile);
     const int64_t groups = (int64_t)p.tiles * B * HK, want = p.waves == 1 ? 1280 : 512;
