@@ -15,7 +15,7 @@ inline int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 // `straight`: a tile's row, along the row.  `turned`: one of its columns, along 32 of its rows; these are taken in the order in which a product's result
 // lies in its lanes (rows 4 lg + e and 16 + 4 lg + e), so that the scores are the next product's operand without leaving their lanes.  Tiles lie in
 // LDS in rows of DP 16-bit elements, 16-byte piece p of row r at slot(r, p), which spreads both kinds of read over the banks.
-template <int DP> __device__ __forceinline__ int slot(int row, int piece) { return DP == 32 ? piece ^ (row >> 1 & 3) : piece ^ (row & 7); }
+template <int DP> __device__ __forceinline__ int slot(int row, int piece) { return piece ^ (DP == 32 ? row >> 1 & 3 : DP == 64 ? row & 7 : row & 15); }
 template <class F, int DP> __device__ __forceinline__ F read_straight(lds_byte* tile, int row, int t, int lg) {
     return *(__attribute__((address_space(3))) F*)(tile + row * 2 * DP + slot<DP>(row, 4 * t + lg) * 16);
 }
@@ -102,6 +102,10 @@ template <> struct Num<float> {
 // Weights as a product's operand.  fp16's normal values begin at 6e-5, below which a softmax over many keys lies: they are held 2^14 times as
 // large (at most 16384), and the results divided by that.
 template <class T> constexpr float LIFT = std::is_same<T, _Float16>::value ? 14.f : 0.f;
+
+// The sums are rescaled only when a score passes the reference by more than 2^SLACK, which their types hold: fp16 up to 2^(14 + 1.75), the others as they
+// like.  Of a wave's 32 rows some row's largest score grows in nearly every second of 200 tiles.
+template <class T> constexpr float SLACK = std::is_same<T, _Float16>::value ? 1.75f : 8.f;
 
 // rows (keys) of a tile in LDS: 64, or 32 where 64 would take more than 16 KB (24 in fp32's planes)
 template <class T, int DP, int WAVES> constexpr int tile_rows() { return DP <= (WAVES == 1 ? 32 : std::is_same<T, float>::value ? 64 : 128) ? 64 : 32; }
@@ -232,7 +236,7 @@ __device__ __forceinline__ void query_of(const AttentionArgs& a, int r, int& q, 
     g = r - q * a.per;
 }
 
-// ---- forward.  One pass over the keys with a running maximum m and sum l of each row.  S^T = K Q^T in tiles of 16 keys x 16 rows: a lane has four
+// ---- forward.  One pass over the keys with a running reference m (the largest score, or a little less) and sum l of each row.  S^T = K Q^T in tiles of 16 keys x 16 rows: a lane has four
 // keys of one row, so that a row's maximum is a lane's own and two exchanges away, and the weights are the operand of O^T = V^T P^T as
 // they lie.  Weights are rounded once to the operands' type (their sum is not): errors of single weights, at most half a step each, which the sum over
 // keys averages.
@@ -274,6 +278,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 1 ? 1 : 2) void forward_kernel
         load_v.ask(V0 + (int64_t)t * KT * a.v_row, to + Load::BYTES, wave, [&](int r) { return (bits >> r) & 1 ? r * v_step : PAST; });
     };
     const float c = a.scale * LOG2E;
+    const float slack = SLACK<T> / c;
     f32x4 o[DB][QB] = {};
     float m[QB], mc[QB], l[QB];
 #pragma unroll
@@ -324,7 +329,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 1 ? 1 : 2) void forward_kernel
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x = fmaxf(x, s[j][i][e]);
                 top[j] = lanes_max(x);
-                grew |= top[j] > m[j];
+                grew |= top[j] > m[j] + slack;
             }
             if (__any(grew)) {
 #pragma unroll
@@ -789,7 +794,7 @@ __global__ __launch_bounds__(256) void sum_kernel(const float* one, const float*
 }
 
 // Where two blocks of 16 rows (keys) a wave fit its registers.
-constexpr bool two_fit(AttentionPass pass, bool f32, int DP) { return DP <= (!f32 ? 128 : pass == PASS_DKV ? 32 : 64); }
+constexpr bool two_fit(AttentionPass pass, bool f32, int DP) { return DP <= (pass != PASS_DKV ? (f32 ? 64 : 128) : f32 ? 32 : 64); }
 // Few rows take one wave a workgroup.
 constexpr bool one_fits(bool f32, int DP) { return !f32 || DP <= 128; }
 
