@@ -11,6 +11,7 @@ struct AttentionArgs {
     float scale;
     const int* k_lengths; const uint8_t* key_mask;
     void* out; float* lse;                 // [B][Lq][HK * per][D]; [B][HK * per][Lq] or null
+    void *k3, *v3, *q3, *o3;                // fp32: three bf16 planes of k and v, q and d_out, [3][B][L][H][D] each
     float* part_o; float* part_ml;         // splits > 1: [splits][B * HK][rows][D] sums, [..][2] {exponent of two, sum}
     // gradient
     const void* o; const float* saved_lse; const void* d_out;
@@ -19,7 +20,8 @@ struct AttentionArgs {
     float *part_q, *part_k, *part_v;       // splits > 1: [splits] of the gradient's elements
 };
 // How a call is cut up: `tile` rows (keys) a workgroup of `waves` waves, `splits` shares of `share` keys (rows) each.
-struct AttentionPlan { int waves, blocks, tile, tiles, splits, share; };
+// `planes`: fp32 tiles come from three planes that are made first.
+struct AttentionPlan { int waves, blocks, tile, tiles, splits, share; bool planes; };
 enum AttentionPass { PASS_FORWARD = 0, PASS_DQ, PASS_DKV };
 AttentionPlan attention_plan(corr_dtype t, AttentionPass pass, int B, int Lq, int Lk, int HK, int per, int D);
 __host__ __device__ static inline int attention_aux_rows(int rows) { return (rows + 63) & ~63; }

@@ -6,6 +6,9 @@
 
 namespace {
 
+#ifndef PLANES_FROM
+#define PLANES_FROM 256
+#endif
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.69314718055994531f;
 constexpr unsigned PAST = 0x80000000u;      // an offset past every resource's end: the load into LDS writes zeros
 constexpr unsigned RANGE = 0x7ffffff0u;
@@ -99,6 +102,12 @@ template <> struct Num<float> {
         return pack(x);
     }
 };
+// fp32 whose tiles come from three planes that were made before (split_kernel): they land in LDS by themselves, as 16-bit ones do.
+struct Planes;
+template <> struct Num<Planes> : Num<float> {};
+template <class T> struct Elem { typedef T type; };
+template <> struct Elem<Planes> { typedef float type; };
+template <class T> constexpr bool F32 = std::is_same<typename Elem<T>::type, float>::value;
 // Weights as a product's operand.  fp16's normal values begin at 6e-5, below which a softmax over many keys lies: they are held 2^14 times as
 // large (at most 16384), and the results divided by that.
 template <class T> constexpr float LIFT = std::is_same<T, _Float16>::value ? 14.f : 0.f;
@@ -108,7 +117,9 @@ template <class T> constexpr float LIFT = std::is_same<T, _Float16>::value ? 14.
 template <class T> constexpr float SLACK = std::is_same<T, _Float16>::value ? 1.75f : 8.f;
 
 // rows (keys) of a tile in LDS: 64, or 32 where 64 would take more than 16 KB (24 in fp32's planes)
-template <class T, int DP, int WAVES> constexpr int tile_rows() { return DP <= (WAVES == 1 ? 32 : std::is_same<T, float>::value ? 64 : 128) ? 64 : 32; }
+template <class T, int DP, int WAVES> constexpr int tile_rows() {
+    return DP <= (WAVES == 1 || std::is_same<T, Planes>::value ? 32 : std::is_same<T, float>::value ? 64 : 128) ? 64 : 32;
+}
 
 // the largest (sum) over the four lanes that share lane & 15
 struct Both { float one, two; };
@@ -189,8 +200,21 @@ struct Tile<float, DP, ROWS, WAVES> {
         }
     }
 };
+// Planes: two places where they are 24 KB together, else one, whose loads start when the last tiles have been read.
+template <int DP, int ROWS, int WAVES>
+struct Tile<Planes, DP, ROWS, WAVES> : Tile<__bf16, DP, ROWS, WAVES> {
+    typedef Tile<__bf16, DP, ROWS, WAVES> Plane;
+    static constexpr int BYTES = 3 * Plane::BYTES, PLACES = BYTES <= 12288 ? 2 : 1;
+    template <class O> __device__ __forceinline__ void ask(const __bf16* p, int64_t plane, unsigned lds, int wave, O offset) {
+#pragma unroll
+        for (int q = 0; q < 3; ++q) Plane::ask(p + q * plane, lds + q * Plane::BYTES, wave, offset);
+    }
+};
+template <class L> struct Late { static constexpr bool value = false; };
+template <int DP, int ROWS, int WAVES> struct Late<Tile<Planes, DP, ROWS, WAVES>> { static constexpr bool value = Tile<Planes, DP, ROWS, WAVES>::PLACES == 1; };
+
 template <class L> __device__ __forceinline__ void land(const L& one, const L& two, unsigned char* smem) {
-    if constexpr (L::PLACES == 2) arrive_all();
+    if constexpr (L::PLACES == 2 || Late<L>::value) arrive_all();
     else {
         __syncthreads();                                 // the last tiles have been read
         one.store(smem);
@@ -220,6 +244,28 @@ template <class T> __device__ __forceinline__ Keys keys_of(const AttentionArgs& 
 // Tiles of a head follow each other, and so meet its keys at about the same time on every XCD.  Runs of a head's tiles on one XCD would leave XCDs
 // idle whose items are short.
 struct Place { int b, hk, bh, tile, split; };
+// Rows of one head of k or v from some key on: of the caller's array, or of the planes.
+template <class T> struct Source {
+    const T* p; int64_t row;
+    template <class L> __device__ __forceinline__ void ask(L& load, int first, unsigned to, int wave, uint64_t bits) const {
+        const unsigned step = (unsigned)(row * (int)sizeof(T));
+        load.ask(p + first * row, to, wave, [&](int r) { return (bits >> r) & 1 ? r * step : PAST; });
+    }
+};
+template <> struct Source<Planes> {
+    const __bf16* p; int64_t row, plane;
+    template <class L> __device__ __forceinline__ void ask(L& load, int first, unsigned to, int wave, uint64_t bits) const {
+        const unsigned step = (unsigned)(row * 2);
+        load.ask(p + first * row, plane, to, wave, [&](int r) { return (bits >> r) & 1 ? r * step : PAST; });
+    }
+};
+template <class T>
+__device__ __forceinline__ Source<T> source(const void* p, const void* planes, int64_t item, int64_t row, int64_t head, const AttentionArgs& a, const Place& at, int first) {
+    if constexpr (std::is_same<T, Planes>::value) {
+        const int64_t dense = (int64_t)a.HK * a.D;
+        return {(const __bf16*)planes + ((int64_t)at.b * a.Lk + first) * dense + at.hk * a.D, dense, a.B * a.Lk * dense};
+    } else return {(const T*)p + at.b * item + at.hk * head + first * row, row};
+}
 __device__ __forceinline__ Place place_of(const AttentionArgs& a, int tiles, int splits) {
     const int n = blockIdx.x;
     Place p;
@@ -243,6 +289,7 @@ __device__ __forceinline__ void query_of(const AttentionArgs& a, int r, int& q, 
 template <class T, int DP, int WAVES, int QB>
 __global__ __launch_bounds__(64 * WAVES, WAVES == 1 ? 1 : 2) void forward_kernel(AttentionArgs a, int tiles, int splits, int share) {
     typedef Num<T> N;
+    typedef typename Elem<T>::type E;
     typedef typename N::F F;
     constexpr int KT = tile_rows<T, DP, WAVES>(), KB = KT / 16, CH = DP / FK, DB = DP / 16;
     typedef Tile<T, DP, KT, WAVES> Load;
@@ -255,8 +302,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 1 ? 1 : 2) void forward_kernel
     const int k_lo = at.split * share;
     keys.end = min(keys.end, k_lo + share);
     const int steps = keys.end > k_lo ? (keys.end - k_lo + KT - 1) / KT : 0;
-    const T* const K0 = (const T*)a.k + at.b * a.k_item + at.hk * a.k_head + k_lo * a.k_row;
-    const T* const V0 = (const T*)a.v + at.b * a.v_item + at.hk * a.v_head + k_lo * a.v_row;
+    const Source<T> from_k = source<T>(a.k, a.k3, a.k_item, a.k_row, a.k_head, a, at, k_lo), from_v = source<T>(a.v, a.v3, a.v_item, a.v_row, a.v_head, a, at, k_lo);
     const int r0 = (at.tile * WAVES + wave) * 16 * QB;
     F fq[QB][CH];
 #pragma unroll
@@ -264,7 +310,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 1 ? 1 : 2) void forward_kernel
         const int r = r0 + 16 * j + lr;
         int q, g;
         query_of(a, r, q, g);
-        const T* p = (const T*)a.q + at.b * a.q_item + (at.hk * a.per + g) * a.q_head + q * a.q_row;
+        const E* p = (const E*)a.q + at.b * a.q_item + (at.hk * a.per + g) * a.q_head + q * a.q_row;
 #pragma unroll
         for (int t = 0; t < CH; ++t) fq[j][t] = N::load(p, t * FK + lg * 8, a.D, r < a.rows);
     }
@@ -273,9 +319,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 1 ? 1 : 2) void forward_kernel
     load_v.plan(wave, lane, a.D);
     auto ask = [&](int t, uint64_t bits) {
         const unsigned to = lds_at + t % Load::PLACES * 2 * Load::BYTES;
-        const unsigned k_step = (unsigned)(a.k_row * (int)sizeof(T)), v_step = (unsigned)(a.v_row * (int)sizeof(T));
-        load_k.ask(K0 + (int64_t)t * KT * a.k_row, to, wave, [&](int r) { return (bits >> r) & 1 ? r * k_step : PAST; });
-        load_v.ask(V0 + (int64_t)t * KT * a.v_row, to + Load::BYTES, wave, [&](int r) { return (bits >> r) & 1 ? r * v_step : PAST; });
+        from_k.ask(load_k, t * KT, to, wave, bits);
+        from_v.ask(load_v, t * KT, to + Load::BYTES, wave, bits);
     };
     const float c = a.scale * LOG2E;
     const float slack = SLACK<T> / c;
@@ -287,15 +332,19 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 1 ? 1 : 2) void forward_kernel
     unsigned byte = 0;
     if (steps) {
         bits = keys.bits(k_lo, KT, keys.byte(k_lo, lane));
-        if (bits) ask(0, bits);
+        if (bits && !Late<Load>::value) ask(0, bits);
         byte = keys.byte(k_lo + KT, lane);
     }
     for (int t = 0; t < steps; ++t) {
+        if constexpr (Late<Load>::value) {
+            __syncthreads();
+            if (bits) ask(t, bits);
+        }
         land(load_k, load_v, smem);
         uint64_t next = 0;
         if (t + 1 < steps) {
             next = keys.bits(k_lo + (t + 1) * KT, KT, byte);
-            if (next) ask(t + 1, next);
+            if (next && !Late<Load>::value) ask(t + 1, next);
             byte = keys.byte(k_lo + (t + 2) * KT, lane);
         }
         if (bits) {
@@ -384,11 +433,11 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 1 ? 1 : 2) void forward_kernel
             continue;
         }
         const float by = sum == 0.f ? 0.f : 1.f / sum;
-        T* const p = (T*)a.out + (((int64_t)at.b * a.Lq + q) * a.HK * a.per + head) * a.D;
+        E* const p = (E*)a.out + (((int64_t)at.b * a.Lq + q) * a.HK * a.per + head) * a.D;
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
             const float v[4] = {o[d][j][0] * by, o[d][j][1] * by, o[d][j][2] * by, o[d][j][3] * by};
-            if (16 * d + 4 * lg < a.D) store_some<T, 4>(p + 16 * d + 4 * lg, v, 4);
+            if (16 * d + 4 * lg < a.D) store_some<E, 4>(p + 16 * d + 4 * lg, v, 4);
         }
         if (a.lse && lg == 0)
             a.lse[((int64_t)at.b * a.HK * a.per + head) * a.Lq + q] = sum == 0.f ? -INFINITY : (mc[j] - LIFT<T> + log2f(sum)) * LN2;
@@ -510,6 +559,7 @@ template <class T, int N> struct Lifted {
 template <class T, int DP, int QB>
 __global__ __launch_bounds__(256, 2) void dq_kernel(AttentionArgs a, int tiles, int splits, int share) {
     typedef Num<T> N;
+    typedef typename Elem<T>::type E;
     typedef typename N::F F;
     constexpr int KT = tile_rows<T, DP, 4>(), CH = DP / FK, DB = DP / 16, PB = 2;
     typedef Tile<T, DP, KT, 4> Load;
@@ -522,8 +572,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(AttentionArgs a, int tiles, 
     const int k_lo = at.split * share;
     keys.end = min(keys.end, k_lo + share);
     const int steps = keys.end > k_lo ? (keys.end - k_lo + KT - 1) / KT : 0;
-    const T* const K0 = (const T*)a.k + at.b * a.k_item + at.hk * a.k_head + k_lo * a.k_row;
-    const T* const V0 = (const T*)a.v + at.b * a.v_item + at.hk * a.v_head + k_lo * a.v_row;
+    const Source<T> from_k = source<T>(a.k, a.k3, a.k_item, a.k_row, a.k_head, a, at, k_lo), from_v = source<T>(a.v, a.v3, a.v_item, a.v_row, a.v_head, a, at, k_lo);
     const int r0 = (at.tile * 4 + wave) * 16 * QB;
     F fq[QB][CH], fo[QB][CH];
     float low[QB], delta[QB];
@@ -534,8 +583,8 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(AttentionArgs a, int tiles, 
         int q, g;
         query_of(a, r, q, g);
         const int head = at.hk * a.per + g;
-        const T* p = (const T*)a.q + at.b * a.q_item + head * a.q_head + q * a.q_row;
-        const T* w = (const T*)a.d_out + (((int64_t)at.b * a.Lq + q) * a.HK * a.per + head) * a.D;
+        const E* p = (const E*)a.q + at.b * a.q_item + head * a.q_head + q * a.q_row;
+        const E* w = (const E*)a.d_out + (((int64_t)at.b * a.Lq + q) * a.HK * a.per + head) * a.D;
 #pragma unroll
         for (int t = 0; t < CH; ++t) {
             fq[j][t] = N::load(p, t * FK + lg * 8, a.D, there);
@@ -550,9 +599,8 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(AttentionArgs a, int tiles, 
     load_v.plan(wave, lane, a.D);
     auto ask = [&](int t, uint64_t bits) {
         const unsigned to = lds_at + t % Load::PLACES * 2 * Load::BYTES;
-        const unsigned k_step = (unsigned)(a.k_row * (int)sizeof(T)), v_step = (unsigned)(a.v_row * (int)sizeof(T));
-        load_k.ask(K0 + (int64_t)t * KT * a.k_row, to, wave, [&](int r) { return (bits >> r) & 1 ? r * k_step : PAST; });
-        load_v.ask(V0 + (int64_t)t * KT * a.v_row, to + Load::BYTES, wave, [&](int r) { return (bits >> r) & 1 ? r * v_step : PAST; });
+        from_k.ask(load_k, t * KT, to, wave, bits);
+        from_v.ask(load_v, t * KT, to + Load::BYTES, wave, bits);
     };
     const float c = a.scale * LOG2E;
     f32x4 dq[DB][QB] = {};
@@ -561,15 +609,19 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(AttentionArgs a, int tiles, 
     unsigned byte = 0;
     if (steps) {
         bits = keys.bits(k_lo, KT, keys.byte(k_lo, lane));
-        if (bits) ask(0, bits);
+        if (bits && !Late<Load>::value) ask(0, bits);
         byte = keys.byte(k_lo + KT, lane);
     }
     for (int t = 0; t < steps; ++t) {
+        if constexpr (Late<Load>::value) {
+            __syncthreads();
+            if (bits) ask(t, bits);
+        }
         land(load_k, load_v, smem);
         uint64_t next = 0;
         if (t + 1 < steps) {
             next = keys.bits(k_lo + (t + 1) * KT, KT, byte);
-            if (next) ask(t + 1, next);
+            if (next && !Late<Load>::value) ask(t + 1, next);
             byte = keys.byte(k_lo + (t + 2) * KT, lane);
         }
         if (bits) {
@@ -629,7 +681,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(AttentionArgs a, int tiles, 
             if (16 * d + 4 * lg >= a.D) continue;
             const float v[4] = {dq[d][j][0] * by, dq[d][j][1] * by, dq[d][j][2] * by, dq[d][j][3] * by};
             if (splits > 1) store_some<float, 4>(a.part_q + (int64_t)at.split * a.B * a.Lq * a.HK * a.per * a.D + row + 16 * d + 4 * lg, v, 4);
-            else store_some<T, 4>((T*)a.d_q + row + 16 * d + 4 * lg, v, 4);
+            else store_some<E, 4>((E*)a.d_q + row + 16 * d + 4 * lg, v, 4);
         }
     }
 }
@@ -639,6 +691,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(AttentionArgs a, int tiles, 
 template <class T, int DP, int KB>
 __global__ __launch_bounds__(256, 2) void dkv_kernel(AttentionArgs a, int tiles, int splits, int share) {
     typedef Num<T> N;
+    typedef typename Elem<T>::type E;
     typedef typename N::F F;
     constexpr int RT = tile_rows<T, DP, 4>(), CH = DP / FK, DB = DP / 16, PB = 2;
     typedef Tile<T, DP, RT, 4> Load;
@@ -657,8 +710,8 @@ __global__ __launch_bounds__(256, 2) void dkv_kernel(AttentionArgs a, int tiles,
         const int k = k0 + 16 * j + lr;
         counts[j] = k < keys.end && (!keys.mask || keys.mask[k]);
         any |= counts[j];
-        const T* p = (const T*)a.k + at.b * a.k_item + at.hk * a.k_head + k * a.k_row;
-        const T* w = (const T*)a.v + at.b * a.v_item + at.hk * a.v_head + k * a.v_row;
+        const E* p = (const E*)a.k + at.b * a.k_item + at.hk * a.k_head + k * a.k_row;
+        const E* w = (const E*)a.v + at.b * a.v_item + at.hk * a.v_head + k * a.v_row;
 #pragma unroll
         for (int t = 0; t < CH; ++t) {
             fk[j][t] = N::load(p, t * FK + lg * 8, a.D, counts[j]);
@@ -666,8 +719,6 @@ __global__ __launch_bounds__(256, 2) void dkv_kernel(AttentionArgs a, int tiles,
         }
     }
     const int steps = __syncthreads_or(any) ? (r_hi - r_lo + RT - 1) / RT : 0;
-    const T* const Q0 = (const T*)a.q + at.b * a.q_item + (int64_t)at.hk * a.per * a.q_head;
-    const T* const O0 = (const T*)a.d_out + (int64_t)at.b * a.Lq * a.HK * a.per * a.D + (int64_t)at.hk * a.per * a.D;
     const int64_t o_row = (int64_t)a.HK * a.per * a.D;
     Load load_q, load_o;
     load_q.plan(wave, lane, a.D);
@@ -677,24 +728,35 @@ __global__ __launch_bounds__(256, 2) void dkv_kernel(AttentionArgs a, int tiles,
         const int r0 = r_lo + t * RT;
         int q0, g0;
         query_of(a, r0, q0, g0);
-        auto rows = [&](int row, int head) {             // byte offsets of rows from query q0 on
+        auto rows = [&](int row, int head, int es) {     // byte offsets of rows from query q0 on
             return [=, &a](int i) {
                 int q, g;
                 query_of(a, r0 + i, q, g);
-                return r0 + i < r_hi ? (unsigned)(((q - q0) * row + g * head) * (int)sizeof(T)) : PAST;
+                return r0 + i < r_hi ? (unsigned)(((q - q0) * row + g * head) * es) : PAST;
             };
         };
-        load_q.ask(Q0 + q0 * a.q_row, to, wave, rows((int)a.q_row, (int)a.q_head));
-        load_o.ask(O0 + q0 * o_row, to + Load::BYTES, wave, rows((int)o_row, a.D));
+        const int64_t dense = ((int64_t)at.b * a.Lq + q0) * o_row + (int64_t)at.hk * a.per * a.D;
+        if constexpr (std::is_same<T, Planes>::value) {
+            const int64_t plane = (int64_t)a.B * a.Lq * o_row;
+            load_q.ask((const __bf16*)a.q3 + dense, plane, to, wave, rows((int)o_row, a.D, 2));
+            load_o.ask((const __bf16*)a.o3 + dense, plane, to + Load::BYTES, wave, rows((int)o_row, a.D, 2));
+        } else {
+            load_q.ask((const T*)a.q + at.b * a.q_item + (int64_t)at.hk * a.per * a.q_head + q0 * a.q_row, to, wave, rows((int)a.q_row, (int)a.q_head, sizeof(T)));
+            load_o.ask((const T*)a.d_out + dense, to + Load::BYTES, wave, rows((int)o_row, a.D, sizeof(T)));
+        }
     };
     const float c = a.scale * LOG2E;
     const float* const aux = a.aux + 2 * (int64_t)at.bh * attention_aux_rows(a.rows);
     f32x4 dk[DB][KB] = {}, dv[DB][KB] = {};
     Lifted<T, KB> lifted;
-    if (steps) ask(0);
+    if (steps && !Late<Load>::value) ask(0);
     for (int t = 0; t < steps; ++t) {
+        if constexpr (Late<Load>::value) {
+            __syncthreads();
+            ask(t);
+        }
         land(load_q, load_o, smem);
-        if (t + 1 < steps) ask(t + 1);
+        if (t + 1 < steps && !Late<Load>::value) ask(t + 1);
         lds_byte* const tq = lds + t % Load::PLACES * 2 * Load::BYTES;
         lds_byte* const to = tq + Load::BYTES;
 #pragma unroll
@@ -773,8 +835,8 @@ __global__ __launch_bounds__(256, 2) void dkv_kernel(AttentionArgs a, int tiles,
                 store_some<float, 4>(a.part_k + at.split * all + to, x, 4);
                 store_some<float, 4>(a.part_v + at.split * all + to, y, 4);
             } else {
-                store_some<T, 4>((T*)a.d_k + to, x, 4);
-                store_some<T, 4>((T*)a.d_v + to, y, 4);
+                store_some<E, 4>((E*)a.d_k + to, x, 4);
+                store_some<E, 4>((E*)a.d_v + to, y, 4);
             }
         }
     }
@@ -793,19 +855,65 @@ __global__ __launch_bounds__(256) void sum_kernel(const float* one, const float*
     store_some<T, 4>((blockIdx.y ? to_two : to_one) + 4 * i, v, 4);
 }
 
+// fp32 arrays' three planes, [3][B][L][H][D] each: four elements a thread.  A pair of arrays in one launch.
+struct Pair { const float* p; int64_t item, row, head; __bf16* to; };
+__global__ __launch_bounds__(256) void split_kernel(Pair one, Pair two, int L, int H, int D, int64_t quads) {
+    const Pair& x = blockIdx.y ? two : one;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= quads) return;
+    const int across = D / 4;
+    const int64_t n = i / across, r = n / H;
+    const int d = (int)(i - n * across) * 4, h = (int)(n - r * H), b = (int)(r / L);
+    const Some<float, 4>::type v = *reinterpret_cast<const Some<float, 4>::type*>(x.p + b * x.item + (r - (int64_t)b * L) * x.row + h * x.head + d);
+    u32x2 parts[3];
+    split4(f32x4{v[0], v[1], v[2], v[3]}, parts);
+#pragma unroll
+    for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x2*>(x.to + (q * quads + i) * 4) = parts[q];
+}
+void split(const Pair& one, const Pair& two, int B, int L, int H, int D, hipStream_t s) {
+    const int64_t quads = (int64_t)B * L * H * (D / 4);
+    hipLaunchKernelGGL(split_kernel, dim3(cdiv(quads, 256), 2), dim3(256), 0, s, one, two, L, H, D, quads);
+}
+
 // Where two blocks of 16 rows (keys) a wave fit its registers.
 constexpr bool two_fit(AttentionPass pass, bool f32, int DP) { return DP <= (pass != PASS_DKV ? (f32 ? 64 : 128) : f32 ? 32 : 64); }
 // Few rows take one wave a workgroup.
 constexpr bool one_fits(bool f32, int DP) { return !f32 || DP <= 128; }
 
 template <class T, int DP>
-hipError_t forward(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) {
+void forward_pass(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) {
     const dim3 grid(p.tiles * p.splits * a.B * a.HK);
-    constexpr bool F32 = std::is_same<T, float>::value;
-    if (p.waves == 1) {
-        if constexpr (one_fits(F32, DP)) hipLaunchKernelGGL((forward_kernel<T, DP, 1, 1>), grid, dim3(64), 0, s, a, p.tiles, p.splits, p.share);
-    } else if (p.blocks == 1) hipLaunchKernelGGL((forward_kernel<T, DP, 4, 1>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
-    else if constexpr (two_fit(PASS_FORWARD, F32, DP)) hipLaunchKernelGGL((forward_kernel<T, DP, 4, 2>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
+    if (p.blocks == 1) hipLaunchKernelGGL((forward_kernel<T, DP, 4, 1>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
+    else if constexpr (two_fit(PASS_FORWARD, F32<T>, DP)) hipLaunchKernelGGL((forward_kernel<T, DP, 4, 2>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
+}
+template <class T, int DP>
+void dq_pass(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) {
+    const dim3 grid(p.tiles * p.splits * a.B * a.HK);
+    if (p.blocks == 1) hipLaunchKernelGGL((dq_kernel<T, DP, 1>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
+    else if constexpr (two_fit(PASS_DQ, F32<T>, DP)) hipLaunchKernelGGL((dq_kernel<T, DP, 2>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
+}
+template <class T, int DP>
+void dkv_pass(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) {
+    const dim3 grid(p.tiles * p.splits * a.B * a.HK);
+    if (p.blocks == 1) hipLaunchKernelGGL((dkv_kernel<T, DP, 1>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
+    else if constexpr (two_fit(PASS_DKV, F32<T>, DP)) hipLaunchKernelGGL((dkv_kernel<T, DP, 2>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
+}
+void split_keys(const AttentionArgs& a, hipStream_t s) {
+    split({(const float*)a.k, a.k_item, a.k_row, a.k_head, (__bf16*)a.k3}, {(const float*)a.v, a.v_item, a.v_row, a.v_head, (__bf16*)a.v3}, a.B, a.Lk, a.HK, a.D, s);
+}
+template <class T, int DP>
+hipError_t forward(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) {
+    bool done = false;
+    if constexpr (F32<T>) if (p.planes) {
+        split_keys(a, s);
+        forward_pass<Planes, DP>(a, p, s);
+        done = true;
+    }
+    if constexpr (one_fits(F32<T>, DP)) if (p.waves == 1) {
+        hipLaunchKernelGGL((forward_kernel<T, DP, 1, 1>), dim3(p.tiles * p.splits * a.B * a.HK), dim3(64), 0, s, a, p.tiles, p.splits, p.share);
+        done = true;
+    }
+    if (!done) forward_pass<T, DP>(a, p, s);
     if (p.splits > 1) {
         int across = 2, shares = 1;
         while (4 * across < a.D) across *= 2;
@@ -818,20 +926,29 @@ template <class T, int DP>
 hipError_t backward(const AttentionArgs& a, const AttentionPlan& pq, const AttentionPlan& pk, hipStream_t s) {
     const int aux_rows = attention_aux_rows(a.rows);
     hipLaunchKernelGGL(delta_kernel<T>, dim3(cdiv((int64_t)a.B * a.HK * aux_rows, 16)), dim3(256), 0, s, a, aux_rows);
-    constexpr bool F32 = std::is_same<T, float>::value;
     if (a.d_q) {
-        const dim3 grid(pq.tiles * pq.splits * a.B * a.HK);
-        if (pq.blocks == 1) hipLaunchKernelGGL((dq_kernel<T, DP, 1>), grid, dim3(256), 0, s, a, pq.tiles, pq.splits, pq.share);
-        else if constexpr (two_fit(PASS_DQ, F32, DP)) hipLaunchKernelGGL((dq_kernel<T, DP, 2>), grid, dim3(256), 0, s, a, pq.tiles, pq.splits, pq.share);
+        bool done = false;
+        if constexpr (F32<T>) if (pq.planes) {
+            split_keys(a, s);
+            dq_pass<Planes, DP>(a, pq, s);
+            done = true;
+        }
+        if (!done) dq_pass<T, DP>(a, pq, s);
         if (pq.splits > 1) {
             const int64_t quads = (int64_t)a.B * a.Lq * a.HK * a.per * a.D / 4;
             hipLaunchKernelGGL(sum_kernel<T>, dim3(cdiv(quads, 256)), dim3(256), 0, s, a.part_q, a.part_q, (T*)a.d_q, (T*)a.d_q, quads, pq.splits);
         }
     }
     if (a.d_k) {
-        const dim3 grid(pk.tiles * pk.splits * a.B * a.HK);
-        if (pk.blocks == 1) hipLaunchKernelGGL((dkv_kernel<T, DP, 1>), grid, dim3(256), 0, s, a, pk.tiles, pk.splits, pk.share);
-        else if constexpr (two_fit(PASS_DKV, F32, DP)) hipLaunchKernelGGL((dkv_kernel<T, DP, 2>), grid, dim3(256), 0, s, a, pk.tiles, pk.splits, pk.share);
+        bool done = false;
+        if constexpr (F32<T>) if (pk.planes) {
+            const int H = a.HK * a.per;
+            const int64_t row = (int64_t)H * a.D;
+            split({(const float*)a.q, a.q_item, a.q_row, a.q_head, (__bf16*)a.q3}, {(const float*)a.d_out, a.Lq * row, row, a.D, (__bf16*)a.o3}, a.B, a.Lq, H, a.D, s);
+            dkv_pass<Planes, DP>(a, pk, s);
+            done = true;
+        }
+        if (!done) dkv_pass<T, DP>(a, pk, s);
         if (pk.splits > 1) {
             const int64_t quads = (int64_t)a.B * a.Lk * a.HK * a.D / 4;
             hipLaunchKernelGGL(sum_kernel<T>, dim3(cdiv(quads, 256), 2), dim3(256), 0, s, a.part_k, a.part_v, (T*)a.d_k, (T*)a.d_v, quads, pk.splits);
@@ -856,6 +973,7 @@ AttentionPlan attention_plan(corr_dtype t, AttentionPass pass, int B, int Lq, in
     AttentionPlan p;
     p.waves = pass == PASS_FORWARD && along <= 16 && one_fits(f32, pad) ? 1 : 4;
     p.blocks = p.waves == 4 && two_fit(pass, f32, pad) && (int64_t)cdiv(along, 128) * B * HK >= 256 ? 2 : 1;
+    p.planes = f32 && p.waves == 4 && along >= PLANES_FROM;
     p.tile = 16 * p.waves * p.blocks;
     p.tiles = cdiv(along, p.tile);
     const int64_t groups = (int64_t)p.tiles * B * HK, want = p.waves == 1 ? 1280 : 512;

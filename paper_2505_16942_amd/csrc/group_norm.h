@@ -18,6 +18,8 @@ struct GroupNormArgs {
     float* part;                   // forward: [B][parts][C][2] {mean, squares about it}; gradient: [B][parts][2][C] {sum of dz hat, sum of dz}
     float* sums;                   // gradient: [B][2][C]
     int parts; int64_t share;
+    bool past;                     // y, d_x are stored past the caches
+    int held;                      // a workgroup holds a group: threads across its channels; else 0
 };
 // fills in parts and share
 void group_norm_plan(GroupNormArgs& a, bool gradient);

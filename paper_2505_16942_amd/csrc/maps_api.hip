@@ -51,7 +51,7 @@ AttentionArgs kernel_args(const corr_attention_args* a) {
 }
 bool too_many(const AttentionPlan& p, int64_t B, int64_t HK) { return (int64_t)p.tiles * p.splits * B * HK >= 1LL << 31; }
 
-struct AttentionLayout { AttentionPlan plan; size_t o, ml, total; };
+struct AttentionLayout { AttentionPlan plan; size_t o, ml, k3, v3, total; };
 AttentionLayout attention_layout(corr_dtype t, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t HK, int64_t D) {
     AttentionLayout l = {};
     Carver c;
@@ -59,10 +59,13 @@ AttentionLayout attention_layout(corr_dtype t, int64_t B, int64_t Lq, int64_t Lk
     const size_t rows = l.plan.splits > 1 ? (size_t)l.plan.splits * B * H * Lq : 0;
     l.o = c.take(rows * D * 4);
     l.ml = c.take(rows * 8);
+    const size_t planes = l.plan.planes ? (size_t)B * Lk * HK * D * 6 : 0;
+    l.k3 = c.take(planes);
+    l.v3 = c.take(planes);
     l.total = c.used;
     return l;
 }
-struct GradientLayout { AttentionPlan q, kv; size_t aux, part_q, part_k, part_v, total; };
+struct GradientLayout { AttentionPlan q, kv; size_t aux, part_q, part_k, part_v, k3, v3, q3, o3, total; };
 GradientLayout gradient_layout(corr_dtype t, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t HK, int64_t D) {
     GradientLayout l = {};
     Carver c;
@@ -74,6 +77,11 @@ GradientLayout gradient_layout(corr_dtype t, int64_t B, int64_t Lq, int64_t Lk, 
     const size_t keys = l.kv.splits > 1 ? (size_t)l.kv.splits * B * Lk * HK * D * 4 : 0;
     l.part_k = c.take(keys);
     l.part_v = c.take(keys);
+    const size_t key_planes = l.q.planes ? (size_t)B * Lk * HK * D * 6 : 0, row_planes = l.kv.planes ? (size_t)B * Lq * H * D * 6 : 0;
+    l.k3 = c.take(key_planes);
+    l.v3 = c.take(key_planes);
+    l.q3 = c.take(row_planes);
+    l.o3 = c.take(row_planes);
     l.total = c.used;
     return l;
 }
@@ -195,6 +203,7 @@ corr_status corr_attention(const corr_attention_args* a, void* out, float* lse, 
     k.out = out; k.lse = lse;
     char* const ws = static_cast<char*>(workspace);
     k.part_o = reinterpret_cast<float*>(ws + l.o); k.part_ml = reinterpret_cast<float*>(ws + l.ml);
+    k.k3 = ws + l.k3; k.v3 = ws + l.v3;
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = hipErrorInvalidValue;
 #define TYPE(T, name) if (a->type == CORR_TYPE_##T) e = launch_attention_##name(k, l.plan, s);
@@ -241,6 +250,7 @@ corr_status corr_attention_backward(const corr_attention_args* a, const void* ou
     k.part_q = reinterpret_cast<float*>(ws + l.part_q);
     k.part_k = reinterpret_cast<float*>(ws + l.part_k);
     k.part_v = reinterpret_cast<float*>(ws + l.part_v);
+    k.k3 = ws + l.k3; k.v3 = ws + l.v3; k.q3 = ws + l.q3; k.o3 = ws + l.o3;
     k.d_q = d_q; k.d_k = d_k; k.d_v = d_v;
     e = hipErrorInvalidValue;
 #define TYPE(T, name) if (a->type == CORR_TYPE_##T) e = launch_attention_backward_##name(k, l.q, l.kv, s);
