@@ -6,9 +6,6 @@
 
 namespace {
 
-#ifndef PLANES_FROM
-#define PLANES_FROM 256
-#endif
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.69314718055994531f;
 constexpr unsigned PAST = 0x80000000u;      // an offset past every resource's end: the load into LDS writes zeros
 constexpr unsigned RANGE = 0x7ffffff0u;
@@ -964,22 +961,61 @@ hipError_t backward(const AttentionArgs& a, const AttentionPlan& pq, const Atten
 hipError_t launch_attention_f32(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) { return BY_LENGTH(forward, float, a, p, s); }
 hipError_t launch_attention_backward_f32(const AttentionArgs& a, const AttentionPlan& pq, const AttentionPlan& pk, hipStream_t s) { return BY_LENGTH(backward, float, a, pq, pk, s); }
 
-// Rows of a workgroup: 128 (two blocks of 16 a wave) where that gives one to every compute unit, else 64, and 16 in one wave where there are no more.
-// Shares of the long axis where there are still too few workgroups: as many as fill the chip, of four tiles at least.
+// What a call costs, in multiples of the time that a compute unit with all the workgroups it holds at a time (`held`) takes for a whole one: rounds
+// of them, the last one with fewer, which use the unit less well (2 x 2852 x 7285 x 4 x 64 fp32, 360 workgroups: forward 373 us, in two shares
+// 263, in three 294; 1 x 14400 x 14400 x 256 bf16, 225: 314 in two, 417 in three, 329 in four).
+namespace {
+double rounds(int64_t groups, int held) {
+    const int64_t whole = groups / (256 * held), rest = groups - whole * 256 * held, n = (rest + 255) / 256;
+    const double use[] = {1, held == 1 ? 1. : held == 2 ? .65 : .6, held == 2 ? 1. : .85, 1, 1};
+    return whole * held + n / use[n];
+}
+// as the kernels' registers and LDS allow
+int held_at_once(bool f32, AttentionPass pass, int pad, int blocks) {
+    if (pad == 256) return f32 ? 1 : 2;
+    if (pad == 128) return f32 && pass == PASS_FORWARD ? 3 : 2;
+    if (f32) return blocks == 2 && pass == (pad == 64 ? PASS_DQ : PASS_DKV) ? 2 : 3;
+    return pad == 32 || blocks == 1 ? 4 : pass == PASS_DKV ? 2 : 3;
+}
+}  // namespace
+
+// Rows of a workgroup: 16 in one wave where there are no more (shares of the keys for five on every compute unit), else 64, or 128 in two blocks of 16
+// a wave.  Shares of the long axis, of four tiles at least, where they make the rounds of workgroups fuller by more than their join costs (about
+// 4 us and the sums' way to memory and back).
 AttentionPlan attention_plan(corr_dtype t, AttentionPass pass, int B, int Lq, int Lk, int HK, int per, int D) {
     const int pad = D <= 32 ? 32 : D <= 64 ? 64 : D <= 128 ? 128 : 256;
     const bool f32 = t == CORR_TYPE_F32;
-    const int rows = Lq * per, along = pass == PASS_DKV ? Lk : rows, over = pass == PASS_DKV ? rows : Lk;
+    const int rows = Lq * per, along = pass == PASS_DKV ? Lk : rows, over = pass == PASS_DKV ? rows : Lk, most = over > 256 ? cdiv(over, 256) : 1;
+    const int64_t heads = (int64_t)B * HK;
     AttentionPlan p;
     p.waves = pass == PASS_FORWARD && along <= 16 && one_fits(f32, pad) ? 1 : 4;
-    p.blocks = p.waves == 4 && two_fit(pass, f32, pad) && (int64_t)cdiv(along, 128) * B * HK >= 256 ? 2 : 1;
-    p.planes = f32 && p.waves == 4 && along >= PLANES_FROM;
+    p.blocks = 1;
+    // Planes are made once a call and read by every tile of rows: from 2048 rows on (2852 x 2852 x 4 x 32: 51 us, 53 without; 7200 x 7200 x 2 x 32: 102 and
+    // 117; 256 x 20000 x 2 x 128: 71 and 51).
+    p.planes = f32 && p.waves == 4 && along >= 2048;
+    int splits = 1;
+    if (p.waves == 1) {
+        const int64_t want = heads > 0 ? (1280 + heads - 1) / heads : 1;
+        splits = (int)(want < most ? want : most);
+    } else {
+        const int products = pass == PASS_FORWARD ? 2 : pass == PASS_DQ ? 3 : 4;
+        // products a microsecond of one compute unit, and the bytes that the join moves in one
+        const double rate = (f32 ? pad == 32 ? 140e6 : 190e6 : pad == 32 ? 450e6 : 700e6) / 256, bytes = 4e6;
+        double best = 1e30;
+        for (int blocks = 1; blocks <= (two_fit(pass, f32, pad) ? 2 : 1); ++blocks) {
+            const int64_t groups = cdiv(along, 64 * blocks) * heads;
+            const int held = held_at_once(f32, pass, pad, blocks);
+            // one block a wave reads its tiles for half as many products
+            const double one = (blocks == 1 ? pass == PASS_DKV ? 1.2 : 1.05 : 1.) * 2. * products * 64 * blocks * over * (double)pad / rate;
+            for (int s = 1; s <= most && (s == 1 || groups * (s - 1) < 2048); ++s) {
+                const double join = s == 1 ? 0 : 4 + 8. * s * heads * along * D * (pass == PASS_DKV ? 2 : 1) / bytes;
+                const double cost = rounds(groups * s, held) * one / s + join;
+                if (cost < best) { best = cost; splits = s; p.blocks = blocks; }
+            }
+        }
+    }
     p.tile = 16 * p.waves * p.blocks;
     p.tiles = cdiv(along, p.tile);
-    const int64_t groups = (int64_t)p.tiles * B * HK, want = p.waves == 1 ? 1280 : 512;
-    int64_t splits = groups < want / 2 ? want / (groups ? groups : 1) : 1;
-    const int most = over > 256 ? cdiv(over, 256) : 1;
-    if (splits > most) splits = most;
     p.share = over > 0 ? (cdiv(over, splits) + 63) & ~63 : 64;
     p.splits = over > 0 ? cdiv(over, p.share) : 1;
     return p;

@@ -27,7 +27,8 @@ def _gen(seed):
 SIZES = [(1, 1, 1, 1, 1, 8), (1, 1, 5, 2, 1, 32), (2, 1, 1000, 8, 2, 128), (1, 3, 70, 4, 4, 40), (1, 16, 64, 1, 1, 64), (2, 17, 65, 3, 1, 64),
          (1, 64, 63, 2, 2, 128), (1, 65, 129, 6, 2, 96), (3, 5, 33, 1, 1, 256), (1, 130, 31, 1, 1, 256), (1, 40, 700, 2, 1, 160), (1, 700, 40, 4, 2, 72),
          (2, 129, 300, 1, 1, 32), (1, 1, 3001, 1, 1, 64), (1, 2, 2, 128, 1, 16), (1, 257, 1, 2, 2, 24),
-         (1, 300, 290, 1, 1, 256), (2, 135, 270, 4, 2, 200), (1, 260, 330, 2, 2, 32)]
+         (1, 300, 290, 1, 1, 256), (2, 135, 270, 4, 2, 200), (1, 2100, 70, 1, 1, 24), (1, 70, 2100, 1, 1, 32), (1, 1025, 40, 2, 1, 64), (1, 40, 2060, 1, 1, 56),
+         (1, 2050, 33, 1, 1, 128), (2, 33, 2049, 1, 1, 104), (1, 2049, 65, 1, 1, 256), (1, 65, 2050, 1, 1, 200)]
 
 
 def _case(size, dtype, seed, sigma=2.0):

@@ -44,8 +44,9 @@ def _forward(b, **kw):
 
 
 @pytest.mark.parametrize("kw,status", REFUSED + [
-    (dict(out=None), -1), (dict(out=OUT + 1), -1), (dict(lse=LSE + 2), -1), (dict(ws=None), -1), (dict(size=64), -1), (dict(ws=WS + 8), -1),
-    (dict(out=Q), -1), (dict(out=K + 500 * 128 * 2), -1), (dict(out=V - 2), -1), (dict(lse=OUT), -1), (dict(ws=OUT), -1), (dict(ws=MASK), -1),
+    (dict(out=None), -1), (dict(out=OUT + 1), -1), (dict(lse=LSE + 2), -1), (dict(Lk=50000, ws=None), -1), (dict(Lk=50000, size=64), -1),
+    (dict(Lk=50000, ws=WS + 8), -1),
+    (dict(out=Q), -1), (dict(out=K + 500 * 128 * 2), -1), (dict(out=V - 2), -1), (dict(lse=OUT), -1), (dict(Lk=50000, ws=OUT), -1), (dict(Lk=50000, ws=MASK), -1),
     (dict(out=LENGTHS), -1), (dict(lse=Q + 4), -1),
 ])
 def test_attention_refusals(kw, status):
