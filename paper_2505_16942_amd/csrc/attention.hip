@@ -284,7 +284,7 @@ __device__ __forceinline__ void query_of(const AttentionArgs& a, int r, int& q, 
 // they lie.  Weights are rounded once to the operands' type (their sum is not): errors of single weights, at most half a step each, which the sum over
 // keys averages.
 template <class T, int DP, int WAVES, int QB>
-__global__ __launch_bounds__(64 * WAVES, WAVES == 1 ? 1 : 2) void forward_kernel(AttentionArgs a, int tiles, int splits, int share) {
+__global__ __launch_bounds__(64 * WAVES, WAVES == 1 || (DP == 256 && F32<T>) ? 1 : 2) void forward_kernel(AttentionArgs a, int tiles, int splits, int share) {
     typedef Num<T> N;
     typedef typename Elem<T>::type E;
     typedef typename N::F F;
@@ -491,7 +491,7 @@ __global__ __launch_bounds__(256) void forward_join_kernel(AttentionArgs a, int 
 
 // ---- gradient.  With P = exp(s - lse) and delta = sum over d of d_out out: dV = P^T dO, dS = P (dO V^T - delta), dQ = scale dS K,
 // dK = scale dS^T Q.  Rows' sums meet in one workgroup and keys' sums in another, so scores are computed twice and nothing is added by atomics.
-// delta, and lse in powers of two, in the order of rows; rows behind the last have a weight of zero.
+// delta, and lse in powers of two (less LIFT: the weights are 2^LIFT times as large), in the order of rows; rows behind the last have a weight of zero.
 template <class T>
 __global__ __launch_bounds__(256) void delta_kernel(AttentionArgs a, int aux_rows) {
     const int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
@@ -511,7 +511,7 @@ __global__ __launch_bounds__(256) void delta_kernel(AttentionArgs a, int aux_row
             for (int e = 0; e < 8; ++e) sum = fmaf(x[e], y[e], sum);
         }
         low = a.saved_lse[((int64_t)b * a.HK * a.per + head) * a.Lq + q] * LOG2E;
-        if (low == -INFINITY) low = INFINITY;            // a row without a key: no weight
+        low = low == -INFINITY ? INFINITY : low - LIFT<T>;       // a row without a key: no weight
     }
 #pragma unroll
     for (int x = 1; x < 16; x *= 2) sum += __shfl_xor(sum, x);
@@ -519,13 +519,14 @@ __global__ __launch_bounds__(256) void delta_kernel(AttentionArgs a, int aux_row
 }
 
 // dS as a product's operand.  bf16 has fp32's range: rounded once.  fp16 would lose what is small: a row's (key's) elements are held
-// times a power of two that brings the largest so far to 2^13 .. 2^15, and the sums follow when it changes.
+// times a power of two that brings the largest so far to 2^13 .. 2^15, and the sums follow when it changes.  The elements come 2^LIFT times as large, as the
+// weights in them.
 template <class T, int N> struct Lifted {
     static constexpr bool ON = std::is_same<T, _Float16>::value;
     float by[N];
     __device__ __forceinline__ Lifted() {
 #pragma unroll
-        for (int j = 0; j < N; ++j) by[j] = 0x1p60f;
+        for (int j = 0; j < N; ++j) by[j] = 0x1p46f;
     }
     // x: the tile's elements, [N][X] quads
     template <int X, int DB> __device__ __forceinline__ void lift(f32x4 (&x)[N][X], f32x4 (&sums)[DB][N]) {
@@ -550,11 +551,11 @@ template <class T, int N> struct Lifted {
             }
         }
     }
-    __device__ __forceinline__ float back(int j) const { return ON ? 1.f / by[j] : 1.f; }
+    __device__ __forceinline__ float back(int j) const { return ON ? 1.f / (16384.f * by[j]) : 1.f; }
 };
 
 template <class T, int DP, int QB>
-__global__ __launch_bounds__(256, 2) void dq_kernel(AttentionArgs a, int tiles, int splits, int share) {
+__global__ __launch_bounds__(256, DP == 256 && F32<T> ? 1 : 2) void dq_kernel(AttentionArgs a, int tiles, int splits, int share) {
     typedef Num<T> N;
     typedef typename Elem<T>::type E;
     typedef typename N::F F;
@@ -686,7 +687,7 @@ __global__ __launch_bounds__(256, 2) void dq_kernel(AttentionArgs a, int tiles, 
 // A workgroup has 64 KB keys in its waves' registers and goes over the rows of the query heads that read them.  S = Q K^T here: a lane has four rows
 // of one key.  A key that does not count has sums of its own, which are not stored.
 template <class T, int DP, int KB>
-__global__ __launch_bounds__(256, 2) void dkv_kernel(AttentionArgs a, int tiles, int splits, int share) {
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void dkv_kernel(AttentionArgs a, int tiles, int splits, int share) {
     typedef Num<T> N;
     typedef typename Elem<T>::type E;
     typedef typename N::F F;
@@ -792,7 +793,7 @@ __global__ __launch_bounds__(256, 2) void dkv_kernel(AttentionArgs a, int tiles,
                     for (int e = 0; e < 4; ++e) {
                         const float p = __builtin_amdgcn_exp2f(fmaf(s[j][i][e], c, -low[i][e]));
                         dp[j][i][e] = p * (dp[j][i][e] - delta[i][e]);
-                        s[j][i][e] = LIFT<T> ? p * 16384.f : p;
+                        s[j][i][e] = p;
                     }
                 fp[j] = N::pack(s[j]);
             }
@@ -972,7 +973,7 @@ double rounds(int64_t groups, int held) {
 }
 // as the kernels' registers and LDS allow
 int held_at_once(bool f32, AttentionPass pass, int pad, int blocks) {
-    if (pad == 256) return f32 ? 1 : 2;
+    if (pad == 256) return f32 || pass == PASS_DKV ? 1 : 2;
     if (pad == 128) return f32 && pass == PASS_FORWARD ? 3 : 2;
     if (f32) return blocks == 2 && pass == (pad == 64 ? PASS_DQ : PASS_DKV) ? 2 : 3;
     return pad == 32 || blocks == 1 ? 4 : pass == PASS_DKV ? 2 : 3;
