@@ -494,28 +494,30 @@ __global__ __launch_bounds__(256) void forward_join_kernel(AttentionArgs a, int 
 // delta, and lse in powers of two (less LIFT: the weights are 2^LIFT times as large), in the order of rows; rows behind the last have a weight of zero.
 template <class T>
 __global__ __launch_bounds__(256) void delta_kernel(AttentionArgs a, int aux_rows) {
-    const int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16;
-    const int lane = threadIdx.x & 15, bh = (int)(row / aux_rows), r = (int)(row - (int64_t)bh * aux_rows), b = bh / a.HK, hk = bh - b * a.HK;
-    if (row >= (int64_t)a.B * a.HK * aux_rows) return;
-    float sum = 0.f, low = INFINITY;
-    if (r < a.rows) {
-        int q, g;
-        query_of(a, r, q, g);
-        const int head = hk * a.per + g;
-        const int64_t at = (((int64_t)b * a.Lq + q) * a.HK * a.per + head) * a.D;
-        for (int d = 8 * lane; d < a.D; d += 128) {
-            float x[8], y[8];
-            load_some<T, 8>((const T*)a.o + at + d, x, 8);
-            load_some<T, 8>((const T*)a.d_out + at + d, y, 8);
+    const int lane = threadIdx.x & 15;
+    const int64_t all = (int64_t)a.B * a.HK * aux_rows;
+    for (int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 16; row < all; row += (int64_t)gridDim.x * 16) {      // 16 lanes a row
+        const int bh = (int)(row / aux_rows), r = (int)(row - (int64_t)bh * aux_rows), b = bh / a.HK, hk = bh - b * a.HK;
+        float sum = 0.f, low = INFINITY;
+        if (r < a.rows) {
+            int q, g;
+            query_of(a, r, q, g);
+            const int head = hk * a.per + g;
+            const int64_t at = (((int64_t)b * a.Lq + q) * a.HK * a.per + head) * a.D;
+            for (int d = 8 * lane; d < a.D; d += 128) {
+                float x[8], y[8];
+                load_some<T, 8>((const T*)a.o + at + d, x, 8);
+                load_some<T, 8>((const T*)a.d_out + at + d, y, 8);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum = fmaf(x[e], y[e], sum);
+                for (int e = 0; e < 8; ++e) sum = fmaf(x[e], y[e], sum);
+            }
+            low = a.saved_lse[((int64_t)b * a.HK * a.per + head) * a.Lq + q] * LOG2E;
+            low = low == -INFINITY ? INFINITY : low - LIFT<T>;           // a row without a key: no weight
         }
-        low = a.saved_lse[((int64_t)b * a.HK * a.per + head) * a.Lq + q] * LOG2E;
-        low = low == -INFINITY ? INFINITY : low - LIFT<T>;       // a row without a key: no weight
-    }
 #pragma unroll
-    for (int x = 1; x < 16; x *= 2) sum += __shfl_xor(sum, x);
-    if (lane == 0) { a.aux[2 * row] = low; a.aux[2 * row + 1] = low == INFINITY ? 0.f : sum; }
+        for (int x = 1; x < 16; x *= 2) sum += __shfl_xor(sum, x);
+        if (lane == 0) { a.aux[2 * row] = low; a.aux[2 * row + 1] = low == INFINITY ? 0.f : sum; }
+    }
 }
 
 // dS as a product's operand.  bf16 has fp32's range: rounded once.  fp16 would lose what is small: a row's (key's) elements are held
@@ -857,20 +859,21 @@ __global__ __launch_bounds__(256) void sum_kernel(const float* one, const float*
 struct Pair { const float* p; int64_t item, row, head; __bf16* to; };
 __global__ __launch_bounds__(256) void split_kernel(Pair one, Pair two, int L, int H, int D, int64_t quads) {
     const Pair& x = blockIdx.y ? two : one;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= quads) return;
     const int across = D / 4;
-    const int64_t n = i / across, r = n / H;
-    const int d = (int)(i - n * across) * 4, h = (int)(n - r * H), b = (int)(r / L);
-    const Some<float, 4>::type v = *reinterpret_cast<const Some<float, 4>::type*>(x.p + b * x.item + (r - (int64_t)b * L) * x.row + h * x.head + d);
-    u32x2 parts[3];
-    split4(f32x4{v[0], v[1], v[2], v[3]}, parts);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < quads; i += (int64_t)gridDim.x * 256) {
+        const int64_t n = i / across, r = n / H;
+        const int d = (int)(i - n * across) * 4, h = (int)(n - r * H), b = (int)(r / L);
+        const Some<float, 4>::type v = *reinterpret_cast<const Some<float, 4>::type*>(x.p + b * x.item + (r - (int64_t)b * L) * x.row + h * x.head + d);
+        u32x2 parts[3];
+        split4(f32x4{v[0], v[1], v[2], v[3]}, parts);
 #pragma unroll
-    for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x2*>(x.to + (q * quads + i) * 4) = parts[q];
+        for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x2*>(x.to + (q * quads + i) * 4) = parts[q];
+    }
 }
+inline unsigned blocks_of(int64_t n) { return (unsigned)(n < 1 << 20 ? n : 1 << 20); }
 void split(const Pair& one, const Pair& two, int B, int L, int H, int D, hipStream_t s) {
     const int64_t quads = (int64_t)B * L * H * (D / 4);
-    hipLaunchKernelGGL(split_kernel, dim3(cdiv(quads, 256), 2), dim3(256), 0, s, one, two, L, H, D, quads);
+    hipLaunchKernelGGL(split_kernel, dim3(blocks_of((quads + 255) / 256), 2), dim3(256), 0, s, one, two, L, H, D, quads);
 }
 
 // Where two blocks of 16 rows (keys) a wave fit its registers.
@@ -923,7 +926,7 @@ hipError_t forward(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s
 template <class T, int DP>
 hipError_t backward(const AttentionArgs& a, const AttentionPlan& pq, const AttentionPlan& pk, hipStream_t s) {
     const int aux_rows = attention_aux_rows(a.rows);
-    hipLaunchKernelGGL(delta_kernel<T>, dim3(cdiv((int64_t)a.B * a.HK * aux_rows, 16)), dim3(256), 0, s, a, aux_rows);
+    hipLaunchKernelGGL(delta_kernel<T>, dim3(blocks_of(((int64_t)a.B * a.HK * aux_rows + 15) / 16)), dim3(256), 0, s, a, aux_rows);
     if (a.d_q) {
         bool done = false;
         if constexpr (F32<T>) if (pq.planes) {

@@ -49,7 +49,8 @@ AttentionArgs kernel_args(const corr_attention_args* a) {
     k.scale = a->scale; k.k_lengths = a->k_lengths; k.key_mask = a->key_mask;
     return k;
 }
-bool too_many(const AttentionPlan& p, int64_t B, int64_t HK) { return (int64_t)p.tiles * p.splits * B * HK >= 1LL << 31; }
+// a launch has fewer than 2^32 threads
+bool too_many(const AttentionPlan& p, int64_t B, int64_t HK) { return (int64_t)p.tiles * p.splits * B * HK * p.waves >= 1LL << 26; }
 
 struct AttentionLayout { AttentionPlan plan; size_t o, ml, k3, v3, total; };
 AttentionLayout attention_layout(corr_dtype t, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t HK, int64_t D) {

@@ -34,6 +34,7 @@ REFUSED = [
     (dict(k=K + 2), -1), (dict(v=V + 1), -1), (dict(q_row=255), -1), (dict(k_head=63), -1), (dict(v_item=-2), -1), (dict(q_row=(1 << 21) + 2), -2),
     (dict(k_row=(1 << 21) + 2), -2), (dict(v_head=(1 << 21) + 2), -2), (dict(q_item=(1 << 40) + 2), -2), (dict(scale=0.0), -1), (dict(scale=-1.0), -1),
     (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(k_lengths=LENGTHS + 2), -1),
+    (dict(B=1 << 20, H=1, HK=1, D=8, Lq=4096, Lk=8192), -2),          # more workgroups than a launch has
 ]
 
 
