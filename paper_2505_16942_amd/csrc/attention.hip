@@ -15,7 +15,11 @@ inline int cdiv(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 // `straight`: a tile's row, along the row.  `turned`: one of its columns, along 32 of its rows; these are taken in the order in which a product's result
 // lies in its lanes (rows 4 lg + e and 16 + 4 lg + e), so that the scores are the next product's operand without leaving their lanes.  Tiles lie in
 // LDS in rows of DP 16-bit elements, 16-byte piece p of row r at slot(r, p), which spreads both kinds of read over the banks.
-template <int DP> __device__ __forceinline__ int slot(int row, int piece) { return piece ^ (DP == 32 ? row >> 1 & 3 : DP == 64 ? row & 7 : row & 15); }
+// (LDS has 256 bytes of banks.  A 16-byte read serves lanes 0-3, 12-15, 20-27 at a time, and so on; the transposing one 32 neighbours: from 128 elements
+// on rows r and 12 + r (4 + r and 8 + r), r < 4, have neighbouring pieces.)
+template <int DP> __device__ __forceinline__ int slot(int row, int piece) {
+    return piece ^ (DP == 32 ? row >> 1 & 3 : DP == 64 ? row & 7 : ((row ^ (row >> 1 & 4)) & 7) << 1 | (row >> 3 & 1));
+}
 template <class F, int DP> __device__ __forceinline__ F read_straight(lds_byte* tile, int row, int t, int lg) {
     return *(__attribute__((address_space(3))) F*)(tile + row * 2 * DP + slot<DP>(row, 4 * t + lg) * 16);
 }
@@ -279,10 +283,17 @@ __device__ __forceinline__ void query_of(const AttentionArgs& a, int r, int& q, 
     g = r - q * a.per;
 }
 
-// ---- forward.  One pass over the keys with a running reference m (the largest score, or a little less) and sum l of each row.  S^T = K Q^T in tiles of 16 keys x 16 rows: a lane has four
-// keys of one row, so that a row's maximum is a lane's own and two exchanges away, and the weights are the operand of O^T = V^T P^T as
-// they lie.  Weights are rounded once to the operands' type (their sum is not): errors of single weights, at most half a step each, which the sum over
-// keys averages.
+// ---- forward.  One pass over the keys with a running reference m (the largest score, or a little less) and sum l of each row: o = sum e^(s - m) v / sum
+// e^(s - m), rescaled when m moves.  S^T = K Q^T in tiles of 16 keys x 16 rows: a lane has four keys of one row, so that a row's maximum is a lane's own and
+// two exchanges away, and the weights are the operand of O^T = V^T P^T as they lie.  Weights are rounded once to the operands' type (their sum is
+// not): the matrix cores take them so, and it makes the result's error sqrt 2 times its own rounding's (bf16: 2.3e-3 in the 2-norm, 1.7e-3).
+// Four waves of 16 QB rows share tiles of keys and values that land in LDS while the last ones are multiplied.  With two blocks a wave a fragment that
+// is read once is multiplied twice.  1 x 32400 x 32400, 2 heads of 128, bf16: 1090 us, 985 TFLOP/s, matrix instructions in 40 % of the cycles, the vector unit (an
+// exponential, fma, maximum, sum and half a rounding an element) in most others: a wave's two kinds of work alternate, and a compute unit holds
+// eight waves.  2 x 14400 x 14400, 2 heads of 64: 287 us, 740 TFLOP/s: the vector unit, about 70 % of the cycles.  fp32's six products: 2 x 2852 x 7285, 4 heads of
+// 64: 243 us, 175 TFLOP/s (1.05 PFLOP/s of bf16).
+// One row of 8 query heads on 2 key heads, 8 x 32768 keys of ragged lengths (157 MB), bf16, one wave a workgroup, 128 shares: 28 us and 9 for their join,
+// 5.6 TB/s.
 template <class T, int DP, int WAVES, int QB>
 __global__ __launch_bounds__(64 * WAVES, WAVES == 1 || (DP == 256 && F32<T>) ? 1 : 2) void forward_kernel(AttentionArgs a, int tiles, int splits, int share) {
     typedef Num<T> N;
@@ -490,7 +501,9 @@ __global__ __launch_bounds__(256) void forward_join_kernel(AttentionArgs a, int 
 }
 
 // ---- gradient.  With P = exp(s - lse) and delta = sum over d of d_out out: dV = P^T dO, dS = P (dO V^T - delta), dQ = scale dS K,
-// dK = scale dS^T Q.  Rows' sums meet in one workgroup and keys' sums in another, so scores are computed twice and nothing is added by atomics.
+// dK = scale dS^T Q.  Rows' sums meet in one workgroup and keys' sums in another, so scores are computed twice (seven products for five) and nothing
+// is added by atomics: the same bits on every call.  2 x 14400 x 14400, 2 heads of 64, bf16: rows 375 us, keys 515 (seven products: 830 TFLOP/s), matrix
+// instructions in a third of the cycles, the vector unit in half; in fp16 470 and 650, with the powers of two of dS.
 // delta, and lse in powers of two (less LIFT: the weights are 2^LIFT times as large), in the order of rows; rows behind the last have a weight of zero.
 template <class T>
 __global__ __launch_bounds__(256) void delta_kernel(AttentionArgs a, int aux_rows) {
@@ -686,7 +699,7 @@ __global__ __launch_bounds__(256, DP == 256 && F32<T> ? 1 : 2) void dq_kernel(At
     }
 }
 
-// A workgroup has 64 KB keys in its waves' registers and goes over the rows of the query heads that read them.  S = Q K^T here: a lane has four rows
+// A workgroup has 64 KB keys in its waves' registers (KB blocks of 16 a wave) and goes over the rows of the query heads that read them.  S = Q K^T here: a lane has four rows
 // of one key.  A key that does not count has sums of its own, which are not stored.
 template <class T, int DP, int KB>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void dkv_kernel(AttentionArgs a, int tiles, int splits, int share) {
@@ -876,7 +889,8 @@ void split(const Pair& one, const Pair& two, int B, int L, int H, int D, hipStre
     hipLaunchKernelGGL(split_kernel, dim3(blocks_of((quads + 255) / 256), 2), dim3(256), 0, s, one, two, L, H, D, quads);
 }
 
-// Where two blocks of 16 rows (keys) a wave fit its registers.
+// Where two blocks of 16 rows (keys) a wave fit its registers: keys of heads of 128 would spill 75 (1 x 32400 x 32400 x 2 x 128 bf16: 4060 us, with one block
+// 2600; all registers of a wave: 2800 to 2900), fp32's of 64 77.
 constexpr bool two_fit(AttentionPass pass, bool f32, int DP) { return DP <= (pass != PASS_DKV ? (f32 ? 64 : 128) : f32 ? 32 : 64); }
 // Few rows take one wave a workgroup.
 constexpr bool one_fits(bool f32, int DP) { return !f32 || DP <= 128; }
