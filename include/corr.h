@@ -321,6 +321,7 @@ corr_status corr_residual_norm_backward(const corr_residual_norm_args* args, con
  *   stats        : NULL, or fp32 [B, G, 2]: mean and 1 / sqrt(var + eps), which the gradient reads.
  *   y            : [B * P, C] dense; may be x (if x_stride == C).
  * Limits: C <= 16384, B <= 65535, B * C <= 2^23, B * P <= 2^30, strides <= 2^21; beyond: CORR_ERR_UNSUPPORTED.  eps > 0.  Without pixels (P = 0) stats are zeros.
+ * Squares about the mean are added in fp32: where their sum passes 3.4e38 the normalised group is zero.
  */
 size_t corr_group_norm_workspace_bytes(corr_dtype type, int64_t B, int64_t P, int64_t C, int64_t G);
 corr_status corr_group_norm(corr_dtype type, corr_activation act, const void* x, int64_t x_stride, const float* weight, const float* bias,
@@ -351,7 +352,8 @@ corr_status corr_group_norm_backward(corr_dtype type, corr_activation act, const
  * Weights meet v as `type` values: rounded once each (fp16: 2^14 times as large, so that weights down to 4e-9 of a row's largest keep their
  * digits); their sum is not.
  * Limits: D a multiple of 8 up to 256, H <= 128, strides of rows and heads <= 2^21 and of items <= 2^40, B * HK <= 2^20, Lq * H / HK and Lk <= 2^30, B * Lq * H * D and
- * B * Lk * HK * D <= 2^36; beyond: CORR_ERR_UNSUPPORTED.  scale is positive and finite.
+ * B * Lk * HK * D <= 2^36, and no more work than one launch takes (2^24 workgroups of 64 rows or keys of a key head); beyond: CORR_ERR_UNSUPPORTED.  scale is
+ * positive and finite.  fp32 products carry fp32's precision as corr_linear's; an infinity in an fp32 operand that counts may come out as NaN.
  */
 typedef struct {
     corr_dtype type;

@@ -110,7 +110,7 @@ template <class T> struct Elem { typedef T type; };
 template <> struct Elem<Planes> { typedef float type; };
 template <class T> constexpr bool F32 = std::is_same<typename Elem<T>::type, float>::value;
 // Weights as a product's operand.  fp16's normal values begin at 6e-5, below which a softmax over many keys lies: they are held 2^14 times as
-// large (at most 16384), and the results divided by that.
+// large (at most 2^(14 + SLACK)), and the results divided by that.
 template <class T> constexpr float LIFT = std::is_same<T, _Float16>::value ? 14.f : 0.f;
 
 // The sums are rescaled only when a score passes the reference by more than 2^SLACK, which their types hold: fp16 up to 2^(14 + 1.75), the others as they
@@ -454,12 +454,12 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 1 || (DP == 256 && F32<T>) ? 1
 
 // The splits' sums of a row, brought to one exponent.  `across` threads have four elements each; `shares` of them take turns at the splits, in a
 // fixed order.
-template <class T>
-__global__ __launch_bounds__(256) void forward_join_kernel(AttentionArgs a, int splits, int across, int shares) {
-    __shared__ f32x4 sums[256];
-    __shared__ float tops[256], totals[256];
+template <class T, int THREADS>
+__global__ __launch_bounds__(THREADS) void forward_join_kernel(AttentionArgs a, int splits, int across, int shares) {
+    __shared__ f32x4 sums[THREADS];
+    __shared__ float tops[THREADS], totals[THREADS];
     const int tid = threadIdx.x, team = across * shares, lane = tid % across, share = tid / across % shares, d = 4 * lane;
-    const int64_t all = (int64_t)a.B * a.HK * a.rows, row = (int64_t)blockIdx.x * (256 / team) + tid / team;
+    const int64_t all = (int64_t)a.B * a.HK * a.rows, row = (int64_t)blockIdx.x * (THREADS / team) + tid / team;
     float top = -INFINITY, sum = 0.f;
     f32x4 x = {};
     if (row < all && d < a.D) {
@@ -932,8 +932,11 @@ hipError_t forward(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s
     if (p.splits > 1) {
         int across = 2, shares = 1;
         while (4 * across < a.D) across *= 2;
-        while (2 * shares * across <= 256 && 4 * shares <= p.splits) shares *= 2;
-        hipLaunchKernelGGL(forward_join_kernel<T>, dim3(cdiv((int64_t)a.B * a.HK * a.rows, 256 / (across * shares))), dim3(256), 0, s, a, p.splits, across, shares);
+        const int threads = p.splits >= 32 ? 1024 : 256;
+        while (2 * shares * across <= threads && 4 * shares <= p.splits) shares *= 2;
+        const dim3 grid(cdiv((int64_t)a.B * a.HK * a.rows, threads / (across * shares)));
+        if (threads == 1024) hipLaunchKernelGGL((forward_join_kernel<T, 1024>), grid, dim3(1024), 0, s, a, p.splits, across, shares);
+        else hipLaunchKernelGGL((forward_join_kernel<T, 256>), grid, dim3(256), 0, s, a, p.splits, across, shares);
     }
     return hipGetLastError();
 }
@@ -1014,7 +1017,8 @@ AttentionPlan attention_plan(corr_dtype t, AttentionPass pass, int B, int Lq, in
     int splits = 1;
     if (p.waves == 1) {
         const int64_t want = heads > 0 ? (1280 + heads - 1) / heads : 1;
-        splits = (int)(want < most ? want : most);
+        const int finest = over > 64 ? cdiv(over, 64) : 1;
+        splits = (int)(want < finest ? want : finest);
     } else {
         const int products = pass == PASS_FORWARD ? 2 : pass == PASS_DQ ? 3 : 4;
         // products a microsecond of one compute unit, and the bytes that the join moves in one
