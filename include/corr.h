@@ -373,7 +373,8 @@ corr_status corr_attention(const corr_attention_args* args, void* out, float* ls
  *   d_q      : [B, Lq, H, D] dense, or NULL;  d_k, d_v : [B, Lk, HK, D] dense, or both NULL.  Shared heads' gradients are their query heads' sums;
  *              keys that do not count get zeros.
  * Weights and dS = P (d_out v^T - sum d_out out) meet the other operand as `type` values, rounded once each (fp16: dS times a power of two of
- * its row or key, so that small gradients keep their digits).
+ * its row or key, so that small gradients keep their digits).  out is read as it was rounded: where one key has nearly all of a row's weight, dS is small beside
+ * d_out v^T and its error is that rounding's, half a step of out times d_out.
  */
 size_t corr_attention_backward_workspace_bytes(corr_dtype type, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t HK, int64_t D);
 corr_status corr_attention_backward(const corr_attention_args* args, const void* out, const float* lse, const void* d_out,
