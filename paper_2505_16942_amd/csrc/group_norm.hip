@@ -106,9 +106,7 @@ __global__ __launch_bounds__(THREADS) void stats_kernel(GroupNormArgs a, int ct)
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int e = 0; e < V; ++e) s[e] += (float)now[0].x[u][e];
-#pragma unroll
-                for (int e = 0; e < V; ++e) s[e] *= 1.f / U;
+                    for (int e = 0; e < V; ++e) s[e] = fmaf((float)now[0].x[u][e], 1.f / U, s[e]);
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -317,7 +315,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(GroupNormArgs a, int
     float* const out = blockIdx.y ? a.d_bias : a.d_weight;
     if (items == a.B && out && share == 0 && c < a.C) out[c] = all;
 }
-// d_x = rho (w dz - S1 / n - hat S2 / n), S1 and S2 the group's sums of w dz and w dz hat.  Each thread adds up its channels' groups by itself.
+// d_x = rho (w dz - S1 / n - hat S2 / n), S1 and S2 the group's sums of w dz and w dz hat, which every workgroup adds up for its columns.
 template <class T, int V, int ACT>
 __global__ __launch_bounds__(THREADS) void dx_kernel(GroupNormArgs a, int ct) {
     constexpr int U = 4;

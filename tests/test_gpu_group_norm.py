@@ -101,9 +101,11 @@ def test_means_far_above_the_spread():
     x, g = new(2, 1000, 32, mean=4096.0), new(2, 1000, 32)
     y, stats, _ = _compare("far", x, 4, new(32, mean=1.0), new(32), g, "none")
     assert (stats[..., 1] > 0.5).all() and (stats[..., 1] < 2).all()
-    x = torch.full((1, 500, 8), 3e20, device="cuda")           # their squares overflow, their differences are zero
-    y = _b().corr_group_norm(x, 2)
-    assert not y.any()
+    for value in (3e20, 3e38):                                  # squares and sums overflow, differences are zero
+        for P in (500, 50000):
+            x = torch.full((1, P, 8), value, device="cuda")
+            stats = torch.empty(1, 2, 2, device="cuda")
+            assert not _b().corr_group_norm(x, 2, stats=stats).any() and (stats[..., 0] == x[0, 0, 0]).all()
 
 
 @pytest.mark.parametrize("dtype", TYPES)
