@@ -884,7 +884,7 @@ __global__ __launch_bounds__(SLOPE_THREADS) void slope_gated_kernel(int act, con
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 d[1][e] = d[0][e] * gate[e];
-                d[0][e] *= up[e] * slope[e];
+                d[0][e] = d[0][e] * slope[e] * up[e];    // in this order: of the two, only up can be large
                 sum[0][e] += d[0][e];
                 sum[1][e] += d[1][e];
             }

@@ -158,6 +158,18 @@ def test_half_gradients_keep_small_and_large_values():
             ref.check("%s %g" % (what, sigma), g, v, e)
 
 
+@pytest.mark.parametrize("dtype", [F32, torch.bfloat16])
+def test_factors_near_the_largest(dtype):
+    """A second half of 3.3e38 where gelu's slope is 1.13: their product alone has no place in the type, the small gradient's has."""
+    m, new = _b(), _gen(10)
+    M, N, K = 40, 24, 32
+    x, w, z = new(M, K, dtype=dtype), new(2 * N, K, sigma=0.1, dtype=dtype), new(M, 2 * N, dtype=dtype)
+    z[:, :N], z[:, N:] = 1.5, 3.3e38
+    dy = new(M, N, sigma=1e-6, dtype=dtype)
+    for g, (v, e), what in zip(m.corr_gated_linear_backward(x, w, dy, z, act=m.CORR_ACT_GELU), ref.gated_backward(x, w, dy, z, "gelu"), ("d_x", "d_w", "d_b")):
+        ref.check(what, g, v, e)
+
+
 def test_differences():
     """The gradient against differences of the forward call in fp32: what the quotient itself is off by is computed in float64."""
     m, new = _b(), _gen(6)
