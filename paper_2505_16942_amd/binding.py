@@ -882,6 +882,8 @@ def _attention_args(q, k, v, scale, k_lengths, key_mask):
     vs, *pv = _heads(v, "v", q.dtype, device)
     B, Lq, H, D = qs
     Lk, HK = ks[1], ks[2]
+    if D < 1:
+        raise ValueError("q must have heads of at least one element")
     if ks != vs or ks[0] != B or ks[3] != D or HK < 1 or H % HK:
         raise ValueError("k and v must be [%d, keys, heads, %d], with a number of heads that divides q's" % (B, D))
     pl = None if k_lengths is None else _dense(k_lengths, "k_lengths", torch.int32, device, (B,))

@@ -294,3 +294,23 @@ def test_far_offsets():
     want = _run(q, k.contiguous(), v.contiguous(), g)
     got = _run(q, k, v, g)
     assert torch.equal(want[0], got[0]) and all(torch.equal(x, y) for x, y in zip(want[2], got[2]))
+
+
+def test_binding_refusals():
+    """What the library cannot see, a tensor's type, device and shape, is refused before it is called."""
+    b = _b()
+    q, k = torch.zeros(2, 3, 4, 16, device="cuda"), torch.zeros(2, 5, 2, 16, device="cuda")
+    lse = torch.empty(2, 4, 3, device="cuda")
+    good = b.corr_attention(q, k, k, lse=lse)
+    for args, kw in [
+        ((q[0], k, k), {}), ((q, k[:, :, :, :8], k), {}), ((q, k, k[:, :4]), {}), ((q, k[:1], k[:1]), {}), ((q[:, :, :3], k, k), {}),
+        ((q[..., :0], k[..., :0], k[..., :0]), {}), ((q, k[:, :, :0], k[:, :, :0]), {}), ((q.half(), k, k), {}), ((q.int(), k, k), {}), ((q, k.cpu(), k), {}),
+        ((q.transpose(1, 3).contiguous().transpose(1, 3), k, k), {}), ((q, k, k), dict(lse=lse[:, :, :2])), ((q, k, k), dict(lse=lse.half())),
+        ((q, k, k), dict(out=torch.empty(2, 3, 64, device="cuda"))), ((q, k, k), dict(out=good.transpose(1, 2).contiguous().transpose(1, 2))),
+        ((q, k, k), dict(k_lengths=torch.tensor([5, 5], device="cuda"))), ((q, k, k), dict(k_lengths=torch.ones(2, dtype=torch.int32))),
+        ((q, k, k), dict(key_mask=torch.ones(2, 4, dtype=torch.bool, device="cuda"))), ((q, k, k), dict(key_mask=torch.ones(2, 5, device="cuda"))),
+    ]:
+        with pytest.raises((TypeError, ValueError)):
+            b.corr_attention(*args, **kw)
+    with pytest.raises((TypeError, ValueError)):
+        b.corr_attention_backward(q, k, k, good, lse, good.transpose(1, 2).contiguous().transpose(1, 2))
