@@ -77,11 +77,9 @@ __device__ __forceinline__ void load_bias(const ProductArgs& g, float (&bias)[V]
 }
 // Gated: V elements of both halves.  g.N columns of y; bias and pre have 2 N, the gate's first.
 template <class T, int V>
-__device__ __forceinline__ void finish_gated(const ProductArgs& g, float (&gate)[V], float (&up)[V], const float (&bias)[2][V], int m, int n) {
+__device__ __forceinline__ void store_gated(const ProductArgs& g, float (&gate)[V], const float (&up)[V], int m, int n) {
     const int left = g.N - n;
     if (m >= g.M || left <= 0) return;
-#pragma unroll
-    for (int e = 0; e < V; ++e) { gate[e] += bias[0][e]; up[e] += bias[1][e]; }
     if (g.pre) {
         T* const z = (T*)g.pre + (int64_t)m * 2 * g.N + n;
         store_some<T, V>(z, gate, left, g.past);
@@ -91,6 +89,12 @@ __device__ __forceinline__ void finish_gated(const ProductArgs& g, float (&gate)
 #pragma unroll
     for (int e = 0; e < V; ++e) gate[e] *= up[e];
     store_some<T, V>((T*)g.y + (int64_t)m * g.ldy + n, gate, left, g.past);
+}
+template <class T, int V>
+__device__ __forceinline__ void finish_gated(const ProductArgs& g, float (&gate)[V], float (&up)[V], const float (&bias)[2][V], int m, int n) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) { gate[e] += bias[0][e]; up[e] += bias[1][e]; }
+    store_gated<T, V>(g, gate, up, m, n);
 }
 template <int V>
 __device__ __forceinline__ void load_gated_bias(const ProductArgs& g, float (&bias)[2][V], int n) {
@@ -273,7 +277,7 @@ __device__ __forceinline__ V keep_first(V v, int left) {
 // 265).  A sum of the low part's products that is not finite says that an element of the second operand is not (fp16's values
 // cannot overflow it): then the high part alone gives what the whole would.
 // GATED: the second operand's rows come in turns from its two halves of g.N (BN / 2 columns of y a tile), so that a lane's sums have both factors of
-// the same columns and the sums need no memory: 32400 x 256 -> 2 x 1024 bf16 with silu and preact 67 us (217 MB, 3.2 TB/s), 14570 x 256 -> 2 x 682 fp32
+// the same columns and the sums need no memory: 14400 x 320 -> 2 x 1280 bf16 with silu and preact 51 us (120 MB), 14570 x 256 -> 2 x 682 fp32
 // with gelu 65 us (157 TFLOP/s), bound as the products without a gate.
 template <class T, bool AR, bool BR, int BM, int BN, int WM, int WN, int BK, bool TWO, bool GATED = false>
 __global__ __launch_bounds__(64 * WM * WN, BK == 32 ? 4 : 2) void product16_kernel(ProductArgs g, int tm, int tn, int splits, int steps_per) {
@@ -373,6 +377,147 @@ __global__ __launch_bounds__(64 * WM * WN, BK == 32 ? 4 : 2) void product16_kern
     if constexpr (GATED) {
         if (busy) finish_gated_wave<T, FM, FN>(g, acc, (float*)smem + wave * box_floats<FN>(), m0 + wm, n0 + wn / 2, lane, split, splits);
     } else if (busy) finish_wave<T, FM, FN>(g, acc, (float*)smem + wave * box_floats<FN>(), m0 + wm, n0 + wn, lane, split, splits);
+}
+
+// ------------------------------------------------------------------------------------------------ gated, short k
+// Where k is short a tile's loads, products and stores each wait for the others. Here rows stay: a wave holds its 16 FM rows of x, at most 32 KS k of
+// them, in registers as second operands, and the weights pass by in chunks of 32 columns of y (both halves: 64 rows of w) in two buffers of LDS that
+// take turns. A block's row 4 lg + e is the chunk's column 8 lg + 4 c + e (c: which of two blocks), so that a lane's sums are eight columns of one row in
+// both halves and go to memory from the registers. Two chunks are stored together, for whole lines of 128 bytes (one by one, 32400 x 256 -> 2 x 1024 bf16
+// with silu and preact took 73 us, 129600 x 256 -> 2 x 512 with gelu and preact 148), and have the next chunk's products to leave.
+// In tiles (tiles of 128 x 256 above) and here, us: 32400 x 256 -> 2 x 1024 with preact 80 and 62, without 67 and 53; 129600 x 256 -> 2 x 512 160 and 120 (464 MB, 3.9
+// TB/s), 117 and 86; 129600 x 128 -> 2 x 256 64 and 57, 48 and 38. With a preact bound by stores, else by the LDS reads of weights (27 us of 86 at their
+// peak; 64 rows a wave would halve them but spill with two chunks of results) and the activation.
+// as dma16, four bytes a lane
+__device__ __forceinline__ void dma4(i32x4 rsrc, unsigned lds, unsigned voff) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+                 :: "s"(lds), "v"(voff), "s"(rsrc) : "memory");
+}
+constexpr unsigned NOWHERE = 0x7ffffff8u;                // beyond any resource's size
+template <class T, int FM, int WAVES, int KS>
+__global__ __launch_bounds__(64 * WAVES, WAVES / 2) void short_gated_kernel(ProductArgs g, int tm, int parts, int per) {
+    constexpr int ROW = KS * 64, HALF = 64 * ROW, LOADS = HALF / (1024 * WAVES), IN_HALF = HALF / 2048;
+    typedef typename Frag<T>::type F;
+    __shared__ __align__(1024) unsigned char smem[2 * HALF];
+    __shared__ __align__(256) float bias[2][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lr = lane & 15, lg = lane >> 4;
+    // an XCD takes all chunks of the rows that it takes
+    const int turn = blockIdx.x >> 3, mt = turn / parts * 8 + (blockIdx.x & 7), part = turn % parts;
+    if (mt >= tm) return;
+    const int chunks = (g.N + 31) >> 5, lo = part * per, hi = min(chunks, lo + per);
+    const int m0 = (mt * WAVES + wave) * 16 * FM;
+    Window wg = window<false, 2, 32>(g.b, g.ldb, g.N, g.K, 32 * lo, 0), wu = wg;
+    wg.step = wu.step = 64 * g.ldb;
+    wu.at += (int64_t)g.N * g.ldb * 2;
+    unsigned voff[LOADS];
+#pragma unroll
+    for (int q = 0; q < LOADS; ++q) {
+        const int p = (q * WAVES + wave) * 64 + lane, r = p / (4 * KS) & 31, piece = (p % (4 * KS)) ^ ((r & 3) | (r >> 3 & 1) << 2);
+        voff[q] = 8 * piece < g.K ? (unsigned)(r * g.ldb * 2) + piece * 16 : NOWHERE;
+    }
+    const i32x4 rb = {__builtin_amdgcn_readfirstlane((int)(uint64_t)g.bias), __builtin_amdgcn_readfirstlane((int)((uint64_t)g.bias >> 32) & 0xffff),
+                      g.bias ? 8 * g.N : 0, 0x00020000};
+    const unsigned lds_at = (unsigned)(uintptr_t)(lds_byte*)smem, bias_at = (unsigned)(uintptr_t)(lds_byte*)bias;
+    int asked = 32 * lo;
+    auto ask = [&](int half) {
+        const i32x4 one = wg.rsrc(), two = wu.rsrc();
+#pragma unroll
+        for (int q = 0; q < LOADS; ++q)
+            dma16(q * WAVES + wave >= IN_HALF ? two : one, lds_at + half * HALF + (q * WAVES + wave) * 1024, voff[q]);
+        if (wave == 0) {
+            const int n = asked + (lane & 31);
+            dma4(rb, bias_at + half * 256, n < g.N ? (unsigned)(n + (lane >> 5) * g.N) * 4 : NOWHERE);
+        }
+        wg.next(); wu.next(); asked += 32;
+    };
+    ask(0);
+    F x[KS][FM];
+#pragma unroll
+    for (int j = 0; j < FM; ++j) {
+        const T* const row = (const T*)g.a + (int64_t)min(m0 + 16 * j + lr, g.M - 1) * g.lda;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const int k = 32 * s + 8 * lg;
+            const F v = __builtin_bit_cast(F, *reinterpret_cast<const typename Some<T, 8>::type*>(row + (k < g.K ? k : 0)));
+            x[s][j] = k < g.K ? v : F{};
+        }
+    }
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int j = 0; j < FM; ++j) asm volatile("" : "+v"(x[s][j]));
+    arrive_all();
+    if (lo + 1 < hi) ask(1);
+    const int row_at = (8 * (lr >> 2) + (lr & 3)) * ROW, even = row_at + ((lg ^ (lr & 7)) << 4), odd = row_at + (((4 + lg) ^ (lr & 7)) << 4);
+    typedef typename Some<T, 8>::type Row8;
+    Row8 held[FM][3];                                    // the first chunk of two, to go with the second one's as whole lines
+    auto chunk = [&](int c, auto turn) {
+        constexpr int half = decltype(turn)::value;
+        const unsigned char* const tile = smem + half * HALF;
+        f32x4 acc[4][FM];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(&bias[half][(b >> 1) * 32 + 8 * lg + 4 * (b & 1)]);
+#pragma unroll
+            for (int j = 0; j < FM; ++j) acc[b][j] = v;
+        }
+        auto weights = [&](F (&w)[4], int s) {
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                w[b] = *reinterpret_cast<const F*>(tile + (s & 1 ? odd : even) + (s >> 1) * 128 + (b & 1) * 4 * ROW + (b >> 1) * 32 * ROW);
+        };
+        F w[2][4];
+        weights(w[0], 0);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            if (s + 1 < KS) weights(w[(s + 1) & 1], s + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int j = 0; j < FM; ++j) acc[b][j] = mma(w[s & 1][b], x[s][j], acc[b][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+        arrive_all();                                    // the next chunk is there, and this one has been read
+        if (c + 2 < hi) ask(half);
+        const bool both = half ? 32 * c + 32 <= g.N : c + 1 < hi && 32 * c + 64 <= g.N;
+        const int n = 32 * c + 8 * lg;
+#pragma unroll
+        for (int j = 0; j < FM; ++j) {
+            const int m = m0 + 16 * j + lr;
+            float gate[8], up[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { gate[e] = acc[e >> 2][j][e & 3]; up[e] = acc[2 + (e >> 2)][j][e & 3]; }
+            if (!both) { store_gated<T, 8>(g, gate, up, m, n); continue; }
+            Row8 v[3];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { v[1][e] = (T)gate[e]; v[2][e] = (T)up[e]; }
+            row_act_all(g.act, gate);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[0][e] = (T)(gate[e] * up[e]);
+            if constexpr (!half) {
+#pragma unroll
+                for (int i = 0; i < 3; ++i) held[j][i] = v[i];
+            } else if (m < g.M) {
+                auto store = [&](T* to, int i) {
+                    Row8* const one = reinterpret_cast<Row8*>(to - 32); Row8* const two = reinterpret_cast<Row8*>(to);
+                    if (g.past) { __builtin_nontemporal_store(held[j][i], one); __builtin_nontemporal_store(v[i], two); }
+                    else { *one = held[j][i]; *two = v[i]; }
+                };
+                store((T*)g.y + (int64_t)m * g.ldy + n, 0);
+                if (g.pre) {
+                    T* const z = (T*)g.pre + (int64_t)m * 2 * g.N + n;
+                    store(z, 1); store(z + g.N, 2);
+                }
+            }
+        }
+    };
+    for (int c = lo; c < hi; c += 2) {
+        chunk(c, std::integral_constant<int, 0>{});
+        if (c + 1 < hi) chunk(c + 1, std::integral_constant<int, 1>{});
+    }
 }
 
 // ------------------------------------------------------------------------------------------------ fp32 operands
@@ -1044,6 +1189,30 @@ void product_tile(const ProductPlan& p, int& rows, int& cols) {
     cols = p.tile == TILE_256 || p.tile == TILE_ROWS ? 256 : p.tile == TILE_128 ? 128 : p.tile == TILE_64 ? 64 : 16;
 }
 
+namespace {
+constexpr int SHORT_FM = 2, SHORT_WAVES = 4, SHORT_ROWS = 16 * SHORT_FM * SHORT_WAVES, SHORT_SLOTS = 512;      // two workgroups a compute unit
+// Whole pieces of k, and seven chunks for every workgroup that fits at a time (bf16 with silu and preact, tiles and here: 14570 x 256 -> 2 x 1024 38 and 34 us, 57600 x
+// 128 -> 2 x 256 32 and 27; below: 14570 x 256 -> 2 x 384 18 and 22, 8192 x 256 -> 2 x 1024 20 and 22).
+bool short_rows(const ProductArgs& g) {
+    return g.gated && g.type != CORR_TYPE_F32 && g.K <= 256 && g.K % 8 == 0 && (int64_t)cdiv(g.M, SHORT_ROWS) * cdiv(g.N, 32) >= 7 * SHORT_SLOTS;
+}
+template <class T>
+void short_gated(const ProductArgs& g, hipStream_t s) {
+    const int tm = cdiv(g.M, SHORT_ROWS), chunks = cdiv(g.N, 32);
+    int per = 0;
+    int64_t best = INT64_MAX;
+    for (int p = 1; p <= min(chunks, 32); ++p) {          // rounds of workgroups, times two chunks at a time and about one for the rows
+        const int some = 2 * cdiv(chunks, 2 * p);
+        const int64_t cost = ((int64_t)tm * cdiv(chunks, some) + SHORT_SLOTS - 1) / SHORT_SLOTS * (some + 1);
+        if (cost < best) { best = cost; per = some; }
+    }
+    const int parts = cdiv(chunks, per);
+    const dim3 grid(8 * cdiv(tm, 8) * parts), threads(64 * SHORT_WAVES);
+    if (g.K <= 128) hipLaunchKernelGGL((short_gated_kernel<T, SHORT_FM, SHORT_WAVES, 4>), grid, threads, 0, s, g, tm, parts, per);
+    else hipLaunchKernelGGL((short_gated_kernel<T, SHORT_FM, SHORT_WAVES, 8>), grid, threads, 0, s, g, tm, parts, per);
+}
+}  // namespace
+
 hipError_t launch_product(const ProductArgs& args, hipStream_t s) {
     ProductArgs g = args;
     const ProductPlan p = product_plan(g.type, g.a_rows, g.b_rows, g.M, g.gated ? 2 * g.N : g.N, g.K);
@@ -1051,6 +1220,11 @@ hipError_t launch_product(const ProductArgs& args, hipStream_t s) {
     // bf16: 137 -> 119 us); whole lines only (rows of 648 bytes: 43 -> 46 us).
     const int64_t row = g.ldy * corr_elem_bytes(g.type);
     g.past = (int64_t)g.M * row >= (128 << 20) && row % 64 == 0 && ((uintptr_t)g.y & 63) == 0;
+    if (short_rows(g)) {
+        if (g.type == CORR_TYPE_BF16) short_gated<__bf16>(g, s);
+        else short_gated<_Float16>(g, s);
+        return hipGetLastError();
+    }
     if (g.type == CORR_TYPE_F32) product32(g, p, s);
     else if (g.type == CORR_TYPE_BF16) product16<__bf16>(g, p, s);
     else product16<_Float16>(g, p, s);

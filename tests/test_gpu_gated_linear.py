@@ -67,6 +67,38 @@ def test_every_tile(kind, dtype):
     ref.check("%s z" % kind, z, wz, ez)
 
 
+# many rows of a short k, whose rows stay in registers: one and more pieces of k, half a chunk of 32 columns, odd numbers of chunks, all of 256 k
+SHORT = [(230000, 33, 8), (60100, 250, 72), (153000, 96, 256), (14500, 1000, 200), (115100, 128, 128)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("size", SHORT)
+def test_many_rows_of_a_short_k(size, dtype):
+    """Columns of a wider buffer as rows, results apart, an infinity in one row: that row's sums alone, and nothing beside the results."""
+    m, (M, N, K) = _b(), size
+    new = _gen(M + N + K)
+    wide = torch.full((M, K + 16), float("nan"), dtype=dtype, device="cuda")
+    x = wide[:, 8:8 + K]
+    x.copy_(new(M, K, dtype=dtype))
+    w = new(2 * N, K, sigma=K ** -0.5, dtype=dtype)
+    name = ACTS[(M + N + K) % 6]
+    for bias in (None, new(2 * N, sigma=0.3)):
+        z = torch.full((M + 1, 2 * N), 7.0, dtype=dtype, device="cuda")
+        out = torch.full((M + 1, N + 3), 7.0, dtype=dtype, device="cuda")
+        y = m.corr_gated_linear(x, w, bias=bias, act=_act(name), out=out[:M, 1:N + 1], preact=z[:M])
+        assert (z[M] == 7).all() and (out[M] == 7).all() and (out[:, 0] == 7).all() and (out[:, N + 1:] == 7).all()
+        assert torch.equal(y, m.corr_gated_linear(x, w, bias=bias, act=_act(name))), "with and without a preact differ"
+        wy, wz, ey, ez = ref.gated(x, w, bias, name)
+        ref.check("y %s %s %s" % (size, dtype, name), y, wy, ey)
+        ref.check("z", z[:M], wz, ez)
+    clean = m.corr_gated_linear(x, w, act=m.CORR_ACT_SIGMOID)
+    x[M - 2, K - 1] = float("inf")
+    got = m.corr_gated_linear(x, w, act=m.CORR_ACT_NONE, preact=z[:M])
+    assert not z[M - 2].isfinite().any() and not got[M - 2].isfinite().any()
+    got = m.corr_gated_linear(x, w, act=m.CORR_ACT_SIGMOID)
+    assert torch.equal(got[:M - 2], clean[:M - 2]) and torch.equal(got[M - 1], clean[M - 1])
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("size", SIZES)
 def test_gated_linear_backward(size, dtype):
