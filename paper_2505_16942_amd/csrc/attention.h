@@ -21,7 +21,8 @@ struct AttentionArgs {
 };
 // How a call is cut up: `tile` rows (keys) a workgroup of `waves` waves, `splits` shares of `share` keys (rows) each.
 // `planes`: fp32 tiles come from three planes that are made first.
-struct AttentionPlan { int waves, blocks, tile, tiles, splits, share; bool planes; };
+// `two`: 16-bit weights and dS in two parts, and one block of rows (keys) a wave.
+struct AttentionPlan { int waves, blocks, tile, tiles, splits, share; bool planes, two; };
 enum AttentionPass { PASS_FORWARD = 0, PASS_DQ, PASS_DKV };
 AttentionPlan attention_plan(corr_dtype t, AttentionPass pass, int B, int Lq, int Lk, int HK, int per, int D);
 __host__ __device__ static inline int attention_aux_rows(int rows) { return (rows + 63) & ~63; }

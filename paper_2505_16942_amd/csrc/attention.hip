@@ -42,6 +42,16 @@ template <class T> struct Num {
         for (int e = 0; e < 8; ++e) f[e] = (T)x[e >> 2][e & 3];
         return f;
     }
+    // what pack() left out
+    static __device__ __forceinline__ F rest(const f32x4* x, const F& high) {
+        F f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float r = x[e >> 2][e & 3] - (float)high[e];
+            f[e] = (T)(fabsf(r) < INFINITY ? r : 0.f);
+        }
+        return f;
+    }
     static __device__ __forceinline__ f32x4 times(const F& a, const F& b, f32x4 c) { return mma(a, b, c); }
     // elements d .. d + 7 of row `p`, zeros behind D or without a row
     static __device__ __forceinline__ F load(const T* p, int d, int D, bool there) {
@@ -295,7 +305,7 @@ __device__ __forceinline__ void query_of(const AttentionArgs& a, int r, int& q, 
 // 64: 243 us, 175 TFLOP/s (1.05 PFLOP/s of bf16).
 // One row of 8 query heads on 2 key heads, 8 x 32768 keys of ragged lengths (157 MB), bf16, one wave a workgroup, 74 shares: 38 us from memory, 4.1 TB/s
 // (28 from the memory-side cache), and 8 for their join; 110 or 172 shares make no difference.
-template <class T, int DP, int WAVES, int QB>
+template <class T, int DP, int WAVES, int QB, bool TWO = false>
 __global__ __launch_bounds__(64 * WAVES, WAVES == 1 || (DP == 256 && F32<T>) ? 1 : 2) void forward_kernel(AttentionArgs a, int tiles, int splits, int share) {
     typedef Num<T> N;
     typedef typename Elem<T>::type E;
@@ -412,14 +422,20 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 1 || (DP == 256 && F32<T>) ? 1
                     }
 #pragma unroll
             for (int i = 0; i < KB; i += 2) {
-                F fp[QB];
+                F fp[QB], lp[QB];
 #pragma unroll
-                for (int j = 0; j < QB; ++j) fp[j] = N::pack(&s[j][i]);
+                for (int j = 0; j < QB; ++j) {
+                    fp[j] = N::pack(&s[j][i]);
+                    if constexpr (TWO) lp[j] = N::rest(&s[j][i], fp[j]);
+                }
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
                     const F f = N::template turned<DP, KT>(tv, 16 * i, d, lr, lg);
 #pragma unroll
-                    for (int j = 0; j < QB; ++j) o[d][j] = N::times(f, fp[j], o[d][j]);
+                    for (int j = 0; j < QB; ++j) {
+                        if constexpr (TWO) o[d][j] = N::times(f, lp[j], o[d][j]);
+                        o[d][j] = N::times(f, fp[j], o[d][j]);
+                    }
                 }
             }
         }
@@ -570,8 +586,8 @@ template <class T, int N> struct Lifted {
     __device__ __forceinline__ float back(int j) const { return ON ? 1.f / (16384.f * by[j]) : 1.f; }
 };
 
-template <class T, int DP, int QB>
-__global__ __launch_bounds__(256, DP == 256 && F32<T> ? 1 : 2) void dq_kernel(AttentionArgs a, int tiles, int splits, int share) {
+template <class T, int DP, int QB, bool TWO = false>
+__global__ __launch_bounds__(256, DP == 256 && (F32<T> || TWO) ? 1 : 2) void dq_kernel(AttentionArgs a, int tiles, int splits, int share) {
     typedef Num<T> N;
     typedef typename Elem<T>::type E;
     typedef typename N::F F;
@@ -677,14 +693,20 @@ __global__ __launch_bounds__(256, DP == 256 && F32<T> ? 1 : 2) void dq_kernel(At
                             if (some) dp[j][i][e] = (mine >> (FK * kk + 16 * i + e)) & 1 ? dp[j][i][e] : 0.f;
                         }
                 lifted.lift(dp, dq);
-                F fs[QB];
+                F fs[QB], ls[QB];
 #pragma unroll
-                for (int j = 0; j < QB; ++j) fs[j] = N::pack(dp[j]);
+                for (int j = 0; j < QB; ++j) {
+                    fs[j] = N::pack(dp[j]);
+                    if constexpr (TWO) ls[j] = N::rest(dp[j], fs[j]);
+                }
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
                     const F f = N::template turned<DP, KT>(tk, FK * kk, d, lr, lg);
 #pragma unroll
-                    for (int j = 0; j < QB; ++j) dq[d][j] = N::times(f, fs[j], dq[d][j]);
+                    for (int j = 0; j < QB; ++j) {
+                        if constexpr (TWO) dq[d][j] = N::times(f, ls[j], dq[d][j]);
+                        dq[d][j] = N::times(f, fs[j], dq[d][j]);
+                    }
                 }
             }
         }
@@ -710,7 +732,7 @@ __global__ __launch_bounds__(256, DP == 256 && F32<T> ? 1 : 2) void dq_kernel(At
 
 // A workgroup has 64 KB keys in its waves' registers (KB blocks of 16 a wave) and goes over the rows of the query heads that read them.  S = Q K^T here: a lane has four rows
 // of one key.  A key that does not count has sums of its own, which are not stored.
-template <class T, int DP, int KB>
+template <class T, int DP, int KB, bool TWO = false>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void dkv_kernel(AttentionArgs a, int tiles, int splits, int share) {
     typedef Num<T> N;
     typedef typename Elem<T>::type E;
@@ -808,7 +830,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void dkv_kernel(AttentionAr
                         dp[j][i] = N::times(w, fv[j][h], dp[j][i]);
                     }
                 }
-            F fp[KB], fs[KB];
+            F fp[KB], fs[KB], lp[KB], ls[KB];
 #pragma unroll
             for (int j = 0; j < KB; ++j) {
 #pragma unroll
@@ -820,16 +842,24 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void dkv_kernel(AttentionAr
                         s[j][i][e] = p;
                     }
                 fp[j] = N::pack(s[j]);
+                if constexpr (TWO) lp[j] = N::rest(s[j], fp[j]);
             }
             lifted.lift(dp, dk);
 #pragma unroll
-            for (int j = 0; j < KB; ++j) fs[j] = N::pack(dp[j]);
+            for (int j = 0; j < KB; ++j) {
+                fs[j] = N::pack(dp[j]);
+                if constexpr (TWO) ls[j] = N::rest(dp[j], fs[j]);
+            }
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
                 const F f = N::template turned<DP, RT>(to, FK * kk, d, lr, lg);
                 const F w = N::template turned<DP, RT>(tq, FK * kk, d, lr, lg);
 #pragma unroll
                 for (int j = 0; j < KB; ++j) {
+                    if constexpr (TWO) {
+                        dv[d][j] = N::times(f, lp[j], dv[d][j]);
+                        dk[d][j] = N::times(w, ls[j], dk[d][j]);
+                    }
                     dv[d][j] = N::times(f, fp[j], dv[d][j]);
                     dk[d][j] = N::times(w, fs[j], dk[d][j]);
                 }
@@ -907,18 +937,30 @@ constexpr bool one_fits(bool f32, int DP) { return !f32 || DP <= 128; }
 template <class T, int DP>
 void forward_pass(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) {
     const dim3 grid(p.tiles * p.splits * a.B * a.HK);
+    if constexpr (!F32<T>) if (p.two) {
+        hipLaunchKernelGGL((forward_kernel<T, DP, 4, 1, true>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
+        return;
+    }
     if (p.blocks == 1) hipLaunchKernelGGL((forward_kernel<T, DP, 4, 1>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
     else if constexpr (two_fit(PASS_FORWARD, F32<T>, DP)) hipLaunchKernelGGL((forward_kernel<T, DP, 4, 2>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
 }
 template <class T, int DP>
 void dq_pass(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) {
     const dim3 grid(p.tiles * p.splits * a.B * a.HK);
+    if constexpr (!F32<T>) if (p.two) {
+        hipLaunchKernelGGL((dq_kernel<T, DP, 1, true>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
+        return;
+    }
     if (p.blocks == 1) hipLaunchKernelGGL((dq_kernel<T, DP, 1>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
     else if constexpr (two_fit(PASS_DQ, F32<T>, DP)) hipLaunchKernelGGL((dq_kernel<T, DP, 2>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
 }
 template <class T, int DP>
 void dkv_pass(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s) {
     const dim3 grid(p.tiles * p.splits * a.B * a.HK);
+    if constexpr (!F32<T>) if (p.two) {
+        hipLaunchKernelGGL((dkv_kernel<T, DP, 1, true>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
+        return;
+    }
     if (p.blocks == 1) hipLaunchKernelGGL((dkv_kernel<T, DP, 1>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
     else if constexpr (two_fit(PASS_DKV, F32<T>, DP)) hipLaunchKernelGGL((dkv_kernel<T, DP, 2>), grid, dim3(256), 0, s, a, p.tiles, p.splits, p.share);
 }
@@ -934,7 +976,7 @@ hipError_t forward(const AttentionArgs& a, const AttentionPlan& p, hipStream_t s
         done = true;
     }
     if constexpr (one_fits(F32<T>, DP)) if (p.waves == 1) {
-        hipLaunchKernelGGL((forward_kernel<T, DP, 1, 1>), dim3(p.tiles * p.splits * a.B * a.HK), dim3(64), 0, s, a, p.tiles, p.splits, p.share);
+        hipLaunchKernelGGL((forward_kernel<T, DP, 1, 1, !F32<T>>), dim3(p.tiles * p.splits * a.B * a.HK), dim3(64), 0, s, a, p.tiles, p.splits, p.share);
         done = true;
     }
     if (!done) forward_pass<T, DP>(a, p, s);
@@ -1020,6 +1062,10 @@ AttentionPlan attention_plan(corr_dtype t, AttentionPass pass, int B, int Lq, in
     AttentionPlan p;
     p.waves = pass == PASS_FORWARD && along <= 16 && one_fits(f32, pad) ? 1 : 4;
     p.blocks = 1;
+    // One rounding of weights and dS is as large as the result's own, together sqrt 2 of it, where many weights share in it. Up to some hundred rows a few large ones
+    // can make up most of it and their roundings be the largest there are (scores of a spread of two, in a hundredth of all calls: 1.8 times the result's at one row, 1.6 at
+    // 64, 1.5 at 256): the second part costs 3 % of a call of one row, and up to 15 % of a gradient's time at 512 (64-wide heads are in most of those bound by launches).
+    p.two = !f32 && (p.waves == 1 || heads * rows <= 512);
     // Planes are made once a call and read by every tile of rows: from 2048 rows on (2852 x 2852 x 4 x 32: 51 us, 53 without; 7200 x 7200 x 2 x 32: 102 and
     // 117; 256 x 20000 x 2 x 128: 71 and 51).
     p.planes = f32 && p.waves == 4 && along >= 2048;
@@ -1033,7 +1079,7 @@ AttentionPlan attention_plan(corr_dtype t, AttentionPass pass, int B, int Lq, in
         // products a microsecond of one compute unit, and the bytes that the join moves in one
         const double rate = (f32 ? pad == 32 ? 140e6 : 190e6 : pad == 32 ? 450e6 : 700e6) / 256, bytes = 4e6;
         double best = 1e30;
-        for (int blocks = 1; blocks <= (two_fit(pass, f32, pad) ? 2 : 1); ++blocks) {
+        for (int blocks = 1; blocks <= (two_fit(pass, f32, pad) && !p.two ? 2 : 1); ++blocks) {
             const int64_t groups = cdiv(along, 64 * blocks) * heads;
             const int held = held_at_once(f32, pass, pad, blocks);
             // one block a wave reads its tiles for half as many products

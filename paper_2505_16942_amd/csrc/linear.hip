@@ -273,7 +273,7 @@ __device__ __forceinline__ V keep_first(V v, int left) {
 }
 
 // TWO: the first operand is in two parts (rows_internal.h), multiplied one after the other, the low one first: twice the matrix work and twice the
-// loads (fp16 gradients with silu, and with relu: 14570 x 243 -> 126: 51 and 41 us; 32400 x 256 -> 1024: 153 and 104; 4096^3: 503 and
+// loads (fp16, and bf16 gradients of few gated elements; fp16 gradients with silu, and with relu: 14570 x 243 -> 126: 51 and 41 us; 32400 x 256 -> 1024: 153 and 104; 4096^3: 503 and
 // 265).  A sum of the low part's products that is not finite says that an element of the second operand is not (fp16's values
 // cannot overflow it): then the high part alone gives what the whole would.
 // GATED: the second operand's rows come in turns from its two halves of g.N (BN / 2 columns of y a tile), so that a lane's sums have both factors of
@@ -1004,8 +1004,8 @@ __global__ __launch_bounds__(SLOPE_THREADS) void slope_kernel(int act, const T* 
     }
 }
 
-// Gated: dz of both halves, [M][2 N]: d_y up act'(gate) and d_y act(gate), rounded (fp16: in two parts) as above, and their column sums.  fp16's parts
-// hold values up to 1.3e5.  Bound by bytes: 129600 x 512 bf16 with gelu: 146 us, 663 MB, 4.5 TB/s.
+// Gated: dz of both halves, [M][2 N]: d_y up act'(gate) and d_y act(gate), rounded as above (two parts where dz_lo is there), and their column sums.  fp16's
+// parts hold values up to 1.3e5.  Bound by bytes: 129600 x 512 bf16 with gelu: 146 us, 663 MB, 4.5 TB/s.
 template <class T, int V>
 __global__ __launch_bounds__(SLOPE_THREADS) void slope_gated_kernel(int act, const T* __restrict__ dy, int64_t ld_dy, const T* __restrict__ z,
                                                                    T* __restrict__ dz, T* __restrict__ dz_lo, int64_t ld_dz, float* __restrict__ part,
@@ -1037,12 +1037,12 @@ __global__ __launch_bounds__(SLOPE_THREADS) void slope_gated_kernel(int act, con
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int64_t to = m * ld_dz + h * N + n;
-                if constexpr (std::is_same<T, _Float16>::value) {
+                if constexpr (sizeof(T) == 2) if (dz_lo) {
                     float lo_part[V];
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
                         const float x = HIGH_PART * d[h][e], r = x - (float)(T)x;
-                        lo_part[e] = r == r ? LOW_PART * r : 0.f;        // an infinity or NaN is in the high part
+                        lo_part[e] = fabsf(r) < INFINITY ? LOW_PART * r : 0.f;       // an infinity or NaN is in the high part
                         d[h][e] = x;
                     }
                     store_some<T, V>(dz_lo + to, lo_part, left);
@@ -1077,7 +1077,7 @@ void run16(const ProductArgs& g, const ProductPlan& p, hipStream_t s) {
         }
     }
     const int tm = cdiv(g.M, BM), tn = cdiv(g.N, BN);
-    if constexpr (std::is_same<T, _Float16>::value && BR) {
+    if constexpr (BR) {
         if (g.a_lo) {
             hipLaunchKernelGGL((product16_kernel<T, AR, BR, BM, BN, WM, WN, BK, true>), dim3(tm * tn * p.splits), dim3(64 * WM * WN), 0, s, g, tm, tn, p.splits, p.steps);
             return;

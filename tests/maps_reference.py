@@ -6,11 +6,11 @@ U, EPS and `rounded` are rows_reference's: half a step of a type, 2^-24 an fp32 
 attention.  A score s = scale <q, k> is off by (2 D + 12) EPS S, S the magnitudes' sum.  A weight e^(s - m) is formed as 2^(s c - m c), c = scale log2 e: the
     roundings of c, m c, the exponent and the power are 8 EPS (|s| + |m| + 1), relative; m's own error is the row's and cancels.  Sums are rescaled
     when the maximum grows, at most once a tile of 16 keys: 2 EPS each, and the power's 4 EPS.  So a weight is off by w = (2 D + 12) EPS S +
-    EPS (8 (|s| + |m| + 1) + 6 (Lk / 16 + 1)), relative, and as an operand by U (16-bit types) more.  out = sum p v with sum p = 1:
+    EPS (8 (|s| + |m| + 1) + 6 (Lk / 16 + 1)), relative, and as an operand by U (16-bit types; up to 512 rows by U U, in two parts) more.  out = sum p v with sum p = 1:
     sum p (w + U) |v| + |out| sum p w + (4 Lk + 16) EPS sum p |v|; lse: sum p w + (2 Lk + 8) EPS + 8 EPS |lse|.
 gradient.  P = e^(s - lse) with the lse that was stored (off by e_l): relative error w + e_l + 8 EPS |lse|.  dP: (2 D + 8) EPS sum |dO v|.  delta = sum dO out
     with the out that was stored: its bound times |dO|, and (2 D + 8) EPS sum |dO out|.  dS = P (dP - delta): P (rel |dP - delta| + e_dP +
-    e_delta) + 4 EPS |P (dP - delta)|, and U |dS| as an operand.  The three products are sums of Lk or rows terms.  fp16 keeps weights to 2^-39 of
+    e_delta) + 4 EPS |P (dP - delta)|, and as an operand as the weights.  The three products are sums of Lk or rows terms.  fp16 keeps weights to 2^-39 of
     the largest and dS to 2^-39 of the row's (key's) largest: FLOOR.
     The power and the matrix instructions take values below fp32's normal ones (2^-126) as zero: a weight may be off by LEAST = 2^-126, dS by that
     times |dP - delta| and once more for its own product, and each term of a sum by LEAST.
@@ -43,7 +43,8 @@ class Attention:
         self.T = q.dtype
         (B, Lq, H, D), Lk = q.shape, k.shape[1]
         self.per, self.scale = H // k.shape[2], scale
-        self.lp = U[self.T] if self.T != F32 else 0.0
+        # in two parts up to 512 rows: the second one is U of what the first left, U of it
+        self.lp = 0.0 if self.T == F32 else U[self.T] ** 2 if B * Lq * H <= 512 else U[self.T]
         keep = valid_keys(B, Lk, k_lengths, key_mask)[:, None, None]
         clean = lambda t: torch.where(keep[:, 0, 0, :, None, None], t.cpu(), torch.zeros((), dtype=t.dtype))  # noqa: E731
         self.q, self.k, self.v = q.double().cpu().transpose(1, 2), heads_of(clean(k), self.per), heads_of(clean(v), self.per)
@@ -204,7 +205,8 @@ def gated(x, w, b, name):
 
 
 def gated_backward(x, w, dy, z, name):
-    """((d_x, bound), (d_w, bound), (d_b, bound)).  dz as an operand: bf16 rounded once, fp16 in two parts of 22 bits together with a floor of 2^-36."""
+    """((d_x, bound), (d_w, bound), (d_b, bound)).  dz as an operand: bf16 rounded once, up to 2048 elements of
+    d_y in two parts (U U, and the low part's own 2^-126), fp16 in two parts of 22 bits together with a floor of 2^-36."""
     from rows_reference import act, slope
     dtype, (M, K), N = x.dtype, x.shape, w.shape[0] // 2
     x, w, dy, z = (t.double().cpu() for t in (x, w, dy, z))
@@ -212,7 +214,10 @@ def gated_backward(x, w, dy, z, name):
     far = 16 * EPS * (2 + gate.abs()) if name != "none" else 0
     dz = torch.cat([dy * up * slope(name, gate), dy * act(name, gate)], 1)
     e = torch.cat([(dy * up).abs() * far, dy.abs() * far], 1) + 3 * EPS * dz.abs()
-    ep = e + {F32: 0.0, torch.bfloat16: U[torch.bfloat16], torch.float16: 2.0 ** -21}[dtype] * (dz.abs() + e)
+    low = U[torch.bfloat16] ** 2 if M * N <= 2048 else U[torch.bfloat16]
+    ep = e + {F32: 0.0, torch.bfloat16: low, torch.float16: 2.0 ** -21}[dtype] * (dz.abs() + e)
+    if dtype == torch.bfloat16:
+        ep = ep + LEAST
     if dtype == torch.float16:
         ep = ep + 2.0 ** -35
     per = 12 if dtype == F32 else 2
