@@ -349,8 +349,8 @@ corr_status corr_group_norm_backward(corr_dtype type, corr_activation act, const
  *                that does not count is not read or has no influence, infinities and NaN included.
  *   out        : [B, Lq, H, D] dense.  A row of which no key counts, or whose every score is -infinity, is zeros.
  *   lse        : NULL, or fp32 [B, H, Lq]: the logarithm of the sum of e^score, which the gradient reads (-infinity for rows of zeros).
- * Weights meet v as `type` values: rounded once each, up to B Lq H = 512 in two parts (fp16: 2^14 times as large, so that weights down to 4e-9 of a row's largest keep their
- * digits); their sum is not.
+ * Weights meet v as `type` values: rounded once each, up to B Lq H = 512 in two parts (fp16: 2^14 times as large, so that weights down
+ * to 4e-9 of a row's largest keep their digits); their sum is not.
  * Limits: D a multiple of 8 up to 256, H <= 128, strides of rows and heads <= 2^21 and of items <= 2^40, B * HK <= 2^20, Lq * H / HK and Lk <= 2^30, B * Lq * H * D and
  * B * Lk * HK * D <= 2^36, and no more work than one launch takes (2^24 workgroups of 64 rows or keys of a key head); beyond: CORR_ERR_UNSUPPORTED.  scale is
  * positive and finite.  fp32 products carry fp32's precision as corr_linear's; an infinity in an fp32 operand that counts may come out as NaN.
@@ -372,8 +372,8 @@ corr_status corr_attention(const corr_attention_args* args, void* out, float* ls
  *   d_out    : [B, Lq, H, D] dense, on a 4-byte border.
  *   d_q      : [B, Lq, H, D] dense, or NULL;  d_k, d_v : [B, Lk, HK, D] dense, or both NULL.  Shared heads' gradients are their query heads' sums;
  *              keys that do not count get zeros.
- * Weights and dS = P (d_out v^T - sum d_out out) meet the other operand as `type` values, rounded once each, up to B Lq H = 512 in two parts (fp16: dS times a power of two of
- * its row or key, so that small gradients keep their digits).  out is read as it was rounded: where one key has nearly all of a row's weight, dS is small beside
+ * Weights and dS = P (d_out v^T - sum d_out out) meet the other operand as `type` values, rounded once each, up to B Lq H = 512 in two parts, for d_k
+ * and d_v also up to B Lk HK = 64 (fp16: dS times a power of two of its row or key, so that small gradients keep their digits).  out is read as it was rounded: where one key has nearly all of a row's weight, dS is small beside
  * d_out v^T and its error is that rounding's, half a step of out times d_out.
  */
 size_t corr_attention_backward_workspace_bytes(corr_dtype type, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t HK, int64_t D);
@@ -396,7 +396,7 @@ corr_status corr_gated_linear(corr_dtype type, corr_activation act, const void* 
  * With z = (gate, up) from preact: dz = (d_y up act'(gate), d_y act(gate)),  d_x = dz w,  d_w = dz^T x,  d_bias = sum over rows of dz.
  *   preact : [M, 2 N] dense, as corr_gated_linear left it;  d_y : [M, N] rows, d_y_stride.  x and w of 16 bits start on a 4-byte border.
  *   d_x    : [M, K] dense or NULL;  d_w : [2 N, K] dense or NULL;  d_bias : fp32 [2 N] or NULL.
- * dz is rounded as corr_linear_backward's (bf16 once, or in two parts if M N <= 2048, fp16 in two parts, fp32 whole); fp16's holds values up to 1.3e5, beyond which it is infinite.
+ * dz is rounded as corr_linear_backward's (bf16 once, or in two parts if M min(N, K) <= 2048, fp16 in two parts, fp32 whole); fp16's holds values up to 1.3e5, beyond which it is infinite.
  */
 size_t corr_gated_linear_backward_workspace_bytes(corr_dtype type, int64_t M, int64_t N, int64_t K, int64_t x_stride);
 corr_status corr_gated_linear_backward(corr_dtype type, corr_activation act, const void* x, int64_t x_stride, const void* w,

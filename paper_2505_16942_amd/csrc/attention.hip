@@ -1064,8 +1064,9 @@ AttentionPlan attention_plan(corr_dtype t, AttentionPass pass, int B, int Lq, in
     p.blocks = 1;
     // One rounding of weights and dS is as large as the result's own, together sqrt 2 of it, where many weights share in it. Up to some hundred rows a few large ones
     // can make up most of it and their roundings be the largest there are (scores of a spread of two, in a hundredth of all calls: 1.8 times the result's at one row, 1.6 at
-    // 64, 1.5 at 256): the second part costs 3 % of a call of one row, and up to 15 % of a gradient's time at 512 (64-wide heads are in most of those bound by launches).
-    p.two = !f32 && (p.waves == 1 || heads * rows <= 512);
+    // 64, 1.5 at 256), and few keys' gradients have few elements to share them. The second part costs 3 % of a call of one row (8 x 32768 keys: 74 and 77 us) and 12 % of a
+    // gradient at 700 rows of 4 heads (56 and 63 us, 2852 keys).
+    p.two = !f32 && (p.waves == 1 || heads * rows <= 512 || (pass == PASS_DKV && heads * Lk <= 64));
     // Planes are made once a call and read by every tile of rows: from 2048 rows on (2852 x 2852 x 4 x 32: 51 us, 53 without; 7200 x 7200 x 2 x 32: 102 and
     // 117; 256 x 20000 x 2 x 128: 71 and 51).
     p.planes = f32 && p.waves == 4 && along >= 2048;

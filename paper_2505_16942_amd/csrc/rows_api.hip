@@ -82,9 +82,9 @@ corr_status check_gated(corr_dtype type, corr_activation act, int64_t M, int64_t
 }
 // dz is always a matrix of its own, and in two parts for fp16 and for bf16 with few elements: rounded once, they add as much error as the result's own
 // rounding, 1.4 times that in all, where many share in it; of few some carry most, and their roundings can be the largest there are (1.6 times in a hundredth of
-// the calls of 256 elements, 1.5 at 1024, 1.45 at 4096).
+// the calls of 256 elements, 1.5 at 1024, 1.45 at 4096), and so can their sum's in a few elements of d_x (112: 1.5).
 BackwardLayout gated_backward_layout(corr_dtype t, int64_t M, int64_t N, int64_t K, int64_t x_stride) {
-    return backward_layout(t, CORR_ACT_SILU, M, 2 * N, K, x_stride, 2 * N, t == CORR_TYPE_BF16 && M * N <= 2048);
+    return backward_layout(t, CORR_ACT_SILU, M, 2 * N, K, x_stride, 2 * N, t == CORR_TYPE_BF16 && M * (N < K ? N : K) <= 2048);
 }
 
 corr_status check_norm(const corr_residual_norm_args* a) {

@@ -205,8 +205,8 @@ def gated(x, w, b, name):
 
 
 def gated_backward(x, w, dy, z, name):
-    """((d_x, bound), (d_w, bound), (d_b, bound)).  dz as an operand: bf16 rounded once, up to 2048 elements of
-    d_y in two parts (U U, and the low part's own 2^-126), fp16 in two parts of 22 bits together with a floor of 2^-36."""
+    """((d_x, bound), (d_w, bound), (d_b, bound)).  dz as an operand: bf16 rounded once, up to M min(N, K)
+    = 2048 in two parts (U U, and the low part's own 2^-126), fp16 in two parts of 22 bits together with a floor of 2^-36."""
     from rows_reference import act, slope
     dtype, (M, K), N = x.dtype, x.shape, w.shape[0] // 2
     x, w, dy, z = (t.double().cpu() for t in (x, w, dy, z))
@@ -214,7 +214,7 @@ def gated_backward(x, w, dy, z, name):
     far = 16 * EPS * (2 + gate.abs()) if name != "none" else 0
     dz = torch.cat([dy * up * slope(name, gate), dy * act(name, gate)], 1)
     e = torch.cat([(dy * up).abs() * far, dy.abs() * far], 1) + 3 * EPS * dz.abs()
-    low = U[torch.bfloat16] ** 2 if M * N <= 2048 else U[torch.bfloat16]
+    low = U[torch.bfloat16] ** 2 if M * min(N, K) <= 2048 else U[torch.bfloat16]
     ep = e + {F32: 0.0, torch.bfloat16: low, torch.float16: 2.0 ** -21}[dtype] * (dz.abs() + e)
     if dtype == torch.bfloat16:
         ep = ep + LEAST
