@@ -99,6 +99,23 @@ def test_many_rows_of_a_short_k(size, dtype):
     assert torch.equal(got[:M - 2], clean[:M - 2]) and torch.equal(got[M - 1], clean[M - 1])
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_many_rows_on_borders_of_four_bytes(dtype):
+    """x, its rows and w begin on 4-byte borders that are none of 16; an odd stride is another way through: the same sums within their bounds."""
+    m, new = _b(), _gen(11)
+    M, N, K = 60000, 256, 120
+    even = torch.full((M, K + 6), float("nan"), dtype=dtype, device="cuda")[:, 2:K + 2]
+    odd = torch.full((M, K + 5), float("nan"), dtype=dtype, device="cuda")[:, 4:K + 4]
+    even.copy_(new(M, K, dtype=dtype))
+    odd.copy_(even)
+    w = torch.empty(2 * N * K + 2, dtype=dtype, device="cuda")[2:].view(2 * N, K)
+    w.copy_(new(2 * N, K, sigma=K ** -0.5, dtype=dtype))
+    assert even.data_ptr() % 16 == 4 and w.data_ptr() % 16 == 4
+    wy, _, ey, _ = ref.gated(even, w, None, "gelu_tanh")
+    for x in (even, odd):
+        ref.check("y", m.corr_gated_linear(x, w, act=m.CORR_ACT_GELU_TANH), wy, ey)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("size", SIZES)
 def test_gated_linear_backward(size, dtype):
