@@ -303,8 +303,8 @@ __device__ __forceinline__ void query_of(const AttentionArgs& a, int r, int& q, 
 // eight waves.  2 x 14400 x 14400, 2 heads of 64: 287 us, 740 TFLOP/s: the vector unit, about 80 % of the cycles with
 // the exponentials' turns.  fp32's six products: 2 x 2852 x 7285, 4 heads of
 // 64: 243 us, 175 TFLOP/s (1.05 PFLOP/s of bf16).
-// One row of 8 query heads on 2 key heads, 8 x 32768 keys of ragged lengths (157 MB), bf16, one wave a workgroup, 74 shares: 38 us from memory, 4.1 TB/s
-// (28 from the memory-side cache), and 8 for their join; 110 or 172 shares make no difference.
+// One row of 8 query heads on 2 key heads, 8 x 32768 keys of ragged lengths (157 MB), bf16, one wave a workgroup, 74 shares: 40 us from memory, 3.9 TB/s
+// (28 from the memory-side cache), 38 with weights in one part, and 8 for their join; 110 or 172 shares make no difference.
 template <class T, int DP, int WAVES, int QB, bool TWO = false>
 __global__ __launch_bounds__(64 * WAVES, WAVES == 1 || (DP == 256 && F32<T>) ? 1 : 2) void forward_kernel(AttentionArgs a, int tiles, int splits, int share) {
     typedef Num<T> N;
