@@ -52,6 +52,31 @@ template <class T> struct Num {
         }
         return f;
     }
+    // Weights, none of which is negative, in two parts: rounded towards zero, and what that left out and a trace more, so that an infinity of the other
+    // operand is multiplied by two parts above zero and stays one.
+    static __device__ __forceinline__ F pack_under(const f32x4* x) {
+        if constexpr (std::is_same<T, __bf16>::value) {
+            u32x4 u;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                u[e] = __float_as_uint(x[e >> 1][2 * (e & 1)]) >> 16 | (__float_as_uint(x[e >> 1][2 * (e & 1) + 1]) & 0xffff0000u);
+            return __builtin_bit_cast(F, u);
+        } else {
+            u32x4 u;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[e] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_pkrtz(x[e >> 1][2 * (e & 1)], x[e >> 1][2 * (e & 1) + 1]));
+            return __builtin_bit_cast(F, u);
+        }
+    }
+    static __device__ __forceinline__ F rest_over(const f32x4* x, const F& high) {
+        F f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float w = x[e >> 2][e & 3], r = w - (float)high[e];
+            f[e] = (T)(std::is_same<T, __bf16>::value ? fmaf(w, 0x1p-30f, r) : r + fminf(w, 0x1p-24f));
+        }
+        return f;
+    }
     static __device__ __forceinline__ f32x4 times(const F& a, const F& b, f32x4 c) { return mma(a, b, c); }
     // elements d .. d + 7 of row `p`, zeros behind D or without a row
     static __device__ __forceinline__ F load(const T* p, int d, int D, bool there) {
@@ -425,8 +450,10 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 1 || (DP == 256 && F32<T>) ? 1
                 F fp[QB], lp[QB];
 #pragma unroll
                 for (int j = 0; j < QB; ++j) {
-                    fp[j] = N::pack(&s[j][i]);
-                    if constexpr (TWO) lp[j] = N::rest(&s[j][i], fp[j]);
+                    if constexpr (TWO) {
+                        fp[j] = N::pack_under(&s[j][i]);
+                        lp[j] = N::rest_over(&s[j][i], fp[j]);
+                    } else fp[j] = N::pack(&s[j][i]);
                 }
 #pragma unroll
                 for (int d = 0; d < DB; ++d) {
@@ -841,8 +868,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void dkv_kernel(AttentionAr
                         dp[j][i][e] = p * (dp[j][i][e] - delta[i][e]);
                         s[j][i][e] = p;
                     }
-                fp[j] = N::pack(s[j]);
-                if constexpr (TWO) lp[j] = N::rest(s[j], fp[j]);
+                if constexpr (TWO) {
+                    fp[j] = N::pack_under(s[j]);
+                    lp[j] = N::rest_over(s[j], fp[j]);
+                } else fp[j] = N::pack(s[j]);
             }
             lifted.lift(dp, dk);
 #pragma unroll

@@ -6,7 +6,7 @@ U, EPS and `rounded` are rows_reference's: half a step of a type, 2^-24 an fp32 
 attention.  A score s = scale <q, k> is off by (2 D + 12) EPS S, S the magnitudes' sum.  A weight e^(s - m) is formed as 2^(s c - m c), c = scale log2 e: the
     roundings of c, m c, the exponent and the power are 8 EPS (|s| + |m| + 1), relative; m's own error is the row's and cancels.  Sums are rescaled
     when the maximum grows, at most once a tile of 16 keys: 2 EPS each, and the power's 4 EPS.  So a weight is off by w = (2 D + 12) EPS S +
-    EPS (8 (|s| + |m| + 1) + 6 (Lk / 16 + 1)), relative, and as an operand by U (16-bit types; up to 512 rows by U U, in two parts) more.  out = sum p v with sum p = 1:
+    EPS (8 (|s| + |m| + 1) + 6 (Lk / 16 + 1)), relative, and as an operand by U (16-bit types; up to 512 rows by 2 U U, in two parts) more.  out = sum p v with sum p = 1:
     sum p (w + U) |v| + |out| sum p w + (4 Lk + 16) EPS sum p |v|; lse: sum p w + (2 Lk + 8) EPS + 8 EPS |lse|.
 gradient.  P = e^(s - lse) with the lse that was stored (off by e_l): relative error w + e_l + 8 EPS |lse|.  dP: (2 D + 8) EPS sum |dO v|.  delta = sum dO out
     with the out that was stored: its bound times |dO|, and (2 D + 8) EPS sum |dO out|.  dS = P (dP - delta): P (rel |dP - delta| + e_dP +
@@ -43,8 +43,11 @@ class Attention:
         self.T = q.dtype
         (B, Lq, H, D), Lk = q.shape, k.shape[1]
         self.per, self.scale = H // k.shape[2], scale
-        # in two parts up to 512 rows: the second one is U of what the first left, U of it
-        self.lp = 0.0 if self.T == F32 else U[self.T] ** 2 if B * Lq * H <= 512 else U[self.T]
+        # in two parts up to 512 rows: the first, towards zero, leaves up to 2 U, of which the second is U off, and up to 2^-30 (fp16: half of FLOOR) more is
+        # added: (2 U + 2^-30) U + 2^-30
+        few = B * Lq * H <= 512
+        self.lp = 0.0 if self.T == F32 else 2 * U[self.T] ** 2 + 2.0 ** -29 if few else U[self.T]
+        self.floor = 2 * FLOOR if few else FLOOR
         keep = valid_keys(B, Lk, k_lengths, key_mask)[:, None, None]
         clean = lambda t: torch.where(keep[:, 0, 0, :, None, None], t.cpu(), torch.zeros((), dtype=t.dtype))  # noqa: E731
         self.q, self.k, self.v = q.double().cpu().transpose(1, 2), heads_of(clean(k), self.per), heads_of(clean(v), self.per)
@@ -69,7 +72,7 @@ class Attention:
         pw = (self.p * self.w).sum(3, keepdim=True)
         e = (self.p * (self.w + self.lp) + LEAST) @ av + self.out.abs() * pw + (4 * Lk + 16) * EPS * (self.p @ av) + Lk * LEAST
         if self.T == torch.float16:
-            e = e + FLOOR * keep.double().expand_as(self.p) @ av
+            e = e + self.floor * keep.double().expand_as(self.p) @ av
         self.e_out = 1.01 * e + rounded(self.out, self.T)
         finite = torch.where(self.lse == low, 0.0, self.lse)
         self.finite = finite[..., None]
@@ -95,7 +98,7 @@ class Attention:
         if self.T == torch.float16 and Lk and Lq:
             size = (ds.abs() + e_ds)
             e_ds = e_ds + FLOOR * torch.maximum(size.max(3, keepdim=True).values, size.max(2, keepdim=True).values)
-            e_p = e_p + FLOOR
+            e_p = e_p + self.floor
 
         def product(a, b, ea, terms, by):
             v = by * (a @ b)

@@ -314,3 +314,26 @@ def test_binding_refusals():
             b.corr_attention(*args, **kw)
     with pytest.raises((TypeError, ValueError)):
         b.corr_attention_backward(q, k, k, good, lse, good.transpose(1, 2).contiguous().transpose(1, 2))
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float16])
+@pytest.mark.parametrize("Lq", [3, 40, 700])
+def test_infinities_that_count(Lq, dtype):
+    """An infinity in a value is one in its column of the result, and one in d_out is one in its column of d_v: also where weights have a second part that is
+    zero or negative.  The other columns are the same bits."""
+    b, g = _b(), torch.Generator(device="cuda").manual_seed(Lq)
+    new = lambda *s: torch.randn(*s, device="cuda", generator=g).to(dtype)  # noqa: E731
+    q, k, v, do = new(1, Lq, 1, 40), new(1, 70, 1, 40), new(1, 70, 1, 40), new(1, Lq, 1, 40)
+    lse = torch.empty(1, 1, Lq, device="cuda")
+    out = b.corr_attention(q, k, v, lse=lse)
+    _, _, dv = b.corr_attention_backward(q, k, v, out, lse, do)
+    rest = torch.arange(40, device="cuda") != 11
+    for sign in (1, -1):
+        bad = v.clone()
+        bad[0, 33, 0, 11] = sign * float("inf")
+        got = b.corr_attention(q, k, bad)
+        assert (got[..., 11] == sign * float("inf")).all() and torch.equal(got[..., rest], out[..., rest])
+        bad = do.clone()
+        bad[0, Lq // 2, 0, 11] = sign * float("inf")
+        got = b.corr_attention_backward(q, k, v, out, lse, bad)[2]
+        assert (got[..., 11] == sign * float("inf")).all() and torch.equal(got[..., rest], dv[..., rest])
