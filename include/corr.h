@@ -349,6 +349,7 @@ corr_status corr_group_norm_backward(corr_dtype type, corr_activation act, const
  *                that does not count is not read or has no influence, infinities and NaN included.
  *   out        : [B, Lq, H, D] dense.  A row of which no key counts, or whose every score is -infinity, is zeros.
  *   lse        : NULL, or fp32 [B, H, Lq]: the logarithm of the sum of e^score, which the gradient reads (-infinity for rows of zeros).
+ * Scores are fp32 and may lie as far from zero as fp32 reaches (scale times a score below 2^127); their weights are those of their differences.
  * Weights meet v as `type` values: rounded once each, up to B Lq H = 512 in two parts (fp16: 2^14 times as large, so that weights down
  * to 4e-9 of a row's largest keep their digits); their sum is not.
  * Limits: D a multiple of 8 up to 256, H <= 128, strides of rows and heads <= 2^21 and of items <= 2^40, B * HK <= 2^20, Lq * H / HK and Lk <= 2^30, B * Lq * H * D and

@@ -152,6 +152,18 @@ template <class T> constexpr float LIFT = std::is_same<T, _Float16>::value ? 14.
 // like.  Of a wave's 32 rows some row's largest score grows in nearly every second of 200 tiles.
 template <class T> constexpr float SLACK = std::is_same<T, _Float16>::value ? 1.75f : 8.f;
 
+// Scores far from zero.  The exponent s c - m c is one rounding of the exact product less a rounded m c.  That rounding is common to the row and divides out,
+// but it grows with m: past 2^21 it takes the quarter of a bit that fp16 has left above SLACK, past 2^31 fp32's range.  A workgroup with a row of |m c|
+// above FAR (a rounding of 2^-8) walks over its keys once more with the exponent (s - m) c, m its largest score.  In the one walk that others need, a
+// subtraction under a condition took 50 registers more and a workgroup of three from each compute unit.
+constexpr float FAR = 65536.f;
+__device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m; }
+// x scale - y in two roundings
+__device__ __forceinline__ float less(float x, float scale, float y) {
+#pragma clang fp contract(off)
+    const float p = x * scale;
+    return p - y;
+}
 // rows (keys) of a tile in LDS: 64, or 32 where 64 would take more than 16 KB (24 in fp32's planes)
 template <class T, int DP, int WAVES> constexpr int tile_rows() {
     return DP <= (WAVES == 1 || std::is_same<T, Planes>::value ? 32 : std::is_same<T, float>::value ? 64 : 128) ? 64 : 32;
@@ -367,106 +379,128 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 1 || (DP == 256 && F32<T>) ? 1
         from_v.ask(load_v, t * KT, to + Load::BYTES, wave, bits);
     };
     const float c = a.scale * LOG2E;
-    const float slack = SLACK<T> / c;
+    float slack = SLACK<T> / c;
     f32x4 o[DB][QB] = {};
-    float m[QB], mc[QB], l[QB];
+    // a weight is 2^(s c + k), in the second walk 2^((s - m) c + LIFT)
+    float m[QB], k[QB], l[QB];
+    bool far = false;
 #pragma unroll
-    for (int j = 0; j < QB; ++j) { m[j] = -INFINITY; mc[j] = 0.f; l[j] = 0.f; }
-    uint64_t bits = 0;
-    unsigned byte = 0;
-    if (steps) {
-        bits = keys.bits(k_lo, KT, keys.byte(k_lo, lane));
-        if (bits && !Late<Load>::value) ask(0, bits);
-        byte = keys.byte(k_lo + KT, lane);
-    }
-    for (int t = 0; t < steps; ++t) {
-        if constexpr (Late<Load>::value) {
-            __syncthreads();
-            if (bits) ask(t, bits);
+    for (int j = 0; j < QB; ++j) { m[j] = -INFINITY; k[j] = LIFT<T>; l[j] = 0.f; }
+    // FROM_M: m is known
+    auto walk = [&](auto from_m) {
+        constexpr bool FROM_M = decltype(from_m)::value;
+        uint64_t bits = 0;
+        unsigned byte = 0;
+        if (steps) {
+            bits = keys.bits(k_lo, KT, keys.byte(k_lo, lane));
+            if (bits && !Late<Load>::value) ask(0, bits);
+            byte = keys.byte(k_lo + KT, lane);
         }
-        land(load_k, load_v, smem);
-        uint64_t next = 0;
-        if (t + 1 < steps) {
-            next = keys.bits(k_lo + (t + 1) * KT, KT, byte);
-            if (next && !Late<Load>::value) ask(t + 1, next);
-            byte = keys.byte(k_lo + (t + 2) * KT, lane);
-        }
-        if (bits) {
-            lds_byte* const tk = lds + t % Load::PLACES * 2 * Load::BYTES;
-            lds_byte* const tv = tk + Load::BYTES;
-            f32x4 s[QB][KB] = {};
-#pragma unroll
-            for (int h = 0; h < CH; ++h)
-#pragma unroll
-                for (int i = 0; i < KB; ++i) {
-                    const F f = N::template straight<DP, KT>(tk, 16 * i + lr, h, lg);
-#pragma unroll
-                    for (int j = 0; j < QB; ++j) s[j][i] = N::times(f, fq[j][h], s[j][i]);
-                }
-            if (bits != ~0ull >> (64 - KT)) {
-                const uint64_t mine = bits >> (4 * lg);
-#pragma unroll
-                for (int i = 0; i < KB; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-#pragma unroll
-                        for (int j = 0; j < QB; ++j) s[j][i][e] = (mine >> (16 * i + e)) & 1 ? s[j][i][e] : -INFINITY;
+        for (int t = 0; t < steps; ++t) {
+            if constexpr (Late<Load>::value) {
+                __syncthreads();
+                if (bits) ask(t, bits);
             }
-            bool grew = false;
-            float top[QB];
-#pragma unroll
-            for (int j = 0; j < QB; ++j) {
-                float x = s[j][0][0];
-#pragma unroll
-                for (int i = 0; i < KB; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x = fmaxf(x, s[j][i][e]);
-                top[j] = lanes_max(x);
-                grew |= top[j] > m[j] + slack;
+            land(load_k, load_v, smem);
+            uint64_t next = 0;
+            if (t + 1 < steps) {
+                next = keys.bits(k_lo + (t + 1) * KT, KT, byte);
+                if (next && !Late<Load>::value) ask(t + 1, next);
+                byte = keys.byte(k_lo + (t + 2) * KT, lane);
             }
-            if (__any(grew)) {
+            if (bits) {
+                lds_byte* const tk = lds + t % Load::PLACES * 2 * Load::BYTES;
+                lds_byte* const tv = tk + Load::BYTES;
+                f32x4 s[QB][KB] = {};
 #pragma unroll
-                for (int j = 0; j < QB; ++j) {
-                    const float was = m[j];
-                    m[j] = fmaxf(was, top[j]);
-                    const float now = m[j] == -INFINITY ? 0.f : m[j] * c, by = was == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc[j] - now);
-                    mc[j] = now;
-                    l[j] *= by;
+                for (int h = 0; h < CH; ++h)
 #pragma unroll
-                    for (int d = 0; d < DB; ++d) o[d][j] *= by;
-                }
-            }
+                    for (int i = 0; i < KB; ++i) {
+                        const F f = N::template straight<DP, KT>(tk, 16 * i + lr, h, lg);
 #pragma unroll
-            for (int j = 0; j < QB; ++j)
-#pragma unroll
-                for (int i = 0; i < KB; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        s[j][i][e] = __builtin_amdgcn_exp2f(fmaf(s[j][i][e], c, LIFT<T> - mc[j]));
-                        l[j] += s[j][i][e];
+                        for (int j = 0; j < QB; ++j) s[j][i] = N::times(f, fq[j][h], s[j][i]);
                     }
+                if (bits != ~0ull >> (64 - KT)) {
+                    const uint64_t mine = bits >> (4 * lg);
 #pragma unroll
-            for (int i = 0; i < KB; i += 2) {
-                F fp[QB], lp[QB];
+                    for (int i = 0; i < KB; ++i)
 #pragma unroll
-                for (int j = 0; j < QB; ++j) {
-                    if constexpr (TWO) {
-                        fp[j] = N::pack_under(&s[j][i]);
-                        lp[j] = N::rest_over(&s[j][i], fp[j]);
-                    } else fp[j] = N::pack(&s[j][i]);
+                        for (int e = 0; e < 4; ++e)
+#pragma unroll
+                            for (int j = 0; j < QB; ++j) s[j][i][e] = (mine >> (16 * i + e)) & 1 ? s[j][i][e] : -INFINITY;
                 }
-#pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                    const F f = N::template turned<DP, KT>(tv, 16 * i, d, lr, lg);
+                if constexpr (!FROM_M) {
+                    bool grew = false;
+                    float top[QB];
 #pragma unroll
                     for (int j = 0; j < QB; ++j) {
-                        if constexpr (TWO) o[d][j] = N::times(f, lp[j], o[d][j]);
-                        o[d][j] = N::times(f, fp[j], o[d][j]);
+                        float x = s[j][0][0];
+#pragma unroll
+                        for (int i = 0; i < KB; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) x = fmaxf(x, s[j][i][e]);
+                        top[j] = lanes_max(x);
+                        grew |= top[j] - m[j] > slack;
+                    }
+                    if (__any(grew)) {
+                        bool past = false;
+#pragma unroll
+                        for (int j = 0; j < QB; ++j) {
+                            const bool first = m[j] == -INFINITY;
+                            m[j] = fmaxf(m[j], top[j]);
+                            const float now = fmaf(-reference(m[j]), c, LIFT<T>), by = first ? 0.f : __builtin_amdgcn_exp2f(now - k[j]);
+                            k[j] = now;
+                            past |= !(fabsf(now) <= FAR) && m[j] < INFINITY;       // an infinite score is NaN either way
+                            l[j] *= by;
+#pragma unroll
+                            for (int d = 0; d < DB; ++d) o[d][j] *= by;
+                        }
+                        if (__any(past)) { far = true; slack = 0.f; }
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < QB; ++j)
+#pragma unroll
+                    for (int i = 0; i < KB; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            s[j][i][e] = __builtin_amdgcn_exp2f(FROM_M ? fmaf(s[j][i][e] - reference(m[j]), c, LIFT<T>) : fmaf(s[j][i][e], c, k[j]));
+                            l[j] += s[j][i][e];
+                        }
+#pragma unroll
+                for (int i = 0; i < KB; i += 2) {
+                    F fp[QB], lp[QB];
+#pragma unroll
+                    for (int j = 0; j < QB; ++j) {
+                        if constexpr (TWO) {
+                            fp[j] = N::pack_under(&s[j][i]);
+                            lp[j] = N::rest_over(&s[j][i], fp[j]);
+                        } else fp[j] = N::pack(&s[j][i]);
+                    }
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) {
+                        const F f = N::template turned<DP, KT>(tv, 16 * i, d, lr, lg);
+#pragma unroll
+                        for (int j = 0; j < QB; ++j) {
+                            if constexpr (TWO) o[d][j] = N::times(f, lp[j], o[d][j]);
+                            o[d][j] = N::times(f, fp[j], o[d][j]);
+                        }
                     }
                 }
             }
+            bits = next;
         }
-        bits = next;
+    };
+    walk(std::false_type{});
+    if (__syncthreads_or(far)) {
+        far = true;
+#pragma unroll
+        for (int j = 0; j < QB; ++j) {
+            l[j] = 0.f;
+#pragma unroll
+            for (int d = 0; d < DB; ++d) o[d][j] = f32x4{};
+        }
+        walk(std::true_type{});
     }
 #pragma unroll
     for (int j = 0; j < QB; ++j) {
@@ -476,12 +510,14 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 1 || (DP == 256 && F32<T>) ? 1
         int q, g;
         query_of(a, r, q, g);
         const int head = at.hk * a.per + g;
+        const float ref = reference(m[j]), lift = far ? LIFT<T> : fmaf(ref, c, k[j]);       // the power of two that weights at the reference have
         if (splits > 1) {
+            const float by = __builtin_amdgcn_exp2f(-lift);
             const int64_t row = ((int64_t)at.split * a.B * a.HK + at.bh) * a.rows + r;
 #pragma unroll
             for (int d = 0; d < DB; ++d)
-                if (16 * d + 4 * lg < a.D) *reinterpret_cast<f32x4*>(a.part_o + row * a.D + 16 * d + 4 * lg) = o[d][j];
-            if (lg == 0) { a.part_ml[2 * row] = mc[j] - LIFT<T>; a.part_ml[2 * row + 1] = sum; }
+                if (16 * d + 4 * lg < a.D) *reinterpret_cast<f32x4*>(a.part_o + row * a.D + 16 * d + 4 * lg) = o[d][j] * by;
+            if (lg == 0) { a.part_ml[2 * row] = ref; a.part_ml[2 * row + 1] = sum * by; }
             continue;
         }
         const float by = sum == 0.f ? 0.f : 1.f / sum;
@@ -492,11 +528,11 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 1 || (DP == 256 && F32<T>) ? 1
             if (16 * d + 4 * lg < a.D) store_some<E, 4>(p + 16 * d + 4 * lg, v, 4);
         }
         if (a.lse && lg == 0)
-            a.lse[((int64_t)at.b * a.HK * a.per + head) * a.Lq + q] = sum == 0.f ? -INFINITY : (mc[j] - LIFT<T> + log2f(sum)) * LN2;
+            a.lse[((int64_t)at.b * a.HK * a.per + head) * a.Lq + q] = sum == 0.f ? -INFINITY : less(ref, a.scale, (lift - log2f(sum)) * LN2);
     }
 }
 
-// The splits' sums of a row, brought to one exponent.  `across` threads have four elements each; `shares` of them take turns at the splits, in a
+// The splits' sums of a row, brought to one reference.  `across` threads have four elements each; `shares` of them take turns at the splits, in a
 // fixed order.
 template <class T, int THREADS>
 __global__ __launch_bounds__(THREADS) void forward_join_kernel(AttentionArgs a, int splits, int across, int shares) {
@@ -504,6 +540,7 @@ __global__ __launch_bounds__(THREADS) void forward_join_kernel(AttentionArgs a, 
     __shared__ float tops[THREADS], totals[THREADS];
     const int tid = threadIdx.x, team = across * shares, lane = tid % across, share = tid / across % shares, d = 4 * lane;
     const int64_t all = (int64_t)a.B * a.HK * a.rows, row = (int64_t)blockIdx.x * (THREADS / team) + tid / team;
+    const float c = a.scale * LOG2E;
     float top = -INFINITY, sum = 0.f;
     f32x4 x = {};
     if (row < all && d < a.D) {
@@ -514,7 +551,7 @@ __global__ __launch_bounds__(THREADS) void forward_join_kernel(AttentionArgs a, 
             const float m = ml[0], l = ml[1];
             const f32x4 v = *reinterpret_cast<const f32x4*>(o);
             if (l == 0.f) continue;
-            const float now = fmaxf(top, m), was = __builtin_amdgcn_exp2f(top - now), is = __builtin_amdgcn_exp2f(m - now);
+            const float now = fmaxf(top, m), was = __builtin_amdgcn_exp2f((top - now) * c), is = __builtin_amdgcn_exp2f((m - now) * c);
             sum = sum * was + l * is;
             x = x * was + v * is;
             top = now;
@@ -527,7 +564,7 @@ __global__ __launch_bounds__(THREADS) void forward_join_kernel(AttentionArgs a, 
         for (int i = 1; i < shares; ++i) {
             const int other = tid + i * across;
             if (totals[other] == 0.f) continue;
-            const float now = fmaxf(top, tops[other]), was = __builtin_amdgcn_exp2f(top - now), is = __builtin_amdgcn_exp2f(tops[other] - now);
+            const float now = fmaxf(top, tops[other]), was = __builtin_amdgcn_exp2f((top - now) * c), is = __builtin_amdgcn_exp2f((tops[other] - now) * c);
             sum = sum * was + totals[other] * is;
             x = x * was + sums[other] * is;
             top = now;
@@ -541,7 +578,7 @@ __global__ __launch_bounds__(THREADS) void forward_join_kernel(AttentionArgs a, 
     const float by = sum == 0.f ? 0.f : 1.f / sum;
     const float v[4] = {x[0] * by, x[1] * by, x[2] * by, x[3] * by};
     store_some<T, 4>((T*)a.out + (((int64_t)b * a.Lq + q) * a.HK * a.per + head) * a.D + d, v, 4);
-    if (a.lse && lane == 0) a.lse[((int64_t)b * a.HK * a.per + head) * a.Lq + q] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * LN2;
+    if (a.lse && lane == 0) a.lse[((int64_t)b * a.HK * a.per + head) * a.Lq + q] = sum == 0.f ? -INFINITY : less(top, a.scale, -log2f(sum) * LN2);
 }
 
 // ---- gradient.  With P = exp(s - lse) and delta = sum over d of d_out out: dV = P^T dO, dS = P (dO V^T - delta), dQ = scale dS K,
