@@ -376,6 +376,8 @@ corr_status corr_attention(const corr_attention_args* args, void* out, float* ls
  * Weights and dS = P (d_out v^T - sum d_out out) meet the other operand as `type` values, rounded once each, up to B Lq H = 512 in two parts, for d_k
  * and d_v also up to B Lk HK = 64 (fp16: dS times a power of two of its row or key, so that small gradients keep their digits).  out is read as it was rounded: where one key has nearly all of a row's weight, dS is small beside
  * d_out v^T and its error is that rounding's, half a step of out times d_out.
+ * lse is read as fp32 holds it: the weights e^(score - lse) are off by its rounding, 6e-8 |lse| relative (6e-4 at 1e4); a key which has all of a row's weight
+ * has one at any size.
  */
 size_t corr_attention_backward_workspace_bytes(corr_dtype type, int64_t B, int64_t Lq, int64_t Lk, int64_t H, int64_t HK, int64_t D);
 corr_status corr_attention_backward(const corr_attention_args* args, const void* out, const float* lse, const void* d_out,

@@ -15,7 +15,7 @@ struct AttentionArgs {
     float* part_o; float* part_ml;         // splits > 1: [splits][B * HK][rows][D] sums, [..][2] {exponent of two, sum}
     // gradient
     const void* o; const float* saved_lse; const void* d_out;
-    float* aux;                            // [B * HK][rows up to a multiple of 64][2]: {lse log2 e, sum of d_out out}
+    float* aux;                            // [2][B * HK][rows up to a multiple of 64]: lse log2 e (less LIFT; 2 lse of far rows), sum of d_out out
     void *d_q, *d_k, *d_v;                 // each may be null (d_k and d_v together)
     float *part_q, *part_k, *part_v;       // splits > 1: [splits] of the gradient's elements
 };

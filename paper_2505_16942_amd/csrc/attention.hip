@@ -78,6 +78,8 @@ template <class T> struct Num {
         return f;
     }
     static __device__ __forceinline__ f32x4 times(const F& a, const F& b, f32x4 c) { return mma(a, b, c); }
+    // the transposed product, bit by bit what times(b, a) makes
+    static __device__ __forceinline__ f32x4 times_back(const F& a, const F& b, f32x4 c) { return mma(a, b, c); }
     // elements d .. d + 7 of row `p`, zeros behind D or without a row
     static __device__ __forceinline__ F load(const T* p, int d, int D, bool there) {
         F f = {};
@@ -129,6 +131,12 @@ template <> struct Num<float> {
         for (int q = 0; q < 6; ++q) c = mma(a.p[QA[q]], b.p[QB[q]], c);
         return c;
     }
+    static __device__ __forceinline__ f32x4 times_back(const F& a, const F& b, f32x4 c) {
+        constexpr int QA[6] = {0, 2, 1, 0, 1, 0}, QB[6] = {2, 0, 1, 1, 0, 0};
+#pragma unroll
+        for (int q = 0; q < 6; ++q) c = mma(a.p[QA[q]], b.p[QB[q]], c);
+        return c;
+    }
     static __device__ __forceinline__ F load(const float* p, int d, int D, bool there) {
         f32x4 x[2] = {};
         if (there && d < D) {
@@ -157,6 +165,9 @@ template <class T> constexpr float SLACK = std::is_same<T, _Float16>::value ? 1.
 // above FAR (a rounding of 2^-8) walks over its keys once more with the exponent (s - m) c, m its largest score.  In the one walk that others need, a
 // subtraction under a condition took 50 registers more and a workgroup of three from each compute unit.
 constexpr float FAR = 65536.f;
+// The gradient's P = e^(s - lse) has what lse log2 e is rounded by.  Workgroups with a row of |lse| from FAR_LSE on (1e-5 there) take the difference before the
+// factor, of s scale rounded as the forward pass rounds it into lse, so that a key which has all of a row's weight has 1.  What is left is lse's own rounding.
+constexpr float FAR_LSE = 256.f;
 __device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m; }
 // x scale - y in two roundings
 __device__ __forceinline__ float less(float x, float scale, float y) {
@@ -164,6 +175,13 @@ __device__ __forceinline__ float less(float x, float scale, float y) {
     const float p = x * scale;
     return p - y;
 }
+// a score's weight: `low` is the row's lse log2 e - LIFT, where far its lse
+template <class T, bool FAR_ROWS> __device__ __forceinline__ float power(float s, float scale, float c, float low) {
+    if constexpr (!FAR_ROWS) return __builtin_amdgcn_exp2f(fmaf(s, c, -low));
+    const float x = less(s, scale, low);
+    return __builtin_amdgcn_exp2f(fmaf(x > 0.f ? 0.f : x, LOG2E, LIFT<T>));
+}
+
 // rows (keys) of a tile in LDS: 64, or 32 where 64 would take more than 16 KB (24 in fp32's planes)
 template <class T, int DP, int WAVES> constexpr int tile_rows() {
     return DP <= (WAVES == 1 || std::is_same<T, Planes>::value ? 32 : std::is_same<T, float>::value ? 64 : 128) ? 64 : 32;
@@ -585,7 +603,8 @@ __global__ __launch_bounds__(THREADS) void forward_join_kernel(AttentionArgs a, 
 // dK = scale dS^T Q.  Rows' sums meet in one workgroup and keys' sums in another, so scores are computed twice (seven products for five) and nothing
 // is added by atomics: the same bits on every call.  2 x 14400 x 14400, 2 heads of 64, bf16: rows 375 us, keys 515 (seven products: 830 TFLOP/s), matrix
 // instructions in a third of the cycles, the vector unit in six tenths; in fp16 470 and 650, with the powers of two of dS.
-// delta, and lse in powers of two (less LIFT: the weights are 2^LIFT times as large), in the order of rows; rows behind the last have a weight of zero.
+// delta, and lse in powers of two (less LIFT: the weights are 2^LIFT times as large), in the order of rows; rows behind the last have a weight of zero.  A far
+// row has 2 lse there, which is larger than any of the others.
 template <class T>
 __global__ __launch_bounds__(256) void delta_kernel(AttentionArgs a, int aux_rows) {
     const int lane = threadIdx.x & 15;
@@ -605,14 +624,19 @@ __global__ __launch_bounds__(256) void delta_kernel(AttentionArgs a, int aux_row
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum = fmaf(x[e], y[e], sum);
             }
-            low = a.saved_lse[((int64_t)b * a.HK * a.per + head) * a.Lq + q] * LOG2E;
-            low = low == -INFINITY ? INFINITY : low - LIFT<T>;           // a row without a key: no weight
+            const float lse = a.saved_lse[((int64_t)b * a.HK * a.per + head) * a.Lq + q];
+            low = lse == -INFINITY ? INFINITY : fabsf(lse) < FAR_LSE ? lse * LOG2E - LIFT<T> : 2.f * lse;      // a row without a key: no weight
         }
 #pragma unroll
         for (int x = 1; x < 16; x *= 2) sum += __shfl_xor(sum, x);
-        if (lane == 0) { a.aux[2 * row] = low; a.aux[2 * row + 1] = low == INFINITY ? 0.f : sum; }
+        if (lane == 0) { a.aux[row] = low; a.aux[all + row] = low == INFINITY ? 0.f : sum; }
     }
 }
+
+__device__ __forceinline__ bool far_row(float low) { return fabsf(low) >= 2.f * FAR_LSE && low != INFINITY; }
+__device__ __forceinline__ bool far_row(f32x4 low) { return far_row(low[0]) || far_row(low[1]) || far_row(low[2]) || far_row(low[3]); }
+// lse of any row, infinity where it has no key
+template <class T> __device__ __forceinline__ float row_lse(float low) { return fabsf(low) >= 2.f * FAR_LSE ? 0.5f * low : (low + LIFT<T>) * LN2; }
 
 // dS as a product's operand.  bf16 has fp32's range: rounded once.  fp16 would lose what is small: a row's (key's) elements are held
 // times a power of two that brings the largest so far to 2^13 .. 2^15, and the sums follow when it changes.  The elements come 2^LIFT times as large, as the
@@ -687,9 +711,10 @@ __global__ __launch_bounds__(256, DP == 256 && (F32<T> || TWO) ? 1 : 2) void dq_
             fq[j][t] = N::load(p, t * FK + lg * 8, a.D, there);
             fo[j][t] = N::load(w, t * FK + lg * 8, a.D, there);
         }
-        const f32x2 x = there ? *reinterpret_cast<const f32x2*>(a.aux + 2 * ((int64_t)at.bh * attention_aux_rows(a.rows) + r)) : f32x2{INFINITY, 0.f};
-        low[j] = x[0];
-        delta[j] = x[1];
+        const int aux_rows = attention_aux_rows(a.rows);
+        const float* const aux = a.aux + (int64_t)at.bh * aux_rows + r;
+        low[j] = there ? aux[0] : INFINITY;
+        delta[j] = there ? aux[(int64_t)a.B * a.HK * aux_rows] : 0.f;
     }
     Load load_k, load_v;
     load_k.plan(wave, lane, a.D);
@@ -699,83 +724,95 @@ __global__ __launch_bounds__(256, DP == 256 && (F32<T> || TWO) ? 1 : 2) void dq_
         from_k.ask(load_k, t * KT, to, wave, bits);
         from_v.ask(load_v, t * KT, to + Load::BYTES, wave, bits);
     };
+    bool some_far = false;
+#pragma unroll
+    for (int j = 0; j < QB; ++j) some_far |= far_row(low[j]);
+    const bool far = __syncthreads_or(some_far);
+    if (far)
+#pragma unroll
+        for (int j = 0; j < QB; ++j) low[j] = row_lse<T>(low[j]);
     const float c = a.scale * LOG2E;
     f32x4 dq[DB][QB] = {};
     Lifted<T, QB> lifted;
-    uint64_t bits = 0;
-    unsigned byte = 0;
-    if (steps) {
-        bits = keys.bits(k_lo, KT, keys.byte(k_lo, lane));
-        if (bits && !Late<Load>::value) ask(0, bits);
-        byte = keys.byte(k_lo + KT, lane);
-    }
-    for (int t = 0; t < steps; ++t) {
-        if constexpr (Late<Load>::value) {
-            __syncthreads();
-            if (bits) ask(t, bits);
+    auto walk = [&](auto is_far) {
+        constexpr bool IS_FAR = decltype(is_far)::value;
+        uint64_t bits = 0;
+        unsigned byte = 0;
+        if (steps) {
+            bits = keys.bits(k_lo, KT, keys.byte(k_lo, lane));
+            if (bits && !Late<Load>::value) ask(0, bits);
+            byte = keys.byte(k_lo + KT, lane);
         }
-        land(load_k, load_v, smem);
-        uint64_t next = 0;
-        if (t + 1 < steps) {
-            next = keys.bits(k_lo + (t + 1) * KT, KT, byte);
-            if (next && !Late<Load>::value) ask(t + 1, next);
-            byte = keys.byte(k_lo + (t + 2) * KT, lane);
-        }
-        if (bits) {
-            lds_byte* const tk = lds + t % Load::PLACES * 2 * Load::BYTES;
-            lds_byte* const tv = tk + Load::BYTES;
-            const bool some = bits != ~0ull >> (64 - KT);
-            const uint64_t mine = bits >> (4 * lg);
+        for (int t = 0; t < steps; ++t) {
+            if constexpr (Late<Load>::value) {
+                __syncthreads();
+                if (bits) ask(t, bits);
+            }
+            land(load_k, load_v, smem);
+            uint64_t next = 0;
+            if (t + 1 < steps) {
+                next = keys.bits(k_lo + (t + 1) * KT, KT, byte);
+                if (next && !Late<Load>::value) ask(t + 1, next);
+                byte = keys.byte(k_lo + (t + 2) * KT, lane);
+            }
+            if (bits) {
+                lds_byte* const tk = lds + t % Load::PLACES * 2 * Load::BYTES;
+                lds_byte* const tv = tk + Load::BYTES;
+                const bool some = bits != ~0ull >> (64 - KT);
+                const uint64_t mine = bits >> (4 * lg);
 #pragma unroll
-            for (int kk = 0; kk < KT / FK; ++kk) {
-                f32x4 s[QB][PB] = {}, dp[QB][PB] = {};
-                if constexpr (FROM)
+                for (int kk = 0; kk < KT / FK; ++kk) {
+                    f32x4 s[QB][PB] = {}, dp[QB][PB] = {};
+                    if constexpr (FROM)
+#pragma unroll
+                        for (int j = 0; j < QB; ++j)
+#pragma unroll
+                            for (int i = 0; i < PB; ++i) dp[j][i] = f32x4{-delta[j], -delta[j], -delta[j], -delta[j]};
+#pragma unroll
+                    for (int h = 0; h < CH; ++h)
+#pragma unroll
+                        for (int i = 0; i < PB; ++i) {
+                            const F f = N::template straight<DP, KT>(tk, FK * kk + 16 * i + lr, h, lg);
+                            const F w = N::template straight<DP, KT>(tv, FK * kk + 16 * i + lr, h, lg);
+#pragma unroll
+                            for (int j = 0; j < QB; ++j) {
+                                s[j][i] = N::times(f, fq[j][h], s[j][i]);
+                                dp[j][i] = N::times(w, fo[j][h], dp[j][i]);
+                            }
+                        }
 #pragma unroll
                     for (int j = 0; j < QB; ++j)
 #pragma unroll
-                        for (int i = 0; i < PB; ++i) dp[j][i] = f32x4{-delta[j], -delta[j], -delta[j], -delta[j]};
+                        for (int i = 0; i < PB; ++i)
 #pragma unroll
-                for (int h = 0; h < CH; ++h)
-#pragma unroll
-                    for (int i = 0; i < PB; ++i) {
-                        const F f = N::template straight<DP, KT>(tk, FK * kk + 16 * i + lr, h, lg);
-                        const F w = N::template straight<DP, KT>(tv, FK * kk + 16 * i + lr, h, lg);
-#pragma unroll
-                        for (int j = 0; j < QB; ++j) {
-                            s[j][i] = N::times(f, fq[j][h], s[j][i]);
-                            dp[j][i] = N::times(w, fo[j][h], dp[j][i]);
-                        }
-                    }
-#pragma unroll
-                for (int j = 0; j < QB; ++j)
-#pragma unroll
-                    for (int i = 0; i < PB; ++i)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float p = __builtin_amdgcn_exp2f(fmaf(s[j][i][e], c, -low[j]));
-                            dp[j][i][e] = p * (FROM ? dp[j][i][e] : dp[j][i][e] - delta[j]);
-                            if (some) dp[j][i][e] = (mine >> (FK * kk + 16 * i + e)) & 1 ? dp[j][i][e] : 0.f;
-                        }
-                lifted.lift(dp, dq);
-                F fs[QB], ls[QB];
-#pragma unroll
-                for (int j = 0; j < QB; ++j) {
-                    fs[j] = N::pack(dp[j]);
-                    if constexpr (TWO) ls[j] = N::rest(dp[j], fs[j]);
-                }
-#pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                    const F f = N::template turned<DP, KT>(tk, FK * kk, d, lr, lg);
+                            for (int e = 0; e < 4; ++e) {
+                                const float p = power<T, IS_FAR>(s[j][i][e], a.scale, c, low[j]);
+                                dp[j][i][e] = p * (FROM ? dp[j][i][e] : dp[j][i][e] - delta[j]);
+                                if (some) dp[j][i][e] = (mine >> (FK * kk + 16 * i + e)) & 1 ? dp[j][i][e] : 0.f;
+                            }
+                    lifted.lift(dp, dq);
+                    F fs[QB], ls[QB];
 #pragma unroll
                     for (int j = 0; j < QB; ++j) {
-                        if constexpr (TWO) dq[d][j] = N::times(f, ls[j], dq[d][j]);
-                        dq[d][j] = N::times(f, fs[j], dq[d][j]);
+                        fs[j] = N::pack(dp[j]);
+                        if constexpr (TWO) ls[j] = N::rest(dp[j], fs[j]);
+                    }
+#pragma unroll
+                    for (int d = 0; d < DB; ++d) {
+                        const F f = N::template turned<DP, KT>(tk, FK * kk, d, lr, lg);
+#pragma unroll
+                        for (int j = 0; j < QB; ++j) {
+                            if constexpr (TWO) dq[d][j] = N::times(f, ls[j], dq[d][j]);
+                            dq[d][j] = N::times(f, fs[j], dq[d][j]);
+                        }
                     }
                 }
             }
+            bits = next;
         }
-        bits = next;
-    }
+    };
+    if (far) walk(std::true_type{});
+    else walk(std::false_type{});
 #pragma unroll
     for (int j = 0; j < QB; ++j) {
         const int r = r0 + 16 * j + lr;
@@ -804,12 +841,21 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void dkv_kernel(AttentionAr
     constexpr int RT = tile_rows<T, DP, 4>(), CH = DP / FK, DB = DP / 16, PB = 2;
     typedef Tile<T, DP, RT, 4> Load;
     __shared__ __align__(1024) unsigned char smem[2 * Load::PLACES * Load::BYTES];
+    __shared__ int answers[4];                           // of the waves: 1, a key counts; 2, a row is far
     lds_byte* const lds = (lds_byte*)smem;
     const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)lds);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lr = lane & 15, lg = lane >> 4;
     const Place at = place_of(a, tiles, splits);
     const Keys keys = keys_of<T>(a, at.b);
     const int k0 = (at.tile * 4 + wave) * 16 * KB, r_lo = at.split * share, r_hi = min(a.rows, r_lo + share);
+    const int aux_rows = attention_aux_rows(a.rows);
+    const float* const lows = a.aux + (int64_t)at.bh * aux_rows;
+    const float* const deltas = lows + (int64_t)a.B * a.HK * aux_rows;
+    // whether a row of the share is far: the first rows' answer comes with the keys
+    const f32x4 first = r_lo + 4 * tid < r_hi ? *reinterpret_cast<const f32x4*>(lows + r_lo + 4 * tid) : f32x4{};
+    bool some_far = false;
+#pragma unroll 8
+    for (int r = r_lo + 4 * (tid + 256); r < r_hi; r += 4 * 256) some_far |= far_row(*reinterpret_cast<const f32x4*>(lows + r));
     F fk[KB][CH], fv[KB][CH];
     bool counts[KB];
     bool any = false;
@@ -826,7 +872,12 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void dkv_kernel(AttentionAr
             fv[j][t] = N::load(w, t * FK + lg * 8, a.D, counts[j]);
         }
     }
-    const int steps = __syncthreads_or(any) ? (r_hi - r_lo + RT - 1) / RT : 0;
+    const int mine = (__any(any) ? 1 : 0) | (__any(some_far || far_row(first)) ? 2 : 0);
+    if (lane == 0) answers[wave] = mine;
+    __syncthreads();
+    const int answer = __builtin_amdgcn_readfirstlane(answers[0] | answers[1] | answers[2] | answers[3]);
+    const int steps = answer & 1 ? (r_hi - r_lo + RT - 1) / RT : 0;
+    const bool far = answer & 2;
     const int64_t o_row = (int64_t)a.HK * a.per * a.D;
     Load load_q, load_o;
     load_q.plan(wave, lane, a.D);
@@ -854,84 +905,92 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void dkv_kernel(AttentionAr
         }
     };
     const float c = a.scale * LOG2E;
-    const float* const aux = a.aux + 2 * (int64_t)at.bh * attention_aux_rows(a.rows);
     f32x4 dk[DB][KB] = {}, dv[DB][KB] = {};
     Lifted<T, KB> lifted;
-    if (steps && !Late<Load>::value) ask(0);
-    for (int t = 0; t < steps; ++t) {
-        if constexpr (Late<Load>::value) {
-            __syncthreads();
-            ask(t);
-        }
-        land(load_q, load_o, smem);
-        if (t + 1 < steps && !Late<Load>::value) ask(t + 1);
-        lds_byte* const tq = lds + t % Load::PLACES * 2 * Load::BYTES;
-        lds_byte* const to = tq + Load::BYTES;
-#pragma unroll
-        for (int kk = 0; kk < RT / FK; ++kk) {
-            f32x4 low[PB], delta[PB];
-#pragma unroll
-            for (int i = 0; i < PB; ++i) {               // share and tiles are multiples of 16, and so is the array's length
-                const int r = r_lo + t * RT + FK * kk + 16 * i + 4 * lg;
-                f32x4 x = {INFINITY, 0.f, INFINITY, 0.f}, y = x;
-                if (r < r_hi) {
-                    x = *reinterpret_cast<const f32x4*>(aux + 2 * r);
-                    y = *reinterpret_cast<const f32x4*>(aux + 2 * r + 4);
-                }
-                low[i] = f32x4{x[0], x[2], y[0], y[2]};
-                delta[i] = f32x4{x[1], x[3], y[1], y[3]};
+    auto walk = [&](auto is_far) {
+        constexpr bool IS_FAR = decltype(is_far)::value;
+        if (steps && !Late<Load>::value) ask(0);
+        for (int t = 0; t < steps; ++t) {
+            if constexpr (Late<Load>::value) {
+                __syncthreads();
+                ask(t);
             }
-            f32x4 s[KB][PB] = {}, dp[KB][PB] = {};
+            land(load_q, load_o, smem);
+            if (t + 1 < steps && !Late<Load>::value) ask(t + 1);
+            lds_byte* const tq = lds + t % Load::PLACES * 2 * Load::BYTES;
+            lds_byte* const to = tq + Load::BYTES;
 #pragma unroll
-            for (int h = 0; h < CH; ++h)
+            for (int kk = 0; kk < RT / FK; ++kk) {
+                f32x4 low[PB], delta[PB];
 #pragma unroll
-                for (int i = 0; i < PB; ++i) {
-                    const F f = N::template straight<DP, RT>(tq, FK * kk + 16 * i + lr, h, lg);
-                    const F w = N::template straight<DP, RT>(to, FK * kk + 16 * i + lr, h, lg);
-#pragma unroll
-                    for (int j = 0; j < KB; ++j) {
-                        s[j][i] = N::times(f, fk[j][h], s[j][i]);
-                        dp[j][i] = N::times(w, fv[j][h], dp[j][i]);
+                for (int i = 0; i < PB; ++i) {               // share and tiles are multiples of 16, and so is the array's length
+                    const int r = r_lo + t * RT + FK * kk + 16 * i + 4 * lg;
+                    low[i] = f32x4{INFINITY, INFINITY, INFINITY, INFINITY};
+                    delta[i] = f32x4{};
+                    if (r < r_hi) {
+                        low[i] = *reinterpret_cast<const f32x4*>(lows + r);
+                        delta[i] = *reinterpret_cast<const f32x4*>(deltas + r);
                     }
+                    if constexpr (IS_FAR)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) low[i][e] = row_lse<T>(low[i][e]);
                 }
-            F fp[KB], fs[KB], lp[KB], ls[KB];
+                f32x4 s[KB][PB] = {}, dp[KB][PB] = {};
 #pragma unroll
-            for (int j = 0; j < KB; ++j) {
+                for (int h = 0; h < CH; ++h)
 #pragma unroll
-                for (int i = 0; i < PB; ++i)
+                    for (int i = 0; i < PB; ++i) {
+                        const F f = N::template straight<DP, RT>(tq, FK * kk + 16 * i + lr, h, lg);
+                        const F w = N::template straight<DP, RT>(to, FK * kk + 16 * i + lr, h, lg);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float p = __builtin_amdgcn_exp2f(fmaf(s[j][i][e], c, -low[i][e]));
-                        dp[j][i][e] = p * (dp[j][i][e] - delta[i][e]);
-                        s[j][i][e] = p;
+                        for (int j = 0; j < KB; ++j) {
+                            s[j][i] = IS_FAR ? N::times_back(f, fk[j][h], s[j][i]) : N::times(f, fk[j][h], s[j][i]);
+                            dp[j][i] = N::times(w, fv[j][h], dp[j][i]);
+                        }
                     }
-                if constexpr (TWO) {
-                    fp[j] = N::pack_under(s[j]);
-                    lp[j] = N::rest_over(s[j], fp[j]);
-                } else fp[j] = N::pack(s[j]);
-            }
-            lifted.lift(dp, dk);
-#pragma unroll
-            for (int j = 0; j < KB; ++j) {
-                fs[j] = N::pack(dp[j]);
-                if constexpr (TWO) ls[j] = N::rest(dp[j], fs[j]);
-            }
-#pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                const F f = N::template turned<DP, RT>(to, FK * kk, d, lr, lg);
-                const F w = N::template turned<DP, RT>(tq, FK * kk, d, lr, lg);
+                // products and weights one after the other: 50 spilled registers less (2 x 1000 x 1000 x 4 x 256 fp32: 185 -> 153 us)
+                if constexpr (F32<T> && DP == 256) __builtin_amdgcn_sched_barrier(0);
+                F fp[KB], fs[KB], lp[KB], ls[KB];
 #pragma unroll
                 for (int j = 0; j < KB; ++j) {
+#pragma unroll
+                    for (int i = 0; i < PB; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float p = power<T, IS_FAR>(s[j][i][e], a.scale, c, low[i][e]);
+                            dp[j][i][e] = p * (dp[j][i][e] - delta[i][e]);
+                            s[j][i][e] = p;
+                        }
                     if constexpr (TWO) {
-                        dv[d][j] = N::times(f, lp[j], dv[d][j]);
-                        dk[d][j] = N::times(w, ls[j], dk[d][j]);
+                        fp[j] = N::pack_under(s[j]);
+                        lp[j] = N::rest_over(s[j], fp[j]);
+                    } else fp[j] = N::pack(s[j]);
+                }
+                lifted.lift(dp, dk);
+#pragma unroll
+                for (int j = 0; j < KB; ++j) {
+                    fs[j] = N::pack(dp[j]);
+                    if constexpr (TWO) ls[j] = N::rest(dp[j], fs[j]);
+                }
+#pragma unroll
+                for (int d = 0; d < DB; ++d) {
+                    const F f = N::template turned<DP, RT>(to, FK * kk, d, lr, lg);
+                    const F w = N::template turned<DP, RT>(tq, FK * kk, d, lr, lg);
+#pragma unroll
+                    for (int j = 0; j < KB; ++j) {
+                        if constexpr (TWO) {
+                            dv[d][j] = N::times(f, lp[j], dv[d][j]);
+                            dk[d][j] = N::times(w, ls[j], dk[d][j]);
+                        }
+                        dv[d][j] = N::times(f, fp[j], dv[d][j]);
+                        dk[d][j] = N::times(w, fs[j], dk[d][j]);
                     }
-                    dv[d][j] = N::times(f, fp[j], dv[d][j]);
-                    dk[d][j] = N::times(w, fs[j], dk[d][j]);
                 }
             }
         }
-    }
+    };
+    if (far) walk(std::true_type{});
+    else walk(std::false_type{});
     const int64_t all = (int64_t)a.B * a.Lk * a.HK * a.D;
 #pragma unroll
     for (int j = 0; j < KB; ++j) {
