@@ -3,6 +3,7 @@
 // d_y twice.  2 x 518400 x 256 in 32 groups, bf16 (265 MB an item: no cache holds it): 346 us, of that statistics 140 (while the last result leaves the
 // memory-side cache) and y 191 (5.5 TB/s), 4.6 TB/s over three passes, a copy's rate.  Gradient of 2 x 129600 x 128 in 8 groups, bf16: 85 us, sums 38
 // (3.6 TB/s), d_x 41 (4.9 TB/s).  Small ones are launches: 4 x 7285 x 96 in 32, fp32: gradient 24 us in three of 10, 6 and 11.
+#include <algorithm>
 #include <type_traits>
 #include "matrix.h"
 #include "group_norm.h"
@@ -169,29 +170,35 @@ template <int WAVES> __device__ __forceinline__ float sum_all(float x, float* ro
     return x;
 }
 
-// A group's parts: mean and 1 / spread.  One workgroup a group and item.  The parts' means are averaged first and the squares taken about that.
-__global__ __launch_bounds__(JOIN_THREADS) void finish_stats_kernel(GroupNormArgs a) {
-    __shared__ float room[JOIN_THREADS / 64];
-    const int g = blockIdx.x % a.G, b = blockIdx.x / a.G, width = a.C / a.G, all = a.parts * width;
-    const float* const part = a.part + 2 * ((int64_t)b * a.parts * a.C + g * width);
+// A group's parts: mean and 1 / spread.  One workgroup a group and item, or several after each other.  The parts' means are averaged first and the squares
+// taken about that.
+constexpr int MOST_GROUPS = 1 << 20;                     // workgroups: a launch has fewer than 2^32 threads
+template <int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void finish_stats_kernel(GroupNormArgs a) {
+    __shared__ float room[WAVES];
+    const int width = a.C / a.G, all = a.parts * width;
     const float n = (float)a.P * (float)width;
-    float mean = 0.f, square = 0.f;
-    auto each = [&](auto f) {
+    for (int at = blockIdx.x; at < a.B * a.G; at += gridDim.x) {
+        const int g = at % a.G, b = at / a.G;
+        const float* const part = a.part + 2 * ((int64_t)b * a.parts * a.C + g * width);
+        float mean = 0.f, square = 0.f;
+        auto each = [&](auto f) {
 #pragma unroll 4
-        for (int i = threadIdx.x; i < all; i += JOIN_THREADS) {
-            const int p = (unsigned)i / (unsigned)width;
-            const float* const q = part + 2 * ((int64_t)p * a.C + (i - p * width));
-            f(q, (float)min(a.share, a.P - p * a.share));
+            for (int i = threadIdx.x; i < all; i += 64 * WAVES) {
+                const int p = (unsigned)i / (unsigned)width;
+                const float* const q = part + 2 * ((int64_t)p * a.C + (i - p * width));
+                f(q, (float)min(a.share, a.P - p * a.share));
+            }
+        };
+        const float some = part[0];                      // differences from it: a constant's mean is that constant, however large
+        each([&](const float* q, float m) { mean = fmaf(q[0] - some, m / n, mean); });
+        mean = some + sum_all<WAVES>(mean, room);
+        each([&](const float* q, float m) { const float d = q[0] - mean; square += fmaf(m * d, d, q[1]); });
+        square = sum_all<WAVES>(square, room);
+        if (threadIdx.x == 0) {
+            a.stats[2 * at] = mean;
+            a.stats[2 * at + 1] = 1.f / sqrtf(square / n + a.eps);
         }
-    };
-    const float some = part[0];                          // differences from it: a constant's mean is that constant, however large
-    each([&](const float* q, float m) { mean = fmaf(q[0] - some, m / n, mean); });
-    mean = some + sum_all<JOIN_THREADS / 64>(mean, room);
-    each([&](const float* q, float m) { const float d = q[0] - mean; square += fmaf(m * d, d, q[1]); });
-    square = sum_all<JOIN_THREADS / 64>(square, room);
-    if (threadIdx.x == 0) {
-        a.stats[2 * blockIdx.x] = mean;
-        a.stats[2 * blockIdx.x + 1] = 1.f / sqrtf(square / n + a.eps);
     }
 }
 
@@ -511,16 +518,22 @@ template <class F> void with_act(int act, F f) {
     }
 }
 template <class T, int V>
-void forward(const GroupNormArgs& a, hipStream_t s) {
+hipError_t forward(const GroupNormArgs& a, hipStream_t s) {
     if (a.held) {
         with_act(a.act, [&](auto act) { hipLaunchKernelGGL((held_kernel<T, V, decltype(act)::value>), dim3(a.B * a.G), dim3(HELD_THREADS), 0, s, a, a.held); });
-        return;
+        return hipGetLastError();
     }
     const int ct = threads_across<V>(a.C);
     const dim3 grid((unsigned)cdiv(a.C, ct * V), a.parts, a.B);
     hipLaunchKernelGGL((stats_kernel<T, V>), grid, dim3(THREADS), 0, s, a, ct);
-    hipLaunchKernelGGL(finish_stats_kernel, dim3(a.B * a.G), dim3(JOIN_THREADS), 0, s, a);
+    const dim3 groups((unsigned)std::min(a.B * a.G, MOST_GROUPS));
+    // few parts: one wave (64 x 64 x 512 in 512 groups bf16, the whole call: 146 -> 26 us)
+    if (a.parts * (a.C / a.G) <= 64) hipLaunchKernelGGL(finish_stats_kernel<1>, groups, dim3(64), 0, s, a);
+    else hipLaunchKernelGGL(finish_stats_kernel<JOIN_THREADS / 64>, groups, dim3(JOIN_THREADS), 0, s, a);
+    const hipError_t e = hipGetLastError();              // without statistics there is no result
+    if (e != hipSuccess) return e;
     with_act(a.act, [&](auto act) { hipLaunchKernelGGL((apply_kernel<T, V, decltype(act)::value>), grid, dim3(THREADS), 0, s, a, ct); });
+    return hipGetLastError();
 }
 // Few items' sums follow each other in one launch.
 bool joined_at_once(const GroupNormArgs& a) { return a.B == 1 || (a.B <= 4 && !a.held); }
@@ -557,10 +570,7 @@ void group_norm_plan(GroupNormArgs& a, bool gradient) {
     a.held = whole && pieces <= HELD_THREADS * PIECES && pieces * a.B * a.G <= (gradient ? 1 << 17 : 1 << 18) ? (int)across_group : 0;
 }
 hipError_t launch_group_norm(const GroupNormArgs& a, hipStream_t s) {
-    if (a.type == CORR_TYPE_F32) forward<float, 4>(a, s);
-    else if (a.type == CORR_TYPE_BF16) forward<__bf16, 8>(a, s);
-    else forward<_Float16, 8>(a, s);
-    return hipGetLastError();
+    return a.type == CORR_TYPE_F32 ? forward<float, 4>(a, s) : a.type == CORR_TYPE_BF16 ? forward<__bf16, 8>(a, s) : forward<_Float16, 8>(a, s);
 }
 hipError_t launch_group_norm_backward(const GroupNormArgs& a, hipStream_t s) {
     if (a.type == CORR_TYPE_F32) backward<float, 4>(a, s);

@@ -5,7 +5,7 @@ import itertools
 import pytest
 
 import maps_reference as ref
-from rows_reference import ACTS
+from rows_reference import ACTS, slope
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -211,3 +211,33 @@ def test_nothing_to_do():
         assert m.corr_group_norm(x, 2, stats=stats).shape == x.shape and not stats.any()
         dx, dw, db = m.corr_group_norm_backward(x, 2, stats, x)
         assert dx.shape == x.shape and not dw.any() and not db.any()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("size", [(16384, 3, 256, 256), (65535, 2, 128, 64), (65535, 2, 128, 128), (512, 16, 16384, 16384)])
+def test_millions_of_groups(size, dtype):
+    """2^22 items times groups and more, where a workgroup of 1024 threads each would be 2^32 threads: some items against float64, all of them written."""
+    m, new, (B, P, C, G) = _b(), _gen(14), size
+    x = torch.randn(B, P, C, device="cuda").to(dtype)
+    g = torch.randn(B, P, C, device="cuda").mul_(0.1).to(dtype)
+    w, b = new(C, mean=1.0, sigma=0.1), new(C, sigma=0.1)
+    y, stats, (dx, dw, db) = _run(x, G, w, b, g, m.CORR_ACT_SILU)
+    assert y.isfinite().all() and stats.isfinite().all() and (stats[..., 1] > 0).all() and dx.isfinite().all()
+    some = torch.tensor([0, B // 2, B - 1], device="cuda")
+    want = ref.GroupNorm(x[some], G, w, b, "silu", EPS)
+    (wy, ey), (ws, es) = want.forward()
+    ref.check("y", y[some], wy, ey)
+    ref.check("stats", stats[some], ws, es)
+    ref.check("d_x", dx[some], *want.backward(g[some])[0])
+    # two channels' vectors: B items are up to B / 64 + 64 additions more
+    W = C // G
+    for c in (0, C - 1):
+        lo = c // W * W
+        cut = lambda t: t[..., lo:lo + W].contiguous()  # noqa: E731
+        one = ref.GroupNorm(cut(x), 1, cut(w), cut(b), "silu", EPS)
+        _, (v, e), (vb, eb) = one.backward(cut(g))
+        dz = cut(g).double().cpu().view(one.z.shape) * slope("silu", one.z)
+        more = (B / 64 + 64) * ref.EPS
+        for what, got, val, bound, terms in (("d_weight", dw, v, e, dz * one.hat), ("d_bias", db, vb, eb, dz)):
+            ref.check(what, got[lo:lo + W], val, bound + more * terms.abs().sum((0, 1)).reshape(-1))
+    assert torch.equal(m.corr_group_norm(x, G, weight=w, bias=b, act=m.CORR_ACT_SILU, eps=EPS, out=x), y)
