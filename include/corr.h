@@ -321,7 +321,7 @@ corr_status corr_residual_norm_backward(const corr_residual_norm_args* args, con
  *   stats        : NULL, or fp32 [B, G, 2]: mean and 1 / sqrt(var + eps), which the gradient reads.
  *   y            : [B * P, C] dense; may be x (if x_stride == C).
  * Limits: C <= 16384, B <= 65535, B * C <= 2^23, B * P <= 2^30, strides <= 2^21; beyond: CORR_ERR_UNSUPPORTED.  eps > 0.  Without pixels (P = 0) stats are zeros.
- * Squares about the mean are added in fp32: where their sum passes 3.4e38 the normalised group is zero.
+ * Squares about the mean are added in fp32: where their sum passes 3.4e38 the group's stats are zeros, and so is the normalised group.
  */
 size_t corr_group_norm_workspace_bytes(corr_dtype type, int64_t B, int64_t P, int64_t C, int64_t G);
 corr_status corr_group_norm(corr_dtype type, corr_activation act, const void* x, int64_t x_stride, const float* weight, const float* bias,

@@ -28,13 +28,19 @@ template <int V> int threads_across(int C) {
     return ct;
 }
 
+// Half the difference of two values, which no finite ones overflow.
+__device__ __forceinline__ float half_apart(float x, float y) { return 0.5f * x - 0.5f * y; }
 // n values with mean and sum of squares about it, and m more: Chan, Golub and LeVeque's rule, which cancels nothing however large the mean is
 __device__ __forceinline__ void merge(float n, float& mean, float& square, float m, float mean2, float square2) {
     if (m == 0.f) return;
-    const float d = mean2 - mean, f = m / (n + m);
-    mean = fmaf(d, f, mean);
-    square += square2 + d * (n * f) * d;
+    const float d = half_apart(mean2, mean), f = m / (n + m);
+    mean = fmaf(d, 2.f * f, mean);
+    square += square2 + d * (4.f * n * f) * d;
 }
+// A first mean, of values times their shares of one, is off by the roundings of sums as large as the values; the shares of what the values differ from it
+// put that right, and make a constant's mean that constant.  (Differences from one of the values instead would have the roundings of that one, however far
+// it lies from the others.)  Rounded past the largest value it would be infinite; NaN and infinities come back with the differences.
+__device__ __forceinline__ float finite(float mean) { return fminf(fmaxf(mean, -3.4028235e38f), 3.4028235e38f); }
 
 // U rows of a thread's V channels as they are stored, rt rows apart.
 template <class T, int V, int U> struct Chunk {
@@ -103,20 +109,28 @@ __global__ __launch_bounds__(THREADS) void stats_kernel(GroupNormArgs a, int ct)
         each_chunk<T, V, U, 1>({(const T*)a.x + at.c + (item + lo) * a.x_stride}, {a.x_stride}, rows, at.r0, at.rt, at.left, [&](auto& now, int, auto many) {
             if constexpr (!std::is_same<decltype(many), int>::value) {
                 const float f = (float)U / (n + U), nf = n * f;
-                float s[V] = {}, q[V] = {};
+                float s[V], q[V] = {};
+                // in pairs, which are exact for equal values
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+                for (int e = 0; e < V; ++e) {
+                    float two[U / 2];
 #pragma unroll
-                    for (int e = 0; e < V; ++e) s[e] = fmaf((float)now[0].x[u][e], 1.f / U, s[e]);
+                    for (int u = 0; u < U / 2; ++u) two[u] = fmaf((float)now[0].x[2 * u][e], 1.f / U, (float)now[0].x[2 * u + 1][e] * (1.f / U));
+#pragma unroll
+                    for (int step = 1; step < U / 2; step *= 2)
+#pragma unroll
+                        for (int u = 0; u + step < U / 2; u += 2 * step) two[u] += two[u + step];
+                    s[e] = two[0];
+                }
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
                     for (int e = 0; e < V; ++e) { const float d = (float)now[0].x[u][e] - s[e]; q[e] = fmaf(d, d, q[e]); }
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float d = s[e] - mean[e];
-                    mean[e] = fmaf(d, f, mean[e]);
-                    square[e] += fmaf(d * nf, d, q[e]);
+                    const float d = half_apart(s[e], mean[e]);
+                    mean[e] = fmaf(d, 2.f * f, mean[e]);
+                    square[e] += fmaf(d * (4.f * nf), d, q[e]);
                 }
                 n += U;
             } else {
@@ -170,10 +184,10 @@ template <int WAVES> __device__ __forceinline__ float sum_all(float x, float* ro
     return x;
 }
 
-// A group's parts: mean and 1 / spread.  One workgroup a group and item, or several after each other.  The parts' means are averaged first and the squares
-// taken about that.
+// A group's parts: mean and 1 / spread.  One workgroup a group and item, or several after each other.  The parts' means are averaged first, in two goes,
+// and the squares taken about that.
 constexpr int MOST_GROUPS = 1 << 20;                     // workgroups: a launch has fewer than 2^32 threads
-template <int WAVES>
+template <int WAVES, int HELD_PARTS>
 __global__ __launch_bounds__(64 * WAVES) void finish_stats_kernel(GroupNormArgs a) {
     __shared__ float room[WAVES];
     const int width = a.C / a.G, all = a.parts * width;
@@ -181,23 +195,41 @@ __global__ __launch_bounds__(64 * WAVES) void finish_stats_kernel(GroupNormArgs 
     for (int at = blockIdx.x; at < a.B * a.G; at += gridDim.x) {
         const int g = at % a.G, b = at / a.G;
         const float* const part = a.part + 2 * ((int64_t)b * a.parts * a.C + g * width);
-        float mean = 0.f, square = 0.f;
+        auto load = [&](int i, float& mean, float& square, float& rows) {
+            const int p = (unsigned)i / (unsigned)width;
+            const float* const q = part + 2 * ((int64_t)p * a.C + (i - p * width));
+            mean = q[0];
+            square = q[1];
+            rows = (float)min(a.share, a.P - p * a.share);
+        };
+        // a thread's first parts stay in its registers; any more are read in each go
+        float m[HELD_PARTS], q[HELD_PARTS], rows[HELD_PARTS];
+#pragma unroll
+        for (int j = 0; j < HELD_PARTS; ++j) {
+            const int i = threadIdx.x + j * 64 * WAVES;
+            m[j] = q[j] = rows[j] = 0.f;
+            if (i < all) load(i, m[j], q[j], rows[j]);
+        }
         auto each = [&](auto f) {
-#pragma unroll 4
-            for (int i = threadIdx.x; i < all; i += 64 * WAVES) {
-                const int p = (unsigned)i / (unsigned)width;
-                const float* const q = part + 2 * ((int64_t)p * a.C + (i - p * width));
-                f(q, (float)min(a.share, a.P - p * a.share));
+#pragma unroll
+            for (int j = 0; j < HELD_PARTS; ++j) if (rows[j] > 0.f) f(m[j], q[j], rows[j]);
+            for (int i = threadIdx.x + HELD_PARTS * 64 * WAVES; i < all; i += 64 * WAVES) {
+                float mean, square, rows;
+                load(i, mean, square, rows);
+                f(mean, square, rows);
             }
         };
-        const float some = part[0];                      // differences from it: a constant's mean is that constant, however large
-        each([&](const float* q, float m) { mean = fmaf(q[0] - some, m / n, mean); });
-        mean = some + sum_all<WAVES>(mean, room);
-        each([&](const float* q, float m) { const float d = q[0] - mean; square += fmaf(m * d, d, q[1]); });
+        float mean = 0.f, rest = 0.f, square = 0.f;
+        each([&](float x, float, float r) { mean = fmaf(x, r / n, mean); });
+        mean = finite(sum_all<WAVES>(mean, room));
+        each([&](float x, float, float r) { rest = fmaf(half_apart(x, mean), 2.f * (r / n), rest); });
+        mean += sum_all<WAVES>(rest, room);
+        each([&](float x, float y, float r) { const float d = x - mean; square += fmaf(r * d, d, y); });
         square = sum_all<WAVES>(square, room);
         if (threadIdx.x == 0) {
-            a.stats[2 * at] = mean;
-            a.stats[2 * at + 1] = 1.f / sqrtf(square / n + a.eps);
+            const float rho = 1.f / sqrtf(square / n + a.eps);
+            a.stats[2 * at] = rho == 0.f ? 0.f : mean;   // squares past the largest value: a difference from the mean may be as well
+            a.stats[2 * at + 1] = rho;
         }
     }
 }
@@ -405,20 +437,26 @@ __global__ __launch_bounds__(HELD_THREADS) void held_kernel(GroupNormArgs a, int
         w[e] = a.weight && e < at.left ? a.weight[at.c + e] : 1.f;
         bias[e] = a.bias && e < at.left ? a.bias[at.c + e] : 0.f;
     }
-    const float some = (float)((const T*)a.x)[b * a.P * a.x_stride + blockIdx.x % a.G * (a.C / a.G)];     // as above
-    float mean = 0.f, square = 0.f;
+    float mean = 0.f, rest = 0.f, square = 0.f;
 #pragma unroll
     for (int j = 0; j < PIECES; ++j)
         if (at.pixel + j * at.step < a.P)
 #pragma unroll
-            for (int e = 0; e < V; ++e) if (e < at.left) mean = fmaf((float)k.x[j][e] - some, by, mean);
-    mean = some + sum_all<HELD_THREADS / 64>(mean, room);
+            for (int e = 0; e < V; ++e) if (e < at.left) mean = fmaf((float)k.x[j][e], by, mean);
+    mean = finite(sum_all<HELD_THREADS / 64>(mean, room));
+#pragma unroll
+    for (int j = 0; j < PIECES; ++j)
+        if (at.pixel + j * at.step < a.P)
+#pragma unroll
+            for (int e = 0; e < V; ++e) if (e < at.left) rest = fmaf(half_apart((float)k.x[j][e], mean), 2.f * by, rest);
+    mean += sum_all<HELD_THREADS / 64>(rest, room);
 #pragma unroll
     for (int j = 0; j < PIECES; ++j)
         if (at.pixel + j * at.step < a.P)
 #pragma unroll
             for (int e = 0; e < V; ++e) if (e < at.left) { const float d = (float)k.x[j][e] - mean; square = fmaf(d, d, square); }
     const float rho = 1.f / sqrtf(sum_all<HELD_THREADS / 64>(square, room) * by + a.eps);
+    if (rho == 0.f) mean = 0.f;                          // as above
     if (a.stats && threadIdx.x == 0) { a.stats[2 * blockIdx.x] = mean; a.stats[2 * blockIdx.x + 1] = rho; }
     T* const y = (T*)a.y + (b * a.P + at.pixel) * a.C + at.c;
 #pragma unroll
@@ -528,8 +566,10 @@ hipError_t forward(const GroupNormArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((stats_kernel<T, V>), grid, dim3(THREADS), 0, s, a, ct);
     const dim3 groups((unsigned)std::min(a.B * a.G, MOST_GROUPS));
     // few parts: one wave (64 x 64 x 512 in 512 groups bf16, the whole call: 146 -> 26 us)
-    if (a.parts * (a.C / a.G) <= 64) hipLaunchKernelGGL(finish_stats_kernel<1>, groups, dim3(64), 0, s, a);
-    else hipLaunchKernelGGL(finish_stats_kernel<JOIN_THREADS / 64>, groups, dim3(JOIN_THREADS), 0, s, a);
+    const int all = a.parts * (a.C / a.G);
+    if (all <= 64) hipLaunchKernelGGL((finish_stats_kernel<1, 1>), groups, dim3(64), 0, s, a);
+    else if (all <= JOIN_THREADS) hipLaunchKernelGGL((finish_stats_kernel<JOIN_THREADS / 64, 1>), groups, dim3(JOIN_THREADS), 0, s, a);
+    else hipLaunchKernelGGL((finish_stats_kernel<JOIN_THREADS / 64, 8>), groups, dim3(JOIN_THREADS), 0, s, a);
     const hipError_t e = hipGetLastError();              // without statistics there is no result
     if (e != hipSuccess) return e;
     with_act(a.act, [&](auto act) { hipLaunchKernelGGL((apply_kernel<T, V, decltype(act)::value>), grid, dim3(THREADS), 0, s, a, ct); });

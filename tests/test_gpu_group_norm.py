@@ -241,3 +241,61 @@ def test_millions_of_groups(size, dtype):
         for what, got, val, bound, terms in (("d_weight", dw, v, e, dz * one.hat), ("d_bias", db, vb, eb, dz)):
             ref.check(what, got[lo:lo + W], val, bound + more * terms.abs().sum((0, 1)).reshape(-1))
     assert torch.equal(m.corr_group_norm(x, G, weight=w, bias=b, act=m.CORR_ACT_SILU, eps=EPS, out=x), y)
+
+
+#: (B, P, C, G): a group in a workgroup's registers; sums by parts, of one group and of several; groups of three channels
+MEANS = [(1, 8192, 4, 1), (2, 2048, 64, 8), (1, 50000, 8, 1), (2, 40000, 24, 8), (3, 9000, 96, 32)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("size", MEANS)
+def test_a_value_far_from_the_others(size, dtype):
+    """One value of 1e6 (6e4 in fp16) among ones of about one, first, last or anywhere: the mean is off by its sums' roundings, OPS of them relative to the mean of
+    the magnitudes (a running mean's rounding counts as many values as it stands for), wherever the one lies."""
+    m, (B, P, C, G) = _b(), size
+    x = _gen(P + C)(B, P, C)
+    ops = 3 * (33 + P * (C // G) / 2048) + 8
+    for pixel, channel in ((0, 0), (P - 1, C - 1), (P // 3, C // 2)):
+        x2 = x.clone()
+        x2[:, pixel, channel] = 6e4 if dtype == F16 else 1e6
+        x2 = x2.to(dtype)
+        stats = torch.empty(B, G, 2, device="cuda")
+        y = m.corr_group_norm(x2, G, eps=EPS, stats=stats)
+        d = x2.double().cpu().view(B, P, G, C // G)
+        mean, size = d.mean((1, 3), keepdim=True), d.abs().mean((1, 3), keepdim=True)
+        rho = 1 / torch.sqrt(((d - mean) ** 2).mean((1, 3), keepdim=True) + EPS)
+        e_mean = ops * ref.EPS * size + ref.EPS * mean.abs()
+        ref.check("mean", stats[..., 0], mean.view(B, G), e_mean.view(B, G))
+        want = (d - mean) * rho
+        e = rho * e_mean + want.abs() * ops * ref.EPS + 4 * ref.EPS * rho * (d.abs() + mean.abs())
+        ref.check("y", y, want.view(B, P, C), (1.01 * e + ref.rounded(want, dtype)).view(B, P, C))
+
+
+@pytest.mark.parametrize("P", [500, 50000])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_largest_values_of_either_sign(P, dtype):
+    """Squares and differences that overflow: the normalised group is zero, with zero gradients."""
+    m = _b()
+    sign = (torch.rand(2, P, 16, generator=torch.Generator().manual_seed(P)) < 0.5).float().mul(2).sub(1)
+    b = _gen(3)(16)
+    for value in (2e38, 3.38e38):
+        x = (sign * value).to(dtype).cuda()
+        y, stats, (dx, dw, db) = _run(x, 2, None, b, torch.ones_like(x), m.CORR_ACT_NONE)
+        assert torch.equal(y, b.to(dtype).expand_as(y)) and not stats.any()
+        assert not dx.any() and not dw.any() and (db == 2 * P).all()
+
+
+@pytest.mark.parametrize("P", [500, 50000])
+def test_constants(P):
+    """A group of one value has that value for its mean, whatever it is, and is zero when it is normalised."""
+    m = _b()
+    values = torch.rand(64, generator=torch.Generator().manual_seed(1)) + 1
+    for scale in (1.0, 2.0 ** 20, 2.0 ** 127):
+        x = (values * scale).clamp(max=3.4028234e38).cuda().view(1, 1, 64).repeat(1, P, 1)
+        stats = torch.empty(1, 64, 2, device="cuda")
+        y = m.corr_group_norm(x, 64, stats=stats)
+        assert torch.equal(stats[0, :, 0], x[0, 0]) and not y.any()
+        x = x.repeat_interleave(8, 2)
+        stats = torch.empty(1, 64, 2, device="cuda")
+        y = m.corr_group_norm(x, 64, stats=stats)
+        assert torch.equal(stats[0, :, 0], x[0, 0, ::8]) and not y.any()
