@@ -274,8 +274,8 @@ __device__ __forceinline__ V keep_first(V v, int left) {
 
 // TWO: the first operand is in two parts (rows_internal.h), multiplied one after the other, the low one first: twice the matrix work and twice the
 // loads (fp16, and bf16 gradients of few gated elements; fp16 gradients with silu, and with relu: 14570 x 243 -> 126: 51 and 41 us; 32400 x 256 -> 1024: 153 and 104; 4096^3: 503 and
-// 265).  A sum of the low part's products that is not finite says that an element of the second operand is not (fp16's values
-// cannot overflow it): then the high part alone gives what the whole would.
+// 265).  A sum of the low part's products that is not finite says that an element of the second operand is not, or (bf16; fp16's values
+// cannot overflow it) that the high part's sum is not either: then the high part alone gives what the whole would.
 // GATED: the second operand's rows come in turns from its two halves of g.N (BN / 2 columns of y a tile), so that a lane's sums have both factors of
 // the same columns and the sums need no memory: 14400 x 320 -> 2 x 1280 bf16 with silu and preact 51 us (120 MB), 14570 x 256 -> 2 x 682 fp32
 // with gelu 65 us (157 TFLOP/s), bound as the products without a gate.
@@ -361,7 +361,7 @@ __global__ __launch_bounds__(64 * WM * WN, BK == 32 ? 4 : 2) void product16_kern
     };
     if constexpr (TWO) {
         pass();
-        scale(1.f / LOW_PART);
+        scale(1.f / LOW_PART<T>);
         wa = window<AR, 2, BK>(g.a, g.lda, g.M, g.K, m0, k0);
         wb = window<BR, 2, BK>(g.b, g.ldb, g.N, g.K, n0, k0);
         arrive_all();                                    // the tiles have been read
@@ -371,7 +371,7 @@ __global__ __launch_bounds__(64 * WM * WN, BK == 32 ? 4 : 2) void product16_kern
 #pragma unroll
         for (int i = 0; i < FN; ++i)
 #pragma unroll
-            for (int j = 0; j < FM; ++j) acc[i][j] *= 1.f / HIGH_PART;
+            for (int j = 0; j < FM; ++j) acc[i][j] *= 1.f / HIGH_PART<T>;
     }
     __syncthreads();                                     // the tiles have been read
     if constexpr (GATED) {
@@ -982,8 +982,8 @@ __global__ __launch_bounds__(SLOPE_THREADS) void slope_kernel(int act, const T* 
                     float lo[V];
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
-                        const float x = HIGH_PART * v[u][e], d = x - (float)(T)x;
-                        lo[e] = d == d ? LOW_PART * d : 0.f;         // an infinity or NaN is in the high part
+                        const float x = HIGH_PART<T> * v[u][e], d = x - (float)(T)x;
+                        lo[e] = d == d ? LOW_PART<T> * d : 0.f;         // an infinity or NaN is in the high part
                         v[u][e] = x;
                     }
                     store_some<T, V>(dz_lo + (m + u * rt) * ld_dz + n, lo, left);
@@ -1041,8 +1041,8 @@ __global__ __launch_bounds__(SLOPE_THREADS) void slope_gated_kernel(int act, con
                     float lo_part[V];
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
-                        const float x = HIGH_PART * d[h][e], r = x - (float)(T)x;
-                        lo_part[e] = fabsf(r) < INFINITY ? LOW_PART * r : 0.f;       // an infinity or NaN is in the high part
+                        const float x = HIGH_PART<T> * d[h][e], r = x - (float)(T)x;
+                        lo_part[e] = fabsf(r) < INFINITY ? LOW_PART<T> * r : 0.f;       // an infinity or NaN is in the high part
                         d[h][e] = x;
                     }
                     store_some<T, V>(dz_lo + to, lo_part, left);

@@ -2,16 +2,20 @@
 #pragma once
 #include "rows.h"
 
-// A first operand in two fp16 parts (`a_lo` is there): HIGH_PART x = a + a_lo / LOW_PART, so that fp16 holds x, an fp32 value, to 22 bits: no |x| up
-// to 1.13 times fp16's largest overflows, and what is below its normal values keeps its digits in the low part.
-constexpr float HIGH_PART = 0.5f, LOW_PART = 2048.f;
+// A first operand in two parts (`a_lo` is there): HIGH_PART x = a + a_lo / LOW_PART.  fp16 so holds x, an fp32 value, to 22 bits: no |x| up
+// to 1.13 times its largest overflows, and what is below its normal values keeps its digits in the low part.  bf16, which has fp32's range, holds
+// 16 bits, and no low part or sum of them is infinite where the high ones are not.
+template <class T> constexpr float HIGH_PART = 1.f;
+template <class T> constexpr float LOW_PART = 1.f;
+template <> inline constexpr float HIGH_PART<_Float16> = 0.5f;
+template <> inline constexpr float LOW_PART<_Float16> = 2048.f;
 
 // C[m][n] = sum over k < K of A(m, k) B(n, k).  An operand is stored with its k contiguous ([m][k], `lda` elements from row to
 // row) or with its rows contiguous ([k][m]); which of the two is part of the kernel chosen.
 struct ProductArgs {
     corr_dtype type;
     const void* a; const void* b;
-    const void* a_lo;          // laid out as a; null but for fp16 whose second operand has its rows contiguous
+    const void* a_lo;          // laid out as a; null but for 16-bit types whose second operand has its rows contiguous
     int64_t lda, ldb;
     int a_rows, b_rows;        // 1: rows contiguous ([k][m] / [k][n])
     int M, N, K;

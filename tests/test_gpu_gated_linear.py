@@ -219,6 +219,20 @@ def test_factors_near_the_largest(dtype):
         ref.check(what, g, v, e)
 
 
+@pytest.mark.parametrize("name", ["none", "relu", "silu"])
+def test_two_parts_of_the_largest_gradients(name):
+    """bf16 dz in two parts up to 3.3e38: the second part is there also where 2048 times it has no place in the type."""
+    m, new = _b(), _gen(12)
+    M, N, K = 40, 24, 32
+    x, w = new(M, K, sigma=1e-3, dtype=BF16), new(2 * N, K, sigma=1e-3, dtype=BF16)
+    z = (torch.rand(M, 2 * N, generator=torch.Generator().manual_seed(4)) / 2 + 0.5).to(BF16).cuda()
+    for most in (1e36, 1e38, 3.3e38):
+        dy = ((torch.rand(M, N, generator=torch.Generator().manual_seed(3)) * 2 - 1) * most).to(BF16).cuda()
+        got = m.corr_gated_linear_backward(x, w, dy, z, act=_act(name), want_bias=False)
+        for g, (v, e), what in zip(got, ref.gated_backward(x, w, dy, z, name), ("d_x", "d_w")):
+            ref.check("%s %g" % (what, most), g, v, e)
+
+
 def test_differences():
     """The gradient against differences of the forward call in fp32: what the quotient itself is off by is computed in float64."""
     m, new = _b(), _gen(6)
