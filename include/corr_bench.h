@@ -120,6 +120,8 @@ corr_status corr_debug_read_level(const corr_pyramid* pyr, unsigned rep, int lev
 #define CORR_PRODUCT_DX 1
 #define CORR_PRODUCT_DW 2
 corr_status corr_debug_linear_tile(corr_dtype type, int product, int64_t M, int64_t N, int64_t K, int* tile_rows, int* tile_cols, int* splits);
+/* The same of corr_gated_linear's M x 2 N sums; 128 x 64: many rows with a short k, which stay in registers. */
+corr_status corr_debug_gated_tile(corr_dtype type, int64_t M, int64_t N, int64_t K, int* tile_rows, int* tile_cols, int* splits);
 
 #ifdef __cplusplus
 }

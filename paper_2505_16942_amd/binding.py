@@ -45,7 +45,7 @@ EXPORTS = [
 BENCH_EXPORTS = [
     "corr_last_block_stats", "corr_profile_enable", "corr_profile_read", "corr_bin_geometry", "corr_copy_f32",
     "corr_debug_read_plan", "corr_debug_cell_coords", "corr_debug_read_level", "corr_debug_item_map",
-    "corr_debug_linear_tile",
+    "corr_debug_linear_tile", "corr_debug_gated_tile",
     "corr_debug_set_level_split",
     "corr_debug_set_backward_form",
 ]
@@ -181,6 +181,8 @@ def load_library():
     lib.corr_debug_item_map.restype = ci
     lib.corr_debug_linear_tile.argtypes = [ci, ci, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64] + [ctypes.POINTER(ci)] * 3
     lib.corr_debug_linear_tile.restype = ci
+    lib.corr_debug_gated_tile.argtypes = [ci, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64] + [ctypes.POINTER(ci)] * 3
+    lib.corr_debug_gated_tile.restype = ci
     lib.corr_debug_set_level_split.argtypes = [ci]
     lib.corr_debug_set_level_split.restype = ci
     lib.corr_debug_set_backward_form.argtypes = [ci]
@@ -1043,6 +1045,15 @@ def corr_debug_linear_tile(dtype: torch.dtype, product: int, M: int, N: int, K: 
     st = load_library().corr_debug_linear_tile(_TYPES[dtype], product, M, N, K, *[ctypes.byref(v) for v in vals])
     if st != CORR_OK:
         raise CorrError(st, "corr_debug_linear_tile")
+    return tuple(v.value for v in vals)
+
+
+def corr_debug_gated_tile(dtype: torch.dtype, M: int, N: int, K: int):
+    """(rows, columns, splits) of the tiles in which corr_gated_linear makes its M x 2 N sums; (128, 64, 1): rows with a short k."""
+    vals = [ctypes.c_int() for _ in range(3)]
+    st = load_library().corr_debug_gated_tile(_TYPES[dtype], M, N, K, *[ctypes.byref(v) for v in vals])
+    if st != CORR_OK:
+        raise CorrError(st, "corr_debug_gated_tile")
     return tuple(v.value for v in vals)
 
 

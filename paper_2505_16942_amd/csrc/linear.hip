@@ -1192,9 +1192,12 @@ void product_tile(const ProductPlan& p, int& rows, int& cols) {
 namespace {
 constexpr int SHORT_FM = 2, SHORT_WAVES = 4, SHORT_ROWS = 16 * SHORT_FM * SHORT_WAVES, SHORT_SLOTS = 512;      // two workgroups a compute unit
 // Whole pieces of k, and seven chunks for every workgroup that fits at a time (bf16 with silu and preact, tiles and here: 14570 x 256 -> 2 x 1024 38 and 34 us, 57600 x
-// 128 -> 2 x 256 32 and 27; below: 14570 x 256 -> 2 x 384 18 and 22, 8192 x 256 -> 2 x 1024 20 and 22).
+// 128 -> 2 x 256 32 and 27; below: 14570 x 256 -> 2 x 384 18 and 22, 8192 x 256 -> 2 x 1024 20 and 22).  An XCD takes every eighth 128 rows, so the rows have to be 16 times that many and
+// leave no more than one place idle beside 15 taken ones (k = 256, the same product of rows and columns, here and tiles: 1 x 114688 162 and 29, 1000 x 14336 30 and 26,
+// 2048 x 7168 26 and 26, 2500 x 5760 36 and 26, 4096 x 3584 24 and 26, 9300 x 1600 27 and 26, 10000 x 1472 24 and 26).
 bool short_rows(const ProductArgs& g) {
-    return g.gated && g.type != CORR_TYPE_F32 && g.K <= 256 && g.K % 8 == 0 && (int64_t)cdiv(g.M, SHORT_ROWS) * cdiv(g.N, 32) >= 7 * SHORT_SLOTS;
+    const int64_t tm = cdiv(g.M, SHORT_ROWS);
+    return g.gated && g.type != CORR_TYPE_F32 && g.K <= 256 && g.K % 8 == 0 && tm * cdiv(g.N, 32) >= 7 * SHORT_SLOTS && tm >= 16 && 8 * cdiv(tm, 8) * 15 <= 16 * tm;
 }
 template <class T>
 void short_gated(const ProductArgs& g, hipStream_t s) {
@@ -1212,6 +1215,15 @@ void short_gated(const ProductArgs& g, hipStream_t s) {
     else hipLaunchKernelGGL((short_gated_kernel<T, SHORT_FM, SHORT_WAVES, 8>), grid, threads, 0, s, g, tm, parts, per);
 }
 }  // namespace
+
+void gated_tile(corr_dtype type, int M, int N, int K, int& rows, int& cols, int& splits) {
+    ProductArgs g = {};
+    g.type = type; g.gated = 1; g.M = M; g.N = N; g.K = K;
+    const ProductPlan p = product_plan(type, 0, 0, M, 2 * N, K);
+    product_tile(p, rows, cols);
+    splits = p.splits;
+    if (short_rows(g)) { rows = SHORT_ROWS; cols = 64; splits = 1; }
+}
 
 hipError_t launch_product(const ProductArgs& args, hipStream_t s) {
     ProductArgs g = args;

@@ -316,6 +316,12 @@ corr_status corr_debug_linear_tile(corr_dtype type, int product, int64_t M, int6
     return CORR_OK;
 }
 
+corr_status corr_debug_gated_tile(corr_dtype type, int64_t M, int64_t N, int64_t K, int* tile_rows, int* tile_cols, int* splits) {
+    if (!tile_rows || !tile_cols || !splits || M <= 0 || check_gated(type, CORR_ACT_NONE, M, N, K) != CORR_OK) return CORR_ERR_INVALID_ARG;
+    gated_tile(type, (int)M, (int)N, (int)K, *tile_rows, *tile_cols, *splits);
+    return CORR_OK;
+}
+
 corr_status corr_residual_norm(const corr_residual_norm_args* a, void* h_out, void* n_out, void* stream) {
     corr_status st = check_norm(a);
     if (st != CORR_OK) return st;

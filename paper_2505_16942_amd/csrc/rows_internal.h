@@ -32,6 +32,7 @@ struct ProductArgs {
 struct ProductPlan { int tile, splits, steps; };   // steps of the k loop per split
 ProductPlan product_plan(corr_dtype type, int a_rows, int b_rows, int M, int N, int K);
 void product_tile(const ProductPlan& p, int& rows, int& cols);   // no rows: few rows, without tiles
+void gated_tile(corr_dtype type, int M, int N, int K, int& rows, int& cols, int& splits);      // of both halves' columns; 128 x 64: rows with a short k
 static inline size_t product_part_bytes(const ProductPlan& p, int M, int N) {
     return p.splits > 1 ? (size_t)p.splits * M * N * 4 : 0;
 }

@@ -194,3 +194,21 @@ def test_gated_tiles():
                 want = (128, 128)
             assert (rows, cols) == want, (dtype, kind, rows, cols)
             assert ("split" in kind) == (splits > 1), (dtype, kind, splits)
+
+
+def test_gated_tiles_of_a_short_k():
+    """The sizes that are there for rows in registers go there; few rows or ones that leave XCDs idle, other lengths and fp32 go to the products' tiles."""
+    b = _b()
+    import test_gpu_gated_linear as t
+    short = (128, 64, 1)
+    for dtype in (torch.bfloat16, torch.float16):
+        for size in t.SHORT + [(60000, 256, 120), (32400, 1024, 256), (129600, 512, 256)]:
+            assert b.corr_debug_gated_tile(dtype, *size) == short, size
+        for M, N, K in [(1, 114688, 256), (16, 1 << 20, 64), (33, 114688, 256), (128, 500000, 128), (1000, 14336, 256), (2500, 5760, 256), (9300, 1600, 256),
+                        (32400, 1024, 264), (32400, 1024, 252)] + list(t.TILES.values()):
+            tile = b.corr_debug_gated_tile(dtype, M, N, K)
+            assert tile != short and tile == b.corr_debug_linear_tile(dtype, 0, M, 2 * N, K), (M, N, K)
+    assert b.corr_debug_gated_tile(torch.float32, 32400, 1024, 256) == (128, 128, 1)
+    for bad in ((torch.bfloat16, 0, 8, 8), (torch.bfloat16, 8, 0, 8), (torch.bfloat16, 8, 8, 0), (torch.bfloat16, 8, (1 << 20) + 1, 8)):
+        with pytest.raises(b.CorrError):
+            b.corr_debug_gated_tile(*bad)
