@@ -351,8 +351,9 @@ corr_status corr_group_norm_backward(corr_dtype type, corr_activation act, const
  *   out        : [B, Lq, H, D] dense.  A row of which no key counts, or whose every score is -infinity, is zeros.
  *   lse        : NULL, or fp32 [B, H, Lq]: the logarithm of the sum of e^score, which the gradient reads (-infinity for rows of zeros).
  * Scores are fp32 and may lie as far from zero as fp32 reaches (scale times a score below 2^127); their weights are those of their differences.
- * Weights meet v as `type` values: rounded once each, up to B Lq H = 512 in two parts (fp16: 2^14 times as large, so that weights down
- * to 4e-9 of a row's largest keep their digits); their sum is not.
+ * Weights meet v as `type` values, rounded once each, which adds as much error as the result's own rounding; or in two parts, which adds none to speak of, where a call
+ * is small and the second part costs nothing: up to B Lq H = 512, and up to Lq H / HK = 16 whatever B is.  So a row may come out a rounding apart beside fewer or more
+ * others.  fp16: 2^14 times as large, so that weights down to 4e-9 of a row's largest keep their digits.  Their sum is not rounded.
  * Limits: D a multiple of 8 up to 256, H <= 128, strides of rows and heads <= 2^21 and of items <= 2^40, B * HK <= 2^20, Lq * H / HK and Lk <= 2^30, B * Lq * H * D and
  * B * Lk * HK * D <= 2^36, and no more work than one launch takes (2^24 workgroups of 64 rows or keys of a key head); beyond: CORR_ERR_UNSUPPORTED.  scale is
  * positive and finite.  fp32 products carry fp32's precision as corr_linear's; an infinity in an fp32 operand that counts may come out as NaN.

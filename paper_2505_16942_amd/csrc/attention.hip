@@ -1187,10 +1187,10 @@ AttentionPlan attention_plan(corr_dtype t, AttentionPass pass, int B, int Lq, in
     AttentionPlan p;
     p.waves = pass == PASS_FORWARD && along <= 16 && one_fits(f32, pad) ? 1 : 4;
     p.blocks = 1;
-    // One rounding of weights and dS is as large as the result's own, together sqrt 2 of it, where many weights share in it. Up to some hundred rows a few large ones
-    // can make up most of it and their roundings be the largest there are (scores of a spread of two, in a hundredth of all calls: 1.8 times the result's at one row, 1.6 at
-    // 64, 1.5 at 256), and few keys' gradients have few elements to share them. The second part costs 3 % of a call of one row (8 x 32768 keys: 74 and 77 us) and 12 % of a
-    // gradient at 700 rows of 4 heads (56 and 63 us, 2852 keys).
+    // Rounded once, weights and dS add as much error as the result's own rounding does; a second part takes that away at half the products again.  It is there where
+    // launches and loads are what takes the time (bf16, 4 heads of 64, keys 2852; forward, rows' and keys' gradient in one part and in two, us: 512 rows and heads 14.9
+    // 20.7 20.6 and 15.2 21.1 20.6; 2800: 18.9 21.9 25.8 and 20.0 21.6 29.2; 11408: 27.5 33.8 43 and 32.3 39.7 54; 28800, 7200 keys: 88 117 150 and 125 159 240; 8 x
+    // 32768 keys, one row: 74 and 77), and for the gradients of few keys, of which the same holds.
     p.two = !f32 && (p.waves == 1 || heads * rows <= 512 || (pass == PASS_DKV && heads * Lk <= 64));
     // Planes are made once a call and read by every tile of rows: from 2048 rows on (2852 x 2852 x 4 x 32: 51 us, 53 without; 7200 x 7200 x 2 x 32: 102 and
     // 117; 256 x 20000 x 2 x 128: 71 and 51).
