@@ -356,7 +356,7 @@ corr_status corr_group_norm_backward(corr_dtype type, corr_activation act, const
  * others.  fp16: 2^14 times as large, so that weights down to 4e-9 of a row's largest keep their digits.  Their sum is not rounded.
  * Limits: D a multiple of 8 up to 256, H <= 128, strides of rows and heads <= 2^21 and of items <= 2^40, B * HK <= 2^20, Lq * H / HK and Lk <= 2^30, B * Lq * H * D and
  * B * Lk * HK * D <= 2^36, and no more work than one launch takes (2^24 workgroups of 64 rows or keys of a key head); beyond: CORR_ERR_UNSUPPORTED.  scale is
- * positive and finite.  fp32 products carry fp32's precision as corr_linear's; an infinity in an fp32 operand that counts may come out as NaN.
+ * positive and at most 2^127.  fp32 products carry fp32's precision as corr_linear's; an infinity in an fp32 operand that counts may come out as NaN.
  */
 typedef struct {
     corr_dtype type;

@@ -1,5 +1,4 @@
 // Host side of the operators on maps declared in include/corr.h: argument checks, the workspace's layout and the order of kernels.
-#include <math.h>
 #include "attention.h"
 #include "checks.h"
 #include "group_norm.h"
@@ -36,7 +35,7 @@ corr_status check_attention(const corr_attention_args* a) {
     corr_status st = check_sizes(a->type, a->B, a->Lq, a->Lk, a->H, a->HK, a->D);
     for (const Strided& x : {q_of(a), k_of(a), v_of(a)}) if (st == CORR_OK) st = check_strided(a, x);
     if (st != CORR_OK) return st;
-    if (!(a->scale > 0.f) || isinf(a->scale) || !on(a->k_lengths, 4)) return CORR_ERR_INVALID_ARG;
+    if (!(a->scale > 0.f && a->scale <= 0x1p127f) || !on(a->k_lengths, 4)) return CORR_ERR_INVALID_ARG;      // scale log2 e is finite
     return CORR_OK;
 }
 AttentionArgs kernel_args(const corr_attention_args* a) {

@@ -212,3 +212,11 @@ def test_gated_tiles_of_a_short_k():
     for bad in ((torch.bfloat16, 0, 8, 8), (torch.bfloat16, 8, 0, 8), (torch.bfloat16, 8, 8, 0), (torch.bfloat16, 8, (1 << 20) + 1, 8)):
         with pytest.raises(b.CorrError):
             b.corr_debug_gated_tile(*bad)
+
+
+def test_attention_scales():
+    """scale log2 e has to be finite; without keys and rows the checks alone answer."""
+    b = _b()
+    for scale, status in ((2.0 ** 127, 0), (2.0 ** -149, 0), (1.8e38, -1), (3.4e38, -1), (-2.0 ** -149, -1)):
+        assert _forward(b, B=0, q=None, k=None, v=None, out=None, ws=None, scale=scale) == status
+        assert _backward(b, B=0, out=None, lse=None, d_out=None, ws=None, scale=scale) == status
