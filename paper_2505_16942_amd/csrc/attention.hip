@@ -356,11 +356,11 @@ __device__ __forceinline__ void query_of(const AttentionArgs& a, int r, int& q, 
 // Four waves of 16 QB rows share tiles of keys and values that land in LDS while the last ones are multiplied.  With two blocks a wave a fragment that
 // is read once is multiplied twice.  1 x 32400 x 32400, 2 heads of 128, bf16: 1090 us, 985 TFLOP/s, matrix instructions in 40 % of the cycles, the vector unit (an
 // exponential, fma, maximum, sum and half a rounding an element) in most others: a wave's two kinds of work alternate, and a compute unit holds
-// eight waves.  2 x 14400 x 14400, 2 heads of 64: 287 us, 740 TFLOP/s: the vector unit, about 80 % of the cycles with
+// eight waves.  2 x 14400 x 14400, 2 heads of 64: 282 us, 750 TFLOP/s: the vector unit, about 80 % of the cycles with
 // the exponentials' turns.  fp32's six products: 2 x 2852 x 7285, 4 heads of
-// 64: 243 us, 175 TFLOP/s (1.05 PFLOP/s of bf16).
-// One row of 8 query heads on 2 key heads, 8 x 32768 keys of ragged lengths (157 MB), bf16, one wave a workgroup, 74 shares: 40 us from memory, 3.9 TB/s
-// (28 from the memory-side cache), 38 with weights in one part, and 8 for their join; 110 or 172 shares make no difference.
+// 64: 232 us, 183 TFLOP/s (1.1 PFLOP/s of bf16).
+// One row of 8 query heads on 2 key heads, 8 x 32768 keys of ragged lengths (157 MB), bf16, one wave a workgroup, 74 shares: 38 us from memory, 4.1 TB/s
+// (28 from the memory-side cache), and 8 for their join; 110 or 172 shares make no difference.
 template <class T, int DP, int WAVES, int QB, bool TWO = false>
 __global__ __launch_bounds__(64 * WAVES, WAVES == 1 || (DP == 256 && F32<T>) ? 1 : 2) void forward_kernel(AttentionArgs a, int tiles, int splits, int share) {
     typedef Num<T> N;
@@ -602,8 +602,8 @@ __global__ __launch_bounds__(THREADS) void forward_join_kernel(AttentionArgs a, 
 
 // ---- gradient.  With P = exp(s - lse) and delta = sum over d of d_out out: dV = P^T dO, dS = P (dO V^T - delta), dQ = scale dS K,
 // dK = scale dS^T Q.  Rows' sums meet in one workgroup and keys' sums in another, so scores are computed twice (seven products for five) and nothing
-// is added by atomics: the same bits on every call.  2 x 14400 x 14400, 2 heads of 64, bf16: rows 375 us, keys 515 (seven products: 830 TFLOP/s), matrix
-// instructions in a third of the cycles, the vector unit in six tenths; in fp16 470 and 650, with the powers of two of dS.
+// is added by atomics: the same bits on every call.  2 x 14400 x 14400, 2 heads of 64, bf16: rows 378 us, keys 522 (seven products: 830 TFLOP/s), matrix
+// instructions in a third of the cycles, the vector unit in six tenths; in fp16 460 and 618, with the powers of two of dS.
 // delta, and lse in powers of two (less LIFT: the weights are 2^LIFT times as large), in the order of rows; rows behind the last have a weight of zero.  A far
 // row has 2 lse there, which is larger than any of the others.
 template <class T>
